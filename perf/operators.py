@@ -7,9 +7,9 @@ Kinds:
   fork     one turn of a search: rows released, others forked into them, room made for the next token
   compact  live pages moved to the low end of the pool, the page table rewritten
 
-A cache is four tensors: k [layers, pages, kv_heads, page, D] and v [layers, pages, kv_heads, D, page] in e4m3,
-scale fp32 [layers, pages, kv_heads, 2] (K's, V's) and kmean bf16 [layers, pages, kv_heads, D], the mean of the keys
-of each complete page.  table int32 [seqs, max_pages] names the pages of each sequence in order (-1: none), lens
+A cache is four tensors: k and v [layers, pages, kv_heads, page * D] in e4m3, scale fp32 [layers, pages, kv_heads, 2]
+(K's, V's) and kmean bf16 [layers, pages, kv_heads, D], the mean of the keys of each complete page.  The codes of a
+page lie in the order of the matrix instructions' operands, 16 tokens after 16 tokens (_k_order, _v_order).  table int32 [seqs, max_pages] names the pages of each sequence in order (-1: none), lens
 int32 [seqs] the tokens it holds with this call's, cu int32 [seqs + 1] where its new tokens lie in the packed arrays.
 
 Sequences of a ragged case hold 50 to 100 % of `length`, bring 25 to 100 % of `new`, and every fifth one is idle.
@@ -122,24 +122,50 @@ def _pow2(e):
     return ((e.to(torch.int32).clamp(min=-126) + 127) << 23).view(torch.float32)
 
 
+def _k_order(x):
+    """[..., page, D] as a page keeps it: [16 tokens][64 channels][16 of them][token][channel]."""
+    x = x.unflatten(-2, (-1, 16)).unflatten(-1, (-1, 4, 16))
+    return x.movedim(-4, -2).flatten(-5)
+
+
+def _k_rows(x, d):
+    x = x.unflatten(-1, (-1, d // 64, 4, 16, 16)).movedim(-2, -4)
+    return x.flatten(-3).flatten(-3, -2)
+
+
+def _v_order(x):
+    """[..., page, D] as a page keeps it: [16 tokens][64 channels][4 of the tokens][16 channels][4 such][token]."""
+    x = x.unflatten(-2, (-1, 4, 4)).unflatten(-1, (-1, 4, 16))
+    n = x.dim()
+    return x.permute(*range(n - 5), n - 3, n - 5, n - 1, n - 2, n - 4).flatten(-6)
+
+
+def _v_rows(x, d):
+    x = x.unflatten(-1, (-1, d // 64, 4, 16, 4, 4))
+    n = x.dim()
+    return x.permute(*range(n - 5), n - 4, n - 1, n - 5, n - 2, n - 3).flatten(-3).flatten(-4, -2)
+
+
 def _make_pool(c, pages, g):
     dev = "cuda"
     shape = (c["layers"], pages, c["kv_heads"])
-    pool = {"k": torch.empty(shape + (c["page"], c["d"]), dtype=_E4M3, device=dev),
-            "v": torch.empty(shape + (c["d"], c["page"]), dtype=_E4M3, device=dev),
+    rows = (pages, c["kv_heads"], c["page"], c["d"])
+    pool = {"k": torch.empty(shape + (c["page"] * c["d"],), dtype=_E4M3, device=dev),
+            "v": torch.empty(shape + (c["page"] * c["d"],), dtype=_E4M3, device=dev),
             "scale": torch.empty(shape + (2,), dtype=torch.float32, device=dev),
             "kmean": torch.empty(shape + (c["d"],), dtype=torch.bfloat16, device=dev)}
     for layer in range(c["layers"]):
         for i, name in enumerate(("k", "v")):
-            x = torch.randn(pool[name].shape[1:], generator=g, device=dev)
+            x = torch.randn(rows, generator=g, device=dev)
             x *= 0.5
             if name == "k":      # pages differ in where their keys point, as the topics of a text do
                 x += 0.5 * torch.randn(x.shape[:2] + (1, c["d"]), generator=g, device=dev)
             s = _pow2(_exponent(x.abs().amax((-1, -2))))
             pool["scale"][layer, ..., i] = s
-            pool[name][layer] = (x / s[..., None, None]).to(_E4M3)
+            x = (x / s[..., None, None]).to(_E4M3)
+            pool[name][layer] = _k_order(x) if name == "k" else _v_order(x)
             if name == "k":
-                pool["kmean"][layer] = (pool["k"][layer].float().sum(-2) * (s / c["page"])[..., None]).to(torch.bfloat16)
+                pool["kmean"][layer] = (x.float().sum(-2) * (s / c["page"])[..., None]).to(torch.bfloat16)
     return pool
 
 
@@ -217,12 +243,11 @@ def _plain_append(st):
         e = _exponent(torch.where(new, x, 0).abs().amax((-1, -2)))                                  # [T, H]
         before = torch.frexp(st["scale"][0, phys, :, i])[1] - 1
         e = torch.where(is_old.any(1)[:, None], torch.maximum(e, before), e)
-        codes = st[name][0, phys]
-        codes = codes if name == "k" else codes.transpose(-1, -2)
+        codes = _k_rows(st[name][0, phys], c["d"]) if name == "k" else _v_rows(st[name][0, phys], c["d"])
         old = (codes.float() * _pow2((before - e).clamp(max=0))[..., None, None]).to(_E4M3)
         out = torch.where(is_old[:, None, :, None], old.float(), codes.float())
         out = torch.where(new, (x * _pow2(-e)[..., None, None]).to(_E4M3).float(), out).to(_E4M3)
-        st[name][0, phys] = out if name == "k" else out.transpose(-1, -2)
+        st[name][0, phys] = _k_order(out) if name == "k" else _v_order(out)
         st["scale"][0, phys, :, i] = _pow2(e)
         if name == "k":
             full = (lp + 1) * page <= held[seq]
@@ -245,8 +270,8 @@ def _plain_attend(st, lists=None):
     rows, there, n = _rows_of(st)
     table = st["table"].long().clamp(min=0)
     scale = st["scale"][0][table]                                                                   # [S, P, H, 2]
-    k = (st["k"][0][table].float() * scale[..., 0, None, None]).transpose(1, 2).reshape(len(n), kv, -1, d)
-    v = (st["v"][0][table].float() * scale[..., 1, None, None]).permute(0, 2, 1, 4, 3).reshape(len(n), kv, -1, d)
+    k = (_k_rows(st["k"][0][table], d).float() * scale[..., 0, None, None]).transpose(1, 2).reshape(len(n), kv, -1, d)
+    v = (_v_rows(st["v"][0][table], d).float() * scale[..., 1, None, None]).transpose(1, 2).reshape(len(n), kv, -1, d)
     grp = c["heads"] // kv
     q = st["q"].float()[rows].view(len(n), -1, kv, grp, d).permute(0, 2, 1, 3, 4).reshape(len(n), kv, -1, d)
     s = torch.matmul(q, k.transpose(-1, -2)) / math.sqrt(d)
@@ -416,16 +441,26 @@ def _e4m3_of(x):
     return torch.round(x / step) * step
 
 
+def _places(page, d):
+    """[page, D] the byte of a page that holds token t's channel ch, of K and of V."""
+    t, ch = torch.arange(page, device="cuda")[:, None], torch.arange(d, device="cuda")
+    block = (t // 16) * 16 * d + (ch // 64) * 1024
+    k = block + (ch % 64 // 16) * 256 + (t % 16) * 16 + ch % 16
+    return k, block + (t % 16 // 4) * 256 + (ch % 16) * 16 + (ch % 64 // 16) * 4 + t % 4
+
+
 def _exact_append(c, st):
     page = c["page"]
     at = 0
+    kat, vat = _places(page, c["d"])
     k, v, scale, mean = (st[x].double() for x in ("k", "v", "scale", "kmean"))
     for s, (held, n) in enumerate(_sequences(c)):
         start = held - n
         for lp in range(start // page, -(-held // page) if n else 0):
             phys = int(st["table"][s, lp])
             a, b = max(start, lp * page), min(held, (lp + 1) * page)
-            for pool, i, x in ((k[0, phys], 0, st["new_k"]), (v[0, phys].transpose(-1, -2), 1, st["new_v"])):
+            for codes, where, i, x in ((k[0, phys], kat, 0, st["new_k"]), (v[0, phys], vat, 1, st["new_v"])):
+                pool = codes[:, where]                                                 # [H, page, D]
                 new = x[at + a - start:at + b - start].double().transpose(0, 1)        # [H, tokens, D]
                 top = new.abs().amax((1, 2)).clamp(min=2.0 ** -200)
                 e = torch.ceil(torch.log2(top / 448)).clamp(min=_MIN_EXP)
@@ -438,6 +473,7 @@ def _exact_append(c, st):
                     pool[:, :a - lp * page] = _e4m3_of(old * (was / torch.exp2(e))[:, None, None])
                 scale[0, phys, :, i] = torch.exp2(e)
                 pool[:, a - lp * page:b - lp * page] = _e4m3_of(new / torch.exp2(e)[:, None, None])
+                codes[:, where] = pool
                 if i == 0 and held >= (lp + 1) * page:
                     mean[0, phys] = pool.mean(1) * torch.exp2(e)[:, None]
         at += n
@@ -483,6 +519,7 @@ def exact(case, seed):
         return None
     page, kv, d = c["page"], c["kv_heads"], c["d"]
     grp = c["heads"] // kv
+    kat, vat = _places(page, d)
     out = torch.empty((st["rows"], c["heads"], d), dtype=torch.float64, device="cuda")
     at = 0
     for s, (held, n) in enumerate(seqs):
@@ -496,9 +533,9 @@ def exact(case, seed):
         if c["kind"] == "sparse":
             sees = sees & _exact_lists(c, st, s, held, n, q).repeat_interleave(page, -1)
         for h in range(kv):
-            k = st["k"][0, ids, h].double() * st["scale"][0, ids, h, 0].double()[:, None, None]
-            v = st["v"][0, ids, h].double() * st["scale"][0, ids, h, 1].double()[:, None, None]
-            k, v = k.reshape(-1, d), v.transpose(1, 2).reshape(-1, d)
+            k = st["k"][0, ids, h].double()[:, kat] * st["scale"][0, ids, h, 0].double()[:, None, None]
+            v = st["v"][0, ids, h].double()[:, vat] * st["scale"][0, ids, h, 1].double()[:, None, None]
+            k, v = k.reshape(-1, d), v.reshape(-1, d)
             for g in range(grp):
                 w = (q[:, h, g] @ k.T) * d ** -0.5
                 w = torch.softmax(torch.where(sees[:, h], w, -math.inf), -1)
