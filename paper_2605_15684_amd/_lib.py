@@ -34,7 +34,11 @@ EXPORTS = ("ssba_abi_version", "ssba_status_str", "ssba_workspace_size", "ssba_b
            "ssba_probe_mfma", "ssba_build_index_ex", "ssba_forward_ex", "ssba_forward_topk_ex",
            "ssba_forward_train_ex", "ssba_backward_ex", "ssba_forward_layers_ex",
            "ssba_read_device_status_ex", "ssba_forward_topk_noalloc", "ssba_pool_keys_ex",
-           "ssba_forward_gated_ex", "ssba_rope_pool_keys_ex", "ssba_forward_topk_rope_ex")
+           "ssba_forward_gated_ex", "ssba_rope_pool_keys_ex", "ssba_forward_topk_rope_ex",
+           "ssba_cache_append", "ssba_cache_select_workspace_size", "ssba_cache_select",
+           "ssba_cache_attend_workspace_size", "ssba_cache_attend", "ssba_pages_workspace_size",
+           "ssba_pages_reserve", "ssba_pages_fork", "ssba_pages_release", "ssba_pages_compact",
+           "ssba_pages_copy")
 
 # Byte count that the binding passes for a buffer it cannot size (None).
 UNSIZED = ctypes.c_size_t(-1).value
@@ -60,6 +64,30 @@ class SsbaLayer(ctypes.Structure):
 class HaarDesc(ctypes.Structure):
     _fields_ = [("n", ctypes.c_int32), ("c", ctypes.c_int32), ("h", ctypes.c_int32), ("w", ctypes.c_int32),
                 ("levels", ctypes.c_int32), ("dtype", ctypes.c_int32)]
+
+
+class CacheDesc(ctypes.Structure):          # ssba_cache
+    _fields_ = [("layers", ctypes.c_int32), ("pages", ctypes.c_int32), ("kv_heads", ctypes.c_int32),
+                ("head_dim", ctypes.c_int32), ("page", ctypes.c_int32), ("k", ctypes.c_void_p),
+                ("v", ctypes.c_void_p), ("scale", ctypes.c_void_p), ("kmean", ctypes.c_void_p)]
+
+
+class CacheBatch(ctypes.Structure):         # ssba_cache_batch
+    _fields_ = [("seqs", ctypes.c_int32), ("max_pages", ctypes.c_int32), ("rows", ctypes.c_int32),
+                ("max_new", ctypes.c_int32), ("max_len", ctypes.c_int32), ("table", ctypes.c_void_p),
+                ("lens", ctypes.c_void_p), ("cu", ctypes.c_void_p)]
+
+
+class CacheQuery(ctypes.Structure):         # ssba_cache_query
+    _fields_ = [("heads", ctypes.c_int32), ("dtype", ctypes.c_int32), ("causal", ctypes.c_int32),
+                ("keep", ctypes.c_int32), ("first", ctypes.c_int32), ("last", ctypes.c_int32),
+                ("softmax_scale", ctypes.c_float), ("q_stride_t", ctypes.c_int64), ("q_stride_h", ctypes.c_int64),
+                ("o_stride_t", ctypes.c_int64), ("o_stride_h", ctypes.c_int64)]
+
+
+class CachePages(ctypes.Structure):         # ssba_pages
+    _fields_ = [("rows", ctypes.c_int32), ("max_pages", ctypes.c_int32), ("table", ctypes.c_void_p),
+                ("lens", ctypes.c_void_p), ("refs", ctypes.c_void_p)]
 
 
 class SsbaError(RuntimeError):
@@ -128,6 +156,8 @@ def load(path: str = None) -> ctypes.CDLL:
     lib.ssba_read_device_status.argtypes = [dp, vp, ctypes.POINTER(ctypes.c_int), vp]
     lib.ssba_probe_mfma.restype = ctypes.c_int
     lib.ssba_probe_mfma.argtypes = [ctypes.c_int32, ctypes.c_int32, vp, vp]
+    i32, i64 = ctypes.c_int32, ctypes.c_int64
+    cp, bp, qp, pp = (ctypes.POINTER(t) for t in (CacheDesc, CacheBatch, CacheQuery, CachePages))
     for name, args in (("ssba_build_index_ex", [dp, vp, vp, vp, sz, vp, sz, vp]),
                        ("ssba_forward_ex", [dp, vp, vp, vp, vp, sz, vp, vp]),
                        ("ssba_forward_topk_ex", [dp, vp, vp, vp, vp, sz, vp, sz, vp, vp]),
@@ -141,7 +171,18 @@ def load(path: str = None) -> ctypes.CDLL:
                        ("ssba_forward_gated_ex", [dp, vp, vp, vp, vp, sz, vp, sz, vp, vp]),
                        ("ssba_rope_pool_keys_ex", [dp, vp, vp, vp, vp, ctypes.c_float, vp, sz, vp]),
                        ("ssba_forward_topk_rope_ex", [dp, vp, vp, vp, vp, vp, ctypes.c_float, vp, sz, vp, sz,
-                                                      vp, vp])):
+                                                      vp, vp]),
+                       ("ssba_cache_append", [cp, i32, bp, i32, vp, vp, i64, i64, vp]),
+                       ("ssba_cache_select_workspace_size", [cp, bp, qp, ctypes.POINTER(sz)]),
+                       ("ssba_cache_select", [cp, i32, bp, qp, vp, vp, sz, vp, sz, vp]),
+                       ("ssba_cache_attend_workspace_size", [cp, bp, qp, i32, ctypes.POINTER(sz)]),
+                       ("ssba_cache_attend", [cp, i32, bp, qp, vp, vp, sz, vp, vp, sz, vp]),
+                       ("ssba_pages_workspace_size", [cp, pp, i32, ctypes.POINTER(sz)]),
+                       ("ssba_pages_reserve", [cp, pp, vp, vp, sz, vp]),
+                       ("ssba_pages_fork", [cp, pp, i32, vp, vp, vp, vp, sz, vp]),
+                       ("ssba_pages_release", [cp, pp, i32, vp, vp, vp, sz, vp]),
+                       ("ssba_pages_compact", [cp, pp, vp, vp, vp, vp, sz, vp]),
+                       ("ssba_pages_copy", [cp, cp, i32, vp, vp, vp])):
         fn = getattr(lib, name)
         fn.restype = ctypes.c_int
         fn.argtypes = args

@@ -33,6 +33,13 @@ SOURCES = {
     "ssba_bwd.hip": [],
     "ssba_probe.hip": [],
     "ssba_noalloc.hip": [],
+    "ssba_cache_api.cpp": [],
+    "ssba_cache_append.hip": [],
+    # MFMA results in ordinary VGPRs, as above.
+    "ssba_cache_attn.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form"],
+    # 64-bit scores: no contraction of multiply-add, so lists do not depend on the compiler.
+    "ssba_cache_select.hip": ["-ffp-contract=off"],
+    "ssba_cache_pages.hip": [],
 }
 
 COMMON = [

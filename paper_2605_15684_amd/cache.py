@@ -1,0 +1,310 @@
+"""Torch-facing binding of the paged 8-bit key/value cache (include/ssba_cache.h).
+
+Argument marshalling only, like ssba.py: tensors are checked, outputs and
+scratch allocated with torch, and raw device pointers plus the current HIP
+stream of the tensors' device passed to the HIP kernels in libssba.so.
+Importing fails if the library is not built.
+
+    pool = cache.alloc(layers, pages, kv_heads, head_dim, page=64)
+    rows = cache.alloc_rows(pool, rows, max_pages)          # table, lens, refs
+    ...                                                     # lens += new tokens
+    cache.reserve(pool, *rows)
+    batch = cache.Batch(table, lens, cu, max_new)
+    cache.append(pool, layer, batch, k, v)                  # [tokens, kv_heads, D]
+    o = cache.attend(pool, layer, batch, q)                 # [tokens, heads, D]
+    lists = cache.select(pool, layer, batch, q, keep=32)    # or: the best 32 pages of each token
+    o = cache.attend(pool, layer, batch, q, lists=lists)
+"""
+from __future__ import annotations
+
+import ctypes
+from typing import Optional, Tuple
+
+import torch
+
+from . import _lib
+
+_L = _lib.load()   # fail loudly at import if the HIP library is missing
+
+__all__ = ["PagedCache", "Batch", "alloc", "alloc_rows", "append", "select", "attend", "reserve", "fork", "release",
+           "compact", "copy_pages", "SsbaError"]
+
+SsbaError = _lib.SsbaError
+E4M3 = torch.float8_e4m3fn
+_DTYPES = {torch.bfloat16: _lib.DT_BF16, torch.float32: _lib.DT_F32}
+
+
+def _stream(dev) -> int:
+    return torch.cuda.current_stream(dev).cuda_stream
+
+
+def _on(dev):
+    """Makes `dev` the current device for a call (nothing to do if it is)."""
+    return torch.cuda.device(dev)
+
+
+def _check(t, shape, dtype, dev, what: str) -> None:
+    if not (isinstance(t, torch.Tensor) and t.is_cuda and t.dtype == dtype and t.is_contiguous()
+            and (shape is None or tuple(t.shape) == tuple(shape))):
+        raise ValueError(f"{what}: expected a contiguous {dtype} GPU tensor" +
+                         (f" of shape {tuple(shape)}" if shape is not None else ""))
+    if dev is not None and t.device != dev:
+        raise ValueError(f"{what}: all tensors must be on one device")
+
+
+class PagedCache:
+    """The arrays of a cache: k, v [layers, pages, kv_heads, page * D] e4m3, scale fp32
+    [layers, pages, kv_heads, 2], kmean bf16 [layers, pages, kv_heads, D] (byte order of the pages:
+    include/ssba_cache.h).  Holds references to the tensors, copies nothing."""
+
+    def __init__(self, k: torch.Tensor, v: torch.Tensor, scale: torch.Tensor, kmean: torch.Tensor):
+        if not isinstance(k, torch.Tensor) or k.dim() != 4 or not isinstance(kmean, torch.Tensor) or kmean.dim() != 4:
+            raise ValueError("k and kmean: expected [layers, pages, kv_heads, ...] tensors")
+        layers, pages, kv_heads, size = k.shape
+        d = kmean.shape[-1]
+        dev = k.device
+        _check(k, None, E4M3, None, "k")
+        _check(v, k.shape, E4M3, dev, "v")
+        _check(scale, (layers, pages, kv_heads, 2), torch.float32, dev, "scale")
+        _check(kmean, (layers, pages, kv_heads, d), torch.bfloat16, dev, "kmean")
+        if d < 1 or size % d:
+            raise ValueError("k: the last dimension must be page * D")
+        self.k, self.v, self.scale, self.kmean, self.device = k, v, scale, kmean, dev
+        self.layers, self.pages, self.kv_heads, self.head_dim, self.page = layers, pages, kv_heads, d, size // d
+        self.desc = _lib.CacheDesc(layers, pages, kv_heads, d, size // d, k.data_ptr(), v.data_ptr(),
+                                   scale.data_ptr(), kmean.data_ptr())
+
+
+class Batch:
+    """Sequences of a call: table int32 [seqs, max_pages], lens int32 [seqs] (tokens held, the new ones
+    included), cu int32 [seqs + 1] (the new tokens' rows in the packed arrays).  max_new: at least the new
+    tokens of any sequence; max_len: about the longest sequence (work is split by it; results are not)."""
+
+    def __init__(self, table: torch.Tensor, lens: torch.Tensor, cu: torch.Tensor, max_new: int,
+                 max_len: Optional[int] = None):
+        if not isinstance(table, torch.Tensor) or table.dim() != 2:
+            raise ValueError("table: expected a [seqs, max_pages] tensor")
+        seqs, max_pages = table.shape
+        _check(table, None, torch.int32, None, "table")
+        _check(lens, (seqs,), torch.int32, table.device, "lens")
+        _check(cu, (seqs + 1,), torch.int32, table.device, "cu")
+        self.table, self.lens, self.cu, self.device = table, lens, cu, table.device
+        self.desc = _lib.CacheBatch(seqs, max_pages, 0, int(max_new), int(max_len or 0), table.data_ptr(),
+                                    lens.data_ptr(), cu.data_ptr())
+
+    def _with_rows(self, rows: int) -> _lib.CacheBatch:
+        d = self.desc
+        return _lib.CacheBatch(d.seqs, d.max_pages, rows, d.max_new, d.max_len, d.table, d.lens, d.cu)
+
+
+def alloc(layers: int, pages: int, kv_heads: int, head_dim: int, page: int = 64, device="cuda") -> PagedCache:
+    """A new cache (its contents are arbitrary until appended to)."""
+    shape = (layers, pages, kv_heads)
+    return PagedCache(torch.empty(shape + (page * head_dim,), dtype=E4M3, device=device),
+                      torch.empty(shape + (page * head_dim,), dtype=E4M3, device=device),
+                      torch.empty(shape + (2,), dtype=torch.float32, device=device),
+                      torch.empty(shape + (head_dim,), dtype=torch.bfloat16, device=device))
+
+
+def alloc_rows(pool: PagedCache, rows: int, max_pages: int) -> Tuple[torch.Tensor, torch.Tensor, torch.Tensor]:
+    """Empty page table, lens and refs of `rows` sequences over the pages of `pool`."""
+    return (torch.full((rows, max_pages), -1, dtype=torch.int32, device=pool.device),
+            torch.zeros(rows, dtype=torch.int32, device=pool.device),
+            torch.zeros(pool.pages, dtype=torch.int32, device=pool.device))
+
+
+def _packed(t, rows, heads, pool: PagedCache, dtype, what: str):
+    """Checks a packed [rows, heads, D] tensor; its (token, head) strides."""
+    if not (isinstance(t, torch.Tensor) and t.is_cuda and t.dim() == 3 and t.dtype in _DTYPES):
+        raise ValueError(f"{what}: expected a [tokens, heads, D] GPU tensor, bf16 or fp32")
+    if t.device != pool.device:
+        raise ValueError(f"{what}: all tensors must be on one device")
+    if dtype is not None and t.dtype != dtype:
+        raise ValueError(f"{what}: expected {dtype}")
+    if t.shape[2] != pool.head_dim or (heads is not None and t.shape[1] != heads) or \
+            (rows is not None and t.shape[0] != rows):
+        raise ValueError(f"{what}: expected shape [{'tokens' if rows is None else rows}, "
+                         f"{'heads' if heads is None else heads}, {pool.head_dim}]")
+    st, sh, sc = t.stride()
+    if sc != 1 and t.numel():
+        raise ValueError(f"{what}: channel stride must be 1")
+    # A dimension of one has no stride that matters; torch may report any.
+    return (st if t.shape[0] > 1 else t.shape[1] * max(sh, pool.head_dim) if t.shape[1] > 1 else pool.head_dim,
+            sh if t.shape[1] > 1 else pool.head_dim)
+
+
+def _same_device(pool: PagedCache, batch: Batch) -> None:
+    if pool.device != batch.device:
+        raise ValueError("cache and batch must be on one device")
+
+
+def append(pool: PagedCache, layer: int, batch: Batch, k: torch.Tensor, v: torch.Tensor) -> None:
+    """Quantises the new tokens' keys and values ([tokens, kv_heads, D]) into `layer` of the cache."""
+    _same_device(pool, batch)
+    strides = _packed(k, None, pool.kv_heads, pool, None, "k")
+    if _packed(v, k.shape[0], pool.kv_heads, pool, k.dtype, "v") != strides:
+        raise ValueError("k and v must share their strides")
+    with _on(pool.device):
+        _lib.check(_L.ssba_cache_append(pool.desc, layer, batch._with_rows(k.shape[0]), _DTYPES[k.dtype], k.data_ptr(),
+                                        v.data_ptr(), *strides, _stream(pool.device)), "ssba_cache_append")
+
+
+def _scratch(size: int, given, dev):
+    if given is not None:
+        if not (isinstance(given, torch.Tensor) and given.is_cuda and given.is_contiguous() and given.device == dev):
+            raise ValueError("scratch must be a contiguous GPU tensor on the cache's device")
+        return given, given.numel() * given.element_size()
+    return torch.empty(size, dtype=torch.uint8, device=dev), size
+
+
+def select(pool: PagedCache, layer: int, batch: Batch, q: torch.Tensor, *, keep: int, first: int = 1, last: int = 1,
+           causal: bool = True, lists: Optional[torch.Tensor] = None,
+           scratch: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """The `keep` pages each new token reads: int32 [tokens, kv_heads, 1 + keep] (count, pages of the sequence
+    ascending, -1 padding).  `first` leading and `last` trailing pages are always among them."""
+    _same_device(pool, batch)
+    qs = _packed(q, None, None, pool, None, "q")
+    rows, heads = q.shape[:2]
+    b = batch._with_rows(rows)
+    desc = _lib.CacheQuery(heads, _DTYPES[q.dtype], int(bool(causal)), keep, first, last, 0.0, *qs, 0, 0)
+    size = ctypes.c_size_t(0)
+    _lib.check(_L.ssba_cache_select_workspace_size(pool.desc, b, desc, ctypes.byref(size)),
+               "ssba_cache_select_workspace_size")
+    if lists is None:
+        lists = torch.empty((rows, pool.kv_heads, 1 + keep), dtype=torch.int32, device=pool.device)
+    _check(lists, (rows, pool.kv_heads, 1 + keep), torch.int32, pool.device, "lists")
+    scratch, have = _scratch(size.value, scratch, pool.device)
+    with _on(pool.device):
+        _lib.check(_L.ssba_cache_select(pool.desc, layer, b, desc, q.data_ptr(), lists.data_ptr(), lists.numel() * 4,
+                                        scratch.data_ptr(), have, _stream(pool.device)), "ssba_cache_select")
+    return lists
+
+
+def attend(pool: PagedCache, layer: int, batch: Batch, q: torch.Tensor, *, lists: Optional[torch.Tensor] = None,
+           causal: bool = True, scale: Optional[float] = None, out: Optional[torch.Tensor] = None,
+           scratch: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """Attention of the new tokens' queries [tokens, heads, D] over what their sequences hold, or over the pages
+    that `lists` (of select) names.  Rows of no sequence are left as they are in `out`."""
+    _same_device(pool, batch)
+    qs = _packed(q, None, None, pool, None, "q")
+    rows, heads = q.shape[:2]
+    if out is None:
+        out = torch.empty((rows, heads, pool.head_dim), dtype=q.dtype, device=q.device)
+    os = _packed(out, rows, heads, pool, q.dtype, "out")
+    keep, lp, lb = 0, None, 0
+    if lists is not None:
+        if not (isinstance(lists, torch.Tensor) and lists.dim() == 3 and lists.shape[2] > 1):
+            raise ValueError("lists: expected [tokens, kv_heads, 1 + keep]")
+        _check(lists, (rows, pool.kv_heads, lists.shape[2]), torch.int32, pool.device, "lists")
+        keep, lp, lb = lists.shape[2] - 1, lists.data_ptr(), lists.numel() * 4
+    b = batch._with_rows(rows)
+    desc = _lib.CacheQuery(heads, _DTYPES[q.dtype], int(bool(causal)), keep, 0, 0,
+                           0.0 if scale is None else float(scale), *qs, *os)
+    size = ctypes.c_size_t(0)
+    _lib.check(_L.ssba_cache_attend_workspace_size(pool.desc, b, desc, int(lists is not None), ctypes.byref(size)),
+               "ssba_cache_attend_workspace_size")
+    scratch, have = _scratch(size.value, scratch, pool.device)
+    with _on(pool.device):
+        _lib.check(_L.ssba_cache_attend(pool.desc, layer, b, desc, q.data_ptr(), lp, lb, out.data_ptr(),
+                                        scratch.data_ptr(), have, _stream(pool.device)), "ssba_cache_attend")
+    return out
+
+
+def _rows(pool: PagedCache, table, lens, refs) -> _lib.CachePages:
+    if not isinstance(table, torch.Tensor) or table.dim() != 2:
+        raise ValueError("table: expected a [rows, max_pages] tensor")
+    _check(table, None, torch.int32, pool.device, "table")
+    _check(lens, (table.shape[0],), torch.int32, pool.device, "lens")
+    _check(refs, (pool.pages,), torch.int32, pool.device, "refs")
+    return _lib.CachePages(table.shape[0], table.shape[1], table.data_ptr(), lens.data_ptr(), refs.data_ptr())
+
+
+def _pages_scratch(pool: PagedCache, desc, n: int, given):
+    size = ctypes.c_size_t(0)
+    _lib.check(_L.ssba_pages_workspace_size(pool.desc, desc, n, ctypes.byref(size)), "ssba_pages_workspace_size")
+    return _scratch(size.value, given, pool.device)
+
+
+def _info(pool: PagedCache, given) -> torch.Tensor:
+    if given is None:
+        return torch.empty(2, dtype=torch.int32, device=pool.device)
+    _check(given, (2,), torch.int32, pool.device, "info")
+    return given
+
+
+def _numbers(pool: PagedCache, t, n, what: str) -> torch.Tensor:
+    _check(t, None, torch.int32, pool.device, what)
+    if t.dim() != 1 or (n is not None and t.shape[0] != n):
+        raise ValueError(f"{what}: expected a vector" + (f" of {n}" if n is not None else ""))
+    return t
+
+
+def reserve(pool: PagedCache, table, lens, refs, info=None, scratch=None) -> torch.Tensor:
+    """Gives every row the pages that lens tokens need, lowest free page first.  Updates table and refs; returns
+    info = {entries served, entries left without a page}."""
+    desc = _rows(pool, table, lens, refs)
+    info = _info(pool, info)
+    scratch, have = _pages_scratch(pool, desc, 0, scratch)
+    with _on(pool.device):
+        _lib.check(_L.ssba_pages_reserve(pool.desc, desc, info.data_ptr(), scratch.data_ptr(), have,
+                                         _stream(pool.device)), "ssba_pages_reserve")
+    return info
+
+
+def fork(pool: PagedCache, table, lens, refs, src, dst, info=None, scratch=None) -> torch.Tensor:
+    """Row dst[j] becomes a copy of row src[j]: complete pages shared, an incomplete last one copied.  Updates
+    table, lens and refs; returns info = {pairs forked, of them cut for lack of a page}."""
+    desc = _rows(pool, table, lens, refs)
+    n = _numbers(pool, src, None, "src").shape[0]
+    _numbers(pool, dst, n, "dst")
+    info = _info(pool, info)
+    scratch, have = _pages_scratch(pool, desc, n, scratch)
+    with _on(pool.device):
+        _lib.check(_L.ssba_pages_fork(pool.desc, desc, n, src.data_ptr(), dst.data_ptr(), info.data_ptr(),
+                                      scratch.data_ptr(), have, _stream(pool.device)), "ssba_pages_fork")
+    return info
+
+
+def release(pool: PagedCache, table, lens, refs, rows, info=None, scratch=None) -> torch.Tensor:
+    """Empties rows.  Updates table, lens and refs; returns info = {entries released, pages that became free}."""
+    desc = _rows(pool, table, lens, refs)
+    n = _numbers(pool, rows, None, "rows").shape[0]
+    info = _info(pool, info)
+    scratch, have = _pages_scratch(pool, desc, n, scratch)
+    with _on(pool.device):
+        _lib.check(_L.ssba_pages_release(pool.desc, desc, n, rows.data_ptr(), info.data_ptr(), scratch.data_ptr(),
+                                         have, _stream(pool.device)), "ssba_pages_release")
+    return info
+
+
+def compact(pool: PagedCache, table, refs, table_out=None, refs_out=None, info=None, scratch=None):
+    """Moves the pages in use to the low end of the pool.  Returns (table, refs, info) after it, info = {pages in
+    use, pages moved}; table_out and refs_out may be table and refs themselves."""
+    table_out = torch.empty_like(table) if table_out is None else table_out
+    refs_out = torch.empty_like(refs) if refs_out is None else refs_out
+    info = _info(pool, info)
+    if not isinstance(table, torch.Tensor) or table.dim() != 2:
+        raise ValueError("table: expected a [rows, max_pages] tensor")
+    _check(table, None, torch.int32, pool.device, "table")
+    _check(refs, (pool.pages,), torch.int32, pool.device, "refs")
+    _check(table_out, table.shape, torch.int32, pool.device, "table_out")
+    _check(refs_out, refs.shape, torch.int32, pool.device, "refs_out")
+    # lens takes no part; any array stands in its place
+    desc = _lib.CachePages(table.shape[0], table.shape[1], table.data_ptr(), refs.data_ptr(), refs.data_ptr())
+    scratch, have = _pages_scratch(pool, desc, 0, scratch)
+    with _on(pool.device):
+        _lib.check(_L.ssba_pages_compact(pool.desc, desc, table_out.data_ptr(), refs_out.data_ptr(), info.data_ptr(),
+                                         scratch.data_ptr(), have, _stream(pool.device)), "ssba_pages_compact")
+    return table_out, refs_out, info
+
+
+def copy_pages(pool: PagedCache, src, dst, to: Optional[PagedCache] = None) -> None:
+    """Copies pages of all layers, to.pages[dst[j]] = pool.pages[src[j]] (`to`: another cache of the same layout)."""
+    to = pool if to is None else to
+    if to.device != pool.device:
+        raise ValueError("both caches must be on one device")
+    n = _numbers(pool, src, None, "src").shape[0]
+    _numbers(pool, dst, n, "dst")
+    with _on(pool.device):
+        _lib.check(_L.ssba_pages_copy(pool.desc, to.desc, n, src.data_ptr(), dst.data_ptr(), _stream(pool.device)),
+                   "ssba_pages_copy")

@@ -1,0 +1,137 @@
+// Internal declarations of the paged 8-bit key/value cache (include/ssba_cache.h).
+#pragma once
+
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+#include "../../include/ssba_cache.h"
+
+namespace ssba {
+
+// One layer of a cache.
+struct CacheView {
+  uint8_t* k;
+  uint8_t* v;
+  float* scale;      // [pages][kv_heads][2]
+  uint16_t* kmean;   // [pages][kv_heads][D]
+  int64_t page_bytes;  // kv_heads * page * D: one page of k or v
+  int pages, kv_heads, head_dim;
+  int page_log2;
+};
+
+struct BatchView {
+  const int32_t* table;
+  const int32_t* lens;
+  const int32_t* cu;
+  int seqs, max_pages, rows, max_new;
+};
+
+// A sequence of the batch as the kernels see it: whatever the arrays hold,
+// begin + n <= rows and 0 <= len <= max_pages * page.
+struct SeqView {
+  int begin, n, len;
+};
+
+__device__ __forceinline__ SeqView seq_view(const BatchView& b, int page_log2, int s) {
+  SeqView v;
+  v.begin = min(max(b.cu[s], 0), b.rows);
+  v.n = max(min(b.cu[s + 1], b.rows), v.begin) - v.begin;
+  v.len = min(max(b.lens[s], 0), b.max_pages << page_log2);
+  return v;
+}
+
+// Sequence of packed row r: the number of ends cu[1..seqs] that are <= r
+// (seqs: no sequence).  One wave; every lane gets the result.
+__device__ __forceinline__ int seq_of_row(const BatchView& b, int r, int lane) {
+  int s = 0;
+  for (int j0 = 1; j0 <= b.seqs; j0 += 64) {
+    const int j = j0 + lane;
+    const bool past = j <= b.seqs && b.cu[j] <= r;
+    const int c = __popcll(__builtin_amdgcn_ballot_w64(past));
+    s += c;
+    if (c < 64) break;   // cu does not decrease
+  }
+  return __builtin_amdgcn_readfirstlane(s);
+}
+
+struct AppendArgs {
+  CacheView c;
+  BatchView b;
+  const void* k;
+  const void* v;
+  int64_t st, sh;
+  int slots;   // pages a sequence can touch
+};
+
+struct SelectArgs {
+  CacheView c;
+  BatchView b;
+  const void* q;
+  int64_t st, sh;
+  int32_t* lists;
+  uint64_t* keys;   // [rows][kv_heads][max_pages] ranking keys of the scored pages
+  int group, causal, keep, first, last;
+  int chunks;       // workgroups that share a row's pages
+};
+constexpr int kSelectPages = 256;   // pages a workgroup scores at a time
+
+struct AttendArgs {
+  CacheView c;
+  BatchView b;
+  const void* q;
+  void* o;
+  int64_t q_st, q_sh, o_st, o_sh;
+  const int32_t* lists;   // [rows][kv_heads][1 + keep] or null
+  float* part;            // partial results of split items
+  float scale_log2;
+  int group, causal, keep;
+  int col_tiles;          // column tiles of an item
+  int splits;             // workgroups that share an item's keys
+};
+
+// What the attention launch does (ssba_cache_api.cpp decides).
+struct AttendPlan {
+  int tiles16;      // R: column tiles of 16 per wave
+  bool listed;
+  bool by_columns;  // the waves of a workgroup take different columns (else different keys)
+  int col_tiles, splits;
+  int64_t items;    // (sequence or row, kv head, column tile)
+};
+
+hipError_t launch_cache_append(const AppendArgs& a, int dtype, hipStream_t s);
+hipError_t launch_cache_select(const SelectArgs& a, int dtype, hipStream_t s);
+hipError_t launch_cache_attend(const AttendArgs& a, const AttendPlan& p, int dtype, hipStream_t s);
+
+struct PagesArgs {
+  int rows, max_pages, pages, page_log2;
+  int32_t* table;
+  int32_t* lens;
+  int32_t* refs;
+  int32_t* info;
+  int32_t* scratch;
+  const int32_t* src;
+  const int32_t* dst;
+  int32_t* table_out;
+  int32_t* refs_out;
+  int n;
+};
+// A whole cache for page copies: per page and layer the bytes of each array.
+struct CopyArgs {
+  const char* from[4];
+  char* to[4];
+  int64_t bytes[4];          // per page
+  int64_t from_layer[4], to_layer[4];   // bytes per layer
+  int layers, from_pages, to_pages;
+  const int32_t* src;
+  const int32_t* dst;
+  const int32_t* count;      // pairs (null: n)
+  int n;
+};
+
+hipError_t launch_pages_reserve(const PagesArgs& a, hipStream_t s);
+hipError_t launch_pages_fork(const PagesArgs& a, hipStream_t s);
+hipError_t launch_pages_release(const PagesArgs& a, hipStream_t s);
+hipError_t launch_pages_compact(const PagesArgs& a, hipStream_t s);
+hipError_t launch_pages_copy(const CopyArgs& a, hipStream_t s);
+
+}  // namespace ssba
