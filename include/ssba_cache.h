@@ -22,8 +22,9 @@
  *            K: 16 D T + 1024 (c/64) + 256 (c%64 / 16) + 16 r + c%16
  *            V: 16 D T + 1024 (c/64) + 256 (r/4) + 16 (c%16) + 4 (c%64 / 16) + r%4
  *          of its page (16-byte loads of a wave are 1024 consecutive bytes).
- *   scale  fp32 [layers][pages][kv_heads][2]: a key is scale[0] * code, a
- *          value scale[1] * code.
+ *   scale  fp32 [layers][pages][kv_heads][2], 8-byte aligned: a key is
+ *          scale[0] * code, a value scale[1] * code; positive (append writes
+ *          powers of two).
  *   kmean  bf16 [layers][pages][kv_heads][D], 16-byte aligned: the mean of the
  *          keys of a complete page (select reads it; attend does not).
  * Nothing has to be initialised: slots behind a sequence's end are never used,

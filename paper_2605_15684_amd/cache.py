@@ -34,18 +34,29 @@ E4M3 = torch.float8_e4m3fn
 _DTYPES = {torch.bfloat16: _lib.DT_BF16, torch.float32: _lib.DT_F32}
 
 
-def _stream(dev) -> int:
-    return torch.cuda.current_stream(dev).cuda_stream
+# The current HIP stream of a device as a number.  A call of this module costs
+# a few microseconds on the host, of which torch.cuda.current_stream() (it
+# makes a Stream object) would be two.
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or \
+    (lambda index: torch.cuda.current_stream(index).cuda_stream)
 
 
-def _on(dev):
-    """Makes `dev` the current device for a call (nothing to do if it is)."""
-    return torch.cuda.device(dev)
+def _call(pool, fn, name: str, *args) -> None:
+    """fn(*args, stream) on the current stream of the cache's device."""
+    index = pool.index
+    if torch.cuda.current_device() == index:
+        st = fn(*args, _raw_stream(index))
+    else:
+        with torch.cuda.device(index):
+            st = fn(*args, _raw_stream(index))
+    if st:
+        _lib.check(st, name)
 
 
 def _check(t, shape, dtype, dev, what: str) -> None:
+    """A contiguous GPU tensor of `dtype` (and of `shape`, on `dev`, where given)."""
     if not (isinstance(t, torch.Tensor) and t.is_cuda and t.dtype == dtype and t.is_contiguous()
-            and (shape is None or tuple(t.shape) == tuple(shape))):
+            and (shape is None or t.shape == shape)):
         raise ValueError(f"{what}: expected a contiguous {dtype} GPU tensor" +
                          (f" of shape {tuple(shape)}" if shape is not None else ""))
     if dev is not None and t.device != dev:
@@ -60,16 +71,16 @@ class PagedCache:
     def __init__(self, k: torch.Tensor, v: torch.Tensor, scale: torch.Tensor, kmean: torch.Tensor):
         if not isinstance(k, torch.Tensor) or k.dim() != 4 or not isinstance(kmean, torch.Tensor) or kmean.dim() != 4:
             raise ValueError("k and kmean: expected [layers, pages, kv_heads, ...] tensors")
-        layers, pages, kv_heads, size = k.shape
-        d = kmean.shape[-1]
-        dev = k.device
+        shape, dev = k.shape, k.device
+        layers, pages, kv_heads, size = shape
+        d = kmean.shape[3]
         _check(k, None, E4M3, None, "k")
-        _check(v, k.shape, E4M3, dev, "v")
+        _check(v, shape, E4M3, dev, "v")
         _check(scale, (layers, pages, kv_heads, 2), torch.float32, dev, "scale")
         _check(kmean, (layers, pages, kv_heads, d), torch.bfloat16, dev, "kmean")
         if d < 1 or size % d:
             raise ValueError("k: the last dimension must be page * D")
-        self.k, self.v, self.scale, self.kmean, self.device = k, v, scale, kmean, dev
+        self.k, self.v, self.scale, self.kmean, self.device, self.index = k, v, scale, kmean, dev, dev.index
         self.layers, self.pages, self.kv_heads, self.head_dim, self.page = layers, pages, kv_heads, d, size // d
         self.desc = _lib.CacheDesc(layers, pages, kv_heads, d, size // d, k.data_ptr(), v.data_ptr(),
                                    scale.data_ptr(), kmean.data_ptr())
@@ -85,16 +96,17 @@ class Batch:
         if not isinstance(table, torch.Tensor) or table.dim() != 2:
             raise ValueError("table: expected a [seqs, max_pages] tensor")
         seqs, max_pages = table.shape
+        dev = table.device
         _check(table, None, torch.int32, None, "table")
-        _check(lens, (seqs,), torch.int32, table.device, "lens")
-        _check(cu, (seqs + 1,), torch.int32, table.device, "cu")
-        self.table, self.lens, self.cu, self.device = table, lens, cu, table.device
-        self.desc = _lib.CacheBatch(seqs, max_pages, 0, int(max_new), int(max_len or 0), table.data_ptr(),
-                                    lens.data_ptr(), cu.data_ptr())
+        _check(lens, (seqs,), torch.int32, dev, "lens")
+        _check(cu, (seqs + 1,), torch.int32, dev, "cu")
+        self.table, self.lens, self.cu, self.device = table, lens, cu, dev
+        self._desc = (seqs, max_pages, int(max_new), int(max_len or 0), table.data_ptr(), lens.data_ptr(),
+                      cu.data_ptr())
 
-    def _with_rows(self, rows: int) -> _lib.CacheBatch:
-        d = self.desc
-        return _lib.CacheBatch(d.seqs, d.max_pages, rows, d.max_new, d.max_len, d.table, d.lens, d.cu)
+    def desc(self, rows: int) -> _lib.CacheBatch:
+        seqs, max_pages, new, length, table, lens, cu = self._desc
+        return _lib.CacheBatch(seqs, max_pages, rows, new, length, table, lens, cu)
 
 
 def alloc(layers: int, pages: int, kv_heads: int, head_dim: int, page: int = 64, device="cuda") -> PagedCache:
@@ -114,23 +126,26 @@ def alloc_rows(pool: PagedCache, rows: int, max_pages: int) -> Tuple[torch.Tenso
 
 
 def _packed(t, rows, heads, pool: PagedCache, dtype, what: str):
-    """Checks a packed [rows, heads, D] tensor; its (token, head) strides."""
+    """Checks a packed [rows, heads, D] tensor (rows, heads, dtype None: any); its (token, head) strides."""
     if not (isinstance(t, torch.Tensor) and t.is_cuda and t.dim() == 3 and t.dtype in _DTYPES):
         raise ValueError(f"{what}: expected a [tokens, heads, D] GPU tensor, bf16 or fp32")
     if t.device != pool.device:
         raise ValueError(f"{what}: all tensors must be on one device")
     if dtype is not None and t.dtype != dtype:
         raise ValueError(f"{what}: expected {dtype}")
-    if t.shape[2] != pool.head_dim or (heads is not None and t.shape[1] != heads) or \
-            (rows is not None and t.shape[0] != rows):
+    n, h, d = t.shape
+    if d != pool.head_dim or (heads is not None and h != heads) or (rows is not None and n != rows):
         raise ValueError(f"{what}: expected shape [{'tokens' if rows is None else rows}, "
                          f"{'heads' if heads is None else heads}, {pool.head_dim}]")
     st, sh, sc = t.stride()
-    if sc != 1 and t.numel():
+    if sc != 1 and n * h:
         raise ValueError(f"{what}: channel stride must be 1")
     # A dimension of one has no stride that matters; torch may report any.
-    return (st if t.shape[0] > 1 else t.shape[1] * max(sh, pool.head_dim) if t.shape[1] > 1 else pool.head_dim,
-            sh if t.shape[1] > 1 else pool.head_dim)
+    if h < 2:
+        sh = d
+    if n < 2:
+        st = h * sh
+    return st, sh
 
 
 def _same_device(pool: PagedCache, batch: Batch) -> None:
@@ -142,19 +157,23 @@ def append(pool: PagedCache, layer: int, batch: Batch, k: torch.Tensor, v: torch
     """Quantises the new tokens' keys and values ([tokens, kv_heads, D]) into `layer` of the cache."""
     _same_device(pool, batch)
     strides = _packed(k, None, pool.kv_heads, pool, None, "k")
-    if _packed(v, k.shape[0], pool.kv_heads, pool, k.dtype, "v") != strides:
+    rows = k.shape[0]
+    if _packed(v, rows, pool.kv_heads, pool, k.dtype, "v") != strides:
         raise ValueError("k and v must share their strides")
-    with _on(pool.device):
-        _lib.check(_L.ssba_cache_append(pool.desc, layer, batch._with_rows(k.shape[0]), _DTYPES[k.dtype], k.data_ptr(),
-                                        v.data_ptr(), *strides, _stream(pool.device)), "ssba_cache_append")
+    _call(pool, _L.ssba_cache_append, "ssba_cache_append", pool.desc, layer, batch.desc(rows), _DTYPES[k.dtype],
+          k.data_ptr(), v.data_ptr(), *strides)
 
 
 def _scratch(size: int, given, dev):
+    """(tensor to keep alive, address, bytes) of a workspace."""
     if given is not None:
         if not (isinstance(given, torch.Tensor) and given.is_cuda and given.is_contiguous() and given.device == dev):
             raise ValueError("scratch must be a contiguous GPU tensor on the cache's device")
-        return given, given.numel() * given.element_size()
-    return torch.empty(size, dtype=torch.uint8, device=dev), size
+        return given, given.data_ptr(), given.numel() * given.element_size()
+    if size == 0:
+        return None, None, 0
+    t = torch.empty(size, dtype=torch.uint8, device=dev)
+    return t, t.data_ptr(), size
 
 
 def select(pool: PagedCache, layer: int, batch: Batch, q: torch.Tensor, *, keep: int, first: int = 1, last: int = 1,
@@ -164,19 +183,18 @@ def select(pool: PagedCache, layer: int, batch: Batch, q: torch.Tensor, *, keep:
     ascending, -1 padding).  `first` leading and `last` trailing pages are always among them."""
     _same_device(pool, batch)
     qs = _packed(q, None, None, pool, None, "q")
-    rows, heads = q.shape[:2]
-    b = batch._with_rows(rows)
-    desc = _lib.CacheQuery(heads, _DTYPES[q.dtype], int(bool(causal)), keep, first, last, 0.0, *qs, 0, 0)
+    rows, heads, _ = q.shape
+    b = batch.desc(rows)
+    desc = _lib.CacheQuery(heads, _DTYPES[q.dtype], 1 if causal else 0, keep, first, last, 0.0, *qs, 0, 0)
     size = ctypes.c_size_t(0)
-    _lib.check(_L.ssba_cache_select_workspace_size(pool.desc, b, desc, ctypes.byref(size)),
-               "ssba_cache_select_workspace_size")
+    _lib.check(_L.ssba_cache_select_workspace_size(pool.desc, b, desc, size), "ssba_cache_select_workspace_size")
     if lists is None:
         lists = torch.empty((rows, pool.kv_heads, 1 + keep), dtype=torch.int32, device=pool.device)
-    _check(lists, (rows, pool.kv_heads, 1 + keep), torch.int32, pool.device, "lists")
-    scratch, have = _scratch(size.value, scratch, pool.device)
-    with _on(pool.device):
-        _lib.check(_L.ssba_cache_select(pool.desc, layer, b, desc, q.data_ptr(), lists.data_ptr(), lists.numel() * 4,
-                                        scratch.data_ptr(), have, _stream(pool.device)), "ssba_cache_select")
+    else:
+        _check(lists, (rows, pool.kv_heads, 1 + keep), torch.int32, pool.device, "lists")
+    alive, at, have = _scratch(size.value, scratch, pool.device)
+    _call(pool, _L.ssba_cache_select, "ssba_cache_select", pool.desc, layer, b, desc, q.data_ptr(), lists.data_ptr(),
+          lists.numel() * 4, at, have)
     return lists
 
 
@@ -187,26 +205,28 @@ def attend(pool: PagedCache, layer: int, batch: Batch, q: torch.Tensor, *, lists
     that `lists` (of select) names.  Rows of no sequence are left as they are in `out`."""
     _same_device(pool, batch)
     qs = _packed(q, None, None, pool, None, "q")
-    rows, heads = q.shape[:2]
+    rows, heads, d = q.shape
     if out is None:
-        out = torch.empty((rows, heads, pool.head_dim), dtype=q.dtype, device=q.device)
-    os = _packed(out, rows, heads, pool, q.dtype, "out")
+        out = torch.empty((rows, heads, d), dtype=q.dtype, device=pool.device)
+        os = (heads * d, d)
+    else:
+        os = _packed(out, rows, heads, pool, q.dtype, "out")
     keep, lp, lb = 0, None, 0
     if lists is not None:
         if not (isinstance(lists, torch.Tensor) and lists.dim() == 3 and lists.shape[2] > 1):
             raise ValueError("lists: expected [tokens, kv_heads, 1 + keep]")
-        _check(lists, (rows, pool.kv_heads, lists.shape[2]), torch.int32, pool.device, "lists")
-        keep, lp, lb = lists.shape[2] - 1, lists.data_ptr(), lists.numel() * 4
-    b = batch._with_rows(rows)
-    desc = _lib.CacheQuery(heads, _DTYPES[q.dtype], int(bool(causal)), keep, 0, 0,
+        keep = lists.shape[2] - 1
+        _check(lists, (rows, pool.kv_heads, 1 + keep), torch.int32, pool.device, "lists")
+        lp, lb = lists.data_ptr(), lists.numel() * 4
+    b = batch.desc(rows)
+    desc = _lib.CacheQuery(heads, _DTYPES[q.dtype], 1 if causal else 0, keep, 0, 0,
                            0.0 if scale is None else float(scale), *qs, *os)
     size = ctypes.c_size_t(0)
-    _lib.check(_L.ssba_cache_attend_workspace_size(pool.desc, b, desc, int(lists is not None), ctypes.byref(size)),
+    _lib.check(_L.ssba_cache_attend_workspace_size(pool.desc, b, desc, 0 if lists is None else 1, size),
                "ssba_cache_attend_workspace_size")
-    scratch, have = _scratch(size.value, scratch, pool.device)
-    with _on(pool.device):
-        _lib.check(_L.ssba_cache_attend(pool.desc, layer, b, desc, q.data_ptr(), lp, lb, out.data_ptr(),
-                                        scratch.data_ptr(), have, _stream(pool.device)), "ssba_cache_attend")
+    alive, at, have = _scratch(size.value, scratch, pool.device)
+    _call(pool, _L.ssba_cache_attend, "ssba_cache_attend", pool.desc, layer, b, desc, q.data_ptr(), lp, lb,
+          out.data_ptr(), at, have)
     return out
 
 
@@ -221,7 +241,7 @@ def _rows(pool: PagedCache, table, lens, refs) -> _lib.CachePages:
 
 def _pages_scratch(pool: PagedCache, desc, n: int, given):
     size = ctypes.c_size_t(0)
-    _lib.check(_L.ssba_pages_workspace_size(pool.desc, desc, n, ctypes.byref(size)), "ssba_pages_workspace_size")
+    _lib.check(_L.ssba_pages_workspace_size(pool.desc, desc, n, size), "ssba_pages_workspace_size")
     return _scratch(size.value, given, pool.device)
 
 
@@ -232,11 +252,12 @@ def _info(pool: PagedCache, given) -> torch.Tensor:
     return given
 
 
-def _numbers(pool: PagedCache, t, n, what: str) -> torch.Tensor:
+def _numbers(pool: PagedCache, t, n, what: str) -> int:
+    """Checks a vector of row or page numbers (of length n, if given); its length."""
     _check(t, None, torch.int32, pool.device, what)
     if t.dim() != 1 or (n is not None and t.shape[0] != n):
         raise ValueError(f"{what}: expected a vector" + (f" of {n}" if n is not None else ""))
-    return t
+    return t.shape[0]
 
 
 def reserve(pool: PagedCache, table, lens, refs, info=None, scratch=None) -> torch.Tensor:
@@ -244,10 +265,8 @@ def reserve(pool: PagedCache, table, lens, refs, info=None, scratch=None) -> tor
     info = {entries served, entries left without a page}."""
     desc = _rows(pool, table, lens, refs)
     info = _info(pool, info)
-    scratch, have = _pages_scratch(pool, desc, 0, scratch)
-    with _on(pool.device):
-        _lib.check(_L.ssba_pages_reserve(pool.desc, desc, info.data_ptr(), scratch.data_ptr(), have,
-                                         _stream(pool.device)), "ssba_pages_reserve")
+    alive, at, have = _pages_scratch(pool, desc, 0, scratch)
+    _call(pool, _L.ssba_pages_reserve, "ssba_pages_reserve", pool.desc, desc, info.data_ptr(), at, have)
     return info
 
 
@@ -255,46 +274,43 @@ def fork(pool: PagedCache, table, lens, refs, src, dst, info=None, scratch=None)
     """Row dst[j] becomes a copy of row src[j]: complete pages shared, an incomplete last one copied.  Updates
     table, lens and refs; returns info = {pairs forked, of them cut for lack of a page}."""
     desc = _rows(pool, table, lens, refs)
-    n = _numbers(pool, src, None, "src").shape[0]
+    n = _numbers(pool, src, None, "src")
     _numbers(pool, dst, n, "dst")
     info = _info(pool, info)
-    scratch, have = _pages_scratch(pool, desc, n, scratch)
-    with _on(pool.device):
-        _lib.check(_L.ssba_pages_fork(pool.desc, desc, n, src.data_ptr(), dst.data_ptr(), info.data_ptr(),
-                                      scratch.data_ptr(), have, _stream(pool.device)), "ssba_pages_fork")
+    alive, at, have = _pages_scratch(pool, desc, n, scratch)
+    _call(pool, _L.ssba_pages_fork, "ssba_pages_fork", pool.desc, desc, n, src.data_ptr(), dst.data_ptr(),
+          info.data_ptr(), at, have)
     return info
 
 
 def release(pool: PagedCache, table, lens, refs, rows, info=None, scratch=None) -> torch.Tensor:
     """Empties rows.  Updates table, lens and refs; returns info = {entries released, pages that became free}."""
     desc = _rows(pool, table, lens, refs)
-    n = _numbers(pool, rows, None, "rows").shape[0]
+    n = _numbers(pool, rows, None, "rows")
     info = _info(pool, info)
-    scratch, have = _pages_scratch(pool, desc, n, scratch)
-    with _on(pool.device):
-        _lib.check(_L.ssba_pages_release(pool.desc, desc, n, rows.data_ptr(), info.data_ptr(), scratch.data_ptr(),
-                                         have, _stream(pool.device)), "ssba_pages_release")
+    alive, at, have = _pages_scratch(pool, desc, n, scratch)
+    _call(pool, _L.ssba_pages_release, "ssba_pages_release", pool.desc, desc, n, rows.data_ptr(), info.data_ptr(), at,
+          have)
     return info
 
 
 def compact(pool: PagedCache, table, refs, table_out=None, refs_out=None, info=None, scratch=None):
     """Moves the pages in use to the low end of the pool.  Returns (table, refs, info) after it, info = {pages in
     use, pages moved}; table_out and refs_out may be table and refs themselves."""
-    table_out = torch.empty_like(table) if table_out is None else table_out
-    refs_out = torch.empty_like(refs) if refs_out is None else refs_out
-    info = _info(pool, info)
+    # lens takes no part: its place is filled by another array
     if not isinstance(table, torch.Tensor) or table.dim() != 2:
         raise ValueError("table: expected a [rows, max_pages] tensor")
     _check(table, None, torch.int32, pool.device, "table")
     _check(refs, (pool.pages,), torch.int32, pool.device, "refs")
+    desc = _lib.CachePages(table.shape[0], table.shape[1], table.data_ptr(), refs.data_ptr(), refs.data_ptr())
+    table_out = torch.empty_like(table) if table_out is None else table_out
+    refs_out = torch.empty_like(refs) if refs_out is None else refs_out
     _check(table_out, table.shape, torch.int32, pool.device, "table_out")
     _check(refs_out, refs.shape, torch.int32, pool.device, "refs_out")
-    # lens takes no part; any array stands in its place
-    desc = _lib.CachePages(table.shape[0], table.shape[1], table.data_ptr(), refs.data_ptr(), refs.data_ptr())
-    scratch, have = _pages_scratch(pool, desc, 0, scratch)
-    with _on(pool.device):
-        _lib.check(_L.ssba_pages_compact(pool.desc, desc, table_out.data_ptr(), refs_out.data_ptr(), info.data_ptr(),
-                                         scratch.data_ptr(), have, _stream(pool.device)), "ssba_pages_compact")
+    info = _info(pool, info)
+    alive, at, have = _pages_scratch(pool, desc, 0, scratch)
+    _call(pool, _L.ssba_pages_compact, "ssba_pages_compact", pool.desc, desc, table_out.data_ptr(),
+          refs_out.data_ptr(), info.data_ptr(), at, have)
     return table_out, refs_out, info
 
 
@@ -303,8 +319,6 @@ def copy_pages(pool: PagedCache, src, dst, to: Optional[PagedCache] = None) -> N
     to = pool if to is None else to
     if to.device != pool.device:
         raise ValueError("both caches must be on one device")
-    n = _numbers(pool, src, None, "src").shape[0]
+    n = _numbers(pool, src, None, "src")
     _numbers(pool, dst, n, "dst")
-    with _on(pool.device):
-        _lib.check(_L.ssba_pages_copy(pool.desc, to.desc, n, src.data_ptr(), dst.data_ptr(), _stream(pool.device)),
-                   "ssba_pages_copy")
+    _call(pool, _L.ssba_pages_copy, "ssba_pages_copy", pool.desc, to.desc, n, src.data_ptr(), dst.data_ptr())

@@ -82,7 +82,8 @@ struct AttendArgs {
   void* o;
   int64_t q_st, q_sh, o_st, o_sh;
   const int32_t* lists;   // [rows][kv_heads][1 + keep] or null
-  float* part;            // partial results of split items
+  float* part;            // parts of split items: O [item][split][columns][D]
+  float* part_ml;         // and their maximum and sum [item][split][columns][2]
   float scale_log2;
   int group, causal, keep;
   int col_tiles;          // column tiles of an item
@@ -90,12 +91,17 @@ struct AttendArgs {
 };
 
 // What the attention launch does (ssba_cache_api.cpp decides).
+enum AttendKind {
+  kAttendFew,    // a workgroup per 16 R columns, its waves share the keys
+  kAttendMany,   // column groups of 64 (fp32: 16)
+  kAttendRow,    // lists: a workgroup per row and kv head, its waves share the keys
+  kAttendRows,   // lists: a wave per row and kv head
+};
 struct AttendPlan {
-  int tiles16;      // R: column tiles of 16 per wave
-  bool listed;
-  bool by_columns;  // the waves of a workgroup take different columns (else different keys)
+  AttendKind kind;
+  int tiles16;            // R: column tiles of 16 per wave
   int col_tiles, splits;
-  int64_t items;    // (sequence or row, kv head, column tile)
+  int64_t items;          // workgroups without the splits
 };
 
 hipError_t launch_cache_append(const AppendArgs& a, int dtype, hipStream_t s);

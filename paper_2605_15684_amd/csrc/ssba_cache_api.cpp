@@ -137,34 +137,35 @@ int select_chunks(const ssba_cache* c, const ssba_cache_batch* b) {
 AttendPlan plan(const ssba_cache* c, const ssba_cache_batch* b, const ssba_cache_query* q, bool listed) {
   AttendPlan p;
   const int64_t group = q->heads / c->kv_heads;
-  const int64_t cols = listed ? group : group * b->max_new;
-  p.listed = listed;
-  p.splits = 1;
+  const int64_t cols = std::max<int64_t>(1, listed ? group : group * b->max_new);
   const bool f32 = q->dtype == SSBA_DT_F32;
   const int64_t keys = listed ? std::min<int64_t>((int64_t)q->keep * c->page, long_of(c, b)) : long_of(c, b);
+  p.splits = p.tiles16 = 1;
   if (listed) {
-    p.tiles16 = 1;
     p.col_tiles = (int)ceil_div(cols, 16);
     const int64_t items = (int64_t)b->rows * c->kv_heads * p.col_tiles;
-    p.by_columns = items >= 4096;
-    p.items = p.by_columns ? ceil_div(b->rows, 4) * c->kv_heads * p.col_tiles : items;
+    p.kind = items >= 4096 ? ssba::kAttendRows : ssba::kAttendRow;
+    p.items = p.kind == ssba::kAttendRows ? ceil_div(b->rows, 4) * c->kv_heads * p.col_tiles : items;
   } else {
-    p.by_columns = cols > 64;
-    p.tiles16 = f32 ? 1 : p.by_columns ? 4 : cols <= 16 ? 1 : cols <= 32 ? 2 : 4;
-    p.col_tiles = (int)ceil_div(std::max<int64_t>(cols, 1), (p.by_columns ? 64 : 16) * p.tiles16);
+    p.kind = cols > 64 ? ssba::kAttendMany : ssba::kAttendFew;
+    const bool many = p.kind == ssba::kAttendMany;
+    if (!f32) p.tiles16 = many ? 4 : cols <= 16 ? 1 : 2;
+    p.col_tiles = (int)ceil_div(cols, (many ? 64 : 16) * p.tiles16);
     p.items = (int64_t)b->seqs * c->kv_heads * p.col_tiles;
   }
-  if (!p.by_columns) {
+  if (p.kind == ssba::kAttendRow || p.kind == ssba::kAttendFew) {
     // 4 waves of at least 2 steps of 32 keys each, up to about 1024 workgroups.
-    const int64_t most = std::max<int64_t>(1, keys / 256);
+    const int64_t most = std::max<int64_t>(1, std::min<int64_t>(256, keys / 256));
     p.splits = (int)std::max<int64_t>(1, std::min<int64_t>(most, ceil_div(1024, std::max<int64_t>(p.items, 1))));
   }
   return p;
 }
 
+// Columns of every part of a split launch.
+size_t part_columns(const AttendPlan& p) { return p.splits == 1 ? 0 : (size_t)p.items * p.splits * p.tiles16 * 16; }
+
 size_t attend_scratch(const ssba_cache* c, const AttendPlan& p) {
-  if (p.splits == 1) return 0;
-  return (size_t)p.items * p.splits * p.tiles16 * 16 * (c->head_dim + 2) * sizeof(float);
+  return part_columns(p) * (c->head_dim + 2) * sizeof(float);
 }
 
 bool too_many(int64_t groups) { return groups > ssba::kMaxGroups256; }
@@ -275,13 +276,14 @@ ssba_status ssba_cache_attend(const ssba_cache* c, int32_t layer, const ssba_cac
   if (need && (!scratch || !aligned(scratch, 16))) return SSBA_ERR_ARG;
   if (scratch_bytes < need || (lists && lists_bytes < (size_t)4 * b->rows * c->kv_heads * (1 + (size_t)q->keep)))
     return SSBA_ERR_WORKSPACE;
-  if (too_many(p.items * p.splits) || too_many(p.items * p.tiles16)) return SSBA_ERR_UNSUPPORTED;
+  if (too_many(p.items * p.splits * 2) || too_many(p.items * p.tiles16 * 4)) return SSBA_ERR_UNSUPPORTED;
   a.c = view(c, layer);
   a.b = view(b);
   a.q = query;
   a.o = o;
   a.lists = lists;
   a.part = static_cast<float*>(scratch);
+  a.part_ml = need ? a.part + part_columns(p) * c->head_dim : nullptr;
   const float scale = q->softmax_scale > 0.f ? q->softmax_scale : 1.0f / std::sqrt((float)c->head_dim);
   a.scale_log2 = scale * 1.4426950408889634f;
   a.group = q->heads / c->kv_heads;

@@ -64,113 +64,156 @@ __device__ __forceinline__ void split_bf16(float x, __bf16 (&t)[NS]) {
   }
 }
 
-// NS: bf16 terms of a query value and of a probability (1: bf16 tensors, 3: fp32).
-template <int D, int R, int NS, bool LISTED, bool BY_COLUMNS>
-__global__ __launch_bounds__(256, R == 1 ? 3 : 2) void k_cache_attend(AttendArgs a) {
-  constexpr int NH = D / 64;   // 64-channel blocks
-  constexpr int NC = D / 16;   // 16-channel tiles of O
-  constexpr int COLS = 16 * R;
+// What a variant is made of.  A workgroup has CG * KP waves: CG column groups,
+// each of whose keys KP waves share.  NQ, NP: bf16 terms of a query value and
+// of a probability.  QLDS: the queries stay in the LDS, not in registers.
+template <int D_, int R_, int NQ_, int NP_, bool F32_, bool LISTED_, int CG_, int KP_, bool QLDS_>
+struct Shape {
+  static constexpr int D = D_, R = R_, NQ = NQ_, NP = NP_, CG = CG_, KP = KP_;
+  static constexpr bool F32 = F32_, LISTED = LISTED_, QLDS = QLDS_;
+  static constexpr int THREADS = 64 * CG * KP;
+  static constexpr int NH = D / 64;   // 64-channel blocks
+  static constexpr int NC = D / 16;   // 16-channel tiles of O
+  static constexpr int COLS = 16 * R; // columns of a wave
+};
+
+// Writes E consecutive channels of an output row.
+template <bool F32, int E>
+__device__ __forceinline__ void store_row(void* o, int64_t at, const float* x) {
+  if (F32) {
+    typedef float f4a4 __attribute__((ext_vector_type(4), aligned(4)));
+#pragma unroll
+    for (int e = 0; e < E; e += 4)
+      *reinterpret_cast<f4a4*>(static_cast<float*>(o) + at + e) = f4a4{x[e], x[e + 1], x[e + 2], x[e + 3]};
+  } else {
+    typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
+#pragma unroll
+    for (int e = 0; e < E; e += 4)
+      *reinterpret_cast<bf16x4*>(static_cast<__bf16*>(o) + at + e) =
+          bf16x4{(__bf16)x[e], (__bf16)x[e + 1], (__bf16)x[e + 2], (__bf16)x[e + 3]};
+  }
+}
+
+// Which item a workgroup (or a part to be joined) belongs to.
+struct Item {
+  int seq, h, cbase, ncols, tok0;   // cbase: first column of the workgroup; tok0: token of column 0
+  SeqView sv;
+};
+
+// unit: sequence, or packed row (LISTED).  False: no such row.
+template <bool LISTED>
+__device__ __forceinline__ bool item_of(const AttendArgs& a, int unit, int lane, Item* it) {
+  it->seq = unit;
+  if (LISTED) {
+    it->seq = unit < a.b.rows ? seq_of_row(a.b, unit, lane) : a.b.seqs;
+    if (it->seq >= a.b.seqs) return false;
+  }
+  it->sv = seq_view(a.b, a.c.page_log2, it->seq);
+  it->tok0 = LISTED ? unit - it->sv.begin : 0;
+  if (LISTED && (it->tok0 < 0 || it->tok0 >= it->sv.n)) return false;
+  it->ncols = LISTED ? a.group : min(it->sv.n, a.b.max_new) * a.group;
+  return true;
+}
+
+// Element offset of channel 0 of a column's row in Q or O.
+template <bool LISTED>
+__device__ __forceinline__ int64_t row_at(const AttendArgs& a, const Item& it, int col, int64_t st, int64_t sh) {
+  const int t = LISTED ? 0 : col / a.group;
+  return (int64_t)(it.sv.begin + it.tok0 + t) * st + (int64_t)(it.h * a.group + col - t * a.group) * sh;
+}
+
+template <typename P>
+__global__ __launch_bounds__(P::THREADS, P::R == 1 ? 3 : 2) void k_cache_attend(AttendArgs a) {
+  constexpr int D = P::D, R = P::R, NQ = P::NQ, NP = P::NP, NH = P::NH, NC = P::NC;
   const int lane = threadIdx.x & 63, n16 = lane & 15, g = lane >> 4;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int cg = wave % P::CG, kp = wave / P::CG;
   const int page_log2 = a.c.page_log2;
   const int gpp_log2 = page_log2 - 4;   // groups per page
 
-  // Which keys and columns.
+  // Which keys and columns.  Consecutive items run on one XCD, so that the
+  // column tiles of a head read its keys from one L2.
   unsigned id = blockIdx.x;
-  int split = 0;
-  if (!BY_COLUMNS) {
-    split = id % a.splits;
-    id /= a.splits;
+  if (P::QLDS) {
+    const unsigned per = gridDim.x / 8, rest = gridDim.x % 8, x = id % 8;
+    id = x * per + min(x, rest) + id / 8;
   }
+  const int split = id % a.splits;
+  id /= a.splits;
   const int ct = id % a.col_tiles;
   id /= a.col_tiles;
-  const int h = id % a.c.kv_heads;
+  Item it;
+  it.h = id % a.c.kv_heads;
   const int unit = id / a.c.kv_heads;
-  int seq, row0 = 0;
-  if (LISTED) {
-    row0 = BY_COLUMNS ? unit * 4 + wave : unit;
-    seq = row0 < a.b.rows ? seq_of_row(a.b, row0, lane) : a.b.seqs;
-    if (seq >= a.b.seqs) return;
-  } else {
-    seq = unit;
-  }
-  const SeqView sv = seq_view(a.b, page_log2, seq);
-  int cbase, ncols, tok0;   // first column, columns, first token
-  if (LISTED) {
-    tok0 = row0 - sv.begin;
-    if (tok0 < 0 || tok0 >= sv.n) return;
-    cbase = ct * COLS;
-    ncols = a.group;
-  } else {
-    tok0 = 0;
-    cbase = (BY_COLUMNS ? ct * 4 + wave : ct) * COLS;
-    ncols = min(sv.n, a.b.max_new) * a.group;
-  }
-  // Waves that share keys stay together for the merge; cbase is the workgroup's then.
-  if (cbase >= ncols) return;
-  const int cend = min(cbase + COLS, ncols) - 1;
-  const int before = sv.len - sv.n;   // tokens in front of the new ones
-  auto limit = [&](int tok) { return a.causal ? min(max(before + tok + 1, 0), sv.len) : sv.len; };
-  const int minlim = limit(tok0 + (LISTED ? 0 : cbase / a.group));
-  const int maxlim = limit(tok0 + (LISTED ? 0 : cend / a.group));
+  // LISTED with several column groups: they are rows.
+  const bool there = item_of<P::LISTED>(a, P::LISTED ? unit * P::CG + cg : unit, lane, &it);
+  if (!there && (P::KP == 1 || P::CG == 1)) return;
+  const int cbase = (P::LISTED ? ct : ct * P::CG + cg) * P::COLS;
+  if ((P::CG == 1 || P::KP == 1) && cbase >= it.ncols) return;
+  if (P::CG > 1 && P::KP > 1 && ct * P::CG * P::COLS >= it.ncols) return;   // the whole workgroup
+  const int cend = min(cbase + P::COLS, it.ncols) - 1;   // < cbase: no columns
+  const int before = it.sv.len - it.sv.n;                // tokens in front of the new ones
+  auto limit = [&](int tok) { return a.causal ? min(max(before + tok + 1, 0), it.sv.len) : it.sv.len; };
+  const int minlim = limit(it.tok0 + (P::LISTED ? 0 : cbase / a.group));
+  const int maxlim = cend < cbase ? 0 : limit(it.tok0 + (P::LISTED ? 0 : cend / a.group));
 
   // This lane's columns.
   int lim[R];
-  int64_t orow[R];
-  Frag q[R][NS][NH * 2];
+  constexpr int QREGS = P::QLDS ? 1 : R;
+  Frag q[QREGS][NQ][NH * 2];
+  __shared__ u32x4 s_q[P::QLDS ? P::CG * R * NH * 2 * 64 : 1];
 #pragma unroll
   for (int r = 0; r < R; ++r) {
     const int col = cbase + r * 16 + n16;
-    const bool there = col <= cend;
-    const int tok = tok0 + (LISTED ? 0 : col / a.group);
-    const int head = h * a.group + (LISTED ? col : col % a.group);
-    lim[r] = there ? limit(tok) : 0;
-    orow[r] = there ? (int64_t)(sv.begin + tok) * a.o_st + (int64_t)head * a.o_sh : -1;
-    const int64_t qo = (int64_t)(sv.begin + tok) * a.q_st + (int64_t)head * a.q_sh;
+    const bool in = col <= cend;
+    lim[r] = in ? limit(it.tok0 + (P::LISTED ? 0 : col / a.group)) : 0;
+    if (P::QLDS && kp != r % P::KP) continue;   // the waves that share columns share the loading
+    const int64_t qo = in ? row_at<P::LISTED>(a, it, col, a.q_st, a.q_sh) : 0;
 #pragma unroll
     for (int x = 0; x < NH * 2; ++x) {
       const int ch = (x >> 1) * 64 + g * 16 + (x & 1) * 8;
-      if (NS == 1) {
+      if (!P::F32) {
         u32x4 w = {0, 0, 0, 0};
-        if (there) w = *reinterpret_cast<const u32x4*>(static_cast<const uint16_t*>(a.q) + qo + ch);
+        if (in) w = *reinterpret_cast<const u32x4*>(static_cast<const uint16_t*>(a.q) + qo + ch);
+        if (P::QLDS) {
+          s_q[((cg * R + r) * NH * 2 + x) * 64 + lane] = w;
+        } else {
 #pragma unroll
-        for (int e = 0; e < 4; ++e) q[r][0][x].u[e] = w[e];
+          for (int e = 0; e < 4; ++e) q[r % QREGS][0][x].u[e] = w[e];
+        }
       } else {
 #pragma unroll
         for (int half = 0; half < 2; ++half) {
           u32x4 w = {0, 0, 0, 0};
-          if (there) w = *reinterpret_cast<const u32x4a4*>(static_cast<const float*>(a.q) + qo + ch + half * 4);
+          if (in) w = *reinterpret_cast<const u32x4a4*>(static_cast<const float*>(a.q) + qo + ch + half * 4);
 #pragma unroll
           for (int e = 0; e < 4; ++e) {
-            __bf16 t[NS];
-            split_bf16<NS>(__uint_as_float(w[e]), t);
+            __bf16 t[NQ];
+            split_bf16<NQ>(__uint_as_float(w[e]), t);
 #pragma unroll
-            for (int s = 0; s < NS; ++s) q[r][s][x].v[half * 4 + e] = t[s];
+            for (int s = 0; s < NQ; ++s) q[r % QREGS][s][x].v[half * 4 + e] = t[s];
           }
         }
       }
     }
   }
+  if (P::QLDS) __syncthreads();
 
   // Groups of 16 keys, and this wave's steps of two groups.
   const int32_t* list = nullptr;
   int groups;
-  if (LISTED) {
-    list = a.lists + ((int64_t)row0 * a.c.kv_heads + h) * (1 + a.keep);
+  if (P::LISTED) {
+    list = a.lists + ((int64_t)(it.sv.begin + it.tok0) * a.c.kv_heads + it.h) * (1 + a.keep);
     groups = min(max(list[0], 0), a.keep) << gpp_log2;
   } else {
     groups = (maxlim + 15) >> 4;
   }
   const int steps = (groups + 1) >> 1;
-  int s0 = 0, s1 = steps;
-  if (!BY_COLUMNS) {
-    const int parts = a.splits * 4, part = split * 4 + wave;
-    s0 = (int)((int64_t)steps * part / parts);
-    s1 = (int)((int64_t)steps * (part + 1) / parts);
-  }
+  const int parts = a.splits * P::KP, part = split * P::KP + kp;
+  const int s0 = (int)((int64_t)steps * part / parts), s1 = (int)((int64_t)steps * (part + 1) / parts);
 
-  const int32_t* table = a.b.table + (int64_t)seq * a.b.max_pages;
-  const int64_t head_off = ((int64_t)h << page_log2) * D;
+  const int32_t* table = a.b.table + (int64_t)it.seq * a.b.max_pages;
+  const int64_t head_off = ((int64_t)it.h << page_log2) * D;
   int m_page = 0, m_key = 0;    // of group chunk * 64 + lane: page (-1: none) and first token
   float m_ks = 1.f, m_vs = 1.f;
   auto load_chunk = [&](int chunk) {
@@ -179,14 +222,14 @@ __global__ __launch_bounds__(256, R == 1 ? 3 : 2) void k_cache_attend(AttendArgs
     float ks = 1.f, vs = 1.f;
     if (gr < groups) {
       const int at = gr >> gpp_log2;
-      const int lp = LISTED ? list[1 + at] : at;
+      const int lp = P::LISTED ? list[1 + at] : at;
       if (lp >= 0 && lp < a.b.max_pages) {
         const int k0 = (lp << page_log2) + ((gr & ((1 << gpp_log2) - 1)) << 4);
         const int p = k0 < maxlim ? table[lp] : -1;
         if (p >= 0 && p < a.c.pages) {
           page = p;
           key = k0;
-          const float* sc = a.c.scale + ((int64_t)p * a.c.kv_heads + h) * 2;
+          const float* sc = a.c.scale + ((int64_t)p * a.c.kv_heads + it.h) * 2;
           ks = sc[0];
           vs = sc[1];
         }
@@ -194,16 +237,23 @@ __global__ __launch_bounds__(256, R == 1 ? 3 : 2) void k_cache_attend(AttendArgs
     }
     m_page = page;
     m_key = key;
-    m_ks = ks;
+    m_ks = ks * a.scale_log2;
     m_vs = vs;
   };
+  int chunk = -1;   // 32 steps a chunk
 
   struct Step {
     u32x4 k[2][NH], v[2][NH];
     int key[2];
     float ks[2], vs[2];
+    int64_t off[2];
   };
-  auto fetch = [&](int s, Step& x) {
+  // The group numbers, scales and K codes of step s, then its V codes.
+  auto fetch_k = [&](int s, Step& x) {
+    if ((s >> 5) != chunk) {
+      chunk = s >> 5;
+      load_chunk(chunk);
+    }
 #pragma unroll
     for (int t = 0; t < 2; ++t) {
       const int l = (2 * s + t) & 63;
@@ -212,14 +262,18 @@ __global__ __launch_bounds__(256, R == 1 ? 3 : 2) void k_cache_attend(AttendArgs
       x.ks[t] = lane_f(m_ks, l);
       x.vs[t] = lane_f(m_vs, l);
       const int sub = ((2 * s + t) & ((1 << gpp_log2) - 1)) * 16 * D;
-      const int64_t off = (int64_t)max(page, 0) * a.c.page_bytes + head_off + sub;
-      const uint8_t* kp = a.c.k + off + lane * 16;
-      const uint8_t* vp = a.c.v + off + lane * 16;
+      x.off[t] = (int64_t)max(page, 0) * a.c.page_bytes + head_off + sub;
+      const uint8_t* kp_ = a.c.k + x.off[t];
 #pragma unroll
-      for (int hh = 0; hh < NH; ++hh) {
-        x.k[t][hh] = *reinterpret_cast<const u32x4*>(kp + hh * 1024);
-        x.v[t][hh] = *reinterpret_cast<const u32x4*>(vp + hh * 1024);
-      }
+      for (int hh = 0; hh < NH; ++hh) x.k[t][hh] = *reinterpret_cast<const u32x4*>(kp_ + lane * 16 + hh * 1024);
+    }
+  };
+  auto fetch_v = [&](Step& x) {
+#pragma unroll
+    for (int t = 0; t < 2; ++t) {
+      const uint8_t* vp = a.c.v + x.off[t];
+#pragma unroll
+      for (int hh = 0; hh < NH; ++hh) x.v[t][hh] = *reinterpret_cast<const u32x4*>(vp + lane * 16 + hh * 1024);
     }
   };
 
@@ -233,36 +287,50 @@ __global__ __launch_bounds__(256, R == 1 ? 3 : 2) void k_cache_attend(AttendArgs
     for (int c = 0; c < NC; ++c) o[r][c] = {0.f, 0.f, 0.f, 0.f};
   }
 
-  auto compute = [&](Step& x) {
-    floatx4 s[2][R];
+  floatx4 s[2][R];
+  auto scores = [&](const Step& x) {
+    // The queries are read from the LDS again each step: hidden from the
+    // compiler, which would otherwise keep them in registers and spill.
+    int q_at = cg * R * NH * 2 * 64 + lane;
+    if (P::QLDS) asm volatile("" : "+v"(q_at));
 #pragma unroll
-    for (int t = 0; t < 2; ++t) {
+    for (int t = 0; t < 2; ++t)
 #pragma unroll
       for (int r = 0; r < R; ++r) s[t][r] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-      for (int hh = 0; hh < NH; ++hh)
+    for (int hh = 0; hh < NH; ++hh)
 #pragma unroll
-        for (int u = 0; u < 2; ++u) {
-          Frag k;
-          k.p[0] = codes_lo(x.k[t][hh][2 * u]);
-          k.p[1] = codes_hi(x.k[t][hh][2 * u]);
-          k.p[2] = codes_lo(x.k[t][hh][2 * u + 1]);
-          k.p[3] = codes_hi(x.k[t][hh][2 * u + 1]);
+      for (int u = 0; u < 2; ++u) {
+        Frag k[2];
 #pragma unroll
-          for (int ns = NS - 1; ns >= 0; --ns)
-#pragma unroll
-            for (int r = 0; r < R; ++r)
-              s[t][r] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k.v, q[r][ns][hh * 2 + u].v, s[t][r], 0, 0, 0);
+        for (int t = 0; t < 2; ++t) {
+          k[t].p[0] = codes_lo(x.k[t][hh][2 * u]);
+          k[t].p[1] = codes_hi(x.k[t][hh][2 * u]);
+          k[t].p[2] = codes_lo(x.k[t][hh][2 * u + 1]);
+          k[t].p[3] = codes_hi(x.k[t][hh][2 * u + 1]);
         }
-    }
+#pragma unroll
+        for (int ns = NQ - 1; ns >= 0; --ns)
+#pragma unroll
+          for (int r = 0; r < R; ++r) {
+            Frag b;
+            if (P::QLDS) {
+              const u32x4 w = s_q[q_at + (r * NH * 2 + hh * 2 + u) * 64];
+#pragma unroll
+              for (int e = 0; e < 4; ++e) b.u[e] = w[e];
+            } else {
+              b = q[r % QREGS][ns][hh * 2 + u];
+            }
+#pragma unroll
+            for (int t = 0; t < 2; ++t)
+              s[t][r] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k[t].v, b.v, s[t][r], 0, 0, 0);
+          }
+      }
+  };
+
+  auto finish = [&](Step& x) {
     // Some column does not see some key of this step.
     const bool edge = max(x.key[0], x.key[1]) + 16 > minlim;
-#pragma unroll
-    for (int t = 0; t < 2; ++t) {
-      const float c = x.ks[t] * a.scale_log2;
-#pragma unroll
-      for (int r = 0; r < R; ++r) s[t][r] *= c;
-    }
     if (edge) {
 #pragma unroll
       for (int t = 0; t < 2; ++t)
@@ -270,17 +338,19 @@ __global__ __launch_bounds__(256, R == 1 ? 3 : 2) void k_cache_attend(AttendArgs
         for (int r = 0; r < R; ++r)
 #pragma unroll
           for (int i = 0; i < 4; ++i)
-            if (x.key[t] + 4 * g + i >= lim[r]) s[t][r][i] = -INFINITY;
+            s[t][r][i] = x.key[t] + 4 * g + i < lim[r] ? s[t][r][i] * x.ks[t] : -INFINITY;
+      x.ks[0] = x.ks[1] = 1.f;
     }
     bool raise = false;
     float top[R];
 #pragma unroll
     for (int r = 0; r < R; ++r) {
-      top[r] = s[0][r][0];
+      float u[2];
 #pragma unroll
-      for (int t = 0; t < 2; ++t)
-#pragma unroll
-        for (int i = 0; i < 4; ++i) top[r] = fmaxf(top[r], s[t][r][i]);
+      for (int t = 0; t < 2; ++t) {
+        u[t] = fmaxf(fmaxf(s[t][r][0], s[t][r][1]), fmaxf(s[t][r][2], s[t][r][3])) * x.ks[t];
+      }
+      top[r] = fmaxf(u[0], u[1]);
       raise |= top[r] > m[r] + kSlack;
     }
     if (__builtin_amdgcn_ballot_w64(raise)) {
@@ -296,7 +366,7 @@ __global__ __launch_bounds__(256, R == 1 ? 3 : 2) void k_cache_attend(AttendArgs
         for (int c = 0; c < NC; ++c) o[r][c] *= f;
       }
     }
-    Frag p[R][NS];
+    Frag p[R][NP];
 #pragma unroll
     for (int r = 0; r < R; ++r) {
       const float mu = m[r] == -INFINITY ? 0.f : m[r];
@@ -304,12 +374,12 @@ __global__ __launch_bounds__(256, R == 1 ? 3 : 2) void k_cache_attend(AttendArgs
       for (int t = 0; t < 2; ++t)
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-          const float e = exp2_(s[t][r][i] - mu);
+          const float e = exp2_(__builtin_fmaf(s[t][r][i], x.ks[t], -mu));
           l[r] += e;
-          __bf16 terms[NS];
-          split_bf16<NS>(e * x.vs[t], terms);
+          __bf16 terms[NP];
+          split_bf16<NP>(e * x.vs[t], terms);
 #pragma unroll
-          for (int ns = 0; ns < NS; ++ns) p[r][ns].v[t * 4 + i] = terms[ns];
+          for (int ns = 0; ns < NP; ++ns) p[r][ns].v[t * 4 + i] = terms[ns];
         }
     }
     if (edge) {
@@ -373,7 +443,7 @@ __global__ __launch_bounds__(256, R == 1 ? 3 : 2) void k_cache_attend(AttendArgs
         v.p[2] = codes_lo(x.v[1][hh][e]);
         v.p[3] = codes_hi(x.v[1][hh][e]);
 #pragma unroll
-        for (int ns = NS - 1; ns >= 0; --ns)
+        for (int ns = NP - 1; ns >= 0; --ns)
 #pragma unroll
           for (int r = 0; r < R; ++r)
             o[r][hh * 4 + e] =
@@ -381,26 +451,16 @@ __global__ __launch_bounds__(256, R == 1 ? 3 : 2) void k_cache_attend(AttendArgs
       }
   };
 
-  Step x, y;
-  int chunk = s0 >> 5;   // 32 steps a chunk
-  if (s0 < s1) {
-    load_chunk(chunk);
-    fetch(s0, x);
-  }
-  auto next = [&](int s, Step& to) {
-    if (s >= s1) return;
-    if ((s >> 5) != chunk) {
-      chunk = s >> 5;
-      load_chunk(chunk);
-    }
-    fetch(s, to);
-  };
-  for (int s = s0; s < s1; s += 2) {
-    next(s + 1, y);
-    compute(x);
-    if (s + 1 >= s1) break;
-    next(s + 2, x);
-    compute(y);
+  // One step's codes are under way or in use: V comes during the scores, the
+  // next K during the softmax and the second product.
+  Step x;
+  if (s0 < s1) fetch_k(s0, x);
+  for (int st = s0; st < s1; ++st) {
+    fetch_v(x);
+    scores(x);
+    Step y = x;
+    if (st + 1 < s1) fetch_k(st + 1, x);
+    finish(y);
   }
 
 #pragma unroll
@@ -409,152 +469,173 @@ __global__ __launch_bounds__(256, R == 1 ? 3 : 2) void k_cache_attend(AttendArgs
     l[r] += __shfl_xor(l[r], 32);
   }
 
-  if (BY_COLUMNS) {
+  if (P::KP == 1) {
 #pragma unroll
     for (int r = 0; r < R; ++r) {
-      if (orow[r] < 0) continue;
+      const int col = cbase + r * 16 + n16;
+      if (col > cend) continue;
+      const int64_t at = row_at<P::LISTED>(a, it, col, a.o_st, a.o_sh) + g * 4;
       const float inv = l[r] == 0.f ? 0.f : 1.f / l[r];
 #pragma unroll
       for (int c = 0; c < NC; ++c) {
-        const floatx4 w = o[r][c] * inv;
-        if (NS == 1) {
-          __bf16* to = static_cast<__bf16*>(a.o) + orow[r] + c * 16 + g * 4;
-          typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
-          *reinterpret_cast<bf16x4*>(to) = bf16x4{(__bf16)w[0], (__bf16)w[1], (__bf16)w[2], (__bf16)w[3]};
-        } else {
-          typedef float f4a4 __attribute__((ext_vector_type(4), aligned(4)));
-          *reinterpret_cast<f4a4*>(static_cast<float*>(a.o) + orow[r] + c * 16 + g * 4) = w;
-        }
+        const float w[4] = {o[r][c][0] * inv, o[r][c][1] * inv, o[r][c][2] * inv, o[r][c][3] * inv};
+        store_row<P::F32, 4>(a.o, at + c * 16, w);
       }
     }
     return;
   }
 
-  // The four waves' shares of the keys, 16 columns at a time: every wave puts
-  // its O, scaled to the common maximum, into the LDS and 16 threads a column
-  // add them up.
-  constexpr int LD = D + 4;
-  __shared__ float s_o[4][16][LD];
-  __shared__ float s_m[4][16], s_l[4][16];
-  const int col = threadIdx.x >> 4, ch = (threadIdx.x & 15) * (D / 16);
+  // The shares of the waves that split the keys, 16 columns at a time: every
+  // wave puts its O, scaled to the common maximum, into the LDS and TPC
+  // threads a column add them up.
+  constexpr int LD = D + 4, TPC = 4 * P::KP, E = D / TPC;
+  __shared__ float s_o[P::KP > 1 ? P::CG * P::KP * 16 * LD : 1];
+  __shared__ float s_m[P::CG][P::KP][16], s_l[P::CG][P::KP][16];
+  const int col = threadIdx.x / TPC, ocg = col >> 4, c16 = col & 15, ch = (threadIdx.x % TPC) * E;
 #pragma unroll
   for (int r = 0; r < R; ++r) {
     if (r) __syncthreads();
     if (g == 0) {
-      s_m[wave][n16] = m[r];
-      s_l[wave][n16] = l[r];
+      s_m[cg][kp][n16] = m[r];
+      s_l[cg][kp][n16] = l[r];
     }
     __syncthreads();
-    const float mall = fmaxf(fmaxf(s_m[0][n16], s_m[1][n16]), fmaxf(s_m[2][n16], s_m[3][n16]));
+    float mall = s_m[cg][0][n16];
+#pragma unroll
+    for (int w = 1; w < P::KP; ++w) mall = fmaxf(mall, s_m[cg][w][n16]);
     const float f = m[r] == mall ? 1.f : exp2_(m[r] - mall);   // -inf on both sides: nothing seen, O and l are 0
 #pragma unroll
     for (int c = 0; c < NC; ++c) {
       const floatx4 w = o[r][c] * f;
-      *reinterpret_cast<floatx4*>(&s_o[wave][n16][c * 16 + g * 4]) = w;
+      *reinterpret_cast<floatx4*>(&s_o[((cg * P::KP + kp) * 16 + n16) * LD + c * 16 + g * 4]) = w;
     }
     __syncthreads();
-    const float cm = fmaxf(fmaxf(s_m[0][col], s_m[1][col]), fmaxf(s_m[2][col], s_m[3][col]));
-    float sum = 0.f, acc[D / 16];
+    float cm = s_m[ocg][0][c16];
 #pragma unroll
-    for (int e = 0; e < D / 16; ++e) acc[e] = 0.f;
+    for (int w = 1; w < P::KP; ++w) cm = fmaxf(cm, s_m[ocg][w][c16]);
+    float sum = 0.f, acc[E];
 #pragma unroll
-    for (int w = 0; w < 4; ++w) {
-      sum += s_l[w][col] * (s_m[w][col] == cm ? 1.f : exp2_(s_m[w][col] - cm));
+    for (int e = 0; e < E; ++e) acc[e] = 0.f;
 #pragma unroll
-      for (int e = 0; e < D / 16; ++e) acc[e] += s_o[w][col][ch + e];
+    for (int w = 0; w < P::KP; ++w) {
+      sum += s_l[ocg][w][c16] * (s_m[ocg][w][c16] == cm ? 1.f : exp2_(s_m[ocg][w][c16] - cm));
+#pragma unroll
+      for (int e = 0; e < E; ++e) acc[e] += s_o[((ocg * P::KP + w) * 16 + c16) * LD + ch + e];
     }
-    const int cc = cbase + r * 16 + col;
-    if (cc > cend) continue;
+    const int cc = (ct * P::CG + ocg) * P::COLS + r * 16 + c16;
+    if (cc >= it.ncols) continue;
     if (a.splits > 1) {
-      float* to = a.part + (((int64_t)blockIdx.x * R + r) * 16 + col) * (D + 2);
+      // [item][split][column][D] and the same with (m, l)
+      const int64_t slot = ((int64_t)blockIdx.x * R + r) * 16 + c16;
+      float* to = a.part + slot * D;
 #pragma unroll
-      for (int e = 0; e < D / 16; ++e) to[ch + e] = acc[e];
+      for (int e = 0; e < E; e += 4)
+        *reinterpret_cast<floatx4*>(to + ch + e) = floatx4{acc[e], acc[e + 1], acc[e + 2], acc[e + 3]};
       if (ch == 0) {
-        to[D] = cm;
-        to[D + 1] = sum;
+        float* ml = a.part_ml + slot * 2;
+        ml[0] = cm;
+        ml[1] = sum;
       }
     } else {
-      const int tok = tok0 + (LISTED ? 0 : cc / a.group);
-      const int head = h * a.group + (LISTED ? cc : cc % a.group);
-      const int64_t oo = (int64_t)(sv.begin + tok) * a.o_st + (int64_t)head * a.o_sh + ch;
       const float inv = sum == 0.f ? 0.f : 1.f / sum;
 #pragma unroll
-      for (int e = 0; e < D / 16; ++e) {
-        if (NS == 1) static_cast<__bf16*>(a.o)[oo + e] = (__bf16)(acc[e] * inv);
-        else static_cast<float*>(a.o)[oo + e] = acc[e] * inv;
-      }
+      for (int e = 0; e < E; ++e) acc[e] *= inv;
+      store_row<P::F32, E>(a.o, row_at<P::LISTED>(a, it, cc, a.o_st, a.o_sh) + ch, acc);
     }
   }
 }
 
-// Joins the parts of split items: 16 threads a column, one workgroup per item
-// and 16 columns.
+// Joins the parts of split items.  One workgroup for 16 columns and 32
+// channels of an item: 8 threads a column take 4 channels each, two sets of
+// them every second part.
+constexpr int kMaxSplits = 256;
+
 template <int D, int R, bool F32, bool LISTED>
 __global__ __launch_bounds__(256) void k_cache_join(AttendArgs a) {
+  __shared__ float s_w[kMaxSplits][16];
+  __shared__ float s_sum[16];
+  __shared__ floatx4 s_acc[128];
   unsigned id = blockIdx.x;
+  const int ch32 = id % (D / 32);
+  id /= D / 32;
   const int r = id % R;
   id /= R;
   const unsigned item = id;
   const int ct = id % a.col_tiles;
   id /= a.col_tiles;
-  const int h = id % a.c.kv_heads;
-  const int unit = id / a.c.kv_heads;
-  const int seq = LISTED ? seq_of_row(a.b, unit, threadIdx.x & 63) : unit;
-  if (seq >= a.b.seqs) return;
-  const SeqView sv = seq_view(a.b, a.c.page_log2, seq);
-  const int tok0 = LISTED ? unit - sv.begin : 0;
-  if (LISTED && (tok0 < 0 || tok0 >= sv.n)) return;
-  const int ncols = LISTED ? a.group : min(sv.n, a.b.max_new) * a.group;
-  const int col = threadIdx.x >> 4, ch = (threadIdx.x & 15) * (D / 16);
-  const int cc = ct * 16 * R + r * 16 + col;
-  if (cc >= ncols) return;
-  const float* part = a.part + (((int64_t)item * a.splits * R + r) * 16 + col) * (D + 2);
-  const int64_t stride = (int64_t)R * 16 * (D + 2);
-  float m = -INFINITY;
-  for (int s = 0; s < a.splits; ++s) m = fmaxf(m, part[s * stride + D]);
-  float sum = 0.f, acc[D / 16];
+  Item it;
+  it.h = id % a.c.kv_heads;
+  if (!item_of<LISTED>(a, id / a.c.kv_heads, threadIdx.x & 63, &it)) return;
+  const int c0 = ct * 16 * R + r * 16;
+  if (c0 >= it.ncols) return;
+  const int64_t slot0 = ((int64_t)item * a.splits * R + r) * 16;   // part s: + s * R * 16
+  {
+    // 16 threads a column: maximum, weights and sum over the parts.
+    const int c = threadIdx.x >> 4, j = threadIdx.x & 15;
+    const float* ml = a.part_ml + (slot0 + c) * 2;
+    const bool in = c0 + c < it.ncols;
+    float m = -INFINITY;
+    if (in)
+      for (int s = j; s < a.splits; s += 16) m = fmaxf(m, ml[(int64_t)s * R * 32]);
 #pragma unroll
-  for (int e = 0; e < D / 16; ++e) acc[e] = 0.f;
-  for (int s = 0; s < a.splits; ++s) {
-    const float* p = part + s * stride;
-    const float f = p[D] == m ? 1.f : exp2_(p[D] - m);
-    sum += p[D + 1] * f;
+    for (int x = 1; x < 16; x <<= 1) m = fmaxf(m, __shfl_xor(m, x));
+    float sum = 0.f;
+    if (in)
+      for (int s = j; s < a.splits; s += 16) {
+        const float ms = ml[(int64_t)s * R * 32];
+        const float w = ms == m ? 1.f : exp2_(ms - m);
+        s_w[s][c] = w;
+        sum += w * ml[(int64_t)s * R * 32 + 1];
+      }
 #pragma unroll
-    for (int e = 0; e < D / 16; ++e) acc[e] += p[ch + e] * f;
+    for (int x = 1; x < 16; x <<= 1) sum += __shfl_xor(sum, x);
+    if (j == 0) s_sum[c] = sum;
   }
-  const int tok = tok0 + (LISTED ? 0 : cc / a.group);
-  const int head = h * a.group + (LISTED ? cc : cc % a.group);
-  const int64_t oo = (int64_t)(sv.begin + tok) * a.o_st + (int64_t)head * a.o_sh + ch;
-  const float inv = sum == 0.f ? 0.f : 1.f / sum;
-#pragma unroll
-  for (int e = 0; e < D / 16; ++e) {
-    if (F32) static_cast<float*>(a.o)[oo + e] = acc[e] * inv;
-    else static_cast<__bf16*>(a.o)[oo + e] = (__bf16)(acc[e] * inv);
+  __syncthreads();
+  const int half = threadIdx.x >> 7, t = threadIdx.x & 127, c = t >> 3, ch = ch32 * 32 + (t & 7) * 4;
+  floatx4 acc = {0.f, 0.f, 0.f, 0.f};
+  const bool in = c0 + c < it.ncols;
+  if (in) {
+    const float* part = a.part + (slot0 + c) * D + ch;
+#pragma unroll 8
+    for (int s = half; s < a.splits; s += 2)
+      acc += *reinterpret_cast<const floatx4*>(part + (int64_t)s * R * 16 * D) * s_w[s][c];
   }
+  if (half) s_acc[t] = acc;
+  __syncthreads();
+  if (half || !in) return;
+  acc += s_acc[t];
+  const float inv = s_sum[c] == 0.f ? 0.f : 1.f / s_sum[c];
+  const float w[4] = {acc[0] * inv, acc[1] * inv, acc[2] * inv, acc[3] * inv};
+  store_row<F32, 4>(a.o, row_at<LISTED>(a, it, c0 + c, a.o_st, a.o_sh) + ch, w);
 }
 
-template <int D, int R, int NS, bool LISTED>
+template <typename P>
 hipError_t launch(const AttendArgs& a, const AttendPlan& p, hipStream_t s) {
-  if (p.by_columns) {
-    k_cache_attend<D, R, NS, LISTED, true><<<(unsigned)p.items, 256, 0, s>>>(a);
-  } else {
-    k_cache_attend<D, R, NS, LISTED, false><<<(unsigned)(p.items * p.splits), 256, 0, s>>>(a);
-    const hipError_t e = hipGetLastError();
-    if (e != hipSuccess) return e;
-    if (p.splits > 1) k_cache_join<D, R, NS == 3, LISTED><<<(unsigned)(p.items * R), 256, 0, s>>>(a);
-  }
+  k_cache_attend<P><<<(unsigned)(p.items * p.splits), P::THREADS, 0, s>>>(a);
+  const hipError_t e = hipGetLastError();
+  if (e != hipSuccess || p.splits == 1) return e;
+  k_cache_join<P::D, P::R, P::F32, P::LISTED><<<(unsigned)(p.items * P::R * (P::D / 32)), 256, 0, s>>>(a);
   return hipGetLastError();
 }
 
 template <int D>
 hipError_t launch_d(const AttendArgs& a, const AttendPlan& p, int dtype, hipStream_t s) {
-  if (dtype == SSBA_DT_F32)
-    return p.listed ? launch<D, 1, 3, true>(a, p, s) : launch<D, 1, 3, false>(a, p, s);
-  if (p.listed) return launch<D, 1, 1, true>(a, p, s);
-  switch (p.tiles16) {
-    case 1: return launch<D, 1, 1, false>(a, p, s);
-    case 2: return launch<D, 2, 1, false>(a, p, s);
-    default: return launch<D, 4, 1, false>(a, p, s);
+  const bool f32 = dtype == SSBA_DT_F32;
+  switch (p.kind) {
+    case kAttendRows:
+      return f32 ? launch<Shape<D, 1, 3, 3, true, true, 4, 1, false>>(a, p, s)
+                 : launch<Shape<D, 1, 1, 1, false, true, 4, 1, false>>(a, p, s);
+    case kAttendRow:
+      return f32 ? launch<Shape<D, 1, 3, 3, true, true, 1, 4, false>>(a, p, s)
+                 : launch<Shape<D, 1, 1, 2, false, true, 1, 4, false>>(a, p, s);
+    case kAttendFew:
+      if (f32) return launch<Shape<D, 1, 3, 3, true, false, 1, 4, false>>(a, p, s);
+      return p.tiles16 == 1 ? launch<Shape<D, 1, 1, 2, false, false, 1, 4, false>>(a, p, s)
+                            : launch<Shape<D, 2, 1, 1, false, false, 1, 4, false>>(a, p, s);
+    default:
+      return f32 ? launch<Shape<D, 1, 3, 3, true, false, 4, 1, false>>(a, p, s)
+                 : launch<Shape<D, 4, 1, 1, false, false, 4, 2, true>>(a, p, s);
   }
 }
 
