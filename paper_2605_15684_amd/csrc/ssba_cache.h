@@ -71,9 +71,18 @@ struct SelectArgs {
   int32_t* lists;
   uint64_t* keys;   // [rows][kv_heads][max_pages] ranking keys of the scored pages
   int group, causal, keep, first, last;
-  int chunks;       // workgroups that share a row's pages
+  int tiles;        // tiles of 16 tokens of a sequence
 };
-constexpr int kSelectPages = 256;   // pages a workgroup scores at a time
+constexpr int kSelectPages = 64;     // pages a workgroup scores at a time
+constexpr int kSelectInLds = 1024;   // pages whose scores of 16 tokens the LDS holds
+
+// What the selection launches (ssba_cache_api.cpp decides).
+enum SelectKind { kSelectRow, kSelectTile, kSelectRowLong, kSelectTileLong };
+struct SelectPlan {
+  SelectKind kind;
+  int chunks;       // long kinds: workgroups that share a row's (a tile's) pages
+  bool scored;      // long kinds: some row may have pages to score
+};
 
 struct AttendArgs {
   CacheView c;
@@ -105,7 +114,7 @@ struct AttendPlan {
 };
 
 hipError_t launch_cache_append(const AppendArgs& a, int dtype, hipStream_t s);
-hipError_t launch_cache_select(const SelectArgs& a, int dtype, hipStream_t s);
+hipError_t launch_cache_select(const SelectArgs& a, const SelectPlan& p, int dtype, hipStream_t s);
 hipError_t launch_cache_attend(const AttendArgs& a, const AttendPlan& p, int dtype, hipStream_t s);
 
 struct PagesArgs {

@@ -124,12 +124,28 @@ int64_t long_of(const ssba_cache* c, const ssba_cache_batch* b) {
 
 int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
 
-size_t select_scratch(const ssba_cache* c, const ssba_cache_batch* b, const ssba_cache_query* q) {
-  return b->max_pages > q->keep ? (size_t)8 * b->rows * c->kv_heads * b->max_pages : 0;
+// Pages to score fit a workgroup's LDS, or go through the scratch; 16 tokens
+// share the pooled keys where sequences bring enough of them: with 8 of 16
+// rows of a tile in use the matrix form needs half the loads.
+ssba::SelectPlan plan_select(const ssba_cache* c, const ssba_cache_batch* b, const ssba_cache_query* q) {
+  ssba::SelectPlan p;
+  const bool tile = b->max_new >= 8;
+  p.scored = b->max_pages > q->keep;
+  p.chunks = 1;
+  if (b->max_pages <= ssba::kSelectInLds) {
+    p.kind = tile ? ssba::kSelectTile : ssba::kSelectRow;
+  } else {
+    p.kind = tile ? ssba::kSelectTileLong : ssba::kSelectRowLong;
+    // A workgroup takes 64 pages at a time; 8 times as many for a tile, whose queries take longer to load.
+    p.chunks = (int)std::min<int64_t>(ceil_div(ceil_div(long_of(c, b), c->page), ssba::kSelectPages * (tile ? 8 : 1)),
+                                      65535);
+  }
+  return p;
 }
 
-int select_chunks(const ssba_cache* c, const ssba_cache_batch* b) {
-  return (int)std::min<int64_t>(ceil_div(ceil_div(long_of(c, b), c->page), ssba::kSelectPages), 65535);
+size_t select_scratch(const ssba_cache* c, const ssba_cache_batch* b, const ssba_cache_query* q) {
+  const ssba::SelectPlan p = plan_select(c, b, q);
+  return p.scored && p.kind >= ssba::kSelectRowLong ? (size_t)8 * b->rows * c->kv_heads * b->max_pages : 0;
 }
 
 // Items are independent (sequence or row, kv head, column tile); one workgroup
@@ -220,7 +236,7 @@ ssba_status ssba_cache_select(const ssba_cache* c, int32_t layer, const ssba_cac
   a.sh = q->q_stride_h;
   if ((st = strides_of(q->dtype, q->heads, c->head_dim, b->rows, &a.st, &a.sh)) != SSBA_OK) return st;
   if ((st = check_arrays(c)) != SSBA_OK || (st = check_batch_arrays(b)) != SSBA_OK) return st;
-  if (b->rows == 0) return SSBA_OK;
+  if (b->rows == 0 || b->max_new == 0) return SSBA_OK;
   const size_t need = select_scratch(c, b, q);
   if (!query || !lists || !aligned(query, q->dtype == SSBA_DT_BF16 ? 16 : 4) || !aligned(lists, 4)) return SSBA_ERR_ARG;
   if (need && (!scratch || !aligned(scratch, 16))) return SSBA_ERR_ARG;
@@ -236,9 +252,14 @@ ssba_status ssba_cache_select(const ssba_cache* c, int32_t layer, const ssba_cac
   a.keep = q->keep;
   a.first = q->first;
   a.last = q->last;
-  a.chunks = select_chunks(c, b);
-  if (too_many((int64_t)b->rows * c->kv_heads * a.chunks)) return SSBA_ERR_UNSUPPORTED;
-  return ssba::launch_cache_select(a, q->dtype, static_cast<hipStream_t>(stream)) == hipSuccess ? SSBA_OK : SSBA_ERR_HIP;
+  a.tiles = (int)ceil_div(b->max_new, 16);
+  const ssba::SelectPlan p = plan_select(c, b, q);
+  // 1024 threads at most rank a row, 512 score one where its keys stay in the LDS.
+  if (too_many((int64_t)b->rows * c->kv_heads * std::max(p.chunks, 4)) ||
+      too_many((int64_t)b->seqs * c->kv_heads * a.tiles * p.chunks * 2))
+    return SSBA_ERR_UNSUPPORTED;
+  return ssba::launch_cache_select(a, p, q->dtype, static_cast<hipStream_t>(stream)) == hipSuccess ? SSBA_OK
+                                                                                                   : SSBA_ERR_HIP;
 }
 
 ssba_status ssba_cache_attend_workspace_size(const ssba_cache* c, const ssba_cache_batch* b,

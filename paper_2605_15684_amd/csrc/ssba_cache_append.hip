@@ -1,11 +1,14 @@
 // New keys and values into the pages of a cache (include/ssba_cache.h).
 //
 // One workgroup per (sequence, page it touches, kv head).  A thread holds 4
-// tokens x 16 channels of K or of V: for K that is four 16-byte pieces of the
-// page, for V 16 words of 4 tokens, so both are written from registers.  The
-// page's exponent is the maximum over its new tokens and what it had; the
-// codes' sum over a page is exact in fp32 (64 codes of at most 448 in steps of
-// 2^-9: 24 bits), in any order.
+// tokens x 8 channels of K and the same of V, so that 16 (D 128) lanes read a
+// row's 256 bytes at once.  The page's exponent is the maximum over its new
+// tokens and what it had.  The codes of a page that is new as a whole are put
+// together in the LDS in the page's byte order and leave in 16-byte stores,
+// 1 KB a wave; other pages get their few bytes directly.
+// The sum of a page's codes is exact in fp32 (at most 64 codes of at most 448
+// in steps of 2^-9: 24 bits), in any order.
+// Bound by bytes: new rows read once, one byte a value written.
 #include <hip/hip_runtime.h>
 #include <hip/hip_bf16.h>
 
@@ -31,14 +34,10 @@ __device__ __forceinline__ float pow2(int e) {   // e <= 127; below -126 too sma
   return __uint_as_float((uint32_t)(max(e, -126) + 127) << 23);
 }
 
-__device__ __forceinline__ float saturate(float x) {   // NaN stays
-  return fabsf(x) > 448.f ? copysignf(448.f, x) : x;
-}
-
-// Four values as e4m3, to nearest even.
+// Four values of at most 448 as e4m3, to nearest even; NaN stays NaN.
 __device__ __forceinline__ uint32_t codes_of(float a, float b, float c, float d) {
-  int w = __builtin_amdgcn_cvt_pk_fp8_f32(saturate(a), saturate(b), 0, false);
-  return (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(saturate(c), saturate(d), w, true);
+  const int w = __builtin_amdgcn_cvt_pk_fp8_f32(a, b, 0, false);
+  return (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(c, d, w, true);
 }
 
 __device__ __forceinline__ void values_of(uint32_t w, float (&x)[4]) {
@@ -51,30 +50,30 @@ __device__ __forceinline__ void values_of(uint32_t w, float (&x)[4]) {
 }
 
 template <bool F32>
-__device__ __forceinline__ void load16(const void* base, int64_t off, float (&x)[16]) {
+__device__ __forceinline__ void load8(const void* base, int64_t off, float (&x)[8]) {
   if (F32) {
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
+    for (int i = 0; i < 2; ++i) {
       const u32x4 w = *reinterpret_cast<const u32x4a4*>(static_cast<const float*>(base) + off + 4 * i);
 #pragma unroll
       for (int e = 0; e < 4; ++e) x[4 * i + e] = __uint_as_float(w[e]);
     }
   } else {
+    const u32x4 w = *reinterpret_cast<const u32x4*>(static_cast<const uint16_t*>(base) + off);
 #pragma unroll
-    for (int i = 0; i < 2; ++i) {
-      const u32x4 w = *reinterpret_cast<const u32x4*>(static_cast<const uint16_t*>(base) + off + 8 * i);
-#pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        x[8 * i + 2 * e] = __uint_as_float(w[e] << 16);
-        x[8 * i + 2 * e + 1] = __uint_as_float(w[e] & 0xffff0000u);
-      }
+    for (int e = 0; e < 4; ++e) {
+      x[2 * e] = __uint_as_float(w[e] << 16);
+      x[2 * e + 1] = __uint_as_float(w[e] & 0xffff0000u);
     }
   }
 }
 
 template <int D, bool F32>
 __global__ __launch_bounds__(256) void k_cache_append(AppendArgs a) {
-  constexpr int NCH = D / 16;
+  constexpr int NCH = D / 8;
+  __shared__ uint32_t s_top[2];
+  __shared__ float s_sum[4][D];
+  __shared__ u32x4 s_page[2][64 * D / 16];   // the codes of a new page
   const int page = 1 << a.c.page_log2;
   unsigned id = blockIdx.x;
   const int h = id % a.c.kv_heads;
@@ -90,21 +89,21 @@ __global__ __launch_bounds__(256) void k_cache_append(AppendArgs a) {
   const int phys = a.b.table[(int64_t)seq * a.b.max_pages + lp];
   if (phys < 0 || phys >= a.c.pages) return;
 
-  const int units = page * D / 64;             // threads of K, and of V
-  const int which = threadIdx.x / units;       // 0: K, 1: V, above: idle
-  const int u = threadIdx.x - which * units;
-  const int ch16 = u % NCH, tq = u / NCH;      // channels 16 ch16 .., tokens 4 tq ..
-  const bool active = which < 2;
+  const int units = page * NCH / 4;            // threads with a part of the page
+  const bool active = (int)threadIdx.x < units;
+  const int ch8 = threadIdx.x % NCH, tq = threadIdx.x / NCH;   // channels 8 ch8 .., tokens 4 tq ..
   const bool complete = p0 + page <= sv.len;
   const bool has_old = p0 < start;
-
-  __shared__ uint32_t s_top[2];
-  __shared__ float s_sum[2][D];
+  float* scale = a.c.scale + ((int64_t)phys * a.c.kv_heads + h) * 2;
+  uint32_t was[2] = {0, 0};
+  if (has_old) {
+    was[0] = __float_as_uint(scale[0]);
+    was[1] = __float_as_uint(scale[1]);
+  }
   if (threadIdx.x < 2) s_top[threadIdx.x] = 0;
-  __syncthreads();
+  __syncthreads();   // every thread has the old scales before they are replaced
 
-  float x[4][16];
-  uint32_t top = 0;
+  float x[2][4][8];
   bool fresh[4], old[4];
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
@@ -112,99 +111,182 @@ __global__ __launch_bounds__(256) void k_cache_append(AppendArgs a) {
     fresh[i] = active && pos >= start && pos < sv.len;
     old[i] = active && pos < start;
     if (fresh[i]) {
-      const int64_t off = (int64_t)(sv.begin + pos - start) * a.st + (int64_t)h * a.sh + ch16 * 16;
-      load16<F32>(which ? a.v : a.k, off, x[i]);
-#pragma unroll
-      for (int e = 0; e < 16; ++e) {
-        const uint32_t b = __float_as_uint(x[i][e]) & 0x7fffffffu;
-        top = max(top, b < 0x7f800000u ? b : 0u);
-      }
+      const int64_t off = (int64_t)(sv.begin + pos - start) * a.st + (int64_t)h * a.sh + ch8 * 8;
+      load8<F32>(a.k, off, x[0][i]);
+      load8<F32>(a.v, off, x[1][i]);
     }
   }
-  if (top) atomicMax(&s_top[which & 1], top);
-  __syncthreads();
-
-  const int kv = which & 1;
-  float* scale = a.c.scale + ((int64_t)phys * a.c.kv_heads + h) * 2;
-  int e = exponent_of(s_top[kv]), e0 = e;
-  if (has_old) {
-    e0 = min(max((int)((__float_as_uint(scale[kv]) >> 23) & 0xff) - 127, kMinExp), kMaxExp);
-    e = max(e, e0);
-  }
-  __syncthreads();   // every thread has the old scale before it is replaced
-  if (active && u == 0) scale[kv] = pow2(e);
-
-  const float inv = pow2(-e), restate = pow2(e0 - e);
-  const bool grows = has_old && e > e0;
-  uint8_t* base = (kv ? a.c.v : a.c.k) + (int64_t)phys * a.c.page_bytes + (int64_t)h * page * D +
-                  (tq >> 2) * 16 * D + (ch16 >> 2) * 1024;
-  float sum[16];
+  // The largest magnitude; fmaxf passes over NaN.
+  float top[2] = {0.f, 0.f};
 #pragma unroll
-  for (int c = 0; c < 16; ++c) sum[c] = 0.f;
+  for (int kv = 0; kv < 2; ++kv) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      if (fresh[i]) {
+#pragma unroll
+        for (int e = 0; e < 8; ++e) top[kv] = fmaxf(top[kv], fabsf(x[kv][i][e]));
+      }
+#pragma unroll
+    for (int off = 1; off < 64; off <<= 1) top[kv] = fmaxf(top[kv], __shfl_xor(top[kv], off));
+    if ((threadIdx.x & 63) == 0) atomicMax(&s_top[kv], __float_as_uint(top[kv]));
+  }
+  __syncthreads();
+  const bool infinite[2] = {s_top[0] == 0x7f800000u, s_top[1] == 0x7f800000u};
+  if (infinite[0] || infinite[1]) {   // rare: once more over the finite ones
+    __syncthreads();
+    if (threadIdx.x < 2) s_top[threadIdx.x] = 0;
+    __syncthreads();
+#pragma unroll
+    for (int kv = 0; kv < 2; ++kv) {
+      uint32_t t = 0;
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+        if (fresh[i]) {
+#pragma unroll
+          for (int e = 0; e < 8; ++e) {
+            const uint32_t b = __float_as_uint(x[kv][i][e]) & 0x7fffffffu;
+            t = max(t, b < 0x7f800000u ? b : 0u);
+          }
+        }
+      if (t) atomicMax(&s_top[kv], t);
+    }
+    __syncthreads();
+  }
 
-  if (active && kv == 0) {
+  int e[2];
+  float inv[2], restate[2];
+  bool grows[2];
+#pragma unroll
+  for (int kv = 0; kv < 2; ++kv) {
+    e[kv] = exponent_of(s_top[kv]);
+    int e0 = e[kv];
+    if (has_old) {
+      e0 = min(max((int)((was[kv] >> 23) & 0xff) - 127, kMinExp), kMaxExp);
+      e[kv] = max(e[kv], e0);
+    }
+    grows[kv] = e[kv] > e0;
+    inv[kv] = pow2(-e[kv]);
+    restate[kv] = pow2(e0 - e[kv]);
+    if (threadIdx.x == 0) scale[kv] = pow2(e[kv]);
+    if (infinite[kv]) {   // infinities take the largest code
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+#pragma unroll
+        for (int c = 0; c < 8; ++c)
+          if (fabsf(x[kv][i][c]) == INFINITY) x[kv][i][c] = copysignf(448.f * pow2(e[kv]), x[kv][i][c]);
+    }
+  }
+  const int64_t image = (int64_t)phys * a.c.page_bytes + (int64_t)h * page * D;
+  // Bytes of this thread's first token in the page: 8 of K (then 16 on per
+  // token), a word of V per channel.
+  const int block = (tq >> 2) * 16 * D + (ch8 >> 3) * 1024;
+  const int k_at = block + (ch8 >> 1 & 3) * 256 + (tq & 3) * 64 + (ch8 & 1) * 8;
+  const int v_at = block + (tq & 3) * 256 + (ch8 & 1) * 128 + (ch8 >> 1 & 3) * 4;
+  float sum[8];
+#pragma unroll
+  for (int c = 0; c < 8; ++c) sum[c] = 0.f;
+
+  if (complete && !has_old) {
+    // The whole page is new.
+    if (active) {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const float(&y)[8] = x[0][i];
+        const float f = inv[0];
+        const uint32_t w0 = codes_of(y[0] * f, y[1] * f, y[2] * f, y[3] * f);
+        const uint32_t w1 = codes_of(y[4] * f, y[5] * f, y[6] * f, y[7] * f);
+        *reinterpret_cast<uint2*>(reinterpret_cast<char*>(s_page[0]) + k_at + 16 * i) = make_uint2(w0, w1);
+        float z[4];
+        values_of(w0, z);
+#pragma unroll
+        for (int c = 0; c < 4; ++c) sum[c] += z[c];
+        values_of(w1, z);
+#pragma unroll
+        for (int c = 0; c < 4; ++c) sum[4 + c] += z[c];
+      }
+#pragma unroll
+      for (int c = 0; c < 8; ++c) {
+        const float f = inv[1];
+        *reinterpret_cast<uint32_t*>(reinterpret_cast<char*>(s_page[1]) + v_at + 16 * c) =
+            codes_of(x[1][0][c] * f, x[1][1][c] * f, x[1][2][c] * f, x[1][3][c] * f);
+      }
+    }
+    __syncthreads();
+    for (int i = threadIdx.x; i < page * D / 16; i += blockDim.x) {
+      *reinterpret_cast<u32x4*>(a.c.k + image + 16 * i) = s_page[0][i];
+      *reinterpret_cast<u32x4*>(a.c.v + image + 16 * i) = s_page[1][i];
+    }
+  } else if (active) {
+    uint8_t* kp = a.c.k + image + k_at;
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-      uint8_t* at = base + (ch16 & 3) * 256 + ((tq & 3) * 4 + i) * 16;
-      u32x4 w = {0, 0, 0, 0};
-      const bool read = old[i] && (grows || complete);
-      if (read) w = *reinterpret_cast<const u32x4*>(at);
+      uint32_t w[2] = {0, 0};   // stays 0 for what is neither read nor new: those count for nothing below
+      const bool read = old[i] && (grows[0] || complete);
+      if (read) {
+        const uint2 c = *reinterpret_cast<const uint2*>(kp + 16 * i);
+        w[0] = c.x;
+        w[1] = c.y;
+      }
 #pragma unroll
-      for (int q = 0; q < 4; ++q) {
+      for (int q = 0; q < 2; ++q) {
         float y[4];
         if (fresh[i]) {
-          w[q] = codes_of(x[i][4 * q] * inv, x[i][4 * q + 1] * inv, x[i][4 * q + 2] * inv, x[i][4 * q + 3] * inv);
-        } else if (read && grows) {
+          const float f = inv[0];
+          w[q] = codes_of(x[0][i][4 * q] * f, x[0][i][4 * q + 1] * f, x[0][i][4 * q + 2] * f, x[0][i][4 * q + 3] * f);
+        } else if (read && grows[0]) {
           values_of(w[q], y);
-          w[q] = codes_of(y[0] * restate, y[1] * restate, y[2] * restate, y[3] * restate);
+          w[q] = codes_of(y[0] * restate[0], y[1] * restate[0], y[2] * restate[0], y[3] * restate[0]);
         }
-        values_of(w[q], y);   // 0 where neither: not complete, or no such token
+        values_of(w[q], y);
 #pragma unroll
         for (int z = 0; z < 4; ++z) sum[4 * q + z] += y[z];
       }
-      if (fresh[i] || (old[i] && grows)) *reinterpret_cast<u32x4*>(at) = w;
+      if (fresh[i] || (old[i] && grows[0])) *reinterpret_cast<uint2*>(kp + 16 * i) = make_uint2(w[0], w[1]);
     }
-  } else if (active) {
-    uint8_t* at = base + (tq & 3) * 256 + (ch16 & 3) * 4;
+    uint8_t* vp = a.c.v + image + v_at;
     bool write[4];
 #pragma unroll
-    for (int i = 0; i < 4; ++i) write[i] = fresh[i] || (old[i] && grows);
+    for (int i = 0; i < 4; ++i) write[i] = fresh[i] || (old[i] && grows[1]);
     const bool all = write[0] && write[1] && write[2] && write[3];
-    const bool any_old = grows && (old[0] || old[1] || old[2] || old[3]);
+    const bool any_old = grows[1] && (old[0] || old[1] || old[2] || old[3]);
+    if (write[0] || write[1] || write[2] || write[3]) {
 #pragma unroll
-    for (int c = 0; c < 16; ++c) {
-      float y[4] = {0.f, 0.f, 0.f, 0.f};
-      if (any_old) values_of(*reinterpret_cast<const uint32_t*>(at + c * 16), y);
+      for (int c = 0; c < 8; ++c) {
+        float y[4] = {0.f, 0.f, 0.f, 0.f};
+        if (any_old) values_of(*reinterpret_cast<const uint32_t*>(vp + c * 16), y);
 #pragma unroll
-      for (int i = 0; i < 4; ++i) y[i] = fresh[i] ? x[i][c] * inv : y[i] * restate;
-      const uint32_t w = codes_of(y[0], y[1], y[2], y[3]);
-      if (all) {
-        *reinterpret_cast<uint32_t*>(at + c * 16) = w;
-      } else {
+        for (int i = 0; i < 4; ++i) y[i] = fresh[i] ? x[1][i][c] * inv[1] : y[i] * restate[1];
+        const uint32_t w = codes_of(y[0], y[1], y[2], y[3]);
+        if (all) {
+          *reinterpret_cast<uint32_t*>(vp + c * 16) = w;
+        } else {
 #pragma unroll
-        for (int i = 0; i < 4; ++i)
-          if (write[i]) at[c * 16 + i] = (uint8_t)(w >> (8 * i));
+          for (int i = 0; i < 4; ++i)
+            if (write[i]) vp[c * 16 + i] = (uint8_t)(w >> (8 * i));
+        }
       }
     }
   }
 
   if (!complete) return;
-  // Sum of the codes over the page's tokens: the K threads of a channel block
+  // Sum of the codes over the page's tokens: the threads of a channel block
   // are NCH apart.
 #pragma unroll
-  for (int c = 0; c < 16; ++c)
-    for (int off = NCH; off < min(units, 64); off <<= 1) sum[c] += __shfl_xor(sum[c], off);
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  if (active && kv == 0 && lane < NCH) {
+  for (int c = 0; c < 8; ++c)
 #pragma unroll
-    for (int c = 0; c < 16; ++c) s_sum[wave][lane * 16 + c] = sum[c];
+    for (int off = NCH; off < 64; off <<= 1) sum[c] += __shfl_xor(sum[c], off);
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  if (lane < NCH) {
+#pragma unroll
+    for (int c = 0; c < 8; ++c) s_sum[wave][lane * 8 + c] = sum[c];
   }
   __syncthreads();
-  if (active && kv == 0) {
-    const float f = pow2(e) / (float)page;
-    __hip_bfloat16* mean = reinterpret_cast<__hip_bfloat16*>(a.c.kmean) + ((int64_t)phys * a.c.kv_heads + h) * D;
-    for (int c = u; c < D; c += units)
-      mean[c] = __float2bfloat16((units > 64 ? s_sum[0][c] + s_sum[1][c] : s_sum[0][c]) * f);
+  const float f = pow2(e[0]) / (float)page;
+  __hip_bfloat16* mean = reinterpret_cast<__hip_bfloat16*>(a.c.kmean) + ((int64_t)phys * a.c.kv_heads + h) * D;
+  for (int c = threadIdx.x; c < D; c += blockDim.x) {
+    float t = s_sum[0][c];
+    for (int w = 1; w < (int)blockDim.x / 64; ++w) t += s_sum[w][c];
+    mean[c] = __float2bfloat16(t * f);
   }
 }
 
@@ -212,7 +294,7 @@ __global__ __launch_bounds__(256) void k_cache_append(AppendArgs a) {
 
 hipError_t launch_cache_append(const AppendArgs& a, int dtype, hipStream_t s) {
   const int64_t groups = (int64_t)a.b.seqs * a.slots * a.c.kv_heads;
-  const int threads = max(64, (2 << a.c.page_log2) * a.c.head_dim / 64);
+  const int threads = max(64, (a.c.head_dim << a.c.page_log2) / 32);
   const bool f32 = dtype == SSBA_DT_F32;
   auto go = [&](auto k) { k<<<(unsigned)groups, threads, 0, s>>>(a); };
   if (a.c.head_dim == 64) f32 ? go(k_cache_append<64, true>) : go(k_cache_append<64, false>);

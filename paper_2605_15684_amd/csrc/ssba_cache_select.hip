@@ -2,10 +2,21 @@
 // page between the ones always kept, then the largest of them per token and kv
 // head.
 //
-// Scores are in 64 bits: a sum of bf16 products over at most 128 channels has
-// few roundings there, in a fixed order, so a list depends on nothing but the
-// data.  k_select_scores is bound by the pooled keys it reads (2 D bytes a page
-// and head); k_select_top ranks 64-bit keys whose order is that of the scores.
+// Scores are in 64 bits, where a sum of products of bf16 numbers over at most
+// 128 channels has few roundings or none: lists are those of the exact scores
+// except where two of these differ by less than about 1e-16 of their terms.
+// Within a list every page's sum is formed in the same order, so equal pages
+// have equal scores.  Ranking is on 64-bit keys whose order is that of the
+// scores (rank_key).
+//
+//   k_select_row     one (token, kv head) per workgroup, tables of at most 1024
+//                    pages: scores into the LDS, one wave ranks them.  Bound by
+//                    the pooled keys, 2 D bytes a page.
+//   k_select_tile    16 tokens of a sequence per workgroup: a page's pooled key
+//                    serves them all, on v_mfma_f64_16x16x4_f64.  Scores into
+//                    the LDS (at most 1024 pages), or to the scratch.
+//   k_select_scores, k_select_top   longer tables: a row's pages are shared out
+//                    over workgroups, then one workgroup ranks the row.
 #include <hip/hip_runtime.h>
 
 #include "ssba_cache.h"
@@ -15,6 +26,8 @@ namespace ssba {
 namespace {
 
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+typedef uint32_t u32x4a4 __attribute__((ext_vector_type(4), aligned(4)));
+typedef double doublex4 __attribute__((ext_vector_type(4)));
 
 // The pages a token can choose from: [first, first + middle) are scored.
 struct Range {
@@ -29,17 +42,257 @@ __device__ __forceinline__ Range range_of(const SelectArgs& a, const SeqView& sv
   return r;
 }
 
-template <bool F32>
-__device__ __forceinline__ double q_at(const void* q, int64_t i) {
-  if (F32) return (double)static_cast<const float*>(q)[i];
-  return (double)__uint_as_float((uint32_t) static_cast<const uint16_t*>(q)[i] << 16);
+// Sum over the group's query heads of N channels from `ch` of a row.
+template <bool F32, int N>
+__device__ __forceinline__ void q_sum(const SelectArgs& a, int row, int h, int ch, double (&q)[N]) {
+#pragma unroll
+  for (int c = 0; c < N; ++c) q[c] = 0.0;
+  const int64_t at = (int64_t)row * a.st + (int64_t)h * a.group * a.sh + ch;
+#pragma unroll 2
+  for (int g = 0; g < a.group; ++g) {
+    if (F32) {
+      const float* x = static_cast<const float*>(a.q) + at + g * a.sh;
+#pragma unroll
+      for (int c = 0; c < N; c += 4) {
+        const u32x4 w = *reinterpret_cast<const u32x4a4*>(x + c);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) q[c + e] += (double)__uint_as_float(w[e]);
+      }
+    } else {
+      const uint16_t* x = static_cast<const uint16_t*>(a.q) + at + g * a.sh;
+#pragma unroll
+      for (int c = 0; c < N; c += 8) {
+        const u32x4 w = *reinterpret_cast<const u32x4*>(x + c);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          q[c + 2 * e] += (double)__uint_as_float(w[e] << 16);
+          q[c + 2 * e + 1] += (double)__uint_as_float(w[e] & 0xffff0000u);
+        }
+      }
+    }
+  }
 }
 
-// D / 8 lanes to a page, 8 channels each.
+__device__ __forceinline__ bool page_of(const SelectArgs& a, const int32_t* table, int j, int* p) {
+  *p = table[j];
+  const bool there = *p >= 0 && *p < a.c.pages;
+  if (!there) *p = 0;
+  return there;
+}
+
+// What every list begins and ends with; false if that is all of it.  `t` of
+// `n` threads.
+__device__ __forceinline__ bool list_ends(const SelectArgs& a, const Range& r, int32_t* list, int t, int n) {
+  const int count = min(r.total, a.keep);
+  if (t == 0) list[0] = count;
+  if (r.middle == 0) {
+    for (int i = t; i < a.keep; i += n) list[1 + i] = i < count ? i : -1;
+    return false;
+  }
+  for (int i = t; i < a.first; i += n) list[1 + i] = i;
+  for (int i = t; i < a.last; i += n) list[1 + a.keep - a.last + i] = r.total - a.last + i;
+  return a.keep - a.first - a.last > 0;
+}
+
+__device__ __forceinline__ uint32_t wave_or(uint32_t x) {
+#pragma unroll
+  for (int off = 1; off < 64; off <<= 1) x |= __shfl_xor(x, off);
+  return x;
+}
+
+// One wave: the pages of the `need` largest of n <= 64 C keys, ascending, to
+// out (page = base + index).  n > need.  The threshold is found bit by bit,
+// first among the keys' high words (from the first bit in which they differ),
+// then among the low words of those equal there; the search ends where exactly
+// as many keys lie above as are needed.
+template <int C>
+__device__ __forceinline__ void wave_top(const uint64_t* keys, int n, int need, int base, int32_t* out, int lane) {
+  uint32_t hi[C], lo[C];
+  uint32_t differ = 0;
+  const uint32_t some = (uint32_t)(keys[0] >> 32);
+#pragma unroll
+  for (int c = 0; c < C; ++c) {
+    const bool in = c * 64 + lane < n;
+    const uint64_t k = in ? keys[c * 64 + lane] : 0;
+    hi[c] = (uint32_t)(k >> 32);
+    lo[c] = (uint32_t)k;
+    differ |= in ? hi[c] ^ some : 0;
+  }
+  differ = __builtin_amdgcn_readfirstlane(wave_or(differ));
+  // The bits in front of the first difference are every key's; those behind the end are 0 and below.
+  int b = differ ? 31 - __builtin_clz(differ) : -1;
+  uint32_t th = b == 31 ? 0 : some & ~((2u << b) - 1u), tl = 0;
+  if (b < 0) th = some;
+  int left = need;       // places for keys whose high word is th
+  bool low = true;       // the low words decide
+  for (; b >= 0; --b) {
+    const uint32_t cand = th | (1u << b);
+    int cnt = 0;
+#pragma unroll
+    for (int c = 0; c < C; ++c) cnt += __popcll(__builtin_amdgcn_ballot_w64(hi[c] >= cand));
+    if (cnt >= need) {
+      th = cand;
+      if (cnt == need) {
+        low = false;
+        break;
+      }
+    }
+  }
+  if (low) {
+#pragma unroll
+    for (int c = 0; c < C; ++c) left -= __popcll(__builtin_amdgcn_ballot_w64(hi[c] > th));
+    for (int bl = 31; bl >= 0; --bl) {
+      const uint32_t cand = tl | (1u << bl);
+      int cnt = 0;
+#pragma unroll
+      for (int c = 0; c < C; ++c) cnt += __popcll(__builtin_amdgcn_ballot_w64(hi[c] == th && lo[c] >= cand));
+      if (cnt >= left) {
+        tl = cand;
+        if (cnt == left) break;
+      }
+    }
+  }
+  // Above the threshold, and of those at it the first ones.
+  int at_rest = need, at = 0;
+#pragma unroll
+  for (int c = 0; c < C; ++c)
+    at_rest -= __popcll(__builtin_amdgcn_ballot_w64(hi[c] > th || (low && hi[c] == th && lo[c] > tl)));
+  const uint64_t below = (1ull << lane) - 1;
+#pragma unroll
+  for (int c = 0; c < C; ++c) {
+    const bool in = c * 64 + lane < n;
+    const bool gt = hi[c] > th || (low && hi[c] == th && lo[c] > tl);
+    const bool eq = in && hi[c] == th && (!low || lo[c] == tl);
+    const uint64_t meq = __builtin_amdgcn_ballot_w64(eq);
+    const bool take = gt || (eq && __popcll(meq & below) < at_rest);
+    const uint64_t mt = __builtin_amdgcn_ballot_w64(take);
+    if (take) out[at + __popcll(mt & below)] = base + c * 64 + lane;
+    at += __popcll(mt);
+    at_rest -= min(at_rest, __popcll(meq));
+  }
+}
+
+__device__ __forceinline__ void wave_top_any(const uint64_t* keys, int n, int need, int base, int32_t* out, int lane) {
+  if (n <= 128) wave_top<2>(keys, n, need, base, out, lane);
+  else if (n <= 256) wave_top<4>(keys, n, need, base, out, lane);
+  else if (n <= 512) wave_top<8>(keys, n, need, base, out, lane);
+  else wave_top<16>(keys, n, need, base, out, lane);
+}
+
+// Ranking keys of pages j0, j0 + step, ... below `end` by one row's queries: D / 8 lanes to a page.
+template <int D, int UNROLL>
+__device__ __forceinline__ void score_pages(const SelectArgs& a, const int32_t* table, int h, const double (&q)[8],
+                                            int sub, int j0, int step, int end, uint64_t* keys) {
+  constexpr int LPP = D / 8;
+  for (int j = j0; j < end; j += step * UNROLL) {
+    u32x4 w[UNROLL];
+    bool there[UNROLL];
+    int p[UNROLL];
+#pragma unroll
+    for (int u = 0; u < UNROLL; ++u) there[u] = page_of(a, table, min(j + u * step, end - 1), &p[u]);
+#pragma unroll
+    for (int u = 0; u < UNROLL; ++u)
+      w[u] = *reinterpret_cast<const u32x4*>(a.c.kmean + ((int64_t)p[u] * a.c.kv_heads + h) * D + sub * 8);
+#pragma unroll
+    for (int u = 0; u < UNROLL; ++u) {
+      double s = 0.0;
+#pragma unroll
+      for (int c = 0; c < 4; ++c) {
+        s += q[2 * c] * (double)__uint_as_float(w[u][c] << 16);
+        s += q[2 * c + 1] * (double)__uint_as_float(w[u][c] & 0xffff0000u);
+      }
+#pragma unroll
+      for (int off = 1; off < LPP; off <<= 1) s += __shfl_xor(s, off);
+      if (sub == 0 && j + u * step < end) keys[j + u * step] = there[u] ? rank_key(s) : 0;
+    }
+  }
+}
+
+constexpr int kRowThreads = 512;
+
+template <int D, bool F32>
+__global__ __launch_bounds__(kRowThreads) void k_select_row(SelectArgs a) {
+  constexpr int LPP = D / 8;
+  __shared__ uint64_t s_keys[kSelectInLds];
+  const int lane = threadIdx.x & 63;
+  const int row = blockIdx.x / a.c.kv_heads, h = blockIdx.x % a.c.kv_heads;
+  double q[8];   // its loads go out before those that find the row's sequence
+  q_sum<F32, 8>(a, row, h, lane % LPP * 8, q);
+  const int seq = seq_of_row(a.b, row, lane);
+  if (seq >= a.b.seqs) return;
+  const SeqView sv = seq_view(a.b, a.c.page_log2, seq);
+  const int tok = row - sv.begin;
+  if (tok < 0 || tok >= sv.n) return;
+  const Range r = range_of(a, sv, tok);
+  int32_t* list = a.lists + ((int64_t)row * a.c.kv_heads + h) * (1 + a.keep);
+  if (!list_ends(a, r, list, threadIdx.x, kRowThreads)) return;
+  const int32_t* table = a.b.table + (int64_t)seq * a.b.max_pages + a.first;
+  score_pages<D, 4>(a, table, h, q, lane % LPP, threadIdx.x / LPP, kRowThreads / LPP, r.middle, s_keys);
+  __syncthreads();
+  if (threadIdx.x < 64)
+    wave_top_any(s_keys, r.middle, a.keep - a.first - a.last, a.first, list + 1 + a.first, lane);
+}
+
+// 16 tokens x all their pages.  A: the tokens' query sums, channels
+// g D/4 .. of lane group g; B: 16 pages' pooled keys, the same channels; a
+// lane gets the scores of tokens 4 i + g with page lane % 16.
+template <int D, bool F32, int CAP, bool LDS>
+__global__ __launch_bounds__(kRowThreads) void k_select_tile(SelectArgs a) {
+  constexpr int CH = D / 4, WAVES = kRowThreads / 64;
+  __shared__ uint64_t s_keys[LDS ? 16 * CAP : 1];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, n16 = lane & 15, g = lane >> 4;
+  unsigned id = blockIdx.x;
+  const int tile = id % a.tiles;
+  id /= a.tiles;
+  const int h = id % a.c.kv_heads, seq = id / a.c.kv_heads;
+  const SeqView sv = seq_view(a.b, a.c.page_log2, seq);
+  const int tok0 = tile * 16, last = min(min(sv.n, a.b.max_new), tok0 + 16) - 1;
+  if (last < tok0) return;
+  const int most = range_of(a, sv, last).middle;   // later tokens see more
+  if (most > 0 && a.keep > a.first + a.last) {
+    double q[CH];
+    q_sum<F32, CH>(a, sv.begin + min(tok0 + n16, last), h, g * CH, q);
+    const int32_t* table = a.b.table + (int64_t)seq * a.b.max_pages + a.first;
+    int middle[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) middle[i] = tok0 + 4 * i + g <= last ? range_of(a, sv, tok0 + 4 * i + g).middle : 0;
+    for (int j0 = (wave * gridDim.y + blockIdx.y) * 16; j0 < most; j0 += WAVES * 16 * gridDim.y) {
+      int p;
+      const bool there = page_of(a, table, min(j0 + n16, most - 1), &p);
+      const uint16_t* mean = a.c.kmean + ((int64_t)p * a.c.kv_heads + h) * D + g * CH;
+      u32x4 w[CH / 8];
+#pragma unroll
+      for (int c = 0; c < CH / 8; ++c) w[c] = *reinterpret_cast<const u32x4*>(mean + c * 8);
+      doublex4 s = {0.0, 0.0, 0.0, 0.0};
+#pragma unroll
+      for (int c = 0; c < CH; ++c) {
+        const uint32_t x = w[c / 8][(c % 8) / 2];
+        s = __builtin_amdgcn_mfma_f64_16x16x4f64(q[c], (double)__uint_as_float(c & 1 ? x & 0xffff0000u : x << 16), s, 0,
+                                                 0, 0);
+      }
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        if (j0 + n16 >= middle[i]) continue;
+        const uint64_t key = there ? rank_key(s[i]) : 0;
+        if (LDS) s_keys[(4 * i + g) * CAP + j0 + n16] = key;
+        else a.keys[((int64_t)(sv.begin + tok0 + 4 * i + g) * a.c.kv_heads + h) * a.b.max_pages + j0 + n16] = key;
+      }
+    }
+  }
+  if (!LDS) return;
+  __syncthreads();
+  for (int t = wave; t <= last - tok0; t += WAVES) {
+    const Range r = range_of(a, sv, tok0 + t);
+    int32_t* list = a.lists + ((int64_t)(sv.begin + tok0 + t) * a.c.kv_heads + h) * (1 + a.keep);
+    if (list_ends(a, r, list, lane, 64))
+      wave_top_any(&s_keys[t * CAP], r.middle, a.keep - a.first - a.last, a.first, list + 1 + a.first, lane);
+  }
+}
+
 template <int D, bool F32>
 __global__ __launch_bounds__(256) void k_select_scores(SelectArgs a) {
-  constexpr int LPP = D / 8, PPW = 64 / LPP;
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  constexpr int LPP = D / 8;
+  const int lane = threadIdx.x & 63;
   const int row = blockIdx.x / a.c.kv_heads, h = blockIdx.x % a.c.kv_heads;
   const int seq = seq_of_row(a.b, row, lane);
   if (seq >= a.b.seqs) return;
@@ -48,38 +301,20 @@ __global__ __launch_bounds__(256) void k_select_scores(SelectArgs a) {
   if (tok < 0 || tok >= sv.n) return;
   const Range r = range_of(a, sv, tok);
   if ((int)blockIdx.y * kSelectPages >= r.middle) return;
-  const int sub = lane % LPP;
   double q[8];
-#pragma unroll
-  for (int c = 0; c < 8; ++c) q[c] = 0.0;
-  for (int g = 0; g < a.group; ++g) {
-    const int64_t at = (int64_t)row * a.st + (int64_t)(h * a.group + g) * a.sh + sub * 8;
-#pragma unroll
-    for (int c = 0; c < 8; ++c) q[c] += q_at<F32>(a.q, at + c);
-  }
+  q_sum<F32, 8>(a, row, h, lane % LPP * 8, q);
   const int32_t* table = a.b.table + (int64_t)seq * a.b.max_pages + a.first;
   uint64_t* keys = a.keys + ((int64_t)row * a.c.kv_heads + h) * a.b.max_pages;
   for (int j0 = blockIdx.y * kSelectPages; j0 < r.middle; j0 += gridDim.y * kSelectPages)
-  for (int j = j0 + wave * PPW + lane / LPP, end = min(j0 + kSelectPages, r.middle); j < end; j += 4 * PPW) {
-    const int p = table[j];
-    const bool there = p >= 0 && p < a.c.pages;
-    const uint16_t* mean = a.c.kmean + ((int64_t)(there ? p : 0) * a.c.kv_heads + h) * D + sub * 8;
-    const u32x4 w = *reinterpret_cast<const u32x4*>(mean);
-    double s = 0.0;
-#pragma unroll
-    for (int c = 0; c < 4; ++c) {
-      s += q[2 * c] * (double)__uint_as_float(w[c] << 16);
-      s += q[2 * c + 1] * (double)__uint_as_float(w[c] & 0xffff0000u);
-    }
-#pragma unroll
-    for (int off = 1; off < LPP; off <<= 1) s += __shfl_xor(s, off);
-    if (sub == 0) keys[j] = there ? rank_key(s) : 0;
-  }
+    score_pages<D, kSelectPages * LPP / 256>(a, table, h, q, lane % LPP, j0 + threadIdx.x / LPP, 256 / LPP,
+                                             min(j0 + kSelectPages, r.middle), keys);
 }
 
 // One workgroup per (row, kv head): the `need` largest keys by radix, 8 bits a
 // pass, then their pages in ascending order.
-__global__ __launch_bounds__(256) void k_select_top(SelectArgs a) {
+constexpr int kTopThreads = 1024, kTopWaves = kTopThreads / 64, kTopRegs = 8;
+
+__global__ __launch_bounds__(kTopThreads) void k_select_top(SelectArgs a) {
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const int row = blockIdx.x / a.c.kv_heads, h = blockIdx.x % a.c.kv_heads;
   const int seq = seq_of_row(a.b, row, lane);
@@ -89,30 +324,48 @@ __global__ __launch_bounds__(256) void k_select_top(SelectArgs a) {
   if (tok < 0 || tok >= sv.n) return;
   const Range r = range_of(a, sv, tok);
   int32_t* list = a.lists + ((int64_t)row * a.c.kv_heads + h) * (1 + a.keep);
-  const int count = min(r.total, a.keep);
-  if (threadIdx.x == 0) list[0] = count;
-  if (r.middle == 0) {
-    for (int i = threadIdx.x; i < a.keep; i += 256) list[1 + i] = i < count ? i : -1;
-    return;
-  }
-  for (int i = threadIdx.x; i < a.first; i += 256) list[1 + i] = i;
-  for (int i = threadIdx.x; i < a.last; i += 256) list[1 + a.keep - a.last + i] = r.total - a.last + i;
+  if (!list_ends(a, r, list, threadIdx.x, kTopThreads)) return;
   const int need = a.keep - a.first - a.last;
-  if (need == 0) return;
-
   const uint64_t* keys = a.keys + ((int64_t)row * a.c.kv_heads + h) * a.b.max_pages;
+
+  // The first kTopRegs keys of each thread stay in registers.
+  uint64_t mine[kTopRegs];
+#pragma unroll
+  for (int i = 0; i < kTopRegs; ++i) {
+    const int j = i * kTopThreads + threadIdx.x;
+    mine[i] = j < r.middle ? keys[j] : 0;
+  }
   __shared__ int s_hist[256];
-  __shared__ int s_bin, s_left, s_wave[4];
+  __shared__ int s_bin, s_left, s_wave[kTopWaves];
   uint64_t prefix = 0;   // the threshold's high bits
   int left = need;       // places for keys that match the prefix
   int shift = 64;
+  // Keys share their high bytes, so lanes of a wave with the same digit add once.
+  auto count = [&](uint64_t k, bool in) {
+    const int digit = (int)((k >> shift) & 255);
+    bool todo = in && (shift == 56 || (k >> (shift + 8)) == (prefix >> (shift + 8)));
+#pragma unroll
+    for (int turn = 0; turn < 2; ++turn) {
+      const uint64_t m = __builtin_amdgcn_ballot_w64(todo);
+      if (!m) return;
+      const int first = __builtin_ctzll(m);
+      const bool same = todo && digit == __builtin_amdgcn_readlane(digit, first);
+      const uint64_t ms = __builtin_amdgcn_ballot_w64(same);
+      if (lane == first) atomicAdd(&s_hist[digit], __popcll(ms));
+      if (same) todo = false;
+    }
+    if (todo) atomicAdd(&s_hist[digit], 1);
+  };
   while (shift > 0) {
     shift -= 8;
-    s_hist[threadIdx.x] = 0;
+    if (threadIdx.x < 256) s_hist[threadIdx.x] = 0;
     __syncthreads();
-    for (int j = threadIdx.x; j < r.middle; j += 256) {
-      const uint64_t k = keys[j];
-      if (shift == 56 || (k >> (shift + 8)) == (prefix >> (shift + 8))) atomicAdd(&s_hist[(k >> shift) & 255], 1);
+#pragma unroll
+    for (int i = 0; i < kTopRegs; ++i)
+      if (i * kTopThreads < r.middle) count(mine[i], i * kTopThreads + (int)threadIdx.x < r.middle);
+    for (int j0 = kTopRegs * kTopThreads; j0 < r.middle; j0 += kTopThreads) {
+      const int j = j0 + threadIdx.x;
+      count(j < r.middle ? keys[j] : 0, j < r.middle);
     }
     __syncthreads();
     // Bins from the top: the one in which the `left`-th key lies.
@@ -148,7 +401,7 @@ __global__ __launch_bounds__(256) void k_select_top(SelectArgs a) {
   }
   // Taken: keys above the threshold's prefix, and of those equal to it the first `left`.
   int base = a.first, equal_before = 0;
-  for (int j0 = 0; j0 < r.middle; j0 += 256) {
+  for (int j0 = 0; j0 < r.middle; j0 += kTopThreads) {
     const int j = j0 + threadIdx.x;
     bool gt = false, eq = false;
     if (j < r.middle) {
@@ -156,40 +409,58 @@ __global__ __launch_bounds__(256) void k_select_top(SelectArgs a) {
       gt = k > t;
       eq = k == t;
     }
-    const uint64_t meq = __builtin_amdgcn_ballot_w64(eq);
-    if (lane == 0) s_wave[wave] = __popcll(meq);
+    // Equal and larger ones in front of this thread, counted together (16 bits each).
+    const uint64_t meq = __builtin_amdgcn_ballot_w64(eq), mgt = __builtin_amdgcn_ballot_w64(gt);
     __syncthreads();
-    int rank = equal_before + __popcll(meq & ((1ull << lane) - 1));
-    for (int w = 0; w < wave; ++w) rank += s_wave[w];
-    equal_before += s_wave[0] + s_wave[1] + s_wave[2] + s_wave[3];
+    if (lane == 0) s_wave[wave] = __popcll(meq) | (__popcll(mgt) << 16);
     __syncthreads();
+    const uint64_t below = (1ull << lane) - 1;
+    int before = __popcll(meq & below) | (__popcll(mgt & below) << 16), total = 0;
+    for (int w = 0; w < kTopWaves; ++w) {
+      if (w < wave) before += s_wave[w];
+      total += s_wave[w];
+    }
+    const int rank = equal_before + (before & 0xffff);
     const bool take = gt || (eq && rank < left);
-    const uint64_t mt = __builtin_amdgcn_ballot_w64(take);
-    if (lane == 0) s_wave[wave] = __popcll(mt);
-    __syncthreads();
-    int at = base + __popcll(mt & ((1ull << lane) - 1));
-    for (int w = 0; w < wave; ++w) at += s_wave[w];
-    if (take) list[1 + at] = a.first + j;
-    base += s_wave[0] + s_wave[1] + s_wave[2] + s_wave[3];
-    __syncthreads();
+    // Taken ones in front: all larger ones, and the equal ones that have a place.
+    if (take) list[1 + base + (before >> 16) + min(rank, left) - min(equal_before, left)] = a.first + j;
+    base += (total >> 16) + min(equal_before + (total & 0xffff), left) - min(equal_before, left);
+    equal_before += total & 0xffff;
   }
+}
+
+template <int D, bool F32>
+hipError_t launch(const SelectArgs& a, const SelectPlan& p, hipStream_t s) {
+  const unsigned rows = (unsigned)a.b.rows * a.c.kv_heads;
+  const unsigned tiles = (unsigned)a.b.seqs * a.c.kv_heads * a.tiles;
+  switch (p.kind) {
+    case kSelectRow:
+      k_select_row<D, F32><<<rows, kRowThreads, 0, s>>>(a);
+      break;
+    case kSelectTile:
+      if (a.b.max_pages <= 256) k_select_tile<D, F32, 256, true><<<tiles, kRowThreads, 0, s>>>(a);
+      else if (a.b.max_pages <= 512) k_select_tile<D, F32, 512, true><<<tiles, kRowThreads, 0, s>>>(a);
+      else k_select_tile<D, F32, kSelectInLds, true><<<tiles, kRowThreads, 0, s>>>(a);
+      break;
+    default: {
+      if (p.scored) {
+        if (p.kind == kSelectTileLong) k_select_tile<D, F32, 1, false><<<dim3(tiles, p.chunks), kRowThreads, 0, s>>>(a);
+        else k_select_scores<D, F32><<<dim3(rows, p.chunks), 256, 0, s>>>(a);
+        const hipError_t e = hipGetLastError();
+        if (e != hipSuccess) return e;
+      }
+      k_select_top<<<rows, kTopThreads, 0, s>>>(a);
+    }
+  }
+  return hipGetLastError();
 }
 
 }  // namespace
 
-hipError_t launch_cache_select(const SelectArgs& a, int dtype, hipStream_t s) {
-  const unsigned items = (unsigned)a.b.rows * a.c.kv_heads;
-  if (a.b.max_pages > a.keep) {
-    const dim3 grid(items, (unsigned)a.chunks);
-    const bool f32 = dtype == SSBA_DT_F32;
-    auto go = [&](auto k) { k<<<grid, 256, 0, s>>>(a); };
-    if (a.c.head_dim == 64) f32 ? go(k_select_scores<64, true>) : go(k_select_scores<64, false>);
-    else f32 ? go(k_select_scores<128, true>) : go(k_select_scores<128, false>);
-    const hipError_t e = hipGetLastError();
-    if (e != hipSuccess) return e;
-  }
-  k_select_top<<<items, 256, 0, s>>>(a);
-  return hipGetLastError();
+hipError_t launch_cache_select(const SelectArgs& a, const SelectPlan& p, int dtype, hipStream_t s) {
+  const bool f32 = dtype == SSBA_DT_F32;
+  if (a.c.head_dim == 64) return f32 ? launch<64, true>(a, p, s) : launch<64, false>(a, p, s);
+  return f32 ? launch<128, true>(a, p, s) : launch<128, false>(a, p, s);
 }
 
 }  // namespace ssba

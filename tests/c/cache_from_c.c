@@ -22,7 +22,7 @@ int main(void) {
   c.head_dim = 64;
   c.page = 16;
   b.seqs = 2;
-  b.max_pages = 4;
+  b.max_pages = 4000;
   b.rows = 2;
   b.max_new = 1;
   q.heads = 4;

@@ -104,11 +104,13 @@ def test_refusals_of_select(lib):
     for kw in (dict(keep=0), dict(first=-1), dict(last=0), dict(first=3, last=2), dict(first=2 ** 31 - 1)):
         assert select(lib, q=query(**kw)) == ARG, kw
     assert select(lib, lists=None) == ARG and select(lib, lists=P + 2) == ARG
-    assert select(lib, scratch=None) == ARG and select(lib, scratch=P + 8) == ARG
     assert select(lib, lists_bytes=4 * 3 * 2 * 5 - 1) == WORKSPACE
     size = ctypes.c_size_t(0)
-    assert lib.ssba_cache_select_workspace_size(cache(), batch(), query(), size) == OK
-    assert select(lib, bytes_=size.value - 1) == WORKSPACE
+    long = batch(max_pages=2048)
+    assert lib.ssba_cache_select_workspace_size(cache(), long, query(), size) == OK and size.value == 8 * 3 * 2 * 2048
+    assert select(lib, b=long, bytes_=size.value - 1) == WORKSPACE
+    assert select(lib, b=long, scratch=None) == ARG and select(lib, b=long, scratch=P + 8) == ARG
+    assert lib.ssba_cache_select_workspace_size(cache(), batch(), query(), size) == OK and size.value == 0
     assert select(lib, b=batch(rows=0), lists=None, scratch=None) == OK
     for kw, st in BAD_QUERY + [(dict(keep=0), ARG)]:
         assert lib.ssba_cache_select_workspace_size(cache(), batch(), query(**kw), size) == st, kw

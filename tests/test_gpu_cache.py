@@ -374,6 +374,12 @@ SELECTS = [  # page, D, heads, kv, dtype, causal, keep, first, last, sequences
     (16, 64, 2, 1, BF16, True, 9, 2, 3, [(5000, 2)]),                     # more pages than a workgroup takes at once
     (16, 128, 8, 2, F32, True, 300, 1, 1, [(9000, 1)]),
     (16, 64, 2, 2, BF16, True, 50, 1, 1, [(100, 5)]),                     # more places than the table has columns
+    (16, 128, 4, 2, BF16, True, 20, 1, 2, [(3000, 40), (9, 9), (100, 17), (5000, 16)]),   # tiles of 16 tokens
+    (16, 64, 3, 1, F32, False, 7, 2, 1, [(8000, 33), (640, 8)]),          # the same, half of the LDS
+    (32, 128, 2, 1, F32, True, 260, 1, 1, [(30000, 20)]),                 # 938 pages, 258 of them chosen
+    (16, 64, 2, 1, BF16, True, 5, 1, 1, [(17000, 1), (40, 1)]),           # too many pages for the LDS
+    (16, 128, 2, 1, BF16, True, 11, 1, 1, [(20000, 18), (500, 9)]),       # the same in tiles
+    (16, 64, 1, 1, BF16, True, 2000, 1, 1, [(150000, 1)]),                # more pages than registers of a workgroup
 ]
 
 
@@ -392,7 +398,9 @@ def test_select(page, d, heads, kv, dtype, causal, keep, first, last, seqs):
     assert np.array_equal(lists.cpu().numpy(), want)
 
 
-def test_select_ties_nan_and_missing_pages():
+@pytest.mark.parametrize("columns", [40, 300, 700, 1500])
+@pytest.mark.parametrize("max_new", [2, 8])
+def test_select_ties_nan_and_missing_pages(columns, max_new):
     """Equal scores keep the lower page, zeros of both signs are equal, NaN and missing pages come last; the hint
     and rows of no sequence do not matter."""
     from paper_2605_15684_amd import cache
@@ -404,7 +412,8 @@ def test_select_ties_nan_and_missing_pages():
     pool["kmean"][0, 5::9] = -0.0
     pool["kmean"][0, 7, 0, 3] = np.nan
     pool["kmean"][0, 11] = np.inf
-    table = np.arange(40, dtype=np.int32)[None].repeat(3, 0)
+    table = np.full((3, columns), -1, dtype=np.int32)        # the width of the table picks the kernel
+    table[:, :40] = np.arange(40)
     table[1, 5:20] = -1
     table[1, 21] = 40
     table[2, 3:39] = 77                                      # fewer pages there than places
@@ -412,7 +421,7 @@ def test_select_ties_nan_and_missing_pages():
     q, q64 = rounded(rng, (6, 4, d), BF16)
     lists = torch.full((6, kv, 1 + keep), -7, dtype=torch.int32, device="cuda")
     for hint in (None, 20):
-        cache.select(gpu_pool(pool), 0, gpu_batch((table, lens, cu), 2, hint), q.cuda(), keep=keep, lists=lists)
+        cache.select(gpu_pool(pool), 0, gpu_batch((table, lens, cu), max_new, hint), q.cuda(), keep=keep, lists=lists)
         with np.errstate(invalid="ignore"):
             want = C.select(pool, 0, (table, lens, cu), q64, page, keep)
         assert np.array_equal(lists.cpu().numpy(), want)
