@@ -101,14 +101,14 @@ struct AttendArgs {
 
 // What the attention launch does (ssba_cache_api.cpp decides).
 enum AttendKind {
-  kAttendFew,    // a workgroup per 16 R columns, its waves share the keys
-  kAttendMany,   // column groups of 64 (fp32: 16)
-  kAttendRow,    // lists: a workgroup per row and kv head, its waves share the keys
-  kAttendRows,   // lists: a wave per row and kv head
+  kAttendSeq,    // items: (sequence, kv head, column tile)
+  kAttendRow,    // lists; items: (row, kv head, column tile), the waves of a workgroup share the keys
+  kAttendRows,   // lists; a wave per such item
 };
 struct AttendPlan {
   AttendKind kind;
-  int tiles16;            // R: column tiles of 16 per wave
+  int tiles;              // tiles of 16 columns of an item
+  int threads;
   int col_tiles, splits;
   int64_t items;          // workgroups without the splits
 };

@@ -149,36 +149,51 @@ size_t select_scratch(const ssba_cache* c, const ssba_cache_batch* b, const ssba
 }
 
 // Items are independent (sequence or row, kv head, column tile); one workgroup
-// each, or several that share the item's keys where there are few.
+// each, or several that share the item's keys where there are few items.
 AttendPlan plan(const ssba_cache* c, const ssba_cache_batch* b, const ssba_cache_query* q, bool listed) {
   AttendPlan p;
   const int64_t group = q->heads / c->kv_heads;
   const int64_t cols = std::max<int64_t>(1, listed ? group : group * b->max_new);
   const bool f32 = q->dtype == SSBA_DT_F32;
   const int64_t keys = listed ? std::min<int64_t>((int64_t)q->keep * c->page, long_of(c, b)) : long_of(c, b);
-  p.splits = p.tiles16 = 1;
+  p.splits = p.tiles = 1;
+  p.threads = 256;
   if (listed) {
     p.col_tiles = (int)ceil_div(cols, 16);
     const int64_t items = (int64_t)b->rows * c->kv_heads * p.col_tiles;
     p.kind = items >= 4096 ? ssba::kAttendRows : ssba::kAttendRow;
     p.items = p.kind == ssba::kAttendRows ? ceil_div(b->rows, 4) * c->kv_heads * p.col_tiles : items;
   } else {
-    p.kind = cols > 64 ? ssba::kAttendMany : ssba::kAttendFew;
-    const bool many = p.kind == ssba::kAttendMany;
-    if (!f32) p.tiles16 = many ? 4 : cols <= 16 ? 1 : 2;
-    p.col_tiles = (int)ceil_div(cols, (many ? 64 : 16) * p.tiles16);
+    // As many columns to a workgroup as there are, up to 256 (fp32: 32): its waves read the keys once for all.
+    p.kind = ssba::kAttendSeq;
+    while (p.tiles < (f32 ? 2 : 16) && cols > 16 * p.tiles) p.tiles *= 2;
+    if (p.tiles >= 4) p.threads = 512;
+    p.col_tiles = (int)ceil_div(cols, 16 * p.tiles);
     p.items = (int64_t)b->seqs * c->kv_heads * p.col_tiles;
   }
-  if (p.kind == ssba::kAttendRow || p.kind == ssba::kAttendFew) {
+  const int64_t items = std::max<int64_t>(p.items, 1);
+  if (p.threads == 512) {
+    // One workgroup fills a CU.  Parts of at least 256 keys; as many as make
+    // the rounds over the 256 CUs fullest, each part counted as 1/16 round for
+    // writing and joining it.
+    double best = (double)ceil_div(items, 256);
+    for (int s = 2; s <= 256 && s * 256 <= keys; ++s) {
+      const double cost = (double)ceil_div(items * s, 256) / s + (items * s > 256 ? 0.0625 * s : 0.0);
+      if (cost < best * 0.95) {
+        best = cost;
+        p.splits = s;
+      }
+    }
+  } else if (p.kind != ssba::kAttendRows) {
     // 4 waves of at least 2 steps of 32 keys each, up to about 1024 workgroups.
     const int64_t most = std::max<int64_t>(1, std::min<int64_t>(256, keys / 256));
-    p.splits = (int)std::max<int64_t>(1, std::min<int64_t>(most, ceil_div(1024, std::max<int64_t>(p.items, 1))));
+    p.splits = (int)std::max<int64_t>(1, std::min<int64_t>(most, ceil_div(1024, items)));
   }
   return p;
 }
 
 // Columns of every part of a split launch.
-size_t part_columns(const AttendPlan& p) { return p.splits == 1 ? 0 : (size_t)p.items * p.splits * p.tiles16 * 16; }
+size_t part_columns(const AttendPlan& p) { return p.splits == 1 ? 0 : (size_t)p.items * p.splits * p.tiles * 16; }
 
 size_t attend_scratch(const ssba_cache* c, const AttendPlan& p) {
   return part_columns(p) * (c->head_dim + 2) * sizeof(float);
@@ -297,7 +312,7 @@ ssba_status ssba_cache_attend(const ssba_cache* c, int32_t layer, const ssba_cac
   if (need && (!scratch || !aligned(scratch, 16))) return SSBA_ERR_ARG;
   if (scratch_bytes < need || (lists && lists_bytes < (size_t)4 * b->rows * c->kv_heads * (1 + (size_t)q->keep)))
     return SSBA_ERR_WORKSPACE;
-  if (too_many(p.items * p.splits * 2) || too_many(p.items * p.tiles16 * 4)) return SSBA_ERR_UNSUPPORTED;
+  if (too_many(p.items * p.splits * 2) || too_many(p.items * p.tiles * 4)) return SSBA_ERR_UNSUPPORTED;
   a.c = view(c, layer);
   a.b = view(b);
   a.q = query;

@@ -168,12 +168,15 @@ __global__ __launch_bounds__(256) void k_cache_append(AppendArgs a) {
     inv[kv] = pow2(-e[kv]);
     restate[kv] = pow2(e0 - e[kv]);
     if (threadIdx.x == 0) scale[kv] = pow2(e[kv]);
-    if (infinite[kv]) {   // infinities take the largest code
+    if (infinite[kv]) {   // infinities take the largest code: scaled here, once and for all
 #pragma unroll
       for (int i = 0; i < 4; ++i)
 #pragma unroll
-        for (int c = 0; c < 8; ++c)
-          if (fabsf(x[kv][i][c]) == INFINITY) x[kv][i][c] = copysignf(448.f * pow2(e[kv]), x[kv][i][c]);
+        for (int c = 0; c < 8; ++c) {
+          const float y = x[kv][i][c] * inv[kv];
+          x[kv][i][c] = fabsf(y) > 448.f ? copysignf(448.f, y) : y;
+        }
+      inv[kv] = 1.f;
     }
   }
   const int64_t image = (int64_t)phys * a.c.page_bytes + (int64_t)h * page * D;

@@ -14,9 +14,12 @@
 // exact in bf16 (v_cvt_scalef32_pk_bf16_fp8).
 // The page numbers and scales of 64 groups are loaded at once, one group per
 // lane, and read back with v_readlane: no load waits on another in the loop.
-// The maximum m is raised only when a score exceeds it by 2^kSlack: p stays
-// below 2^kSlack, whose products and sums fp32 holds, and most steps need no
-// reduction across lanes.
+// No maximum is taken in most steps: a column's m stays until a lane's sum of
+// probabilities exceeds 2^20 (the scores have outgrown m), a column has none
+// yet or keys are masked; then m is raised and the step's probabilities are
+// formed again.  What m lags behind is harmless in fp32 and bf16.
+// bf16: V's page scale is added in the exponent (log2) instead of multiplying
+// every probability; the lane's sum is divided by it again.
 #include <hip/hip_runtime.h>
 #include <hip/hip_bf16.h>
 
@@ -31,7 +34,7 @@ typedef float floatx4 __attribute__((ext_vector_type(4)));
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 typedef uint32_t u32x4a4 __attribute__((ext_vector_type(4), aligned(4)));
 
-constexpr float kSlack = 16.0f;
+constexpr float kMost = 1048576.f;   // a lane's sum of probabilities of a step: 2^20
 constexpr int kNoKey = 0x40000000;   // first token of a group that is not there: behind every sequence
 
 union Frag {
@@ -140,7 +143,10 @@ __global__ __launch_bounds__(P::THREADS, P::R == 1 ? 3 : 2) void k_cache_attend(
   }
   const int split = id % a.splits;
   id /= a.splits;
-  const int ct = id % a.col_tiles;
+  int ct = id % a.col_tiles;
+  const unsigned first = id - ct;
+  if (a.causal) ct = a.col_tiles - 1 - ct;   // later tokens see more: their tiles start first
+  const unsigned item = first + ct;
   id /= a.col_tiles;
   Item it;
   it.h = id % a.c.kv_heads;
@@ -215,7 +221,7 @@ __global__ __launch_bounds__(P::THREADS, P::R == 1 ? 3 : 2) void k_cache_attend(
   const int32_t* table = a.b.table + (int64_t)it.seq * a.b.max_pages;
   const int64_t head_off = ((int64_t)it.h << page_log2) * D;
   int m_page = 0, m_key = 0;    // of group chunk * 64 + lane: page (-1: none) and first token
-  float m_ks = 1.f, m_vs = 1.f;
+  float m_ks = 1.f, m_vs = 1.f, m_lv = 0.f;   // its scales; log2 of V's
   auto load_chunk = [&](int chunk) {
     const int gr = chunk * 64 + lane;
     int page = -1, key = kNoKey;
@@ -238,14 +244,15 @@ __global__ __launch_bounds__(P::THREADS, P::R == 1 ? 3 : 2) void k_cache_attend(
     m_page = page;
     m_key = key;
     m_ks = ks * a.scale_log2;
-    m_vs = vs;
+    m_vs = P::F32 ? vs : 1.f / vs;
+    m_lv = P::F32 ? 0.f : __builtin_amdgcn_logf(vs);
   };
   int chunk = -1;   // 32 steps a chunk
 
   struct Step {
     u32x4 k[2][NH], v[2][NH];
     int key[2];
-    float ks[2], vs[2];
+    float ks[2], vs[2], lv[2];
     int64_t off[2];
   };
   // The group numbers, scales and K codes of step s, then its V codes.
@@ -261,6 +268,7 @@ __global__ __launch_bounds__(P::THREADS, P::R == 1 ? 3 : 2) void k_cache_attend(
       x.key[t] = lane_i(m_key, l);
       x.ks[t] = lane_f(m_ks, l);
       x.vs[t] = lane_f(m_vs, l);
+      if (!P::F32) x.lv[t] = lane_f(m_lv, l);
       const int sub = ((2 * s + t) & ((1 << gpp_log2) - 1)) * 16 * D;
       x.off[t] = (int64_t)max(page, 0) * a.c.page_bytes + head_off + sub;
       const uint8_t* kp_ = a.c.k + x.off[t];
@@ -328,6 +336,7 @@ __global__ __launch_bounds__(P::THREADS, P::R == 1 ? 3 : 2) void k_cache_attend(
       }
   };
 
+  bool settled = false;   // every column has a maximum
   auto finish = [&](Step& x) {
     // Some column does not see some key of this step.
     const bool edge = max(x.key[0], x.key[1]) + 16 > minlim;
@@ -341,47 +350,60 @@ __global__ __launch_bounds__(P::THREADS, P::R == 1 ? 3 : 2) void k_cache_attend(
             s[t][r][i] = x.key[t] + 4 * g + i < lim[r] ? s[t][r][i] * x.ks[t] : -INFINITY;
       x.ks[0] = x.ks[1] = 1.f;
     }
-    bool raise = false;
-    float top[R];
-#pragma unroll
-    for (int r = 0; r < R; ++r) {
-      float u[2];
-#pragma unroll
-      for (int t = 0; t < 2; ++t) {
-        u[t] = fmaxf(fmaxf(s[t][r][0], s[t][r][1]), fmaxf(s[t][r][2], s[t][r][3])) * x.ks[t];
-      }
-      top[r] = fmaxf(u[0], u[1]);
-      raise |= top[r] > m[r] + kSlack;
-    }
-    if (__builtin_amdgcn_ballot_w64(raise)) {
+    // Probabilities with the maximum so far, and each lane's sum of them.
+    Frag p[R][NP];
+    float sum[R];
+    bool high = false;
+    auto probabilities = [&]() {
 #pragma unroll
       for (int r = 0; r < R; ++r) {
-        float mx = fmaxf(top[r], __shfl_xor(top[r], 16));
+        const float mu = m[r] == -INFINITY ? 0.f : m[r];
+        float half[2];
+#pragma unroll
+        for (int t = 0; t < 2; ++t) {
+          // bf16: V's scale 2^lv goes into the exponent and out of the sum again.
+          const float shift = P::F32 ? mu : mu - x.lv[t];
+          half[t] = 0.f;
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            const float e = exp2_(__builtin_fmaf(s[t][r][i], x.ks[t], -shift));
+            half[t] = i ? half[t] + e : e;
+            __bf16 terms[NP];
+            split_bf16<NP>(P::F32 ? e * x.vs[t] : e, terms);
+#pragma unroll
+            for (int ns = 0; ns < NP; ++ns) p[r][ns].v[t * 4 + i] = terms[ns];
+          }
+        }
+        sum[r] = P::F32 ? half[0] + half[1] : __builtin_fmaf(half[0], x.vs[0], half[1] * x.vs[1]);
+        high |= sum[r] > kMost;
+      }
+    };
+    probabilities();
+    if (edge || !settled || __builtin_amdgcn_ballot_w64(high)) {
+      // Some column has no maximum yet, or has outgrown it.
+      bool none = false;
+#pragma unroll
+      for (int r = 0; r < R; ++r) {
+        float mx = -INFINITY;
+#pragma unroll
+        for (int t = 0; t < 2; ++t)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) mx = fmaxf(mx, s[t][r][i] * x.ks[t]);
+        mx = fmaxf(mx, __shfl_xor(mx, 16));
         mx = fmaxf(mx, __shfl_xor(mx, 32));
         const float to = fmaxf(m[r], mx);
         const float f = to > m[r] ? exp2_(m[r] - to) : 1.f;
         m[r] = to;
+        none |= to == -INFINITY && lim[r] > 0;
         l[r] *= f;
 #pragma unroll
         for (int c = 0; c < NC; ++c) o[r][c] *= f;
       }
+      settled = !__builtin_amdgcn_ballot_w64(none);
+      probabilities();
     }
-    Frag p[R][NP];
 #pragma unroll
-    for (int r = 0; r < R; ++r) {
-      const float mu = m[r] == -INFINITY ? 0.f : m[r];
-#pragma unroll
-      for (int t = 0; t < 2; ++t)
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          const float e = exp2_(__builtin_fmaf(s[t][r][i], x.ks[t], -mu));
-          l[r] += e;
-          __bf16 terms[NP];
-          split_bf16<NP>(e * x.vs[t], terms);
-#pragma unroll
-          for (int ns = 0; ns < NP; ++ns) p[r][ns].v[t * 4 + i] = terms[ns];
-        }
-    }
+    for (int r = 0; r < R; ++r) l[r] += sum[r];
     if (edge) {
       // What no column sees may hold anything: its codes become 0, so that a
       // zero probability times them is 0.  A NaN that some columns see and
@@ -400,14 +422,17 @@ __global__ __launch_bounds__(P::THREADS, P::R == 1 ? 3 : 2) void k_cache_attend(
           }
       }
       if (__builtin_amdgcn_ballot_w64(some != 0)) {
+        // 1 where a column sees a key, times 1 where the key's value is NaN (bit
+        // arithmetic: comparisons would take a scalar register pair each).
+        constexpr uint32_t kOne = 0x3f80;   // bf16
         Frag sees[R];
 #pragma unroll
         for (int r = 0; r < R; ++r)
 #pragma unroll
-          for (int t = 0; t < 2; ++t)
-#pragma unroll
-            for (int i = 0; i < 4; ++i)
-              sees[r].v[t * 4 + i] = (__bf16)(x.key[t] + 4 * g + i < lim[r] ? 1.f : 0.f);
+          for (int w = 0; w < 4; ++w) {
+            const int k = x.key[w >> 1] + 4 * g + (w & 1) * 2 - lim[r];   // negative: seen
+            sees[r].u[w] = ((uint32_t)(k >> 31) & kOne) | ((uint32_t)((k + 1) >> 31) & (kOne << 16));
+          }
 #pragma unroll
         for (int hh = 0; hh < NH; ++hh)
 #pragma unroll
@@ -415,24 +440,25 @@ __global__ __launch_bounds__(P::THREADS, P::R == 1 ? 3 : 2) void k_cache_attend(
             Frag bad;
 #pragma unroll
             for (int t = 0; t < 2; ++t) {
-              uint32_t w = x.v[t][hh][e];
+              const uint32_t w = x.v[t][hh][e];
               const uint32_t nan = (((w & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u) >> 7;
-              w &= ~(nan * 0xffu);
-              x.v[t][hh][e] = w;
-#pragma unroll
-              for (int i = 0; i < 4; ++i) bad.v[t * 4 + i] = (__bf16)((nan >> (8 * i)) & 1u ? 1.f : 0.f);
+              x.v[t][hh][e] = w & ~(nan * 0xffu);
+              bad.u[2 * t] = ((nan & 1u) | ((nan & 0x100u) << 8)) * kOne;
+              bad.u[2 * t + 1] = ((nan >> 16 & 1u) | (nan >> 8 & 0x10000u)) * kOne;
             }
 #pragma unroll
             for (int r = 0; r < R; ++r) {
               const floatx4 zero = {0.f, 0.f, 0.f, 0.f};
               const floatx4 hit = __builtin_amdgcn_mfma_f32_16x16x32_bf16(bad.v, sees[r].v, zero, 0, 0, 0);
 #pragma unroll
-              for (int i = 0; i < 4; ++i)
-                if (hit[i] > 0.f) o[r][hh * 4 + e][i] = NAN;
+              for (int i = 0; i < 4; ++i)   // hit is 0 or at least 1
+                o[r][hh * 4 + e][i] = __uint_as_float(__float_as_uint(o[r][hh * 4 + e][i]) |
+                                                      ((uint32_t)(-__float_as_int(hit[i]) >> 31) & 0x7fc00000u));
             }
           }
       }
     }
+    if (P::QLDS) __builtin_amdgcn_s_setprio(1);
 #pragma unroll
     for (int hh = 0; hh < NH; ++hh)
 #pragma unroll
@@ -457,7 +483,11 @@ __global__ __launch_bounds__(P::THREADS, P::R == 1 ? 3 : 2) void k_cache_attend(
   if (s0 < s1) fetch_k(s0, x);
   for (int st = s0; st < s1; ++st) {
     fetch_v(x);
+    // The wave in its products goes first, so that the other of its SIMD has
+    // its softmax under them.
+    if (P::QLDS) __builtin_amdgcn_s_setprio(1);
     scores(x);
+    if (P::QLDS) __builtin_amdgcn_s_setprio(0);
     Step y = x;
     if (st + 1 < s1) fetch_k(st + 1, x);
     finish(y);
@@ -488,7 +518,7 @@ __global__ __launch_bounds__(P::THREADS, P::R == 1 ? 3 : 2) void k_cache_attend(
   // The shares of the waves that split the keys, 16 columns at a time: every
   // wave puts its O, scaled to the common maximum, into the LDS and TPC
   // threads a column add them up.
-  constexpr int LD = D + 4, TPC = 4 * P::KP, E = D / TPC;
+  constexpr int LD = D + 4, TPC = 4 * P::KP < D / 4 ? 4 * P::KP : D / 4, E = D / TPC;
   __shared__ float s_o[P::KP > 1 ? P::CG * P::KP * 16 * LD : 1];
   __shared__ float s_m[P::CG][P::KP][16], s_l[P::CG][P::KP][16];
   const int col = threadIdx.x / TPC, ocg = col >> 4, c16 = col & 15, ch = (threadIdx.x % TPC) * E;
@@ -510,6 +540,7 @@ __global__ __launch_bounds__(P::THREADS, P::R == 1 ? 3 : 2) void k_cache_attend(
       *reinterpret_cast<floatx4*>(&s_o[((cg * P::KP + kp) * 16 + n16) * LD + c * 16 + g * 4]) = w;
     }
     __syncthreads();
+    if (ocg >= P::CG) continue;   // more threads than 4 channels each need
     float cm = s_m[ocg][0][c16];
 #pragma unroll
     for (int w = 1; w < P::KP; ++w) cm = fmaxf(cm, s_m[ocg][w][c16]);
@@ -526,7 +557,7 @@ __global__ __launch_bounds__(P::THREADS, P::R == 1 ? 3 : 2) void k_cache_attend(
     if (cc >= it.ncols) continue;
     if (a.splits > 1) {
       // [item][split][column][D] and the same with (m, l)
-      const int64_t slot = ((int64_t)blockIdx.x * R + r) * 16 + c16;
+      const int64_t slot = (((int64_t)item * a.splits + split) * (P::CG * R) + ocg * R + r) * 16 + c16;
       float* to = a.part + slot * D;
 #pragma unroll
       for (int e = 0; e < E; e += 4)
@@ -550,7 +581,8 @@ __global__ __launch_bounds__(P::THREADS, P::R == 1 ? 3 : 2) void k_cache_attend(
 // them every second part.
 constexpr int kMaxSplits = 256;
 
-template <int D, int R, bool F32, bool LISTED>
+// RC: tiles of 16 columns of an item.
+template <int D, int RC, bool F32, bool LISTED>
 __global__ __launch_bounds__(256) void k_cache_join(AttendArgs a) {
   __shared__ float s_w[kMaxSplits][16];
   __shared__ float s_sum[16];
@@ -558,17 +590,17 @@ __global__ __launch_bounds__(256) void k_cache_join(AttendArgs a) {
   unsigned id = blockIdx.x;
   const int ch32 = id % (D / 32);
   id /= D / 32;
-  const int r = id % R;
-  id /= R;
+  const int r = id % RC;
+  id /= RC;
   const unsigned item = id;
   const int ct = id % a.col_tiles;
   id /= a.col_tiles;
   Item it;
   it.h = id % a.c.kv_heads;
   if (!item_of<LISTED>(a, id / a.c.kv_heads, threadIdx.x & 63, &it)) return;
-  const int c0 = ct * 16 * R + r * 16;
+  const int c0 = ct * 16 * RC + r * 16;
   if (c0 >= it.ncols) return;
-  const int64_t slot0 = ((int64_t)item * a.splits * R + r) * 16;   // part s: + s * R * 16
+  const int64_t slot0 = ((int64_t)item * a.splits * RC + r) * 16;   // part s: + s * RC * 16
   {
     // 16 threads a column: maximum, weights and sum over the parts.
     const int c = threadIdx.x >> 4, j = threadIdx.x & 15;
@@ -576,16 +608,16 @@ __global__ __launch_bounds__(256) void k_cache_join(AttendArgs a) {
     const bool in = c0 + c < it.ncols;
     float m = -INFINITY;
     if (in)
-      for (int s = j; s < a.splits; s += 16) m = fmaxf(m, ml[(int64_t)s * R * 32]);
+      for (int s = j; s < a.splits; s += 16) m = fmaxf(m, ml[(int64_t)s * RC * 32]);
 #pragma unroll
     for (int x = 1; x < 16; x <<= 1) m = fmaxf(m, __shfl_xor(m, x));
     float sum = 0.f;
     if (in)
       for (int s = j; s < a.splits; s += 16) {
-        const float ms = ml[(int64_t)s * R * 32];
+        const float ms = ml[(int64_t)s * RC * 32];
         const float w = ms == m ? 1.f : exp2_(ms - m);
         s_w[s][c] = w;
-        sum += w * ml[(int64_t)s * R * 32 + 1];
+        sum += w * ml[(int64_t)s * RC * 32 + 1];
       }
 #pragma unroll
     for (int x = 1; x < 16; x <<= 1) sum += __shfl_xor(sum, x);
@@ -599,7 +631,7 @@ __global__ __launch_bounds__(256) void k_cache_join(AttendArgs a) {
     const float* part = a.part + (slot0 + c) * D + ch;
 #pragma unroll 8
     for (int s = half; s < a.splits; s += 2)
-      acc += *reinterpret_cast<const floatx4*>(part + (int64_t)s * R * 16 * D) * s_w[s][c];
+      acc += *reinterpret_cast<const floatx4*>(part + (int64_t)s * RC * 16 * D) * s_w[s][c];
   }
   if (half) s_acc[t] = acc;
   __syncthreads();
@@ -615,13 +647,15 @@ hipError_t launch(const AttendArgs& a, const AttendPlan& p, hipStream_t s) {
   k_cache_attend<P><<<(unsigned)(p.items * p.splits), P::THREADS, 0, s>>>(a);
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess || p.splits == 1) return e;
-  k_cache_join<P::D, P::R, P::F32, P::LISTED><<<(unsigned)(p.items * P::R * (P::D / 32)), 256, 0, s>>>(a);
+  constexpr int RC = P::LISTED ? P::R : P::CG * P::R;
+  k_cache_join<P::D, RC, P::F32, P::LISTED><<<(unsigned)(p.items * RC * (P::D / 32)), 256, 0, s>>>(a);
   return hipGetLastError();
 }
 
 template <int D>
 hipError_t launch_d(const AttendArgs& a, const AttendPlan& p, int dtype, hipStream_t s) {
   const bool f32 = dtype == SSBA_DT_F32;
+  // D, R, NQ, NP, fp32, lists, column groups, waves that share keys, queries in the LDS
   switch (p.kind) {
     case kAttendRows:
       return f32 ? launch<Shape<D, 1, 3, 3, true, true, 4, 1, false>>(a, p, s)
@@ -629,13 +663,17 @@ hipError_t launch_d(const AttendArgs& a, const AttendPlan& p, int dtype, hipStre
     case kAttendRow:
       return f32 ? launch<Shape<D, 1, 3, 3, true, true, 1, 4, false>>(a, p, s)
                  : launch<Shape<D, 1, 1, 2, false, true, 1, 4, false>>(a, p, s);
-    case kAttendFew:
-      if (f32) return launch<Shape<D, 1, 3, 3, true, false, 1, 4, false>>(a, p, s);
-      return p.tiles16 == 1 ? launch<Shape<D, 1, 1, 2, false, false, 1, 4, false>>(a, p, s)
-                            : launch<Shape<D, 2, 1, 1, false, false, 1, 4, false>>(a, p, s);
     default:
-      return f32 ? launch<Shape<D, 1, 3, 3, true, false, 4, 1, false>>(a, p, s)
-                 : launch<Shape<D, 4, 1, 1, false, false, 4, 2, true>>(a, p, s);
+      if (f32)
+        return p.tiles == 1 ? launch<Shape<D, 1, 3, 3, true, false, 1, 4, false>>(a, p, s)
+                            : launch<Shape<D, 1, 3, 3, true, false, 2, 2, false>>(a, p, s);
+      switch (p.tiles) {
+        case 1: return launch<Shape<D, 1, 1, 2, false, false, 1, 4, false>>(a, p, s);
+        case 2: return launch<Shape<D, 2, 1, 1, false, false, 1, 4, false>>(a, p, s);
+        case 4: return launch<Shape<D, 4, 1, 1, false, false, 1, 8, true>>(a, p, s);
+        case 8: return launch<Shape<D, 4, 1, 1, false, false, 2, 4, true>>(a, p, s);
+        default: return launch<Shape<D, 4, 1, 1, false, false, 4, 2, true>>(a, p, s);
+      }
   }
 }
 

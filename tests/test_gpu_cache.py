@@ -95,7 +95,7 @@ def test_append_extreme_values():
     k[16:32] = float("inf")
     k[32:48] = 0.0
     k[33, 0, 1], k[34, 0, 1] = 1e-45, -1e-38
-    k[48, 0, 0], k[49, 0, 1], k[50] = 3.4028234e38, -3.4028234e38, 1e30
+    k[48, 0, 0], k[49, 0, 1], k[50], k[51, 0, 3] = 3.4028234e38, -3.4028234e38, 1e30, float("inf")
     v = -k
     pool = make_pool(rng, 1, 4, kv, d, page)
     gpool = gpu_pool(pool)
@@ -152,6 +152,9 @@ ATTENDS = [  # page, D, heads, kv heads, dtype, causal, sequences
     (32, 128, 8, 2, BF16, False, [(300, 12), (12, 12), (77, 1)]),         # four
     (64, 128, 4, 2, BF16, True, [(200, 130), (70, 70), (300, 64)]),       # by columns
     (16, 64, 3, 1, BF16, False, [(333, 100), (22, 22)]),
+    (16, 64, 12, 4, BF16, True, [(3000, 20), (40, 17), (333, 5)]),        # 64 columns, keys shared by 8 waves and split
+    (32, 128, 8, 2, BF16, False, [(2000, 25), (60, 32)]),                 # 128 columns, keys split
+    (64, 64, 6, 1, BF16, True, [(1500, 90), (600, 600)]),                 # tiles of 256 columns
     (64, 128, 5, 1, F32, True, [(1, 1), (700, 1)]),
     (16, 64, 6, 2, F32, True, [(50, 7), (7, 7), (129, 2)]),
     (32, 128, 4, 2, F32, False, [(150, 60), (64, 33)]),
