@@ -53,14 +53,22 @@ def _call(pool, fn, name: str, *args) -> None:
         _lib.check(st, name)
 
 
-def _check(t, shape, dtype, dev, what: str) -> None:
-    """A contiguous GPU tensor of `dtype` (and of `shape`, on `dev`, where given)."""
-    if not (isinstance(t, torch.Tensor) and t.is_cuda and t.dtype == dtype and t.is_contiguous()
-            and (shape is None or t.shape == shape)):
-        raise ValueError(f"{what}: expected a contiguous {dtype} GPU tensor" +
-                         (f" of shape {tuple(shape)}" if shape is not None else ""))
-    if dev is not None and t.device != dev:
+def _check(t, shape, dtype, index, what: str) -> None:
+    """A contiguous tensor of `dtype` on GPU `index`, of `shape` where given."""
+    if isinstance(t, torch.Tensor) and t.dtype is dtype and t.get_device() == index and t.is_contiguous() and \
+            (shape is None or t.shape == shape):
+        return
+    if isinstance(t, torch.Tensor) and t.is_cuda and t.get_device() != index:
         raise ValueError(f"{what}: all tensors must be on one device")
+    raise ValueError(f"{what}: expected a contiguous {dtype} GPU tensor" +
+                     (f" of shape {tuple(shape)}" if shape is not None else ""))
+
+
+def _gpu_of(t, dims: int, what: str) -> int:
+    """The GPU of a tensor of `dims` dimensions."""
+    if not isinstance(t, torch.Tensor) or not t.is_cuda or t.dim() != dims:
+        raise ValueError(f"{what}: expected a GPU tensor of {dims} dimensions")
+    return t.get_device()
 
 
 class PagedCache:
@@ -68,22 +76,25 @@ class PagedCache:
     [layers, pages, kv_heads, 2], kmean bf16 [layers, pages, kv_heads, D] (byte order of the pages:
     include/ssba_cache.h).  Holds references to the tensors, copies nothing."""
 
+    __slots__ = ("k", "v", "scale", "kmean", "device", "index", "layers", "pages", "kv_heads", "head_dim", "page", "desc")
+
     def __init__(self, k: torch.Tensor, v: torch.Tensor, scale: torch.Tensor, kmean: torch.Tensor):
-        if not isinstance(k, torch.Tensor) or k.dim() != 4 or not isinstance(kmean, torch.Tensor) or kmean.dim() != 4:
-            raise ValueError("k and kmean: expected [layers, pages, kv_heads, ...] tensors")
-        shape, dev = k.shape, k.device
+        index = _gpu_of(k, 4, "k")
+        _gpu_of(kmean, 4, "kmean")
+        shape = k.shape
         layers, pages, kv_heads, size = shape
         d = kmean.shape[3]
-        _check(k, None, E4M3, None, "k")
-        _check(v, shape, E4M3, dev, "v")
-        _check(scale, (layers, pages, kv_heads, 2), torch.float32, dev, "scale")
-        _check(kmean, (layers, pages, kv_heads, d), torch.bfloat16, dev, "kmean")
+        _check(k, None, E4M3, index, "k")
+        _check(v, shape, E4M3, index, "v")
+        _check(scale, (layers, pages, kv_heads, 2), torch.float32, index, "scale")
+        _check(kmean, (layers, pages, kv_heads, d), torch.bfloat16, index, "kmean")
         if d < 1 or size % d:
             raise ValueError("k: the last dimension must be page * D")
-        self.k, self.v, self.scale, self.kmean, self.device, self.index = k, v, scale, kmean, dev, dev.index
-        self.layers, self.pages, self.kv_heads, self.head_dim, self.page = layers, pages, kv_heads, d, size // d
-        self.desc = _lib.CacheDesc(layers, pages, kv_heads, d, size // d, k.data_ptr(), v.data_ptr(),
-                                   scale.data_ptr(), kmean.data_ptr())
+        page = size // d
+        self.k, self.v, self.scale, self.kmean, self.device, self.index = k, v, scale, kmean, k.device, index
+        self.layers, self.pages, self.kv_heads, self.head_dim, self.page = layers, pages, kv_heads, d, page
+        self.desc = _lib.CacheDesc(layers, pages, kv_heads, d, page, k.data_ptr(), v.data_ptr(), scale.data_ptr(),
+                                   kmean.data_ptr())
 
 
 class Batch:
@@ -91,16 +102,16 @@ class Batch:
     included), cu int32 [seqs + 1] (the new tokens' rows in the packed arrays).  max_new: at least the new
     tokens of any sequence; max_len: about the longest sequence (work is split by it; results are not)."""
 
+    __slots__ = ("table", "lens", "cu", "index", "_desc")
+
     def __init__(self, table: torch.Tensor, lens: torch.Tensor, cu: torch.Tensor, max_new: int,
                  max_len: Optional[int] = None):
-        if not isinstance(table, torch.Tensor) or table.dim() != 2:
-            raise ValueError("table: expected a [seqs, max_pages] tensor")
+        index = _gpu_of(table, 2, "table")
         seqs, max_pages = table.shape
-        dev = table.device
-        _check(table, None, torch.int32, None, "table")
-        _check(lens, (seqs,), torch.int32, dev, "lens")
-        _check(cu, (seqs + 1,), torch.int32, dev, "cu")
-        self.table, self.lens, self.cu, self.device = table, lens, cu, dev
+        _check(table, None, torch.int32, index, "table")
+        _check(lens, (seqs,), torch.int32, index, "lens")
+        _check(cu, (seqs + 1,), torch.int32, index, "cu")
+        self.table, self.lens, self.cu, self.index = table, lens, cu, index
         self._desc = (seqs, max_pages, int(max_new), int(max_len or 0), table.data_ptr(), lens.data_ptr(),
                       cu.data_ptr())
 
@@ -129,7 +140,7 @@ def _packed(t, rows, heads, pool: PagedCache, dtype, what: str):
     """Checks a packed [rows, heads, D] tensor (rows, heads, dtype None: any); its (token, head) strides."""
     if not (isinstance(t, torch.Tensor) and t.is_cuda and t.dim() == 3 and t.dtype in _DTYPES):
         raise ValueError(f"{what}: expected a [tokens, heads, D] GPU tensor, bf16 or fp32")
-    if t.device != pool.device:
+    if t.get_device() != pool.index:
         raise ValueError(f"{what}: all tensors must be on one device")
     if dtype is not None and t.dtype != dtype:
         raise ValueError(f"{what}: expected {dtype}")
@@ -149,7 +160,7 @@ def _packed(t, rows, heads, pool: PagedCache, dtype, what: str):
 
 
 def _same_device(pool: PagedCache, batch: Batch) -> None:
-    if pool.device != batch.device:
+    if pool.index != batch.index:
         raise ValueError("cache and batch must be on one device")
 
 
@@ -164,15 +175,15 @@ def append(pool: PagedCache, layer: int, batch: Batch, k: torch.Tensor, v: torch
           k.data_ptr(), v.data_ptr(), *strides)
 
 
-def _scratch(size: int, given, dev):
+def _scratch(size: int, given, pool):
     """(tensor to keep alive, address, bytes) of a workspace."""
     if given is not None:
-        if not (isinstance(given, torch.Tensor) and given.is_cuda and given.is_contiguous() and given.device == dev):
+        if not (isinstance(given, torch.Tensor) and given.get_device() == pool.index and given.is_contiguous()):
             raise ValueError("scratch must be a contiguous GPU tensor on the cache's device")
         return given, given.data_ptr(), given.numel() * given.element_size()
     if size == 0:
         return None, None, 0
-    t = torch.empty(size, dtype=torch.uint8, device=dev)
+    t = torch.empty(size, dtype=torch.uint8, device=pool.device)
     return t, t.data_ptr(), size
 
 
@@ -191,8 +202,8 @@ def select(pool: PagedCache, layer: int, batch: Batch, q: torch.Tensor, *, keep:
     if lists is None:
         lists = torch.empty((rows, pool.kv_heads, 1 + keep), dtype=torch.int32, device=pool.device)
     else:
-        _check(lists, (rows, pool.kv_heads, 1 + keep), torch.int32, pool.device, "lists")
-    alive, at, have = _scratch(size.value, scratch, pool.device)
+        _check(lists, (rows, pool.kv_heads, 1 + keep), torch.int32, pool.index, "lists")
+    alive, at, have = _scratch(size.value, scratch, pool)
     _call(pool, _L.ssba_cache_select, "ssba_cache_select", pool.desc, layer, b, desc, q.data_ptr(), lists.data_ptr(),
           lists.numel() * 4, at, have)
     return lists
@@ -216,7 +227,7 @@ def attend(pool: PagedCache, layer: int, batch: Batch, q: torch.Tensor, *, lists
         if not (isinstance(lists, torch.Tensor) and lists.dim() == 3 and lists.shape[2] > 1):
             raise ValueError("lists: expected [tokens, kv_heads, 1 + keep]")
         keep = lists.shape[2] - 1
-        _check(lists, (rows, pool.kv_heads, 1 + keep), torch.int32, pool.device, "lists")
+        _check(lists, (rows, pool.kv_heads, 1 + keep), torch.int32, pool.index, "lists")
         lp, lb = lists.data_ptr(), lists.numel() * 4
     b = batch.desc(rows)
     desc = _lib.CacheQuery(heads, _DTYPES[q.dtype], 1 if causal else 0, keep, 0, 0,
@@ -224,37 +235,36 @@ def attend(pool: PagedCache, layer: int, batch: Batch, q: torch.Tensor, *, lists
     size = ctypes.c_size_t(0)
     _lib.check(_L.ssba_cache_attend_workspace_size(pool.desc, b, desc, 0 if lists is None else 1, size),
                "ssba_cache_attend_workspace_size")
-    alive, at, have = _scratch(size.value, scratch, pool.device)
+    alive, at, have = _scratch(size.value, scratch, pool)
     _call(pool, _L.ssba_cache_attend, "ssba_cache_attend", pool.desc, layer, b, desc, q.data_ptr(), lp, lb,
           out.data_ptr(), at, have)
     return out
 
 
 def _rows(pool: PagedCache, table, lens, refs) -> _lib.CachePages:
-    if not isinstance(table, torch.Tensor) or table.dim() != 2:
-        raise ValueError("table: expected a [rows, max_pages] tensor")
-    _check(table, None, torch.int32, pool.device, "table")
-    _check(lens, (table.shape[0],), torch.int32, pool.device, "lens")
-    _check(refs, (pool.pages,), torch.int32, pool.device, "refs")
+    _gpu_of(table, 2, "table")
+    _check(table, None, torch.int32, pool.index, "table")
+    _check(lens, (table.shape[0],), torch.int32, pool.index, "lens")
+    _check(refs, (pool.pages,), torch.int32, pool.index, "refs")
     return _lib.CachePages(table.shape[0], table.shape[1], table.data_ptr(), lens.data_ptr(), refs.data_ptr())
 
 
 def _pages_scratch(pool: PagedCache, desc, n: int, given):
     size = ctypes.c_size_t(0)
     _lib.check(_L.ssba_pages_workspace_size(pool.desc, desc, n, size), "ssba_pages_workspace_size")
-    return _scratch(size.value, given, pool.device)
+    return _scratch(size.value, given, pool)
 
 
 def _info(pool: PagedCache, given) -> torch.Tensor:
     if given is None:
         return torch.empty(2, dtype=torch.int32, device=pool.device)
-    _check(given, (2,), torch.int32, pool.device, "info")
+    _check(given, (2,), torch.int32, pool.index, "info")
     return given
 
 
 def _numbers(pool: PagedCache, t, n, what: str) -> int:
     """Checks a vector of row or page numbers (of length n, if given); its length."""
-    _check(t, None, torch.int32, pool.device, what)
+    _check(t, None, torch.int32, pool.index, what)
     if t.dim() != 1 or (n is not None and t.shape[0] != n):
         raise ValueError(f"{what}: expected a vector" + (f" of {n}" if n is not None else ""))
     return t.shape[0]
@@ -298,15 +308,14 @@ def compact(pool: PagedCache, table, refs, table_out=None, refs_out=None, info=N
     """Moves the pages in use to the low end of the pool.  Returns (table, refs, info) after it, info = {pages in
     use, pages moved}; table_out and refs_out may be table and refs themselves."""
     # lens takes no part: its place is filled by another array
-    if not isinstance(table, torch.Tensor) or table.dim() != 2:
-        raise ValueError("table: expected a [rows, max_pages] tensor")
-    _check(table, None, torch.int32, pool.device, "table")
-    _check(refs, (pool.pages,), torch.int32, pool.device, "refs")
+    _gpu_of(table, 2, "table")
+    _check(table, None, torch.int32, pool.index, "table")
+    _check(refs, (pool.pages,), torch.int32, pool.index, "refs")
     desc = _lib.CachePages(table.shape[0], table.shape[1], table.data_ptr(), refs.data_ptr(), refs.data_ptr())
     table_out = torch.empty_like(table) if table_out is None else table_out
     refs_out = torch.empty_like(refs) if refs_out is None else refs_out
-    _check(table_out, table.shape, torch.int32, pool.device, "table_out")
-    _check(refs_out, refs.shape, torch.int32, pool.device, "refs_out")
+    _check(table_out, table.shape, torch.int32, pool.index, "table_out")
+    _check(refs_out, refs.shape, torch.int32, pool.index, "refs_out")
     info = _info(pool, info)
     alive, at, have = _pages_scratch(pool, desc, 0, scratch)
     _call(pool, _L.ssba_pages_compact, "ssba_pages_compact", pool.desc, desc, table_out.data_ptr(),
@@ -317,7 +326,7 @@ def compact(pool: PagedCache, table, refs, table_out=None, refs_out=None, info=N
 def copy_pages(pool: PagedCache, src, dst, to: Optional[PagedCache] = None) -> None:
     """Copies pages of all layers, to.pages[dst[j]] = pool.pages[src[j]] (`to`: another cache of the same layout)."""
     to = pool if to is None else to
-    if to.device != pool.device:
+    if to.index != pool.index:
         raise ValueError("both caches must be on one device")
     n = _numbers(pool, src, None, "src")
     _numbers(pool, dst, n, "dst")

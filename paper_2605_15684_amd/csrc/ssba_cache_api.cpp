@@ -184,6 +184,12 @@ AttendPlan plan(const ssba_cache* c, const ssba_cache_batch* b, const ssba_cache
         p.splits = s;
       }
     }
+  } else if (!f32 && p.kind != ssba::kAttendRows && p.tiles == 1 && keys > 256 && items <= 256 &&
+             keys <= (items >= 128 ? 4096 : 1024)) {
+    // 16 waves of one workgroup instead of parts that a second launch joins: where such workgroups fill half the
+    // chip (256 items of 2048 keys, D 128: 23.6 us, in 4 parts 23.5 + 4.1), or an item is short.  A few long ones
+    // need more CUs (4 items of 4096 keys, D 64: 14.8 us, in 16 parts 5.3 + 3.5).  fp32 has no registers for it.
+    p.threads = 1024;
   } else if (p.kind != ssba::kAttendRows) {
     // 4 waves of at least 2 steps of 32 keys each, up to about 1024 workgroups.
     const int64_t most = std::max<int64_t>(1, std::min<int64_t>(256, keys / 256));
@@ -312,7 +318,7 @@ ssba_status ssba_cache_attend(const ssba_cache* c, int32_t layer, const ssba_cac
   if (need && (!scratch || !aligned(scratch, 16))) return SSBA_ERR_ARG;
   if (scratch_bytes < need || (lists && lists_bytes < (size_t)4 * b->rows * c->kv_heads * (1 + (size_t)q->keep)))
     return SSBA_ERR_WORKSPACE;
-  if (too_many(p.items * p.splits * 2) || too_many(p.items * p.tiles * 4)) return SSBA_ERR_UNSUPPORTED;
+  if (too_many(p.items * p.splits * 4) || too_many(p.items * p.tiles * 4)) return SSBA_ERR_UNSUPPORTED;
   a.c = view(c, layer);
   a.b = view(b);
   a.q = query;

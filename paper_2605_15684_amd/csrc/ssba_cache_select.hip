@@ -94,35 +94,49 @@ __device__ __forceinline__ bool list_ends(const SelectArgs& a, const Range& r, i
   return a.keep - a.first - a.last > 0;
 }
 
-__device__ __forceinline__ uint32_t wave_or(uint32_t x) {
-#pragma unroll
-  for (int off = 1; off < 64; off <<= 1) x |= __shfl_xor(x, off);
-  return x;
+// Maximum over the wave, on the VALU (row shifts within 16 lanes, then
+// broadcasts of a row's last lane); lanes whose source is not there keep 0.
+__device__ __forceinline__ uint32_t wave_max(uint32_t x) {
+  x = max(x, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0x111, 0xf, 0xf, false));   // row_shr 1
+  x = max(x, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0x112, 0xf, 0xf, false));
+  x = max(x, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0x114, 0xf, 0xf, false));
+  x = max(x, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0x118, 0xf, 0xf, false));
+  x = max(x, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0x142, 0xa, 0xf, false));   // row_bcast 15
+  x = max(x, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0x143, 0xc, 0xf, false));   // row_bcast 31
+  return (uint32_t)__builtin_amdgcn_readlane((int)x, 63);
 }
 
 // One wave: the pages of the `need` largest of n <= 64 C keys, ascending, to
 // out (page = base + index).  n > need.  The threshold is found bit by bit,
-// first among the keys' high words (from the first bit in which they differ),
-// then among the low words of those equal there; the search ends where exactly
-// as many keys lie above as are needed.
+// first among the keys' high words, then among the low words of those equal
+// there; the search ends where exactly as many keys lie above as are needed.
+// If enough scores are within 1/8 of the largest, the search starts at the
+// first bit in which keys of that range differ.
 template <int C>
 __device__ __forceinline__ void wave_top(const uint64_t* keys, int n, int need, int base, int32_t* out, int lane) {
   uint32_t hi[C], lo[C];
-  uint32_t differ = 0;
-  const uint32_t some = (uint32_t)(keys[0] >> 32);
+  uint32_t most = 0;
 #pragma unroll
   for (int c = 0; c < C; ++c) {
-    const bool in = c * 64 + lane < n;
-    const uint64_t k = in ? keys[c * 64 + lane] : 0;
+    const uint64_t k = c * 64 + lane < n ? keys[c * 64 + lane] : 0;
     hi[c] = (uint32_t)(k >> 32);
     lo[c] = (uint32_t)k;
-    differ |= in ? hi[c] ^ some : 0;
+    most = max(most, hi[c]);
   }
-  differ = __builtin_amdgcn_readfirstlane(wave_or(differ));
-  // The bits in front of the first difference are every key's; those behind the end are 0 and below.
-  int b = differ ? 31 - __builtin_clz(differ) : -1;
-  uint32_t th = b == 31 ? 0 : some & ~((2u << b) - 1u), tl = 0;
-  if (b < 0) th = some;
+  most = wave_max(most);
+  uint32_t th = 0, tl = 0;
+  int b = 31;
+  constexpr uint32_t kEighth = 3u << 20;   // of the exponent, in a key's high word
+  if (most >= 0x80000000u + kEighth) {
+    const uint32_t from = most - kEighth;
+    int cnt = 0;
+#pragma unroll
+    for (int c = 0; c < C; ++c) cnt += __popcll(__builtin_amdgcn_ballot_w64(hi[c] >= from));
+    if (cnt >= need) {   // from <= threshold <= most
+      b = 31 - __builtin_clz(from ^ most);
+      th = most & ~((2u << b) - 1u);
+    }
+  }
   int left = need;       // places for keys whose high word is th
   bool low = true;       // the low words decide
   for (; b >= 0; --b) {
@@ -172,11 +186,14 @@ __device__ __forceinline__ void wave_top(const uint64_t* keys, int n, int need, 
   }
 }
 
+// n <= CAP
+template <int CAP>
 __device__ __forceinline__ void wave_top_any(const uint64_t* keys, int n, int need, int base, int32_t* out, int lane) {
   if (n <= 128) wave_top<2>(keys, n, need, base, out, lane);
   else if (n <= 256) wave_top<4>(keys, n, need, base, out, lane);
-  else if (n <= 512) wave_top<8>(keys, n, need, base, out, lane);
-  else wave_top<16>(keys, n, need, base, out, lane);
+  else if (CAP > 256 && n <= 384) wave_top<6>(keys, n, need, base, out, lane);
+  else if (CAP > 256 && n <= 512) wave_top<8>(keys, n, need, base, out, lane);
+  else if (CAP > 512) wave_top<16>(keys, n, need, base, out, lane);
 }
 
 // Ranking keys of pages j0, j0 + step, ... below `end` by one row's queries: D / 8 lanes to a page.
@@ -230,7 +247,7 @@ __global__ __launch_bounds__(kRowThreads) void k_select_row(SelectArgs a) {
   score_pages<D, 4>(a, table, h, q, lane % LPP, threadIdx.x / LPP, kRowThreads / LPP, r.middle, s_keys);
   __syncthreads();
   if (threadIdx.x < 64)
-    wave_top_any(s_keys, r.middle, a.keep - a.first - a.last, a.first, list + 1 + a.first, lane);
+    wave_top_any<kSelectInLds>(s_keys, r.middle, a.keep - a.first - a.last, a.first, list + 1 + a.first, lane);
 }
 
 // 16 tokens x all their pages.  A: the tokens' query sums, channels
@@ -285,7 +302,7 @@ __global__ __launch_bounds__(kRowThreads) void k_select_tile(SelectArgs a) {
     const Range r = range_of(a, sv, tok0 + t);
     int32_t* list = a.lists + ((int64_t)(sv.begin + tok0 + t) * a.c.kv_heads + h) * (1 + a.keep);
     if (list_ends(a, r, list, lane, 64))
-      wave_top_any(&s_keys[t * CAP], r.middle, a.keep - a.first - a.last, a.first, list + 1 + a.first, lane);
+      wave_top_any<CAP>(&s_keys[t * CAP], r.middle, a.keep - a.first - a.last, a.first, list + 1 + a.first, lane);
   }
 }
 
