@@ -58,7 +58,7 @@ extern "C" {
 #endif
 
 typedef struct ssba_cache {
-  int32_t layers, pages;     /* layers >= 1, 1 <= pages <= 2^24                  */
+  int32_t layers, pages;     /* 1 <= layers <= 65534, 1 <= pages <= 2^24          */
   int32_t kv_heads;          /* 1 .. 1024                                        */
   int32_t head_dim;          /* 64 or 128                                        */
   int32_t page;              /* tokens per page: 16, 32 or 64                    */

@@ -141,6 +141,11 @@ struct CopyArgs {
   const int32_t* dst;
   const int32_t* count;      // pairs (null: n)
   int n;
+  // A compaction's page table: table_out[e] = map[table[e]] (map null: none).
+  const int32_t* map;
+  const int32_t* table;
+  int32_t* table_out;
+  int64_t entries;
 };
 
 hipError_t launch_pages_reserve(const PagesArgs& a, hipStream_t s);

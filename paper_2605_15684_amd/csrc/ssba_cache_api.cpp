@@ -30,7 +30,7 @@ constexpr int64_t kMaxTokens = (int64_t)1 << 30;
 ssba_status check_shape(const ssba_cache* c) {
   if (!c) return SSBA_ERR_ARG;
   if (c->layers < 1 || c->pages < 1 || c->kv_heads < 1) return SSBA_ERR_SHAPE;
-  if (c->pages > kMaxPages || c->kv_heads > 1024 || c->layers > 65535) return SSBA_ERR_UNSUPPORTED;
+  if (c->pages > kMaxPages || c->kv_heads > 1024 || c->layers > 65534) return SSBA_ERR_UNSUPPORTED;
   if (c->head_dim != 64 && c->head_dim != 128) return SSBA_ERR_UNSUPPORTED;
   if (c->page != 16 && c->page != 32 && c->page != 64) return SSBA_ERR_UNSUPPORTED;
   return SSBA_OK;
@@ -465,6 +465,10 @@ ssba_status ssba_pages_compact(const ssba_cache* c, const ssba_pages* p, int32_t
   m.src = a.scratch + 4;
   m.dst = m.src + c->pages;
   m.n = std::max(1, c->pages / 2);   // at most half of the pages move
+  m.map = m.dst + c->pages;
+  m.table = p->table;
+  m.table_out = table_out;
+  m.entries = (int64_t)p->rows * p->max_pages;
   return status_of(ssba::launch_pages_copy(m, hs));
 }
 

@@ -245,33 +245,46 @@ __global__ __launch_bounds__(kThreads) void k_pages_compact(PagesArgs a) {
   }
 }
 
-__global__ __launch_bounds__(256) void k_pages_remap(PagesArgs a) {
-  const int* map = a.scratch + 4 + 2 * (int64_t)a.pages;
-  const int64_t n = (int64_t)a.rows * a.max_pages;
-  for (int64_t e = (int64_t)blockIdx.x * 256 + threadIdx.x; e < n; e += (int64_t)gridDim.x * 256) {
-    const int p = a.table[e];
-    a.table_out[e] = is_page(a, p) ? map[p] : p;
+// Bytes from `f` to `t` by the workgroup, 16 a thread at a time; four loads go
+// out before the first store.
+__device__ __forceinline__ void copy_bytes(const char* f, char* t, int64_t n) {
+  for (int64_t b = threadIdx.x * 16; b < n; b += 4 * 256 * 16) {
+    u32x4 w[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      if (b + i * 4096 < n) w[i] = *reinterpret_cast<const u32x4*>(f + b + i * 4096);
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      if (b + i * 4096 < n) *reinterpret_cast<u32x4*>(t + b + i * 4096) = w[i];
   }
 }
 
-// Workgroup (x, y): pairs x, x + gridDim.x, ... of layer y.
+// Workgroup (x, y): pairs x, x + gridDim.x, ... of layer y.  A compaction's
+// page table is rewritten by the workgroups of one more y.
 __global__ __launch_bounds__(256) void k_pages_copy(CopyArgs a) {
+  if ((int)blockIdx.y == a.layers) {
+    for (int64_t e = (int64_t)blockIdx.x * 256 + threadIdx.x; e < a.entries; e += (int64_t)gridDim.x * 256) {
+      const int p = a.table[e];
+      a.table_out[e] = p >= 0 && p < a.from_pages ? a.map[p] : p;
+    }
+    return;
+  }
   const int n = a.count ? *a.count : a.n;
   for (int j = blockIdx.x; j < n; j += gridDim.x) {
     const int x = a.src[j], y = a.dst[j];
     if (x < 0 || x >= a.from_pages || y < 0 || y >= a.to_pages) continue;
+    const char* f[4];
+    char* t[4];
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-      const char* f = a.from[i] + blockIdx.y * a.from_layer[i] + x * a.bytes[i];
-      char* t = a.to[i] + blockIdx.y * a.to_layer[i] + y * a.bytes[i];
-      if (i == 2) {   // the scales: 8 bytes a head
-        for (int64_t b = threadIdx.x * 8; b < a.bytes[i]; b += 256 * 8)
-          *reinterpret_cast<uint64_t*>(t + b) = *reinterpret_cast<const uint64_t*>(f + b);
-      } else {
-        for (int64_t b = threadIdx.x * 16; b < a.bytes[i]; b += 256 * 16)
-          *reinterpret_cast<u32x4*>(t + b) = *reinterpret_cast<const u32x4*>(f + b);
-      }
+      f[i] = a.from[i] + blockIdx.y * a.from_layer[i] + x * a.bytes[i];
+      t[i] = a.to[i] + blockIdx.y * a.to_layer[i] + y * a.bytes[i];
     }
+    copy_bytes(f[0], t[0], a.bytes[0]);
+    copy_bytes(f[1], t[1], a.bytes[1]);
+    copy_bytes(f[3], t[3], a.bytes[3]);
+    for (int64_t b = threadIdx.x * 8; b < a.bytes[2]; b += 256 * 8)   // the scales: 8 bytes a head
+      *reinterpret_cast<uint64_t*>(t[2] + b) = *reinterpret_cast<const uint64_t*>(f[2] + b);
   }
 }
 
@@ -294,15 +307,11 @@ hipError_t launch_pages_release(const PagesArgs& a, hipStream_t s) {
 
 hipError_t launch_pages_compact(const PagesArgs& a, hipStream_t s) {
   k_pages_compact<<<1, kThreads, 0, s>>>(a);
-  const hipError_t e = hipGetLastError();
-  if (e != hipSuccess) return e;
-  const int64_t n = (int64_t)a.rows * a.max_pages;
-  k_pages_remap<<<(unsigned)min((n + 255) / 256, (int64_t)2048), 256, 0, s>>>(a);
   return hipGetLastError();
 }
 
 hipError_t launch_pages_copy(const CopyArgs& a, hipStream_t s) {
-  k_pages_copy<<<dim3(min(a.n, 1024), a.layers), 256, 0, s>>>(a);
+  k_pages_copy<<<dim3(min(a.n, 1024), a.layers + (a.map ? 1 : 0)), 256, 0, s>>>(a);
   return hipGetLastError();
 }
 

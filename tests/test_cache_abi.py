@@ -41,7 +41,7 @@ def rows(**kw):
 
 BAD_CACHE = [(dict(layers=0), SHAPE), (dict(pages=0), SHAPE), (dict(kv_heads=-1), SHAPE), (dict(head_dim=96), UNSUPPORTED),
              (dict(page=8), UNSUPPORTED), (dict(page=128), UNSUPPORTED), (dict(pages=(1 << 24) + 1), UNSUPPORTED),
-             (dict(kv_heads=1025), UNSUPPORTED), (dict(layers=65536), UNSUPPORTED)]
+             (dict(kv_heads=1025), UNSUPPORTED), (dict(layers=65535), UNSUPPORTED)]
 BAD_ARRAYS = [(dict(k=None), ARG), (dict(v=P + 8), ARG), (dict(scale=P + 4), ARG), (dict(kmean=P + 2), ARG)]
 BAD_BATCH = [(dict(seqs=0), SHAPE), (dict(max_pages=0), SHAPE), (dict(rows=-1), SHAPE), (dict(max_new=-1), SHAPE),
              (dict(max_len=-1), SHAPE), (dict(seqs=65536), UNSUPPORTED), (dict(max_pages=1 << 27), UNSUPPORTED)]
