@@ -49,24 +49,32 @@ __device__ __forceinline__ void values_of(uint32_t w, float (&x)[4]) {
   x[3] = hi[1];
 }
 
+// Eight consecutive values as they are in memory, and as numbers.
 template <bool F32>
-__device__ __forceinline__ void load8(const void* base, int64_t off, float (&x)[8]) {
-  if (F32) {
-#pragma unroll
-    for (int i = 0; i < 2; ++i) {
-      const u32x4 w = *reinterpret_cast<const u32x4a4*>(static_cast<const float*>(base) + off + 4 * i);
-#pragma unroll
-      for (int e = 0; e < 4; ++e) x[4 * i + e] = __uint_as_float(w[e]);
-    }
-  } else {
-    const u32x4 w = *reinterpret_cast<const u32x4*>(static_cast<const uint16_t*>(base) + off);
-#pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      x[2 * e] = __uint_as_float(w[e] << 16);
-      x[2 * e + 1] = __uint_as_float(w[e] & 0xffff0000u);
+struct Raw {
+  u32x4 w[F32 ? 2 : 1];
+  __device__ __forceinline__ void load(const void* base, int64_t off) {
+    if (F32) {
+      const float* p = static_cast<const float*>(base) + off;
+      w[0] = *reinterpret_cast<const u32x4a4*>(p);
+      w[F32 ? 1 : 0] = *reinterpret_cast<const u32x4a4*>(p + 4);
+    } else {
+      w[0] = *reinterpret_cast<const u32x4*>(static_cast<const uint16_t*>(base) + off);
     }
   }
-}
+  __device__ __forceinline__ void get(float (&x)[8]) const {
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      if (F32) {
+        x[e] = __uint_as_float(w[0][e]);
+        x[4 + e] = __uint_as_float(w[F32 ? 1 : 0][e]);
+      } else {
+        x[2 * e] = __uint_as_float(w[0][e] << 16);
+        x[2 * e + 1] = __uint_as_float(w[0][e] & 0xffff0000u);
+      }
+    }
+  }
+};
 
 template <int D, bool F32>
 __global__ __launch_bounds__(256) void k_cache_append(AppendArgs a) {
@@ -101,21 +109,26 @@ __global__ __launch_bounds__(256) void k_cache_append(AppendArgs a) {
     was[1] = __float_as_uint(scale[1]);
   }
   if (threadIdx.x < 2) s_top[threadIdx.x] = 0;
-  __syncthreads();   // every thread has the old scales before they are replaced
 
-  float x[2][4][8];
+  // Every thread loads four rows at once; where it has none of the page's new
+  // ones, the sequence's first new row stands in (its values count for nothing).
   bool fresh[4], old[4];
+  Raw<F32> raw[2][4];
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
     const int pos = p0 + 4 * tq + i;
     fresh[i] = active && pos >= start && pos < sv.len;
     old[i] = active && pos < start;
-    if (fresh[i]) {
-      const int64_t off = (int64_t)(sv.begin + pos - start) * a.st + (int64_t)h * a.sh + ch8 * 8;
-      load8<F32>(a.k, off, x[0][i]);
-      load8<F32>(a.v, off, x[1][i]);
-    }
+    const int64_t off = (int64_t)(sv.begin + (fresh[i] ? pos - start : 0)) * a.st + (int64_t)h * a.sh + ch8 * 8;
+    raw[0][i].load(a.k, off);
+    raw[1][i].load(a.v, off);
   }
+  float x[2][4][8];
+#pragma unroll
+  for (int kv = 0; kv < 2; ++kv)
+#pragma unroll
+    for (int i = 0; i < 4; ++i) raw[kv][i].get(x[kv][i]);
+  __syncthreads();   // every thread has the old scales before they are replaced
   // The largest magnitude; fmaxf passes over NaN.
   float top[2] = {0.f, 0.f};
 #pragma unroll
