@@ -12,23 +12,60 @@ typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 
 constexpr int kThreads = 1024;
 constexpr int kWaves = kThreads / 64;
+constexpr int kSlices = 8;   // arrays are walked in up to 8 slices of kThreads elements at a time
 
-// Number of set flags in front of this thread's, and their total, over the
-// workgroup.  `s` is LDS of kWaves ints.
-__device__ __forceinline__ int block_rank(bool flag, int* s, int* total) {
+// Sum of `n` over the threads in front of this one, and over all of them.  `s`
+// is LDS of kWaves ints.
+__device__ __forceinline__ int block_sum(int n, int* s, int* total) {
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  const uint64_t m = __builtin_amdgcn_ballot_w64(flag);
+  int incl = n;
+#pragma unroll
+  for (int off = 1; off < 64; off <<= 1) {
+    const int o = __shfl_up(incl, off);
+    if (lane >= off) incl += o;
+  }
   __syncthreads();
-  if (lane == 0) s[wave] = __popcll(m);
+  if (lane == 63) s[wave] = incl;
   __syncthreads();
-  int before = 0, sum = 0;
+  int before = incl - n, sum = 0;
 #pragma unroll
   for (int w = 0; w < kWaves; ++w) {
     before += w < wave ? s[w] : 0;
     sum += s[w];
   }
   *total = sum;
-  return before + __popcll(m & ((1ull << lane) - 1));
+  return before;
+}
+
+// Ranks of flags over `slices` slices of kThreads elements in order (element
+// i kThreads + thread is slice i's): how many set ones are in front of each of
+// this thread's, and their total.  `s` is LDS of kSlices * kWaves ints.
+__device__ __forceinline__ void slice_ranks(const bool (&flag)[kSlices], int slices, int* s, int (&rank)[kSlices],
+                                            int* total) {
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const uint64_t below = (1ull << lane) - 1;
+  __syncthreads();
+#pragma unroll
+  for (int i = 0; i < kSlices; ++i) {
+    if (i >= slices) break;
+    const uint64_t m = __builtin_amdgcn_ballot_w64(flag[i]);
+    rank[i] = __popcll(m & below);
+    if (lane == 0) s[i * kWaves + wave] = __popcll(m);
+  }
+  __syncthreads();
+  int sum = 0;
+#pragma unroll
+  for (int i = 0; i < kSlices; ++i) {
+    if (i >= slices) break;
+    rank[i] += sum;
+#pragma unroll
+    for (int w = 0; w < kWaves; ++w) {
+      const int c = s[i * kWaves + w];
+      rank[i] += w < wave ? c : 0;
+      sum += c;
+    }
+  }
+  *total = sum;
 }
 
 __device__ __forceinline__ int held(const PagesArgs& a, int row) {
@@ -42,37 +79,75 @@ __device__ __forceinline__ int fresh(const int32_t* p) {
   return __hip_atomic_load(p, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
 }
 
-// The lowest `n` free pages, in order: fn(j, page) for j < n; returns how many there are (at most n).
+// The lowest `n` free pages, in order: fn(j, page) for j < n; returns how many
+// of them there are.
 template <typename F>
 __device__ __forceinline__ int take_free(const PagesArgs& a, int n, int* s, F fn) {
   int got = 0;
-  for (int p0 = 0; p0 < a.pages && got < n; p0 += kThreads) {
-    const int p = p0 + threadIdx.x;
-    int total;
-    const bool free = p < a.pages && fresh(&a.refs[p]) == 0;
-    const int rank = got + block_rank(free, s, &total);
-    if (free && rank < n) fn(rank, p);
+  for (int p0 = 0; p0 < a.pages && got < n; p0 += kThreads * kSlices) {
+    const int slices = min((a.pages - p0 + kThreads - 1) / kThreads, kSlices);
+    bool free[kSlices];
+    int rank[kSlices], total;
+#pragma unroll
+    for (int i = 0; i < kSlices; ++i) {
+      const int p = p0 + i * kThreads + threadIdx.x;
+      free[i] = p < a.pages && fresh(&a.refs[p]) == 0;
+    }
+    slice_ranks(free, slices, s, rank, &total);
+#pragma unroll
+    for (int i = 0; i < kSlices; ++i)
+      if (free[i] && got + rank[i] < n) fn(got + rank[i], p0 + i * kThreads + (int)threadIdx.x);
     got += total;
   }
   return min(got, n);
 }
 
+// scratch: the entries that lack a page, then how many each row has.  A wave
+// takes a row.
 __global__ __launch_bounds__(kThreads) void k_pages_reserve(PagesArgs a) {
-  __shared__ int s[kWaves];
+  __shared__ int s[kSlices * kWaves];
   int* miss = a.scratch;
-  int n = 0;
-  const int64_t entries = (int64_t)a.rows * a.max_pages;
-  for (int64_t e0 = 0; e0 < entries; e0 += kThreads) {
-    const int64_t e = e0 + threadIdx.x;
-    bool lacks = false;
-    if (e < entries) {
-      const int row = (int)(e / a.max_pages), i = (int)(e - (int64_t)row * a.max_pages);
-      lacks = (i << a.page_log2) < held(a, row) && !is_page(a, a.table[e]);
+  int* of_row = miss + (int64_t)a.rows * a.max_pages;
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  // fn(entry, how many lack a page in front of it in the row); the row's number of them
+  auto lacking = [&](int row, auto fn) {
+    const int need = (held(a, row) + (1 << a.page_log2) - 1) >> a.page_log2;
+    const int32_t* t = a.table + (int64_t)row * a.max_pages;
+    int n = 0;
+    for (int i0 = 0; i0 < need; i0 += 256) {
+      bool lacks[4];
+#pragma unroll
+      for (int u = 0; u < 4; ++u) {
+        const int i = i0 + u * 64 + lane;
+        lacks[u] = i < need && !is_page(a, t[i]);
+      }
+#pragma unroll
+      for (int u = 0; u < 4; ++u) {
+        const uint64_t m = __builtin_amdgcn_ballot_w64(lacks[u]);
+        if (lacks[u]) fn(i0 + u * 64 + lane, n + __popcll(m & ((1ull << lane) - 1)));
+        n += __popcll(m);
+      }
     }
+    return n;
+  };
+  for (int row = wave; row < a.rows; row += kWaves) {
+    const int n = lacking(row, [](int, int) {});
+    if (lane == 0) of_row[row] = n;
+  }
+  __syncthreads();
+  int n = 0;
+  for (int r0 = 0; r0 < a.rows; r0 += kThreads) {   // counts to places in the list
+    const int r = r0 + threadIdx.x;
+    const int mine = r < a.rows ? of_row[r] : 0;
     int total;
-    const int rank = n + block_rank(lacks, s, &total);
-    if (lacks) miss[rank] = (int)e;
+    const int before = n + block_sum(mine, s, &total);
+    if (r < a.rows) of_row[r] = mine ? before : -1;
     n += total;
+  }
+  __syncthreads();
+  for (int row = wave; row < a.rows; row += kWaves) {
+    const int at = of_row[row];
+    if (at >= 0) lacking(row, [&](int i, int j) { miss[at + j] = row * a.max_pages + i; });
   }
   __syncthreads();
   const int got = take_free(a, n, s, [&](int j, int p) {
@@ -85,15 +160,15 @@ __global__ __launch_bounds__(kThreads) void k_pages_reserve(PagesArgs a) {
   }
 }
 
-// scratch: [0] copies, then src and dst pages of the copies (n each), then
-// per row: is a src; the first pair that names it as dst; then per pair the
-// rank of its incomplete page.
+// scratch: [0] copies, [4..] src pages, dst pages and pairs of the incomplete
+// pages (n each), then per row: is a src; the first pair that names it as dst.
 __global__ __launch_bounds__(kThreads) void k_pages_fork(PagesArgs a) {
-  __shared__ int s[kWaves];
+  __shared__ int s[kSlices * kWaves];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   int* count = a.scratch;
   int* from = count + 4;
   int* to = from + a.n;
-  int* pair = to + a.n;        // of the j-th incomplete page
+  int* pair = to + a.n;
   int* is_src = pair + a.n;
   int* first = is_src + a.rows;
   for (int r = threadIdx.x; r < a.rows; r += kThreads) {
@@ -111,19 +186,28 @@ __global__ __launch_bounds__(kThreads) void k_pages_fork(PagesArgs a) {
     const int x = a.src[j], y = a.dst[j];
     return x >= 0 && x < a.rows && y >= 0 && y < a.rows && fresh(&first[y]) == j && !is_src[y];
   };
-  // Complete pages are shared.
-  const int64_t entries = (int64_t)a.n * a.max_pages;
-  for (int64_t e = threadIdx.x; e < entries; e += kThreads) {
-    const int j = (int)(e / a.max_pages), i = (int)(e - (int64_t)j * a.max_pages);
+  // Complete pages are shared; a wave takes a pair.
+  for (int j = wave; j < a.n; j += kWaves) {
     if (!valid(j)) continue;
-    const int x = a.src[j];
-    int p = -1;
-    if (i < held(a, x) >> a.page_log2) {
-      p = a.table[(int64_t)x * a.max_pages + i];
-      if (is_page(a, p)) atomicAdd(&a.refs[p], 1);
-      else p = -1;
+    const int x = a.src[j], full = held(a, x) >> a.page_log2;
+    const int32_t* f = a.table + (int64_t)x * a.max_pages;
+    int32_t* t = a.table + (int64_t)a.dst[j] * a.max_pages;
+    for (int i0 = 0; i0 < a.max_pages; i0 += 256) {
+      int p[4];
+#pragma unroll
+      for (int u = 0; u < 4; ++u) {
+        const int i = i0 + u * 64 + lane;
+        p[u] = i < full ? f[i] : -1;
+      }
+#pragma unroll
+      for (int u = 0; u < 4; ++u) {
+        const int i = i0 + u * 64 + lane;
+        if (i >= a.max_pages) continue;
+        if (is_page(a, p[u])) atomicAdd(&a.refs[p[u]], 1);
+        else p[u] = -1;
+        t[i] = p[u];
+      }
     }
-    a.table[(int64_t)a.dst[j] * a.max_pages + i] = p;
   }
   // Pairs with an incomplete last page.
   int n = 0, forked = 0;
@@ -137,12 +221,11 @@ __global__ __launch_bounds__(kThreads) void k_pages_fork(PagesArgs a) {
              is_page(a, a.table[(int64_t)a.src[j] * a.max_pages + (len >> a.page_log2)]);
       a.lens[a.dst[j]] = len;
     }
-    int total;
-    const int rank = n + block_rank(part, s, &total);
+    int total;   // both counts in one sum
+    const int rank = n + (block_sum(part | ok << 16, s, &total) & 0xffff);
     if (part) pair[rank] = j;
-    n += total;
-    block_rank(ok, s, &total);
-    forked += total;
+    n += total & 0xffff;
+    forked += total >> 16;
   }
   __syncthreads();
   const int got = take_free(a, n, s, [&](int r, int p) {
@@ -163,9 +246,10 @@ __global__ __launch_bounds__(kThreads) void k_pages_fork(PagesArgs a) {
   }
 }
 
-// scratch: per row the first place that names it.
+// scratch: per row the first place that names it.  A wave takes a row.
 __global__ __launch_bounds__(kThreads) void k_pages_release(PagesArgs a) {
   __shared__ int s_info[2];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   int* first = a.scratch;
   if (threadIdx.x < 2) s_info[threadIdx.x] = 0;
   for (int r = threadIdx.x; r < a.rows; r += kThreads) first[r] = a.n;
@@ -175,22 +259,31 @@ __global__ __launch_bounds__(kThreads) void k_pages_release(PagesArgs a) {
     if (x >= 0 && x < a.rows) atomicMin(&first[x], j);
   }
   __syncthreads();
-  const int64_t entries = (int64_t)a.n * a.max_pages;
   int dropped = 0, freed = 0;
-  for (int64_t e = threadIdx.x; e < entries; e += kThreads) {
-    const int j = (int)(e / a.max_pages), i = (int)(e - (int64_t)j * a.max_pages);
+  for (int j = wave; j < a.n; j += kWaves) {
     const int x = a.src[j];
     if (x < 0 || x >= a.rows || fresh(&first[x]) != j) continue;
-    int32_t* at = a.table + (int64_t)x * a.max_pages + i;
-    const int p = *at;
-    if (is_page(a, p)) {
-      const int was = atomicSub(&a.refs[p], 1);
-      if (was <= 0) atomicAdd(&a.refs[p], 1);   // named by more entries than it had references
-      dropped += 1;
-      freed += was == 1;
+    int32_t* t = a.table + (int64_t)x * a.max_pages;
+    for (int i0 = 0; i0 < a.max_pages; i0 += 256) {
+      int p[4], was[4];
+#pragma unroll
+      for (int u = 0; u < 4; ++u) {
+        const int i = i0 + u * 64 + lane;
+        p[u] = i < a.max_pages ? t[i] : -1;
+      }
+#pragma unroll
+      for (int u = 0; u < 4; ++u) was[u] = is_page(a, p[u]) ? atomicSub(&a.refs[p[u]], 1) : 2;
+#pragma unroll
+      for (int u = 0; u < 4; ++u) {
+        const int i = i0 + u * 64 + lane;
+        if (i < a.max_pages) t[i] = -1;
+        if (!is_page(a, p[u])) continue;
+        if (was[u] <= 0) atomicAdd(&a.refs[p[u]], 1);   // named by more entries than it had references
+        dropped += 1;
+        freed += was[u] == 1;
+      }
     }
-    *at = -1;
-    if (i == 0) a.lens[x] = 0;
+    if (lane == 0) a.lens[x] = 0;
   }
   if (dropped) atomicAdd(&s_info[0], dropped);
   if (freed) atomicAdd(&s_info[1], freed);
@@ -200,35 +293,41 @@ __global__ __launch_bounds__(kThreads) void k_pages_release(PagesArgs a) {
 
 // scratch: [0] copies, [4..] src pages, dst pages, then where each page goes.
 __global__ __launch_bounds__(kThreads) void k_pages_compact(PagesArgs a) {
-  __shared__ int s[kWaves];
+  __shared__ int s[kSlices * kWaves];
   int* count = a.scratch;
   int* from = count + 4;
   int* to = from + a.pages;
   int* map = to + a.pages;
   int live = 0;
-  for (int p0 = 0; p0 < a.pages; p0 += kThreads) {
-    const int p = p0 + threadIdx.x;
-    const int r = p < a.pages ? a.refs[p] : 0;
-    if (p < a.pages) {
-      map[p] = p;
-      a.refs_out[p] = r;
-    }
-    int total;
-    block_rank(r > 0, s, &total);
-    live += total;
+  for (int p = threadIdx.x; p < a.pages; p += kThreads) {
+    const int r = a.refs[p];
+    map[p] = p;
+    a.refs_out[p] = r;
+    live += r > 0;
   }
+  block_sum(live, s, &live);
   int holes = 0, movers = 0;
-  for (int p0 = 0; p0 < a.pages; p0 += kThreads) {
-    const int p = p0 + threadIdx.x;
-    const bool used = p < a.pages && a.refs[p] > 0;
-    const bool hole = p < live && !used, mover = used && p >= live;
-    int total;
-    int rank = holes + block_rank(hole, s, &total);
+  for (int p0 = 0; p0 < a.pages; p0 += kThreads * kSlices) {
+    const int slices = min((a.pages - p0 + kThreads - 1) / kThreads, kSlices);
+    bool hole[kSlices], mover[kSlices];
+    int rank[kSlices], total;
+#pragma unroll
+    for (int i = 0; i < kSlices; ++i) {
+      const int p = p0 + i * kThreads + threadIdx.x;
+      const bool used = p < a.pages && a.refs[p] > 0;
+      hole[i] = p < live && !used;
+      mover[i] = used && p >= live;
+    }
+    slice_ranks(hole, slices, s, rank, &total);
+#pragma unroll
+    for (int i = 0; i < kSlices; ++i)
+      if (hole[i]) to[holes + rank[i]] = p0 + i * kThreads + threadIdx.x;
     holes += total;
-    if (hole) to[rank] = p;
-    rank = movers + block_rank(mover, s, &total);
+    slice_ranks(mover, slices, s, rank, &total);
+#pragma unroll
+    for (int i = 0; i < kSlices; ++i)
+      if (mover[i]) from[movers + rank[i]] = p0 + i * kThreads + threadIdx.x;
     movers += total;
-    if (mover) from[rank] = p;
   }
   __syncthreads();
   for (int r = threadIdx.x; r < movers; r += kThreads) {

@@ -443,18 +443,19 @@ def _same_rows(gpu, host):
         assert np.array_equal(a.cpu().numpy(), b)
 
 
-@pytest.mark.parametrize("pages,rows,columns,page", [(7, 1, 1, 16), (60, 5, 9, 16), (3000, 40, 50, 64), (50, 30, 7, 32)])
+@pytest.mark.parametrize("pages,rows,columns,page", [(7, 1, 1, 16), (60, 5, 9, 16), (3000, 40, 50, 64), (50, 30, 7, 32),
+                                                     (20000, 33, 700, 16), (300, 1200, 3, 16)])
 def test_pages(pages, rows, columns, page):
     """reserve, fork, release, compact in turn, with what the header allows: rows twice, rows that are none, pools
     that run out of pages."""
     from paper_2605_15684_amd import cache
     rng = np.random.default_rng(pages)
-    pool = make_pool(rng, 3, pages, 3, 64, page)
+    pool = make_pool(rng, 3 if pages < 5000 else 1, pages, 3 if pages < 5000 else 1, 64, page)
     gpool = gpu_pool(pool)
     table = np.full((rows, columns), -1, dtype=np.int32)
     lens, refs = np.zeros(rows, dtype=np.int32), np.zeros(pages, dtype=np.int32)
     g = _gpu_rows(table, lens, refs)
-    for turn in range(6):
+    for turn in range(6 if pages < 5000 else 2):
         some = rng.random(rows) < 0.6
         lens[some] = rng.integers(0, columns * page + page, int(some.sum()))
         lens[~some] = np.minimum(lens[~some] + 1, columns * page)
