@@ -40,18 +40,29 @@ __device__ __forceinline__ SeqView seq_view(const BatchView& b, int page_log2, i
   return v;
 }
 
-// Sequence of packed row r: the number of ends cu[1..seqs] that are <= r
-// (seqs: no sequence).  One wave; every lane gets the result.
-__device__ __forceinline__ int seq_of_row(const BatchView& b, int r, int lane) {
-  int s = 0;
+// The sequence of packed row r and its view; false if the row is no
+// sequence's new token.  One wave, every lane gets the result.  The sequence
+// is the number of ends cu[1..seqs] that are <= r (cu does not decrease); a
+// lane holds one end and the length of the sequence that begins behind the
+// last one, so that nothing is loaded after the search.
+__device__ __forceinline__ bool seq_of_row(const BatchView& b, int page_log2, int r, int lane, int* seq, SeqView* v) {
+  int begin = b.cu[0];
   for (int j0 = 1; j0 <= b.seqs; j0 += 64) {
     const int j = j0 + lane;
-    const bool past = j <= b.seqs && b.cu[j] <= r;
-    const int c = __popcll(__builtin_amdgcn_ballot_w64(past));
-    s += c;
-    if (c < 64) break;   // cu does not decrease
+    const bool in = j <= b.seqs;
+    const int end = in ? b.cu[j] : 0, len = in ? b.lens[j - 1] : 0;
+    const int c = __popcll(__builtin_amdgcn_ballot_w64(in && end <= r));
+    if (c > 0) begin = __builtin_amdgcn_readlane(end, c - 1);
+    if (c < 64) {
+      *seq = j0 - 1 + c;
+      if (*seq >= b.seqs) return false;
+      v->begin = min(max(begin, 0), b.rows);
+      v->n = max(min(__builtin_amdgcn_readlane(end, c), b.rows), v->begin) - v->begin;
+      v->len = min(max(__builtin_amdgcn_readlane(len, c), 0), b.max_pages << page_log2);
+      return r >= v->begin && r - v->begin < v->n;
+    }
   }
-  return __builtin_amdgcn_readfirstlane(s);
+  return false;
 }
 
 struct AppendArgs {

@@ -106,14 +106,13 @@ struct Item {
 // unit: sequence, or packed row (LISTED).  False: no such row.
 template <bool LISTED>
 __device__ __forceinline__ bool item_of(const AttendArgs& a, int unit, int lane, Item* it) {
-  it->seq = unit;
   if (LISTED) {
-    it->seq = unit < a.b.rows ? seq_of_row(a.b, unit, lane) : a.b.seqs;
-    if (it->seq >= a.b.seqs) return false;
+    if (unit >= a.b.rows || !seq_of_row(a.b, a.c.page_log2, unit, lane, &it->seq, &it->sv)) return false;
+  } else {
+    it->seq = unit;
+    it->sv = seq_view(a.b, a.c.page_log2, unit);
   }
-  it->sv = seq_view(a.b, a.c.page_log2, it->seq);
   it->tok0 = LISTED ? unit - it->sv.begin : 0;
-  if (LISTED && (it->tok0 < 0 || it->tok0 >= it->sv.n)) return false;
   it->ncols = LISTED ? a.group : min(it->sv.n, a.b.max_new) * a.group;
   return true;
 }
@@ -263,17 +262,20 @@ __global__ __launch_bounds__(P::THREADS, P::R > 1 ? 2 : P::THREADS > 512 ? 4 : 3
     }
 #pragma unroll
     for (int t = 0; t < 2; ++t) {
-      const int l = (2 * s + t) & 63;
-      const int page = lane_i(m_page, l);
-      x.key[t] = lane_i(m_key, l);
-      x.ks[t] = lane_f(m_ks, l);
-      x.vs[t] = lane_f(m_vs, l);
-      if (!P::F32) x.lv[t] = lane_f(m_lv, l);
+      const int page = lane_i(m_page, (2 * s + t) & 63);
       const int sub = ((2 * s + t) & ((1 << gpp_log2) - 1)) * 16 * D;
       x.off[t] = (int64_t)max(page, 0) * a.c.page_bytes + head_off + sub;
       const uint8_t* kp_ = a.c.k + x.off[t];
 #pragma unroll
       for (int hh = 0; hh < NH; ++hh) x.k[t][hh] = *reinterpret_cast<const u32x4*>(kp_ + lane * 16 + hh * 1024);
+    }
+#pragma unroll
+    for (int t = 0; t < 2; ++t) {   // behind the loads: the scales may still be on their way
+      const int l = (2 * s + t) & 63;
+      x.key[t] = lane_i(m_key, l);
+      x.ks[t] = lane_f(m_ks, l);
+      x.vs[t] = lane_f(m_vs, l);
+      if (!P::F32) x.lv[t] = lane_f(m_lv, l);
     }
   };
   auto fetch_v = [&](Step& x) {

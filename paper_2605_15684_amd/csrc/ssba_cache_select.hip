@@ -235,11 +235,10 @@ __global__ __launch_bounds__(kRowThreads) void k_select_row(SelectArgs a) {
   const int row = blockIdx.x / a.c.kv_heads, h = blockIdx.x % a.c.kv_heads;
   double q[8];   // its loads go out before those that find the row's sequence
   q_sum<F32, 8>(a, row, h, lane % LPP * 8, q);
-  const int seq = seq_of_row(a.b, row, lane);
-  if (seq >= a.b.seqs) return;
-  const SeqView sv = seq_view(a.b, a.c.page_log2, seq);
+  int seq;
+  SeqView sv;
+  if (!seq_of_row(a.b, a.c.page_log2, row, lane, &seq, &sv)) return;
   const int tok = row - sv.begin;
-  if (tok < 0 || tok >= sv.n) return;
   const Range r = range_of(a, sv, tok);
   int32_t* list = a.lists + ((int64_t)row * a.c.kv_heads + h) * (1 + a.keep);
   if (!list_ends(a, r, list, threadIdx.x, kRowThreads)) return;
@@ -311,11 +310,10 @@ __global__ __launch_bounds__(256) void k_select_scores(SelectArgs a) {
   constexpr int LPP = D / 8;
   const int lane = threadIdx.x & 63;
   const int row = blockIdx.x / a.c.kv_heads, h = blockIdx.x % a.c.kv_heads;
-  const int seq = seq_of_row(a.b, row, lane);
-  if (seq >= a.b.seqs) return;
-  const SeqView sv = seq_view(a.b, a.c.page_log2, seq);
+  int seq;
+  SeqView sv;
+  if (!seq_of_row(a.b, a.c.page_log2, row, lane, &seq, &sv)) return;
   const int tok = row - sv.begin;
-  if (tok < 0 || tok >= sv.n) return;
   const Range r = range_of(a, sv, tok);
   if ((int)blockIdx.y * kSelectPages >= r.middle) return;
   double q[8];
@@ -334,11 +332,10 @@ constexpr int kTopThreads = 1024, kTopWaves = kTopThreads / 64, kTopRegs = 8;
 __global__ __launch_bounds__(kTopThreads) void k_select_top(SelectArgs a) {
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const int row = blockIdx.x / a.c.kv_heads, h = blockIdx.x % a.c.kv_heads;
-  const int seq = seq_of_row(a.b, row, lane);
-  if (seq >= a.b.seqs) return;
-  const SeqView sv = seq_view(a.b, a.c.page_log2, seq);
+  int seq;
+  SeqView sv;
+  if (!seq_of_row(a.b, a.c.page_log2, row, lane, &seq, &sv)) return;
   const int tok = row - sv.begin;
-  if (tok < 0 || tok >= sv.n) return;
   const Range r = range_of(a, sv, tok);
   int32_t* list = a.lists + ((int64_t)row * a.c.kv_heads + h) * (1 + a.keep);
   if (!list_ends(a, r, list, threadIdx.x, kTopThreads)) return;
