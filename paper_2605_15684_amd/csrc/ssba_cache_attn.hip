@@ -214,8 +214,14 @@ __global__ __launch_bounds__(P::THREADS, P::R > 1 ? 2 : P::THREADS > 512 ? 4 : 3
     groups = (maxlim + 15) >> 4;
   }
   const int steps = (groups + 1) >> 1;
-  const int parts = a.splits * P::KP, part = split * P::KP + kp;
-  const int s0 = (int)((int64_t)steps * part / parts), s1 = (int)((int64_t)steps * (part + 1) / parts);
+  // Shares that differ by one step at most.
+  int s0 = 0, s1 = steps;
+  if (!P::LISTED || P::KP > 1) {
+    const unsigned parts = a.splits * P::KP, part = split * P::KP + kp;
+    const unsigned each = (unsigned)steps / parts, more = steps - each * parts;
+    s0 = each * part + min(part, more);
+    s1 = s0 + each + (part < more ? 1 : 0);
+  }
 
   const int32_t* table = a.b.table + (int64_t)it.seq * a.b.max_pages;
   const int64_t head_off = ((int64_t)it.h << page_log2) * D;
@@ -303,10 +309,7 @@ __global__ __launch_bounds__(P::THREADS, P::R > 1 ? 2 : P::THREADS > 512 ? 4 : 3
     // compiler, which would otherwise keep them in registers and spill.
     int q_at = cg * R * NH * 2 * 64 + lane;
     if (P::QLDS) asm volatile("" : "+v"(q_at));
-#pragma unroll
-    for (int t = 0; t < 2; ++t)
-#pragma unroll
-      for (int r = 0; r < R; ++r) s[t][r] = {0.f, 0.f, 0.f, 0.f};
+    const floatx4 zero = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
     for (int hh = 0; hh < NH; ++hh)
 #pragma unroll
@@ -333,7 +336,8 @@ __global__ __launch_bounds__(P::THREADS, P::R > 1 ? 2 : P::THREADS > 512 ? 4 : 3
             }
 #pragma unroll
             for (int t = 0; t < 2; ++t)
-              s[t][r] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k[t].v, b.v, s[t][r], 0, 0, 0);
+              s[t][r] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(
+                  k[t].v, b.v, hh + u == 0 && ns == NQ - 1 ? zero : s[t][r], 0, 0, 0);
           }
       }
   };
