@@ -6,7 +6,7 @@
 #include <cmath>
 #include <cstring>
 
-#include "ssba_cache.h"
+#include "ssba_cache_common.h"
 #include "ssba_common.h"
 
 namespace {

@@ -23,7 +23,7 @@
 #include <hip/hip_runtime.h>
 #include <hip/hip_bf16.h>
 
-#include "ssba_cache.h"
+#include "ssba_cache_common.h"
 
 namespace ssba {
 namespace {

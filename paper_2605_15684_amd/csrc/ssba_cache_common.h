@@ -4,7 +4,7 @@
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
-#include "../../include/ssba_cache.h"
+#include "ssba_cache.h"
 
 namespace ssba {
 

@@ -3,7 +3,7 @@
 // a second launch moves the pages of all layers.
 #include <hip/hip_runtime.h>
 
-#include "ssba_cache.h"
+#include "ssba_cache_common.h"
 
 namespace ssba {
 namespace {

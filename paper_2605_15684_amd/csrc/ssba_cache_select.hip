@@ -19,7 +19,7 @@
 //                    over workgroups, then one workgroup ranks the row.
 #include <hip/hip_runtime.h>
 
-#include "ssba_cache.h"
+#include "ssba_cache_common.h"
 #include "ssba_common.h"
 
 namespace ssba {
