@@ -121,7 +121,8 @@ ssba_status ssba_cache_select_workspace_size(const ssba_cache* c, const ssba_cac
  * pages that are not there rank last.  `lists` int32 [rows][kv_heads][1 + keep]:
  * the count, page numbers of the sequence (columns of the table) ascending,
  * then -1.  Appending must come first: only complete pages are scored.
- * `scratch` 16-byte aligned. */
+ * `scratch` 16-byte aligned (NULL where its size is 0: tables of up to 1024
+ * pages). */
 ssba_status ssba_cache_select(const ssba_cache* c, int32_t layer, const ssba_cache_batch* b,
                               const ssba_cache_query* q, const void* query, int32_t* lists, size_t lists_bytes,
                               void* scratch, size_t scratch_bytes, void* hip_stream);
@@ -136,11 +137,15 @@ ssba_status ssba_cache_attend_workspace_size(const ssba_cache* c, const ssba_cac
  * counts are cut to 0 .. keep, entries that are no page of the sequence are
  * passed over, one that is named twice counts twice).  A token that sees
  * nothing gets zeros.
- *   bf16: Q as it is, codes exact in bf16, products and sums in fp32,
- * probabilities rounded to bf16 for the value product.  fp32: Q and the
- * probabilities as three bf16 terms each (24 bits), so products are those of
- * fp32.  bf16 Q and O 16-byte aligned with strides in multiples of 8, fp32
- * 4-byte aligned; `scratch` 16-byte aligned.  O must not overlap Q. */
+ *   bf16: Q as it is, codes exact in bf16, products and sums in fp32;
+ * probabilities enter the value product with 16 bits where a kv head's new
+ * queries of a sequence are 16 or fewer, rounded to bf16 where they are more
+ * (and where lists are read by one wave a row).  fp32: Q and the probabilities
+ * as three bf16 terms each (24 bits), so products are those of fp32.  Sums are
+ * formed before they are normalised: values beyond 2^90 may overflow.
+ * bf16 Q and O 16-byte aligned with strides in multiples of 8, fp32 4-byte
+ * aligned; `scratch` 16-byte aligned (NULL where its size is 0).  O must not
+ * overlap Q. */
 ssba_status ssba_cache_attend(const ssba_cache* c, int32_t layer, const ssba_cache_batch* b,
                               const ssba_cache_query* q, const void* query, const int32_t* lists, size_t lists_bytes,
                               void* o, void* scratch, size_t scratch_bytes, void* hip_stream);

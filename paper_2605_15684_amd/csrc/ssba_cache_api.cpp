@@ -178,7 +178,7 @@ AttendPlan plan(const ssba_cache* c, const ssba_cache_batch* b, const ssba_cache
     // the rounds over the 256 CUs fullest, each part counted as 1/16 round for
     // writing and joining it.
     double best = (double)ceil_div(items, 256);
-    for (int s = 2; s <= 256 && s * 256 <= keys; ++s) {
+    for (int s = 2; s <= 256 && s * 256 <= keys && s * items <= 1024; ++s) {
       const double cost = (double)ceil_div(items * s, 256) / s + (items * s > 256 ? 0.0625 * s : 0.0);
       if (cost < best * 0.95) {
         best = cost;

@@ -507,6 +507,53 @@ def test_copy_pages():
     assert_same_pool(host_pool(ga), a)
 
 
+def test_binding_refusals():
+    from paper_2605_15684_amd import cache
+    pool = cache.alloc(1, 4, 2, 64, 16)
+    table, lens, refs = cache.alloc_rows(pool, 2, 2000)
+    cu = torch.tensor([0, 1, 2], dtype=torch.int32, device="cuda")
+    batch = cache.Batch(table, lens, cu, 1)
+    k = torch.zeros(2, 2, 64, dtype=BF16, device="cuda")
+    q = torch.zeros(2, 4, 64, dtype=BF16, device="cuda")
+    lists = torch.zeros(2, 2, 4, dtype=torch.int32, device="cuda")
+    one = torch.zeros(1, dtype=torch.int32, device="cuda")
+    bad = [lambda: cache.append(pool, 0, batch, k.cpu(), k), lambda: cache.append(pool, 0, batch, k, k.float()),
+           lambda: cache.append(pool, 0, batch, k.half(), k.half()), lambda: cache.append(pool, 0, batch, k[:, :1], k[:, :1]),
+           lambda: cache.append(pool, 0, batch, k, torch.zeros(2, 4, 64, dtype=BF16, device="cuda")[:, ::2]),
+           lambda: cache.attend(pool, 0, batch, q[..., :32]), lambda: cache.attend(pool, 0, batch, q[0]),
+           lambda: cache.attend(pool, 0, batch, torch.zeros(2, 4, 128, dtype=BF16, device="cuda")[..., ::2]),
+           lambda: cache.attend(pool, 0, batch, q, out=q.float()), lambda: cache.attend(pool, 0, batch, q, out=q[:1]),
+           lambda: cache.attend(pool, 0, batch, q, lists=lists[:1]), lambda: cache.attend(pool, 0, batch, q, lists=lists.long()),
+           lambda: cache.attend(pool, 0, batch, q, scratch=q.cpu()), lambda: cache.select(pool, 0, batch, q, keep=3, lists=lists[:, :1]),
+           lambda: cache.Batch(table, lens[:1], cu, 1), lambda: cache.Batch(table, lens, cu[:2], 1),
+           lambda: cache.Batch(table[:, ::2], lens, cu, 1), lambda: cache.reserve(pool, table, lens, refs[:2]),
+           lambda: cache.fork(pool, table, lens, refs, one, cu), lambda: cache.release(pool, table, lens, refs, one.long()),
+           lambda: cache.compact(pool, table, refs, table_out=table[:1]), lambda: cache.copy_pages(pool, one, cu),
+           lambda: cache.PagedCache(pool.k, pool.v[:, :2], pool.scale, pool.kmean),
+           lambda: cache.PagedCache(pool.k, pool.v, pool.scale.double(), pool.kmean)]
+    for i, call in enumerate(bad):
+        with pytest.raises(ValueError):
+            call()
+            raise AssertionError(f"call {i} was not refused")
+    for st, call in ((1, lambda: cache.attend(pool, 1, batch, q)), (1, lambda: cache.append(pool, -1, batch, k, k)),
+                     (1, lambda: cache.select(pool, 0, batch, q, keep=0)), (1, lambda: cache.select(pool, 0, batch, q, keep=2, first=2)),
+                     (2, lambda: cache.attend(pool, 0, batch, q[:, :3])), (1, lambda: cache.attend(pool, 0, batch, q, scale=float("nan"))),
+                     (4, lambda: cache.select(pool, 0, batch, q, keep=3, scratch=torch.zeros(4, device="cuda"))),
+                     (4, lambda: cache.attend(pool, 0, batch, q, scratch=torch.zeros(4, device="cuda"))),
+                     (4, lambda: cache.reserve(pool, table, lens, refs, scratch=torch.zeros(4, device="cuda")))):
+        with pytest.raises(cache.SsbaError) as e:
+            call()
+        assert e.value.status == st
+    # nothing to do is no error
+    none = torch.zeros(0, 4, 64, dtype=BF16, device="cuda")
+    assert cache.attend(pool, 0, batch, none).shape == none.shape
+    cache.append(pool, 0, batch, none[:, :2], none[:, :2])
+    empty = one[:0]
+    assert cache.fork(pool, table, lens, refs, empty, empty).tolist() == [0, 0]
+    assert cache.release(pool, table, lens, refs, empty).tolist() == [0, 0]
+    cache.copy_pages(pool, empty, empty)
+
+
 # ---- a run of all of them -------------------------------------------------------------
 
 @pytest.mark.parametrize("dtype", [BF16, F32])
