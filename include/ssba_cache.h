@@ -121,7 +121,7 @@ ssba_status ssba_cache_select_workspace_size(const ssba_cache* c, const ssba_cac
  * pages that are not there rank last.  `lists` int32 [rows][kv_heads][1 + keep]:
  * the count, page numbers of the sequence (columns of the table) ascending,
  * then -1.  Appending must come first: only complete pages are scored.
- * `scratch` 16-byte aligned (NULL where its size is 0: tables of up to 1024
+ * `scratch` 16-byte aligned (NULL where its size is 0: tables of up to 1152
  * pages). */
 ssba_status ssba_cache_select(const ssba_cache* c, int32_t layer, const ssba_cache_batch* b,
                               const ssba_cache_query* q, const void* query, int32_t* lists, size_t lists_bytes,

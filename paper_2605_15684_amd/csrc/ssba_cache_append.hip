@@ -8,7 +8,9 @@
 // 1 KB a wave; other pages get their few bytes directly.
 // The sum of a page's codes is exact in fp32 (at most 64 codes of at most 448
 // in steps of 2^-9: 24 bits), in any order.
-// Bound by bytes: new rows read once, one byte a value written.
+// Bound by bytes, new rows read once and one byte a value written: four prompts
+// of 5 to 8 thousand tokens, 8 heads, D 128 bf16 (109 MB) take 24 us, 4.5 TB/s;
+// one token of each of 8 sequences takes 6 us, its chain of dependent loads.
 #include <hip/hip_runtime.h>
 #include <hip/hip_bf16.h>
 

@@ -20,6 +20,19 @@
 // formed again.  What m lags behind is harmless in fp32 and bf16.
 // bf16: V's page scale is added in the exponent (log2) instead of multiplying
 // every probability; the lane's sum is divided by it again.
+//
+// What bounds it, and what it reaches (launch alone):
+//   few columns   the pages' bytes: 64 sequences of 8 to 16 thousand tokens, 4 kv
+//                 heads, D 128: 121 us, 5.4 TB/s.  Three waves a SIMD with one
+//                 step under way each; four (128 registers) take 148 us, two
+//                 steps under way as long as one.
+//   many columns  matrix and vector work: 4096 tokens x 16 heads over 16384
+//                 keys, D 128: 450 us, 1.22 PFLOP/s.  Two waves a SIMD, 64
+//                 columns each: their O takes half of the registers, so the
+//                 queries stay in the LDS.
+//   lists         few columns of a tile are in use, so vector issue: 1024 tokens
+//                 x 8 kv heads x 20 pages of 32, D 64, G 3: 48 us, 14 TB/s
+//                 from the L2.
 #include <hip/hip_runtime.h>
 #include <hip/hip_bf16.h>
 
@@ -133,20 +146,32 @@ __global__ __launch_bounds__(P::THREADS, P::R > 1 ? 2 : P::THREADS > 512 ? 4 : 3
   const int page_log2 = a.c.page_log2;
   const int gpp_log2 = page_log2 - 4;   // groups per page
 
-  // Which keys and columns.  Consecutive items run on one XCD, so that the
-  // column tiles of a head read its keys from one L2.
+  // Which keys and columns.  With several column tiles to a head, the items of
+  // one XCD (blockIdx mod 8) are consecutive, so that the tiles of a head read
+  // its keys from one L2.  Causal tiles differ in length, later tokens see
+  // more: long ones start first, within a head, or within all heads of the XCD
+  // where these come out even (4 prompts of up to 2048 tokens, 16 heads on 4, D
+  // 128: 72.6 us, heads one after another 75.1).
   unsigned id = blockIdx.x;
-  if (P::QLDS) {
-    const unsigned per = gridDim.x / 8, rest = gridDim.x % 8, x = id % 8;
-    id = x * per + min(x, rest) + id / 8;
+  int split, ct;
+  const unsigned heads = (unsigned)a.b.seqs * a.c.kv_heads;
+  if (P::QLDS && a.causal && heads % 8 == 0) {
+    const unsigned per = heads / 8 * a.splits, i = id / 8, rest = i % per;
+    split = rest % a.splits;
+    ct = a.col_tiles - 1 - i / per;
+    id = id % 8 * (heads / 8) + rest / a.splits;   // (sequence, head)
+  } else {
+    if (P::QLDS) {
+      const unsigned per = gridDim.x / 8, rest = gridDim.x % 8, x = id % 8;
+      id = x * per + min(x, rest) + id / 8;
+    }
+    split = id % a.splits;
+    id /= a.splits;
+    ct = id % a.col_tiles;
+    if (a.causal) ct = a.col_tiles - 1 - ct;
+    id /= a.col_tiles;
   }
-  const int split = id % a.splits;
-  id /= a.splits;
-  int ct = id % a.col_tiles;
-  const unsigned first = id - ct;
-  if (a.causal) ct = a.col_tiles - 1 - ct;   // later tokens see more: their tiles start first
-  const unsigned item = first + ct;
-  id /= a.col_tiles;
+  const unsigned item = id * a.col_tiles + ct;
   Item it;
   it.h = id % a.c.kv_heads;
   const int unit = id / a.c.kv_heads;

@@ -85,7 +85,7 @@ struct SelectArgs {
   int tiles;        // tiles of 16 tokens of a sequence
 };
 constexpr int kSelectPages = 64;     // pages a workgroup scores at a time
-constexpr int kSelectInLds = 1024;   // pages whose scores of 16 tokens the LDS holds
+constexpr int kSelectInLds = 1152;   // pages whose scores of 16 tokens the LDS holds (144 of its 160 KB)
 
 // What the selection launches (ssba_cache_api.cpp decides).
 enum SelectKind { kSelectRow, kSelectTile, kSelectRowLong, kSelectTileLong };

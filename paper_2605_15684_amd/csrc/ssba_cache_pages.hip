@@ -1,6 +1,9 @@
 // Page bookkeeping of the cache (include/ssba_cache.h): one workgroup walks
 // the small arrays (references, page table) and leaves a list of page copies;
-// a second launch moves the pages of all layers.
+// a second launch moves the pages of all layers.  The walk is bound by the
+// latency of its steps (16 rows x 33 entries, 640 pages: fork 5.7 us, release
+// 3.9, reserve 3.0; 64 rows x 257 entries: 18, 22, 17), the copy by HBM (100
+// pages x 24 layers of 35 KB: 31 us, 5.6 TB/s read and written).
 #include <hip/hip_runtime.h>
 
 #include "ssba_cache_common.h"

@@ -9,14 +9,18 @@
 // have equal scores.  Ranking is on 64-bit keys whose order is that of the
 // scores (rank_key).
 //
-//   k_select_row     one (token, kv head) per workgroup, tables of at most 1024
+//   k_select_row     one (token, kv head) per workgroup, tables of at most 1152
 //                    pages: scores into the LDS, one wave ranks them.  Bound by
 //                    the pooled keys, 2 D bytes a page.
 //   k_select_tile    16 tokens of a sequence per workgroup: a page's pooled key
 //                    serves them all, on v_mfma_f64_16x16x4_f64.  Scores into
-//                    the LDS (at most 1024 pages), or to the scratch.
-//   k_select_scores, k_select_top   longer tables: a row's pages are shared out
-//                    over workgroups, then one workgroup ranks the row.
+//                    the LDS (at most 1152 pages), or to the scratch.
+//   k_select_scores, k_select_top(_waves)   longer tables: a row's pages are
+//                    shared out over workgroups, then one workgroup (where
+//                    there are many rows, one wave) ranks the row.
+// Measured, D 128: 52 tokens x 4 heads x 130 to 256 pages 9.4 us (row); 1024
+// tokens x 8 heads x 384 pages, D 64, 22.7 us (tile, 13 of it the ranking); one
+// token x 4 heads x 4096 pages 5.0 + 10.8 us.
 #include <hip/hip_runtime.h>
 
 #include "ssba_cache_common.h"
@@ -193,7 +197,7 @@ __device__ __forceinline__ void wave_top_any(const uint64_t* keys, int n, int ne
   else if (n <= 256) wave_top<4>(keys, n, need, base, out, lane);
   else if (CAP > 256 && n <= 384) wave_top<6>(keys, n, need, base, out, lane);
   else if (CAP > 256 && n <= 512) wave_top<8>(keys, n, need, base, out, lane);
-  else if (CAP > 512) wave_top<16>(keys, n, need, base, out, lane);
+  else if (CAP > 512) wave_top<kSelectInLds / 64>(keys, n, need, base, out, lane);
 }
 
 // Ranking keys of pages j0, j0 + step, ... below `end` by one row's queries: D / 8 lanes to a page.
@@ -443,6 +447,24 @@ __global__ __launch_bounds__(kTopThreads) void k_select_top(SelectArgs a) {
   }
 }
 
+// Many rows of moderate length: a wave ranks a row of at most 64 C pages, its
+// keys in registers.
+template <int C>
+__global__ __launch_bounds__(256) void k_select_top_waves(SelectArgs a) {
+  const int lane = threadIdx.x & 63;
+  const unsigned id = blockIdx.x * 4 + (threadIdx.x >> 6);
+  const int row = __builtin_amdgcn_readfirstlane(id / a.c.kv_heads);
+  const int h = __builtin_amdgcn_readfirstlane(id % a.c.kv_heads);
+  int seq;
+  SeqView sv;
+  if (row >= a.b.rows || !seq_of_row(a.b, a.c.page_log2, row, lane, &seq, &sv)) return;
+  const Range r = range_of(a, sv, row - sv.begin);
+  const int64_t at = (int64_t)row * a.c.kv_heads + h;
+  int32_t* list = a.lists + at * (1 + a.keep);
+  if (list_ends(a, r, list, lane, 64))
+    wave_top<C>(a.keys + at * a.b.max_pages, r.middle, a.keep - a.first - a.last, a.first, list + 1 + a.first, lane);
+}
+
 template <int D, bool F32>
 hipError_t launch(const SelectArgs& a, const SelectPlan& p, hipStream_t s) {
   const unsigned rows = (unsigned)a.b.rows * a.c.kv_heads;
@@ -463,7 +485,10 @@ hipError_t launch(const SelectArgs& a, const SelectPlan& p, hipStream_t s) {
         const hipError_t e = hipGetLastError();
         if (e != hipSuccess) return e;
       }
-      k_select_top<<<rows, kTopThreads, 0, s>>>(a);
+      // 8192 rows of 1025 pages: a workgroup each 173 us, a wave each 36; 4 rows of 4096: 11 us in workgroups.
+      if (rows >= 1024 && a.b.max_pages <= 2048) k_select_top_waves<32><<<(rows + 3) / 4, 256, 0, s>>>(a);
+      else if (rows >= 1024 && a.b.max_pages <= 4096) k_select_top_waves<64><<<(rows + 3) / 4, 256, 0, s>>>(a);
+      else k_select_top<<<rows, kTopThreads, 0, s>>>(a);
     }
   }
   return hipGetLastError();

@@ -155,6 +155,8 @@ ATTENDS = [  # page, D, heads, kv heads, dtype, causal, sequences
     (16, 64, 12, 4, BF16, True, [(3000, 20), (40, 17), (333, 5)]),        # 64 columns, keys shared by 8 waves and split
     (32, 128, 8, 2, BF16, False, [(2000, 25), (60, 32)]),                 # 128 columns, keys split
     (64, 64, 6, 1, BF16, True, [(1500, 90), (600, 600)]),                 # tiles of 256 columns
+    (16, 64, 8, 4, BF16, True, [(300, 300), (700, 150), (129, 129), (400, 5)]),   # the same, heads a multiple of 8
+    (16, 64, 16, 8, BF16, True, [(2000, 40)]),                            # and keys split
     (64, 128, 5, 1, F32, True, [(1, 1), (700, 1)]),
     (16, 64, 6, 2, F32, True, [(50, 7), (7, 7), (129, 2)]),
     (32, 128, 4, 2, F32, False, [(150, 60), (64, 33)]),
@@ -382,6 +384,9 @@ SELECTS = [  # page, D, heads, kv, dtype, causal, keep, first, last, sequences
     (32, 128, 2, 1, F32, True, 260, 1, 1, [(30000, 20)]),                 # 938 pages, 258 of them chosen
     (16, 64, 2, 1, BF16, True, 5, 1, 1, [(17000, 1), (40, 1)]),           # too many pages for the LDS
     (16, 128, 2, 1, BF16, True, 11, 1, 1, [(20000, 18), (500, 9)]),       # the same in tiles
+    (16, 64, 1, 1, BF16, True, 6, 1, 1, [(18400, 1), (18500, 20)]),       # the last that fit, the first that do not
+    (16, 64, 32, 32, BF16, True, 30, 1, 1, [(20000, 40)]),                # many rows: a wave ranks one
+    (16, 64, 64, 64, F32, False, 400, 0, 2, [(50000, 17)]),               # the same, longer
     (16, 64, 1, 1, BF16, True, 2000, 1, 1, [(150000, 1)]),                # more pages than registers of a workgroup
     (16, 64, 2, 2, BF16, True, 120, 1, 1, [(2000, 1), (2300, 12), (5000, 9), (9000, 1), (12000, 3)]),   # half of them
     (16, 64, 2, 2, F32, True, 300, 0, 1, [(5000, 1), (6100, 1), (8000, 1), (16000, 1)]),   # negative ones among them
@@ -403,7 +408,7 @@ def test_select(page, d, heads, kv, dtype, causal, keep, first, last, seqs):
     assert np.array_equal(lists.cpu().numpy(), want)
 
 
-@pytest.mark.parametrize("columns", [40, 300, 700, 1500])
+@pytest.mark.parametrize("columns", [40, 300, 700, 1152, 1500])
 @pytest.mark.parametrize("max_new", [2, 8])
 def test_select_ties_nan_and_missing_pages(columns, max_new):
     """Equal scores keep the lower page, zeros of both signs are equal, NaN and missing pages come last; the hint
