@@ -173,7 +173,7 @@ AttendPlan plan(const ssba_cache* c, const ssba_cache_batch* b, const ssba_cache
     p.items = (int64_t)b->seqs * c->kv_heads * p.col_tiles;
   }
   const int64_t items = std::max<int64_t>(p.items, 1);
-  if (p.threads == 512) {
+  if (p.tiles >= 4) {
     // One workgroup fills a CU.  Parts of at least 256 keys; as many as make
     // the rounds over the 256 CUs fullest, each part counted as 1/16 round for
     // writing and joining it.
@@ -187,10 +187,12 @@ AttendPlan plan(const ssba_cache* c, const ssba_cache_batch* b, const ssba_cache
     }
   } else if (!f32 && p.kind != ssba::kAttendRows && p.tiles == 1 && keys > 256 && items <= 256 &&
              keys <= (items >= 128 ? 4096 : 1024)) {
-    // 16 waves of one workgroup instead of parts that a second launch joins: where such workgroups fill half the
-    // chip (256 items of 2048 keys, D 128: 23.6 us, in 4 parts 23.5 + 4.1), or an item is short.  A few long ones
-    // need more CUs (4 items of 4096 keys, D 64: 14.8 us, in 16 parts 5.3 + 3.5).  fp32 has no registers for it.
-    p.threads = 1024;
+    // 8 waves of one workgroup instead of parts that a second launch joins: where such workgroups fill half the
+    // chip (208 items of 2048 listed keys, D 128: 20.3 us, in 3 parts 21.5 + 4.0; 160 items of 4000: 28.7 us, in 4
+    // parts 29.8 + 4.2), or an item is short.  Few long ones need more CUs (64 items of 4000 keys, D 128: 21.0 us,
+    // in 8 parts 14.6 + 3.9; 4 items of 4096 keys, D 64: 14.6 us, in 16 parts 5.2 + 3.4), and long ragged ones more
+    // parts (40 sequences of up to 8000 keys: 57 us, in parts 53).  fp32 has no registers for it.
+    p.threads = 512;
   } else if (p.kind != ssba::kAttendRows) {
     // 4 waves of at least 2 steps of 32 keys each, up to about 512 workgroups: more of them fill the chip more
     // evenly but begin and end more often (one sequence of 131072 keys, 4 heads, D 128: 512 33 us, 1024 41 us;

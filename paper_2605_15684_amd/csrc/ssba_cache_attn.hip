@@ -138,7 +138,7 @@ __device__ __forceinline__ int64_t row_at(const AttendArgs& a, const Item& it, i
 }
 
 template <typename P>
-__global__ __launch_bounds__(P::THREADS, P::R > 1 ? 2 : P::THREADS > 512 ? 4 : 3) void k_cache_attend(AttendArgs a) {
+__global__ __launch_bounds__(P::THREADS, P::R > 1 ? 2 : 3) void k_cache_attend(AttendArgs a) {
   constexpr int D = P::D, R = P::R, NQ = P::NQ, NP = P::NP, NH = P::NH, NC = P::NC;
   const int lane = threadIdx.x & 63, n16 = lane & 15, g = lane >> 4;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -692,11 +692,11 @@ hipError_t launch_d(const AttendArgs& a, const AttendPlan& p, int dtype, hipStre
       return f32 ? launch<Shape<D, 1, 3, 3, true, true, 4, 1, false>>(a, p, s)
                  : launch<Shape<D, 1, 1, 1, false, true, 4, 1, false>>(a, p, s);
     case kAttendRow:
-      if (p.threads == 1024) return launch<Shape<D, 1, 1, 2, false, true, 1, 16, false>>(a, p, s);
+      if (p.threads == 512) return launch<Shape<D, 1, 1, 2, false, true, 1, 8, false>>(a, p, s);
       return f32 ? launch<Shape<D, 1, 3, 3, true, true, 1, 4, false>>(a, p, s)
                  : launch<Shape<D, 1, 1, 2, false, true, 1, 4, false>>(a, p, s);
     default:
-      if (p.threads == 1024) return launch<Shape<D, 1, 1, 2, false, false, 1, 16, false>>(a, p, s);
+      if (p.threads == 512 && p.tiles == 1) return launch<Shape<D, 1, 1, 2, false, false, 1, 8, false>>(a, p, s);
       if (f32)
         return p.tiles == 1 ? launch<Shape<D, 1, 3, 3, true, false, 1, 4, false>>(a, p, s)
                             : launch<Shape<D, 1, 3, 3, true, false, 2, 2, false>>(a, p, s);
