@@ -4,11 +4,21 @@ tests/sanitize/cache_driver.cpp, whose stand-ins for the launchers check grid
 sizes, workspace bounds and plans for 60 000 descriptors at the edges of the
 integer ranges.  No GPU is used; the sanitizers apply to host code only."""
 import os
+import shutil
 import subprocess
 
 import pytest
 
-from test_host_sanitize import CSRC, FLAGS, HIPCC, SAN
+ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+CSRC = os.path.join(ROOT, "paper_2605_15684_amd", "csrc")
+SAN = os.path.join(ROOT, "tests", "sanitize")
+HIPCC = shutil.which("hipcc") or "/opt/rocm/bin/hipcc"
+
+# Host-only compilation; each sanitizer flag applies to the host side only.
+FLAGS = ["-x", "hip", "--cuda-host-only", "-O1", "-g", "-std=c++17", "-fno-omit-frame-pointer",
+         "-Xarch_host", "-fsanitize=address", "-Xarch_host", "-fsanitize=undefined",
+         "-Xarch_host", "-fno-sanitize-recover=all",
+         "-I", os.path.join(ROOT, "include"), "-I", CSRC]
 
 
 @pytest.mark.skipif(not os.path.exists(HIPCC), reason="hipcc not installed")
