@@ -30,9 +30,11 @@
 //                 keys, D 128: 450 us, 1.22 PFLOP/s.  Two waves a SIMD, 64
 //                 columns each: their O takes half of the registers, so the
 //                 queries stay in the LDS.
-//   lists         few columns of a tile are in use, so vector issue: 1024 tokens
-//                 x 8 kv heads x 20 pages of 32, D 64, G 3: 48 us, 14 TB/s
-//                 from the L2.
+//   lists         few columns of a tile are in use, so vector issue.  Where a
+//                 wave has a row alone and G is at most 8, a tile is two times
+//                 the same 8 columns with other keys (J): half the exponentials.
+//                 1024 tokens x 8 kv heads x 20 pages of 32, D 64, G 3: 43 us, 16
+//                 TB/s from the L2; J 1 48 us, J 4 49 us (registers).
 #include <hip/hip_runtime.h>
 #include <hip/hip_bf16.h>
 
@@ -43,6 +45,7 @@ namespace {
 
 typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef float floatx2 __attribute__((ext_vector_type(2)));
 typedef float floatx4 __attribute__((ext_vector_type(4)));
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 typedef uint32_t u32x4a4 __attribute__((ext_vector_type(4), aligned(4)));
@@ -83,14 +86,17 @@ __device__ __forceinline__ void split_bf16(float x, __bf16 (&t)[NS]) {
 // What a variant is made of.  A workgroup has CG * KP waves: CG column groups,
 // each of whose keys KP waves share.  NQ, NP: bf16 terms of a query value and
 // of a probability.  QLDS: the queries stay in the LDS, not in registers.
-template <int D_, int R_, int NQ_, int NP_, bool F32_, bool LISTED_, int CG_, int KP_, bool QLDS_>
+// J: a tile of 16 columns is J times the same 16 / J columns, each with other
+// keys.
+template <int D_, int R_, int NQ_, int NP_, bool F32_, bool LISTED_, int CG_, int KP_, bool QLDS_, int J_ = 1>
 struct Shape {
-  static constexpr int D = D_, R = R_, NQ = NQ_, NP = NP_, CG = CG_, KP = KP_;
+  static constexpr int D = D_, R = R_, NQ = NQ_, NP = NP_, CG = CG_, KP = KP_, J = J_;
   static constexpr bool F32 = F32_, LISTED = LISTED_, QLDS = QLDS_;
   static constexpr int THREADS = 64 * CG * KP;
   static constexpr int NH = D / 64;   // 64-channel blocks
   static constexpr int NC = D / 16;   // 16-channel tiles of O
-  static constexpr int COLS = 16 * R; // columns of a wave
+  static constexpr int COLS = 16 * R / J;   // columns of a wave
+  static_assert(J == 1 || (LISTED && R == 1 && KP == 1 && !QLDS), "");
 };
 
 // Writes E consecutive channels of an output row.
@@ -138,9 +144,10 @@ __device__ __forceinline__ int64_t row_at(const AttendArgs& a, const Item& it, i
 }
 
 template <typename P>
-__global__ __launch_bounds__(P::THREADS, P::R > 1 ? 2 : 3) void k_cache_attend(AttendArgs a) {
-  constexpr int D = P::D, R = P::R, NQ = P::NQ, NP = P::NP, NH = P::NH, NC = P::NC;
+__global__ __launch_bounds__(P::THREADS, P::R > 1 ? 2 : P::J > 1 && P::D == 128 ? 2 : 3) void k_cache_attend(AttendArgs a) {
+  constexpr int D = P::D, R = P::R, NQ = P::NQ, NP = P::NP, NH = P::NH, NC = P::NC, J = P::J;
   const int lane = threadIdx.x & 63, n16 = lane & 15, g = lane >> 4;
+  const int mine = J > 1 ? n16 / P::COLS : 0;   // which of the J keys' share this lane's column has
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int cg = wave % P::CG, kp = wave / P::CG;
   const int page_log2 = a.c.page_log2;
@@ -194,7 +201,7 @@ __global__ __launch_bounds__(P::THREADS, P::R > 1 ? 2 : 3) void k_cache_attend(A
   __shared__ u32x4 s_q[P::QLDS ? P::CG * R * NH * 2 * 64 : 1];
 #pragma unroll
   for (int r = 0; r < R; ++r) {
-    const int col = cbase + r * 16 + n16;
+    const int col = cbase + r * 16 + (J > 1 ? n16 % P::COLS : n16);
     const bool in = col <= cend;
     lim[r] = in ? limit(it.tok0 + (P::LISTED ? 0 : col / a.group)) : 0;
     if (P::QLDS && kp != r % P::KP) continue;   // the waves that share columns share the loading
@@ -228,8 +235,19 @@ __global__ __launch_bounds__(P::THREADS, P::R > 1 ? 2 : 3) void k_cache_attend(A
     }
   }
   if (P::QLDS) __syncthreads();
+  // J > 1: share j's product has the queries in share j's columns, 0 in the others, so that one tile collects all J.
+  Frag qj[J][NQ][NH * 2];
+  if (J > 1)
+#pragma unroll
+    for (int j = 0; j < J; ++j)
+#pragma unroll
+      for (int ns = 0; ns < NQ; ++ns)
+#pragma unroll
+        for (int x = 0; x < NH * 2; ++x)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) qj[j][ns][x].u[e] = mine == j ? q[0][ns][x].u[e] : 0u;
 
-  // Groups of 16 keys, and this wave's steps of two groups.
+  // Groups of 16 keys, and this wave's steps of J times two groups.
   const int32_t* list = nullptr;
   int groups;
   if (P::LISTED) {
@@ -238,7 +256,7 @@ __global__ __launch_bounds__(P::THREADS, P::R > 1 ? 2 : 3) void k_cache_attend(A
   } else {
     groups = (maxlim + 15) >> 4;
   }
-  const int steps = (groups + 1) >> 1;
+  const int steps = (groups + 2 * J - 1) / (2 * J);
   // Shares that differ by one step at most.
   int s0 = 0, s1 = steps;
   if (!P::LISTED || P::KP > 1) {
@@ -277,24 +295,25 @@ __global__ __launch_bounds__(P::THREADS, P::R > 1 ? 2 : 3) void k_cache_attend(A
     m_vs = P::F32 ? vs : 1.f / vs;
     m_lv = P::F32 ? 0.f : __builtin_amdgcn_logf(vs);
   };
-  int chunk = -1;   // 32 steps a chunk
+  int chunk = -1;   // 32 / J steps a chunk
 
   struct Step {
-    u32x4 k[2][NH], v[2][NH];
-    int key[2];
+    u32x4 k[2 * J][NH], v[2 * J][NH];
+    int key[2];   // J > 1: these four of the lane's share
     float ks[2], vs[2], lv[2];
-    int64_t off[2];
+    int64_t off[2 * J];
   };
   // The group numbers, scales and K codes of step s, then its V codes.
   auto fetch_k = [&](int s, Step& x) {
-    if ((s >> 5) != chunk) {
-      chunk = s >> 5;
+    if (s * J >> 5 != chunk) {
+      chunk = s * J >> 5;
       load_chunk(chunk);
     }
 #pragma unroll
-    for (int t = 0; t < 2; ++t) {
-      const int page = lane_i(m_page, (2 * s + t) & 63);
-      const int sub = ((2 * s + t) & ((1 << gpp_log2) - 1)) * 16 * D;
+    for (int t = 0; t < 2 * J; ++t) {
+      const int gr = 2 * J * s + t;
+      const int page = lane_i(m_page, gr & 63);
+      const int sub = (gr & ((1 << gpp_log2) - 1)) * 16 * D;
       x.off[t] = (int64_t)max(page, 0) * a.c.page_bytes + head_off + sub;
       const uint8_t* kp_ = a.c.k + x.off[t];
 #pragma unroll
@@ -302,16 +321,23 @@ __global__ __launch_bounds__(P::THREADS, P::R > 1 ? 2 : 3) void k_cache_attend(A
     }
 #pragma unroll
     for (int t = 0; t < 2; ++t) {   // behind the loads: the scales may still be on their way
-      const int l = (2 * s + t) & 63;
-      x.key[t] = lane_i(m_key, l);
-      x.ks[t] = lane_f(m_ks, l);
-      x.vs[t] = lane_f(m_vs, l);
-      if (!P::F32) x.lv[t] = lane_f(m_lv, l);
+      const int l = (2 * J * s + t) & 63;
+      if (J > 1) {
+        x.key[t] = __shfl(m_key, l + 2 * mine);
+        x.ks[t] = __shfl(m_ks, l + 2 * mine);
+        x.vs[t] = __shfl(m_vs, l + 2 * mine);
+        if (!P::F32) x.lv[t] = __shfl(m_lv, l + 2 * mine);
+      } else {
+        x.key[t] = lane_i(m_key, l);
+        x.ks[t] = lane_f(m_ks, l);
+        x.vs[t] = lane_f(m_vs, l);
+        if (!P::F32) x.lv[t] = lane_f(m_lv, l);
+      }
     }
   };
   auto fetch_v = [&](Step& x) {
 #pragma unroll
-    for (int t = 0; t < 2; ++t) {
+    for (int t = 0; t < 2 * J; ++t) {
       const uint8_t* vp = a.c.v + x.off[t];
 #pragma unroll
       for (int hh = 0; hh < NH; ++hh) x.v[t][hh] = *reinterpret_cast<const u32x4*>(vp + lane * 16 + hh * 1024);
@@ -329,48 +355,61 @@ __global__ __launch_bounds__(P::THREADS, P::R > 1 ? 2 : 3) void k_cache_attend(A
   }
 
   floatx4 s[2][R];
-  auto scores = [&](const Step& x) {
+  auto scores = [&](Step& x) {
+    if (J > 1 && __builtin_amdgcn_ballot_w64(max(x.key[0], x.key[1]) + 16 > minlim)) {
+      // Keys that are not seen become 0: 0 times a NaN would reach the other shares' columns (their sums run over
+      // the same tile).  A NaN that is seen makes all of a row's columns NaN anyway.
+#pragma unroll
+      for (int t = 0; t < 2 * J; ++t)
+        if (lane_i(x.key[t & 1], (t >> 1) * P::COLS) + n16 >= maxlim)
+#pragma unroll
+          for (int hh = 0; hh < NH; ++hh) x.k[t][hh] = u32x4{0, 0, 0, 0};
+    }
     // The queries are read from the LDS again each step: hidden from the
     // compiler, which would otherwise keep them in registers and spill.
     int q_at = cg * R * NH * 2 * 64 + lane;
     if (P::QLDS) asm volatile("" : "+v"(q_at));
     const floatx4 zero = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-    for (int hh = 0; hh < NH; ++hh)
+    for (int j = 0; j < J; ++j)
 #pragma unroll
-      for (int u = 0; u < 2; ++u) {
-        Frag k[2];
+      for (int hh = 0; hh < NH; ++hh)
 #pragma unroll
-        for (int t = 0; t < 2; ++t) {
-          k[t].p[0] = codes_lo(x.k[t][hh][2 * u]);
-          k[t].p[1] = codes_hi(x.k[t][hh][2 * u]);
-          k[t].p[2] = codes_lo(x.k[t][hh][2 * u + 1]);
-          k[t].p[3] = codes_hi(x.k[t][hh][2 * u + 1]);
-        }
+        for (int u = 0; u < 2; ++u) {
+          Frag k[2];
 #pragma unroll
-        for (int ns = NQ - 1; ns >= 0; --ns)
-#pragma unroll
-          for (int r = 0; r < R; ++r) {
-            Frag b;
-            if (P::QLDS) {
-              const u32x4 w = s_q[q_at + (r * NH * 2 + hh * 2 + u) * 64];
-#pragma unroll
-              for (int e = 0; e < 4; ++e) b.u[e] = w[e];
-            } else {
-              b = q[r % QREGS][ns][hh * 2 + u];
-            }
-#pragma unroll
-            for (int t = 0; t < 2; ++t)
-              s[t][r] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(
-                  k[t].v, b.v, hh + u == 0 && ns == NQ - 1 ? zero : s[t][r], 0, 0, 0);
+          for (int t = 0; t < 2; ++t) {
+            const u32x4 w = x.k[2 * j + t][hh];
+            k[t].p[0] = codes_lo(w[2 * u]);
+            k[t].p[1] = codes_hi(w[2 * u]);
+            k[t].p[2] = codes_lo(w[2 * u + 1]);
+            k[t].p[3] = codes_hi(w[2 * u + 1]);
           }
-      }
+#pragma unroll
+          for (int ns = NQ - 1; ns >= 0; --ns)
+#pragma unroll
+            for (int r = 0; r < R; ++r) {
+              Frag b;
+              if (P::QLDS) {
+                const u32x4 w = s_q[q_at + (r * NH * 2 + hh * 2 + u) * 64];
+#pragma unroll
+                for (int e = 0; e < 4; ++e) b.u[e] = w[e];
+              } else {
+                b = J > 1 ? qj[j][ns][hh * 2 + u] : q[r % QREGS][ns][hh * 2 + u];
+              }
+#pragma unroll
+              for (int t = 0; t < 2; ++t)
+                s[t][r] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(
+                    k[t].v, b.v, j + hh + u == 0 && ns == NQ - 1 ? zero : s[t][r], 0, 0, 0);
+            }
+        }
   };
 
   bool settled = false;   // every column has a maximum
   auto finish = [&](Step& x) {
     // Some column does not see some key of this step.
-    const bool edge = max(x.key[0], x.key[1]) + 16 > minlim;
+    const bool far = max(x.key[0], x.key[1]) + 16 > minlim;
+    const bool edge = J > 1 ? __builtin_amdgcn_ballot_w64(far) != 0 : far;
     if (edge) {
 #pragma unroll
       for (int t = 0; t < 2; ++t)
@@ -396,13 +435,22 @@ __global__ __launch_bounds__(P::THREADS, P::R > 1 ? 2 : 3) void k_cache_attend(A
           const float shift = P::F32 ? mu : mu - x.lv[t];
           half[t] = 0.f;
 #pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            const float e = exp2_(__builtin_fmaf(s[t][r][i], x.ks[t], -shift));
-            half[t] = i ? half[t] + e : e;
-            __bf16 terms[NP];
-            split_bf16<NP>(P::F32 ? e * x.vs[t] : e, terms);
+          for (int i = 0; i < 2; ++i) {
+            floatx2 e;
 #pragma unroll
-            for (int ns = 0; ns < NP; ++ns) p[r][ns].v[t * 4 + i] = terms[ns];
+            for (int w = 0; w < 2; ++w) {
+              e[w] = exp2_(__builtin_fmaf(s[t][r][2 * i + w], x.ks[t], -shift));
+              half[t] = i + w ? half[t] + e[w] : e[w];
+              if (P::F32) e[w] *= x.vs[t];
+            }
+#pragma unroll
+            for (int ns = 0; ns < NP; ++ns) {   // both at once: one conversion
+              p[r][ns].p[t * 2 + i] = __builtin_convertvector(e, bf16x2);
+              if (ns + 1 < NP) {
+                e[0] -= (float)p[r][ns].p[t * 2 + i][0];
+                e[1] -= (float)p[r][ns].p[t * 2 + i][1];
+              }
+            }
           }
         }
         sum[r] = P::F32 ? half[0] + half[1] : __builtin_fmaf(half[0], x.vs[0], half[1] * x.vs[1]);
@@ -441,8 +489,9 @@ __global__ __launch_bounds__(P::THREADS, P::R > 1 ? 2 : 3) void k_cache_attend(A
       // others do not is taken out as well and given to those that see it.
       uint32_t some = 0;
 #pragma unroll
-      for (int t = 0; t < 2; ++t) {
-        const int left = min(max(maxlim - x.key[t] - 4 * g, 0), 4);
+      for (int t = 0; t < 2 * J; ++t) {
+        const int key = J > 1 ? lane_i(x.key[t & 1], (t >> 1) * P::COLS) : x.key[t & 1];
+        const int left = min(max(maxlim - key - 4 * g, 0), 4);
         const uint32_t keep = left == 4 ? ~0u : (1u << (8 * left)) - 1u;
 #pragma unroll
         for (int hh = 0; hh < NH; ++hh)
@@ -452,7 +501,7 @@ __global__ __launch_bounds__(P::THREADS, P::R > 1 ? 2 : 3) void k_cache_attend(A
             some |= ((x.v[t][hh][e] & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u;
           }
       }
-      if (__builtin_amdgcn_ballot_w64(some != 0)) {
+      if (!P::LISTED && __builtin_amdgcn_ballot_w64(some != 0)) {   // lists: all columns see the same
         // 1 where a column sees a key, times 1 where the key's value is NaN (bit
         // arithmetic: comparisons would take a scalar register pair each).
         constexpr uint32_t kOne = 0x3f80;   // bf16
@@ -491,21 +540,30 @@ __global__ __launch_bounds__(P::THREADS, P::R > 1 ? 2 : 3) void k_cache_attend(A
     }
     if (P::QLDS) __builtin_amdgcn_s_setprio(1);
 #pragma unroll
-    for (int hh = 0; hh < NH; ++hh)
+    for (int j = 0; j < J; ++j) {
+      Frag pj[NP];   // share j's columns, 0 in the others
+      if (J > 1)
 #pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        Frag v;
-        v.p[0] = codes_lo(x.v[0][hh][e]);
-        v.p[1] = codes_hi(x.v[0][hh][e]);
-        v.p[2] = codes_lo(x.v[1][hh][e]);
-        v.p[3] = codes_hi(x.v[1][hh][e]);
+        for (int ns = 0; ns < NP; ++ns)
 #pragma unroll
-        for (int ns = NP - 1; ns >= 0; --ns)
+          for (int e = 0; e < 4; ++e) pj[ns].u[e] = mine == j ? p[0][ns].u[e] : 0u;
 #pragma unroll
-          for (int r = 0; r < R; ++r)
-            o[r][hh * 4 + e] =
-                __builtin_amdgcn_mfma_f32_16x16x32_bf16(v.v, p[r][ns].v, o[r][hh * 4 + e], 0, 0, 0);
-      }
+      for (int hh = 0; hh < NH; ++hh)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          Frag v;
+          v.p[0] = codes_lo(x.v[2 * j][hh][e]);
+          v.p[1] = codes_hi(x.v[2 * j][hh][e]);
+          v.p[2] = codes_lo(x.v[2 * j + 1][hh][e]);
+          v.p[3] = codes_hi(x.v[2 * j + 1][hh][e]);
+#pragma unroll
+          for (int ns = NP - 1; ns >= 0; --ns)
+#pragma unroll
+            for (int r = 0; r < R; ++r)
+              o[r][hh * 4 + e] =
+                  __builtin_amdgcn_mfma_f32_16x16x32_bf16(v.v, J > 1 ? pj[ns].v : p[r][ns].v, o[r][hh * 4 + e], 0, 0, 0);
+        }
+    }
   };
 
   // One step's codes are under way or in use: V comes during the scores, the
@@ -530,11 +588,30 @@ __global__ __launch_bounds__(P::THREADS, P::R > 1 ? 2 : 3) void k_cache_attend(A
     l[r] += __shfl_xor(l[r], 32);
   }
 
+  if (J > 1) {
+    // The shares of a column, scaled to their common maximum (-inf: nothing seen, O and l are 0).
+    float mall = m[0];
+#pragma unroll
+    for (int x = P::COLS; x < 16; x <<= 1) mall = fmaxf(mall, __shfl_xor(mall, x));
+    const float f = m[0] == mall ? 1.f : exp2_(m[0] - mall);
+    l[0] *= f;
+#pragma unroll
+    for (int x = P::COLS; x < 16; x <<= 1) l[0] += __shfl_xor(l[0], x);
+#pragma unroll
+    for (int c = 0; c < NC; ++c) {
+      o[0][c] *= f;
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+#pragma unroll
+        for (int x = P::COLS; x < 16; x <<= 1) o[0][c][i] += __shfl_xor(o[0][c][i], x);
+    }
+  }
+
   if (P::KP == 1) {
 #pragma unroll
     for (int r = 0; r < R; ++r) {
       const int col = cbase + r * 16 + n16;
-      if (col > cend) continue;
+      if (col > cend || (J > 1 && mine)) continue;
       const int64_t at = row_at<P::LISTED>(a, it, col, a.o_st, a.o_sh) + g * 4;
       const float inv = l[r] == 0.f ? 0.f : 1.f / l[r];
 #pragma unroll
@@ -686,11 +763,12 @@ hipError_t launch(const AttendArgs& a, const AttendPlan& p, hipStream_t s) {
 template <int D>
 hipError_t launch_d(const AttendArgs& a, const AttendPlan& p, int dtype, hipStream_t s) {
   const bool f32 = dtype == SSBA_DT_F32;
-  // D, R, NQ, NP, fp32, lists, column groups, waves that share keys, queries in the LDS
+  // D, R, NQ, NP, fp32, lists, column groups, waves that share keys, queries in the LDS, shares of a tile
   switch (p.kind) {
     case kAttendRows:
-      return f32 ? launch<Shape<D, 1, 3, 3, true, true, 4, 1, false>>(a, p, s)
-                 : launch<Shape<D, 1, 1, 1, false, true, 4, 1, false>>(a, p, s);
+      if (f32) return launch<Shape<D, 1, 3, 3, true, true, 4, 1, false>>(a, p, s);
+      return a.group <= 8 ? launch<Shape<D, 1, 1, 1, false, true, 4, 1, false, 2>>(a, p, s)
+                          : launch<Shape<D, 1, 1, 1, false, true, 4, 1, false>>(a, p, s);
     case kAttendRow:
       if (p.threads == 512) return launch<Shape<D, 1, 1, 2, false, true, 1, 8, false>>(a, p, s);
       return f32 ? launch<Shape<D, 1, 3, 3, true, true, 1, 4, false>>(a, p, s)

@@ -345,6 +345,9 @@ LISTED = [  # page, D, heads, kv, dtype, causal, keep, sequences
     (64, 64, 2, 1, F32, True, 2, [(500, 1)]),
     (16, 64, 32, 32, BF16, True, 3, [(150, 130)]),                        # a wave per row
     (32, 128, 64, 32, F32, True, 2, [(140, 131)]),
+    (32, 64, 48, 16, BF16, True, 5, [(300, 131), (40, 9)]),               # the same with 3 query heads to a kv head
+    (16, 128, 128, 16, BF16, True, 7, [(260, 140)]),                      # 8
+    (64, 64, 144, 16, BF16, False, 3, [(400, 133)]),                      # 9
 ]
 
 
@@ -369,6 +372,48 @@ def test_attend_lists(page, d, heads, kv, dtype, causal, keep, seqs):
                        lists=torch.from_numpy(lists).cuda())
     check_attend(got, C.attend(pool, 0, batch, q64, page, lists, causal), keep * page, d, dtype)
     assert (got[0, : heads // kv] == 0).all()
+
+
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("new,kv,group", [(5, 2, 4), (137, 16, 1), (130, 16, 5), (130, 16, 12)])
+def test_attend_lists_nan(d, new, kv, group):
+    """NaN in every place that no listed token holds; then one key and one value that are seen."""
+    from paper_2605_15684_amd import cache
+    rng = np.random.default_rng(new + d + group)
+    page, held, keep = 16, 403, 9
+    clean = make_pool(rng, 1, 30, kv, d, page)
+    batch = make_batch(rng, [(held, new)], page, 30)
+    table, pages = batch[0][0], -(-held // page)
+    lists = np.full((new, kv, 1 + keep), -1, dtype=np.int32)
+    for r in range(new):
+        own = (held - new + r) // page
+        for h in range(kv):
+            n = int(rng.integers(1, keep + 1))
+            lists[r, h, 0] = n
+            lists[r, h, 1:1 + n] = rng.permutation(np.append(rng.permutation(own)[:n - 1], own))
+    assert (lists[..., 0] > 0).all() and lists.max() < pages
+    ko, vo = C.orders(page, d)
+    pool = {x: y.copy() for x, y in clean.items()}
+    for x, order in (("k", ko), ("v", vo)):
+        kept = np.zeros((30, page * d), dtype=bool)          # the last page: tokens behind the sequence are NaN
+        for i in range(pages):
+            kept[table[i], order[: min(held - i * page, page)].ravel()] = True
+        pool[x][0][np.broadcast_to(~kept[:, None], pool[x][0].shape)] = 127
+    q, q64 = rounded(rng, (new, kv * group, d), BF16, 0.3)
+    run = lambda: cache.attend(gpu_pool(pool), 0, gpu_batch(batch, new), q.cuda(), lists=torch.from_numpy(lists).cuda())
+    ref = C.attend(clean, 0, batch, q64, page, lists, True)
+    check_attend(run(), ref, keep * page, d, BF16)
+    at = held - new - 3                                      # a token that all rows see whose list has its page
+    pool["k"][0, table[at // page], 0, ko[at % page, 9]] = 255
+    pool["v"][0, table[at // page], 1, vo[at % page, 7]] = 127
+    got = run().float().cpu().numpy().reshape(new, kv, group, d)
+    want = np.zeros(got.shape, dtype=bool)
+    sees = [[at // page in lists[r, h, 1:1 + lists[r, h, 0]] for h in range(kv)] for r in range(new)]
+    for r in range(new):
+        want[r, 0] = sees[r][0]
+        want[r, 1, :, 7] = sees[r][1]
+    assert want.any() and not want.all(axis=(0, 2, 3)).any()
+    assert np.array_equal(np.isnan(got), want)
 
 
 SELECTS = [  # page, D, heads, kv, dtype, causal, keep, first, last, sequences
