@@ -20,7 +20,7 @@
 //                    there are many rows, one wave) ranks the row.
 // Measured, D 128: 52 tokens x 4 heads x 130 to 256 pages 9.4 us (row); 1024
 // tokens x 8 heads x 384 pages, D 64, 22.7 us (tile, 13 of it the ranking); one
-// token x 4 heads x 4096 pages 5.0 + 10.8 us.
+// token x 4 heads x 4096 pages 5.0 + 8.5 us.
 #include <hip/hip_runtime.h>
 
 #include "ssba_cache_common.h"
@@ -330,11 +330,27 @@ __global__ __launch_bounds__(256) void k_select_scores(SelectArgs a) {
 }
 
 // One workgroup per (row, kv head): the `need` largest keys by radix, 8 bits a
-// pass, then their pages in ascending order.
+// pass, then their pages in ascending order.  Digits are of the keys' distance
+// from the largest high word: where enough scores are within 2^-16 of the
+// largest, whose distances share their first byte, that pass is left out.  A
+// pass has one barrier: every wave looks through the bins, of which there are
+// three sets, one counted, one looked through, one cleared.
+// 4 rows of 4096 pages: 8.5 us (16 waves: few barriers, long chains).
 constexpr int kTopThreads = 1024, kTopWaves = kTopThreads / 64, kTopRegs = 8;
+constexpr int kTopKeys = kTopRegs * kTopThreads;
+
+// Inclusive sum over the lanes up to each.
+__device__ __forceinline__ int wave_scan(int x, int lane) {
+#pragma unroll
+  for (int off = 1; off < 64; off <<= 1) {
+    const int o = __shfl_up(x, off);
+    if (lane >= off) x += o;
+  }
+  return x;
+}
 
 __global__ __launch_bounds__(kTopThreads) void k_select_top(SelectArgs a) {
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int row = blockIdx.x / a.c.kv_heads, h = blockIdx.x % a.c.kv_heads;
   int seq;
   SeqView sv;
@@ -343,25 +359,39 @@ __global__ __launch_bounds__(kTopThreads) void k_select_top(SelectArgs a) {
   const Range r = range_of(a, sv, tok);
   int32_t* list = a.lists + ((int64_t)row * a.c.kv_heads + h) * (1 + a.keep);
   if (!list_ends(a, r, list, threadIdx.x, kTopThreads)) return;
-  const int need = a.keep - a.first - a.last;
+  const int need = a.keep - a.first - a.last;   // < r.middle
   const uint64_t* keys = a.keys + ((int64_t)row * a.c.kv_heads + h) * a.b.max_pages;
 
   // The first kTopRegs keys of each thread stay in registers.
   uint64_t mine[kTopRegs];
+  uint32_t most = 0;
 #pragma unroll
   for (int i = 0; i < kTopRegs; ++i) {
     const int j = i * kTopThreads + threadIdx.x;
     mine[i] = j < r.middle ? keys[j] : 0;
+    most = max(most, (uint32_t)(mine[i] >> 32));
   }
-  __shared__ int s_hist[256];
-  __shared__ int s_bin, s_left, s_wave[kTopWaves];
+  for (int j = kTopKeys + threadIdx.x; j < r.middle; j += kTopThreads) most = max(most, (uint32_t)(keys[j] >> 32));
+  __shared__ int s_hist[3][256];
+  __shared__ uint32_t s_most[kTopWaves];
+  __shared__ int s_wave[kTopRegs * kTopWaves];
+  most = wave_max(most);
+  if (lane == 0) s_most[wave] = most;
+  if (threadIdx.x < 3 * 256) s_hist[threadIdx.x >> 8][threadIdx.x & 255] = 0;
+  __syncthreads();
+#pragma unroll
+  for (int w = 0; w < kTopWaves; ++w) most = max(most, s_most[w]);
+  const uint64_t top = (uint64_t)most << 32 | 0xffffffffu;
+#pragma unroll
+  for (int i = 0; i < kTopRegs; ++i) mine[i] = top - mine[i];   // distances: the smallest are wanted
+
   uint64_t prefix = 0;   // the threshold's high bits
-  int left = need;       // places for keys that match the prefix
-  int shift = 64;
-  // Keys share their high bytes, so lanes of a wave with the same digit add once.
-  auto count = [&](uint64_t k, bool in) {
-    const int digit = (int)((k >> shift) & 255);
-    bool todo = in && (shift == 56 || (k >> (shift + 8)) == (prefix >> (shift + 8)));
+  int left = need;       // places for distances that match the prefix
+  int shift = 56, set = 0;
+  // Distances share their high bytes, so lanes of a wave with the same digit add once.
+  auto count = [&](uint64_t d, bool in) {
+    const int digit = (int)(d >> shift) & 255;
+    bool todo = in && (shift == 56 || (d >> (shift + 8)) == (prefix >> (shift + 8)));
 #pragma unroll
     for (int turn = 0; turn < 2; ++turn) {
       const uint64_t m = __builtin_amdgcn_ballot_w64(todo);
@@ -369,79 +399,97 @@ __global__ __launch_bounds__(kTopThreads) void k_select_top(SelectArgs a) {
       const int first = __builtin_ctzll(m);
       const bool same = todo && digit == __builtin_amdgcn_readlane(digit, first);
       const uint64_t ms = __builtin_amdgcn_ballot_w64(same);
-      if (lane == first) atomicAdd(&s_hist[digit], __popcll(ms));
+      if (lane == first) atomicAdd(&s_hist[set][digit], __popcll(ms));
       if (same) todo = false;
     }
-    if (todo) atomicAdd(&s_hist[digit], 1);
+    if (todo) atomicAdd(&s_hist[set][digit], 1);
   };
-  while (shift > 0) {
-    shift -= 8;
-    if (threadIdx.x < 256) s_hist[threadIdx.x] = 0;
-    __syncthreads();
+  for (bool skip = true;;) {
+    if (skip) shift = 48;   // distances whose first byte is 0
 #pragma unroll
     for (int i = 0; i < kTopRegs; ++i)
       if (i * kTopThreads < r.middle) count(mine[i], i * kTopThreads + (int)threadIdx.x < r.middle);
-    for (int j0 = kTopRegs * kTopThreads; j0 < r.middle; j0 += kTopThreads) {
+    for (int j0 = kTopKeys; j0 < r.middle; j0 += kTopThreads) {
       const int j = j0 + threadIdx.x;
-      count(j < r.middle ? keys[j] : 0, j < r.middle);
+      count(j < r.middle ? top - keys[j] : 0, j < r.middle);
     }
     __syncthreads();
-    // Bins from the top: the one in which the `left`-th key lies.
-    if (wave == 0) {
-      int c[4], sum = 0;   // bins 255 - 4 lane - i
+    // The bin in which the `left`-th distance lies.
+    int c[4], sum = 0;
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        c[i] = s_hist[255 - 4 * lane - i];
-        sum += c[i];
-      }
-      int incl = sum;
-#pragma unroll
-      for (int off = 1; off < 64; off <<= 1) {
-        const int o = __shfl_up(incl, off);
-        if (lane >= off) incl += o;
-      }
-      int above = incl - sum;
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        if (above < left && above + c[i] >= left) {
-          s_bin = 255 - 4 * lane - i;
-          s_left = left - above;
-        }
-        above += c[i];
-      }
+    for (int i = 0; i < 4; ++i) {
+      c[i] = s_hist[set][4 * lane + i];
+      sum += c[i];
     }
-    __syncthreads();
-    prefix |= (uint64_t)s_bin << shift;
-    left = s_left;
-    const int in_bin = s_hist[s_bin];
-    __syncthreads();
-    if (in_bin == left) break;   // the whole bin is taken
+    const int third = set == 0 ? 2 : set - 1;   // counted two passes on
+    if (threadIdx.x < 256) s_hist[third][threadIdx.x] = 0;
+    set = set == 2 ? 0 : set + 1;
+    const int incl = wave_scan(sum, lane);
+    const uint64_t reach = __builtin_amdgcn_ballot_w64(incl >= left);
+    if (!reach) {   // fewer than `need` have a first byte of 0
+      skip = false;
+      shift = 56;
+      continue;
+    }
+    skip = false;
+    int before = incl - sum, bin = 0, in_bin = 0, above = 0;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      if (before < left && before + c[i] >= left) {
+        bin = 4 * lane + i;
+        in_bin = c[i];
+        above = before;
+      }
+      before += c[i];
+    }
+    const int at = __builtin_ctzll(reach);
+    bin = __builtin_amdgcn_readlane(bin, at);
+    in_bin = __builtin_amdgcn_readlane(in_bin, at);
+    prefix |= (uint64_t)bin << shift;
+    left -= __builtin_amdgcn_readlane(above, at);
+    if (in_bin == left || shift == 0) break;   // the whole bin is taken
+    shift -= 8;
   }
-  // Taken: keys above the threshold's prefix, and of those equal to it the first `left`.
+
+  // Taken: distances below the threshold's prefix, and of those equal to it the first `left`.
+  const uint64_t t = prefix >> shift;
   int base = a.first, equal_before = 0;
-  for (int j0 = 0; j0 < r.middle; j0 += kTopThreads) {
-    const int j = j0 + threadIdx.x;
-    bool gt = false, eq = false;
-    if (j < r.middle) {
-      const uint64_t k = keys[j] >> shift, t = prefix >> shift;
-      gt = k > t;
-      eq = k == t;
+  for (int c0 = 0; c0 < r.middle; c0 += kTopKeys) {
+    if (c0) {
+#pragma unroll
+      for (int i = 0; i < kTopRegs; ++i) {
+        const int j = c0 + i * kTopThreads + threadIdx.x;
+        mine[i] = j < r.middle ? top - keys[j] : 0;
+      }
+      __syncthreads();
     }
-    // Equal and larger ones in front of this thread, counted together (16 bits each).
-    const uint64_t meq = __builtin_amdgcn_ballot_w64(eq), mgt = __builtin_amdgcn_ballot_w64(gt);
+    // Equal and nearer ones of each wave and turn, counted together (16 bits each).
+#pragma unroll
+    for (int i = 0; i < kTopRegs; ++i) {
+      const bool in = c0 + i * kTopThreads + (int)threadIdx.x < r.middle;
+      const uint64_t d = mine[i] >> shift;
+      const uint64_t meq = __builtin_amdgcn_ballot_w64(in && d == t), mlt = __builtin_amdgcn_ballot_w64(in && d < t);
+      if (lane == 0) s_wave[i * kTopWaves + wave] = __popcll(meq) | (__popcll(mlt) << 16);
+    }
     __syncthreads();
-    if (lane == 0) s_wave[wave] = __popcll(meq) | (__popcll(mgt) << 16);
-    __syncthreads();
+    const int e0 = s_wave[2 * lane], e1 = s_wave[2 * lane + 1];
+    const int incl = wave_scan(e0 + e1, lane), total = __builtin_amdgcn_readlane(incl, 63);
+    const int ahead = wave & 1 ? incl - e1 : incl - e0 - e1;   // of the lane's entry of this wave's parity
     const uint64_t below = (1ull << lane) - 1;
-    int before = __popcll(meq & below) | (__popcll(mgt & below) << 16), total = 0;
-    for (int w = 0; w < kTopWaves; ++w) {
-      if (w < wave) before += s_wave[w];
-      total += s_wave[w];
+#pragma unroll
+    for (int i = 0; i < kTopRegs; ++i) {
+      const int j = c0 + i * kTopThreads + threadIdx.x;
+      const bool in = j < r.middle;
+      const uint64_t d = mine[i] >> shift;
+      const bool eq = in && d == t, lt = in && d < t;
+      const uint64_t meq = __builtin_amdgcn_ballot_w64(eq), mlt = __builtin_amdgcn_ballot_w64(lt);
+      const int before = __builtin_amdgcn_readlane(ahead, (i * kTopWaves + wave) >> 1) +
+                         (__popcll(meq & below) | (__popcll(mlt & below) << 16));
+      const int rank = equal_before + (before & 0xffff);
+      // Taken ones in front: all nearer ones, and the equal ones that have a place.
+      if (lt || (eq && rank < left))
+        list[1 + base + (before >> 16) + min(rank, left) - min(equal_before, left)] = a.first + j;
     }
-    const int rank = equal_before + (before & 0xffff);
-    const bool take = gt || (eq && rank < left);
-    // Taken ones in front: all larger ones, and the equal ones that have a place.
-    if (take) list[1 + base + (before >> 16) + min(rank, left) - min(equal_before, left)] = a.first + j;
     base += (total >> 16) + min(equal_before + (total & 0xffff), left) - min(equal_before, left);
     equal_before += total & 0xffff;
   }
@@ -485,7 +533,7 @@ hipError_t launch(const SelectArgs& a, const SelectPlan& p, hipStream_t s) {
         const hipError_t e = hipGetLastError();
         if (e != hipSuccess) return e;
       }
-      // 8192 rows of 1025 pages: a workgroup each 173 us, a wave each 36; 4 rows of 4096: 11 us in workgroups.
+      // 8192 rows of 1025 pages: a workgroup each 173 us, a wave each 36; 4 rows of 4096: 8.5 us in workgroups.
       if (rows >= 1024 && a.b.max_pages <= 2048) k_select_top_waves<32><<<(rows + 3) / 4, 256, 0, s>>>(a);
       else if (rows >= 1024 && a.b.max_pages <= 4096) k_select_top_waves<64><<<(rows + 3) / 4, 256, 0, s>>>(a);
       else k_select_top<<<rows, kTopThreads, 0, s>>>(a);

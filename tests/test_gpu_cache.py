@@ -435,6 +435,7 @@ SELECTS = [  # page, D, heads, kv, dtype, causal, keep, first, last, sequences
     (16, 64, 1, 1, BF16, True, 2000, 1, 1, [(150000, 1)]),                # more pages than registers of a workgroup
     (16, 64, 2, 2, BF16, True, 120, 1, 1, [(2000, 1), (2300, 12), (5000, 9), (9000, 1), (12000, 3)]),   # half of them
     (16, 64, 2, 2, F32, True, 300, 0, 1, [(5000, 1), (6100, 1), (8000, 1), (16000, 1)]),   # negative ones among them
+    (16, 64, 2, 1, F32, True, 1800, 1, 1, [(40000, 1), (30000, 3), (18500, 2)]),           # the same, longer
 ]
 
 
