@@ -19,9 +19,11 @@
 //                    shared out over workgroups, then one workgroup (where
 //                    there are many rows, one wave) ranks the row.
 // Measured, D 128: 52 tokens x 4 heads x 130 to 256 pages 9.4 us (row); 1024
-// tokens x 8 heads x 384 pages, D 64, 22.7 us (tile, 13 of it the ranking); one
-// token x 4 heads x 4096 pages 5.0 + 8.5 us.
+// tokens x 8 heads x 384 pages, D 64, 21.4 us (tile; the ranking 7, the matrix
+// instructions 5); one token x 4 heads x 4096 pages 5.0 + 8.5 us.
 #include <hip/hip_runtime.h>
+
+#include <cstring>
 
 #include "ssba_cache_common.h"
 #include "ssba_common.h"
@@ -30,7 +32,6 @@ namespace ssba {
 namespace {
 
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
-typedef uint32_t u32x4a4 __attribute__((ext_vector_type(4), aligned(4)));
 typedef double doublex4 __attribute__((ext_vector_type(4)));
 
 // The pages a token can choose from: [first, first + middle) are scored.
@@ -46,32 +47,26 @@ __device__ __forceinline__ Range range_of(const SelectArgs& a, const SeqView& sv
   return r;
 }
 
-// Sum over the group's query heads of N channels from `ch` of a row.
+// Sum over the group's query heads, in order, of N channels from `ch` of a row.
 template <bool F32, int N>
 __device__ __forceinline__ void q_sum(const SelectArgs& a, int row, int h, int ch, double (&q)[N]) {
+  constexpr int W = F32 ? N : N / 2;   // words
 #pragma unroll
   for (int c = 0; c < N; ++c) q[c] = 0.0;
   const int64_t at = (int64_t)row * a.st + (int64_t)h * a.group * a.sh + ch;
 #pragma unroll 2
   for (int g = 0; g < a.group; ++g) {
+    uint32_t w[W];
     if (F32) {
-      const float* x = static_cast<const float*>(a.q) + at + g * a.sh;
+      std::memcpy(w, __builtin_assume_aligned(static_cast<const float*>(a.q) + at + g * a.sh, 4), 4 * W);
 #pragma unroll
-      for (int c = 0; c < N; c += 4) {
-        const u32x4 w = *reinterpret_cast<const u32x4a4*>(x + c);
-#pragma unroll
-        for (int e = 0; e < 4; ++e) q[c + e] += (double)__uint_as_float(w[e]);
-      }
+      for (int c = 0; c < W; ++c) q[c] += (double)__uint_as_float(w[c]);
     } else {
-      const uint16_t* x = static_cast<const uint16_t*>(a.q) + at + g * a.sh;
+      std::memcpy(w, __builtin_assume_aligned(static_cast<const uint16_t*>(a.q) + at + g * a.sh, 2 * N), 4 * W);
 #pragma unroll
-      for (int c = 0; c < N; c += 8) {
-        const u32x4 w = *reinterpret_cast<const u32x4*>(x + c);
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          q[c + 2 * e] += (double)__uint_as_float(w[e] << 16);
-          q[c + 2 * e + 1] += (double)__uint_as_float(w[e] & 0xffff0000u);
-        }
+      for (int c = 0; c < W; ++c) {
+        q[2 * c < N ? 2 * c : 0] += (double)__uint_as_float(w[c] << 16);
+        q[2 * c + 1 < N ? 2 * c + 1 : 0] += (double)__uint_as_float(w[c] & 0xffff0000u);
       }
     }
   }
@@ -258,9 +253,11 @@ __global__ __launch_bounds__(kRowThreads) void k_select_row(SelectArgs a) {
 // lane gets the scores of tokens 4 i + g with page lane % 16.
 template <int D, bool F32, int CAP, bool LDS>
 __global__ __launch_bounds__(kRowThreads) void k_select_tile(SelectArgs a) {
-  constexpr int CH = D / 4, WAVES = kRowThreads / 64;
-  __shared__ uint64_t s_keys[LDS ? 16 * CAP : 1];
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, n16 = lane & 15, g = lane >> 4;
+  constexpr int CH = D / 4, WAVES = kRowThreads / 64, QL = D + 2;   // QL: 16 rows in 16 banks
+  __shared__ alignas(16) uint64_t s_keys[16 * (LDS ? CAP : QL)];
+  static_assert(!LDS || CAP >= QL, "");
+  const int lane = threadIdx.x & 63, n16 = lane & 15, g = lane >> 4;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   unsigned id = blockIdx.x;
   const int tile = id % a.tiles;
   id /= a.tiles;
@@ -270,8 +267,21 @@ __global__ __launch_bounds__(kRowThreads) void k_select_tile(SelectArgs a) {
   if (last < tok0) return;
   const int most = range_of(a, sv, last).middle;   // later tokens see more
   if (most > 0 && a.keep > a.first + a.last) {
+    // The tokens' query sums through the LDS, a share of them by each thread: additions of 64 bits are slow (512
+    // tokens x 4 heads, D 128, 16 query heads each: 15.5 us, every wave for itself 26).
+    {
+      constexpr int PT = D / 32;   // channels of a thread
+      const int t = threadIdx.x / 32, c0 = threadIdx.x % 32 * PT;
+      double sum[PT];
+      q_sum<F32, PT>(a, sv.begin + min(tok0 + t, last), h, c0, sum);
+#pragma unroll
+      for (int c = 0; c < PT; ++c) s_keys[t * QL + c0 + c] = (uint64_t)__double_as_longlong(sum[c]);
+    }
+    __syncthreads();
     double q[CH];
-    q_sum<F32, CH>(a, sv.begin + min(tok0 + n16, last), h, g * CH, q);
+#pragma unroll
+    for (int c = 0; c < CH; ++c) q[c] = __longlong_as_double((long long)s_keys[n16 * QL + g * CH + c]);
+    if (LDS) __syncthreads();
     const int32_t* table = a.b.table + (int64_t)seq * a.b.max_pages + a.first;
     int middle[4];
 #pragma unroll
