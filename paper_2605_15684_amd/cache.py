@@ -36,15 +36,17 @@ _DTYPES = {torch.bfloat16: _lib.DT_BF16, torch.float32: _lib.DT_F32}
 
 # The current HIP stream of a device as a number.  A call of this module costs
 # a few microseconds on the host, of which torch.cuda.current_stream() (it
-# makes a Stream object) would be two.
+# makes a Stream object) would be two.  Likewise the current device, a quarter
+# of a microsecond through torch.cuda.
 _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or \
     (lambda index: torch.cuda.current_stream(index).cuda_stream)
+_current_device = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)
 
 
 def _call(pool, fn, name: str, *args) -> None:
     """fn(*args, stream) on the current stream of the cache's device."""
     index = pool.index
-    if torch.cuda.current_device() == index:
+    if _current_device() == index:
         st = fn(*args, _raw_stream(index))
     else:
         with torch.cuda.device(index):
@@ -218,7 +220,7 @@ def attend(pool: PagedCache, layer: int, batch: Batch, q: torch.Tensor, *, lists
     qs = _packed(q, None, None, pool, None, "q")
     rows, heads, d = q.shape
     if out is None:
-        out = torch.empty((rows, heads, d), dtype=q.dtype, device=pool.device)
+        out = torch.empty_like(q, memory_format=torch.contiguous_format)
         os = (heads * d, d)
     else:
         os = _packed(out, rows, heads, pool, q.dtype, "out")
