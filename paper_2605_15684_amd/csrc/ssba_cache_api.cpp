@@ -186,14 +186,15 @@ AttendPlan plan(const ssba_cache* c, const ssba_cache_batch* b, const ssba_cache
         p.splits = s;
       }
     }
-  } else if (!f32 && p.kind != ssba::kAttendRows && p.tiles == 1 && keys > 256 && items <= 256 &&
-             keys <= (items >= 128 ? 4096 : 2048)) {
+  } else if (p.kind != ssba::kAttendRows && p.tiles == 1 && keys > 256 && items <= 256 &&
+             keys <= (items >= (f32 ? 256 : 128) ? 4096 : 2048)) {
     // 8 waves of one workgroup instead of parts that a second launch joins: where such workgroups fill half the
     // chip (208 items of 2048 listed keys, D 128: 20.3 us, in 3 parts 21.5 + 4.0; 160 items of 4000: 28.7 us, in 4
     // parts 29.8 + 4.2), or an item is short (D 128, launches on the device, then calls from Python: 4 items of 1024
     // keys 7.8 and 13.6 us, in parts 8.1 and 18; 64 of 1536 11.3 and 13.6, 11.8 and 18; 4 of 2048 11.5 and 13.5, 8.8
     // and 18).  Few long ones need more CUs (4 items of 4096 keys 18.6 and 18.8 us, in parts 8.1 and 18), and long
-    // ragged ones more parts (40 sequences of up to 8000 keys: 57 us, in parts 53).  fp32 has no registers for it.
+    // ragged ones more parts (40 sequences of up to 8000 keys: 57 us, in parts 53).  fp32 (more vector work), D
+    // 128: 256 items of 4000 keys 52 us, in parts 58; 128 of 2000 17.8, 20.1; 128 ragged ones of up to 2999 21.0, 20.2.
     p.threads = 512;
   } else if (p.kind != ssba::kAttendRows) {
     // 4 waves of at least 2 steps of 32 keys each, up to about 512 workgroups: more of them fill the chip more

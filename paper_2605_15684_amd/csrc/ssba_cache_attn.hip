@@ -144,7 +144,7 @@ __device__ __forceinline__ int64_t row_at(const AttendArgs& a, const Item& it, i
 }
 
 template <typename P>
-__global__ __launch_bounds__(P::THREADS, P::R > 1 ? 2 : P::J > 1 && P::D == 128 ? 2 : 3) void k_cache_attend(AttendArgs a) {
+__global__ __launch_bounds__(P::THREADS, P::R > 1 || (P::D == 128 && (P::J > 1 || (P::F32 && P::KP == 8))) ? 2 : 3) void k_cache_attend(AttendArgs a) {
   constexpr int D = P::D, R = P::R, NQ = P::NQ, NP = P::NP, NH = P::NH, NC = P::NC, J = P::J;
   const int lane = threadIdx.x & 63, n16 = lane & 15, g = lane >> 4;
   const int mine = J > 1 ? n16 / P::COLS : 0;   // which of the J keys' share this lane's column has
@@ -770,11 +770,15 @@ hipError_t launch_d(const AttendArgs& a, const AttendPlan& p, int dtype, hipStre
       return a.group <= 8 ? launch<Shape<D, 1, 1, 1, false, true, 4, 1, false, 2>>(a, p, s)
                           : launch<Shape<D, 1, 1, 1, false, true, 4, 1, false>>(a, p, s);
     case kAttendRow:
-      if (p.threads == 512) return launch<Shape<D, 1, 1, 2, false, true, 1, 8, false>>(a, p, s);
+      if (p.threads == 512)
+        return f32 ? launch<Shape<D, 1, 3, 3, true, true, 1, 8, false>>(a, p, s)
+                   : launch<Shape<D, 1, 1, 2, false, true, 1, 8, false>>(a, p, s);
       return f32 ? launch<Shape<D, 1, 3, 3, true, true, 1, 4, false>>(a, p, s)
                  : launch<Shape<D, 1, 1, 2, false, true, 1, 4, false>>(a, p, s);
     default:
-      if (p.threads == 512 && p.tiles == 1) return launch<Shape<D, 1, 1, 2, false, false, 1, 8, false>>(a, p, s);
+      if (p.threads == 512 && p.tiles == 1)
+        return f32 ? launch<Shape<D, 1, 3, 3, true, false, 1, 8, false>>(a, p, s)
+                   : launch<Shape<D, 1, 1, 2, false, false, 1, 8, false>>(a, p, s);
       if (f32)
         return p.tiles == 1 ? launch<Shape<D, 1, 3, 3, true, false, 1, 4, false>>(a, p, s)
                             : launch<Shape<D, 1, 3, 3, true, false, 2, 2, false>>(a, p, s);

@@ -158,6 +158,9 @@ ATTENDS = [  # page, D, heads, kv heads, dtype, causal, sequences
     (16, 64, 8, 4, BF16, True, [(300, 300), (700, 150), (129, 129), (400, 5)]),   # the same, heads a multiple of 8
     (16, 64, 16, 8, BF16, True, [(2000, 40)]),                            # and keys split
     (64, 128, 5, 1, F32, True, [(1, 1), (700, 1)]),
+    (64, 128, 5, 1, F32, True, [(2900, 2), (700, 3)]),
+    (16, 64, 6, 2, F32, False, [(1500, 4), (3, 3), (0, 0)]),
+    (32, 64, 4, 2, F32, True, [(5000, 1)]),
     (16, 64, 6, 2, F32, True, [(50, 7), (7, 7), (129, 2)]),
     (32, 128, 4, 2, F32, False, [(150, 60), (64, 33)]),
 ]
@@ -348,6 +351,10 @@ LISTED = [  # page, D, heads, kv, dtype, causal, keep, sequences
     (32, 64, 48, 16, BF16, True, 5, [(300, 131), (40, 9)]),               # the same with 3 query heads to a kv head
     (16, 128, 128, 16, BF16, True, 7, [(260, 140)]),                      # 8
     (64, 64, 144, 16, BF16, False, 3, [(400, 133)]),                      # 9
+    (64, 128, 16, 4, BF16, True, 40, [(5000, 2), (130, 1)]),              # long lists: parts that are joined
+    (16, 64, 6, 2, F32, True, 150, [(3500, 1), (900, 2)]),
+    (64, 128, 6, 2, F32, True, 8, [(1000, 1), (640, 3)]),                 # 8 waves to a row
+    (32, 64, 3, 3, F32, False, 12, [(700, 2)]),
 ]
 
 
