@@ -175,18 +175,21 @@ AttendPlan plan(const ssba_cache* c, const ssba_cache_batch* b, const ssba_cache
   }
   const int64_t items = std::max<int64_t>(p.items, 1);
   if (p.tiles >= 4) {
-    // One workgroup fills a CU.  Parts of at least 256 keys; as many as make
-    // the rounds over the 256 CUs fullest, each part counted as 1/16 round for
-    // writing and joining it.
-    double best = (double)ceil_div(items, 256);
+    // One workgroup fills a CU.  Parts of at least 256 keys, as many as take the least time by these measured costs
+    // in us: each round over the 256 CUs its beginning and end and its keys, the joining launch itself and its bytes
+    // (written and read).  100 new tokens of 16 sequences, 16 heads on 4, D 64: of 600 tokens 21 us whole, 30 in two
+    // parts; of 2000 48 us whole, 41 in two.
+    const double d = c->head_dim, round = 3 + p.tiles * d / 400, key = p.tiles * (8e-4 + 6e-6 * d);
+    const double column_bytes = 2.0 * 16 * p.tiles * d * 4;
+    double best = ceil_div(items, 256) * (round + key * keys);
     for (int s = 2; s <= 256 && s * 256 <= keys && s * items <= 1024; ++s) {
-      const double cost = (double)ceil_div(items * s, 256) / s + (items * s > 256 ? 0.0625 * s : 0.0);
-      if (cost < best * 0.95) {
+      const double cost = ceil_div(items * s, 256) * (round + key * keys / s) + 3.5 + items * s * column_bytes / 3.6e6;
+      if (cost < best * 0.98) {
         best = cost;
         p.splits = s;
       }
     }
-  } else if (p.kind != ssba::kAttendRows && p.tiles == 1 && keys > 256 && items <= 256 &&
+  } else if (p.kind != ssba::kAttendRows && (p.tiles == 1 || !f32) && keys > 256 && items <= 256 &&
              keys <= (items >= (f32 ? 256 : 128) ? 4096 : 2048)) {
     // 8 waves of one workgroup instead of parts that a second launch joins: where such workgroups fill half the
     // chip (208 items of 2048 listed keys, D 128: 20.3 us, in 3 parts 21.5 + 4.0; 160 items of 4000: 28.7 us, in 4
@@ -195,6 +198,7 @@ AttendPlan plan(const ssba_cache* c, const ssba_cache_batch* b, const ssba_cache
     // and 18).  Few long ones need more CUs (4 items of 4096 keys 18.6 and 18.8 us, in parts 8.1 and 18), and long
     // ragged ones more parts (40 sequences of up to 8000 keys: 57 us, in parts 53).  fp32 (more vector work), D
     // 128: 256 items of 4000 keys 52 us, in parts 58; 128 of 2000 17.8, 20.1; 128 ragged ones of up to 2999 21.0, 20.2.
+    // 32 columns, D 128: 64 items of 600 keys 9.7 us, in parts 11.7.
     p.threads = 512;
   } else if (p.kind != ssba::kAttendRows) {
     // 4 waves of at least 2 steps of 32 keys each, up to about 512 workgroups: more of them fill the chip more

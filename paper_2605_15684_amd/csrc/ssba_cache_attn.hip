@@ -784,7 +784,9 @@ hipError_t launch_d(const AttendArgs& a, const AttendPlan& p, int dtype, hipStre
                             : launch<Shape<D, 1, 3, 3, true, false, 2, 2, false>>(a, p, s);
       switch (p.tiles) {
         case 1: return launch<Shape<D, 1, 1, 2, false, false, 1, 4, false>>(a, p, s);
-        case 2: return launch<Shape<D, 2, 1, 1, false, false, 1, 4, false>>(a, p, s);
+        case 2:
+          return p.threads == 512 ? launch<Shape<D, 2, 1, 1, false, false, 1, 8, false>>(a, p, s)
+                                  : launch<Shape<D, 2, 1, 1, false, false, 1, 4, false>>(a, p, s);
         case 4: return launch<Shape<D, 4, 1, 1, false, false, 1, 8, true>>(a, p, s);
         case 8: return launch<Shape<D, 4, 1, 1, false, false, 2, 4, true>>(a, p, s);
         default: return launch<Shape<D, 4, 1, 1, false, false, 4, 2, true>>(a, p, s);

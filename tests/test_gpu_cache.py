@@ -149,6 +149,8 @@ ATTENDS = [  # page, D, heads, kv heads, dtype, causal, sequences
     (16, 128, 6, 2, BF16, True, [(17, 1), (16, 1), (15, 1), (500, 1)]),
     (32, 64, 40, 2, BF16, True, [(100, 1), (31, 1)]),                     # 20 query heads to a kv head
     (16, 64, 6, 2, BF16, True, [(40, 9), (9, 9), (200, 3)]),              # two column tiles a wave
+    (64, 128, 16, 4, BF16, True, [(1000, 8), (300, 5), (2, 2)]),          # the same, 8 waves
+    (16, 64, 16, 4, BF16, False, [(5000, 7)]),                            # in parts
     (32, 128, 8, 2, BF16, False, [(300, 12), (12, 12), (77, 1)]),         # four
     (64, 128, 4, 2, BF16, True, [(200, 130), (70, 70), (300, 64)]),       # by columns
     (16, 64, 3, 1, BF16, False, [(333, 100), (22, 22)]),
