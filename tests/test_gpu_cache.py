@@ -616,6 +616,28 @@ def test_binding_refusals():
 
 # ---- a run of all of them -------------------------------------------------------------
 
+def test_calls_without_rows():
+    """An idle batch: no row in any packed array, nothing written."""
+    from paper_2605_15684_amd import cache
+    rng = np.random.default_rng(20)
+    pool = make_pool(rng, 1, 6, 2, 64, 16)
+    g = gpu_pool(pool)
+    batch = gpu_batch(make_batch(rng, [(20, 0), (33, 0)], 16, 6), 0)
+    k, q = torch.empty(0, 2, 64, dtype=BF16, device="cuda"), torch.empty(0, 8, 64, dtype=BF16, device="cuda")
+    cache.append(g, 0, batch, k, k)
+    lists = cache.select(g, 0, batch, q, keep=2)
+    assert lists.shape == (0, 2, 3)
+    assert cache.attend(g, 0, batch, q).shape == q.shape == cache.attend(g, 0, batch, q, lists=lists).shape
+    assert_same_pool(host_pool(g), pool)
+    # rows of no sequence, among idle ones: left as they are
+    batch = gpu_batch(make_batch(rng, [(20, 0), (33, 0)], 16, 6), 1)
+    out = torch.full((3, 8, 64), 7.0, dtype=BF16, device="cuda")
+    cache.append(g, 0, batch, out[:, :2], out[:, 2:4])
+    cache.attend(g, 0, batch, torch.ones_like(out), out=out)
+    assert (out == 7).all()
+    assert_same_pool(host_pool(g), pool)
+
+
 @pytest.mark.parametrize("dtype", [BF16, F32])
 def test_generation(dtype):
     """Prompts, steps, a fork, steps of both branches, a release, compaction, steps: two layers, dense and selected
