@@ -137,10 +137,12 @@ ssba_status ssba_cache_attend_workspace_size(const ssba_cache* c, const ssba_cac
  * counts are cut to 0 .. keep, entries that are no page of the sequence are
  * passed over, one that is named twice counts twice).  A token that sees
  * nothing gets zeros.
- *   bf16: Q as it is, codes exact in bf16, products and sums in fp32;
- * probabilities enter the value product with 16 bits where a kv head's new
- * queries of a sequence are 16 or fewer, rounded to bf16 where they are more
- * (and where lists are read by one wave a row).  fp32: Q and the probabilities
+ *   bf16: Q as it is, codes exact, products and sums in fp32.  Probabilities
+ * enter the value product with 16 bits (two bf16 terms) where G * max_new is 16
+ * or less, with lists where rows * kv_heads * ceil(G / 16) is below 2048; else
+ * with 11 (fp16, V's scale included; weights of less than 2^-22 of the largest
+ * in steps of 2^-32 of it).  So a token's result depends on the rest of its
+ * batch by such roundings, which are below that of O.  fp32: Q and the probabilities
  * as three bf16 terms each (24 bits), so products are those of fp32.  Sums are
  * formed before they are normalised: values beyond 2^90 may overflow.
  * bf16 Q and O 16-byte aligned with strides in multiples of 8, fp32 4-byte

@@ -20,6 +20,15 @@
 // formed again.  What m lags behind is harmless in fp32 and bf16.
 // bf16: V's page scale is added in the exponent (log2) instead of multiplying
 // every probability; the lane's sum is divided by it again.
+// Probabilities: two bf16 terms (16 bits) where few columns leave the matrix
+// unit idle.  Elsewhere one fp16 term (11 bits), codes being exact in fp16 too:
+// the rounding stays below that of a bf16 output.  fp16 ends at 2^16, so m is
+// taken of the weights p * vs there, 2^8 below the largest, and raised when a
+// lane's sum of four passes 2^15; weights of less than 2^-22 of the largest are
+// held in steps of 2^-32 of it.  A chunk of 4096 tokens over 16384 keys, D 128,
+// takes 473 us and is off by 0.00167 (rms, of which the output's own rounding
+// is 0.00166); with one bf16 term 466 us and 0.00236, with two 613 us.  The
+// selected chunk below takes the same time with either and 8 us more with two.
 //
 // What bounds it, and what it reaches (launch alone):
 //   few columns   the pages' bytes: 64 sequences of 8 to 16 thousand tokens, 4 kv
@@ -45,17 +54,23 @@ namespace {
 
 typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef _Float16 halfx2 __attribute__((ext_vector_type(2)));
+typedef _Float16 halfx8 __attribute__((ext_vector_type(8)));
 typedef float floatx2 __attribute__((ext_vector_type(2)));
 typedef float floatx4 __attribute__((ext_vector_type(4)));
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 typedef uint32_t u32x4a4 __attribute__((ext_vector_type(4), aligned(4)));
 
 constexpr float kMost = 1048576.f;   // a lane's sum of probabilities of a step: 2^20
+// Probabilities in fp16, V's scale included: a lane's sum of four, and how far m is below the largest when it is taken.
+constexpr float kMostHalf = 32768.f, kBelow = 8.f;
 constexpr int kNoKey = 0x40000000;   // first token of a group that is not there: behind every sequence
 
 union Frag {
   bf16x8 v;
   bf16x2 p[4];
+  halfx8 h;
+  halfx2 hp[4];
   uint32_t u[4];
 };
 
@@ -64,6 +79,13 @@ __device__ __forceinline__ bf16x2 codes_lo(uint32_t w) {
 }
 __device__ __forceinline__ bf16x2 codes_hi(uint32_t w) {
   return __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, 1.0f, true);
+}
+
+__device__ __forceinline__ halfx2 half_codes_lo(uint32_t w) {
+  return __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(w, 1.0f, false);
+}
+__device__ __forceinline__ halfx2 half_codes_hi(uint32_t w) {
+  return __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(w, 1.0f, true);
 }
 
 __device__ __forceinline__ float exp2_(float x) { return __builtin_amdgcn_exp2f(x); }
@@ -92,6 +114,7 @@ template <int D_, int R_, int NQ_, int NP_, bool F32_, bool LISTED_, int CG_, in
 struct Shape {
   static constexpr int D = D_, R = R_, NQ = NQ_, NP = NP_, CG = CG_, KP = KP_, J = J_;
   static constexpr bool F32 = F32_, LISTED = LISTED_, QLDS = QLDS_;
+  static constexpr bool HALF = !F32 && NP == 1;   // the second product in fp16
   static constexpr int THREADS = 64 * CG * KP;
   static constexpr int NH = D / 64;   // 64-channel blocks
   static constexpr int NC = D / 16;   // 16-channel tiles of O
@@ -424,7 +447,9 @@ __global__ __launch_bounds__(P::THREADS, P::R > 1 || (P::D == 128 && (P::J > 1 |
     Frag p[R][NP];
     float sum[R];
     bool high = false;
+    float top;   // of the lane's sums of four
     auto probabilities = [&]() {
+      top = 0.f;
 #pragma unroll
       for (int r = 0; r < R; ++r) {
         const float mu = m[r] == -INFINITY ? 0.f : m[r];
@@ -445,6 +470,10 @@ __global__ __launch_bounds__(P::THREADS, P::R > 1 || (P::D == 128 && (P::J > 1 |
             }
 #pragma unroll
             for (int ns = 0; ns < NP; ++ns) {   // both at once: one conversion
+              if (P::HALF) {
+                p[r][ns].hp[t * 2 + i] = __builtin_convertvector(e, halfx2);
+                continue;
+              }
               p[r][ns].p[t * 2 + i] = __builtin_convertvector(e, bf16x2);
               if (ns + 1 < NP) {
                 e[0] -= (float)p[r][ns].p[t * 2 + i][0];
@@ -454,8 +483,10 @@ __global__ __launch_bounds__(P::THREADS, P::R > 1 || (P::D == 128 && (P::J > 1 |
           }
         }
         sum[r] = P::F32 ? half[0] + half[1] : __builtin_fmaf(half[0], x.vs[0], half[1] * x.vs[1]);
-        high |= sum[r] > kMost;
+        if (P::HALF) top = fmaxf(fmaxf(top, half[0]), half[1]);
+        else high |= sum[r] > kMost;
       }
+      if (P::HALF) high = top > kMostHalf;
     };
     probabilities();
     if (edge || !settled || __builtin_amdgcn_ballot_w64(high)) {
@@ -467,10 +498,11 @@ __global__ __launch_bounds__(P::THREADS, P::R > 1 || (P::D == 128 && (P::J > 1 |
 #pragma unroll
         for (int t = 0; t < 2; ++t)
 #pragma unroll
-          for (int i = 0; i < 4; ++i) mx = fmaxf(mx, s[t][r][i] * x.ks[t]);
+          for (int i = 0; i < 4; ++i)
+            mx = fmaxf(mx, P::HALF ? __builtin_fmaf(s[t][r][i], x.ks[t], x.lv[t]) : s[t][r][i] * x.ks[t]);
         mx = fmaxf(mx, __shfl_xor(mx, 16));
         mx = fmaxf(mx, __shfl_xor(mx, 32));
-        const float to = fmaxf(m[r], mx);
+        const float to = fmaxf(m[r], P::HALF ? mx - kBelow : mx);
         const float f = to > m[r] ? exp2_(m[r] - to) : 1.f;
         m[r] = to;
         none |= to == -INFINITY && lim[r] > 0;
@@ -552,16 +584,26 @@ __global__ __launch_bounds__(P::THREADS, P::R > 1 || (P::D == 128 && (P::J > 1 |
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
           Frag v;
-          v.p[0] = codes_lo(x.v[2 * j][hh][e]);
-          v.p[1] = codes_hi(x.v[2 * j][hh][e]);
-          v.p[2] = codes_lo(x.v[2 * j + 1][hh][e]);
-          v.p[3] = codes_hi(x.v[2 * j + 1][hh][e]);
+          if (P::HALF) {
+            v.hp[0] = half_codes_lo(x.v[2 * j][hh][e]);
+            v.hp[1] = half_codes_hi(x.v[2 * j][hh][e]);
+            v.hp[2] = half_codes_lo(x.v[2 * j + 1][hh][e]);
+            v.hp[3] = half_codes_hi(x.v[2 * j + 1][hh][e]);
+          } else {
+            v.p[0] = codes_lo(x.v[2 * j][hh][e]);
+            v.p[1] = codes_hi(x.v[2 * j][hh][e]);
+            v.p[2] = codes_lo(x.v[2 * j + 1][hh][e]);
+            v.p[3] = codes_hi(x.v[2 * j + 1][hh][e]);
+          }
 #pragma unroll
           for (int ns = NP - 1; ns >= 0; --ns)
 #pragma unroll
-            for (int r = 0; r < R; ++r)
-              o[r][hh * 4 + e] =
-                  __builtin_amdgcn_mfma_f32_16x16x32_bf16(v.v, J > 1 ? pj[ns].v : p[r][ns].v, o[r][hh * 4 + e], 0, 0, 0);
+            for (int r = 0; r < R; ++r) {
+              const Frag& w = J > 1 ? pj[ns] : p[r][ns];
+              o[r][hh * 4 + e] = P::HALF
+                                     ? __builtin_amdgcn_mfma_f32_16x16x32_f16(v.h, w.h, o[r][hh * 4 + e], 0, 0, 0)
+                                     : __builtin_amdgcn_mfma_f32_16x16x32_bf16(v.v, w.v, o[r][hh * 4 + e], 0, 0, 0);
+            }
         }
     }
   };
