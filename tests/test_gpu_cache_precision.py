@@ -16,11 +16,11 @@ import torch
 
 from oracle import cache_oracle as C
 
-from _cache import gpu_batch, gpu_pool, make_batch, make_pool
+from _cache import gpu_batch, gpu_pool, make_batch, make_pool, rounded
 
 pytestmark = pytest.mark.gpu
 
-BF16 = torch.bfloat16
+BF16, F32 = torch.bfloat16, torch.float32
 
 FORMS = [  # page, D, heads, kv heads, keep (0: the whole sequence), bits of a bf16 call's probabilities, sequences
     (16, 64, 4, 2, 0, 16, [(250, 1), (90, 1)]),               # up to 16 columns: 4 waves
@@ -99,3 +99,25 @@ def test_attend_bits_of_the_probabilities(page, d, heads, kv, keep, bits, seqs):
     ref = C.attend(pool, 0, batch, q.double().numpy(), page, lists, True, scale)
     length = keep * page if keep else max(h for h, _ in seqs)
     check(got, ref, length, d, BF16, bits, 1.0)
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("page,d,heads,kv,keep,bits,seqs", FORMS)
+def test_attend_scores_that_outgrow_the_maximum(page, d, heads, kv, keep, bits, seqs, dtype):
+    """Scores that grow along the sequence by hundreds, up and down between: the maximum is raised again and again, the
+    last pages weigh the most; V's scales differ by up to 2^18 from page to page."""
+    rng = np.random.default_rng(2)
+    pages, rows = sum(-(-h // page) for h, _ in seqs), sum(n for _, n in seqs)
+    pool = make_pool(rng, 1, pages, kv, d, page)
+    batch = make_batch(rng, seqs, page, pages)
+    for s, (held, _) in enumerate(seqs):
+        ids = batch[0][s][: -(-held // page)]
+        grow = np.linspace(-10, -4, len(ids)) + rng.uniform(-1, 1, len(ids))
+        pool["scale"][0, ids, :, 0] = (2.0 ** grow.round()).astype(np.float32)[:, None]
+    pool["scale"][..., 1] = (2.0 ** rng.integers(-12, 7, pool["scale"].shape[:3])).astype(np.float32)
+    q, q64 = rounded(rng, (rows, heads, d), dtype, 2.0)
+    lists = some_lists(rng, seqs, kv, keep, page) if keep else None
+    got = run(pool, batch, q, lists, seqs)
+    ref = C.attend(pool, 0, batch, q64, page, lists)
+    length = keep * page if keep else max(h for h, _ in seqs)
+    check(got, ref, length, d, dtype, bits, 64.0)
