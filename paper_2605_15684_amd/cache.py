@@ -153,6 +153,9 @@ def _packed(t, rows, heads, pool: PagedCache, dtype, what: str):
     st, sh, sc = t.stride()
     if sc != 1 and n * h:
         raise ValueError(f"{what}: channel stride must be 1")
+    # Broadcast tensors among them: strides of (0, 0) mean a contiguous array to the library.
+    if (n > 1 and h and st < d) or (h > 1 and n and sh < d):
+        raise ValueError(f"{what}: rows and heads must not overlap")
     # A dimension of one has no stride that matters; torch may report any.
     if h < 2:
         sh = d

@@ -1,0 +1,49 @@
+"""What the cache's binding refuses before it calls the library (no GPU: tensors that say they are on one, and nothing
+is launched)."""
+from types import SimpleNamespace
+
+import pytest
+import torch
+
+from paper_2605_15684_amd import cache
+
+POOL = SimpleNamespace(index=0, head_dim=64, kv_heads=4)
+
+
+class OnGpu(torch.Tensor):
+    """A host tensor that says it is on GPU 0."""
+    is_cuda = True
+
+    def get_device(self):
+        return 0
+
+
+def gpu(t):
+    return t.as_subclass(OnGpu)
+
+
+def packed(t, heads=None):
+    return cache._packed(gpu(t), None, heads, POOL, None, "x")
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+def test_rows_that_share_memory_are_refused(dtype):
+    """Strides (0, 0) mean a contiguous array to the library: a broadcast tensor must not get there with them."""
+    x = torch.zeros(6, 4, 64, dtype=dtype)
+    one = x[:1, :1]
+    for bad in (one.expand(1, 4, 64), one.expand(6, 4, 64), one.expand(6, 1, 64), x[:, :1].expand(6, 4, 64),
+                x[:1].expand(6, 4, 64), x.view(-1).as_strided((6, 4, 64), (32, 64, 1)),
+                x.view(-1).as_strided((6, 4, 64), (256, 32, 1))):
+        with pytest.raises(ValueError, match="must not overlap"):
+            packed(bad)
+
+
+def test_strides_of_what_is_accepted():
+    x = torch.zeros(6, 4, 64)
+    assert packed(x) == (256, 64)
+    assert packed(x[:1]) == (256, 64)
+    assert packed(x[:, :1]) == (256, 64)
+    assert packed(x[:1, :1]) == (64, 64)
+    assert packed(torch.zeros(4, 6, 64).transpose(0, 1)) == (64, 384)          # heads first
+    assert packed(torch.zeros(6, 12, 64)[:, 4:8]) == (768, 64)                  # a slice of a projection
+    assert packed(x[:0]) == (256, 64) and packed(x[:1].expand(0, 4, 64))[1] == 64
