@@ -23,8 +23,8 @@
  *            V: 16 D T + 1024 (c/64) + 256 (r/4) + 16 (c%16) + 4 (c%64 / 16) + r%4
  *          of its page (16-byte loads of a wave are 1024 consecutive bytes).
  *   scale  fp32 [layers][pages][kv_heads][2], 8-byte aligned: a key is
- *          scale[0] * code, a value scale[1] * code; positive (append writes
- *          powers of two).
+ *          scale[0] * code, a value scale[1] * code; positive, at most 2^120
+ *          (append writes powers of two).
  *   kmean  bf16 [layers][pages][kv_heads][D], 16-byte aligned: the mean of the
  *          keys of a complete page (select reads it; attend does not).
  * Nothing has to be initialised: slots behind a sequence's end are never used,
@@ -98,11 +98,12 @@ typedef struct ssba_cache_query {
  *   A page's scale is 2^e with the smallest e >= -64 that holds every finite
  * value put into it since its first token: |x| <= 448 * 2^e.  A value is held
  * as code = e4m3(x * 2^-e), to nearest, ties to even; +-inf as +-448, NaN as
- * NaN.  When a later token raises e from e0, the page's older codes are
- * restated as e4m3(code * 2^(e0 - e)).  When the last token of a page comes,
- * kmean = bf16(2^e * sum(codes) / page).  The result does not depend on
- * atomics or on the order of workgroups.  Pages that several rows share
- * (ssba_pages_fork) must be complete; two sequences of a call must not append
+ * NaN.  In a page that holds older tokens 2^e also reaches the scale s that it
+ * has, which may be any positive one; where s is not 2^e, the older codes are
+ * restated as e4m3(code * (s * 2^-e)), the product in fp32.  When the last
+ * token of a page comes, kmean = bf16(2^e * sum(codes) / page).  The result does
+ * not depend on atomics or on the order of workgroups.  Pages that several rows
+ * share (ssba_pages_fork) must be complete; two sequences of a call must not append
  * to one page. */
 ssba_status ssba_cache_append(const ssba_cache* c, int32_t layer, const ssba_cache_batch* b, int32_t dtype,
                               const void* k, const void* v, int64_t stride_t, int64_t stride_h, void* hip_stream);

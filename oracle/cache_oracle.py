@@ -52,6 +52,12 @@ def exponent(amax):
     return e
 
 
+def reach(s):
+    """Smallest e >= MIN_EXP with s <= 2^e."""
+    m, x = np.frexp(s)                                 # s = m 2^x, m in [1/2, 1)
+    return max(int(x) - (m == 0.5), MIN_EXP)
+
+
 def to_bf16(x):
     """float64 -> nearest bf16 (ties to even), as float32; the value must not need double rounding."""
     b = np.asarray(x, dtype=np.float32).view(np.uint32).astype(np.uint64)
@@ -115,11 +121,12 @@ def append(pool, layer, batch, k, v, page):
                     e = exponent(finite.max() if finite.size else 0.0)
                     codes = pool["kv"[which]][layer, phys, h]
                     if lp * page < start:
-                        e0 = int(np.log2(pool["scale"][layer, phys, h, which]))
-                        if e > e0:
+                        was = float(pool["scale"][layer, phys, h, which])
+                        e = max(e, min(reach(was), 120))
+                        f = np.float32(was * 2.0 ** -e)
+                        if f != 1:
                             at = order[which][:lo - lp * page]
-                            codes[at] = e4m3(E4M3[codes[at]] * 2.0 ** (e0 - e))
-                        e = max(e, e0)
+                            codes[at] = e4m3(E4M3[codes[at]].astype(np.float32) * f)
                     codes[order[which][lo - lp * page:hi - lp * page]] = e4m3(new * 2.0 ** -e)
                     pool["scale"][layer, phys, h, which] = 2.0 ** e
                     if which == 0 and held >= (lp + 1) * page:

@@ -170,18 +170,19 @@ __global__ __launch_bounds__(256) void k_cache_append(AppendArgs a) {
 
   int e[2];
   float inv[2], restate[2];
-  bool grows[2];
+  bool grows[2];   // older codes change: the scale is not what it was
 #pragma unroll
   for (int kv = 0; kv < 2; ++kv) {
     e[kv] = exponent_of(s_top[kv]);
-    int e0 = e[kv];
+    restate[kv] = 1.f;
     if (has_old) {
-      e0 = min(max((int)((was[kv] >> 23) & 0xff) - 127, kMinExp), kMaxExp);
-      e[kv] = max(e[kv], e0);
+      // The smallest power of two that reaches the old scale, which need not be one itself.
+      const int up = (was[kv] & 0x7fffffu) ? 1 : 0;
+      e[kv] = max(e[kv], min(max((int)((was[kv] >> 23) & 0xff) - 127 + up, kMinExp), kMaxExp));
+      restate[kv] = __uint_as_float(was[kv]) * pow2(-e[kv]);
     }
-    grows[kv] = e[kv] > e0;
+    grows[kv] = restate[kv] != 1.f;
     inv[kv] = pow2(-e[kv]);
-    restate[kv] = pow2(e0 - e[kv]);
     if (threadIdx.x == 0) scale[kv] = pow2(e[kv]);
     if (infinite[kv]) {   // infinities take the largest code: scaled here, once and for all
 #pragma unroll

@@ -33,3 +33,28 @@ def test_broadcast_tensors_are_refused(tokens):
                  lambda: cache.select(pool, 0, batch, qs, keep=2)):
         with pytest.raises(ValueError):
             call()
+
+
+@pytest.mark.parametrize("page,d,dtype", [(16, 64, BF16), (64, 128, BF16), (32, 128, F32), (64, 64, F32)])
+def test_append_to_pages_with_other_scales(page, d, dtype):
+    """Pages that came with scales of any positive value: older tokens keep what they hold, page by page as the oracle
+    has it; some pages are completed, some scales reach what is new, some do not."""
+    from paper_2605_15684_amd import cache
+    from oracle import cache_oracle as C
+    from _cache import assert_same_pool, gpu_batch, gpu_pool, host_pool, make_batch, make_pool, rounded
+    rng = np.random.default_rng(30)
+    kv, scales = 2, [0.75, 3.1, 2.0 ** -70, 1e-40, 2.0 ** -64, 0.5, 1.0000001, 2.0 ** 120, 1.5 * 2.0 ** 100, 1e-3]
+    seqs = [(page - 2, 3), (page, 5), (page + 4, 9)] * 10
+    need = [-(-h // page) for h, _ in seqs]
+    pool = make_pool(rng, 1, sum(need) + 2, kv, d, page)
+    table, lens, cu = make_batch(rng, seqs, page, sum(need) + 2)
+    for s in range(len(seqs)):
+        for which in (0, 1):
+            pool["scale"][0, table[s, :need[s]], :, which] = scales[(s // 3 + 3 * which) % len(scales)]
+    rows = int(cu[-1])
+    size = torch.from_numpy(10.0 ** rng.uniform(-6, 3, (rows, 1, 1)))
+    (k, k64), (v, v64) = (rounded(rng, (rows, kv, d), dtype, size) for _ in range(2))
+    g = gpu_pool(pool)
+    cache.append(g, 0, gpu_batch((table, lens, cu), 9), k.cuda(), v.cuda())
+    C.append(pool, 0, (table, lens, cu), k64, v64, page)
+    assert_same_pool(host_pool(g), pool)
