@@ -125,6 +125,12 @@ int64_t long_of(const ssba_cache* c, const ssba_cache_batch* b) {
 
 int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
 
+// Workgroups that score, of one share of the pages each; in units of 256
+// threads (512 in the tile form).
+int64_t score_groups(const ssba_cache* c, const ssba_cache_batch* b, bool tile) {
+  return tile ? (int64_t)b->seqs * c->kv_heads * ceil_div(b->max_new, 16) * 2 : (int64_t)b->rows * c->kv_heads;
+}
+
 // Pages to score fit a workgroup's LDS, or go through the scratch; 16 tokens
 // share the pooled keys where sequences bring enough of them: with 8 of 16
 // rows of a tile in use the matrix form needs half the loads.
@@ -137,9 +143,11 @@ ssba::SelectPlan plan_select(const ssba_cache* c, const ssba_cache_batch* b, con
     p.kind = tile ? ssba::kSelectTile : ssba::kSelectRow;
   } else {
     p.kind = tile ? ssba::kSelectTileLong : ssba::kSelectRowLong;
-    // A workgroup takes 64 pages at a time; 8 times as many for a tile, whose queries take longer to load.
+    // A workgroup takes 64 pages at a time; 8 times as many for a tile, whose queries take longer to load.  Shares are
+    // no more than a launch can have.
+    const int64_t most = ssba::kMaxGroups256 / std::max<int64_t>(1, score_groups(c, b, tile));
     p.chunks = (int)std::min<int64_t>(ceil_div(ceil_div(long_of(c, b), c->page), ssba::kSelectPages * (tile ? 8 : 1)),
-                                      65535);
+                                      std::max<int64_t>(1, std::min<int64_t>(most, 65535)));
   }
   return p;
 }
@@ -288,8 +296,8 @@ ssba_status ssba_cache_select(const ssba_cache* c, int32_t layer, const ssba_cac
   a.tiles = (int)ceil_div(b->max_new, 16);
   const ssba::SelectPlan p = plan_select(c, b, q);
   // 1024 threads at most rank a row, 512 score one where its keys stay in the LDS.
-  if (too_many((int64_t)b->rows * c->kv_heads * std::max(p.chunks, 4)) ||
-      too_many((int64_t)b->seqs * c->kv_heads * a.tiles * p.chunks * 2))
+  const bool tile = p.kind == ssba::kSelectTile || p.kind == ssba::kSelectTileLong;
+  if (too_many((int64_t)b->rows * c->kv_heads * 4) || too_many(score_groups(c, b, tile) * p.chunks))
     return SSBA_ERR_UNSUPPORTED;
   return ssba::launch_cache_select(a, p, q->dtype, static_cast<hipStream_t>(stream)) == hipSuccess ? SSBA_OK
                                                                                                    : SSBA_ERR_HIP;
