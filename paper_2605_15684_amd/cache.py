@@ -214,11 +214,22 @@ def select(pool: PagedCache, layer: int, batch: Batch, q: torch.Tensor, *, keep:
     return lists
 
 
+def _softmax_scale(scale: Optional[float]) -> float:
+    """As the library takes it: fp32, where 0 stands for 1 / sqrt(D)."""
+    if scale is None:
+        return 0.0
+    x = ctypes.c_float(scale).value
+    if x <= 0.0:
+        raise ValueError("scale must be positive in fp32 (None: 1 / sqrt(D))")
+    return x
+
+
 def attend(pool: PagedCache, layer: int, batch: Batch, q: torch.Tensor, *, lists: Optional[torch.Tensor] = None,
            causal: bool = True, scale: Optional[float] = None, out: Optional[torch.Tensor] = None,
            scratch: Optional[torch.Tensor] = None) -> torch.Tensor:
     """Attention of the new tokens' queries [tokens, heads, D] over what their sequences hold, or over the pages
-    that `lists` (of select) names.  Rows of no sequence are left as they are in `out`."""
+    that `lists` (of select) names.  scale: positive; None: 1 / sqrt(D).  Rows of no sequence are left as they are
+    in `out`."""
     _same_device(pool, batch)
     qs = _packed(q, None, None, pool, None, "q")
     rows, heads, d = q.shape
@@ -236,7 +247,7 @@ def attend(pool: PagedCache, layer: int, batch: Batch, q: torch.Tensor, *, lists
         lp, lb = lists.data_ptr(), lists.numel() * 4
     b = batch.desc(rows)
     desc = _lib.CacheQuery(heads, _DTYPES[q.dtype], 1 if causal else 0, keep, 0, 0,
-                           0.0 if scale is None else float(scale), *qs, *os)
+                           _softmax_scale(scale), *qs, *os)
     size = ctypes.c_size_t(0)
     _lib.check(_L.ssba_cache_attend_workspace_size(pool.desc, b, desc, 0 if lists is None else 1, size),
                "ssba_cache_attend_workspace_size")

@@ -47,3 +47,19 @@ def test_strides_of_what_is_accepted():
     assert packed(torch.zeros(4, 6, 64).transpose(0, 1)) == (64, 384)          # heads first
     assert packed(torch.zeros(6, 12, 64)[:, 4:8]) == (768, 64)                  # a slice of a projection
     assert packed(x[:0]) == (256, 64) and packed(x[:1].expand(0, 4, 64))[1] == 64
+
+
+def calls():
+    """A pool and a batch of one token that say they are on GPU 0, and its queries."""
+    codes = gpu(torch.zeros(2, 4, 4, 16 * 64, dtype=torch.uint8).view(torch.float8_e4m3fn))
+    pool = cache.PagedCache(codes, codes, gpu(torch.ones(2, 4, 4, 2)), gpu(torch.zeros(2, 4, 4, 64, dtype=torch.bfloat16)))
+    i32 = lambda *x: gpu(torch.tensor(x, dtype=torch.int32))
+    return pool, cache.Batch(i32(0, 1).view(1, 2), i32(1), i32(0, 1), 1), gpu(torch.zeros(1, 8, 64))
+
+
+@pytest.mark.parametrize("scale", [0.0, -0.0, -0.125, 1e-60, float("-inf")])
+def test_scales_that_the_library_takes_for_none(scale):
+    """Its default, 1 / sqrt(D), stands for every scale <= 0 there: here only None does."""
+    pool, batch, q = calls()
+    with pytest.raises(ValueError, match="scale"):
+        cache.attend(pool, 0, batch, q, scale=scale)
