@@ -86,7 +86,7 @@ typedef struct ssba_cache_query {
   int32_t causal;            /* 1: a token sees itself and what is before it; 0: the whole sequence */
   int32_t keep;              /* pages per token and kv head, 1 .. 2^24 (0 without lists) */
   int32_t first, last;       /* select: leading and trailing pages always kept; first >= 0, last >= 1, first + last <= keep */
-  float softmax_scale;       /* <= 0 selects 1 / sqrt(head_dim)                  */
+  float softmax_scale;       /* <= 0 selects 1 / sqrt(head_dim); at most 2^127   */
   int64_t q_stride_t, q_stride_h; /* element strides of Q [rows][heads][D]; both 0 = contiguous */
   int64_t o_stride_t, o_stride_h; /* the same of O                               */
 } ssba_cache_query;

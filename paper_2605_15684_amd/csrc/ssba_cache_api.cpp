@@ -26,6 +26,7 @@ int ilog2(int v) {
 
 constexpr int kMaxPages = 1 << 24;
 constexpr int64_t kMaxTokens = (int64_t)1 << 30;
+constexpr float kLog2e = 1.4426950408889634f;
 
 ssba_status check_shape(const ssba_cache* c) {
   if (!c) return SSBA_ERR_ARG;
@@ -77,7 +78,7 @@ ssba_status check_query(const ssba_cache* c, const ssba_cache_batch* b, const ss
   if (q->heads > 65536) return SSBA_ERR_UNSUPPORTED;
   if (q->dtype != SSBA_DT_BF16 && q->dtype != SSBA_DT_F32) return SSBA_ERR_ARG;
   if (q->causal != 0 && q->causal != 1) return SSBA_ERR_ARG;
-  if (!std::isfinite(q->softmax_scale)) return SSBA_ERR_ARG;
+  if (!std::isfinite(q->softmax_scale * kLog2e)) return SSBA_ERR_ARG;
   if ((int64_t)(q->heads / c->kv_heads) * b->max_new > kMaxTokens) return SSBA_ERR_UNSUPPORTED;
   if (q->keep < 0) return SSBA_ERR_ARG;
   if (q->keep > kMaxPages) return SSBA_ERR_UNSUPPORTED;
@@ -347,7 +348,7 @@ ssba_status ssba_cache_attend(const ssba_cache* c, int32_t layer, const ssba_cac
   a.part = static_cast<float*>(scratch);
   a.part_ml = need ? a.part + part_columns(p) * c->head_dim : nullptr;
   const float scale = q->softmax_scale > 0.f ? q->softmax_scale : 1.0f / std::sqrt((float)c->head_dim);
-  a.scale_log2 = scale * 1.4426950408889634f;
+  a.scale_log2 = scale * kLog2e;
   a.group = q->heads / c->kv_heads;
   a.causal = q->causal;
   a.keep = q->keep;
