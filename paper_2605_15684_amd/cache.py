@@ -66,6 +66,13 @@ def _check(t, shape, dtype, index, what: str) -> None:
                      (f" of shape {tuple(shape)}" if shape is not None else ""))
 
 
+def _int32(what: str, *numbers) -> None:
+    """The library's numbers are int32, and ctypes would cut larger ones."""
+    for x in numbers:
+        if not -0x80000000 <= x < 0x80000000:
+            raise ValueError(f"{what}: outside int32")
+
+
 def _gpu_of(t, dims: int, what: str) -> int:
     """The GPU of a tensor of `dims` dimensions."""
     if not isinstance(t, torch.Tensor) or not t.is_cuda or t.dim() != dims:
@@ -110,12 +117,13 @@ class Batch:
                  max_len: Optional[int] = None):
         index = _gpu_of(table, 2, "table")
         seqs, max_pages = table.shape
+        max_new, max_len = int(max_new), int(max_len or 0)
+        _int32("table, max_new or max_len", seqs, max_pages, max_new, max_len)
         _check(table, None, torch.int32, index, "table")
         _check(lens, (seqs,), torch.int32, index, "lens")
         _check(cu, (seqs + 1,), torch.int32, index, "cu")
         self.table, self.lens, self.cu, self.index = table, lens, cu, index
-        self._desc = (seqs, max_pages, int(max_new), int(max_len or 0), table.data_ptr(), lens.data_ptr(),
-                      cu.data_ptr())
+        self._desc = (seqs, max_pages, max_new, max_len, table.data_ptr(), lens.data_ptr(), cu.data_ptr())
 
     def desc(self, rows: int) -> _lib.CacheBatch:
         seqs, max_pages, new, length, table, lens, cu = self._desc
@@ -174,6 +182,7 @@ def append(pool: PagedCache, layer: int, batch: Batch, k: torch.Tensor, v: torch
     _same_device(pool, batch)
     strides = _packed(k, None, pool.kv_heads, pool, None, "k")
     rows = k.shape[0]
+    _int32("layer", layer)
     if _packed(v, rows, pool.kv_heads, pool, k.dtype, "v") != strides:
         raise ValueError("k and v must share their strides")
     _call(pool, _L.ssba_cache_append, "ssba_cache_append", pool.desc, layer, batch.desc(rows), _DTYPES[k.dtype],
@@ -200,6 +209,7 @@ def select(pool: PagedCache, layer: int, batch: Batch, q: torch.Tensor, *, keep:
     _same_device(pool, batch)
     qs = _packed(q, None, None, pool, None, "q")
     rows, heads, _ = q.shape
+    _int32("layer, keep, first or last", layer, keep, first, last)
     b = batch.desc(rows)
     desc = _lib.CacheQuery(heads, _DTYPES[q.dtype], 1 if causal else 0, keep, first, last, 0.0, *qs, 0, 0)
     size = ctypes.c_size_t(0)
@@ -233,6 +243,7 @@ def attend(pool: PagedCache, layer: int, batch: Batch, q: torch.Tensor, *, lists
     _same_device(pool, batch)
     qs = _packed(q, None, None, pool, None, "q")
     rows, heads, d = q.shape
+    _int32("layer", layer)
     if out is None:
         out = torch.empty_like(q, memory_format=torch.contiguous_format)
         os = (heads * d, d)
@@ -260,6 +271,7 @@ def attend(pool: PagedCache, layer: int, batch: Batch, q: torch.Tensor, *, lists
 def _rows(pool: PagedCache, table, lens, refs) -> _lib.CachePages:
     _gpu_of(table, 2, "table")
     _check(table, None, torch.int32, pool.index, "table")
+    _int32("table", *table.shape)
     _check(lens, (table.shape[0],), torch.int32, pool.index, "lens")
     _check(refs, (pool.pages,), torch.int32, pool.index, "refs")
     return _lib.CachePages(table.shape[0], table.shape[1], table.data_ptr(), lens.data_ptr(), refs.data_ptr())
@@ -283,6 +295,7 @@ def _numbers(pool: PagedCache, t, n, what: str) -> int:
     _check(t, None, torch.int32, pool.index, what)
     if t.dim() != 1 or (n is not None and t.shape[0] != n):
         raise ValueError(f"{what}: expected a vector" + (f" of {n}" if n is not None else ""))
+    _int32(what, t.shape[0])
     return t.shape[0]
 
 
@@ -326,6 +339,7 @@ def compact(pool: PagedCache, table, refs, table_out=None, refs_out=None, info=N
     # lens takes no part: its place is filled by another array
     _gpu_of(table, 2, "table")
     _check(table, None, torch.int32, pool.index, "table")
+    _int32("table", *table.shape)
     _check(refs, (pool.pages,), torch.int32, pool.index, "refs")
     desc = _lib.CachePages(table.shape[0], table.shape[1], table.data_ptr(), refs.data_ptr(), refs.data_ptr())
     table_out = torch.empty_like(table) if table_out is None else table_out

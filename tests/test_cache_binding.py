@@ -63,3 +63,36 @@ def test_scales_that_the_library_takes_for_none(scale):
     pool, batch, q = calls()
     with pytest.raises(ValueError, match="scale"):
         cache.attend(pool, 0, batch, q, scale=scale)
+
+
+@pytest.mark.parametrize("big", [1 << 32, (1 << 32) + 1, -(1 << 32), 1 << 31, -(1 << 31) - 1])
+def test_numbers_that_int32_does_not_hold(big):
+    """The library's numbers are int32; ctypes cuts larger ones to their low bits without a word (2^32 is layer 0)."""
+    pool, batch, q = calls()
+    k = q[:, :4]
+    table, lens, cu = batch.table, batch.lens, batch.cu
+    for call in (lambda: cache.append(pool, big, batch, k, k), lambda: cache.attend(pool, big, batch, q),
+                 lambda: cache.select(pool, big, batch, q, keep=2), lambda: cache.select(pool, 0, batch, q, keep=2, first=big),
+                 lambda: cache.select(pool, 0, batch, q, keep=2, first=0, last=big),
+                 lambda: cache.Batch(table, lens, cu, big), lambda: cache.Batch(table, lens, cu, 1, big)):
+        with pytest.raises(ValueError, match="int32"):
+            call()
+
+
+def wide(rows, columns):
+    """A tensor of a shape that no memory has to hold."""
+    return gpu(torch.zeros(1, dtype=torch.int32).expand(rows, columns))
+
+
+def test_shapes_that_int32_does_not_hold(monkeypatch):
+    pool, batch, q = calls()
+    refs = gpu(torch.zeros(4, dtype=torch.int32))
+    monkeypatch.setattr(OnGpu, "is_contiguous", lambda self: True, raising=False)
+    table = wide(1, (1 << 32) + 1)
+    numbers = wide(1, (1 << 32) + 1)[0]
+    for call in (lambda: cache.Batch(table, batch.lens, batch.cu, 1), lambda: cache.reserve(pool, table, batch.lens, refs),
+                 lambda: cache.compact(pool, table, refs),
+                 lambda: cache.release(pool, batch.table, batch.lens, refs, numbers),
+                 lambda: cache.copy_pages(pool, numbers, numbers)):
+        with pytest.raises(ValueError, match="int32"):
+            call()
