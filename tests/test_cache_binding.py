@@ -1,13 +1,24 @@
 """What the cache's binding refuses before it calls the library (no GPU: tensors that say they are on one, and nothing
 is launched)."""
+import importlib
+import os
 from types import SimpleNamespace
 
 import pytest
 import torch
 
-from paper_2605_15684_amd import cache
+from paper_2605_15684_amd import _lib
 
 POOL = SimpleNamespace(index=0, head_dim=64, kv_heads=4)
+
+
+@pytest.fixture(scope="module", autouse=True)
+def built():
+    global cache
+    if not os.path.exists(_lib.LIB_PATH):
+        from paper_2605_15684_amd import build
+        build.build()
+    cache = importlib.import_module("paper_2605_15684_amd.cache")
 
 
 class OnGpu(torch.Tensor):
