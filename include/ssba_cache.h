@@ -37,8 +37,8 @@
  *   cu     [seqs + 1]: rows cu[s] .. cu[s+1]-1 of the packed arrays (K, V, Q,
  *          O) are the new tokens of sequence s, the last cu[s+1]-cu[s] that it
  *          holds; 0 rows: an idle sequence.  cu must not decrease.
- * Rows of the packed arrays that belong to no sequence are neither read nor
- * written.  The values are read on the device, so a captured call replays with
+ * Rows of the packed arrays that belong to no sequence are not written, and no
+ * result depends on what they hold (select may read them).  The values are read on the device, so a captured call replays with
  * new lengths; whatever they are, no access leaves the arrays (lengths are cut
  * to max_pages * page, rows to `rows`; a sequence that holds fewer tokens than
  * it has new rows is not appended, its earliest rows see nothing).

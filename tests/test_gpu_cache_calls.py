@@ -58,3 +58,37 @@ def test_append_to_pages_with_other_scales(page, d, dtype):
     cache.append(g, 0, gpu_batch((table, lens, cu), 9), k.cuda(), v.cuda())
     C.append(pool, 0, (table, lens, cu), k64, v64, page)
     assert_same_pool(host_pool(g), pool)
+
+
+@pytest.mark.parametrize("new", [1, 9])
+def test_rows_of_no_sequence_do_not_matter(new):
+    """Rows in front of, behind and between sequences: whatever they hold, results are the same, and they stay."""
+    from paper_2605_15684_amd import cache
+    from _cache import assert_same_pool, gpu_batch, gpu_pool, host_pool, make_batch, make_pool, rounded
+    rng = np.random.default_rng(31)
+    page, d, heads, kv = 16, 64, 4, 2
+    pool = make_pool(rng, 1, 22, kv, d, page)
+    table, lens, cu = make_batch(rng, [(140, new), (90, 0), (100, new)], page, 22)
+    cu += 3
+    rows = int(cu[-1]) + 2
+    inside = torch.zeros(rows, dtype=torch.bool)
+    inside[3:int(cu[-1])] = True
+    results = []
+    for fill in (0.0, float("nan"), float("inf")):
+        rng = np.random.default_rng(32)
+        (k, _), (v, _), (q, _) = (rounded(rng, (rows, n, d), BF16) for n in (kv, kv, heads))
+        for x in (k, v, q):
+            x[~inside] = fill
+        g, b = gpu_pool(pool), gpu_batch((table, lens, cu), new)
+        lists = torch.full((rows, kv, 5), -7, dtype=torch.int32, device="cuda")
+        out, listed = (torch.full((rows, heads, d), 5.0, dtype=BF16, device="cuda") for _ in range(2))
+        cache.append(g, 0, b, k.cuda(), v.cuda())
+        cache.select(g, 0, b, q.cuda(), keep=4, lists=lists)
+        cache.attend(g, 0, b, q.cuda(), out=out)
+        cache.attend(g, 0, b, q.cuda(), lists=lists, out=listed)
+        assert (lists.cpu()[~inside] == -7).all()
+        assert (out.cpu()[~inside] == 5).all() and (listed.cpu()[~inside] == 5).all()
+        results.append((lists, out, listed, host_pool(g)))
+    for other in results[1:]:
+        assert all(torch.equal(x, y) for x, y in zip(other[:3], results[0][:3]))
+        assert_same_pool(other[3], results[0][3])
