@@ -121,3 +121,23 @@ def test_attend_scores_that_outgrow_the_maximum(page, d, heads, kv, keep, bits, 
     ref = C.attend(pool, 0, batch, q64, page, lists)
     length = keep * page if keep else max(h for h, _ in seqs)
     check(got, ref, length, d, dtype, bits, 64.0)
+
+
+@pytest.mark.parametrize("page,d,heads,kv,keep,bits,seqs", FORMS)
+def test_attend_queries_that_are_nan(page, d, heads, kv, keep, bits, seqs):
+    """A query with a NaN makes its own output NaN and leaves all others as precise as they are."""
+    rng = np.random.default_rng(3)
+    pages, rows = sum(-(-h // page) for h, _ in seqs), sum(n for _, n in seqs)
+    pool = make_pool(rng, 1, pages, kv, d, page)
+    batch = make_batch(rng, seqs, page, pages)
+    q, q64 = rounded(rng, (rows, heads, d), BF16, 0.3)
+    lists = some_lists(rng, seqs, kv, keep, page) if keep else None
+    o, w, x = C.attend(pool, 0, batch, q64, page, lists)
+    bad = rng.random((rows, heads)) < 0.2
+    bad[0, 0] = True
+    bad[-1, -1] = False
+    q[torch.from_numpy(bad)] = torch.where(torch.arange(d) == 5, float("nan"), q[torch.from_numpy(bad)].float()).to(BF16)
+    got = run(pool, batch, q, lists, seqs).float().cpu().numpy()
+    assert np.isnan(got[bad]).all()
+    length = keep * page if keep else max(h for h, _ in seqs)
+    check(torch.from_numpy(np.where(bad[..., None], o, got)), (o, w, x), length, d, BF16, bits, 2.0 ** -6)
