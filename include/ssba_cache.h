@@ -38,10 +38,12 @@
  *          O) are the new tokens of sequence s, the last cu[s+1]-cu[s] that it
  *          holds; 0 rows: an idle sequence.  cu must not decrease.
  * Rows of the packed arrays that belong to no sequence are not written, and no
- * result depends on what they hold (select may read them).  The values are read on the device, so a captured call replays with
- * new lengths; whatever they are, no access leaves the arrays (lengths are cut
- * to max_pages * page, rows to `rows`; a sequence that holds fewer tokens than
- * it has new rows is not appended, its earliest rows see nothing).
+ * result depends on what they hold (select may read them).  The values are read
+ * on the device, so a captured call replays with new lengths; whatever they are,
+ * no access leaves the arrays.  Tokens of a sequence past max_pages * page are
+ * neither written nor seen, rows past `rows` are not the sequence's; a sequence
+ * that holds fewer tokens than it has new rows is not appended, its earliest
+ * rows see nothing.
  *
  * Ownership, streams and errors as in ssba.h: the caller owns every buffer,
  * calls are asynchronous on `hip_stream`, checks come before any launch, and

@@ -89,13 +89,15 @@ def rows_of(pool, layer, phys, head, which, page, d):
 # ---- the calls ---------------------------------------------------------------
 
 def sequences(batch, page, rows):
-    """(begin, new, len) of each sequence, cut to the arrays as the header says."""
+    """(begin, new, start, len) of each sequence, cut to the arrays as the header says; start: where the first new
+    token is, by the length as it is given."""
     table, lens, cu = batch
     out = []
     for s in range(len(lens)):
         begin = min(max(int(cu[s]), 0), rows)
         end = max(min(int(cu[s + 1]), rows), begin)
-        out.append((begin, end - begin, min(max(int(lens[s]), 0), table.shape[1] * page)))
+        held = max(int(lens[s]), 0)
+        out.append((begin, end - begin, held - (end - begin), min(held, table.shape[1] * page)))
     return out
 
 
@@ -105,8 +107,7 @@ def append(pool, layer, batch, k, v, page):
     rows, heads, d = k.shape
     pages = pool["k"].shape[1]
     order = orders(page, d)
-    for s, (begin, n, held) in enumerate(sequences(batch, page, rows)):
-        start = held - n
+    for s, (begin, n, start, held) in enumerate(sequences(batch, page, rows)):
         if n == 0 or start < 0:
             continue
         for lp in range(start // page, (held - 1) // page + 1):
@@ -133,8 +134,8 @@ def append(pool, layer, batch, k, v, page):
                         pool["kmean"][layer, phys, h] = to_bf16(E4M3[codes[order[0]]].sum(0) * 2.0 ** e / page)
 
 
-def visible(begin, n, held, tok, causal):
-    return min(max(held - n + tok + 1, 0), held) if causal else held
+def visible(start, held, tok, causal):
+    return min(max(start + tok + 1, 0), held) if causal else held
 
 
 def select(pool, layer, batch, q, page, keep, first=1, last=1, causal=True):
@@ -143,9 +144,9 @@ def select(pool, layer, batch, q, page, keep, first=1, last=1, causal=True):
     rows, heads, d = q.shape
     pages, kv = pool["k"].shape[1:3]
     out = np.full((rows, kv, 1 + keep), -7, dtype=np.int32)
-    for s, (begin, n, held) in enumerate(sequences(batch, page, rows)):
+    for s, (begin, n, start, held) in enumerate(sequences(batch, page, rows)):
         for tok in range(n):
-            sees = held - n + tok + 1 if causal else held
+            sees = visible(start, held, tok, causal)
             total = (sees - 1) // page + 1 if sees > 0 else 0
             for h in range(kv):
                 ids = list(range(total))
@@ -177,7 +178,7 @@ def attend(pool, layer, batch, q, page, lists=None, causal=True, scale=None):
     scale = d ** -0.5 if scale is None else scale
     o = np.full((rows, heads, d), np.nan)
     weight, spread = np.zeros((rows, heads, d)), np.zeros((rows, heads))
-    for s, (begin, n, held) in enumerate(sequences(batch, page, rows)):
+    for s, (begin, n, start, held) in enumerate(sequences(batch, page, rows)):
         for h in range(kv):
             known = {}
 
@@ -188,7 +189,7 @@ def attend(pool, layer, batch, q, page, lists=None, causal=True, scale=None):
                 return known[lp]
 
             for tok in range(n):
-                sees = visible(begin, n, held, tok, causal)
+                sees = visible(start, held, tok, causal)
                 if lists is None:
                     use = range(-(-sees // page))
                 else:

@@ -91,11 +91,11 @@ __global__ __launch_bounds__(256) void k_cache_append(AppendArgs a) {
   const int slot = id % a.slots;
   const int seq = id / a.slots;
   const SeqView sv = seq_view(a.b, a.c.page_log2, seq);
-  const int start = sv.len - sv.n;
+  const int start = sv.start;
   if (sv.n == 0 || start < 0) return;
   const int lp = (start >> a.c.page_log2) + slot;
+  if (lp > (sv.len - 1) >> a.c.page_log2) return;
   const int p0 = lp << a.c.page_log2;
-  if (p0 >= sv.len) return;
   const int phys = a.b.table[(int64_t)seq * a.b.max_pages + lp];
   if (phys < 0 || phys >= a.c.pages) return;
 

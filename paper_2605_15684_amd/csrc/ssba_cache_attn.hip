@@ -212,8 +212,7 @@ __global__ __launch_bounds__(P::THREADS, P::R > 1 || (P::D == 128 && (P::J > 1 |
   if ((P::CG == 1 || P::KP == 1) && cbase >= it.ncols) return;
   if (P::CG > 1 && P::KP > 1 && ct * P::CG * P::COLS >= it.ncols) return;   // the whole workgroup
   const int cend = min(cbase + P::COLS, it.ncols) - 1;   // < cbase: no columns
-  const int before = it.sv.len - it.sv.n;                // tokens in front of the new ones
-  auto limit = [&](int tok) { return a.causal ? min(max(before + tok + 1, 0), it.sv.len) : it.sv.len; };
+  auto limit = [&](int tok) { return a.causal ? min(max(it.sv.start + tok + 1, 0), it.sv.len) : it.sv.len; };
   const int minlim = limit(it.tok0 + (P::LISTED ? 0 : cbase / a.group));
   const int maxlim = cend < cbase ? 0 : limit(it.tok0 + (P::LISTED ? 0 : cend / a.group));
 

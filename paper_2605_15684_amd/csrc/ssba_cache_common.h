@@ -27,16 +27,20 @@ struct BatchView {
 };
 
 // A sequence of the batch as the kernels see it: whatever the arrays hold,
-// begin + n <= rows and 0 <= len <= max_pages * page.
+// begin + n <= rows and 0 <= len <= max_pages * page.  The first of the n new
+// tokens is at position start: negative where the sequence holds fewer, len
+// where it has outgrown its table by all of them.
 struct SeqView {
-  int begin, n, len;
+  int begin, n, start, len;
 };
 
 __device__ __forceinline__ SeqView seq_view(const BatchView& b, int page_log2, int s) {
   SeqView v;
   v.begin = min(max(b.cu[s], 0), b.rows);
   v.n = max(min(b.cu[s + 1], b.rows), v.begin) - v.begin;
-  v.len = min(max(b.lens[s], 0), b.max_pages << page_log2);
+  const int all = max(b.lens[s], 0);
+  v.len = min(all, b.max_pages << page_log2);
+  v.start = min(all - v.n, v.len);
   return v;
 }
 
@@ -58,7 +62,9 @@ __device__ __forceinline__ bool seq_of_row(const BatchView& b, int page_log2, in
       if (*seq >= b.seqs) return false;
       v->begin = min(max(begin, 0), b.rows);
       v->n = max(min(__builtin_amdgcn_readlane(end, c), b.rows), v->begin) - v->begin;
-      v->len = min(max(__builtin_amdgcn_readlane(len, c), 0), b.max_pages << page_log2);
+      const int all = max(__builtin_amdgcn_readlane(len, c), 0);
+      v->len = min(all, b.max_pages << page_log2);
+      v->start = min(all - v->n, v->len);
       return r >= v->begin && r - v->begin < v->n;
     }
   }

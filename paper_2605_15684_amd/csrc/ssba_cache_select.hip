@@ -40,7 +40,7 @@ struct Range {
 };
 
 __device__ __forceinline__ Range range_of(const SelectArgs& a, const SeqView& sv, int tok) {
-  const int seen = a.causal ? sv.len - sv.n + tok + 1 : sv.len;
+  const int seen = a.causal ? min(sv.start + tok + 1, sv.len) : sv.len;
   Range r;
   r.total = seen > 0 ? ((seen - 1) >> a.c.page_log2) + 1 : 0;
   r.middle = r.total > a.keep ? r.total - a.first - a.last : 0;

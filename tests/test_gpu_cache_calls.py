@@ -92,3 +92,37 @@ def test_rows_of_no_sequence_do_not_matter(new):
     for other in results[1:]:
         assert all(torch.equal(x, y) for x, y in zip(other[:3], results[0][:3]))
         assert_same_pool(other[3], results[0][3])
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("columns", [3, 1200])
+def test_sequences_that_outgrow_their_table(columns, dtype):
+    """Tokens past the table's last page are not written, and move nothing that is there: the ones that still fit are at
+    their own positions, the last pages keep what they held (a sharing row may read it); queries past it see all."""
+    from paper_2605_15684_amd import cache
+    from oracle import cache_oracle as C
+    from _cache import assert_same_pool, gpu_batch, gpu_pool, host_pool, make_pool, rounded
+    from test_gpu_cache import check_attend
+    rng = np.random.default_rng(33)
+    page, d, heads, kv, keep = 16, 64, 4, 2, 2
+    end = columns * page
+    over = [(end + 1, 1), (end + 5, 10), (end + 70, 10), (2 ** 31 - 1, 3), (end, 4), (end - 3, 2)]
+    pool = make_pool(rng, 1, 6 * 3, kv, d, page)
+    table = np.full((len(over), columns), -1, dtype=np.int32)
+    table[:, -3:] = rng.permutation(18).reshape(6, 3)
+    batch = (table, np.array([h for h, _ in over], dtype=np.int32), np.cumsum([0] + [n for _, n in over]).astype(np.int32))
+    rows = int(batch[2][-1])
+    (k, k64), (v, v64), (q, q64) = (rounded(rng, (rows, n, d), dtype, 0.3) for n in (kv, kv, heads))
+    g, b = gpu_pool(pool), gpu_batch(batch, 10)
+    cache.append(g, 0, b, k.cuda(), v.cuda())
+    before = host_pool(gpu_pool(pool))
+    C.append(pool, 0, batch, k64, v64, page)
+    assert_same_pool(host_pool(g), pool)
+    for s in (0, 2, 3):                              # nothing of these fits
+        for x in before:
+            assert np.array_equal(before[x][0, table[s, -3:]], pool[x][0, table[s, -3:]])
+    lists = cache.select(g, 0, b, q.cuda(), keep=keep)
+    want = C.select(pool, 0, batch, q64, page, keep)
+    assert np.array_equal(lists.cpu().numpy(), want)
+    check_attend(cache.attend(g, 0, b, q.cuda()), C.attend(pool, 0, batch, q64, page), end, d, dtype)
+    check_attend(cache.attend(g, 0, b, q.cuda(), lists=lists), C.attend(pool, 0, batch, q64, page, want), end, d, dtype)
