@@ -110,7 +110,9 @@ typedef struct ssba_cache_query {
 ssba_status ssba_cache_append(const ssba_cache* c, int32_t layer, const ssba_cache_batch* b, int32_t dtype,
                               const void* k, const void* v, int64_t stride_t, int64_t stride_h, void* hip_stream);
 
-/* Device bytes of the scratch of ssba_cache_select for this cache, batch and query. */
+/* Device bytes of the scratch of ssba_cache_select for this cache, batch and
+ * query: 0 for tables of up to 1152 pages or up to `keep`, else 8 * rows *
+ * kv_heads * max_pages (4096 rows, 8 heads, 16384 pages: 4.3 GB). */
 ssba_status ssba_cache_select_workspace_size(const ssba_cache* c, const ssba_cache_batch* b,
                                              const ssba_cache_query* q, size_t* scratch_bytes);
 
@@ -124,8 +126,7 @@ ssba_status ssba_cache_select_workspace_size(const ssba_cache* c, const ssba_cac
  * pages that are not there rank last.  `lists` int32 [rows][kv_heads][1 + keep]:
  * the count, page numbers of the sequence (columns of the table) ascending,
  * then -1.  Appending must come first: only complete pages are scored.
- * `scratch` 16-byte aligned (NULL where its size is 0: tables of up to 1152
- * pages). */
+ * `scratch` 16-byte aligned (NULL where its size is 0). */
 ssba_status ssba_cache_select(const ssba_cache* c, int32_t layer, const ssba_cache_batch* b,
                               const ssba_cache_query* q, const void* query, int32_t* lists, size_t lists_bytes,
                               void* scratch, size_t scratch_bytes, void* hip_stream);

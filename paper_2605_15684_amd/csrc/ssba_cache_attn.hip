@@ -32,11 +32,12 @@
 //
 // What bounds it, and what it reaches (launch alone):
 //   few columns   the pages' bytes: 64 sequences of 8 to 16 thousand tokens, 4 kv
-//                 heads, D 128: 121 us, 5.4 TB/s.  Three waves a SIMD with one
+//                 heads, D 128: 122 us, 5.4 TB/s (659 MB, three sets of inputs
+//                 in turn; row sums read 6.05 TB/s).  Three waves a SIMD with one
 //                 step under way each; four (128 registers) take 148 us, two
 //                 steps under way as long as one.
 //   many columns  matrix and vector work: 4096 tokens x 16 heads over 16384
-//                 keys, D 128: 450 us, 1.22 PFLOP/s.  Two waves a SIMD, 64
+//                 keys, D 128: 475 us, 1.16 PFLOP/s.  Two waves a SIMD, 64
 //                 columns each: their O takes half of the registers, so the
 //                 queries stay in the LDS.
 //   lists         few columns of a tile are in use, so vector issue.  Where a
