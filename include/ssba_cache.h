@@ -23,8 +23,8 @@
  *            V: 16 D T + 1024 (c/64) + 256 (r/4) + 16 (c%16) + 4 (c%64 / 16) + r%4
  *          of its page (16-byte loads of a wave are 1024 consecutive bytes).
  *   scale  fp32 [layers][pages][kv_heads][2], 8-byte aligned: a key is
- *          scale[0] * code, a value scale[1] * code; positive, at most 2^120
- *          (append writes powers of two).
+ *          scale[0] * code, a value scale[1] * code; 2^-64 to 2^120 (append
+ *          writes powers of two).
  *   kmean  bf16 [layers][pages][kv_heads][D], 16-byte aligned: the mean of the
  *          keys of a complete page (select reads it; attend does not).
  * Nothing has to be initialised: slots behind a sequence's end are never used,
@@ -101,7 +101,7 @@ typedef struct ssba_cache_query {
  * value put into it since its first token: |x| <= 448 * 2^e.  A value is held
  * as code = e4m3(x * 2^-e), to nearest, ties to even; +-inf as +-448, NaN as
  * NaN.  In a page that holds older tokens 2^e also reaches the scale s that it
- * has, which may be any positive one; where s is not 2^e, the older codes are
+ * has, which need not be a power of two; where s is not 2^e, the older codes are
  * restated as e4m3(code * (s * 2^-e)), the product in fp32.  When the last
  * token of a page comes, kmean = bf16(2^e * sum(codes) / page).  The result does
  * not depend on atomics or on the order of workgroups.  Pages that several rows

@@ -25,10 +25,12 @@
 // the rounding stays below that of a bf16 output.  fp16 ends at 2^16, so m is
 // taken of the weights p * vs there, 2^8 below the largest, and raised when a
 // lane's sum of four passes 2^15; weights of less than 2^-22 of the largest are
-// held in steps of 2^-32 of it.  A chunk of 4096 tokens over 16384 keys, D 128,
-// takes 473 us and is off by 0.00167 (rms, of which the output's own rounding
-// is 0.00166); with one bf16 term 466 us and 0.00236, with two 613 us.  The
-// selected chunk below takes the same time with either and 8 us more with two.
+// held in steps of 2^-32 of it.  Sums of probabilities are relative to the same
+// m; where V's scales differ by more than 2^40 they are formed apart, as p * vs
+// may be too small for fp32 where p is not.  A chunk of 4096 tokens over 16384
+// keys, D 128, takes 478 us and is off by 0.00167 (rms, of which the output's
+// own rounding is 0.00166); with one bf16 term 460 us and 0.00236, with two
+// 613 us.  The selected chunk: 59.7 us in all, 58.6, 69.
 //
 // What bounds it, and what it reaches (launch alone):
 //   few columns   the pages' bytes: 64 sequences of 8 to 16 thousand tokens, 4 kv
@@ -65,6 +67,7 @@ typedef uint32_t u32x4a4 __attribute__((ext_vector_type(4), aligned(4)));
 constexpr float kMost = 1048576.f;   // a lane's sum of probabilities of a step: 2^20
 // Probabilities in fp16, V's scale included: a lane's sum of four, and how far m is below the largest when it is taken.
 constexpr float kMostHalf = 32768.f, kBelow = 8.f;
+constexpr float kLow = 0x1p40f;      // a V scale that far below another page's: sums are taken apart
 constexpr int kNoKey = 0x40000000;   // first token of a group that is not there: behind every sequence
 
 union Frag {
@@ -90,6 +93,23 @@ __device__ __forceinline__ halfx2 half_codes_hi(uint32_t w) {
 }
 
 __device__ __forceinline__ float exp2_(float x) { return __builtin_amdgcn_exp2f(x); }
+
+// Maximum over the wave (of the bits of numbers >= 0: of the numbers).
+__device__ __forceinline__ uint32_t wave_max(uint32_t x) {
+  x = max(x, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0x111, 0xf, 0xf, false));   // row_shr 1
+  x = max(x, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0x112, 0xf, 0xf, false));
+  x = max(x, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0x114, 0xf, 0xf, false));
+  x = max(x, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0x118, 0xf, 0xf, false));
+  x = max(x, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0x142, 0xa, 0xf, false));   // row_bcast 15
+  x = max(x, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, 0x143, 0xc, 0xf, false));   // row_bcast 31
+  return (uint32_t)__builtin_amdgcn_readlane((int)x, 63);
+}
+
+// x 2^d where 2^d may be less than fp32 holds and the product is not.
+__device__ __forceinline__ float shrink(float x, float d) {
+  const float h = exp2_(0.5f * d);
+  return x * h * h;
+}
 
 __device__ __forceinline__ int lane_i(int v, int l) { return __builtin_amdgcn_readlane(v, l); }
 __device__ __forceinline__ float lane_f(float v, int l) {
@@ -293,6 +313,8 @@ __global__ __launch_bounds__(P::THREADS, P::R > 1 || (P::D == 128 && (P::J > 1 |
   const int64_t head_off = ((int64_t)it.h << page_log2) * D;
   int m_page = 0, m_key = 0;    // of group chunk * 64 + lane: page (-1: none) and first token
   float m_ks = 1.f, m_vs = 1.f, m_lv = 0.f;   // its scales; log2 of V's
+  uint32_t vs_top = 0;          // largest of V's scales so far, of all lanes (bits)
+  bool m_low = false;           // some are far below it
   auto load_chunk = [&](int chunk) {
     const int gr = chunk * 64 + lane;
     int page = -1, key = kNoKey;
@@ -317,6 +339,10 @@ __global__ __launch_bounds__(P::THREADS, P::R > 1 || (P::D == 128 && (P::J > 1 |
     m_ks = ks * a.scale_log2;
     m_vs = P::F32 ? vs : 1.f / vs;
     m_lv = P::F32 ? 0.f : __builtin_amdgcn_logf(vs);
+    if (P::HALF) {
+      vs_top = max(vs_top, wave_max(page < 0 ? 0u : __float_as_uint(vs)));
+      m_low = __builtin_amdgcn_ballot_w64(page >= 0 && vs * kLow < __uint_as_float(vs_top)) != 0;
+    }
   };
   int chunk = -1;   // 32 / J steps a chunk
 
@@ -325,6 +351,7 @@ __global__ __launch_bounds__(P::THREADS, P::R > 1 || (P::D == 128 && (P::J > 1 |
     int key[2];   // J > 1: these four of the lane's share
     float ks[2], vs[2], lv[2];
     int64_t off[2 * J];
+    bool low;     // sums are taken apart
   };
   // The group numbers, scales and K codes of step s, then its V codes.
   auto fetch_k = [&](int s, Step& x) {
@@ -342,6 +369,7 @@ __global__ __launch_bounds__(P::THREADS, P::R > 1 || (P::D == 128 && (P::J > 1 |
 #pragma unroll
       for (int hh = 0; hh < NH; ++hh) x.k[t][hh] = *reinterpret_cast<const u32x4*>(kp_ + lane * 16 + hh * 1024);
     }
+    x.low = m_low;
 #pragma unroll
     for (int t = 0; t < 2; ++t) {   // behind the loads: the scales may still be on their way
       const int l = (2 * J * s + t) & 63;
@@ -351,7 +379,8 @@ __global__ __launch_bounds__(P::THREADS, P::R > 1 || (P::D == 128 && (P::J > 1 |
         x.vs[t] = __shfl(m_vs, l + 2 * mine);
         if (!P::F32) x.lv[t] = __shfl(m_lv, l + 2 * mine);
       } else {
-        x.key[t] = lane_i(m_key, l);
+        // Without lists group g begins at token 16 g: a register less to hold.
+        x.key[t] = P::LISTED ? lane_i(m_key, l) : lane_i(m_page, l) < 0 ? kNoKey : (2 * s + t) << 4;
         x.ks[t] = lane_f(m_ks, l);
         x.vs[t] = lane_f(m_vs, l);
         if (!P::F32) x.lv[t] = lane_f(m_lv, l);
@@ -489,7 +518,7 @@ __global__ __launch_bounds__(P::THREADS, P::R > 1 || (P::D == 128 && (P::J > 1 |
       if (P::HALF) high = top > kMostHalf;
     };
     probabilities();
-    if (edge || !settled || __builtin_amdgcn_ballot_w64(high)) {
+    if (edge || (P::HALF && x.low) || !settled || __builtin_amdgcn_ballot_w64(high)) {
       // Some column has no maximum yet, or has outgrown it.
       bool none = false;
 #pragma unroll
@@ -504,13 +533,27 @@ __global__ __launch_bounds__(P::THREADS, P::R > 1 || (P::D == 128 && (P::J > 1 |
         mx = fmaxf(mx, __shfl_xor(mx, 32));
         const float to = fmaxf(m[r], P::HALF ? mx - kBelow : mx);
         const float f = to > m[r] ? exp2_(m[r] - to) : 1.f;
+        l[r] = !P::HALF ? l[r] * f : to > m[r] ? shrink(l[r], m[r] - to) : l[r];
         m[r] = to;
         none |= to == -INFINITY && lim[r] > 0;
-        l[r] *= f;
 #pragma unroll
         for (int c = 0; c < NC; ++c) o[r][c] *= f;
       }
       settled = !__builtin_amdgcn_ballot_w64(none);
+      // The sum of a page's probabilities is that of its weights p * vs over vs, unless these may be too small for
+      // fp32 beside another page's where the probabilities are not (a page of zeros has a V scale of 2^-64).
+      const bool low = P::HALF && x.low;
+      if (low) {
+#pragma unroll
+        for (int r = 0; r < R; ++r) {
+          const float mu = m[r] == -INFINITY ? 0.f : m[r];
+#pragma unroll
+          for (int t = 0; t < 2; ++t)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) l[r] += exp2_(__builtin_fmaf(s[t][r][i], x.ks[t], -mu));
+        }
+        x.vs[0] = x.vs[1] = 0.f;   // those below count for nothing
+      }
       probabilities();
     }
 #pragma unroll
@@ -636,7 +679,7 @@ __global__ __launch_bounds__(P::THREADS, P::R > 1 || (P::D == 128 && (P::J > 1 |
 #pragma unroll
     for (int x = P::COLS; x < 16; x <<= 1) mall = fmaxf(mall, __shfl_xor(mall, x));
     const float f = m[0] == mall ? 1.f : exp2_(m[0] - mall);
-    l[0] *= f;
+    l[0] = !P::HALF ? l[0] * f : m[0] == mall ? l[0] : shrink(l[0], m[0] - mall);
 #pragma unroll
     for (int x = P::COLS; x < 16; x <<= 1) l[0] += __shfl_xor(l[0], x);
 #pragma unroll
@@ -699,7 +742,9 @@ __global__ __launch_bounds__(P::THREADS, P::R > 1 || (P::D == 128 && (P::J > 1 |
     for (int e = 0; e < E; ++e) acc[e] = 0.f;
 #pragma unroll
     for (int w = 0; w < P::KP; ++w) {
-      sum += s_l[ocg][w][c16] * (s_m[ocg][w][c16] == cm ? 1.f : exp2_(s_m[ocg][w][c16] - cm));
+      const float lw = s_l[ocg][w][c16], d = s_m[ocg][w][c16] - cm;
+      if (s_m[ocg][w][c16] == cm) sum += lw;
+      else sum += P::HALF ? shrink(lw, d) : lw * exp2_(d);
 #pragma unroll
       for (int e = 0; e < E; ++e) acc[e] += s_o[((ocg * P::KP + w) * 16 + c16) * LD + ch + e];
     }
@@ -734,6 +779,7 @@ constexpr int kMaxSplits = 256;
 // RC: tiles of 16 columns of an item.
 template <int D, int RC, bool F32, bool LISTED>
 __global__ __launch_bounds__(256) void k_cache_join(AttendArgs a) {
+  constexpr bool HALF = !F32 && !LISTED && RC > 1;
   __shared__ float s_w[kMaxSplits][16];
   __shared__ float s_sum[16];
   __shared__ floatx4 s_acc[128];
@@ -767,7 +813,8 @@ __global__ __launch_bounds__(256) void k_cache_join(AttendArgs a) {
         const float ms = ml[(int64_t)s * RC * 32];
         const float w = ms == m ? 1.f : exp2_(ms - m);
         s_w[s][c] = w;
-        sum += w * ml[(int64_t)s * RC * 32 + 1];
+        const float l = ml[(int64_t)s * RC * 32 + 1];
+        sum += HALF && ms != m ? shrink(l, ms - m) : w * l;
       }
 #pragma unroll
     for (int x = 1; x < 16; x <<= 1) sum += __shfl_xor(sum, x);

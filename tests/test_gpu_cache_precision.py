@@ -141,3 +141,22 @@ def test_attend_queries_that_are_nan(page, d, heads, kv, keep, bits, seqs):
     assert np.isnan(got[bad]).all()
     length = keep * page if keep else max(h for h, _ in seqs)
     check(torch.from_numpy(np.where(bad[..., None], o, got)), (o, w, x), length, d, BF16, bits, 2.0 ** -6)
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("page,d,heads,kv,keep,bits,seqs", FORMS)
+def test_attend_scales_of_every_size(page, d, heads, kv, keep, bits, seqs, dtype):
+    """V's scales from the smallest that append writes to 2^60, powers of two and others, in pages of one sequence; then
+    the smallest alone.  A page of 2^60 outweighs the others, as it does in W."""
+    rng = np.random.default_rng(4)
+    pages, rows = sum(-(-h // page) for h, _ in seqs), sum(n for _, n in seqs)
+    batch = make_batch(rng, seqs, page, pages)
+    q, q64 = rounded(rng, (rows, heads, d), dtype, 0.5)
+    lists = some_lists(rng, seqs, kv, keep, page) if keep else None
+    length = keep * page if keep else max(h for h, _ in seqs)
+    for sizes in ([2.0 ** -64, 1.7 * 2.0 ** -40, 1.0, 0.6, 2.0 ** 60], [2.0 ** -64, 1.3 * 2.0 ** -64]):
+        pool = make_pool(rng, 1, pages, kv, d, page)
+        pool["scale"][..., 0] *= rng.uniform(0.5, 1.0, pool["scale"].shape[:3]).astype(np.float32)
+        pool["scale"][..., 1] = rng.choice(sizes, pool["scale"].shape[:3]).astype(np.float32)
+        got = run(pool, batch, q, lists, seqs)
+        check(got, C.attend(pool, 0, batch, q64, page, lists), length, d, dtype, bits, max(sizes))
