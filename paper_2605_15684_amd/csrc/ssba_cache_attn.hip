@@ -39,14 +39,15 @@
 //                 step under way each; four (128 registers) take 148 us, two
 //                 steps under way as long as one.
 //   many columns  matrix and vector work: 4096 tokens x 16 heads over 16384
-//                 keys, D 128: 475 us, 1.16 PFLOP/s.  Two waves a SIMD, 64
+//                 keys, D 128: 480 us, 1.15 PFLOP/s.  Two waves a SIMD, 64
 //                 columns each: their O takes half of the registers, so the
 //                 queries stay in the LDS.
 //   lists         few columns of a tile are in use, so vector issue.  Where a
 //                 wave has a row alone and G is at most 8, a tile is two times
 //                 the same 8 columns with other keys (J): half the exponentials.
-//                 1024 tokens x 8 kv heads x 20 pages of 32, D 64, G 3: 43 us, 16
-//                 TB/s from the L2; J 1 48 us, J 4 49 us (registers).
+//                 1024 tokens x 8 kv heads x 20 pages of 32, D 64, G 3: 44 us, 16
+//                 TB/s from the L2 (with bf16 probabilities 43; there J 1 took
+//                 48 us, J 4 49: registers).
 #include <hip/hip_runtime.h>
 #include <hip/hip_bf16.h>
 
