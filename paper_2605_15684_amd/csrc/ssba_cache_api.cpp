@@ -171,7 +171,7 @@ AttendPlan plan(const ssba_cache* c, const ssba_cache_batch* b, const ssba_cache
   if (listed) {
     p.col_tiles = (int)ceil_div(cols, 16);
     const int64_t items = (int64_t)b->rows * c->kv_heads * p.col_tiles;
-    // A wave each from 2 waves a SIMD on (2048 items of 2048 keys, D 128: 55 us, in 4 waves each 67; 1024: 38, 37).
+    // A wave each from 2 waves a SIMD on (2048 items of 2048 keys, D 128: 49 us, in 4 waves each 58; 1024: 34.7, 34.4).
     p.kind = items >= 2048 ? ssba::kAttendRows : ssba::kAttendRow;
     p.items = p.kind == ssba::kAttendRows ? ceil_div(b->rows, 4) * c->kv_heads * p.col_tiles : items;
   } else {
@@ -186,8 +186,8 @@ AttendPlan plan(const ssba_cache* c, const ssba_cache_batch* b, const ssba_cache
   if (p.tiles >= 4) {
     // One workgroup fills a CU.  Parts of at least 256 keys, as many as take the least time by these measured costs
     // in us: each round over the 256 CUs its beginning and end and its keys, the joining launch itself and its bytes
-    // (written and read).  100 new tokens of 16 sequences, 16 heads on 4, D 64: of 600 tokens 21 us whole, 30 in two
-    // parts; of 2000 48 us whole, 41 in two.
+    // (written and read).  100 new tokens of 16 sequences, 16 heads on 4, D 64: of 600 tokens 22 us whole, 30 in two
+    // parts; of 2000 48 us whole, 42 in two.
     const double d = c->head_dim, round = 3 + p.tiles * d / 400, key = p.tiles * (8e-4 + 6e-6 * d);
     const double column_bytes = 2.0 * 16 * p.tiles * d * 4;
     double best = ceil_div(items, 256) * (round + key * keys);
@@ -207,7 +207,7 @@ AttendPlan plan(const ssba_cache* c, const ssba_cache_batch* b, const ssba_cache
     // and 18).  Few long ones need more CUs (4 items of 4096 keys 18.6 and 18.8 us, in parts 8.1 and 18), and long
     // ragged ones more parts (40 sequences of up to 8000 keys: 57 us, in parts 53).  fp32 (more vector work), D
     // 128: 256 items of 4000 keys 52 us, in parts 58; 128 of 2000 17.8, 20.1; 128 ragged ones of up to 2999 21.0, 20.2.
-    // 32 columns, D 128: 64 items of 600 keys 9.7 us, in parts 11.7.
+    // 32 columns, D 128: 64 items of 600 keys 9.9 us, in parts 11.9.
     p.threads = 512;
   } else if (p.kind != ssba::kAttendRows) {
     // 4 waves of at least 2 steps of 32 keys each, up to about 512 workgroups: more of them fill the chip more
