@@ -38,7 +38,8 @@ EXPORTS = ("ssba_abi_version", "ssba_status_str", "ssba_workspace_size", "ssba_b
            "ssba_cache_append", "ssba_cache_select_workspace_size", "ssba_cache_select",
            "ssba_cache_attend_workspace_size", "ssba_cache_attend", "ssba_pages_workspace_size",
            "ssba_pages_reserve", "ssba_pages_fork", "ssba_pages_release", "ssba_pages_compact",
-           "ssba_pages_copy")
+           "ssba_pages_copy", "ssba_rope_rotate", "ssba_window_forward",
+           "ssba_window_backward_workspace_size", "ssba_window_backward")
 
 # Byte count that the binding passes for a buffer it cannot size (None).
 UNSIZED = ctypes.c_size_t(-1).value
@@ -88,6 +89,30 @@ class CacheQuery(ctypes.Structure):         # ssba_cache_query
 class CachePages(ctypes.Structure):         # ssba_pages
     _fields_ = [("rows", ctypes.c_int32), ("max_pages", ctypes.c_int32), ("table", ctypes.c_void_p),
                 ("lens", ctypes.c_void_p), ("refs", ctypes.c_void_p)]
+
+
+class RopeDesc(ctypes.Structure):           # ssba_rope
+    _fields_ = [("head_dim", ctypes.c_int32), ("pairs", ctypes.c_int32), ("axes", ctypes.c_int32),
+                ("axis", ctypes.c_void_p), ("freq", ctypes.c_void_p)]
+
+
+class RopeTensor(ctypes.Structure):         # ssba_rope_tensor
+    _fields_ = [("heads", ctypes.c_int32), ("x", ctypes.c_void_p), ("y", ctypes.c_void_p)] + \
+        [(f"{t}_stride_{s}", ctypes.c_int64) for t in "xy" for s in "bht"]
+
+
+class Strides(ctypes.Structure):            # ssba_strides
+    _fields_ = [("b", ctypes.c_int64), ("h", ctypes.c_int64), ("t", ctypes.c_int64)]
+
+
+class WindowDesc(ctypes.Structure):         # ssba_window
+    _fields_ = [(x, ctypes.c_int32) for x in ("batch", "seq", "heads", "kv_heads", "head_dim", "dtype", "window",
+                                              "sinks", "seqs", "max_len")] + \
+        [("softmax_scale", ctypes.c_float), ("cu", ctypes.c_void_p)] + [(x, Strides) for x in "qkvo"]
+
+
+class WindowGrads(ctypes.Structure):        # ssba_window_grads
+    _fields_ = [(x, Strides) for x in ("do_", "dq", "dk", "dv")]
 
 
 class SsbaError(RuntimeError):
@@ -158,6 +183,7 @@ def load(path: str = None) -> ctypes.CDLL:
     lib.ssba_probe_mfma.argtypes = [ctypes.c_int32, ctypes.c_int32, vp, vp]
     i32, i64 = ctypes.c_int32, ctypes.c_int64
     cp, bp, qp, pp = (ctypes.POINTER(t) for t in (CacheDesc, CacheBatch, CacheQuery, CachePages))
+    rp, tp, wp, gp = (ctypes.POINTER(t) for t in (RopeDesc, RopeTensor, WindowDesc, WindowGrads))
     for name, args in (("ssba_build_index_ex", [dp, vp, vp, vp, sz, vp, sz, vp]),
                        ("ssba_forward_ex", [dp, vp, vp, vp, vp, sz, vp, vp]),
                        ("ssba_forward_topk_ex", [dp, vp, vp, vp, vp, sz, vp, sz, vp, vp]),
@@ -182,7 +208,11 @@ def load(path: str = None) -> ctypes.CDLL:
                        ("ssba_pages_fork", [cp, pp, i32, vp, vp, vp, vp, sz, vp]),
                        ("ssba_pages_release", [cp, pp, i32, vp, vp, vp, sz, vp]),
                        ("ssba_pages_compact", [cp, pp, vp, vp, vp, vp, sz, vp]),
-                       ("ssba_pages_copy", [cp, cp, i32, vp, vp, vp])):
+                       ("ssba_pages_copy", [cp, cp, i32, vp, vp, vp]),
+                       ("ssba_rope_rotate", [rp, i32, i32, i32, i32, vp, i64, i64, i32, tp, vp]),
+                       ("ssba_window_forward", [wp, vp, vp, vp, vp, vp, vp]),
+                       ("ssba_window_backward_workspace_size", [wp, ctypes.POINTER(sz)]),
+                       ("ssba_window_backward", [wp, gp, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, sz, vp])):
         fn = getattr(lib, name)
         fn.restype = ctypes.c_int
         fn.argtypes = args

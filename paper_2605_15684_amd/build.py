@@ -40,6 +40,12 @@ SOURCES = {
     # 64-bit scores: no contraction of multiply-add, so lists do not depend on the compiler.
     "ssba_cache_select.hip": ["-ffp-contract=off"],
     "ssba_cache_pages.hip": [],
+    "ssba_rope_api.cpp": [],
+    "ssba_rope.hip": [],
+    "ssba_window_api.cpp": [],
+    # MFMA results in ordinary VGPRs, as above.
+    "ssba_window.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form"],
+    "ssba_window_bwd.hip": [],
 }
 
 COMMON = [

@@ -1,0 +1,193 @@
+// Rotary positions with several axes (include/ssba_rope.h).
+//
+// A workgroup takes 4 tokens: its threads form the cosines and sines of their
+// pairs (one per thread at D 128), leave them in the LDS and then turn the
+// heads, each thread the same pairs of one token in every few heads, with those
+// pairs' cosines and sines in registers.  The first heads' values are loaded
+// before the angles are formed.
+//
+// Angles: x = pos * freq in quarter turns, reduced to |r| <= 1/2 by x - rint(x)
+// in 64 bits (one rounding, of the fused multiply-add), then the Taylor series
+// of the sine and cosine of r pi/2, whose first terms left out are below 2e-11
+// and 2e-10 of 1.
+#include <hip/hip_runtime.h>
+
+#include <type_traits>
+
+#include "ssba_rope_common.h"
+
+namespace ssba {
+namespace {
+
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef float floatx8 __attribute__((ext_vector_type(8)));
+typedef float floatx4 __attribute__((ext_vector_type(4)));
+
+constexpr float kStays = 2.f;   // in a cosine's place: the pair stays as it is
+
+// cos and sin of pos * f quarter turns.
+__device__ __forceinline__ float2 turn(int pos, double f, bool inverse) {
+  const double p = (double)pos;
+  const double n = __builtin_rint(p * f);
+  const double r = __builtin_fma(p, f, -n) * 1.57079632679489661923;
+  const double z = r * r;
+  double s = -1.0 / 39916800, c = -1.0 / 3628800;   // -1/11!, -1/10!
+  s = __builtin_fma(s, z, 1.0 / 362880);
+  c = __builtin_fma(c, z, 1.0 / 40320);
+  s = __builtin_fma(s, z, -1.0 / 5040);
+  c = __builtin_fma(c, z, -1.0 / 720);
+  s = __builtin_fma(s, z, 1.0 / 120);
+  c = __builtin_fma(c, z, 1.0 / 24);
+  s = __builtin_fma(s, z, -1.0 / 6);
+  c = __builtin_fma(c, z, -0.5);
+  s = __builtin_fma(s * z, r, r);
+  c = __builtin_fma(c, z, 1.0);
+  // n mod 4, of an n that may be far outside int.
+  const int q = (int)(n - 4.0 * __builtin_floor(n * 0.25));
+  const double sn = q & 1 ? c : s, cs = q & 1 ? s : c;
+  const float sine = (float)(q & 2 ? -sn : sn), cosine = (float)((q + 1) & 2 ? -cs : cs);
+  return make_float2(cosine, inverse ? -sine : sine);
+}
+
+// Eight consecutive channels (fp32 rows may begin at any multiple of 4 bytes).
+template <bool F32>
+struct Eight {
+  typedef float vec4 __attribute__((ext_vector_type(4), aligned(4)));
+  typedef typename std::conditional<F32, vec4, floatx4>::type vec;
+  floatx4 v[F32 ? 2 : 1];
+  __device__ __forceinline__ void load(const char* p) {
+#pragma unroll
+    for (int i = 0; i < (F32 ? 2 : 1); ++i) v[i] = *reinterpret_cast<const vec*>(p + 16 * i);
+  }
+  __device__ __forceinline__ void store(char* p) const {
+#pragma unroll
+    for (int i = 0; i < (F32 ? 2 : 1); ++i) *reinterpret_cast<vec*>(p + 16 * i) = v[i];
+  }
+  __device__ __forceinline__ floatx8 get() const {
+    if constexpr (F32) {
+      return floatx8{v[0][0], v[0][1], v[0][2], v[0][3], v[1][0], v[1][1], v[1][2], v[1][3]};
+    } else {
+      return __builtin_convertvector(__builtin_bit_cast(bf16x8, v[0]), floatx8);
+    }
+  }
+  __device__ __forceinline__ void set(floatx8 x) {
+    if constexpr (F32) {
+      v[0] = floatx4{x[0], x[1], x[2], x[3]};
+      v[1] = floatx4{x[4], x[5], x[6], x[7]};
+    } else {
+      v[0] = __builtin_bit_cast(floatx4, __builtin_convertvector(x, bf16x8));
+    }
+  }
+};
+
+__device__ __forceinline__ void turn_pair(float& a, float& b, float c, float s) {
+  const float x = __builtin_fmaf(a, c, -(b * s)), y = __builtin_fmaf(b, c, a * s);
+  a = c == kStays ? a : x;
+  b = c == kStays ? b : y;
+}
+
+// One workgroup: kRopeRows tokens, a part of the heads.  A thread holds two
+// eights (HALVES: channels c .. and D/2 + c ..) or one.
+template <int D, bool F32, bool HALVES>
+__global__ __launch_bounds__(256) void k_rope(TurnArgs a) {
+  constexpr int R = kRopeRows, H2 = D / 2, E = HALVES ? 2 : 1, PER = 4 * E;   // pairs of a thread
+  constexpr int TPR = H2 / PER, SLOTS = 256 / (TPR * R), SIZE = F32 ? 4 : 2;
+  constexpr int U = 4;   // heads of a thread under way at once
+  __shared__ float2 s_turn[R][H2];
+  const int64_t tok0 = (int64_t)(blockIdx.x / a.head_parts) * R;
+  const int part = blockIdx.x % a.head_parts;
+  const int at = threadIdx.x % TPR, row = threadIdx.x / TPR % R, slot = threadIdx.x / (TPR * R);
+  const int64_t tok = tok0 + row;
+  const bool in = tok < a.tokens;
+  const int64_t b = in ? tok / a.rows : 0, t = in ? tok - b * a.rows : 0;
+  const int all = a.heads[0] + a.heads[1];
+  const int each = (all + a.head_parts - 1) / a.head_parts;
+  const int h_end = in ? min(all, (part + 1) * each) : 0;
+  const int ch = at * 8;
+  const int64_t x0 = b * a.x_sb[0] + t * a.x_st[0] + ch, x1 = b * a.x_sb[1] + t * a.x_st[1] + ch;
+  const int64_t y0 = b * a.y_sb[0] + t * a.y_st[0] + ch, y1 = b * a.y_sb[1] + t * a.y_st[1] + ch;
+
+  Eight<F32> v[U][E];
+  auto load = [&](int h0) {
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const int h = h0 + u * SLOTS;
+      if (h >= h_end) continue;
+      const bool second = h >= a.heads[0];
+      const char* p = a.x[second] + (second ? x1 + (h - a.heads[0]) * a.x_sh[1] : x0 + h * a.x_sh[0]) * SIZE;
+#pragma unroll
+      for (int e = 0; e < E; ++e) v[u][e].load(p + e * H2 * SIZE);
+    }
+  };
+  int h = part * each + slot;
+  load(h);
+
+  for (int i = threadIdx.x; i < R * H2; i += 256) {
+    const int r = i / H2, j = i % H2;
+    const int64_t tk = tok0 + r;
+    float2 w = make_float2(kStays, 0.f);
+    const int axis = a.axis[j];
+    if (tk < a.tokens && axis >= 0) {
+      const int64_t tb = tk / a.rows;
+      w = turn(a.pos[tb * a.p_sb + (tk - tb * a.rows) * a.p_st + axis], a.freq[j], a.inverse);
+    }
+    s_turn[r][j] = w;
+  }
+  __syncthreads();
+  float2 w[PER];
+#pragma unroll
+  for (int j = 0; j < PER; ++j) w[j] = s_turn[row][at * PER + j];
+
+  for (; h < h_end; h += U * SLOTS) {
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const int hu = h + u * SLOTS;
+      if (hu >= h_end) continue;
+      floatx8 x = v[u][0].get(), y;
+      if constexpr (HALVES) {
+        y = v[u][1].get();
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+          float p = x[j], q = y[j];
+          turn_pair(p, q, w[j].x, w[j].y);
+          x[j] = p;
+          y[j] = q;
+        }
+        v[u][1].set(y);
+      } else {
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          float p = x[2 * j], q = x[2 * j + 1];
+          turn_pair(p, q, w[j].x, w[j].y);
+          x[2 * j] = p;
+          x[2 * j + 1] = q;
+        }
+      }
+      v[u][0].set(x);
+      const bool second = hu >= a.heads[0];
+      char* o = a.y[second] + (second ? y1 + (hu - a.heads[0]) * a.y_sh[1] : y0 + hu * a.y_sh[0]) * SIZE;
+#pragma unroll
+      for (int e = 0; e < E; ++e) v[u][e].store(o + e * H2 * SIZE);
+    }
+    load(h + U * SLOTS);
+  }
+}
+
+template <int D, bool F32>
+hipError_t launch_d(const TurnArgs& a, int pairs, hipStream_t s) {
+  const unsigned grid = (unsigned)((a.tokens + kRopeRows - 1) / kRopeRows * a.head_parts);
+  if (pairs == SSBA_ROPE_HALVES)
+    k_rope<D, F32, true><<<grid, 256, 0, s>>>(a);
+  else
+    k_rope<D, F32, false><<<grid, 256, 0, s>>>(a);
+  return hipGetLastError();
+}
+
+}  // namespace
+
+hipError_t launch_rope_turn(const TurnArgs& a, int head_dim, int dtype, int pairs, hipStream_t s) {
+  if (head_dim == 64) return dtype == SSBA_DT_F32 ? launch_d<64, true>(a, pairs, s) : launch_d<64, false>(a, pairs, s);
+  return dtype == SSBA_DT_F32 ? launch_d<128, true>(a, pairs, s) : launch_d<128, false>(a, pairs, s);
+}
+
+}  // namespace ssba

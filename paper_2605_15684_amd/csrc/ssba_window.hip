@@ -1,0 +1,195 @@
+// Causal attention with a sliding window and sinks, forward
+// (include/ssba_window.h).
+//
+// A workgroup has 128 consecutive queries of one head, 32 a wave, and walks the
+// key tiles that some of them see: those with sinks, then those of the window.
+// K and V tiles are copied to the LDS while the tile before is computed.
+//   S^T = K Q^T, p = exp2(scale log2(e) S - m), O^T += V^T p^T
+// so that a lane has 16 keys of one query and the probabilities are the second
+// product's operand as they are.  m is raised only where a lane's sum of
+// probabilities passes 2^20, or a query has none yet; it may lag behind
+// otherwise, which is harmless in fp32 and bf16.
+//
+// A value that a query does not see must not reach it, and 0 times a NaN would:
+// where a result is not finite, the workgroup computes once more with the tiles
+// that some query sees in part taken row by row.
+#include <hip/hip_runtime.h>
+
+#include "ssba_common.h"
+#include "ssba_window_tiles.h"
+
+namespace ssba {
+namespace {
+
+constexpr float kMost = 1048576.f;   // a lane's sum of probabilities of a half tile: 2^20
+constexpr float kLn2 = 0.69314718055994530942f;
+
+template <class T>
+__global__ __launch_bounds__(256, 2) void k_window_forward(WindowArgs a) {
+  constexpr int NB = T::NB, NDB = T::NDB;
+  __shared__ __attribute__((aligned(16))) char kA[T::TILE];
+  __shared__ __attribute__((aligned(16))) char kB[T::TILE];
+  __shared__ __attribute__((aligned(16))) char vA[T::TILE];
+  __shared__ __attribute__((aligned(16))) char vB[T::TILE];
+  __shared__ int s_bad;
+  const int lane = threadIdx.x & 63, l32 = lane & 31, hw = lane >> 5;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+
+  WPlace p;
+  if (!place_query(a, lane, &p)) return;
+  const int w0 = p.r0 + 32 * wave, w1 = min(w0 + 31, p.len - 1);   // the wave's queries; w1 < w0: none
+  const int i = w0 + l32;
+  const bool in = i < p.len;
+
+  WRow<T> q;
+  {
+    const int64_t at = (int64_t)p.b * a.sq.b + (int64_t)p.h * a.sq.h + (int64_t)(p.begin + min(i, p.len - 1)) * a.sq.t;
+    q.load(static_cast<const char*>(a.q) + at * T::SIZE, hw);
+  }
+  WCopy<T> ck, cv;
+  ck.init(a.k, (int64_t)p.b * a.sk.b + (int64_t)p.kvh * a.sk.h + (int64_t)p.begin * a.sk.t, a.sk.t, wave, lane);
+  cv.init(a.v, (int64_t)p.b * a.sv.b + (int64_t)p.kvh * a.sv.h + (int64_t)p.begin * a.sv.t, a.sv.t, wave, lane);
+
+  // Tiles 0 .. n_sink - 1, then those of the window.
+  const int last = min(p.r0 + kWindowRows, p.len) - 1;
+  const int low = max(p.r0 - a.window + 1, 0) / T::ROWS;
+  const int n_sink = min((int)(((unsigned)min(a.sinks, last + 1) + T::ROWS - 1) / T::ROWS), low);
+  const int n = n_sink + last / T::ROWS - low + 1;
+  auto first_of = [&](int c) { return (c < n_sink ? c : low + c - n_sink) * T::ROWS; };
+
+  floatx16 o[NDB];
+  float m, l;
+  bool settled;
+  const float scale = a.scale_log2;
+
+  auto body = [&](int c, const char* kc, const char* vc, char* kn, char* vn, bool careful) {
+    if (!careful && c + 1 < n) {
+      ck.issue(first_of(c + 1), p.len, kn, wave);
+      cv.issue(first_of(c + 1), p.len, vn, wave);
+    }
+    const int j0 = first_of(c);
+    const bool none = j0 > w1 || (j0 + T::ROWS - 1 <= w0 - a.window && j0 >= a.sinks);
+    if (!none) {
+      const bool whole = j0 + T::ROWS - 1 <= w0 && (j0 + T::ROWS <= a.sinks || j0 > w0 + 31 - a.window);
+      floatx16 s[NB];
+#pragma unroll
+      for (int nb = 0; nb < NB; ++nb) {
+        s[nb] = floatx16{};
+        rows_product<T>(s[nb], kc + nb * T::HALF, q, lane);
+      }
+      if (!whole) {
+#pragma unroll
+        for (int nb = 0; nb < NB; ++nb)
+#pragma unroll
+          for (int e = 0; e < 16; ++e) {
+            const int j = j0 + 32 * nb + 8 * (e >> 2) + 4 * hw + (e & 3);
+            s[nb][e] = window_sees(i, j, a.window, a.sinks) ? s[nb][e] : -INFINITY;
+          }
+      }
+      floatx16 pr[NB];
+      float sum[NB];
+      auto probabilities = [&]() {
+        const float mu = m == -INFINITY ? 0.f : m;
+#pragma unroll
+        for (int nb = 0; nb < NB; ++nb) {
+          sum[nb] = 0.f;
+#pragma unroll
+          for (int e = 0; e < 16; ++e) {
+            pr[nb][e] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[nb][e], scale, -mu));
+            sum[nb] += pr[nb][e];
+          }
+        }
+      };
+      bool high = !settled;
+      if (settled) {
+        probabilities();
+#pragma unroll
+        for (int nb = 0; nb < NB; ++nb) high |= sum[nb] > kMost;
+      }
+      if (__builtin_amdgcn_ballot_w64(high)) {
+        float mx = -INFINITY;
+#pragma unroll
+        for (int nb = 0; nb < NB; ++nb)
+#pragma unroll
+          for (int e = 0; e < 16; ++e) mx = fmaxf(mx, s[nb][e]);
+        mx = fmaxf(mx, __shfl_xor(mx, 32)) * scale;
+        const float to = fmaxf(m, mx);
+        const float f = to > m ? __builtin_amdgcn_exp2f(m - to) : 1.f;
+        m = to;
+        l *= f;
+#pragma unroll
+        for (int db = 0; db < NDB; ++db) o[db] *= f;
+        settled = !__builtin_amdgcn_ballot_w64(m == -INFINITY && in);
+        probabilities();
+      }
+#pragma unroll
+      for (int nb = 0; nb < NB; ++nb) l += sum[nb];
+#pragma unroll
+      for (int nb = 0; nb < NB; ++nb) {
+        if (careful && !whole)
+          cols_product_seen<T>(o, vc + nb * T::HALF, pr[nb],
+                               reinterpret_cast<float*>((wave < T::TILE / 4096 ? kn : vn) + 4096 * (wave % (T::TILE / 4096))),
+                               lane, [&](int row) { return window_sees(i, j0 + 32 * nb + row, a.window, a.sinks); });
+        else
+          cols_product<T>(o, vc + nb * T::HALF, pr[nb], lane);
+      }
+    }
+    __builtin_amdgcn_s_waitcnt(kWaitVm0);
+    __syncthreads();
+  };
+
+  for (int pass = 0; pass < 2; ++pass) {
+    const bool careful = pass != 0;
+    m = -INFINITY;
+    l = 0.f;
+    settled = false;
+#pragma unroll
+    for (int db = 0; db < NDB; ++db) o[db] = floatx16{};
+    if (careful) {   // one tile at a time: the other buffers are room for the rows' weights
+      for (int c = 0; c < n; ++c) {
+        ck.issue(first_of(c), p.len, kA, wave);
+        cv.issue(first_of(c), p.len, vA, wave);
+        __builtin_amdgcn_s_waitcnt(kWaitVm0);
+        __syncthreads();
+        body(c, kA, vA, kB, vB, true);
+      }
+      break;
+    }
+    if (threadIdx.x == 0) s_bad = 0;
+    ck.issue(first_of(0), p.len, kA, wave);
+    cv.issue(first_of(0), p.len, vA, wave);
+    __builtin_amdgcn_s_waitcnt(kWaitVm0);
+    __syncthreads();
+    for (int c = 0; c < n; c += 2) {
+      body(c, kA, vA, kB, vB, false);
+      if (c + 1 < n) body(c + 1, kB, vB, kA, vA, false);
+    }
+    const bool bad = in && not_finite<NDB>(o);
+    if (__builtin_amdgcn_ballot_w64(bad) && lane == 0) s_bad = 1;
+    __syncthreads();
+    if (!s_bad) break;
+  }
+
+  l += __shfl_xor(l, 32);
+  if (!in) return;
+  const int64_t row = p.begin + i;
+  store_cols<T>(static_cast<char*>(a.o) + ((int64_t)p.b * a.so.b + (int64_t)p.h * a.so.h + row * a.so.t) * T::SIZE, o,
+                1.f / l, hw);
+  if (a.lse && hw == 0)
+    a.lse[((int64_t)p.b * a.heads + p.h) * a.seq + row] = (m + __builtin_amdgcn_logf(l)) * kLn2;
+}
+
+template <class T>
+hipError_t launch(const WindowArgs& a, hipStream_t s) {
+  k_window_forward<T><<<(unsigned)((int64_t)a.batch * a.heads * a.slots), 256, 0, s>>>(a);
+  return hipGetLastError();
+}
+
+}  // namespace
+
+hipError_t launch_window_forward(const WindowArgs& a, int head_dim, int dtype, hipStream_t s) {
+  if (head_dim == 64) return dtype == SSBA_DT_F32 ? launch<WTile<64, true>>(a, s) : launch<WTile<64, false>>(a, s);
+  return dtype == SSBA_DT_F32 ? launch<WTile<128, true>>(a, s) : launch<WTile<128, false>>(a, s);
+}
+
+}  // namespace ssba

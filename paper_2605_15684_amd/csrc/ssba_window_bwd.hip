@@ -1,0 +1,449 @@
+// Causal attention with a sliding window and sinks, backward
+// (include/ssba_window.h).
+//
+//   k_window_dq     a workgroup has 128 queries, 32 a wave, as the forward: it
+//                   forms delta = rowsum(do o) and the log-sum-exp in log2 units
+//                   of its rows (kept for the key side), then per key tile
+//                   S^T = K Q^T, P = exp2(c S - lse2), dS^T = P (V dO^T - delta),
+//                   dQ^T += K^T dS^T
+//   k_window_dkdv   a workgroup has 128 keys, 32 a wave, and walks the queries
+//                   that see some of them, head after head of the group:
+//                   S = Q K^T, dV^T += dO^T P, dS = P (dO V^T - delta),
+//                   dK^T += Q^T dS.  Keys that are sinks are seen by every later
+//                   query: their queries are cut into chunks, whose parts
+//   k_window_join   adds up in the chunks' order.
+//
+// What a query does not see must not reach it, nor it what it does not see, and
+// 0 times a NaN would: where a result is not finite, the workgroup computes once
+// more with the tiles that are seen in part taken row by row.
+#include <hip/hip_runtime.h>
+
+#include "ssba_common.h"
+#include "ssba_window_tiles.h"
+
+namespace ssba {
+namespace {
+
+// --------------------------------------------------------------------------
+// dQ
+// --------------------------------------------------------------------------
+template <class T>
+__global__ __launch_bounds__(256, T::F32 ? 1 : 2) void k_window_dq(WindowArgs a) {
+  constexpr int NB = T::NB, NDB = T::NDB;
+  __shared__ __attribute__((aligned(16))) char kA[T::TILE];
+  __shared__ __attribute__((aligned(16))) char kB[T::TILE];
+  __shared__ __attribute__((aligned(16))) char vA[T::TILE];
+  __shared__ __attribute__((aligned(16))) char vB[T::TILE];
+  __shared__ int s_bad;
+  const int lane = threadIdx.x & 63, l32 = lane & 31, hw = lane >> 5;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+
+  WPlace p;
+  if (!place_query(a, lane, &p)) return;
+  const int w0 = p.r0 + 32 * wave, w1 = min(w0 + 31, p.len - 1);
+  const int i = w0 + l32;
+  const bool in = i < p.len;
+  const int64_t row = p.begin + min(i, p.len - 1);
+
+  WRow<T> q, g;
+  float delta = 0.f, lse2;
+  {
+    q.load(static_cast<const char*>(a.q) + ((int64_t)p.b * a.sq.b + (int64_t)p.h * a.sq.h + row * a.sq.t) * T::SIZE, hw);
+    g.load(static_cast<const char*>(a.dout) + ((int64_t)p.b * a.sdo.b + (int64_t)p.h * a.sdo.h + row * a.sdo.t) * T::SIZE, hw);
+    WRow<T> o;
+    o.load(static_cast<const char*>(a.o) + ((int64_t)p.b * a.so.b + (int64_t)p.h * a.so.h + row * a.so.t) * T::SIZE, hw);
+#pragma unroll
+    for (int ks = 0; ks < T::NKS; ++ks)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        if constexpr (T::F32) {
+          delta = __builtin_fmaf(o.f[ks][e], g.f[ks][e], delta);
+        } else {
+          const uint32_t x = __float_as_uint(o.f[ks][e]), y = __float_as_uint(g.f[ks][e]);
+          delta = __builtin_fmaf(__uint_as_float(x << 16), __uint_as_float(y << 16), delta);
+          delta = __builtin_fmaf(__uint_as_float(x & 0xFFFF0000u), __uint_as_float(y & 0xFFFF0000u), delta);
+        }
+      }
+    delta += __shfl_xor(delta, 32);
+    const int64_t at = ((int64_t)p.b * a.heads + p.h) * a.seq + row;
+    lse2 = a.lse[at] * kLog2e;
+    if (in && hw == 0) {
+      a.delta[at] = delta;
+      a.lse2[at] = lse2;
+    }
+  }
+  WCopy<T> ck, cv;
+  ck.init(a.k, (int64_t)p.b * a.sk.b + (int64_t)p.kvh * a.sk.h + (int64_t)p.begin * a.sk.t, a.sk.t, wave, lane);
+  cv.init(a.v, (int64_t)p.b * a.sv.b + (int64_t)p.kvh * a.sv.h + (int64_t)p.begin * a.sv.t, a.sv.t, wave, lane);
+
+  const int last = min(p.r0 + kWindowRows, p.len) - 1;
+  const int low = max(p.r0 - a.window + 1, 0) / T::ROWS;
+  const int n_sink = min((int)(((unsigned)min(a.sinks, last + 1) + T::ROWS - 1) / T::ROWS), low);
+  const int n = n_sink + last / T::ROWS - low + 1;
+  auto first_of = [&](int c) { return (c < n_sink ? c : low + c - n_sink) * T::ROWS; };
+
+  floatx16 acc[NDB];
+  auto body = [&](int c, const char* kc, const char* vc, char* kn, char* vn, bool careful) {
+    if (!careful && c + 1 < n) {
+      ck.issue(first_of(c + 1), p.len, kn, wave);
+      cv.issue(first_of(c + 1), p.len, vn, wave);
+    }
+    const int j0 = first_of(c);
+    const bool none = j0 > w1 || (j0 + T::ROWS - 1 <= w0 - a.window && j0 >= a.sinks);
+    if (!none) {
+      const bool whole = j0 + T::ROWS - 1 <= w0 && (j0 + T::ROWS <= a.sinks || j0 > w0 + 31 - a.window);
+#pragma unroll
+      for (int nb = 0; nb < NB; ++nb) {
+        floatx16 s = {}, ds;
+#pragma unroll
+        for (int e = 0; e < 16; ++e) ds[e] = -delta;
+        rows_product<T>(s, kc + nb * T::HALF, q, lane);
+        rows_product<T>(ds, vc + nb * T::HALF, g, lane);
+#pragma unroll
+        for (int e = 0; e < 16; ++e) ds[e] *= __builtin_amdgcn_exp2f(__builtin_fmaf(s[e], a.scale_log2, -lse2));
+        if (!whole) {
+#pragma unroll
+          for (int e = 0; e < 16; ++e) {
+            const int j = j0 + 32 * nb + 8 * (e >> 2) + 4 * hw + (e & 3);
+            ds[e] = window_sees(i, j, a.window, a.sinks) ? ds[e] : 0.f;
+          }
+        }
+        if (careful && !whole)
+          cols_product_seen<T>(acc, kc + nb * T::HALF, ds,
+                               reinterpret_cast<float*>((wave < T::TILE / 4096 ? kn : vn) + 4096 * (wave % (T::TILE / 4096))),
+                               lane, [&](int r) { return window_sees(i, j0 + 32 * nb + r, a.window, a.sinks); });
+        else
+          cols_product<T>(acc, kc + nb * T::HALF, ds, lane);
+      }
+    }
+    __builtin_amdgcn_s_waitcnt(kWaitVm0);
+    __syncthreads();
+  };
+
+  for (int pass = 0; pass < 2; ++pass) {
+#pragma unroll
+    for (int db = 0; db < NDB; ++db) acc[db] = floatx16{};
+    if (pass) {   // one tile at a time: the other buffers are room for the rows' weights
+      for (int c = 0; c < n; ++c) {
+        ck.issue(first_of(c), p.len, kA, wave);
+        cv.issue(first_of(c), p.len, vA, wave);
+        __builtin_amdgcn_s_waitcnt(kWaitVm0);
+        __syncthreads();
+        body(c, kA, vA, kB, vB, true);
+      }
+      break;
+    }
+    if (threadIdx.x == 0) s_bad = 0;
+    ck.issue(first_of(0), p.len, kA, wave);
+    cv.issue(first_of(0), p.len, vA, wave);
+    __builtin_amdgcn_s_waitcnt(kWaitVm0);
+    __syncthreads();
+    for (int c = 0; c < n; c += 2) {
+      body(c, kA, vA, kB, vB, false);
+      if (c + 1 < n) body(c + 1, kB, vB, kA, vA, false);
+    }
+    const bool bad = in && not_finite<NDB>(acc);
+    if (__builtin_amdgcn_ballot_w64(bad) && lane == 0) s_bad = 1;
+    __syncthreads();
+    if (!s_bad) break;
+  }
+  if (in)
+    store_cols<T>(static_cast<char*>(a.dq) + ((int64_t)p.b * a.sdq.b + (int64_t)p.h * a.sdq.h + row * a.sdq.t) * T::SIZE,
+                  acc, a.scale, hw);
+}
+
+// --------------------------------------------------------------------------
+// dK, dV
+// --------------------------------------------------------------------------
+
+// What a workgroup of the key side does: 128 keys of a kv head and the queries
+// q0 .. q1 - 1 of its sequence.
+struct KeyPlace {
+  int b, kvh, begin, len, k0, q0, q1;
+  int64_t part;   // where its parts go, -1: it has all queries
+};
+
+// Slot of a sequence's chunk 0, as place_slot counts tiles.
+__device__ __forceinline__ int chunk_slot(const WindowArgs& a, int begin, int s) { return begin / a.chunk + s; }
+
+__device__ __forceinline__ bool place_keys(const WindowArgs& a, int lane, KeyPlace* p) {
+  const unsigned units = (unsigned)a.batch * a.kv_heads, cut = (unsigned)a.sink_tiles * a.chunk_slots;
+  const unsigned per = a.slots + cut;
+  unsigned id = blockIdx.x, unit, at;
+  if (a.spread) {
+    unit = id % units;
+    at = id / units;
+  } else {
+    id = xcd_order(id, units * per);
+    unit = id / per;
+    at = id % per;
+  }
+  p->b = unit / a.kv_heads;
+  p->kvh = unit % a.kv_heads;
+  p->part = -1;
+  if (at >= cut) {   // a tile of keys; its queries, or the first chunk of them, end with the window
+    WPlace w;
+    if (!place_slot(a, at - cut, lane, &w)) return false;
+    p->begin = w.begin;
+    p->len = w.len;
+    p->k0 = w.r0;
+    p->q0 = w.r0;
+    if (w.r0 < a.sinks) {
+      if (a.chunk_slots) return false;   // its chunks have workgroups of their own
+      p->q1 = w.len;
+    } else {
+      p->q1 = a.window < w.len - w.r0 - kWindowRows ? w.r0 + kWindowRows - 1 + a.window : w.len;
+    }
+    return true;
+  }
+  const int tile = at / a.chunk_slots, slot = at % a.chunk_slots;
+  int s = 0, c = slot;
+  if (a.cu) {
+    s = seq_of_slot(a.cu, a.seqs, a.seq, a.chunk, slot, lane);
+    seq_rows(a, s, &p->begin, &p->len);
+    c = slot - chunk_slot(a, p->begin, s);
+  } else {
+    p->begin = 0;
+    p->len = a.seq;
+  }
+  p->k0 = tile * kWindowRows;
+  if (c < 0 || p->k0 >= p->len) return false;
+  const int64_t q0 = p->k0 + (int64_t)c * a.chunk;
+  if (q0 >= p->len) return false;
+  p->q0 = (int)q0;
+  p->q1 = p->len - p->q0 < a.chunk ? p->len : p->q0 + a.chunk;
+  p->part = ((int64_t)unit * cut + at) * 2 * kWindowRows;
+  return true;
+}
+
+// 64 floats into the LDS, those from n on as 0.
+__device__ __forceinline__ void copy_values(const float* from, int n, float* dst, int lane) {
+  const __amdgpu_buffer_rsrc_t rs =
+      __builtin_amdgcn_make_buffer_rsrc(const_cast<float*>(from), (short)0, 4 * n, kRawBufferFlags);
+  __builtin_amdgcn_raw_ptr_buffer_load_lds(rs, (lds_void*)dst, 4, 4 * lane, 0, 0, 0);
+}
+
+template <class T>
+__global__ __launch_bounds__(256, 1) void k_window_dkdv(WindowArgs a) {
+  constexpr int NB = T::NB, NDB = T::NDB;
+  __shared__ __attribute__((aligned(16))) char qA[T::TILE];
+  __shared__ __attribute__((aligned(16))) char qB[T::TILE];
+  __shared__ __attribute__((aligned(16))) char gA[T::TILE];
+  __shared__ __attribute__((aligned(16))) char gB[T::TILE];
+  __shared__ __attribute__((aligned(16))) float rA[2][64];   // lse2, delta of the tile's rows
+  __shared__ __attribute__((aligned(16))) float rB[2][64];
+  __shared__ int s_bad;
+  const int lane = threadIdx.x & 63, l32 = lane & 31, hw = lane >> 5;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+
+  KeyPlace p;
+  if (!place_keys(a, lane, &p)) return;
+  const int w0 = p.k0 + 32 * wave, w1 = min(w0 + 31, p.len - 1);   // the wave's keys
+  const int j = w0 + l32;
+  const bool in = j < p.len;
+
+  WRow<T> k, v;
+  {
+    const int64_t row = p.begin + min(j, p.len - 1);
+    k.load(static_cast<const char*>(a.k) + ((int64_t)p.b * a.sk.b + (int64_t)p.kvh * a.sk.h + row * a.sk.t) * T::SIZE, hw);
+    v.load(static_cast<const char*>(a.v) + ((int64_t)p.b * a.sv.b + (int64_t)p.kvh * a.sv.h + row * a.sv.t) * T::SIZE, hw);
+  }
+  WCopy<T> cq, cg;
+  cq.init(a.q, (int64_t)p.b * a.sq.b + (int64_t)p.kvh * a.group * a.sq.h + (int64_t)p.begin * a.sq.t, a.sq.t, wave, lane);
+  cg.init(a.dout, (int64_t)p.b * a.sdo.b + (int64_t)p.kvh * a.group * a.sdo.h + (int64_t)p.begin * a.sdo.t, a.sdo.t, wave,
+          lane);
+  const char* q_base = cq.base;
+  const char* g_base = cg.base;
+  const float* l_base = a.lse2 + ((int64_t)p.b * a.heads + p.kvh * a.group) * a.seq + p.begin;
+  const float* d_base = a.delta + ((int64_t)p.b * a.heads + p.kvh * a.group) * a.seq + p.begin;
+
+  // Tiles of queries, head after head.
+  const int t0 = p.q0 / T::ROWS, per_head = (p.q1 - 1) / T::ROWS - t0 + 1, n = per_head * a.group;
+  int next_g = 0, next_t = 0;   // of the tile that is copied next
+  auto issue = [&](char* qd, char* gd, float (*rd)[64]) {
+    cq.base = q_base + (int64_t)next_g * a.sq.h * T::SIZE;
+    cg.base = g_base + (int64_t)next_g * a.sdo.h * T::SIZE;
+    const int i0 = (t0 + next_t) * T::ROWS;
+    cq.issue(i0, p.len, qd, wave);
+    cg.issue(i0, p.len, gd, wave);
+    if (wave < 2) {
+      const float* from = (wave ? d_base : l_base) + (int64_t)next_g * a.seq + i0;
+      copy_values(from, min(p.len - i0, T::ROWS), rd[wave], lane);
+    }
+    if (++next_t == per_head) {
+      next_t = 0;
+      ++next_g;
+    }
+  };
+
+  floatx16 dk[NDB], dv[NDB];
+  int at = 0;   // tile of the head
+  auto body = [&](int c, const char* qc, const char* gc, float (*rc)[64], char* qn, char* gn, float (*rn)[64], bool careful) {
+    if (!careful && c + 1 < n) issue(qn, gn, rn);
+    const int i0 = (t0 + at) * T::ROWS;
+    if (++at == per_head) at = 0;
+    const bool none = i0 + T::ROWS - 1 < w0 || (w1 <= i0 - a.window && w0 >= a.sinks) || w0 >= p.len;
+    if (!none) {
+      const bool whole = i0 >= max(w0 + 31, p.q0) && i0 + T::ROWS <= p.q1 &&
+                         (w0 + 32 <= a.sinks || w0 > i0 + T::ROWS - 1 - a.window);
+#pragma unroll
+      for (int nb = 0; nb < NB; ++nb) {
+        auto sees = [&](int r) {
+          const int i = i0 + 32 * nb + r;
+          return i >= p.q0 && i < p.q1 && window_sees(i, j, a.window, a.sinks);
+        };
+        floatx16 pr = {}, ds;
+#pragma unroll
+        for (int e = 0; e < 16; e += 4) {
+          const floatx4 d = *reinterpret_cast<const floatx4*>(&rc[1][32 * nb + 2 * e + 4 * hw]);
+#pragma unroll
+          for (int x = 0; x < 4; ++x) ds[e + x] = -d[x];
+        }
+        rows_product<T>(pr, qc + nb * T::HALF, k, lane);
+        rows_product<T>(ds, gc + nb * T::HALF, v, lane);
+#pragma unroll
+        for (int e = 0; e < 16; e += 4) {
+          const floatx4 l = *reinterpret_cast<const floatx4*>(&rc[0][32 * nb + 2 * e + 4 * hw]);
+#pragma unroll
+          for (int x = 0; x < 4; ++x) {
+            pr[e + x] = __builtin_amdgcn_exp2f(__builtin_fmaf(pr[e + x], a.scale_log2, -l[x]));
+            ds[e + x] *= pr[e + x];
+          }
+        }
+        if (!whole) {
+#pragma unroll
+          for (int e = 0; e < 16; ++e) {
+            const bool seen = sees(8 * (e >> 2) + 4 * hw + (e & 3));
+            pr[e] = seen ? pr[e] : 0.f;
+            ds[e] = seen ? ds[e] : 0.f;
+          }
+        }
+        if (careful && !whole) {
+          float* room = reinterpret_cast<float*>((wave < T::TILE / 4096 ? qn : gn) + 4096 * (wave % (T::TILE / 4096)));
+          cols_product_seen<T>(dv, gc + nb * T::HALF, pr, room, lane, sees);
+          cols_product_seen<T>(dk, qc + nb * T::HALF, ds, room, lane, sees);
+        } else {
+          cols_product<T>(dv, gc + nb * T::HALF, pr, lane);
+          cols_product<T>(dk, qc + nb * T::HALF, ds, lane);
+        }
+      }
+    }
+    __builtin_amdgcn_s_waitcnt(kWaitVm0);
+    __syncthreads();
+  };
+
+  for (int pass = 0; pass < 2; ++pass) {
+    next_g = next_t = at = 0;
+#pragma unroll
+    for (int db = 0; db < NDB; ++db) dk[db] = dv[db] = floatx16{};
+    if (pass) {   // one tile at a time: the other buffers are room for the rows' weights
+      for (int c = 0; c < n; ++c) {
+        issue(qA, gA, rA);
+        __builtin_amdgcn_s_waitcnt(kWaitVm0);
+        __syncthreads();
+        body(c, qA, gA, rA, qB, gB, rB, true);
+      }
+      break;
+    }
+    if (threadIdx.x == 0) s_bad = 0;
+    issue(qA, gA, rA);
+    __builtin_amdgcn_s_waitcnt(kWaitVm0);
+    __syncthreads();
+    for (int c = 0; c < n; c += 2) {
+      body(c, qA, gA, rA, qB, gB, rB, false);
+      if (c + 1 < n) body(c + 1, qB, gB, rB, qA, gA, rA, false);
+    }
+    const bool bad = in && (not_finite<NDB>(dk) || not_finite<NDB>(dv));
+    if (__builtin_amdgcn_ballot_w64(bad) && lane == 0) s_bad = 1;
+    __syncthreads();
+    if (!s_bad) break;
+  }
+  if (!in) return;
+  if (p.part >= 0) {
+    using P = WTile<T::D, true>;
+    char* to = reinterpret_cast<char*>(a.part + (p.part + 32 * wave + l32) * T::D);
+    store_cols<P>(to, dk, 1.f, hw);
+    store_cols<P>(to + (int64_t)kWindowRows * T::D * 4, dv, 1.f, hw);
+    return;
+  }
+  const int64_t row = p.begin + j;
+  store_cols<T>(static_cast<char*>(a.dk) + ((int64_t)p.b * a.sdk.b + (int64_t)p.kvh * a.sdk.h + row * a.sdk.t) * T::SIZE, dk,
+                a.scale, hw);
+  store_cols<T>(static_cast<char*>(a.dv) + ((int64_t)p.b * a.sdv.b + (int64_t)p.kvh * a.sdv.h + row * a.sdv.t) * T::SIZE, dv,
+                1.f, hw);
+}
+
+// Adds the chunks' parts of the sink tiles: a workgroup has the first chunk's
+// slot of a tile (the others' leave) and 2048 / D of its rows, 8 channels a
+// thread.
+template <class T>
+__global__ __launch_bounds__(256) void k_window_join(WindowArgs a) {
+  constexpr int D = T::D, ROWS = 2048 / D, PARTS = kWindowRows / ROWS;
+  const int lane = threadIdx.x & 63;
+  unsigned id = blockIdx.x;
+  const int sub = id % PARTS;
+  id /= PARTS;
+  const unsigned cut = (unsigned)a.sink_tiles * a.chunk_slots;
+  const unsigned unit = id / cut, at = id % cut;
+  const int tile = at / a.chunk_slots, slot = at % a.chunk_slots;
+  int begin = 0, len = a.seq;
+  if (a.cu) {
+    const int s = seq_of_slot(a.cu, a.seqs, a.seq, a.chunk, slot, lane);
+    seq_rows(a, s, &begin, &len);
+    if (slot != chunk_slot(a, begin, s)) return;
+  } else if (slot) {
+    return;
+  }
+  const int k0 = tile * kWindowRows, r = sub * ROWS + (int)threadIdx.x / (D / 8), ch = (int)threadIdx.x % (D / 8) * 8;
+  if (k0 + r >= len) return;
+  const int chunks = (len - k0 + a.chunk - 1) / a.chunk;
+  const float* from = a.part + (((int64_t)unit * cut + at) * 2 * kWindowRows + r) * D + ch;
+  const int b = unit / a.kv_heads, kvh = unit % a.kv_heads;
+  const int64_t row = begin + k0 + r;
+#pragma unroll
+  for (int which = 0; which < 2; ++which) {
+    float sum[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+    for (int c = 0; c < chunks; ++c) {
+      const float* x = from + ((int64_t)c * 2 + which) * kWindowRows * D;
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        const floatx4 y = *reinterpret_cast<const floatx4*>(x + 4 * h);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) sum[4 * h + e] += y[e];
+      }
+    }
+    const Strides& st = which ? a.sdv : a.sdk;
+    char* to = static_cast<char*>(which ? a.dv : a.dk) + ((int64_t)b * st.b + (int64_t)kvh * st.h + row * st.t + ch) * T::SIZE;
+    const float f = which ? 1.f : a.scale;
+    if constexpr (T::F32) {
+#pragma unroll
+      for (int h = 0; h < 2; ++h)
+        *reinterpret_cast<floatx4*>(to + 16 * h) =
+            floatx4{sum[4 * h] * f, sum[4 * h + 1] * f, sum[4 * h + 2] * f, sum[4 * h + 3] * f};
+    } else {
+      *reinterpret_cast<uint4*>(to) = make_uint4(pack2(sum[0] * f, sum[1] * f), pack2(sum[2] * f, sum[3] * f),
+                                                 pack2(sum[4] * f, sum[5] * f), pack2(sum[6] * f, sum[7] * f));
+    }
+  }
+}
+
+template <class T>
+hipError_t launch(const WindowArgs& a, hipStream_t s) {
+  const int64_t units = (int64_t)a.batch * a.kv_heads, cut = (int64_t)a.sink_tiles * a.chunk_slots;
+  k_window_dq<T><<<(unsigned)((int64_t)a.batch * a.heads * a.slots), 256, 0, s>>>(a);
+  hipError_t e = hipGetLastError();
+  if (e != hipSuccess) return e;
+  k_window_dkdv<T><<<(unsigned)(units * (a.slots + cut)), 256, 0, s>>>(a);
+  if ((e = hipGetLastError()) != hipSuccess || !cut) return e;
+  k_window_join<T><<<(unsigned)(units * cut * (kWindowRows * T::D / 2048)), 256, 0, s>>>(a);
+  return hipGetLastError();
+}
+
+}  // namespace
+
+hipError_t launch_window_backward(const WindowArgs& a, int head_dim, int dtype, hipStream_t s) {
+  if (head_dim == 64) return dtype == SSBA_DT_F32 ? launch<WTile<64, true>>(a, s) : launch<WTile<64, false>>(a, s);
+  return dtype == SSBA_DT_F32 ? launch<WTile<128, true>>(a, s) : launch<WTile<128, false>>(a, s);
+}
+
+}  // namespace ssba

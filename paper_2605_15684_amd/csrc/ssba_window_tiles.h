@@ -1,0 +1,274 @@
+// What the windowed attention's forward and backward share: which rows a
+// workgroup has, tiles of rows in the LDS, and the two kinds of product.
+//
+// A tile is 64 bf16 rows or 32 fp32 rows (the same bytes), in halves of 32 rows
+// that buffer_load ... lds fills.  Products are 32 x 32 by
+// v_mfma_f32_32x32x16_bf16 or v_mfma_f32_32x32x2_f32, whose result gives lane l
+// column l % 32 and rows 8 (e / 4) + 4 (l / 32) + e % 4, e = 0 .. 15:
+//   rows_product   (tile rows) x (the wave's 32 rows, in registers)
+//   cols_product   (tile columns)^T x (such a result, in registers)
+#pragma once
+
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+#include "ssba_tiles.h"
+#include "ssba_window_common.h"
+
+namespace ssba {
+
+typedef float floatx4 __attribute__((ext_vector_type(4)));
+
+template <int D_, bool F32_>
+struct WTile {
+  static constexpr int D = D_;
+  static constexpr bool F32 = F32_;
+  static constexpr int SIZE = F32 ? 4 : 2;
+  static constexpr int ROWB = D * SIZE;         // bytes of a row
+  static constexpr int CPR = ROWB / 16;         // 16-byte chunks of a row
+  static constexpr int NB = F32 ? 1 : 2;        // halves of a tile
+  static constexpr int ROWS = 32 * NB;
+  static constexpr int HALF = 32 * ROWB;
+  static constexpr int TILE = NB * HALF;        // 8 or 16 KB
+  static constexpr int KPI = 1024 / ROWB;       // rows of a copy instruction
+  static constexpr int NIW = TILE / 4096;       // copy instructions of each of 4 waves
+  static constexpr int NKS = F32 ? D / 8 : D / 16;   // 16-byte operands of a lane in a row
+  static constexpr int NDB = D / 32;
+};
+
+template <class T>
+__device__ __forceinline__ int wswz(int k, int c) {
+  if constexpr (T::F32)
+    return c ^ (k & 7);
+  else
+    return swz<T::D>(k, c);
+}
+
+// The rows of a workgroup: of sequence (batch b or packed), head h.
+struct WPlace {
+  int b, h, kvh, g;
+  int begin, len;   // the sequence's rows
+  int r0;           // first row of the workgroup in the sequence
+};
+
+// The sequence whose slots include slot x, where sequence s has the slots from
+// cu[s] / rows + s on (its tiles need no more of them than the next one's
+// first).  One wave, every lane gets the result.
+__device__ __forceinline__ int seq_of_slot(const int32_t* cu, int seqs, int seq, int rows, int x, int lane) {
+  int lo = 0, n = seqs;
+  while (n > 1) {
+    const int step = (n + 63) / 64;
+    const int s = lo + lane * step;
+    const bool in = lane * step < n && min(max(cu[min(s, seqs - 1)], 0), seq) / rows + s <= x;
+    const int c = __popcll(__builtin_amdgcn_ballot_w64(in));   // cu does not decrease: the first c lanes
+    lo += max(c - 1, 0) * step;
+    n = min(step, seqs - lo);
+  }
+  return lo;
+}
+
+__device__ __forceinline__ void seq_rows(const WindowArgs& a, int s, int* begin, int* len) {
+  *begin = min(max(a.cu[s], 0), a.seq);
+  *len = max(min(a.cu[s + 1], a.seq), *begin) - *begin;
+}
+
+// Workgroup `id` of `n` -> position in the launch's order.  The workgroups of
+// one XCD (id mod 8) are consecutive, so that the heads of a group and
+// neighbouring tiles read their rows from one L2.
+__device__ __forceinline__ unsigned xcd_order(unsigned id, unsigned n) {
+  const unsigned per = n / 8, rest = n % 8, x = id % 8;
+  return x * per + min(x, rest) + id / 8;
+}
+
+// Slot of a (batch, head) -> rows.  False: none.
+__device__ __forceinline__ bool place_slot(const WindowArgs& a, int slot, int lane, WPlace* p) {
+  if (a.cu) {
+    const int s = seq_of_slot(a.cu, a.seqs, a.seq, kWindowRows, slot, lane);
+    seq_rows(a, s, &p->begin, &p->len);
+    p->r0 = (slot - (p->begin / kWindowRows + s)) * kWindowRows;
+  } else {
+    p->begin = 0;
+    p->len = a.seq;
+    p->r0 = slot * kWindowRows;
+  }
+  return p->r0 >= 0 && p->r0 < p->len;
+}
+
+// The workgroup's rows and head, of launches with a workgroup for each slot and
+// query head.
+__device__ __forceinline__ bool place_query(const WindowArgs& a, int lane, WPlace* p) {
+  const unsigned units = (unsigned)a.batch * a.kv_heads;
+  unsigned unit, slot;
+  if (a.spread) {   // tiles of every head in turn, last ones (long ones) first
+    unsigned id = blockIdx.x;
+    unit = id % units;
+    id /= units;
+    p->g = id % a.group;
+    slot = a.slots - 1 - id / a.group;
+  } else {
+    unsigned id = xcd_order(blockIdx.x, gridDim.x);
+    p->g = id % a.group;
+    id /= a.group;
+    slot = a.slots - 1 - id % a.slots;
+    unit = id / a.slots;
+  }
+  p->b = unit / a.kv_heads;
+  p->kvh = unit % a.kv_heads;
+  p->h = p->kvh * a.group + p->g;
+  return place_slot(a, slot, lane, p);
+}
+
+// 1 KB from the `bytes` behind p, zeros for what is past them.
+__device__ __forceinline__ void copy_kb(const char* p, unsigned bytes, unsigned off, char* dst) {
+  const __amdgpu_buffer_rsrc_t rs =
+      __builtin_amdgcn_make_buffer_rsrc(const_cast<char*>(p), (short)0, (int)bytes, kRawBufferFlags);
+  __builtin_amdgcn_raw_ptr_buffer_load_lds(rs, (lds_void*)dst, 16, off, 0, 0, 0);
+}
+
+// This wave's copy of its part of a tile: rows row0 .. of a (b, h) slice, rows
+// from `end` on become 0.
+template <class T>
+struct WCopy {
+  const char* base;   // row 0
+  unsigned rowb;      // bytes from row to row
+  unsigned off[T::NIW];
+  __device__ __forceinline__ void init(const void* p, int64_t elem, int64_t st, int wave, int lane) {
+    base = static_cast<const char*>(p) + elem * T::SIZE;
+    rowb = (unsigned)st * T::SIZE;
+#pragma unroll
+    for (int m = 0; m < T::NIW; ++m) {
+      const int row = T::KPI * (T::NIW * wave + m) + lane / T::CPR;
+      off[m] = (unsigned)row * rowb + 16u * (unsigned)wswz<T>(row & 31, lane % T::CPR);
+    }
+  }
+  __device__ __forceinline__ void issue(int row0, int end, char* dst, int wave) const {
+    const int left = min(end - row0, T::ROWS);
+    const unsigned bytes = left > 0 ? (unsigned)(left - 1) * rowb + T::ROWB : 0u;
+#pragma unroll
+    for (int m = 0; m < T::NIW; ++m)
+      copy_kb(base + (int64_t)row0 * rowb, bytes, off[m], dst + 1024 * (T::NIW * wave + m));
+  }
+};
+
+// 16 bytes of a lane's row: the operands of rows_product, the lane's half of the
+// row (lane / 32).
+template <class T>
+struct WRow {
+  floatx4 f[T::NKS];
+  __device__ __forceinline__ void load(const char* row, int hw) {
+#pragma unroll
+    for (int ks = 0; ks < T::NKS; ++ks) f[ks] = *reinterpret_cast<const floatx4*>(row + 32 * ks + 16 * hw);
+  }
+};
+
+template <class T>
+__device__ __forceinline__ void rows_product(floatx16& acc, const char* half, const WRow<T>& b, int lane) {
+  const int k = lane & 31, hw = lane >> 5;
+#pragma unroll
+  for (int ks = 0; ks < T::NKS; ++ks) {
+    const floatx4 x = *reinterpret_cast<const floatx4*>(half + k * T::ROWB + 16 * wswz<T>(k, 2 * ks + hw));
+    if constexpr (T::F32) {
+#pragma unroll
+      for (int e = 0; e < 4; ++e) acc = __builtin_amdgcn_mfma_f32_32x32x2f32(x[e], b.f[ks][e], acc, 0, 0, 0);
+    } else {
+      acc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, x),
+                                                   __builtin_bit_cast(bf16x8, b.f[ks]), acc, 0, 0, 0);
+    }
+  }
+}
+
+// acc[db] += (channels 32 db .. of the half's rows)^T x, x a 32 x 32 result.
+template <class T>
+__device__ __forceinline__ void cols_product(floatx16 (&acc)[T::NDB], const char* half, const floatx16& x, int lane) {
+  if constexpr (T::F32) {
+    const int l32 = lane & 31, hw = lane >> 5;
+#pragma unroll
+    for (int j = 0; j < 16; ++j) {
+      const int row = 8 * (j >> 2) + 4 * hw + (j & 3);
+#pragma unroll
+      for (int db = 0; db < T::NDB; ++db) {
+        const float w = *reinterpret_cast<const float*>(half + row * T::ROWB + 16 * wswz<T>(row, 8 * db + (l32 >> 2)) +
+                                                        4 * (l32 & 3));
+        acc[db] = __builtin_amdgcn_mfma_f32_32x32x2f32(w, x[j], acc[db], 0, 0, 0);
+      }
+    }
+  } else {
+    uint32_t pk[8];
+#pragma unroll
+    for (int j = 0; j < 8; ++j) pk[j] = pack2(x[2 * j], x[2 * j + 1]);
+#pragma unroll
+    for (int ks = 0; ks < 2; ++ks) {
+      const bf16x8 pb = packed_frag(pk, ks);
+#pragma unroll
+      for (int db = 0; db < T::NDB; ++db)
+        acc[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, tr_frag<T::D>(half, lane, ks, db)), pb,
+                                                         acc[db], 0, 0, 0);
+    }
+  }
+}
+
+// The same where rows that a column does not see must not reach it whatever
+// they hold (0 times NaN): one row after another.  sees(row): this lane's
+// column sees it.  `room`: 4 KB of LDS of the wave.
+template <class T, class Sees>
+__device__ __forceinline__ void cols_product_seen(floatx16 (&acc)[T::NDB], const char* half, const floatx16& x,
+                                                            float* room, int lane, Sees sees) {
+  const int l32 = lane & 31, hw = lane >> 5;
+#pragma unroll
+  for (int j = 0; j < 16; ++j) room[j * 64 + lane] = x[j];
+  __builtin_amdgcn_wave_barrier();
+#pragma unroll 1
+  for (int row = 0; row < 32; ++row) {
+    const int j = 4 * (row >> 3) + (row & 3), from = (row >> 2) & 1;
+    const float w = room[j * 64 + l32 + 32 * from];
+    const bool in = sees(row);
+#pragma unroll
+    for (int db = 0; db < T::NDB; ++db)
+#pragma unroll
+      for (int e = 0; e < 16; ++e) {
+        const int ch = 32 * db + 8 * (e >> 2) + 4 * hw + (e & 3), at = ch * T::SIZE;
+        const char* p = half + row * T::ROWB + 16 * wswz<T>(row, at >> 4) + (at & 15);
+        float y;
+        if constexpr (T::F32)
+          y = *reinterpret_cast<const float*>(p);
+        else
+          y = __uint_as_float((uint32_t)*reinterpret_cast<const u16*>(p) << 16);
+        acc[db][e] = in ? __builtin_fmaf(w, y, acc[db][e]) : acc[db][e];
+      }
+  }
+  __builtin_amdgcn_wave_barrier();
+}
+
+// A result as rows of the lane's column: 4 consecutive channels at a time.
+template <class T>
+__device__ __forceinline__ void store_cols(char* row, const floatx16 (&acc)[T::NDB], float f, int hw) {
+#pragma unroll
+  for (int db = 0; db < T::NDB; ++db)
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      const float x[4] = {acc[db][4 * j] * f, acc[db][4 * j + 1] * f, acc[db][4 * j + 2] * f, acc[db][4 * j + 3] * f};
+      char* p = row + (32 * db + 8 * j + 4 * hw) * T::SIZE;
+      if constexpr (T::F32)
+        *reinterpret_cast<floatx4*>(p) = floatx4{x[0], x[1], x[2], x[3]};
+      else
+        *reinterpret_cast<uint2*>(p) = make_uint2(pack2(x[0], x[1]), pack2(x[2], x[3]));
+    }
+}
+
+// Some element is not finite.
+template <int N>
+__device__ __forceinline__ bool not_finite(const floatx16 (&acc)[N]) {
+  float t = 0.f;
+#pragma unroll
+  for (int i = 0; i < N; ++i)
+#pragma unroll
+    for (int e = 0; e < 16; ++e) t = __builtin_fmaf(acc[i][e], 0.f, t);
+  return t != 0.f;   // NaN
+}
+
+// Whether token i sees token j.
+__device__ __forceinline__ bool window_sees(int i, int j, int window, int sinks) {
+  return j <= i && (j < sinks || j > i - window);
+}
+
+}  // namespace ssba
