@@ -13,6 +13,8 @@
  *            each page (pooled keys) keeps `keep` pages per token and kv head
  *   attend   attention of new tokens over the whole sequence or the selected
  *            pages
+ *   attend_window   the same of a sliding window and the first tokens
+ *   attend_shared   the same of sequences that share a prefix, read once
  *   pages    reserve, fork, release, copy and compact
  *
  * Arrays of a cache (device memory, owned by the caller):
@@ -155,6 +157,46 @@ ssba_status ssba_cache_attend_workspace_size(const ssba_cache* c, const ssba_cac
 ssba_status ssba_cache_attend(const ssba_cache* c, int32_t layer, const ssba_cache_batch* b,
                               const ssba_cache_query* q, const void* query, const int32_t* lists, size_t lists_bytes,
                               void* o, void* scratch, size_t scratch_bytes, void* hip_stream);
+
+/* ssba_cache_attend without lists, of the first `sinks` tokens (>= 0) and the
+ * last `window` (>= 1): a token at position p sees the tokens j with j < sinks
+ * or j > p - window, of those that q->causal lets it see.  Only pages that hold
+ * such tokens are read, so a table's entries between the sinks and the window
+ * may name nothing, or pages that hold something else by now (a table that names
+ * the same pages again and again is a ring).  Precision as without lists; what
+ * a token does not see has no influence on its result, whatever it holds. */
+ssba_status ssba_cache_attend_window_workspace_size(const ssba_cache* c, const ssba_cache_batch* b,
+                                                    const ssba_cache_query* q, int32_t window, int32_t sinks,
+                                                    size_t* scratch_bytes);
+ssba_status ssba_cache_attend_window(const ssba_cache* c, int32_t layer, const ssba_cache_batch* b,
+                                     const ssba_cache_query* q, int32_t window, int32_t sinks, const void* query,
+                                     void* o, void* scratch, size_t scratch_bytes, void* hip_stream);
+
+/* Sequences that share a prefix, by groups of consecutive ones: those from
+ * first[g] to first[g+1] - 1 share their first pages[g] pages (complete ones, as
+ * ssba_pages_fork leaves them).  Device arrays of int32, read on the device;
+ * first must not decrease. */
+typedef struct ssba_cache_prefix {
+  int32_t groups;            /* 1 .. 65535                                       */
+  int32_t max_seqs;          /* at least the sequences of any group, 1 .. 65535; a group of more is attended by sequence */
+  int32_t max_len;           /* about the longest prefix in tokens (only how work is split goes by it) */
+  const int32_t* first;      /* [groups + 1]                                     */
+  const int32_t* pages;      /* [groups]                                         */
+} ssba_cache_prefix;
+
+/* ssba_cache_attend without lists, where the shared pages are read once for all
+ * sequences of a group.  They are those that the table names for the group's
+ * first sequence, the others' entries for them are not read; sequences of no
+ * group are attended as they are.  A prefix counts as far as it lies before the
+ * new tokens of every sequence of its group; the rest is read by sequence.
+ * Precision as without lists, where G * max_new also stands for the columns of a
+ * group, G times its new tokens.  `scratch` is always needed. */
+ssba_status ssba_cache_attend_shared_workspace_size(const ssba_cache* c, const ssba_cache_batch* b,
+                                                    const ssba_cache_query* q, const ssba_cache_prefix* x,
+                                                    size_t* scratch_bytes);
+ssba_status ssba_cache_attend_shared(const ssba_cache* c, int32_t layer, const ssba_cache_batch* b,
+                                     const ssba_cache_query* q, const ssba_cache_prefix* x, const void* query, void* o,
+                                     void* scratch, size_t scratch_bytes, void* hip_stream);
 
 /* ---- pages --------------------------------------------------------------
  * table [rows][max_pages], lens [rows], refs [pages]: how many table entries

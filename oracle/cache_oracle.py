@@ -313,3 +313,51 @@ def compact(pool, table, refs):
     ok = (table >= 0) & (table < len(refs))
     out[ok] = to[table[ok]]
     return out, new, live, len(movers)
+
+
+# ---- attention of a window and the first tokens, and of groups that share a prefix ----
+
+def attend_window(pool, layer, batch, q, page, window, sinks, causal=True, scale=None):
+    """As attend without lists, of the tokens j < sinks or j > p - window of a token at position p."""
+    table = batch[0]
+    rows, heads, d = q.shape
+    pages, kv = pool["k"].shape[1:3]
+    scale = d ** -0.5 if scale is None else scale
+    o = np.full((rows, heads, d), np.nan)
+    weight, spread = np.zeros((rows, heads, d)), np.zeros((rows, heads))
+    for s, (begin, n, start, held) in enumerate(sequences(batch, page, rows)):
+        for tok in range(n):
+            p, sees = start + tok, visible(start, held, tok, causal)
+            j = np.array([x for x in range(sees) if (x < sinks or x > p - window) and
+                          0 <= int(table[s, x // page]) < pages], dtype=np.int64)
+            for h in range(kv):
+                keys, values = (_gather(pool, layer, table[s], j, h, w, page, d) for w in (0, 1))
+                for g in range(heads // kv):
+                    r, head = begin + tok, h * (heads // kv) + g
+                    if not len(j):
+                        o[r, head] = 0.0
+                        continue
+                    w = scale * (keys @ q[r, head])
+                    e = np.exp(w - w.max())
+                    e /= e.sum()
+                    o[r, head] = e @ values
+                    weight[r, head] = e @ np.abs(values)
+                    spread[r, head] = abs(scale) * (np.abs(keys) @ np.abs(q[r, head])).max()
+    return o, weight, spread
+
+
+def _gather(pool, layer, row, j, h, which, page, d):
+    out = np.zeros((len(j), d))
+    for lp in np.unique(j // page):
+        at = j // page == lp
+        out[at] = rows_of(pool, layer, int(row[lp]), h, which, page, d)[j[at] % page]
+    return out
+
+
+def shared_table(batch, first, pages):
+    """The table with the shared pages of every group's first sequence in the rows of its others."""
+    table = batch[0].copy()
+    for g in range(len(pages)):
+        for s in range(first[g], first[g + 1]):
+            table[s, :pages[g]] = table[first[g], :pages[g]]
+    return (table,) + tuple(batch[1:])

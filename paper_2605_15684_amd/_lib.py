@@ -39,7 +39,9 @@ EXPORTS = ("ssba_abi_version", "ssba_status_str", "ssba_workspace_size", "ssba_b
            "ssba_cache_attend_workspace_size", "ssba_cache_attend", "ssba_pages_workspace_size",
            "ssba_pages_reserve", "ssba_pages_fork", "ssba_pages_release", "ssba_pages_compact",
            "ssba_pages_copy", "ssba_rope_rotate", "ssba_window_forward",
-           "ssba_window_backward_workspace_size", "ssba_window_backward")
+           "ssba_window_backward_workspace_size", "ssba_window_backward",
+           "ssba_cache_attend_window_workspace_size", "ssba_cache_attend_window",
+           "ssba_cache_attend_shared_workspace_size", "ssba_cache_attend_shared")
 
 # Byte count that the binding passes for a buffer it cannot size (None).
 UNSIZED = ctypes.c_size_t(-1).value
@@ -89,6 +91,11 @@ class CacheQuery(ctypes.Structure):         # ssba_cache_query
 class CachePages(ctypes.Structure):         # ssba_pages
     _fields_ = [("rows", ctypes.c_int32), ("max_pages", ctypes.c_int32), ("table", ctypes.c_void_p),
                 ("lens", ctypes.c_void_p), ("refs", ctypes.c_void_p)]
+
+
+class CachePrefix(ctypes.Structure):        # ssba_cache_prefix
+    _fields_ = [("groups", ctypes.c_int32), ("max_seqs", ctypes.c_int32), ("max_len", ctypes.c_int32),
+                ("first", ctypes.c_void_p), ("pages", ctypes.c_void_p)]
 
 
 class RopeDesc(ctypes.Structure):           # ssba_rope
@@ -183,7 +190,7 @@ def load(path: str = None) -> ctypes.CDLL:
     lib.ssba_probe_mfma.argtypes = [ctypes.c_int32, ctypes.c_int32, vp, vp]
     i32, i64 = ctypes.c_int32, ctypes.c_int64
     cp, bp, qp, pp = (ctypes.POINTER(t) for t in (CacheDesc, CacheBatch, CacheQuery, CachePages))
-    rp, tp, wp, gp = (ctypes.POINTER(t) for t in (RopeDesc, RopeTensor, WindowDesc, WindowGrads))
+    rp, tp, wp, gp, xp = (ctypes.POINTER(t) for t in (RopeDesc, RopeTensor, WindowDesc, WindowGrads, CachePrefix))
     for name, args in (("ssba_build_index_ex", [dp, vp, vp, vp, sz, vp, sz, vp]),
                        ("ssba_forward_ex", [dp, vp, vp, vp, vp, sz, vp, vp]),
                        ("ssba_forward_topk_ex", [dp, vp, vp, vp, vp, sz, vp, sz, vp, vp]),
@@ -209,6 +216,10 @@ def load(path: str = None) -> ctypes.CDLL:
                        ("ssba_pages_release", [cp, pp, i32, vp, vp, vp, sz, vp]),
                        ("ssba_pages_compact", [cp, pp, vp, vp, vp, vp, sz, vp]),
                        ("ssba_pages_copy", [cp, cp, i32, vp, vp, vp]),
+                       ("ssba_cache_attend_window_workspace_size", [cp, bp, qp, i32, i32, ctypes.POINTER(sz)]),
+                       ("ssba_cache_attend_window", [cp, i32, bp, qp, i32, i32, vp, vp, vp, sz, vp]),
+                       ("ssba_cache_attend_shared_workspace_size", [cp, bp, qp, xp, ctypes.POINTER(sz)]),
+                       ("ssba_cache_attend_shared", [cp, i32, bp, qp, xp, vp, vp, vp, sz, vp]),
                        ("ssba_rope_rotate", [rp, i32, i32, i32, i32, vp, i64, i64, i32, tp, vp]),
                        ("ssba_window_forward", [wp, vp, vp, vp, vp, vp, vp]),
                        ("ssba_window_backward_workspace_size", [wp, ctypes.POINTER(sz)]),

@@ -14,6 +14,9 @@ Importing fails if the library is not built.
     o = cache.attend(pool, layer, batch, q)                 # [tokens, heads, D]
     lists = cache.select(pool, layer, batch, q, keep=32)    # or: the best 32 pages of each token
     o = cache.attend(pool, layer, batch, q, lists=lists)
+    o = cache.attend_window(pool, layer, batch, q, window=1024, sinks=4)     # or: the last 1024 tokens and the first 4
+    prefix = cache.Prefix(first, pages)                     # or, of sequences that share their first pages: reading
+    o = cache.attend_shared(pool, layer, batch, prefix, q)  # these once
 """
 from __future__ import annotations
 
@@ -26,8 +29,8 @@ from . import _lib
 
 _L = _lib.load()   # fail loudly at import if the HIP library is missing
 
-__all__ = ["PagedCache", "Batch", "alloc", "alloc_rows", "append", "select", "attend", "reserve", "fork", "release",
-           "compact", "copy_pages", "SsbaError"]
+__all__ = ["PagedCache", "Batch", "Prefix", "alloc", "alloc_rows", "append", "select", "attend", "attend_window",
+           "attend_shared", "reserve", "fork", "release", "compact", "copy_pages", "SsbaError"]
 
 SsbaError = _lib.SsbaError
 E4M3 = torch.float8_e4m3fn
@@ -128,6 +131,35 @@ class Batch:
     def desc(self, rows: int) -> _lib.CacheBatch:
         seqs, max_pages, new, length, table, lens, cu = self._desc
         return _lib.CacheBatch(seqs, max_pages, rows, new, length, table, lens, cu)
+
+
+class Prefix:
+    """Groups of consecutive sequences that share their first pages: sequences first[g] .. first[g+1]-1 share pages[g]
+    complete pages (first int32 [groups + 1], pages int32 [groups]), named by the table for the first of them.
+    max_seqs: at least the sequences of any group (None: those of the batch); max_len: about the longest prefix in
+    tokens (work is split by it; results are not)."""
+
+    __slots__ = ("first", "pages", "index", "max_seqs", "_desc")
+
+    def __init__(self, first: torch.Tensor, pages: torch.Tensor, max_seqs: Optional[int] = None,
+                 max_len: Optional[int] = None):
+        index = _gpu_of(first, 1, "first")
+        _check(first, None, torch.int32, index, "first")
+        groups = first.shape[0] - 1
+        if groups < 1:
+            raise ValueError("first: expected [groups + 1]")
+        _check(pages, (groups,), torch.int32, index, "pages")
+        max_len = None if max_len is None else int(max_len)
+        max_seqs = None if max_seqs is None else int(max_seqs)
+        _int32("first, max_seqs or max_len", groups, max_seqs or 0, max_len or 0)
+        if max_seqs is not None and max_seqs < 1 or max_len is not None and max_len < 0:
+            raise ValueError("max_seqs must be 1 or more, max_len 0 or more")
+        self.first, self.pages, self.index, self.max_seqs = first, pages, index, max_seqs
+        self._desc = (groups, max_len, first.data_ptr(), pages.data_ptr())
+
+    def desc(self, seqs: int, tokens: int) -> _lib.CachePrefix:
+        groups, max_len, first, pages = self._desc
+        return _lib.CachePrefix(groups, self.max_seqs or seqs, tokens if max_len is None else max_len, first, pages)
 
 
 def alloc(layers: int, pages: int, kv_heads: int, head_dim: int, page: int = 64, device="cuda") -> PagedCache:
@@ -264,6 +296,59 @@ def attend(pool: PagedCache, layer: int, batch: Batch, q: torch.Tensor, *, lists
                "ssba_cache_attend_workspace_size")
     alive, at, have = _scratch(size.value, scratch, pool)
     _call(pool, _L.ssba_cache_attend, "ssba_cache_attend", pool.desc, layer, b, desc, q.data_ptr(), lp, lb,
+          out.data_ptr(), at, have)
+    return out
+
+
+def _query(pool: PagedCache, layer: int, batch: Batch, q, causal: bool, scale, out):
+    """What attention without lists takes: (output, batch, query)."""
+    _same_device(pool, batch)
+    qs = _packed(q, None, None, pool, None, "q")
+    rows, heads, d = q.shape
+    _int32("layer", layer)
+    if out is None:
+        out = torch.empty_like(q, memory_format=torch.contiguous_format)
+        os = (heads * d, d)
+    else:
+        os = _packed(out, rows, heads, pool, q.dtype, "out")
+    return out, batch.desc(rows), _lib.CacheQuery(heads, _DTYPES[q.dtype], 1 if causal else 0, 0, 0, 0,
+                                                  _softmax_scale(scale), *qs, *os)
+
+
+def attend_window(pool: PagedCache, layer: int, batch: Batch, q: torch.Tensor, *, window: int, sinks: int = 0,
+                  causal: bool = True, scale: Optional[float] = None, out: Optional[torch.Tensor] = None,
+                  scratch: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """As `attend` without lists, of the last `window` tokens and the first `sinks`: a token at position p sees j <
+    sinks and j > p - window, of what `causal` lets it see.  Pages between the two are not read.  (window.forward:
+    the form for rows that are not cached, with gradients.)"""
+    out, b, desc = _query(pool, layer, batch, q, causal, scale, out)
+    window, sinks = int(window), int(sinks)
+    _int32("window or sinks", window, sinks)
+    if window < 1 or sinks < 0:
+        raise ValueError("window must be 1 or more, sinks 0 or more")
+    size = ctypes.c_size_t(0)
+    _lib.check(_L.ssba_cache_attend_window_workspace_size(pool.desc, b, desc, window, sinks, size),
+               "ssba_cache_attend_window_workspace_size")
+    alive, at, have = _scratch(size.value, scratch, pool)
+    _call(pool, _L.ssba_cache_attend_window, "ssba_cache_attend_window", pool.desc, layer, b, desc, window, sinks,
+          q.data_ptr(), out.data_ptr(), at, have)
+    return out
+
+
+def attend_shared(pool: PagedCache, layer: int, batch: Batch, prefix: Prefix, q: torch.Tensor, *, causal: bool = True,
+                  scale: Optional[float] = None, out: Optional[torch.Tensor] = None,
+                  scratch: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """As `attend` without lists, of sequences that share their first pages by groups: these are read once for a
+    group, whatever the number of its sequences."""
+    out, b, desc = _query(pool, layer, batch, q, causal, scale, out)
+    if not isinstance(prefix, Prefix) or prefix.index != pool.index:
+        raise ValueError("prefix: expected a cache.Prefix on the cache's device")
+    x = prefix.desc(*batch.table.shape[:1], batch.table.shape[1] * pool.page)
+    size = ctypes.c_size_t(0)
+    _lib.check(_L.ssba_cache_attend_shared_workspace_size(pool.desc, b, desc, x, size),
+               "ssba_cache_attend_shared_workspace_size")
+    alive, at, have = _scratch(size.value, scratch, pool)
+    _call(pool, _L.ssba_cache_attend_shared, "ssba_cache_attend_shared", pool.desc, layer, b, desc, x, q.data_ptr(),
           out.data_ptr(), at, have)
     return out
 

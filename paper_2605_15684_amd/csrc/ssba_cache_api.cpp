@@ -160,12 +160,12 @@ size_t select_scratch(const ssba_cache* c, const ssba_cache_batch* b, const ssba
 
 // Items are independent (sequence or row, kv head, column tile); one workgroup
 // each, or several that share the item's keys where there are few items.
-AttendPlan plan(const ssba_cache* c, const ssba_cache_batch* b, const ssba_cache_query* q, bool listed) {
+// units: sequences, or groups of them, of `cols` columns and `keys` keys.
+AttendPlan plan(const ssba_cache* c, const ssba_cache_batch* b, const ssba_cache_query* q, bool listed, int64_t units,
+                int64_t cols, int64_t keys) {
   AttendPlan p;
-  const int64_t group = q->heads / c->kv_heads;
-  const int64_t cols = std::max<int64_t>(1, listed ? group : group * b->max_new);
+  std::memset(&p, 0, sizeof(p));
   const bool f32 = q->dtype == SSBA_DT_F32;
-  const int64_t keys = listed ? std::min<int64_t>((int64_t)q->keep * c->page, long_of(c, b)) : long_of(c, b);
   p.splits = p.tiles = 1;
   p.threads = 256;
   if (listed) {
@@ -180,7 +180,7 @@ AttendPlan plan(const ssba_cache* c, const ssba_cache_batch* b, const ssba_cache
     while (p.tiles < (f32 ? 2 : 16) && cols > 16 * p.tiles) p.tiles *= 2;
     if (p.tiles >= 4) p.threads = 512;
     p.col_tiles = (int)ceil_div(cols, 16 * p.tiles);
-    p.items = (int64_t)b->seqs * c->kv_heads * p.col_tiles;
+    p.items = units * c->kv_heads * p.col_tiles;
   }
   const int64_t items = std::max<int64_t>(p.items, 1);
   if (p.tiles >= 4) {
@@ -219,6 +219,43 @@ AttendPlan plan(const ssba_cache* c, const ssba_cache_batch* b, const ssba_cache
   return p;
 }
 
+AttendPlan plan(const ssba_cache* c, const ssba_cache_batch* b, const ssba_cache_query* q, bool listed) {
+  const int64_t group = q->heads / c->kv_heads;
+  return plan(c, b, q, listed, b->seqs, std::max<int64_t>(1, listed ? group : group * b->max_new),
+              listed ? std::min<int64_t>((int64_t)q->keep * c->page, long_of(c, b)) : long_of(c, b));
+}
+
+// A window's keys: of the first token to the last one's, and the sinks.
+AttendPlan plan_window(const ssba_cache* c, const ssba_cache_batch* b, const ssba_cache_query* q, int32_t window,
+                       int32_t sinks) {
+  const int64_t cols = std::max<int64_t>(1, (int64_t)(q->heads / c->kv_heads) * b->max_new);
+  AttendPlan p = plan(c, b, q, false, b->seqs, cols,
+                      std::min<int64_t>((int64_t)window + sinks + b->max_new, std::max<int64_t>(1, long_of(c, b))));
+  p.kind = ssba::kAttendWindow;
+  return p;
+}
+
+// Columns of a group of sequences that share a prefix.
+int64_t shared_cols(const ssba_cache* c, const ssba_cache_batch* b, const ssba_cache_query* q, const ssba_cache_prefix* x) {
+  return (int64_t)(q->heads / c->kv_heads) * std::min<int64_t>((int64_t)b->max_new * x->max_seqs, b->rows);
+}
+
+AttendPlan plan_shared(const ssba_cache* c, const ssba_cache_batch* b, const ssba_cache_query* q,
+                       const ssba_cache_prefix* x) {
+  const int64_t most = long_of(c, b), prefix = std::min<int64_t>(x->max_len, most);
+  const AttendPlan f = plan(c, b, q, false, x->groups, std::max<int64_t>(1, shared_cols(c, b, q, x)),
+                            std::max<int64_t>(1, prefix));
+  const int64_t cols = std::max<int64_t>(1, (int64_t)(q->heads / c->kv_heads) * b->max_new);
+  AttendPlan p = plan(c, b, q, false, b->seqs, cols, std::max<int64_t>(1, most - prefix));
+  p.kind = ssba::kAttendShared;
+  p.prefix_tiles = f.tiles;
+  p.prefix_threads = f.threads;
+  p.prefix_col_tiles = f.col_tiles;
+  p.prefix_splits = f.splits;
+  p.prefix_items = f.items;
+  return p;
+}
+
 // Columns of every part of a split launch.
 size_t part_columns(const AttendPlan& p) { return p.splits == 1 ? 0 : (size_t)p.items * p.splits * p.tiles * 16; }
 
@@ -226,7 +263,65 @@ size_t attend_scratch(const ssba_cache* c, const AttendPlan& p) {
   return part_columns(p) * (c->head_dim + 2) * sizeof(float);
 }
 
+// Columns of the parts of a launch of shared prefixes: those of the rests, then the prefixes'.
+size_t rest_columns(const AttendPlan& p) { return (size_t)p.items * p.splits * p.tiles * 16; }
+size_t prefix_columns(const AttendPlan& p) { return (size_t)p.prefix_items * p.prefix_splits * p.prefix_tiles * 16; }
+
+size_t shared_scratch(const ssba_cache* c, const AttendPlan& p) {
+  return (rest_columns(p) + prefix_columns(p)) * (c->head_dim + 2) * sizeof(float);
+}
+
 bool too_many(int64_t groups) { return groups > ssba::kMaxGroups256; }
+
+ssba_status check_prefix(const ssba_cache* c, const ssba_cache_batch* b, const ssba_cache_query* q,
+                         const ssba_cache_prefix* x) {
+  if (!x) return SSBA_ERR_ARG;
+  if (x->groups < 1 || x->max_seqs < 1 || x->max_len < 0) return SSBA_ERR_SHAPE;
+  if (x->groups > 65535 || x->max_seqs > 65535) return SSBA_ERR_UNSUPPORTED;
+  if (shared_cols(c, b, q, x) > kMaxTokens) return SSBA_ERR_UNSUPPORTED;
+  return SSBA_OK;
+}
+
+// What the calls of the attention have in common: checks, and the arguments that go by the descriptors alone.
+ssba_status attend_args(const ssba_cache* c, int32_t layer, const ssba_cache_batch* b, const ssba_cache_query* q,
+                        bool listed, AttendArgs* a) {
+  ssba_status st = check_shape(c);
+  if (st != SSBA_OK) return st;
+  if ((st = check_batch(c, b)) != SSBA_OK || (st = check_query(c, b, q)) != SSBA_OK) return st;
+  if (layer < 0 || layer >= c->layers) return SSBA_ERR_ARG;
+  if (listed && q->keep < 1) return SSBA_ERR_ARG;
+  std::memset(a, 0, sizeof(*a));
+  a->q_st = q->q_stride_t;
+  a->q_sh = q->q_stride_h;
+  a->o_st = q->o_stride_t;
+  a->o_sh = q->o_stride_h;
+  if ((st = strides_of(q->dtype, q->heads, c->head_dim, b->rows, &a->q_st, &a->q_sh)) != SSBA_OK) return st;
+  if ((st = strides_of(q->dtype, q->heads, c->head_dim, b->rows, &a->o_st, &a->o_sh)) != SSBA_OK) return st;
+  if ((st = check_arrays(c)) != SSBA_OK || (st = check_batch_arrays(b)) != SSBA_OK) return st;
+  a->c = view(c, layer);
+  a->b = view(b);
+  const float scale = q->softmax_scale > 0.f ? q->softmax_scale : 1.0f / std::sqrt((float)c->head_dim);
+  a->scale_log2 = scale * kLog2e;
+  a->group = q->heads / c->kv_heads;
+  a->causal = q->causal;
+  a->keep = q->keep;
+  return SSBA_OK;
+}
+
+bool attend_arrays(const ssba_cache_query* q, const void* query, const void* o) {
+  const size_t al = q->dtype == SSBA_DT_BF16 ? 16 : 4;
+  return query && o && aligned(query, al) && aligned(o, al);
+}
+
+ssba_status attend(AttendArgs& a, const AttendPlan& p, const ssba_cache_query* q, const void* query, void* o,
+                   void* stream) {
+  a.q = query;
+  a.o = o;
+  a.col_tiles = p.col_tiles;
+  a.splits = p.splits;
+  return ssba::launch_cache_attend(a, p, q->dtype, static_cast<hipStream_t>(stream)) == hipSuccess ? SSBA_OK
+                                                                                                   : SSBA_ERR_HIP;
+}
 
 }  // namespace
 
@@ -317,45 +412,92 @@ ssba_status ssba_cache_attend_workspace_size(const ssba_cache* c, const ssba_cac
 ssba_status ssba_cache_attend(const ssba_cache* c, int32_t layer, const ssba_cache_batch* b,
                               const ssba_cache_query* q, const void* query, const int32_t* lists, size_t lists_bytes,
                               void* o, void* scratch, size_t scratch_bytes, void* stream) {
-  ssba_status st = check_shape(c);
-  if (st != SSBA_OK) return st;
-  if ((st = check_batch(c, b)) != SSBA_OK || (st = check_query(c, b, q)) != SSBA_OK) return st;
-  if (layer < 0 || layer >= c->layers) return SSBA_ERR_ARG;
-  if (lists && q->keep < 1) return SSBA_ERR_ARG;
   AttendArgs a;
-  std::memset(&a, 0, sizeof(a));
-  a.q_st = q->q_stride_t;
-  a.q_sh = q->q_stride_h;
-  a.o_st = q->o_stride_t;
-  a.o_sh = q->o_stride_h;
-  if ((st = strides_of(q->dtype, q->heads, c->head_dim, b->rows, &a.q_st, &a.q_sh)) != SSBA_OK) return st;
-  if ((st = strides_of(q->dtype, q->heads, c->head_dim, b->rows, &a.o_st, &a.o_sh)) != SSBA_OK) return st;
-  if ((st = check_arrays(c)) != SSBA_OK || (st = check_batch_arrays(b)) != SSBA_OK) return st;
+  const ssba_status st = attend_args(c, layer, b, q, lists != nullptr, &a);
+  if (st != SSBA_OK) return st;
   if (b->rows == 0 || b->max_new == 0) return SSBA_OK;
-  const size_t al = q->dtype == SSBA_DT_BF16 ? 16 : 4;
-  if (!query || !o || !aligned(query, al) || !aligned(o, al) || !aligned(lists, 4)) return SSBA_ERR_ARG;
+  if (!attend_arrays(q, query, o) || !aligned(lists, 4)) return SSBA_ERR_ARG;
   const AttendPlan p = plan(c, b, q, lists != nullptr);
   const size_t need = attend_scratch(c, p);
   if (need && (!scratch || !aligned(scratch, 16))) return SSBA_ERR_ARG;
   if (scratch_bytes < need || (lists && lists_bytes < (size_t)4 * b->rows * c->kv_heads * (1 + (size_t)q->keep)))
     return SSBA_ERR_WORKSPACE;
   if (too_many(p.items * p.splits * 4) || too_many(p.items * p.tiles * 4)) return SSBA_ERR_UNSUPPORTED;
-  a.c = view(c, layer);
-  a.b = view(b);
-  a.q = query;
-  a.o = o;
   a.lists = lists;
   a.part = static_cast<float*>(scratch);
   a.part_ml = need ? a.part + part_columns(p) * c->head_dim : nullptr;
-  const float scale = q->softmax_scale > 0.f ? q->softmax_scale : 1.0f / std::sqrt((float)c->head_dim);
-  a.scale_log2 = scale * kLog2e;
-  a.group = q->heads / c->kv_heads;
-  a.causal = q->causal;
-  a.keep = q->keep;
-  a.col_tiles = p.col_tiles;
-  a.splits = p.splits;
-  return ssba::launch_cache_attend(a, p, q->dtype, static_cast<hipStream_t>(stream)) == hipSuccess ? SSBA_OK
-                                                                                                   : SSBA_ERR_HIP;
+  return attend(a, p, q, query, o, stream);
+}
+
+ssba_status ssba_cache_attend_window_workspace_size(const ssba_cache* c, const ssba_cache_batch* b,
+                                                    const ssba_cache_query* q, int32_t window, int32_t sinks,
+                                                    size_t* scratch_bytes) {
+  ssba_status st = check_shape(c);
+  if (st != SSBA_OK) return st;
+  if ((st = check_batch(c, b)) != SSBA_OK || (st = check_query(c, b, q)) != SSBA_OK) return st;
+  if (window < 1 || sinks < 0) return SSBA_ERR_ARG;
+  if (scratch_bytes) *scratch_bytes = attend_scratch(c, plan_window(c, b, q, window, sinks));
+  return SSBA_OK;
+}
+
+ssba_status ssba_cache_attend_window(const ssba_cache* c, int32_t layer, const ssba_cache_batch* b,
+                                     const ssba_cache_query* q, int32_t window, int32_t sinks, const void* query,
+                                     void* o, void* scratch, size_t scratch_bytes, void* stream) {
+  AttendArgs a;
+  const ssba_status st = attend_args(c, layer, b, q, false, &a);
+  if (st != SSBA_OK) return st;
+  if (window < 1 || sinks < 0) return SSBA_ERR_ARG;
+  if (b->rows == 0 || b->max_new == 0) return SSBA_OK;
+  if (!attend_arrays(q, query, o)) return SSBA_ERR_ARG;
+  const AttendPlan p = plan_window(c, b, q, window, sinks);
+  const size_t need = attend_scratch(c, p);
+  if (need && (!scratch || !aligned(scratch, 16))) return SSBA_ERR_ARG;
+  if (scratch_bytes < need) return SSBA_ERR_WORKSPACE;
+  if (too_many(p.items * p.splits * 4) || too_many(p.items * p.tiles * 4)) return SSBA_ERR_UNSUPPORTED;
+  a.window = (int)std::min<int64_t>(window, kMaxTokens);   // a sequence holds no more
+  a.sinks = (int)std::min<int64_t>(sinks, kMaxTokens);
+  a.part = static_cast<float*>(scratch);
+  a.part_ml = need ? a.part + part_columns(p) * c->head_dim : nullptr;
+  return attend(a, p, q, query, o, stream);
+}
+
+ssba_status ssba_cache_attend_shared_workspace_size(const ssba_cache* c, const ssba_cache_batch* b,
+                                                    const ssba_cache_query* q, const ssba_cache_prefix* x,
+                                                    size_t* scratch_bytes) {
+  ssba_status st = check_shape(c);
+  if (st != SSBA_OK) return st;
+  if ((st = check_batch(c, b)) != SSBA_OK || (st = check_query(c, b, q)) != SSBA_OK ||
+      (st = check_prefix(c, b, q, x)) != SSBA_OK)
+    return st;
+  if (scratch_bytes) *scratch_bytes = shared_scratch(c, plan_shared(c, b, q, x));
+  return SSBA_OK;
+}
+
+ssba_status ssba_cache_attend_shared(const ssba_cache* c, int32_t layer, const ssba_cache_batch* b,
+                                     const ssba_cache_query* q, const ssba_cache_prefix* x, const void* query, void* o,
+                                     void* scratch, size_t scratch_bytes, void* stream) {
+  AttendArgs a;
+  ssba_status st = attend_args(c, layer, b, q, false, &a);
+  if (st != SSBA_OK || (st = check_prefix(c, b, q, x)) != SSBA_OK) return st;
+  if (b->rows == 0 || b->max_new == 0) return SSBA_OK;
+  if (!attend_arrays(q, query, o) || !x->first || !x->pages || !aligned(x->first, 4) || !aligned(x->pages, 4))
+    return SSBA_ERR_ARG;
+  const AttendPlan p = plan_shared(c, b, q, x);
+  if (!scratch || !aligned(scratch, 16)) return SSBA_ERR_ARG;
+  if (scratch_bytes < shared_scratch(c, p)) return SSBA_ERR_WORKSPACE;
+  if (too_many(p.items * p.splits * 4) || too_many(p.items * p.tiles * 4) ||
+      too_many(p.prefix_items * p.prefix_splits * 4))
+    return SSBA_ERR_UNSUPPORTED;
+  a.first = x->first;
+  a.shared = x->pages;
+  a.groups = x->groups;
+  a.shared_cols = (int)shared_cols(c, b, q, x);
+  a.tiles = p.tiles;
+  a.part = static_cast<float*>(scratch);
+  a.prefix_part = a.part + rest_columns(p) * c->head_dim;
+  a.part_ml = a.prefix_part + prefix_columns(p) * c->head_dim;
+  a.prefix_ml = a.part_ml + rest_columns(p) * 2;
+  return attend(a, p, q, query, o, stream);
 }
 
 }  // extern "C"

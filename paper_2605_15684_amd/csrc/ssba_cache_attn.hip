@@ -132,16 +132,27 @@ __device__ __forceinline__ void split_bf16(float x, __bf16 (&t)[NS]) {
 // of a probability.  QLDS: the queries stay in the LDS, not in registers.
 // J: a tile of 16 columns is J times the same 16 / J columns, each with other
 // keys.
-template <int D_, int R_, int NQ_, int NP_, bool F32_, bool LISTED_, int CG_, int KP_, bool QLDS_, int J_ = 1>
+// SPAN: which keys, and whose queries.
+enum Span {
+  kSpanAll,      // a sequence's: all it holds, or those of its lists
+  kSpanWindow,   // a sequence's: the first `sinks` and each token's last `window`
+  kSpanPrefix,   // a group of sequences': the pages that they share
+  kSpanRest,     // a sequence's: what is behind those
+};
+template <int D_, int R_, int NQ_, int NP_, bool F32_, bool LISTED_, int CG_, int KP_, bool QLDS_, int J_ = 1,
+          int SPAN_ = kSpanAll>
 struct Shape {
   static constexpr int D = D_, R = R_, NQ = NQ_, NP = NP_, CG = CG_, KP = KP_, J = J_;
   static constexpr bool F32 = F32_, LISTED = LISTED_, QLDS = QLDS_;
+  static constexpr int SPAN = SPAN_;
+  static constexpr bool PARTS = SPAN == kSpanPrefix || SPAN == kSpanRest;   // to be joined whatever the splits
   static constexpr bool HALF = !F32 && NP == 1;   // the second product in fp16
   static constexpr int THREADS = 64 * CG * KP;
   static constexpr int NH = D / 64;   // 64-channel blocks
   static constexpr int NC = D / 16;   // 16-channel tiles of O
   static constexpr int COLS = 16 * R / J;   // columns of a wave
   static_assert(J == 1 || (LISTED && R == 1 && KP == 1 && !QLDS), "");
+  static_assert(SPAN == kSpanAll || (!LISTED && KP > 1), "");
 };
 
 // Writes E consecutive channels of an output row.
@@ -159,6 +170,57 @@ __device__ __forceinline__ void store_row(void* o, int64_t at, const float* x) {
       *reinterpret_cast<bf16x4*>(static_cast<__bf16*>(o) + at + e) =
           bf16x4{(__bf16)x[e], (__bf16)x[e + 1], (__bf16)x[e + 2], (__bf16)x[e + 3]};
   }
+}
+
+// A group of sequences that share a prefix: its sequences' new rows, and how
+// many pages are read for all of them at once: those that the prefix has, as
+// far as all of them lie before every sequence's new tokens.  0 as well where
+// the group has more columns than the launch has room for.
+struct GroupView {
+  int first, begin, rows, pages;
+};
+
+// One wave, every lane gets the result.
+__device__ __forceinline__ GroupView group_view(const AttendArgs& a, int g, int lane) {
+  GroupView v;
+  v.first = min(max(a.first[g], 0), a.b.seqs);
+  const int last = max(min(a.first[g + 1], a.b.seqs), v.first);
+  v.begin = min(max(a.b.cu[v.first], 0), a.b.rows);
+  v.rows = max(min(a.b.cu[last], a.b.rows), v.begin) - v.begin;
+  int pages = min(max(a.shared[g], 0), a.b.max_pages);
+  for (int s0 = v.first; s0 < last; s0 += 64) {
+    if (s0 + lane < last) {
+      const SeqView sv = seq_view(a.b, a.c.page_log2, s0 + lane);
+      if (sv.n > 0) pages = min(pages, max(sv.start, 0) >> a.c.page_log2);
+    }
+  }
+#pragma unroll
+  for (int x = 1; x < 64; x <<= 1) pages = min(pages, __shfl_xor(pages, x));
+  pages = __builtin_amdgcn_readfirstlane(pages);
+  v.pages = (int64_t)v.rows * a.group > a.shared_cols || v.first >= a.b.seqs ? 0 : pages;
+  return v;
+}
+
+// The group of sequence s, -1: none (first does not decrease).
+__device__ __forceinline__ int group_of_seq(const AttendArgs& a, int s, int lane) {
+  int n = 0;   // first[0 .. n-1] <= s
+  for (int g0 = 0; g0 <= a.groups; g0 += 64) {
+    const int c = __popcll(__builtin_amdgcn_ballot_w64(g0 + lane <= a.groups && a.first[min(g0 + lane, a.groups)] <= s));
+    n += c;
+    if (c < 64) break;
+  }
+  return n > a.groups ? -1 : n - 1;
+}
+
+// How many pages of sequence s are read with its group's, and its group and
+// that group's view if any.
+__device__ __forceinline__ int pages_shared(const AttendArgs& a, int s, const SeqView& sv, int lane, int* g, GroupView* v) {
+  *g = group_of_seq(a, s, lane);
+  if (*g < 0) return 0;
+  *v = group_view(a, *g, lane);
+  // Arrays that decrease somewhere: not a sequence or not rows of that group.
+  if (s < v->first || sv.begin < v->begin || sv.begin + sv.n > v->begin + v->rows) return 0;
+  return v->pages;
 }
 
 // Which item a workgroup (or a part to be joined) belongs to.
@@ -207,7 +269,7 @@ __global__ __launch_bounds__(P::THREADS, P::R > 1 || (P::D == 128 && (P::J > 1 |
   unsigned id = blockIdx.x;
   int split, ct;
   const unsigned heads = (unsigned)a.b.seqs * a.c.kv_heads;
-  if (P::QLDS && a.causal && heads % 8 == 0) {
+  if (P::QLDS && P::SPAN != kSpanPrefix && a.causal && heads % 8 == 0) {
     const unsigned per = heads / 8 * a.splits, i = id / 8, rest = i % per;
     split = rest % a.splits;
     ct = a.col_tiles - 1 - i / per;
@@ -228,18 +290,42 @@ __global__ __launch_bounds__(P::THREADS, P::R > 1 || (P::D == 128 && (P::J > 1 |
   it.h = id % a.c.kv_heads;
   const int unit = id / a.c.kv_heads;
   // LISTED with several column groups: they are rows.
-  const bool there = item_of<P::LISTED>(a, P::LISTED ? unit * P::CG + cg : unit, lane, &it);
+  int prefix = 0;   // tokens of the shared pages
+  bool there = true;
+  if (P::SPAN == kSpanPrefix) {
+    const GroupView v = group_view(a, unit, lane);
+    if (v.pages == 0) return;
+    prefix = v.pages << page_log2;
+    it.seq = v.first;
+    it.sv = SeqView{v.begin, v.rows, prefix, prefix};
+    it.tok0 = 0;
+    it.ncols = v.rows * a.group;
+  } else {
+    there = item_of<P::LISTED>(a, P::LISTED ? unit * P::CG + cg : unit, lane, &it);
+  }
   if (!there && (P::KP == 1 || P::CG == 1)) return;
+  if (P::SPAN == kSpanRest) {
+    int gr;
+    GroupView v;
+    prefix = pages_shared(a, it.seq, it.sv, lane, &gr, &v) << page_log2;
+  }
   const int cbase = (P::LISTED ? ct : ct * P::CG + cg) * P::COLS;
   if ((P::CG == 1 || P::KP == 1) && cbase >= it.ncols) return;
   if (P::CG > 1 && P::KP > 1 && ct * P::CG * P::COLS >= it.ncols) return;   // the whole workgroup
   const int cend = min(cbase + P::COLS, it.ncols) - 1;   // < cbase: no columns
-  auto limit = [&](int tok) { return a.causal ? min(max(it.sv.start + tok + 1, 0), it.sv.len) : it.sv.len; };
+  auto limit = [&](int tok) {
+    if (P::SPAN == kSpanPrefix) return it.sv.len;   // all of it
+    return a.causal ? min(max(it.sv.start + tok + 1, 0), it.sv.len) : it.sv.len;
+  };
+  // kSpanWindow: the first key of a token's window.  A sequence that has outgrown its table counts on.
+  const int at0 = P::SPAN == kSpanWindow ? max(a.b.lens[it.seq], 0) - it.sv.n : 0;
+  auto low_of = [&](int tok) { return max(at0 + tok - a.window + 1, 0); };
+  const int minlow = low_of(cbase / a.group), maxlow = low_of(cend / a.group);
   const int minlim = limit(it.tok0 + (P::LISTED ? 0 : cbase / a.group));
   const int maxlim = cend < cbase ? 0 : limit(it.tok0 + (P::LISTED ? 0 : cend / a.group));
 
   // This lane's columns.
-  int lim[R];
+  int lim[R], low[P::SPAN == kSpanWindow ? R : 1];
   constexpr int QREGS = P::QLDS ? 1 : R;
   Frag q[QREGS][NQ][NH * 2];
   __shared__ u32x4 s_q[P::QLDS ? P::CG * R * NH * 2 * 64 : 1];
@@ -248,6 +334,7 @@ __global__ __launch_bounds__(P::THREADS, P::R > 1 || (P::D == 128 && (P::J > 1 |
     const int col = cbase + r * 16 + (J > 1 ? n16 % P::COLS : n16);
     const bool in = col <= cend;
     lim[r] = in ? limit(it.tok0 + (P::LISTED ? 0 : col / a.group)) : 0;
+    if (P::SPAN == kSpanWindow) low[r % (P::SPAN == kSpanWindow ? R : 1)] = low_of(col / a.group);
     if (P::QLDS && kp != r % P::KP) continue;   // the waves that share columns share the loading
     const int64_t qo = in ? row_at<P::LISTED>(a, it, col, a.q_st, a.q_sh) : 0;
 #pragma unroll
@@ -300,6 +387,22 @@ __global__ __launch_bounds__(P::THREADS, P::R > 1 || (P::D == 128 && (P::J > 1 |
   } else {
     groups = (maxlim + 15) >> 4;
   }
+  // Group gr of those that are read is group gr of the sequence, or from `near`
+  // on gr + gap.
+  int near = 0, gap = 0;
+  if (P::SPAN == kSpanRest) {
+    gap = min(prefix >> 4, groups);
+    groups -= gap;
+  }
+  if (P::SPAN == kSpanWindow) {
+    near = min((min(a.sinks, maxlim) + 15) >> 4, groups);
+    gap = min(max((minlow >> 4) - near, 0), groups - near);
+    groups -= gap;
+  }
+  auto place = [&](int gr) {
+    if (P::SPAN == kSpanRest) return gr + gap;
+    return P::SPAN == kSpanWindow && gr >= near ? gr + gap : gr;
+  };
   const int steps = (groups + 2 * J - 1) / (2 * J);
   // Shares that differ by one step at most.
   int s0 = 0, s1 = steps;
@@ -317,10 +420,10 @@ __global__ __launch_bounds__(P::THREADS, P::R > 1 || (P::D == 128 && (P::J > 1 |
   uint32_t vs_top = 0;          // largest of V's scales so far, of all lanes (bits)
   bool m_low = false;           // some are far below it
   auto load_chunk = [&](int chunk) {
-    const int gr = chunk * 64 + lane;
+    const int nth = chunk * 64 + lane, gr = place(nth);
     int page = -1, key = kNoKey;
     float ks = 1.f, vs = 1.f;
-    if (gr < groups) {
+    if (nth < groups) {
       const int at = gr >> gpp_log2;
       const int lp = P::LISTED ? list[1 + at] : at;
       if (lp >= 0 && lp < a.b.max_pages) {
@@ -362,8 +465,8 @@ __global__ __launch_bounds__(P::THREADS, P::R > 1 || (P::D == 128 && (P::J > 1 |
     }
 #pragma unroll
     for (int t = 0; t < 2 * J; ++t) {
-      const int gr = 2 * J * s + t;
-      const int page = lane_i(m_page, gr & 63);
+      const int nth = 2 * J * s + t, gr = place(nth);
+      const int page = lane_i(m_page, nth & 63);
       const int sub = (gr & ((1 << gpp_log2) - 1)) * 16 * D;
       x.off[t] = (int64_t)max(page, 0) * a.c.page_bytes + head_off + sub;
       const uint8_t* kp_ = a.c.k + x.off[t];
@@ -381,7 +484,7 @@ __global__ __launch_bounds__(P::THREADS, P::R > 1 || (P::D == 128 && (P::J > 1 |
         if (!P::F32) x.lv[t] = __shfl(m_lv, l + 2 * mine);
       } else {
         // Without lists group g begins at token 16 g: a register less to hold.
-        x.key[t] = P::LISTED ? lane_i(m_key, l) : lane_i(m_page, l) < 0 ? kNoKey : (2 * s + t) << 4;
+        x.key[t] = P::LISTED ? lane_i(m_key, l) : lane_i(m_page, l) < 0 ? kNoKey : place(2 * s + t) << 4;
         x.ks[t] = lane_f(m_ks, l);
         x.vs[t] = lane_f(m_vs, l);
         if (!P::F32) x.lv[t] = lane_f(m_lv, l);
@@ -461,7 +564,10 @@ __global__ __launch_bounds__(P::THREADS, P::R > 1 || (P::D == 128 && (P::J > 1 |
   bool settled = false;   // every column has a maximum
   auto finish = [&](Step& x) {
     // Some column does not see some key of this step.
-    const bool far = max(x.key[0], x.key[1]) + 16 > minlim;
+    bool far = max(x.key[0], x.key[1]) + 16 > minlim;
+    if (P::SPAN == kSpanWindow)
+#pragma unroll
+      for (int t = 0; t < 2; ++t) far |= x.key[t] + 16 > a.sinks && x.key[t] < maxlow;
     const bool edge = J > 1 ? __builtin_amdgcn_ballot_w64(far) != 0 : far;
     if (edge) {
 #pragma unroll
@@ -469,8 +575,12 @@ __global__ __launch_bounds__(P::THREADS, P::R > 1 || (P::D == 128 && (P::J > 1 |
 #pragma unroll
         for (int r = 0; r < R; ++r)
 #pragma unroll
-          for (int i = 0; i < 4; ++i)
-            s[t][r][i] = x.key[t] + 4 * g + i < lim[r] ? s[t][r][i] * x.ks[t] : -INFINITY;
+          for (int i = 0; i < 4; ++i) {
+            const int key = x.key[t] + 4 * g + i;
+            bool seen = key < lim[r];
+            if (P::SPAN == kSpanWindow) seen &= key < a.sinks || key >= low[r % (P::SPAN == kSpanWindow ? R : 1)];
+            s[t][r][i] = seen ? s[t][r][i] * x.ks[t] : -INFINITY;
+          }
       x.ks[0] = x.ks[1] = 1.f;
     }
     // Probabilities with the maximum so far, and each lane's sum of them.
@@ -568,7 +678,13 @@ __global__ __launch_bounds__(P::THREADS, P::R > 1 || (P::D == 128 && (P::J > 1 |
       for (int t = 0; t < 2 * J; ++t) {
         const int key = J > 1 ? lane_i(x.key[t & 1], (t >> 1) * P::COLS) : x.key[t & 1];
         const int left = min(max(maxlim - key - 4 * g, 0), 4);
-        const uint32_t keep = left == 4 ? ~0u : (1u << (8 * left)) - 1u;
+        uint32_t keep = left == 4 ? ~0u : (1u << (8 * left)) - 1u;
+        if (P::SPAN == kSpanWindow)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            const int k = key + 4 * g + i;
+            if (k >= a.sinks && k < minlow) keep &= ~(0xffu << (8 * i));
+          }
 #pragma unroll
         for (int hh = 0; hh < NH; ++hh)
 #pragma unroll
@@ -588,6 +704,11 @@ __global__ __launch_bounds__(P::THREADS, P::R > 1 || (P::D == 128 && (P::J > 1 |
           for (int w = 0; w < 4; ++w) {
             const int k = x.key[w >> 1] + 4 * g + (w & 1) * 2 - lim[r];   // negative: seen
             sees[r].u[w] = ((uint32_t)(k >> 31) & kOne) | ((uint32_t)((k + 1) >> 31) & (kOne << 16));
+            if (P::SPAN == kSpanWindow) {
+              const int at = k + lim[r], first = low[r % (P::SPAN == kSpanWindow ? R : 1)];
+              if (at >= a.sinks && at < first) sees[r].u[w] &= ~0xffffu;
+              if (at + 1 >= a.sinks && at + 1 < first) sees[r].u[w] &= 0xffffu;
+            }
           }
 #pragma unroll
         for (int hh = 0; hh < NH; ++hh)
@@ -751,7 +872,7 @@ __global__ __launch_bounds__(P::THREADS, P::R > 1 || (P::D == 128 && (P::J > 1 |
     }
     const int cc = (ct * P::CG + ocg) * P::COLS + r * 16 + c16;
     if (cc >= it.ncols) continue;
-    if (a.splits > 1) {
+    if (P::PARTS || a.splits > 1) {
       // [item][split][column][D] and the same with (m, l)
       const int64_t slot = (((int64_t)item * a.splits + split) * (P::CG * R) + ocg * R + r) * 16 + c16;
       float* to = a.part + slot * D;
@@ -840,20 +961,119 @@ __global__ __launch_bounds__(256) void k_cache_join(AttendArgs a) {
   store_row<F32, 4>(a.o, row_at<LISTED>(a, it, c0 + c, a.o_st, a.o_sh) + ch, w);
 }
 
+// Joins the parts of shared prefixes and of what is behind them, as the join
+// above: r has the launch of the rests (its items are this one's), p that of the
+// prefixes.  A token's columns of its group begin with those of the sequences
+// before it.
+template <int D, bool F32>
+__global__ __launch_bounds__(256) void k_cache_join_shared(AttendArgs r, AttendArgs p) {
+  __shared__ float s_w[2 * kMaxSplits][16];
+  __shared__ float s_sum[16];
+  __shared__ floatx4 s_acc[128];
+  const int lane = threadIdx.x & 63;
+  unsigned id = blockIdx.x;
+  const int ch32 = id % (D / 32);
+  id /= D / 32;
+  const int tile = id % r.tiles;
+  id /= r.tiles;
+  const unsigned item = id;
+  const int ct = id % r.col_tiles;
+  id /= r.col_tiles;
+  Item it;
+  it.h = id % r.c.kv_heads;
+  item_of<false>(r, id / r.c.kv_heads, lane, &it);
+  const int c0 = (ct * r.tiles + tile) * 16;
+  if (c0 >= it.ncols) return;
+  int shared = 0;        // parts of the prefix
+  int64_t pitem = 0;     // item and column of the prefix of column 0 of this tile
+  int pcol = 0;
+  int g;
+  GroupView v;
+  if (pages_shared(r, it.seq, it.sv, lane, &g, &v)) {
+    shared = p.splits;
+    pcol = (it.sv.begin - v.begin) * r.group + c0;
+    pitem = ((int64_t)g * r.c.kv_heads + it.h) * p.col_tiles;
+  }
+  const int parts = shared + r.splits;
+  const int pw = p.tiles * 16, rw = r.tiles * 16;   // columns of an item
+  // Column c of part s: its place among the parts of its launch.
+  auto slot = [&](int s, int c) {
+    const int col = pcol + c;
+    return s < shared ? ((pitem + col / pw) * p.splits + s) * pw + col % pw
+                      : ((int64_t)item * r.splits + s - shared) * rw + tile * 16 + c;
+  };
+  {
+    // 16 threads a column: maximum, weights and sum over the parts.
+    const int c = threadIdx.x >> 4, j = threadIdx.x & 15;
+    const bool in = c0 + c < it.ncols;
+    float m = -INFINITY;
+    if (in)
+      for (int s = j; s < parts; s += 16) m = fmaxf(m, (s < shared ? p : r).part_ml[slot(s, c) * 2]);
+#pragma unroll
+    for (int x = 1; x < 16; x <<= 1) m = fmaxf(m, __shfl_xor(m, x));
+    float sum = 0.f;
+    if (in)
+      for (int s = j; s < parts; s += 16) {
+        const float* ml = (s < shared ? p : r).part_ml + slot(s, c) * 2;
+        const float ms = ml[0];
+        s_w[s][c] = ms == m ? 1.f : exp2_(ms - m);
+        sum += ms == m ? ml[1] : shrink(ml[1], ms - m);
+      }
+#pragma unroll
+    for (int x = 1; x < 16; x <<= 1) sum += __shfl_xor(sum, x);
+    if (j == 0) s_sum[c] = sum;
+  }
+  __syncthreads();
+  const int half = threadIdx.x >> 7, t = threadIdx.x & 127, c = t >> 3, ch = ch32 * 32 + (t & 7) * 4;
+  floatx4 acc = {0.f, 0.f, 0.f, 0.f};
+  const bool in = c0 + c < it.ncols;
+  if (in)
+#pragma unroll 4
+    for (int s = half; s < parts; s += 2)
+      acc += *reinterpret_cast<const floatx4*>((s < shared ? p : r).part + slot(s, c) * D + ch) * s_w[s][c];
+  if (half) s_acc[t] = acc;
+  __syncthreads();
+  if (half || !in) return;
+  acc += s_acc[t];
+  const float inv = s_sum[c] == 0.f ? 0.f : 1.f / s_sum[c];
+  const float w[4] = {acc[0] * inv, acc[1] * inv, acc[2] * inv, acc[3] * inv};
+  store_row<F32, 4>(r.o, row_at<false>(r, it, c0 + c, r.o_st, r.o_sh) + ch, w);
+}
+
 template <typename P>
 hipError_t launch(const AttendArgs& a, const AttendPlan& p, hipStream_t s) {
   k_cache_attend<P><<<(unsigned)(p.items * p.splits), P::THREADS, 0, s>>>(a);
   const hipError_t e = hipGetLastError();
-  if (e != hipSuccess || p.splits == 1) return e;
+  if (e != hipSuccess || P::PARTS || p.splits == 1) return e;
   constexpr int RC = P::LISTED ? P::R : P::CG * P::R;
   k_cache_join<P::D, RC, P::F32, P::LISTED><<<(unsigned)(p.items * RC * (P::D / 32)), 256, 0, s>>>(a);
   return hipGetLastError();
 }
 
+// Items of sequences (or groups of them), without lists.
+template <int D, int SPAN>
+hipError_t launch_seq(const AttendArgs& a, const AttendPlan& p, bool f32, hipStream_t s) {
+  // D, R, NQ, NP, fp32, lists, column groups, waves that share keys, queries in the LDS, shares of a tile, keys
+  if (p.threads == 512 && p.tiles == 1)
+    return f32 ? launch<Shape<D, 1, 3, 3, true, false, 1, 8, false, 1, SPAN>>(a, p, s)
+               : launch<Shape<D, 1, 1, 2, false, false, 1, 8, false, 1, SPAN>>(a, p, s);
+  if (f32)
+    return p.tiles == 1 ? launch<Shape<D, 1, 3, 3, true, false, 1, 4, false, 1, SPAN>>(a, p, s)
+                        : launch<Shape<D, 1, 3, 3, true, false, 2, 2, false, 1, SPAN>>(a, p, s);
+  switch (p.tiles) {
+    case 1: return launch<Shape<D, 1, 1, 2, false, false, 1, 4, false, 1, SPAN>>(a, p, s);
+    case 2:
+      return p.threads == 512 ? launch<Shape<D, 2, 1, 1, false, false, 1, 8, false, 1, SPAN>>(a, p, s)
+                              : launch<Shape<D, 2, 1, 1, false, false, 1, 4, false, 1, SPAN>>(a, p, s);
+    case 4: return launch<Shape<D, 4, 1, 1, false, false, 1, 8, true, 1, SPAN>>(a, p, s);
+    case 8: return launch<Shape<D, 4, 1, 1, false, false, 2, 4, true, 1, SPAN>>(a, p, s);
+    default: return launch<Shape<D, 4, 1, 1, false, false, 4, 2, true, 1, SPAN>>(a, p, s);
+  }
+}
+
 template <int D>
 hipError_t launch_d(const AttendArgs& a, const AttendPlan& p, int dtype, hipStream_t s) {
   const bool f32 = dtype == SSBA_DT_F32;
-  // D, R, NQ, NP, fp32, lists, column groups, waves that share keys, queries in the LDS, shares of a tile
   switch (p.kind) {
     case kAttendRows:
       if (f32) return launch<Shape<D, 1, 3, 3, true, true, 4, 1, false>>(a, p, s);
@@ -865,22 +1085,27 @@ hipError_t launch_d(const AttendArgs& a, const AttendPlan& p, int dtype, hipStre
                    : launch<Shape<D, 1, 1, 2, false, true, 1, 8, false>>(a, p, s);
       return f32 ? launch<Shape<D, 1, 3, 3, true, true, 1, 4, false>>(a, p, s)
                  : launch<Shape<D, 1, 1, 2, false, true, 1, 4, false>>(a, p, s);
-    default:
-      if (p.threads == 512 && p.tiles == 1)
-        return f32 ? launch<Shape<D, 1, 3, 3, true, false, 1, 8, false>>(a, p, s)
-                   : launch<Shape<D, 1, 1, 2, false, false, 1, 8, false>>(a, p, s);
+    case kAttendWindow: return launch_seq<D, kSpanWindow>(a, p, f32, s);
+    case kAttendShared: {
+      AttendArgs pre = a;
+      AttendPlan pp = p;
+      pre.part = a.prefix_part;
+      pre.part_ml = a.prefix_ml;
+      pre.tiles = pp.tiles = p.prefix_tiles;
+      pre.col_tiles = pp.col_tiles = p.prefix_col_tiles;
+      pre.splits = pp.splits = p.prefix_splits;
+      pp.threads = p.prefix_threads;
+      pp.items = p.prefix_items;
+      hipError_t e = launch_seq<D, kSpanPrefix>(pre, pp, f32, s);
+      if (e != hipSuccess || (e = launch_seq<D, kSpanRest>(a, p, f32, s)) != hipSuccess) return e;
+      const unsigned grid = (unsigned)(p.items * p.tiles * (D / 32));
       if (f32)
-        return p.tiles == 1 ? launch<Shape<D, 1, 3, 3, true, false, 1, 4, false>>(a, p, s)
-                            : launch<Shape<D, 1, 3, 3, true, false, 2, 2, false>>(a, p, s);
-      switch (p.tiles) {
-        case 1: return launch<Shape<D, 1, 1, 2, false, false, 1, 4, false>>(a, p, s);
-        case 2:
-          return p.threads == 512 ? launch<Shape<D, 2, 1, 1, false, false, 1, 8, false>>(a, p, s)
-                                  : launch<Shape<D, 2, 1, 1, false, false, 1, 4, false>>(a, p, s);
-        case 4: return launch<Shape<D, 4, 1, 1, false, false, 1, 8, true>>(a, p, s);
-        case 8: return launch<Shape<D, 4, 1, 1, false, false, 2, 4, true>>(a, p, s);
-        default: return launch<Shape<D, 4, 1, 1, false, false, 4, 2, true>>(a, p, s);
-      }
+        k_cache_join_shared<D, true><<<grid, 256, 0, s>>>(a, pre);
+      else
+        k_cache_join_shared<D, false><<<grid, 256, 0, s>>>(a, pre);
+      return hipGetLastError();
+    }
+    default: return launch_seq<D, kSpanAll>(a, p, f32, s);
   }
 }
 

@@ -114,6 +114,14 @@ struct AttendArgs {
   int group, causal, keep;
   int col_tiles;          // column tiles of an item
   int splits;             // workgroups that share an item's keys
+  // What follows is read by the kinds of its name only.
+  int window, sinks;      // kAttendWindow; window <= 2^30
+  const int32_t* first;   // kAttendShared: [groups + 1] first sequence of each group
+  const int32_t* shared;  // [groups] pages of its prefix
+  int groups, shared_cols;   // shared_cols: most columns of a group
+  int tiles;              // tiles of 16 columns of an item
+  float* prefix_part;     // part and part_ml of the prefixes
+  float* prefix_ml;
 };
 
 // What the attention launch does (ssba_cache_api.cpp decides).
@@ -121,6 +129,8 @@ enum AttendKind {
   kAttendSeq,    // items: (sequence, kv head, column tile)
   kAttendRow,    // lists; items: (row, kv head, column tile), the waves of a workgroup share the keys
   kAttendRows,   // lists; a wave per such item
+  kAttendWindow, // as kAttendSeq, keys of the sinks and the window
+  kAttendShared, // as kAttendSeq for what is behind the prefixes; items of these: (group, kv head, column tile)
 };
 struct AttendPlan {
   AttendKind kind;
@@ -128,6 +138,8 @@ struct AttendPlan {
   int threads;
   int col_tiles, splits;
   int64_t items;          // workgroups without the splits
+  int prefix_tiles, prefix_threads, prefix_col_tiles, prefix_splits;   // kAttendShared: the same of the prefixes
+  int64_t prefix_items;
 };
 
 hipError_t launch_cache_append(const AppendArgs& a, int dtype, hipStream_t s);
