@@ -45,7 +45,7 @@ SOURCES = {
     "ssba_window_api.cpp": [],
     # MFMA results in ordinary VGPRs, as above.
     "ssba_window.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form"],
-    "ssba_window_bwd.hip": [],
+    "ssba_window_bwd.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form"],
 }
 
 COMMON = [

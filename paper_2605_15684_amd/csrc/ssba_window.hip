@@ -57,6 +57,7 @@ __global__ __launch_bounds__(256, 2) void k_window_forward(WindowArgs a) {
   const int n = n_sink + last / T::ROWS - low + 1;
   auto first_of = [&](int c) { return (c < n_sink ? c : low + c - n_sink) * T::ROWS; };
 
+  WLane<T> at(lane);
   floatx16 o[NDB];
   float m, l;
   bool settled;
@@ -75,7 +76,7 @@ __global__ __launch_bounds__(256, 2) void k_window_forward(WindowArgs a) {
 #pragma unroll
       for (int nb = 0; nb < NB; ++nb) {
         s[nb] = floatx16{};
-        rows_product<T>(s[nb], kc + nb * T::HALF, q, lane);
+        rows_product<T>(s[nb], kc + nb * T::HALF, q, at);
       }
       if (!whole) {
 #pragma unroll
@@ -131,7 +132,7 @@ __global__ __launch_bounds__(256, 2) void k_window_forward(WindowArgs a) {
                                reinterpret_cast<float*>((wave < T::TILE / 4096 ? kn : vn) + 4096 * (wave % (T::TILE / 4096))),
                                lane, [&](int row) { return window_sees(i, j0 + 32 * nb + row, a.window, a.sinks); });
         else
-          cols_product<T>(o, vc + nb * T::HALF, pr[nb], lane);
+          cols_product<T>(o, vc + nb * T::HALF, pr[nb], at);
       }
     }
     __builtin_amdgcn_s_waitcnt(kWaitVm0);

@@ -18,11 +18,27 @@
 // more with the tiles that are seen in part taken row by row.
 #include <hip/hip_runtime.h>
 
+#include <type_traits>
+
 #include "ssba_common.h"
 #include "ssba_window_tiles.h"
 
 namespace ssba {
 namespace {
+
+// Reads of the LDS run six ahead of the products that use them: with two waves
+// a SIMD a product that waits for its own read leaves the matrix cores idle.
+template <class T>
+__device__ __forceinline__ void order_rows() {
+  if constexpr (T::ORDERED) {
+    __builtin_amdgcn_sched_group_barrier(kDsRead, 6, 0);
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+      __builtin_amdgcn_sched_group_barrier(kMfma, 1, 0);
+      __builtin_amdgcn_sched_group_barrier(kDsRead, 1, 0);
+    }
+  }
+}
 
 // --------------------------------------------------------------------------
 // dQ
@@ -82,6 +98,7 @@ __global__ __launch_bounds__(256, T::F32 ? 1 : 2) void k_window_dq(WindowArgs a)
   const int n = n_sink + last / T::ROWS - low + 1;
   auto first_of = [&](int c) { return (c < n_sink ? c : low + c - n_sink) * T::ROWS; };
 
+  WLane<T> at(lane);
   floatx16 acc[NDB];
   auto body = [&](int c, const char* kc, const char* vc, char* kn, char* vn, bool careful) {
     if (!careful && c + 1 < n) {
@@ -94,11 +111,13 @@ __global__ __launch_bounds__(256, T::F32 ? 1 : 2) void k_window_dq(WindowArgs a)
       const bool whole = j0 + T::ROWS - 1 <= w0 && (j0 + T::ROWS <= a.sinks || j0 > w0 + 31 - a.window);
 #pragma unroll
       for (int nb = 0; nb < NB; ++nb) {
+        if constexpr (T::ORDERED) __builtin_amdgcn_sched_barrier(0);
+        at.forget();
         floatx16 s = {}, ds;
 #pragma unroll
         for (int e = 0; e < 16; ++e) ds[e] = -delta;
-        rows_product<T>(s, kc + nb * T::HALF, q, lane);
-        rows_product<T>(ds, vc + nb * T::HALF, g, lane);
+        rows_products<T>(s, kc + nb * T::HALF, q, ds, vc + nb * T::HALF, g, at);
+        order_rows<T>();
 #pragma unroll
         for (int e = 0; e < 16; ++e) ds[e] *= __builtin_amdgcn_exp2f(__builtin_fmaf(s[e], a.scale_log2, -lse2));
         if (!whole) {
@@ -113,7 +132,8 @@ __global__ __launch_bounds__(256, T::F32 ? 1 : 2) void k_window_dq(WindowArgs a)
                                reinterpret_cast<float*>((wave < T::TILE / 4096 ? kn : vn) + 4096 * (wave % (T::TILE / 4096))),
                                lane, [&](int r) { return window_sees(i, j0 + 32 * nb + r, a.window, a.sinks); });
         else
-          cols_product<T>(acc, kc + nb * T::HALF, ds, lane);
+          cols_product<T>(acc, kc + nb * T::HALF, ds, at);
+        if constexpr (T::ORDERED) __builtin_amdgcn_sched_barrier(0);
       }
     }
     __builtin_amdgcn_s_waitcnt(kWaitVm0);
@@ -224,8 +244,11 @@ __device__ __forceinline__ void copy_values(const float* from, int n, float* dst
 }
 
 template <class T>
-__global__ __launch_bounds__(256, 1) void k_window_dkdv(WindowArgs a) {
+__global__ __launch_bounds__(256, T::F32 ? 1 : 2) void k_window_dkdv(WindowArgs a) {
   constexpr int NB = T::NB, NDB = T::NDB;
+  // The wave's keys as operands in the LDS where registers are short.
+  constexpr bool KLDS = T::ORDERED;
+  __shared__ __attribute__((aligned(16))) char s_k[KLDS ? 4 * T::NKS * 1024 : 16];
   __shared__ __attribute__((aligned(16))) char qA[T::TILE];
   __shared__ __attribute__((aligned(16))) char qB[T::TILE];
   __shared__ __attribute__((aligned(16))) char gA[T::TILE];
@@ -242,10 +265,21 @@ __global__ __launch_bounds__(256, 1) void k_window_dkdv(WindowArgs a) {
   const int j = w0 + l32;
   const bool in = j < p.len;
 
-  WRow<T> k, v;
+  using KRow = typename std::conditional<KLDS, WRowLds<T>, WRow<T>>::type;
+  KRow k;
+  WRow<T> v;
   {
     const int64_t row = p.begin + min(j, p.len - 1);
-    k.load(static_cast<const char*>(a.k) + ((int64_t)p.b * a.sk.b + (int64_t)p.kvh * a.sk.h + row * a.sk.t) * T::SIZE, hw);
+    WRow<T> kr;
+    kr.load(static_cast<const char*>(a.k) + ((int64_t)p.b * a.sk.b + (int64_t)p.kvh * a.sk.h + row * a.sk.t) * T::SIZE, hw);
+    if constexpr (KLDS) {   // read by this wave alone
+      k.at = s_k + 1024 * T::NKS * wave + 16 * lane;
+#pragma unroll
+      for (int ks = 0; ks < T::NKS; ++ks)
+        *reinterpret_cast<floatx4*>(s_k + 1024 * (T::NKS * wave + ks) + 16 * lane) = kr.f[ks];
+    } else {
+      k = kr;
+    }
     v.load(static_cast<const char*>(a.v) + ((int64_t)p.b * a.sv.b + (int64_t)p.kvh * a.sv.h + row * a.sv.t) * T::SIZE, hw);
   }
   WCopy<T> cq, cg;
@@ -276,6 +310,7 @@ __global__ __launch_bounds__(256, 1) void k_window_dkdv(WindowArgs a) {
     }
   };
 
+  WLane<T> place(lane);
   floatx16 dk[NDB], dv[NDB];
   int at = 0;   // tile of the head
   auto body = [&](int c, const char* qc, const char* gc, float (*rc)[64], char* qn, char* gn, float (*rn)[64], bool careful) {
@@ -292,6 +327,8 @@ __global__ __launch_bounds__(256, 1) void k_window_dkdv(WindowArgs a) {
           const int i = i0 + 32 * nb + r;
           return i >= p.q0 && i < p.q1 && window_sees(i, j, a.window, a.sinks);
         };
+        if constexpr (T::ORDERED) __builtin_amdgcn_sched_barrier(0);
+        place.forget();
         floatx16 pr = {}, ds;
 #pragma unroll
         for (int e = 0; e < 16; e += 4) {
@@ -299,8 +336,8 @@ __global__ __launch_bounds__(256, 1) void k_window_dkdv(WindowArgs a) {
 #pragma unroll
           for (int x = 0; x < 4; ++x) ds[e + x] = -d[x];
         }
-        rows_product<T>(pr, qc + nb * T::HALF, k, lane);
-        rows_product<T>(ds, gc + nb * T::HALF, v, lane);
+        rows_products<T>(pr, qc + nb * T::HALF, k, ds, gc + nb * T::HALF, v, place);
+        if constexpr (T::ORDERED) __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
         for (int e = 0; e < 16; e += 4) {
           const floatx4 l = *reinterpret_cast<const floatx4*>(&rc[0][32 * nb + 2 * e + 4 * hw]);
@@ -323,9 +360,11 @@ __global__ __launch_bounds__(256, 1) void k_window_dkdv(WindowArgs a) {
           cols_product_seen<T>(dv, gc + nb * T::HALF, pr, room, lane, sees);
           cols_product_seen<T>(dk, qc + nb * T::HALF, ds, room, lane, sees);
         } else {
-          cols_product<T>(dv, gc + nb * T::HALF, pr, lane);
-          cols_product<T>(dk, qc + nb * T::HALF, ds, lane);
+          cols_product<T>(dv, gc + nb * T::HALF, pr, place);
+          if constexpr (T::ORDERED) __builtin_amdgcn_sched_barrier(0);
+          cols_product<T>(dk, qc + nb * T::HALF, ds, place);
         }
+        if constexpr (T::ORDERED) __builtin_amdgcn_sched_barrier(0);
       }
     }
     __builtin_amdgcn_s_waitcnt(kWaitVm0);
@@ -427,13 +466,14 @@ __global__ __launch_bounds__(256) void k_window_join(WindowArgs a) {
   }
 }
 
-template <class T>
+// T: tiles of the query side and the join; TK: of the key side.
+template <class T, class TK>
 hipError_t launch(const WindowArgs& a, hipStream_t s) {
   const int64_t units = (int64_t)a.batch * a.kv_heads, cut = (int64_t)a.sink_tiles * a.chunk_slots;
   k_window_dq<T><<<(unsigned)((int64_t)a.batch * a.heads * a.slots), 256, 0, s>>>(a);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
-  k_window_dkdv<T><<<(unsigned)(units * (a.slots + cut)), 256, 0, s>>>(a);
+  k_window_dkdv<TK><<<(unsigned)(units * (a.slots + cut)), 256, 0, s>>>(a);
   if ((e = hipGetLastError()) != hipSuccess || !cut) return e;
   k_window_join<T><<<(unsigned)(units * cut * (kWindowRows * T::D / 2048)), 256, 0, s>>>(a);
   return hipGetLastError();
@@ -442,8 +482,10 @@ hipError_t launch(const WindowArgs& a, hipStream_t s) {
 }  // namespace
 
 hipError_t launch_window_backward(const WindowArgs& a, int head_dim, int dtype, hipStream_t s) {
-  if (head_dim == 64) return dtype == SSBA_DT_F32 ? launch<WTile<64, true>>(a, s) : launch<WTile<64, false>>(a, s);
-  return dtype == SSBA_DT_F32 ? launch<WTile<128, true>>(a, s) : launch<WTile<128, false>>(a, s);
+  if (dtype == SSBA_DT_F32)
+    return head_dim == 64 ? launch<WTile<64, true>, WTile<64, true>>(a, s) : launch<WTile<128, true>, WTile<128, true>>(a, s);
+  return head_dim == 64 ? launch<WTile<64, false>, WTile<64, false>>(a, s)
+                        : launch<WTile<128, false>, WTile<128, false, 1>>(a, s);
 }
 
 }  // namespace ssba

@@ -1,8 +1,7 @@
 // What the windowed attention's forward and backward share: which rows a
 // workgroup has, tiles of rows in the LDS, and the two kinds of product.
 //
-// A tile is 64 bf16 rows or 32 fp32 rows (the same bytes), in halves of 32 rows
-// that buffer_load ... lds fills.  Products are 32 x 32 by
+// A tile is 32 or 64 rows, in halves of 32 that buffer_load ... lds fills.  Products are 32 x 32 by
 // v_mfma_f32_32x32x16_bf16 or v_mfma_f32_32x32x2_f32, whose result gives lane l
 // column l % 32 and rows 8 (e / 4) + 4 (l / 32) + e % 4, e = 0 .. 15:
 //   rows_product   (tile rows) x (the wave's 32 rows, in registers)
@@ -19,17 +18,19 @@ namespace ssba {
 
 typedef float floatx4 __attribute__((ext_vector_type(4)));
 
-template <int D_, bool F32_>
+template <int D_, bool F32_, int NB_ = F32_ ? 1 : 2>
 struct WTile {
   static constexpr int D = D_;
   static constexpr bool F32 = F32_;
   static constexpr int SIZE = F32 ? 4 : 2;
   static constexpr int ROWB = D * SIZE;         // bytes of a row
   static constexpr int CPR = ROWB / 16;         // 16-byte chunks of a row
-  static constexpr int NB = F32 ? 1 : 2;        // halves of a tile
+  static constexpr int NB = NB_;                // halves of a tile
   static constexpr int ROWS = 32 * NB;
   static constexpr int HALF = 32 * ROWB;
   static constexpr int TILE = NB * HALF;        // 8 or 16 KB
+  // Registers are short and two waves a SIMD few: reads and products are put in order by hand.
+  static constexpr bool ORDERED = D == 128 && !F32;
   static constexpr int KPI = 1024 / ROWB;       // rows of a copy instruction
   static constexpr int NIW = TILE / 4096;       // copy instructions of each of 4 waves
   static constexpr int NKS = F32 ? D / 8 : D / 16;   // 16-byte operands of a lane in a row
@@ -161,49 +162,109 @@ struct WRow {
   }
 };
 
+// One such operand as a copy in the LDS in the order of its use: 1 KB each.
 template <class T>
-__device__ __forceinline__ void rows_product(floatx16& acc, const char* half, const WRow<T>& b, int lane) {
-  const int k = lane & 31, hw = lane >> 5;
+struct WRowLds {
+  const char* at;   // the wave's, lane's 16 bytes of the first
+  __device__ __forceinline__ floatx4 get(int ks) const { return *reinterpret_cast<const floatx4*>(at + 1024 * ks); }
+};
+template <class T>
+__device__ __forceinline__ floatx4 operand(const WRow<T>& r, int ks) {
+  return r.f[ks];
+}
+template <class T>
+__device__ __forceinline__ floatx4 operand(const WRowLds<T>& r, int ks) {
+  return r.get(ks);
+}
+
+// Where a lane's operands lie in a half tile: all of one kind differ by
+// exclusive ors and sums of constants.
+template <class T>
+struct WLane {
+  int row, col;
+  __device__ __forceinline__ explicit WLane(int lane) {
+    const int l32 = lane & 31, hw = lane >> 5;
+    row = l32 * T::ROWB + 16 * wswz<T>(l32, hw);
+    if constexpr (T::F32) {
+      col = 4 * hw * T::ROWB + 16 * wswz<T>(4 * hw, l32 >> 2) + 4 * (l32 & 3);
+    } else {
+      // As tr_frag: rows 4 hw + li / 4, channels 16 (G & 1) + 4 (li & 3) ..
+      const int G = lane >> 4, li = lane & 15, k = 4 * hw + (li >> 2), ch = 16 * (G & 1) + 4 * (li & 3);
+      col = k * T::ROWB + 16 * wswz<T>(k, ch >> 3) + 2 * (ch & 7);
+    }
+  }
+  // Forgotten by the compiler, which would otherwise keep every address in a
+  // register and spill.
+  __device__ __forceinline__ void forget() {
+    if constexpr (T::ORDERED) asm volatile("" : "+v"(row), "+v"(col));
+  }
+};
+
+// Row l % 32, the 16-byte chunk 2 ks + l / 32.
+template <class T>
+__device__ __forceinline__ floatx4 row_operand(const char* half, const WLane<T>& l, int ks) {
+  return *reinterpret_cast<const floatx4*>(half + (l.row ^ (32 * ks)));
+}
+
+// bf16: channels 32 db .. of rows 16 ks + 8 (e / 4) + 4 (l / 32) + e % 4.
+template <class T>
+__device__ __forceinline__ bf16x8 col_operand(const char* half, const WLane<T>& l, int ks, int db) {
+  s16x4 x[2];
+#pragma unroll
+  for (int rr = 0; rr < 2; ++rr)
+    x[rr] = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+        (lds_s16x4*)(half + (l.col ^ (64 * db + 32 * rr)) + (8 * rr + 16 * ks) * T::ROWB));
+  return __builtin_bit_cast(bf16x8, s16x8{x[0][0], x[0][1], x[0][2], x[0][3], x[1][0], x[1][1], x[1][2], x[1][3]});
+}
+
+template <class T>
+__device__ __forceinline__ void multiply(floatx16& acc, floatx4 x, floatx4 y) {
+  if constexpr (T::F32) {
+#pragma unroll
+    for (int e = 0; e < 4; ++e) acc = __builtin_amdgcn_mfma_f32_32x32x2f32(x[e], y[e], acc, 0, 0, 0);
+  } else {
+    acc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, x), __builtin_bit_cast(bf16x8, y), acc, 0, 0, 0);
+  }
+}
+
+template <class T>
+__device__ __forceinline__ void rows_product(floatx16& acc, const char* half, const WRow<T>& b, const WLane<T>& l) {
+#pragma unroll
+  for (int ks = 0; ks < T::NKS; ++ks) multiply<T>(acc, row_operand<T>(half, l, ks), b.f[ks]);
+}
+
+// Two of them in turn.
+template <class T, class Row1, class Row2>
+__device__ __forceinline__ void rows_products(floatx16& acc1, const char* half1, const Row1& b1, floatx16& acc2,
+                                              const char* half2, const Row2& b2, const WLane<T>& l) {
 #pragma unroll
   for (int ks = 0; ks < T::NKS; ++ks) {
-    const floatx4 x = *reinterpret_cast<const floatx4*>(half + k * T::ROWB + 16 * wswz<T>(k, 2 * ks + hw));
-    if constexpr (T::F32) {
-#pragma unroll
-      for (int e = 0; e < 4; ++e) acc = __builtin_amdgcn_mfma_f32_32x32x2f32(x[e], b.f[ks][e], acc, 0, 0, 0);
-    } else {
-      acc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, x),
-                                                   __builtin_bit_cast(bf16x8, b.f[ks]), acc, 0, 0, 0);
-    }
+    multiply<T>(acc1, row_operand<T>(half1, l, ks), operand<T>(b1, ks));
+    multiply<T>(acc2, row_operand<T>(half2, l, ks), operand<T>(b2, ks));
   }
 }
 
 // acc[db] += (channels 32 db .. of the half's rows)^T x, x a 32 x 32 result.
 template <class T>
-__device__ __forceinline__ void cols_product(floatx16 (&acc)[T::NDB], const char* half, const floatx16& x, int lane) {
+__device__ __forceinline__ void cols_product(floatx16 (&acc)[T::NDB], const char* half, const floatx16& x, const WLane<T>& l) {
   if constexpr (T::F32) {
-    const int l32 = lane & 31, hw = lane >> 5;
 #pragma unroll
-    for (int j = 0; j < 16; ++j) {
-      const int row = 8 * (j >> 2) + 4 * hw + (j & 3);
+    for (int j = 0; j < 16; ++j)
 #pragma unroll
       for (int db = 0; db < T::NDB; ++db) {
-        const float w = *reinterpret_cast<const float*>(half + row * T::ROWB + 16 * wswz<T>(row, 8 * db + (l32 >> 2)) +
-                                                        4 * (l32 & 3));
+        const float w = *reinterpret_cast<const float*>(half + (l.col ^ (16 * (j & 3))) +
+                                                        (8 * (j >> 2) + (j & 3)) * T::ROWB + 128 * db);
         acc[db] = __builtin_amdgcn_mfma_f32_32x32x2f32(w, x[j], acc[db], 0, 0, 0);
       }
-    }
   } else {
     uint32_t pk[8];
 #pragma unroll
     for (int j = 0; j < 8; ++j) pk[j] = pack2(x[2 * j], x[2 * j + 1]);
 #pragma unroll
-    for (int ks = 0; ks < 2; ++ks) {
-      const bf16x8 pb = packed_frag(pk, ks);
+    for (int ks = 0; ks < 2; ++ks)
 #pragma unroll
       for (int db = 0; db < T::NDB; ++db)
-        acc[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(bf16x8, tr_frag<T::D>(half, lane, ks, db)), pb,
-                                                         acc[db], 0, 0, 0);
-    }
+        acc[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(col_operand<T>(half, l, ks, db), packed_frag(pk, ks), acc[db], 0, 0, 0);
   }
 }
 
@@ -217,13 +278,13 @@ __device__ __forceinline__ void cols_product_seen(floatx16 (&acc)[T::NDB], const
 #pragma unroll
   for (int j = 0; j < 16; ++j) room[j * 64 + lane] = x[j];
   __builtin_amdgcn_wave_barrier();
-#pragma unroll 1
-  for (int row = 0; row < 32; ++row) {
-    const int j = 4 * (row >> 3) + (row & 3), from = (row >> 2) & 1;
-    const float w = room[j * 64 + l32 + 32 * from];
-    const bool in = sees(row);
 #pragma unroll
-    for (int db = 0; db < T::NDB; ++db)
+  for (int db = 0; db < T::NDB; ++db)
+#pragma unroll 1
+    for (int row = 0; row < 32; ++row) {
+      const int j = 4 * (row >> 3) + (row & 3), from = (row >> 2) & 1;
+      const float w = room[j * 64 + l32 + 32 * from];
+      const bool in = sees(row);
 #pragma unroll
       for (int e = 0; e < 16; ++e) {
         const int ch = 32 * db + 8 * (e >> 2) + 4 * hw + (e & 3), at = ch * T::SIZE;
@@ -235,7 +296,7 @@ __device__ __forceinline__ void cols_product_seen(floatx16 (&acc)[T::NDB], const
           y = __uint_as_float((uint32_t)*reinterpret_cast<const u16*>(p) << 16);
         acc[db][e] = in ? __builtin_fmaf(w, y, acc[db][e]) : acc[db][e];
       }
-  }
+    }
   __builtin_amdgcn_wave_barrier();
 }
 
@@ -266,9 +327,10 @@ __device__ __forceinline__ bool not_finite(const floatx16 (&acc)[N]) {
   return t != 0.f;   // NaN
 }
 
-// Whether token i sees token j.
+// Whether token i sees token j.  Without branches: a wave decides for 16 pairs a
+// lane.
 __device__ __forceinline__ bool window_sees(int i, int j, int window, int sinks) {
-  return j <= i && (j < sinks || j > i - window);
+  return ((unsigned)(i - j) < (unsigned)window) | (j < min(sinks, i + 1));
 }
 
 }  // namespace ssba
