@@ -168,8 +168,8 @@ ssba_status ssba_window_backward(const ssba_window* w, const ssba_window_grads* 
   a.dk = dk;
   a.dv = dv;
   a.lse2 = static_cast<float*>(scratch);
-  a.delta = a.lse2 + row_bytes(w) / 4;
-  a.part = a.delta + row_bytes(w) / 4;
+  a.ndelta = a.lse2 + row_bytes(w) / 4;
+  a.part = a.ndelta + row_bytes(w) / 4;
   return ssba::launch_window_backward(a, w->head_dim, w->dtype, static_cast<hipStream_t>(hip_stream)) == hipSuccess
              ? SSBA_OK
              : SSBA_ERR_HIP;

@@ -28,14 +28,16 @@ namespace {
 
 // Reads of the LDS run six ahead of the products that use them: with two waves
 // a SIMD a product that waits for its own read leaves the matrix cores idle.
-template <class T>
+template <class T, int AHEAD, int READS>
 __device__ __forceinline__ void order_rows() {
   if constexpr (T::ORDERED) {
-    __builtin_amdgcn_sched_group_barrier(kDsRead, 6, 0);
+    __builtin_amdgcn_sched_group_barrier(kDsRead, AHEAD, 0);
 #pragma unroll
-    for (int i = 0; i < 16; ++i) {
+    for (int i = 0; i < 8; ++i) {
       __builtin_amdgcn_sched_group_barrier(kMfma, 1, 0);
-      __builtin_amdgcn_sched_group_barrier(kDsRead, 1, 0);
+      __builtin_amdgcn_sched_group_barrier(kDsRead, READS / 2, 0);
+      __builtin_amdgcn_sched_group_barrier(kMfma, 1, 0);
+      __builtin_amdgcn_sched_group_barrier(kDsRead, READS - READS / 2, 0);
     }
   }
 }
@@ -84,7 +86,7 @@ __global__ __launch_bounds__(256, T::F32 ? 1 : 2) void k_window_dq(WindowArgs a)
     const int64_t at = ((int64_t)p.b * a.heads + p.h) * a.seq + row;
     lse2 = a.lse[at] * kLog2e;
     if (in && hw == 0) {
-      a.delta[at] = delta;
+      a.ndelta[at] = -delta;
       a.lse2[at] = lse2;
     }
   }
@@ -117,7 +119,7 @@ __global__ __launch_bounds__(256, T::F32 ? 1 : 2) void k_window_dq(WindowArgs a)
 #pragma unroll
         for (int e = 0; e < 16; ++e) ds[e] = -delta;
         rows_products<T>(s, kc + nb * T::HALF, q, ds, vc + nb * T::HALF, g, at);
-        order_rows<T>();
+        order_rows<T, 6, 2>();
 #pragma unroll
         for (int e = 0; e < 16; ++e) ds[e] *= __builtin_amdgcn_exp2f(__builtin_fmaf(s[e], a.scale_log2, -lse2));
         if (!whole) {
@@ -253,7 +255,7 @@ __global__ __launch_bounds__(256, T::F32 ? 1 : 2) void k_window_dkdv(WindowArgs 
   __shared__ __attribute__((aligned(16))) char qB[T::TILE];
   __shared__ __attribute__((aligned(16))) char gA[T::TILE];
   __shared__ __attribute__((aligned(16))) char gB[T::TILE];
-  __shared__ __attribute__((aligned(16))) float rA[2][64];   // lse2, delta of the tile's rows
+  __shared__ __attribute__((aligned(16))) float rA[2][64];   // lse2, -delta of the tile's rows
   __shared__ __attribute__((aligned(16))) float rB[2][64];
   __shared__ int s_bad;
   const int lane = threadIdx.x & 63, l32 = lane & 31, hw = lane >> 5;
@@ -289,7 +291,7 @@ __global__ __launch_bounds__(256, T::F32 ? 1 : 2) void k_window_dkdv(WindowArgs 
   const char* q_base = cq.base;
   const char* g_base = cg.base;
   const float* l_base = a.lse2 + ((int64_t)p.b * a.heads + p.kvh * a.group) * a.seq + p.begin;
-  const float* d_base = a.delta + ((int64_t)p.b * a.heads + p.kvh * a.group) * a.seq + p.begin;
+  const float* d_base = a.ndelta + ((int64_t)p.b * a.heads + p.kvh * a.group) * a.seq + p.begin;
 
   // Tiles of queries, head after head.
   const int t0 = p.q0 / T::ROWS, per_head = (p.q1 - 1) / T::ROWS - t0 + 1, n = per_head * a.group;
@@ -334,9 +336,10 @@ __global__ __launch_bounds__(256, T::F32 ? 1 : 2) void k_window_dkdv(WindowArgs 
         for (int e = 0; e < 16; e += 4) {
           const floatx4 d = *reinterpret_cast<const floatx4*>(&rc[1][32 * nb + 2 * e + 4 * hw]);
 #pragma unroll
-          for (int x = 0; x < 4; ++x) ds[e + x] = -d[x];
+          for (int x = 0; x < 4; ++x) ds[e + x] = d[x];
         }
         rows_products<T>(pr, qc + nb * T::HALF, k, ds, gc + nb * T::HALF, v, place);
+        order_rows<T, 8, 3>();
         if constexpr (T::ORDERED) __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
         for (int e = 0; e < 16; e += 4) {

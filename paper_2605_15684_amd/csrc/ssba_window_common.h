@@ -24,8 +24,8 @@ struct WindowArgs {
   void* dq;
   void* dk;
   void* dv;
-  float* lse2;         // backward scratch: lse in log2 units, delta [batch][heads][seq]
-  float* delta;
+  float* lse2;         // backward scratch: lse in log2 units, -delta [batch][heads][seq]
+  float* ndelta;
   float* part;         // parts of dk and dv of sink tiles [unit][sink tile][chunk slot][2][128][D]
   Strides sq, sk, sv, so, sdo, sdq, sdk, sdv;
   const int32_t* cu;
