@@ -91,14 +91,22 @@ ssba_status plan(const ssba_window* w, WindowArgs* a) {
     if (bytes <= kMostParts) a->chunk_slots = (int)slots;
   }
   const int64_t cut = (int64_t)a->sink_tiles * a->chunk_slots;
+  // The heads of a group are shared evenly by several workgroups where those of whole tiles do not fill the chip (two a
+  // CU; fp32: one), as far as their parts stay within that size.
+  const int64_t tiles = std::max<int64_t>(1, units * (a->slots + cut)), room = w->dtype == SSBA_DT_F32 ? 256 : 512;
+  const int64_t most = kMostParts / (tiles * 2 * kWindowRows * w->head_dim * 4);
+  a->head_parts = 1;
+  for (int n = 2; n <= a->group && n <= most && tiles * a->head_parts < room; ++n)
+    if (a->group % n == 0) a->head_parts = n;
   if ((double)w->batch * w->heads * a->slots > (double)ssba::kMaxGroups256 ||
-      (double)units * (a->slots + cut * 8) > (double)ssba::kMaxGroups256)
+      (double)units * (a->slots + cut) * (a->head_parts > 1 ? 8 * a->head_parts : 8) > (double)ssba::kMaxGroups256)
     return SSBA_ERR_UNSUPPORTED;
   return SSBA_OK;
 }
 
 size_t part_bytes(const ssba_window* w, const WindowArgs& a) {
-  return (size_t)w->batch * w->kv_heads * a.sink_tiles * a.chunk_slots * 2 * kWindowRows * w->head_dim * 4;
+  const size_t kept = (size_t)a.sink_tiles * a.chunk_slots + (a.head_parts > 1 ? a.slots : 0);
+  return (size_t)w->batch * w->kv_heads * kept * a.head_parts * 2 * kWindowRows * w->head_dim * 4;
 }
 
 size_t row_bytes(const ssba_window* w) { return ceil_div((int64_t)w->batch * w->heads * w->seq * 4, 256) * 256; }

@@ -178,11 +178,11 @@ __global__ __launch_bounds__(256, T::F32 ? 1 : 2) void k_window_dq(WindowArgs a)
 // dK, dV
 // --------------------------------------------------------------------------
 
-// What a workgroup of the key side does: 128 keys of a kv head and the queries
-// q0 .. q1 - 1 of its sequence.
+// What a workgroup of the key side does: 128 keys of a kv head, and the queries
+// q0 .. q1 - 1 of its sequence of the group's heads g0 .. g1 - 1.
 struct KeyPlace {
-  int b, kvh, begin, len, k0, q0, q1;
-  int64_t part;   // where its parts go, -1: it has all queries
+  int b, kvh, begin, len, k0, q0, q1, g0, g1;
+  int64_t part;   // where its parts go, -1: it has all queries of all heads
 };
 
 // Slot of a sequence's chunk 0, as place_slot counts tiles.
@@ -190,7 +190,7 @@ __device__ __forceinline__ int chunk_slot(const WindowArgs& a, int begin, int s)
 
 __device__ __forceinline__ bool place_keys(const WindowArgs& a, int lane, KeyPlace* p) {
   const unsigned units = (unsigned)a.batch * a.kv_heads, cut = (unsigned)a.sink_tiles * a.chunk_slots;
-  const unsigned per = a.slots + cut;
+  const unsigned per = (a.slots + cut) * a.head_parts;
   unsigned id = blockIdx.x, unit, at;
   if (a.spread) {
     unit = id % units;
@@ -200,9 +200,14 @@ __device__ __forceinline__ bool place_keys(const WindowArgs& a, int lane, KeyPla
     unit = id / per;
     at = id % per;
   }
+  const int share = at % a.head_parts;
+  at /= a.head_parts;
+  p->g0 = share * a.group / a.head_parts;
+  p->g1 = (share + 1) * a.group / a.head_parts;
   p->b = unit / a.kv_heads;
   p->kvh = unit % a.kv_heads;
-  p->part = -1;
+  const unsigned kept = cut + (a.head_parts > 1 ? a.slots : 0);   // tiles and chunks that leave parts
+  p->part = at < kept ? (((int64_t)unit * kept + at) * a.head_parts + share) * 2 * kWindowRows : -1;
   if (at >= cut) {   // a tile of keys; its queries, or the first chunk of them, end with the window
     WPlace w;
     if (!place_slot(a, at - cut, lane, &w)) return false;
@@ -234,7 +239,6 @@ __device__ __forceinline__ bool place_keys(const WindowArgs& a, int lane, KeyPla
   if (q0 >= p->len) return false;
   p->q0 = (int)q0;
   p->q1 = p->len - p->q0 < a.chunk ? p->len : p->q0 + a.chunk;
-  p->part = ((int64_t)unit * cut + at) * 2 * kWindowRows;
   return true;
 }
 
@@ -285,16 +289,17 @@ __global__ __launch_bounds__(256, T::F32 ? 1 : 2) void k_window_dkdv(WindowArgs 
     v.load(static_cast<const char*>(a.v) + ((int64_t)p.b * a.sv.b + (int64_t)p.kvh * a.sv.h + row * a.sv.t) * T::SIZE, hw);
   }
   WCopy<T> cq, cg;
-  cq.init(a.q, (int64_t)p.b * a.sq.b + (int64_t)p.kvh * a.group * a.sq.h + (int64_t)p.begin * a.sq.t, a.sq.t, wave, lane);
-  cg.init(a.dout, (int64_t)p.b * a.sdo.b + (int64_t)p.kvh * a.group * a.sdo.h + (int64_t)p.begin * a.sdo.t, a.sdo.t, wave,
+  cq.init(a.q, (int64_t)p.b * a.sq.b + ((int64_t)p.kvh * a.group + p.g0) * a.sq.h + (int64_t)p.begin * a.sq.t, a.sq.t, wave, lane);
+  cg.init(a.dout, (int64_t)p.b * a.sdo.b + ((int64_t)p.kvh * a.group + p.g0) * a.sdo.h + (int64_t)p.begin * a.sdo.t, a.sdo.t, wave,
           lane);
+  const int64_t head = (int64_t)p.b * a.heads + p.kvh * a.group + p.g0;
   const char* q_base = cq.base;
   const char* g_base = cg.base;
-  const float* l_base = a.lse2 + ((int64_t)p.b * a.heads + p.kvh * a.group) * a.seq + p.begin;
-  const float* d_base = a.ndelta + ((int64_t)p.b * a.heads + p.kvh * a.group) * a.seq + p.begin;
+  const float* l_base = a.lse2 + head * a.seq + p.begin;
+  const float* d_base = a.ndelta + head * a.seq + p.begin;
 
   // Tiles of queries, head after head.
-  const int t0 = p.q0 / T::ROWS, per_head = (p.q1 - 1) / T::ROWS - t0 + 1, n = per_head * a.group;
+  const int t0 = p.q0 / T::ROWS, per_head = (p.q1 - 1) / T::ROWS - t0 + 1, n = per_head * (p.g1 - p.g0);
   int next_g = 0, next_t = 0;   // of the tile that is copied next
   auto issue = [&](char* qd, char* gd, float (*rd)[64]) {
     cq.base = q_base + (int64_t)next_g * a.sq.h * T::SIZE;
@@ -415,9 +420,9 @@ __global__ __launch_bounds__(256, T::F32 ? 1 : 2) void k_window_dkdv(WindowArgs 
                 1.f, hw);
 }
 
-// Adds the chunks' parts of the sink tiles: a workgroup has the first chunk's
-// slot of a tile (the others' leave) and 2048 / D of its rows, 8 channels a
-// thread.
+// Adds up the parts of a tile's chunks and heads, in their order: a workgroup
+// has a tile's 2048 / D rows, 8 channels a thread.  Of a tile that is cut into
+// chunks the first chunk's does all.
 template <class T>
 __global__ __launch_bounds__(256) void k_window_join(WindowArgs a) {
   constexpr int D = T::D, ROWS = 2048 / D, PARTS = kWindowRows / ROWS;
@@ -425,27 +430,38 @@ __global__ __launch_bounds__(256) void k_window_join(WindowArgs a) {
   unsigned id = blockIdx.x;
   const int sub = id % PARTS;
   id /= PARTS;
-  const unsigned cut = (unsigned)a.sink_tiles * a.chunk_slots;
-  const unsigned unit = id / cut, at = id % cut;
-  const int tile = at / a.chunk_slots, slot = at % a.chunk_slots;
-  int begin = 0, len = a.seq;
-  if (a.cu) {
-    const int s = seq_of_slot(a.cu, a.seqs, a.seq, a.chunk, slot, lane);
-    seq_rows(a, s, &begin, &len);
-    if (slot != chunk_slot(a, begin, s)) return;
-  } else if (slot) {
-    return;
+  const unsigned cut = (unsigned)a.sink_tiles * a.chunk_slots, kept = cut + (a.head_parts > 1 ? a.slots : 0);
+  const unsigned unit = id / kept, at = id % kept;
+  int begin = 0, len = a.seq, k0, parts = a.head_parts;
+  if (at >= cut) {
+    WPlace w;
+    if (!place_slot(a, at - cut, lane, &w)) return;
+    if (a.chunk_slots && w.r0 < a.sinks) return;
+    begin = w.begin;
+    len = w.len;
+    k0 = w.r0;
+  } else {
+    const int tile = at / a.chunk_slots, slot = at % a.chunk_slots;
+    if (a.cu) {
+      const int s = seq_of_slot(a.cu, a.seqs, a.seq, a.chunk, slot, lane);
+      seq_rows(a, s, &begin, &len);
+      if (slot != chunk_slot(a, begin, s)) return;
+    } else if (slot) {
+      return;
+    }
+    k0 = tile * kWindowRows;
+    if (k0 >= len) return;
+    parts *= (len - k0 + a.chunk - 1) / a.chunk;
   }
-  const int k0 = tile * kWindowRows, r = sub * ROWS + (int)threadIdx.x / (D / 8), ch = (int)threadIdx.x % (D / 8) * 8;
+  const int r = sub * ROWS + (int)threadIdx.x / (D / 8), ch = (int)threadIdx.x % (D / 8) * 8;
   if (k0 + r >= len) return;
-  const int chunks = (len - k0 + a.chunk - 1) / a.chunk;
-  const float* from = a.part + (((int64_t)unit * cut + at) * 2 * kWindowRows + r) * D + ch;
+  const float* from = a.part + (((int64_t)unit * kept + at) * a.head_parts * 2 * kWindowRows + r) * D + ch;
   const int b = unit / a.kv_heads, kvh = unit % a.kv_heads;
   const int64_t row = begin + k0 + r;
 #pragma unroll
   for (int which = 0; which < 2; ++which) {
     float sum[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-    for (int c = 0; c < chunks; ++c) {
+    for (int c = 0; c < parts; ++c) {
       const float* x = from + ((int64_t)c * 2 + which) * kWindowRows * D;
 #pragma unroll
       for (int h = 0; h < 2; ++h) {
@@ -473,12 +489,13 @@ __global__ __launch_bounds__(256) void k_window_join(WindowArgs a) {
 template <class T, class TK>
 hipError_t launch(const WindowArgs& a, hipStream_t s) {
   const int64_t units = (int64_t)a.batch * a.kv_heads, cut = (int64_t)a.sink_tiles * a.chunk_slots;
+  const int64_t kept = cut + (a.head_parts > 1 ? a.slots : 0);
   k_window_dq<T><<<(unsigned)((int64_t)a.batch * a.heads * a.slots), 256, 0, s>>>(a);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
-  k_window_dkdv<TK><<<(unsigned)(units * (a.slots + cut)), 256, 0, s>>>(a);
-  if ((e = hipGetLastError()) != hipSuccess || !cut) return e;
-  k_window_join<T><<<(unsigned)(units * cut * (kWindowRows * T::D / 2048)), 256, 0, s>>>(a);
+  k_window_dkdv<TK><<<(unsigned)(units * (a.slots + cut) * a.head_parts), 256, 0, s>>>(a);
+  if ((e = hipGetLastError()) != hipSuccess || !kept) return e;
+  k_window_join<T><<<(unsigned)(units * kept * (kWindowRows * T::D / 2048)), 256, 0, s>>>(a);
   return hipGetLastError();
 }
 
