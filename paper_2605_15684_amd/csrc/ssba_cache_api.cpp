@@ -242,11 +242,27 @@ int64_t shared_cols(const ssba_cache* c, const ssba_cache_batch* b, const ssba_c
 
 AttendPlan plan_shared(const ssba_cache* c, const ssba_cache_batch* b, const ssba_cache_query* q,
                        const ssba_cache_prefix* x) {
-  const int64_t most = long_of(c, b), prefix = std::min<int64_t>(x->max_len, most);
-  const AttendPlan f = plan(c, b, q, false, x->groups, std::max<int64_t>(1, shared_cols(c, b, q, x)),
-                            std::max<int64_t>(1, prefix));
+  const int64_t most = long_of(c, b), prefix = std::max<int64_t>(1, std::min<int64_t>(x->max_len, most));
+  const int64_t columns = std::max<int64_t>(1, shared_cols(c, b, q, x));
+  AttendPlan f = plan(c, b, q, false, x->groups, columns, prefix);
+  const int64_t narrow = (int64_t)x->groups * c->kv_heads * ceil_div(columns, 32);
+  if (f.tiles > 2 && narrow * prefix <= 512 * 1024) {
+    // Columns for more than 32 a workgroup, but not the keys to fill the chip with such: 32 columns, about 256
+    // workgroups (256 columns of 4 heads over 8192 keys, D 128: 15 us, 256 columns a workgroup 28 to 32, 128 20 to 22,
+    // 64 18 to 21; 512 workgroups of 32 columns 16).
+    f.tiles = 2;
+    f.threads = 256;
+    f.col_tiles = (int)ceil_div(columns, 32);
+    f.items = narrow;
+    f.splits = (int)std::max<int64_t>(1, std::min<int64_t>(256 / narrow, prefix / 256));
+  }
   const int64_t cols = std::max<int64_t>(1, (int64_t)(q->heads / c->kv_heads) * b->max_new);
-  AttendPlan p = plan(c, b, q, false, b->seqs, cols, std::max<int64_t>(1, most - prefix));
+  const int64_t rest = std::max<int64_t>(1, most - prefix);
+  AttendPlan p = plan(c, b, q, false, b->seqs, cols, rest);
+  if (p.tiles == 1 && rest <= 2048) {   // one workgroup each, that also adds the prefix's parts
+    p.splits = 1;
+    if (rest > 256) p.threads = 512;
+  }
   p.kind = ssba::kAttendShared;
   p.prefix_tiles = f.tiles;
   p.prefix_threads = f.threads;
@@ -493,6 +509,9 @@ ssba_status ssba_cache_attend_shared(const ssba_cache* c, int32_t layer, const s
   a.groups = x->groups;
   a.shared_cols = (int)shared_cols(c, b, q, x);
   a.tiles = p.tiles;
+  a.prefix_cols = p.prefix_tiles * 16;
+  a.prefix_col_tiles = p.prefix_col_tiles;
+  a.prefix_splits = p.prefix_splits;
   a.part = static_cast<float*>(scratch);
   a.prefix_part = a.part + rest_columns(p) * c->head_dim;
   a.part_ml = a.prefix_part + prefix_columns(p) * c->head_dim;

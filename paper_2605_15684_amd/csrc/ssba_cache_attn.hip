@@ -145,7 +145,7 @@ struct Shape {
   static constexpr int D = D_, R = R_, NQ = NQ_, NP = NP_, CG = CG_, KP = KP_, J = J_;
   static constexpr bool F32 = F32_, LISTED = LISTED_, QLDS = QLDS_;
   static constexpr int SPAN = SPAN_;
-  static constexpr bool PARTS = SPAN == kSpanPrefix || SPAN == kSpanRest;   // to be joined whatever the splits
+  static constexpr bool PARTS = SPAN == kSpanPrefix;   // to be joined whatever the splits
   static constexpr bool HALF = !F32 && NP == 1;   // the second product in fp16
   static constexpr int THREADS = 64 * CG * KP;
   static constexpr int NH = D / 64;   // 64-channel blocks
@@ -291,6 +291,8 @@ __global__ __launch_bounds__(P::THREADS, P::R > 1 || (P::D == 128 && (P::J > 1 |
   const int unit = id / a.c.kv_heads;
   // LISTED with several column groups: they are rows.
   int prefix = 0;   // tokens of the shared pages
+  int64_t prefix_item = 0;   // kSpanRest: first item of the prefixes of this group and head, and the column there of
+  int prefix_col = 0;        // this sequence's first
   bool there = true;
   if (P::SPAN == kSpanPrefix) {
     const GroupView v = group_view(a, unit, lane);
@@ -308,6 +310,10 @@ __global__ __launch_bounds__(P::THREADS, P::R > 1 || (P::D == 128 && (P::J > 1 |
     int gr;
     GroupView v;
     prefix = pages_shared(a, it.seq, it.sv, lane, &gr, &v) << page_log2;
+    if (prefix) {
+      prefix_item = ((int64_t)gr * a.c.kv_heads + it.h) * a.prefix_col_tiles;
+      prefix_col = (it.sv.begin - v.begin) * a.group;
+    }
   }
   const int cbase = (P::LISTED ? ct : ct * P::CG + cg) * P::COLS;
   if ((P::CG == 1 || P::KP == 1) && cbase >= it.ncols) return;
@@ -885,6 +891,34 @@ __global__ __launch_bounds__(P::THREADS, P::R > 1 || (P::D == 128 && (P::J > 1 |
         ml[1] = sum;
       }
     } else {
+      if (P::SPAN == kSpanRest && prefix) {
+        // The parts of the prefix, of which there are few: their maxima first.
+        const int col = prefix_col + cc;
+        const int64_t slot = (prefix_item + col / a.prefix_cols) * a.prefix_splits * a.prefix_cols + col % a.prefix_cols;
+        const float* ml = a.prefix_ml + slot * 2;
+        const float* part = a.prefix_part + slot * D + ch;
+        float top = cm;
+#pragma unroll 8
+        for (int x = 0; x < a.prefix_splits; ++x) top = fmaxf(top, ml[(int64_t)x * a.prefix_cols * 2]);
+        if (top > cm) {
+          const float f = exp2_(cm - top);
+          sum = shrink(sum, cm - top);
+#pragma unroll
+          for (int e = 0; e < E; ++e) acc[e] *= f;
+        }
+#pragma unroll 8
+        for (int x = 0; x < a.prefix_splits; ++x) {
+          const float mx = ml[(int64_t)x * a.prefix_cols * 2], lx = ml[(int64_t)x * a.prefix_cols * 2 + 1];
+          const float f = mx == top ? 1.f : exp2_(mx - top);
+          sum += mx == top ? lx : shrink(lx, mx - top);
+#pragma unroll
+          for (int e = 0; e < E; e += 4) {
+            const floatx4 y = *reinterpret_cast<const floatx4*>(part + (int64_t)x * a.prefix_cols * D + e);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) acc[e + i] = __builtin_fmaf(y[i], f, acc[e + i]);
+          }
+        }
+      }
       const float inv = sum == 0.f ? 0.f : 1.f / sum;
 #pragma unroll
       for (int e = 0; e < E; ++e) acc[e] *= inv;
@@ -961,8 +995,8 @@ __global__ __launch_bounds__(256) void k_cache_join(AttendArgs a) {
   store_row<F32, 4>(a.o, row_at<LISTED>(a, it, c0 + c, a.o_st, a.o_sh) + ch, w);
 }
 
-// Joins the parts of shared prefixes and of what is behind them, as the join
-// above: r has the launch of the rests (its items are this one's), p that of the
+// Joins the parts of shared prefixes and of what is behind them where that is
+// in parts as well (else its own launch adds the prefix's), as the join above: r has the launch of the rests (its items are this one's), p that of the
 // prefixes.  A token's columns of its group begin with those of the sequences
 // before it.
 template <int D, bool F32>
@@ -1044,7 +1078,7 @@ template <typename P>
 hipError_t launch(const AttendArgs& a, const AttendPlan& p, hipStream_t s) {
   k_cache_attend<P><<<(unsigned)(p.items * p.splits), P::THREADS, 0, s>>>(a);
   const hipError_t e = hipGetLastError();
-  if (e != hipSuccess || P::PARTS || p.splits == 1) return e;
+  if (e != hipSuccess || P::SPAN >= kSpanPrefix || p.splits == 1) return e;
   constexpr int RC = P::LISTED ? P::R : P::CG * P::R;
   k_cache_join<P::D, RC, P::F32, P::LISTED><<<(unsigned)(p.items * RC * (P::D / 32)), 256, 0, s>>>(a);
   return hipGetLastError();
@@ -1097,7 +1131,7 @@ hipError_t launch_d(const AttendArgs& a, const AttendPlan& p, int dtype, hipStre
       pp.threads = p.prefix_threads;
       pp.items = p.prefix_items;
       hipError_t e = launch_seq<D, kSpanPrefix>(pre, pp, f32, s);
-      if (e != hipSuccess || (e = launch_seq<D, kSpanRest>(a, p, f32, s)) != hipSuccess) return e;
+      if (e != hipSuccess || (e = launch_seq<D, kSpanRest>(a, p, f32, s)) != hipSuccess || p.splits == 1) return e;
       const unsigned grid = (unsigned)(p.items * p.tiles * (D / 32));
       if (f32)
         k_cache_join_shared<D, true><<<grid, 256, 0, s>>>(a, pre);

@@ -122,6 +122,7 @@ struct AttendArgs {
   int tiles;              // tiles of 16 columns of an item
   float* prefix_part;     // part and part_ml of the prefixes
   float* prefix_ml;
+  int prefix_cols, prefix_col_tiles, prefix_splits;   // of the prefixes: columns of an item, column tiles, splits
 };
 
 // What the attention launch does (ssba_cache_api.cpp decides).
