@@ -190,7 +190,7 @@ def load(path: str = None) -> ctypes.CDLL:
     lib.ssba_probe_mfma.argtypes = [ctypes.c_int32, ctypes.c_int32, vp, vp]
     i32, i64 = ctypes.c_int32, ctypes.c_int64
     cp, bp, qp, pp = (ctypes.POINTER(t) for t in (CacheDesc, CacheBatch, CacheQuery, CachePages))
-    rp, tp, wp, gp, xp = (ctypes.POINTER(t) for t in (RopeDesc, RopeTensor, WindowDesc, WindowGrads, CachePrefix))
+    rp, xp = (ctypes.POINTER(t) for t in (RopeDesc, CachePrefix))
     for name, args in (("ssba_build_index_ex", [dp, vp, vp, vp, sz, vp, sz, vp]),
                        ("ssba_forward_ex", [dp, vp, vp, vp, vp, sz, vp, vp]),
                        ("ssba_forward_topk_ex", [dp, vp, vp, vp, vp, sz, vp, sz, vp, vp]),
@@ -220,10 +220,10 @@ def load(path: str = None) -> ctypes.CDLL:
                        ("ssba_cache_attend_window", [cp, i32, bp, qp, i32, i32, vp, vp, vp, sz, vp]),
                        ("ssba_cache_attend_shared_workspace_size", [cp, bp, qp, xp, ctypes.POINTER(sz)]),
                        ("ssba_cache_attend_shared", [cp, i32, bp, qp, xp, vp, vp, vp, sz, vp]),
-                       ("ssba_rope_rotate", [rp, i32, i32, i32, i32, vp, i64, i64, i32, tp, vp]),
-                       ("ssba_window_forward", [wp, vp, vp, vp, vp, vp, vp]),
-                       ("ssba_window_backward_workspace_size", [wp, ctypes.POINTER(sz)]),
-                       ("ssba_window_backward", [wp, gp, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, sz, vp])):
+                       ("ssba_rope_rotate", [rp, i32, i32, i32, i32, vp, i64, i64, i32, vp, vp]),
+                       ("ssba_window_forward", [vp, vp, vp, vp, vp, vp, vp]),
+                       ("ssba_window_backward_workspace_size", [vp, ctypes.POINTER(sz)]),
+                       ("ssba_window_backward", [vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, sz, vp])):
         fn = getattr(lib, name)
         fn.restype = ctypes.c_int
         fn.argtypes = args

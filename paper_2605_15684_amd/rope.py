@@ -13,6 +13,7 @@ from __future__ import annotations
 
 import ctypes
 import math
+import struct
 from typing import Optional, Sequence
 
 import torch
@@ -85,25 +86,32 @@ def plan(head_dim: int, sections: Sequence[int], *, theta: float = 10000.0, spec
     return Plan(head_dim, len(sections), axis, freq, pairs)
 
 
-def _tensor(t, like, dims, d, index, what):
-    """Checks a [tokens, heads, D] or [B, H, T, D] tensor (like: of its shape and type); its heads and strides."""
-    if not (isinstance(t, torch.Tensor) and t.is_cuda and t.dim() in (3, 4) and t.dtype in _DTYPES):
-        raise ValueError(f"{what}: expected a [tokens, heads, D] or [B, H, T, D] GPU tensor, bf16 or fp32")
+# ssba_rope_tensor as bytes: a call of this module costs a few microseconds on the host, of which filling ctypes
+# structures would be as many again.
+_TENSOR = struct.Struct("=i4xQQ6q")
+assert _TENSOR.size == ctypes.sizeof(_lib.RopeTensor)
+
+
+def _tensor(t, dtype, dim: int, batch: int, rows: int, d: int, index: int, what: str):
+    """Checks a [tokens, heads, D] or [B, H, T, D] tensor; its heads and (batch, head, token) strides."""
+    if not isinstance(t, torch.Tensor) or t.dtype is not dtype or t.dim() != dim:
+        raise ValueError(f"{what}: expected a tensor of q's type and dimensions")
     if t.get_device() != index:
         raise ValueError(f"{what}: all tensors must be on one device")
-    if t.shape[-1] != d:
-        raise ValueError(f"{what}: the plan is for head_dim {d}")
-    if t.dim() == 3:
-        (n, h, _), (st, sh, sc) = t.shape, t.stride()
-        b, sb = 1, 0
+    if dim == 3:
+        n, h, e = t.shape
+        b = 1
     else:
-        (b, h, n, _), (sb, sh, st, sc) = t.shape, t.stride()
-    if (b, n) != dims[:2] or t.dim() != dims[2]:
-        raise ValueError(f"{what}: expected the tokens and dimensions of q")
-    if like is not None and (t.dtype != like.dtype or t.shape != like.shape):
-        raise ValueError(f"{what}: expected the type and shape of its input")
-    if t.numel() == 0:
-        return h, 0, 0, 0
+        b, h, n, e = t.shape
+    if e != d or b != batch or n != rows:
+        raise ValueError(f"{what}: expected the tokens of q, and head_dim {d} as the plan")
+    if t.is_contiguous():
+        return (h, 0, d, h * d) if dim == 3 else (h, h * n * d, n * d, d)
+    if dim == 3:
+        st, sh, sc = t.stride()
+        sb = 0
+    else:
+        sb, sh, st, sc = t.stride()
     if sc != 1:
         raise ValueError(f"{what}: channel stride must be 1")
     # A dimension of one has no stride that matters; torch may report any.
@@ -115,12 +123,6 @@ def _tensor(t, like, dims, d, index, what):
     return h, sb, sh, st
 
 
-def _int32(what, *numbers):
-    for x in numbers:
-        if not -0x80000000 <= x < 0x80000000:
-            raise ValueError(f"{what}: outside int32")
-
-
 def rotate(plan: Plan, pos: torch.Tensor, q: torch.Tensor, k: Optional[torch.Tensor] = None, *, inverse: bool = False,
            q_out: Optional[torch.Tensor] = None, k_out: Optional[torch.Tensor] = None):
     """q (and k, of another number of heads) turned by the positions of their tokens; with `inverse` turned back, which
@@ -128,46 +130,48 @@ def rotate(plan: Plan, pos: torch.Tensor, q: torch.Tensor, k: Optional[torch.Ten
     [B, T, axes].  q_out and k_out may be q and k themselves.  Returns q_out or (q_out, k_out)."""
     if not isinstance(plan, Plan):
         raise ValueError("plan: expected a rope.Plan")
-    if not (isinstance(q, torch.Tensor) and q.is_cuda and q.dim() in (3, 4)):
+    if not isinstance(q, torch.Tensor) or not q.is_cuda or q.dim() not in (3, 4) or q.dtype not in _DTYPES:
         raise ValueError("q: expected a [tokens, heads, D] or [B, H, T, D] GPU tensor, bf16 or fp32")
-    index = q.get_device()
-    batch, rows = (1, q.shape[0]) if q.dim() == 3 else (q.shape[0], q.shape[2])
-    _int32("q", batch, rows)
-    if not (isinstance(pos, torch.Tensor) and pos.dtype is torch.int32 and pos.get_device() == index and
-            pos.dim() in (2, q.dim() - 1) and pos.shape[-1] == plan.axes and pos.shape[-2] == rows and
-            (pos.dim() == 2 or pos.shape[0] == batch)):
+    index, dim, dtype, d = q.get_device(), q.dim(), q.dtype, plan.head_dim
+    batch, rows = (1, q.shape[0]) if dim == 3 else (q.shape[0], q.shape[2])
+    if not isinstance(pos, torch.Tensor) or pos.dtype is not torch.int32 or pos.get_device() != index or \
+            pos.dim() not in (2, dim - 1) or pos.shape[-1] != plan.axes or pos.shape[-2] != rows or \
+            (pos.dim() == 3 and pos.shape[0] != batch):
         raise ValueError(f"pos: expected an int32 tensor [tokens, {plan.axes}]" +
-                         (f" or [B, T, {plan.axes}]" if q.dim() == 4 else "") + " on q's device")
+                         (f" or [B, T, {plan.axes}]" if dim == 4 else "") + " on q's device")
     if plan.axes > 1 and pos.numel() and pos.stride(-1) != 1:
         raise ValueError("pos: the axes of a token must be contiguous")
-    dims = (batch, rows, q.dim())
-    pairs = [("q", q, q_out)]
+    h, *strides = _tensor(q, dtype, dim, batch, rows, d, index, "q")
+    if q_out is None:
+        q_out = torch.empty_like(q, memory_format=torch.contiguous_format)
+    elif isinstance(q_out, torch.Tensor) and q_out.shape != q.shape:
+        raise ValueError("q_out: expected the shape of q")
+    most = h
+    desc = _TENSOR.pack(h, q.data_ptr(), q_out.data_ptr(), *strides,
+                        *_tensor(q_out, dtype, dim, batch, rows, d, index, "q_out")[1:])
     if k is not None:
-        pairs.append(("k", k, k_out))
-        if k.dtype != q.dtype:
-            raise ValueError("q and k must share their type")
+        h, *strides = _tensor(k, dtype, dim, batch, rows, d, index, "k")
+        if k_out is None:
+            k_out = torch.empty_like(k, memory_format=torch.contiguous_format)
+        elif isinstance(k_out, torch.Tensor) and k_out.shape != k.shape:
+            raise ValueError("k_out: expected the shape of k")
+        most = max(most, h)
+        desc += _TENSOR.pack(h, k.data_ptr(), k_out.data_ptr(), *strides,
+                             *_tensor(k_out, dtype, dim, batch, rows, d, index, "k_out")[1:])
     elif k_out is not None:
         raise ValueError("k_out without k")
-    arr = (_lib.RopeTensor * len(pairs))()
-    outs = []
-    for i, (name, x, y) in enumerate(pairs):
-        xs = _tensor(x, None, dims, plan.head_dim, index, name)
-        if y is None:
-            y = torch.empty_like(x, memory_format=torch.contiguous_format)
-        ys = _tensor(y, x, dims, plan.head_dim, index, name + "_out")
-        _int32(name, xs[0])
-        arr[i] = _lib.RopeTensor(xs[0], x.data_ptr(), y.data_ptr(), *xs[1:], *ys[1:])
-        outs.append(y)
-    if q.numel() == 0 and (k is None or k.numel() == 0):
-        return outs[0] if k is None else tuple(outs)
-    sb = pos.stride(0) if pos.dim() == 3 and batch > 1 else 0
-    st = pos.stride(-2) if rows > 1 else 0
-    args = (plan.desc, _DTYPES[q.dtype], 1 if inverse else 0, batch, rows, pos.data_ptr(), sb, st, len(pairs), arr)
-    if _current_device() == index:
-        status = _L.ssba_rope_rotate(*args, _raw_stream(index))
-    else:
-        with torch.cuda.device(index):
+    for x in (batch, rows, most):
+        if x >= 1 << 31:
+            raise ValueError("q: outside int32")
+    if q.numel() or (k is not None and k.numel()):
+        args = (plan.desc, _DTYPES[dtype], 1 if inverse else 0, batch, rows, pos.data_ptr(),
+                pos.stride(0) if pos.dim() == 3 and batch > 1 else 0, pos.stride(-2) if rows > 1 else 0,
+                1 if k is None else 2, desc)
+        if _current_device() == index:
             status = _L.ssba_rope_rotate(*args, _raw_stream(index))
-    if status:
-        _lib.check(status, "ssba_rope_rotate")
-    return outs[0] if k is None else tuple(outs)
+        else:
+            with torch.cuda.device(index):
+                status = _L.ssba_rope_rotate(*args, _raw_stream(index))
+        if status:
+            _lib.check(status, "ssba_rope_rotate")
+    return q_out if k is None else (q_out, k_out)

@@ -13,6 +13,7 @@ that reads the paged cache is cache.attend_window.
 from __future__ import annotations
 
 import ctypes
+import struct
 from typing import Optional, Tuple
 
 import torch
@@ -41,26 +42,30 @@ def _call(index: int, fn, name: str, *args) -> None:
         _lib.check(st, name)
 
 
-def _int32(what: str, *numbers) -> None:
-    """The library's numbers are int32, and ctypes would cut larger ones."""
-    for x in numbers:
-        if not -0x80000000 <= x < 0x80000000:
-            raise ValueError(f"{what}: outside int32")
+# ssba_window and ssba_window_grads as bytes: a call of this module costs a few microseconds on the host, of which
+# filling ctypes structures would be as many again.
+_DESC = struct.Struct("=10if4xQ12q")
+_GRADS = struct.Struct("=12q")
+assert _DESC.size == ctypes.sizeof(_lib.WindowDesc) and _GRADS.size == ctypes.sizeof(_lib.WindowGrads)
 
 
-def _strides(t, shape, like, what: str) -> _lib.Strides:
-    """Checks a tensor of `shape` and of like's type and device; its strides."""
-    if not (isinstance(t, torch.Tensor) and t.is_cuda and t.dtype == like.dtype and t.shape == shape):
-        raise ValueError(f"{what}: expected a {like.dtype} GPU tensor of shape {tuple(shape)}")
-    if t.get_device() != like.get_device():
+def _strides(t, shape, dtype, index: int, what: str) -> Tuple[int, int, int]:
+    """Checks a tensor of a shape, type and device; its (batch, head, row) strides."""
+    if not isinstance(t, torch.Tensor) or t.dtype is not dtype or t.shape != shape:
+        raise ValueError(f"{what}: expected a {dtype} GPU tensor of shape {tuple(shape)}")
+    if t.get_device() != index:
         raise ValueError(f"{what}: all tensors must be on one device")
-    if t.dim() == 3:
-        (n, h, d), (st, sh, sc) = t.shape, t.stride()
+    if len(shape) == 3:
+        n, h, d = shape
+        if t.is_contiguous():
+            return 0, d, h * d
+        st, sh, sc = t.stride()
         b, sb = 1, 0
     else:
-        (b, h, n, d), (sb, sh, st, sc) = t.shape, t.stride()
-    if t.numel() == 0:
-        return _lib.Strides(0, 0, 0)
+        b, h, n, d = shape
+        if t.is_contiguous():
+            return h * n * d, n * d, d
+        sb, sh, st, sc = t.stride()
     if sc != 1:
         raise ValueError(f"{what}: channel stride must be 1")
     # A dimension of one has no stride that matters; torch may report any.
@@ -69,32 +74,30 @@ def _strides(t, shape, like, what: str) -> _lib.Strides:
     sb = sb if b > 1 else 0
     if st < d or sh < d or (b > 1 and sb < d):
         raise ValueError(f"{what}: rows and heads must not overlap")
-    return _lib.Strides(sb, sh, st)
+    return sb, sh, st
 
 
-def _desc(q, k, v, o, window: int, sinks: int, scale: Optional[float], cu, max_len: Optional[int]):
-    if not (isinstance(q, torch.Tensor) and q.is_cuda and q.dim() in (3, 4) and q.dtype in _DTYPES):
+def _desc(q, k, v, o, window: int, sinks: int, scale: Optional[float], cu, max_len: Optional[int]) -> bytes:
+    if not isinstance(q, torch.Tensor) or not q.is_cuda or q.dim() not in (3, 4) or q.dtype not in _DTYPES:
         raise ValueError("q: expected a [B, H, T, D] or [rows, H, D] GPU tensor, bf16 or fp32")
-    if not (isinstance(k, torch.Tensor) and k.dim() == q.dim()):
+    if not isinstance(k, torch.Tensor) or k.dim() != q.dim():
         raise ValueError("k: expected a tensor of q's dimensions")
-    if q.dim() == 4:
+    index, dtype, qs, kv = q.get_device(), q.dtype, q.shape, k.shape[1]
+    if len(qs) == 4:
         if cu is not None:
             raise ValueError("cu goes with packed [rows, H, D] tensors")
-        batch, heads, rows, d = q.shape
-        kv = k.shape[1]
-        shape, seqs, at = (batch, kv, rows, d), 0, None
+        batch, heads, rows, d = qs
+        shape, seqs, at = torch.Size((batch, kv, rows, d)), 0, 0
     else:
-        rows, heads, d = q.shape
-        kv = k.shape[1]
-        batch, shape = 1, (rows, kv, d)
-        if not (isinstance(cu, torch.Tensor) and cu.dtype is torch.int32 and cu.dim() == 1 and cu.shape[0] > 1 and
-                cu.is_contiguous() and cu.get_device() == q.get_device()):
+        rows, heads, d = qs
+        batch, shape = 1, torch.Size((rows, kv, d))
+        if not isinstance(cu, torch.Tensor) or cu.dtype is not torch.int32 or cu.dim() != 1 or cu.shape[0] < 2 or \
+                not cu.is_contiguous() or cu.get_device() != index:
             raise ValueError("cu: expected a contiguous int32 tensor [sequences + 1] on q's device with packed tensors")
         seqs, at = cu.shape[0] - 1, cu.data_ptr()
     if kv < 1 or heads % kv:
         raise ValueError("q must have a multiple of k's heads")
     window, sinks, max_len = int(window), int(sinks), int(max_len or 0)
-    _int32("shape, window, sinks or max_len", batch, rows, heads, window, sinks, max_len, seqs)
     if window < 1 or sinks < 0:
         raise ValueError("window must be 1 or more, sinks 0 or more")
     if scale is None:
@@ -103,9 +106,12 @@ def _desc(q, k, v, o, window: int, sinks: int, scale: Optional[float], cu, max_l
         scale = ctypes.c_float(scale).value
         if not scale > 0.0:
             raise ValueError("scale must be positive in fp32 (None: 1 / sqrt(D))")
-    return _lib.WindowDesc(batch, rows, heads, kv, d, _DTYPES[q.dtype], window, sinks, seqs, max_len, scale, at,
-                           _strides(q, q.shape, q, "q"), _strides(k, shape, q, "k"), _strides(v, shape, q, "v"),
-                           _strides(o, q.shape, q, "out"))
+    strides = _strides(q, qs, dtype, index, "q") + _strides(k, shape, dtype, index, "k") + \
+        _strides(v, shape, dtype, index, "v") + _strides(o, qs, dtype, index, "out")
+    try:
+        return _DESC.pack(batch, rows, heads, kv, d, _DTYPES[dtype], window, sinks, seqs, max_len, scale, at, *strides)
+    except struct.error as e:
+        raise ValueError(f"shape, window, sinks or max_len: outside int32 ({e})") from None
 
 
 def _lse_shape(q):
@@ -147,8 +153,9 @@ def backward(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, out: torch.Tenso
     _check_lse(lse, q)
     mk = lambda t, like: torch.empty_like(like, memory_format=torch.contiguous_format) if t is None else t
     dq, dk, dv = mk(dq, q), mk(dk, k), mk(dv, v)
-    grads = _lib.WindowGrads(_strides(dout, q.shape, q, "dout"), _strides(dq, q.shape, q, "dq"),
-                             _strides(dk, k.shape, q, "dk"), _strides(dv, v.shape, q, "dv"))
+    index, dtype = q.get_device(), q.dtype
+    grads = _GRADS.pack(*_strides(dout, q.shape, dtype, index, "dout"), *_strides(dq, q.shape, dtype, index, "dq"),
+                        *_strides(dk, k.shape, dtype, index, "dk"), *_strides(dv, v.shape, dtype, index, "dv"))
     size = ctypes.c_size_t(0)
     _lib.check(_L.ssba_window_backward_workspace_size(desc, size), "ssba_window_backward_workspace_size")
     if scratch is None:
