@@ -245,7 +245,8 @@ __device__ __forceinline__ void rows_products(floatx16& acc1, const char* half1,
 }
 
 // acc[db] += (channels 32 db .. of the half's rows)^T x, x a 32 x 32 result.
-template <class T>
+// TERMS: bf16 terms of x, each the rounding of what the ones before leave.
+template <class T, int TERMS = 1>
 __device__ __forceinline__ void cols_product(floatx16 (&acc)[T::NDB], const char* half, const floatx16& x, const WLane<T>& l) {
   if constexpr (T::F32) {
 #pragma unroll
@@ -257,14 +258,26 @@ __device__ __forceinline__ void cols_product(floatx16 (&acc)[T::NDB], const char
         acc[db] = __builtin_amdgcn_mfma_f32_32x32x2f32(w, x[j], acc[db], 0, 0, 0);
       }
   } else {
-    uint32_t pk[8];
+    uint32_t pk[TERMS][8];
 #pragma unroll
-    for (int j = 0; j < 8; ++j) pk[j] = pack2(x[2 * j], x[2 * j + 1]);
+    for (int j = 0; j < 8; ++j) {
+      float a = x[2 * j], b = x[2 * j + 1];
+#pragma unroll
+      for (int t = 0; t < TERMS; ++t) {
+        pk[t][j] = pack2(a, b);
+        a -= __uint_as_float(pk[t][j] << 16);
+        b -= __uint_as_float(pk[t][j] & 0xFFFF0000u);
+      }
+    }
 #pragma unroll
     for (int ks = 0; ks < 2; ++ks)
 #pragma unroll
-      for (int db = 0; db < T::NDB; ++db)
-        acc[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(col_operand<T>(half, l, ks, db), packed_frag(pk, ks), acc[db], 0, 0, 0);
+      for (int db = 0; db < T::NDB; ++db) {
+        const bf16x8 w = col_operand<T>(half, l, ks, db);
+#pragma unroll
+        for (int t = TERMS - 1; t >= 0; --t)
+          acc[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(w, packed_frag(pk[t], ks), acc[db], 0, 0, 0);
+      }
   }
 }
 
