@@ -246,7 +246,7 @@ AttendPlan plan_shared(const ssba_cache* c, const ssba_cache_batch* b, const ssb
   const int64_t columns = std::max<int64_t>(1, shared_cols(c, b, q, x));
   AttendPlan f = plan(c, b, q, false, x->groups, columns, prefix);
   const int64_t narrow = (int64_t)x->groups * c->kv_heads * ceil_div(columns, 32);
-  if (f.tiles > 2 && narrow * prefix <= 512 * 1024) {
+  if (f.tiles > 2 && (double)narrow * prefix <= 512 * 1024) {
     // Columns for more than 32 a workgroup, but not the keys to fill the chip with such: 32 columns, about 256
     // workgroups (256 columns of 4 heads over 8192 keys, D 128: 15 us, 256 columns a workgroup 28 to 32, 128 20 to 22,
     // 64 18 to 21; 512 workgroups of 32 columns 16).
@@ -279,8 +279,9 @@ size_t attend_scratch(const ssba_cache* c, const AttendPlan& p) {
   return part_columns(p) * (c->head_dim + 2) * sizeof(float);
 }
 
-// Columns of the parts of a launch of shared prefixes: those of the rests, then the prefixes'.
-size_t rest_columns(const AttendPlan& p) { return (size_t)p.items * p.splits * p.tiles * 16; }
+// Columns of the parts of a launch of shared prefixes (one that fits, see shared_fits): of the rests where these are
+// in parts, then of the prefixes.
+size_t rest_columns(const AttendPlan& p) { return part_columns(p); }
 size_t prefix_columns(const AttendPlan& p) { return (size_t)p.prefix_items * p.prefix_splits * p.prefix_tiles * 16; }
 
 size_t shared_scratch(const ssba_cache* c, const AttendPlan& p) {
@@ -288,6 +289,11 @@ size_t shared_scratch(const ssba_cache* c, const AttendPlan& p) {
 }
 
 bool too_many(int64_t groups) { return groups > ssba::kMaxGroups256; }
+
+bool shared_fits(const AttendPlan& p) {
+  return !too_many(p.items * p.splits * 4) && !too_many(p.items * p.tiles * 4) &&
+         !too_many(p.prefix_items * p.prefix_splits * 4) && !too_many(p.prefix_items * p.prefix_tiles * 4);
+}
 
 ssba_status check_prefix(const ssba_cache* c, const ssba_cache_batch* b, const ssba_cache_query* q,
                          const ssba_cache_prefix* x) {
@@ -485,7 +491,9 @@ ssba_status ssba_cache_attend_shared_workspace_size(const ssba_cache* c, const s
   if ((st = check_batch(c, b)) != SSBA_OK || (st = check_query(c, b, q)) != SSBA_OK ||
       (st = check_prefix(c, b, q, x)) != SSBA_OK)
     return st;
-  if (scratch_bytes) *scratch_bytes = shared_scratch(c, plan_shared(c, b, q, x));
+  const AttendPlan p = plan_shared(c, b, q, x);
+  if (!shared_fits(p)) return SSBA_ERR_UNSUPPORTED;
+  if (scratch_bytes) *scratch_bytes = shared_scratch(c, p);
   return SSBA_OK;
 }
 
@@ -499,11 +507,9 @@ ssba_status ssba_cache_attend_shared(const ssba_cache* c, int32_t layer, const s
   if (!attend_arrays(q, query, o) || !x->first || !x->pages || !aligned(x->first, 4) || !aligned(x->pages, 4))
     return SSBA_ERR_ARG;
   const AttendPlan p = plan_shared(c, b, q, x);
+  if (!shared_fits(p)) return SSBA_ERR_UNSUPPORTED;
   if (!scratch || !aligned(scratch, 16)) return SSBA_ERR_ARG;
   if (scratch_bytes < shared_scratch(c, p)) return SSBA_ERR_WORKSPACE;
-  if (too_many(p.items * p.splits * 4) || too_many(p.items * p.tiles * 4) ||
-      too_many(p.prefix_items * p.prefix_splits * 4))
-    return SSBA_ERR_UNSUPPORTED;
   a.first = x->first;
   a.shared = x->pages;
   a.groups = x->groups;

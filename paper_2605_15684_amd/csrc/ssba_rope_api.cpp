@@ -37,7 +37,7 @@ ssba_status strides_of(int dtype, int64_t batch, int64_t heads, int64_t rows, in
     *sb = heads * rows * d;
   }
   if (*sb < 0 || *sh < 0 || *st < 0) return SSBA_ERR_SHAPE;
-  if ((rows > 1 && *st < d) || (heads > 1 && *sh < d) || (out && batch > 1 && *sb < d)) return SSBA_ERR_SHAPE;
+  if (rows > 0 && ((rows > 1 && *st < d) || (heads > 1 && *sh < d) || (out && batch > 1 && *sb < d))) return SSBA_ERR_SHAPE;
   if (dtype == SSBA_DT_BF16 && ((*sb | *sh | *st) & 7)) return SSBA_ERR_UNSUPPORTED;
   if ((double)batch * *sb + (double)heads * *sh + (double)rows * *st > 2.0e18) return SSBA_ERR_SHAPE;
   return SSBA_OK;

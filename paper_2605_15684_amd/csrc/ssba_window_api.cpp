@@ -45,8 +45,8 @@ ssba_status strides_of(const ssba_window* w, int heads, bool out, const ssba_str
     s->b = heads * s->h;
   }
   if (s->b < 0 || s->h < 0 || s->t < 0) return SSBA_ERR_SHAPE;
-  if ((w->seq > 1 && s->t < w->head_dim) || (heads > 1 && s->h < w->head_dim) ||
-      (out && w->batch > 1 && s->b < w->head_dim))
+  if ((w->seq > 1 && s->t < w->head_dim) || (w->seq > 0 && heads > 1 && s->h < w->head_dim) ||
+      (out && w->seq > 0 && w->batch > 1 && s->b < w->head_dim))
     return SSBA_ERR_SHAPE;
   if ((s->b | s->h | s->t) & (w->dtype == SSBA_DT_BF16 ? 7 : 3)) return SSBA_ERR_UNSUPPORTED;
   if (s->t > (1 << 20)) return SSBA_ERR_UNSUPPORTED;
@@ -75,6 +75,7 @@ ssba_status plan(const ssba_window* w, WindowArgs* a) {
   a->scale = w->softmax_scale > 0.f ? w->softmax_scale : 1.0f / std::sqrt((float)w->head_dim);
   a->scale_log2 = a->scale * kLog2e;
   a->slots = w->seqs ? w->seq / kWindowRows + w->seqs + 1 : (int)ceil_div(w->seq, kWindowRows);
+  if ((double)w->batch * w->heads * a->slots > (double)ssba::kMaxGroups256) return SSBA_ERR_UNSUPPORTED;
   // Tiles of every head in turn, long ones first, where the heads go evenly to the XCDs or tiles differ much in length;
   // else the tiles of a head together.
   const int64_t units = (int64_t)w->batch * w->kv_heads;
@@ -98,8 +99,10 @@ ssba_status plan(const ssba_window* w, WindowArgs* a) {
   a->head_parts = 1;
   for (int n = 2; n <= a->group && n <= most && tiles * a->head_parts < room; ++n)
     if (a->group % n == 0) a->head_parts = n;
-  if ((double)w->batch * w->heads * a->slots > (double)ssba::kMaxGroups256 ||
-      (double)units * (a->slots + cut) * (a->head_parts > 1 ? 8 * a->head_parts : 8) > (double)ssba::kMaxGroups256)
+  // The key side's launch, and the join's of 8 workgroups a part.
+  const int64_t kept = cut + (a->head_parts > 1 ? a->slots : 0);
+  if ((double)units * (a->slots + cut) * a->head_parts > (double)ssba::kMaxGroups256 ||
+      (double)units * kept * 8 > (double)ssba::kMaxGroups256)
     return SSBA_ERR_UNSUPPORTED;
   return SSBA_OK;
 }
