@@ -24,19 +24,13 @@ namespace {
 constexpr float kMost = 1048576.f;   // a lane's sum of probabilities of a half tile: 2^20
 constexpr float kLn2 = 0.69314718055994530942f;
 
-template <class T>
-__global__ __launch_bounds__(256, 2) void k_window_forward(WindowArgs a) {
+// The wave's queries over all key tiles.  CAREFUL: one tile at a time, the
+// other buffers are room for the rows' weights.
+template <class T, bool CAREFUL>
+__device__ __forceinline__ void forward_pass(const WindowArgs& a, const WPlace& p, int wave, int lane, char* kA, char* kB,
+                                             char* vA, char* vB, floatx16 (&o)[T::NDB], float& m, float& l) {
   constexpr int NB = T::NB, NDB = T::NDB;
-  __shared__ __attribute__((aligned(16))) char kA[T::TILE];
-  __shared__ __attribute__((aligned(16))) char kB[T::TILE];
-  __shared__ __attribute__((aligned(16))) char vA[T::TILE];
-  __shared__ __attribute__((aligned(16))) char vB[T::TILE];
-  __shared__ int s_bad;
-  const int lane = threadIdx.x & 63, l32 = lane & 31, hw = lane >> 5;
-  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-
-  WPlace p;
-  if (!place_query(a, lane, &p)) return;
+  const int l32 = lane & 31, hw = lane >> 5;
   const int w0 = p.r0 + 32 * wave, w1 = min(w0 + 31, p.len - 1);   // the wave's queries; w1 < w0: none
   const int i = w0 + l32;
   const bool in = i < p.len;
@@ -58,13 +52,15 @@ __global__ __launch_bounds__(256, 2) void k_window_forward(WindowArgs a) {
   auto first_of = [&](int c) { return (c < n_sink ? c : low + c - n_sink) * T::ROWS; };
 
   WLane<T> at(lane);
-  floatx16 o[NDB];
-  float m, l;
-  bool settled;
+  bool settled = false;
   const float scale = a.scale_log2;
+  m = -INFINITY;
+  l = 0.f;
+#pragma unroll
+  for (int db = 0; db < NDB; ++db) o[db] = floatx16{};
 
-  auto body = [&](int c, const char* kc, const char* vc, char* kn, char* vn, bool careful) {
-    if (!careful && c + 1 < n) {
+  auto body = [&](int c, const char* kc, const char* vc, char* kn, char* vn) {
+    if (!CAREFUL && c + 1 < n) {
       ck.issue(first_of(c + 1), p.len, kn, wave);
       cv.issue(first_of(c + 1), p.len, vn, wave);
     }
@@ -127,49 +123,70 @@ __global__ __launch_bounds__(256, 2) void k_window_forward(WindowArgs a) {
       for (int nb = 0; nb < NB; ++nb) l += sum[nb];
 #pragma unroll
       for (int nb = 0; nb < NB; ++nb) {
-        if (careful && !whole)
-          cols_product_seen<T>(o, vc + nb * T::HALF, pr[nb],
-                               reinterpret_cast<float*>((wave < T::TILE / 4096 ? kn : vn) + 4096 * (wave % (T::TILE / 4096))),
-                               lane, [&](int row) { return window_sees(i, j0 + 32 * nb + row, a.window, a.sinks); });
-        else
-          cols_product<T>(o, vc + nb * T::HALF, pr[nb], at);
+        if constexpr (CAREFUL) {
+          if (!whole) {
+            cols_product_seen<T>(
+                o, vc + nb * T::HALF, pr[nb],
+                reinterpret_cast<float*>((wave < T::TILE / 4096 ? kn : vn) + 4096 * (wave % (T::TILE / 4096))), lane,
+                [&](int row) { return window_sees(i, j0 + 32 * nb + row, a.window, a.sinks); });
+            continue;
+          }
+        }
+        cols_product<T>(o, vc + nb * T::HALF, pr[nb], at);
       }
+    }
+    if (!CAREFUL && c + 1 < n) {
+      ck.land(kn, wave, lane);
+      cv.land(vn, wave, lane);
     }
     __builtin_amdgcn_s_waitcnt(kWaitVm0);
     __syncthreads();
   };
 
-  for (int pass = 0; pass < 2; ++pass) {
-    const bool careful = pass != 0;
-    m = -INFINITY;
-    l = 0.f;
-    settled = false;
-#pragma unroll
-    for (int db = 0; db < NDB; ++db) o[db] = floatx16{};
-    if (careful) {   // one tile at a time: the other buffers are room for the rows' weights
-      for (int c = 0; c < n; ++c) {
-        ck.issue(first_of(c), p.len, kA, wave);
-        cv.issue(first_of(c), p.len, vA, wave);
-        __builtin_amdgcn_s_waitcnt(kWaitVm0);
-        __syncthreads();
-        body(c, kA, vA, kB, vB, true);
-      }
-      break;
-    }
-    if (threadIdx.x == 0) s_bad = 0;
-    ck.issue(first_of(0), p.len, kA, wave);
-    cv.issue(first_of(0), p.len, vA, wave);
+  auto begin = [&](int c) {
+    ck.issue(first_of(c), p.len, kA, wave);
+    cv.issue(first_of(c), p.len, vA, wave);
+    ck.land(kA, wave, lane);
+    cv.land(vA, wave, lane);
     __builtin_amdgcn_s_waitcnt(kWaitVm0);
     __syncthreads();
-    for (int c = 0; c < n; c += 2) {
-      body(c, kA, vA, kB, vB, false);
-      if (c + 1 < n) body(c + 1, kB, vB, kA, vA, false);
+  };
+  if constexpr (CAREFUL) {
+    for (int c = 0; c < n; ++c) {
+      begin(c);
+      body(c, kA, vA, kB, vB);
     }
-    const bool bad = in && not_finite<NDB>(o);
-    if (__builtin_amdgcn_ballot_w64(bad) && lane == 0) s_bad = 1;
-    __syncthreads();
-    if (!s_bad) break;
+  } else {
+    begin(0);
+    for (int c = 0; c < n; c += 2) {
+      body(c, kA, vA, kB, vB);
+      if (c + 1 < n) body(c + 1, kB, vB, kA, vA);
+    }
   }
+}
+
+// T: tiles of the first pass; TC: of the careful one.
+template <class T, class TC>
+__global__ __launch_bounds__(256, T::SPLIT && T::D == 128 ? 1 : 2) void k_window_forward(WindowArgs a) {
+  constexpr int NDB = T::NDB, BYTES = T::TILE > TC::TILE ? T::TILE : TC::TILE;
+  __shared__ __attribute__((aligned(16))) char kA[BYTES];
+  __shared__ __attribute__((aligned(16))) char kB[BYTES];
+  __shared__ __attribute__((aligned(16))) char vA[BYTES];
+  __shared__ __attribute__((aligned(16))) char vB[BYTES];
+  __shared__ int s_bad;
+  const int lane = threadIdx.x & 63, hw = lane >> 5;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  WPlace p;
+  if (!place_query(a, lane, &p)) return;
+  const int i = p.r0 + 32 * wave + (lane & 31);
+  const bool in = i < p.len;
+  floatx16 o[NDB];
+  float m, l;
+  if (threadIdx.x == 0) s_bad = 0;
+  forward_pass<T, false>(a, p, wave, lane, kA, kB, vA, vB, o, m, l);
+  if (__builtin_amdgcn_ballot_w64(in && not_finite<NDB>(o)) && lane == 0) s_bad = 1;
+  __syncthreads();
+  if (s_bad) forward_pass<TC, true>(a, p, wave, lane, kA, kB, vA, vB, o, m, l);
 
   l += __shfl_xor(l, 32);
   if (!in) return;
@@ -180,17 +197,22 @@ __global__ __launch_bounds__(256, 2) void k_window_forward(WindowArgs a) {
     a.lse[((int64_t)p.b * a.heads + p.h) * a.seq + row] = (m + __builtin_amdgcn_logf(l)) * kLn2;
 }
 
-template <class T>
+template <class T, class TC>
 hipError_t launch(const WindowArgs& a, hipStream_t s) {
-  k_window_forward<T><<<(unsigned)((int64_t)a.batch * a.heads * a.slots), 256, 0, s>>>(a);
+  k_window_forward<T, TC><<<(unsigned)((int64_t)a.batch * a.heads * a.slots), 256, 0, s>>>(a);
   return hipGetLastError();
+}
+
+template <int D>
+hipError_t launch_d(const WindowArgs& a, int dtype, hipStream_t s) {
+  if (dtype == SSBA_DT_F32) return launch<WTile<D, kF32Split>, WTile<D, kF32>>(a, s);
+  return launch<WTile<D, kBf16>, WTile<D, kBf16>>(a, s);
 }
 
 }  // namespace
 
 hipError_t launch_window_forward(const WindowArgs& a, int head_dim, int dtype, hipStream_t s) {
-  if (head_dim == 64) return dtype == SSBA_DT_F32 ? launch<WTile<64, true>>(a, s) : launch<WTile<64, false>>(a, s);
-  return dtype == SSBA_DT_F32 ? launch<WTile<128, true>>(a, s) : launch<WTile<128, false>>(a, s);
+  return head_dim == 64 ? launch_d<64>(a, dtype, s) : launch_d<128>(a, dtype, s);
 }
 
 }  // namespace ssba

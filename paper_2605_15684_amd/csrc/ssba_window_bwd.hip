@@ -50,46 +50,17 @@ __device__ __forceinline__ void order_rows() {
 // to 8 bits.  Errors of dq and dk against 64 bits, over that of a result's own
 // rounding (window 64, D 64, 200 rows): 1.58 and 1.53 without either.
 // --------------------------------------------------------------------------
-template <class T, int TERMS>
-__global__ __launch_bounds__(256, T::F32 ? 1 : 2) void k_window_dq(WindowArgs a) {
+template <class T, bool CAREFUL, int TERMS>
+__device__ __forceinline__ void dq_pass(const WindowArgs& a, const WPlace& p, int wave, int lane, char* kA, char* kB,
+                                        char* vA, char* vB, float delta, float lse2, floatx16 (&acc)[T::NDB], float& off) {
   constexpr int NB = T::NB, NDB = T::NDB;
-  __shared__ __attribute__((aligned(16))) char kA[T::TILE];
-  __shared__ __attribute__((aligned(16))) char kB[T::TILE];
-  __shared__ __attribute__((aligned(16))) char vA[T::TILE];
-  __shared__ __attribute__((aligned(16))) char vB[T::TILE];
-  __shared__ int s_bad;
-  const int lane = threadIdx.x & 63, l32 = lane & 31, hw = lane >> 5;
-  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-
-  WPlace p;
-  if (!place_query(a, lane, &p)) return;
+  const int l32 = lane & 31, hw = lane >> 5;
   const int w0 = p.r0 + 32 * wave, w1 = min(w0 + 31, p.len - 1);
   const int i = w0 + l32;
-  const bool in = i < p.len;
   const int64_t row = p.begin + min(i, p.len - 1);
-
   WRow<T> q, g;
-  float delta = 0.f, lse2;
-  {
-    q.load(static_cast<const char*>(a.q) + ((int64_t)p.b * a.sq.b + (int64_t)p.h * a.sq.h + row * a.sq.t) * T::SIZE, hw);
-    g.load(static_cast<const char*>(a.dout) + ((int64_t)p.b * a.sdo.b + (int64_t)p.h * a.sdo.h + row * a.sdo.t) * T::SIZE, hw);
-    WRow<T> o;
-    o.load(static_cast<const char*>(a.o) + ((int64_t)p.b * a.so.b + (int64_t)p.h * a.so.h + row * a.so.t) * T::SIZE, hw);
-#pragma unroll
-    for (int ks = 0; ks < T::NKS; ++ks)
-#pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        if constexpr (T::F32) {
-          delta = __builtin_fmaf(o.f[ks][e], g.f[ks][e], delta);
-        } else {
-          const uint32_t x = __float_as_uint(o.f[ks][e]), y = __float_as_uint(g.f[ks][e]);
-          delta = __builtin_fmaf(__uint_as_float(x << 16), __uint_as_float(y << 16), delta);
-          delta = __builtin_fmaf(__uint_as_float(x & 0xFFFF0000u), __uint_as_float(y & 0xFFFF0000u), delta);
-        }
-      }
-    delta += __shfl_xor(delta, 32);
-    lse2 = a.lse[((int64_t)p.b * a.heads + p.h) * a.seq + row] * kLog2e;
-  }
+  q.load(static_cast<const char*>(a.q) + ((int64_t)p.b * a.sq.b + (int64_t)p.h * a.sq.h + row * a.sq.t) * T::SIZE, hw);
+  g.load(static_cast<const char*>(a.dout) + ((int64_t)p.b * a.sdo.b + (int64_t)p.h * a.sdo.h + row * a.sdo.t) * T::SIZE, hw);
   WCopy<T> ck, cv;
   ck.init(a.k, (int64_t)p.b * a.sk.b + (int64_t)p.kvh * a.sk.h + (int64_t)p.begin * a.sk.t, a.sk.t, wave, lane);
   cv.init(a.v, (int64_t)p.b * a.sv.b + (int64_t)p.kvh * a.sv.h + (int64_t)p.begin * a.sv.t, a.sv.t, wave, lane);
@@ -101,10 +72,12 @@ __global__ __launch_bounds__(256, T::F32 ? 1 : 2) void k_window_dq(WindowArgs a)
   auto first_of = [&](int c) { return (c < n_sink ? c : low + c - n_sink) * T::ROWS; };
 
   WLane<T> at(lane);
-  floatx16 acc[NDB];
-  float off;   // sum of the lane's ds
-  auto body = [&](int c, const char* kc, const char* vc, char* kn, char* vn, bool careful) {
-    if (!careful && c + 1 < n) {
+  off = 0.f;
+#pragma unroll
+  for (int db = 0; db < NDB; ++db) acc[db] = floatx16{};
+
+  auto body = [&](int c, const char* kc, const char* vc, char* kn, char* vn) {
+    if (!CAREFUL && c + 1 < n) {
       ck.issue(first_of(c + 1), p.len, kn, wave);
       cv.issue(first_of(c + 1), p.len, vn, wave);
     }
@@ -132,56 +105,102 @@ __global__ __launch_bounds__(256, T::F32 ? 1 : 2) void k_window_dq(WindowArgs a)
         }
 #pragma unroll
         for (int e = 0; e < 16; ++e) off += ds[e];
-        if (careful && !whole)
-          cols_product_seen<T>(acc, kc + nb * T::HALF, ds,
-                               reinterpret_cast<float*>((wave < T::TILE / 4096 ? kn : vn) + 4096 * (wave % (T::TILE / 4096))),
-                               lane, [&](int r) { return window_sees(i, j0 + 32 * nb + r, a.window, a.sinks); });
-        else
-          cols_product<T, TERMS>(acc, kc + nb * T::HALF, ds, at);
+        if constexpr (CAREFUL) {
+          if (!whole) {
+            cols_product_seen<T>(
+                acc, kc + nb * T::HALF, ds,
+                reinterpret_cast<float*>((wave < T::TILE / 4096 ? kn : vn) + 4096 * (wave % (T::TILE / 4096))), lane,
+                [&](int r) { return window_sees(i, j0 + 32 * nb + r, a.window, a.sinks); });
+            continue;
+          }
+        }
+        cols_product<T, TERMS>(acc, kc + nb * T::HALF, ds, at);
         if constexpr (T::ORDERED) __builtin_amdgcn_sched_barrier(0);
       }
+    }
+    if (!CAREFUL && c + 1 < n) {
+      ck.land(kn, wave, lane);
+      cv.land(vn, wave, lane);
     }
     __builtin_amdgcn_s_waitcnt(kWaitVm0);
     __syncthreads();
   };
 
-  for (int pass = 0; pass < 2; ++pass) {
-    off = 0.f;
-#pragma unroll
-    for (int db = 0; db < NDB; ++db) acc[db] = floatx16{};
-    if (pass) {   // one tile at a time: the other buffers are room for the rows' weights
-      for (int c = 0; c < n; ++c) {
-        ck.issue(first_of(c), p.len, kA, wave);
-        cv.issue(first_of(c), p.len, vA, wave);
-        __builtin_amdgcn_s_waitcnt(kWaitVm0);
-        __syncthreads();
-        body(c, kA, vA, kB, vB, true);
-      }
-      break;
-    }
-    if (threadIdx.x == 0) s_bad = 0;
-    ck.issue(first_of(0), p.len, kA, wave);
-    cv.issue(first_of(0), p.len, vA, wave);
+  auto begin = [&](int c) {
+    ck.issue(first_of(c), p.len, kA, wave);
+    cv.issue(first_of(c), p.len, vA, wave);
+    ck.land(kA, wave, lane);
+    cv.land(vA, wave, lane);
     __builtin_amdgcn_s_waitcnt(kWaitVm0);
     __syncthreads();
-    for (int c = 0; c < n; c += 2) {
-      body(c, kA, vA, kB, vB, false);
-      if (c + 1 < n) body(c + 1, kB, vB, kA, vA, false);
+  };
+  if constexpr (CAREFUL) {   // one tile at a time: the other buffers are room for the rows' weights
+    for (int c = 0; c < n; ++c) {
+      begin(c);
+      body(c, kA, vA, kB, vB);
     }
-    const bool bad = in && not_finite<NDB>(acc);
-    if (__builtin_amdgcn_ballot_w64(bad) && lane == 0) s_bad = 1;
-    __syncthreads();
-    if (!s_bad) break;
+  } else {
+    begin(0);
+    for (int c = 0; c < n; c += 2) {
+      body(c, kA, vA, kB, vB);
+      if (c + 1 < n) body(c + 1, kB, vB, kA, vA);
+    }
   }
+}
+
+// T: tiles of the first pass; TC: of the careful one.
+template <class T, class TC, int TERMS>
+__global__ __launch_bounds__(256, T::SPLIT && T::D == 128 ? 1 : 2) void k_window_dq(WindowArgs a) {
+  constexpr int NDB = T::NDB, BYTES = T::TILE > TC::TILE ? T::TILE : TC::TILE;
+  __shared__ __attribute__((aligned(16))) char kA[BYTES];
+  __shared__ __attribute__((aligned(16))) char kB[BYTES];
+  __shared__ __attribute__((aligned(16))) char vA[BYTES];
+  __shared__ __attribute__((aligned(16))) char vB[BYTES];
+  __shared__ int s_bad;
+  const int lane = threadIdx.x & 63, hw = lane >> 5;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  WPlace p;
+  if (!place_query(a, lane, &p)) return;
+  const int i = p.r0 + 32 * wave + (lane & 31);
+  const bool in = i < p.len;
+  const int64_t row = p.begin + min(i, p.len - 1);
+  const int64_t to = ((int64_t)p.b * a.heads + p.h) * a.seq + row;
+
+  float delta = 0.f;
+  {
+    WRow<TC> o, g;
+    g.load(static_cast<const char*>(a.dout) + ((int64_t)p.b * a.sdo.b + (int64_t)p.h * a.sdo.h + row * a.sdo.t) * T::SIZE, hw);
+    o.load(static_cast<const char*>(a.o) + ((int64_t)p.b * a.so.b + (int64_t)p.h * a.so.h + row * a.so.t) * T::SIZE, hw);
+#pragma unroll
+    for (int ks = 0; ks < TC::NKS; ++ks)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        if constexpr (T::F32) {
+          delta = __builtin_fmaf(o.f[0][ks][e], g.f[0][ks][e], delta);
+        } else {
+          const uint32_t x = __float_as_uint(o.f[0][ks][e]), y = __float_as_uint(g.f[0][ks][e]);
+          delta = __builtin_fmaf(__uint_as_float(x << 16), __uint_as_float(y << 16), delta);
+          delta = __builtin_fmaf(__uint_as_float(x & 0xFFFF0000u), __uint_as_float(y & 0xFFFF0000u), delta);
+        }
+      }
+    delta += __shfl_xor(delta, 32);
+  }
+  const float lse2 = a.lse[to] * kLog2e;
+  floatx16 acc[NDB];
+  float off;   // sum of the lane's ds
+  if (threadIdx.x == 0) s_bad = 0;
+  dq_pass<T, false, TERMS>(a, p, wave, lane, kA, kB, vA, vB, delta, lse2, acc, off);
+  if (__builtin_amdgcn_ballot_w64(in && not_finite<NDB>(acc)) && lane == 0) s_bad = 1;
+  __syncthreads();
+  if (s_bad) dq_pass<TC, true, TERMS>(a, p, wave, lane, kA, kB, vA, vB, delta, lse2, acc, off);
   off += __shfl_xor(off, 32);
-  if (in && hw == 0) {
-    const int64_t to = ((int64_t)p.b * a.heads + p.h) * a.seq + row;
+  if (!in) return;
+  if (hw == 0) {
     a.ndelta[to] = -(delta + off);
     a.lse2[to] = lse2;
   }
-  if (in)
-    store_cols<T>(static_cast<char*>(a.dq) + ((int64_t)p.b * a.sdq.b + (int64_t)p.h * a.sdq.h + row * a.sdq.t) * T::SIZE,
-                  acc, a.scale, hw);
+  store_cols<T>(static_cast<char*>(a.dq) + ((int64_t)p.b * a.sdq.b + (int64_t)p.h * a.sdq.h + row * a.sdq.t) * T::SIZE, acc,
+                a.scale, hw);
 }
 
 // --------------------------------------------------------------------------
@@ -259,27 +278,16 @@ __device__ __forceinline__ void copy_values(const float* from, int n, float* dst
   __builtin_amdgcn_raw_ptr_buffer_load_lds(rs, (lds_void*)dst, 4, 4 * lane, 0, 0, 0);
 }
 
-template <class T>
-__global__ __launch_bounds__(256, T::F32 ? 1 : 2) void k_window_dkdv(WindowArgs a) {
+template <class T, bool CAREFUL>
+__device__ __forceinline__ void dkdv_pass(const WindowArgs& a, const KeyPlace& p, int wave, int lane, char* s_k, char* qA,
+                                          char* qB, char* gA, char* gB, float (*rA)[64], float (*rB)[64],
+                                          floatx16 (&dk)[T::NDB], floatx16 (&dv)[T::NDB]) {
   constexpr int NB = T::NB, NDB = T::NDB;
   // The wave's keys as operands in the LDS where registers are short.
   constexpr bool KLDS = T::ORDERED;
-  __shared__ __attribute__((aligned(16))) char s_k[KLDS ? 4 * T::NKS * 1024 : 16];
-  __shared__ __attribute__((aligned(16))) char qA[T::TILE];
-  __shared__ __attribute__((aligned(16))) char qB[T::TILE];
-  __shared__ __attribute__((aligned(16))) char gA[T::TILE];
-  __shared__ __attribute__((aligned(16))) char gB[T::TILE];
-  __shared__ __attribute__((aligned(16))) float rA[2][64];   // lse2, -delta of the tile's rows
-  __shared__ __attribute__((aligned(16))) float rB[2][64];
-  __shared__ int s_bad;
-  const int lane = threadIdx.x & 63, l32 = lane & 31, hw = lane >> 5;
-  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-
-  KeyPlace p;
-  if (!place_keys(a, lane, &p)) return;
+  const int l32 = lane & 31, hw = lane >> 5;
   const int w0 = p.k0 + 32 * wave, w1 = min(w0 + 31, p.len - 1);   // the wave's keys
   const int j = w0 + l32;
-  const bool in = j < p.len;
 
   using KRow = typename std::conditional<KLDS, WRowLds<T>, WRow<T>>::type;
   KRow k;
@@ -292,16 +300,17 @@ __global__ __launch_bounds__(256, T::F32 ? 1 : 2) void k_window_dkdv(WindowArgs 
       k.at = s_k + 1024 * T::NKS * wave + 16 * lane;
 #pragma unroll
       for (int ks = 0; ks < T::NKS; ++ks)
-        *reinterpret_cast<floatx4*>(s_k + 1024 * (T::NKS * wave + ks) + 16 * lane) = kr.f[ks];
+        *reinterpret_cast<floatx4*>(s_k + 1024 * (T::NKS * wave + ks) + 16 * lane) = kr.f[0][ks];
     } else {
       k = kr;
     }
     v.load(static_cast<const char*>(a.v) + ((int64_t)p.b * a.sv.b + (int64_t)p.kvh * a.sv.h + row * a.sv.t) * T::SIZE, hw);
   }
   WCopy<T> cq, cg;
-  cq.init(a.q, (int64_t)p.b * a.sq.b + ((int64_t)p.kvh * a.group + p.g0) * a.sq.h + (int64_t)p.begin * a.sq.t, a.sq.t, wave, lane);
-  cg.init(a.dout, (int64_t)p.b * a.sdo.b + ((int64_t)p.kvh * a.group + p.g0) * a.sdo.h + (int64_t)p.begin * a.sdo.t, a.sdo.t, wave,
+  cq.init(a.q, (int64_t)p.b * a.sq.b + ((int64_t)p.kvh * a.group + p.g0) * a.sq.h + (int64_t)p.begin * a.sq.t, a.sq.t, wave,
           lane);
+  cg.init(a.dout, (int64_t)p.b * a.sdo.b + ((int64_t)p.kvh * a.group + p.g0) * a.sdo.h + (int64_t)p.begin * a.sdo.t,
+          a.sdo.t, wave, lane);
   const int64_t head = (int64_t)p.b * a.heads + p.kvh * a.group + p.g0;
   const char* q_base = cq.base;
   const char* g_base = cg.base;
@@ -317,10 +326,7 @@ __global__ __launch_bounds__(256, T::F32 ? 1 : 2) void k_window_dkdv(WindowArgs 
     const int i0 = (t0 + next_t) * T::ROWS;
     cq.issue(i0, p.len, qd, wave);
     cg.issue(i0, p.len, gd, wave);
-    if (wave < 2) {
-      const float* from = (wave ? d_base : l_base) + (int64_t)next_g * a.seq + i0;
-      copy_values(from, min(p.len - i0, T::ROWS), rd[wave], lane);
-    }
+    if (wave < 2) copy_values((wave ? d_base : l_base) + (int64_t)next_g * a.seq + i0, min(p.len - i0, T::ROWS), rd[wave], lane);
     if (++next_t == per_head) {
       next_t = 0;
       ++next_g;
@@ -328,10 +334,12 @@ __global__ __launch_bounds__(256, T::F32 ? 1 : 2) void k_window_dkdv(WindowArgs 
   };
 
   WLane<T> place(lane);
-  floatx16 dk[NDB], dv[NDB];
   int at = 0;   // tile of the head
-  auto body = [&](int c, const char* qc, const char* gc, float (*rc)[64], char* qn, char* gn, float (*rn)[64], bool careful) {
-    if (!careful && c + 1 < n) issue(qn, gn, rn);
+#pragma unroll
+  for (int db = 0; db < NDB; ++db) dk[db] = dv[db] = floatx16{};
+
+  auto body = [&](int c, const char* qc, const char* gc, float (*rc)[64], char* qn, char* gn, float (*rn)[64]) {
+    if (!CAREFUL && c + 1 < n) issue(qn, gn, rn);
     const int i0 = (t0 + at) * T::ROWS;
     if (++at == per_head) at = 0;
     const bool none = i0 + T::ROWS - 1 < w0 || (w1 <= i0 - a.window && w0 >= a.sinks) || w0 >= p.len;
@@ -342,7 +350,7 @@ __global__ __launch_bounds__(256, T::F32 ? 1 : 2) void k_window_dkdv(WindowArgs 
       for (int nb = 0; nb < NB; ++nb) {
         auto sees = [&](int r) {
           const int i = i0 + 32 * nb + r;
-          return i >= p.q0 && i < p.q1 && window_sees(i, j, a.window, a.sinks);
+          return (i >= p.q0) & (i < p.q1) & window_sees(i, j, a.window, a.sinks);
         };
         if constexpr (T::ORDERED) __builtin_amdgcn_sched_barrier(0);
         place.forget();
@@ -373,51 +381,76 @@ __global__ __launch_bounds__(256, T::F32 ? 1 : 2) void k_window_dkdv(WindowArgs 
             ds[e] = seen ? ds[e] : 0.f;
           }
         }
-        if (careful && !whole) {
-          float* room = reinterpret_cast<float*>((wave < T::TILE / 4096 ? qn : gn) + 4096 * (wave % (T::TILE / 4096)));
-          cols_product_seen<T>(dv, gc + nb * T::HALF, pr, room, lane, sees);
-          cols_product_seen<T>(dk, qc + nb * T::HALF, ds, room, lane, sees);
-        } else {
-          cols_product<T>(dv, gc + nb * T::HALF, pr, place);
-          if constexpr (T::ORDERED) __builtin_amdgcn_sched_barrier(0);
-          cols_product<T>(dk, qc + nb * T::HALF, ds, place);
+        if constexpr (CAREFUL) {
+          if (!whole) {
+            float* room = reinterpret_cast<float*>((wave < T::TILE / 4096 ? qn : gn) + 4096 * (wave % (T::TILE / 4096)));
+            cols_product_seen<T>(dv, gc + nb * T::HALF, pr, room, lane, sees);
+            cols_product_seen<T>(dk, qc + nb * T::HALF, ds, room, lane, sees);
+            continue;
+          }
         }
+        cols_product<T>(dv, gc + nb * T::HALF, pr, place);
+        if constexpr (T::ORDERED) __builtin_amdgcn_sched_barrier(0);
+        cols_product<T>(dk, qc + nb * T::HALF, ds, place);
         if constexpr (T::ORDERED) __builtin_amdgcn_sched_barrier(0);
       }
+    }
+    if (!CAREFUL && c + 1 < n) {
+      cq.land(qn, wave, lane);
+      cg.land(gn, wave, lane);
     }
     __builtin_amdgcn_s_waitcnt(kWaitVm0);
     __syncthreads();
   };
 
-  for (int pass = 0; pass < 2; ++pass) {
-    next_g = next_t = at = 0;
-#pragma unroll
-    for (int db = 0; db < NDB; ++db) dk[db] = dv[db] = floatx16{};
-    if (pass) {   // one tile at a time: the other buffers are room for the rows' weights
-      for (int c = 0; c < n; ++c) {
-        issue(qA, gA, rA);
-        __builtin_amdgcn_s_waitcnt(kWaitVm0);
-        __syncthreads();
-        body(c, qA, gA, rA, qB, gB, rB, true);
-      }
-      break;
-    }
-    if (threadIdx.x == 0) s_bad = 0;
+  auto begin = [&]() {
     issue(qA, gA, rA);
+    cq.land(qA, wave, lane);
+    cg.land(gA, wave, lane);
     __builtin_amdgcn_s_waitcnt(kWaitVm0);
     __syncthreads();
-    for (int c = 0; c < n; c += 2) {
-      body(c, qA, gA, rA, qB, gB, rB, false);
-      if (c + 1 < n) body(c + 1, qB, gB, rB, qA, gA, rA, false);
+  };
+  if constexpr (CAREFUL) {   // one tile at a time: the other buffers are room for the rows' weights
+    for (int c = 0; c < n; ++c) {
+      begin();
+      body(c, qA, gA, rA, qB, gB, rB);
     }
-    const bool bad = in && (not_finite<NDB>(dk) || not_finite<NDB>(dv));
-    if (__builtin_amdgcn_ballot_w64(bad) && lane == 0) s_bad = 1;
-    __syncthreads();
-    if (!s_bad) break;
+  } else {
+    begin();
+    for (int c = 0; c < n; c += 2) {
+      body(c, qA, gA, rA, qB, gB, rB);
+      if (c + 1 < n) body(c + 1, qB, gB, rB, qA, gA, rA);
+    }
   }
+}
+
+// T: tiles of the first pass; TC: of the careful one.
+template <class T, class TC>
+__global__ __launch_bounds__(256, T::SPLIT && T::D == 128 ? 1 : 2) void k_window_dkdv(WindowArgs a) {
+  constexpr int NDB = T::NDB, BYTES = T::TILE > TC::TILE ? T::TILE : TC::TILE;
+  __shared__ __attribute__((aligned(16))) char s_k[T::ORDERED ? 4 * T::NKS * 1024 : 16];
+  __shared__ __attribute__((aligned(16))) char qA[BYTES];
+  __shared__ __attribute__((aligned(16))) char qB[BYTES];
+  __shared__ __attribute__((aligned(16))) char gA[BYTES];
+  __shared__ __attribute__((aligned(16))) char gB[BYTES];
+  __shared__ __attribute__((aligned(16))) float rA[2][64];   // lse2, -delta of the tile's rows
+  __shared__ __attribute__((aligned(16))) float rB[2][64];
+  __shared__ int s_bad;
+  const int lane = threadIdx.x & 63, l32 = lane & 31, hw = lane >> 5;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  KeyPlace p;
+  if (!place_keys(a, lane, &p)) return;
+  const int j = p.k0 + 32 * wave + l32;
+  const bool in = j < p.len;
+  floatx16 dk[NDB], dv[NDB];
+  if (threadIdx.x == 0) s_bad = 0;
+  dkdv_pass<T, false>(a, p, wave, lane, s_k, qA, qB, gA, gB, rA, rB, dk, dv);
+  if (__builtin_amdgcn_ballot_w64(in && (not_finite<NDB>(dk) || not_finite<NDB>(dv))) && lane == 0) s_bad = 1;
+  __syncthreads();
+  if (s_bad) dkdv_pass<TC, true>(a, p, wave, lane, s_k, qA, qB, gA, gB, rA, rB, dk, dv);
   if (!in) return;
   if (p.part >= 0) {
-    using P = WTile<T::D, true>;
+    using P = WTile<T::D, kF32>;
     char* to = reinterpret_cast<char*>(a.part + (p.part + 32 * wave + l32) * T::D);
     store_cols<P>(to, dk, 1.f, hw);
     store_cols<P>(to + (int64_t)kWindowRows * T::D * 4, dv, 1.f, hw);
@@ -495,31 +528,38 @@ __global__ __launch_bounds__(256) void k_window_join(WindowArgs a) {
   }
 }
 
-// T: tiles of the query side and the join; TK: of the key side.
-template <class T, class TK>
+// T: tiles of the query side, TK: of the key side; TC: of the careful passes
+// (the key side's in those of TK where it is bf16).
+template <class T, class TK, class TC>
 hipError_t launch(const WindowArgs& a, hipStream_t s) {
+  using TKC = typename std::conditional<T::F32, TC, TK>::type;
   const int64_t units = (int64_t)a.batch * a.kv_heads, cut = (int64_t)a.sink_tiles * a.chunk_slots;
   const int64_t kept = cut + (a.head_parts > 1 ? a.slots : 0);
   const unsigned groups = (unsigned)((int64_t)a.batch * a.heads * a.slots);
   if (!T::F32 && (int64_t)a.window + a.sinks <= 1024)
-    k_window_dq<T, T::F32 ? 1 : 2><<<groups, 256, 0, s>>>(a);
+    k_window_dq<T, TC, T::F32 ? 1 : 2><<<groups, 256, 0, s>>>(a);
   else
-    k_window_dq<T, 1><<<groups, 256, 0, s>>>(a);
+    k_window_dq<T, TC, 1><<<groups, 256, 0, s>>>(a);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
-  k_window_dkdv<TK><<<(unsigned)(units * (a.slots + cut) * a.head_parts), 256, 0, s>>>(a);
+  k_window_dkdv<TK, TKC><<<(unsigned)(units * (a.slots + cut) * a.head_parts), 256, 0, s>>>(a);
   if ((e = hipGetLastError()) != hipSuccess || !kept) return e;
   k_window_join<T><<<(unsigned)(units * kept * (kWindowRows * T::D / 2048)), 256, 0, s>>>(a);
   return hipGetLastError();
 }
 
+template <int D>
+hipError_t launch_d(const WindowArgs& a, int dtype, hipStream_t s) {
+  using Split = WTile<D, kF32Split>;
+  using Half = WTile<D, kBf16>;
+  if (dtype == SSBA_DT_F32) return launch<Split, Split, WTile<D, kF32>>(a, s);
+  return launch<Half, WTile<D, kBf16, D == 128 ? 1 : 2>, Half>(a, s);
+}
+
 }  // namespace
 
 hipError_t launch_window_backward(const WindowArgs& a, int head_dim, int dtype, hipStream_t s) {
-  if (dtype == SSBA_DT_F32)
-    return head_dim == 64 ? launch<WTile<64, true>, WTile<64, true>>(a, s) : launch<WTile<128, true>, WTile<128, true>>(a, s);
-  return head_dim == 64 ? launch<WTile<64, false>, WTile<64, false>>(a, s)
-                        : launch<WTile<128, false>, WTile<128, false, 1>>(a, s);
+  return head_dim == 64 ? launch_d<64>(a, dtype, s) : launch_d<128>(a, dtype, s);
 }
 
 }  // namespace ssba

@@ -18,31 +18,55 @@ namespace ssba {
 
 typedef float floatx4 __attribute__((ext_vector_type(4)));
 
-template <int D_, bool F32_, int NB_ = F32_ ? 1 : 2>
+enum WKind {
+  kBf16,
+  kF32,      // fp32 as it is, products by v_mfma_f32_32x32x2_f32
+  kF32Split  // each value as three bf16 terms that make it up exactly, in three planes; products by
+             // v_mfma_f32_32x32x16_bf16, of the six pairs of terms that reach 2^-24 of the product (the others are at
+             // most 2^-24 of it): 192 cycles for 16 channels instead of 512.  An infinity becomes NaN.
+};
+
+template <int D_, int KIND, int NB_ = KIND == kBf16 ? 2 : 1>
 struct WTile {
   static constexpr int D = D_;
-  static constexpr bool F32 = F32_;
-  static constexpr int SIZE = F32 ? 4 : 2;
-  static constexpr int ROWB = D * SIZE;         // bytes of a row
+  static constexpr bool F32 = KIND != kBf16, NATIVE = KIND == kF32, SPLIT = KIND == kF32Split;
+  static constexpr int SIZE = F32 ? 4 : 2;      // bytes of a value in memory
+  static constexpr int ROWB = D * (NATIVE ? 4 : 2);   // bytes of a row in the LDS
   static constexpr int CPR = ROWB / 16;         // 16-byte chunks of a row
   static constexpr int NB = NB_;                // halves of a tile
+  static constexpr int PL = SPLIT ? 3 : 1;      // planes
   static constexpr int ROWS = 32 * NB;
   static constexpr int HALF = 32 * ROWB;
-  static constexpr int TILE = NB * HALF;        // 8 or 16 KB
+  static constexpr int TILE = PL * NB * HALF;   // 8 to 24 KB
   // Registers are short and two waves a SIMD few: reads and products are put in order by hand.
   static constexpr bool ORDERED = D == 128 && !F32;
   static constexpr int KPI = 1024 / ROWB;       // rows of a copy instruction
   static constexpr int NIW = TILE / 4096;       // copy instructions of each of 4 waves
-  static constexpr int NKS = F32 ? D / 8 : D / 16;   // 16-byte operands of a lane in a row
+  static constexpr int NU = D / 64;             // SPLIT: eights of a thread in a tile
+  static constexpr int NKS = NATIVE ? D / 8 : D / 16;   // 16-byte operands of a lane in a row
   static constexpr int NDB = D / 32;
+  static_assert(!SPLIT || NB == 1, "planes follow each other");
 };
 
 template <class T>
 __device__ __forceinline__ int wswz(int k, int c) {
-  if constexpr (T::F32)
+  if constexpr (T::NATIVE)
     return c ^ (k & 7);
   else
     return swz<T::D>(k, c);
+}
+
+// a and b as N bf16 terms each, every one the rounding of what the ones before
+// leave: of 3 (fp32 made up exactly) the second is at most 2^-8, the third 2^-16
+// of the value.
+template <int N>
+__device__ __forceinline__ void split2(float a, float b, uint32_t (&t)[N]) {
+#pragma unroll
+  for (int i = 0; i < N; ++i) {
+    t[i] = pack2(a, b);
+    a -= __uint_as_float(t[i] << 16);
+    b -= __uint_as_float(t[i] & 0xFFFF0000u);
+  }
 }
 
 // The rows of a workgroup: of sequence (batch b or packed), head h.
@@ -126,28 +150,74 @@ __device__ __forceinline__ void copy_kb(const char* p, unsigned bytes, unsigned 
   __builtin_amdgcn_raw_ptr_buffer_load_lds(rs, (lds_void*)dst, 16, off, 0, 0, 0);
 }
 
+// 16 bytes from the `bytes` behind p, zeros for what is past them.
+__device__ __forceinline__ floatx4 load_bounded(const char* p, unsigned bytes, unsigned off) {
+  typedef unsigned int u32x4 __attribute__((ext_vector_type(4)));
+  const __amdgpu_buffer_rsrc_t rs =
+      __builtin_amdgcn_make_buffer_rsrc(const_cast<char*>(p), (short)0, (int)bytes, kRawBufferFlags);
+  const u32x4 x = __builtin_amdgcn_raw_buffer_load_b128(rs, (int)off, 0, 0);
+  return __builtin_bit_cast(floatx4, x);
+}
+
 // This wave's copy of its part of a tile: rows row0 .. of a (b, h) slice, rows
-// from `end` on become 0.
+// from `end` on become 0.  issue() begins it; land() behind the work that hides
+// it, then a wait for vector memory and a barrier, end it.  SPLIT: the values
+// pass through registers, where they are split.
 template <class T>
 struct WCopy {
   const char* base;   // row 0
   unsigned rowb;      // bytes from row to row
-  unsigned off[T::NIW];
+  unsigned off[T::SPLIT ? 1 : T::NIW];
+  floatx4 held[T::SPLIT ? 2 * T::NU : 1];
   __device__ __forceinline__ void init(const void* p, int64_t elem, int64_t st, int wave, int lane) {
     base = static_cast<const char*>(p) + elem * T::SIZE;
     rowb = (unsigned)st * T::SIZE;
+    if constexpr (T::SPLIT) {
+      const int u = 64 * wave + lane;
+      off[0] = (unsigned)(u / (T::D / 8)) * rowb + 32u * (unsigned)(u % (T::D / 8));
+    } else {
 #pragma unroll
-    for (int m = 0; m < T::NIW; ++m) {
-      const int row = T::KPI * (T::NIW * wave + m) + lane / T::CPR;
-      off[m] = (unsigned)row * rowb + 16u * (unsigned)wswz<T>(row & 31, lane % T::CPR);
+      for (int m = 0; m < T::NIW; ++m) {
+        const int row = T::KPI * (T::NIW * wave + m) + lane / T::CPR;
+        off[m] = (unsigned)row * rowb + 16u * (unsigned)wswz<T>(row & 31, lane % T::CPR);
+      }
     }
   }
-  __device__ __forceinline__ void issue(int row0, int end, char* dst, int wave) const {
+  __device__ __forceinline__ void issue(int row0, int end, char* dst, int wave) {
     const int left = min(end - row0, T::ROWS);
-    const unsigned bytes = left > 0 ? (unsigned)(left - 1) * rowb + T::ROWB : 0u;
+    const unsigned bytes = left > 0 ? (unsigned)(left - 1) * rowb + T::D * T::SIZE : 0u;
+    const char* from = base + (int64_t)row0 * rowb;
+    if constexpr (T::SPLIT) {
 #pragma unroll
-    for (int m = 0; m < T::NIW; ++m)
-      copy_kb(base + (int64_t)row0 * rowb, bytes, off[m], dst + 1024 * (T::NIW * wave + m));
+      for (int i = 0; i < T::NU; ++i) {
+        const unsigned at = off[0] + (unsigned)(i * (2048 / T::D)) * rowb;   // 256 eights are 2048 / D rows
+        held[2 * i] = load_bounded(from, bytes, at);
+        held[2 * i + 1] = load_bounded(from, bytes, at + 16);
+      }
+    } else {
+#pragma unroll
+      for (int m = 0; m < T::NIW; ++m) copy_kb(from, bytes, off[m], dst + 1024 * (T::NIW * wave + m));
+    }
+  }
+  __device__ __forceinline__ void land(char* dst, int wave, int lane) const {
+    if constexpr (T::SPLIT) {
+#pragma unroll
+      for (int i = 0; i < T::NU; ++i) {
+        const int u = 64 * wave + lane + 256 * i, row = u / (T::D / 8), c = u % (T::D / 8);
+        uint32_t w[3][4];
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          uint32_t x[3];
+          split2(held[2 * i + e / 2][2 * (e & 1)], held[2 * i + e / 2][2 * (e & 1) + 1], x);
+#pragma unroll
+          for (int t = 0; t < 3; ++t) w[t][e] = x[t];
+        }
+        char* to = dst + row * T::ROWB + 16 * wswz<T>(row, c);
+#pragma unroll
+        for (int t = 0; t < 3; ++t)
+          *reinterpret_cast<uint4*>(to + t * T::HALF) = make_uint4(w[t][0], w[t][1], w[t][2], w[t][3]);
+      }
+    }
   }
 };
 
@@ -155,10 +225,30 @@ struct WCopy {
 // row (lane / 32).
 template <class T>
 struct WRow {
-  floatx4 f[T::NKS];
+  floatx4 f[T::PL][T::NKS];
   __device__ __forceinline__ void load(const char* row, int hw) {
 #pragma unroll
-    for (int ks = 0; ks < T::NKS; ++ks) f[ks] = *reinterpret_cast<const floatx4*>(row + 32 * ks + 16 * hw);
+    for (int ks = 0; ks < T::NKS; ++ks) {
+      if constexpr (T::SPLIT) {
+        uint32_t w[3][4];
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          const floatx4 x = *reinterpret_cast<const floatx4*>(row + 64 * ks + 32 * hw + 16 * h);
+#pragma unroll
+          for (int e = 0; e < 2; ++e) {
+            uint32_t y[3];
+            split2(x[2 * e], x[2 * e + 1], y);
+#pragma unroll
+            for (int t = 0; t < 3; ++t) w[t][2 * h + e] = y[t];
+          }
+        }
+#pragma unroll
+        for (int t = 0; t < 3; ++t)
+          f[t][ks] = __builtin_bit_cast(floatx4, make_uint4(w[t][0], w[t][1], w[t][2], w[t][3]));
+      } else {
+        f[0][ks] = *reinterpret_cast<const floatx4*>(row + 32 * ks + 16 * hw);
+      }
+    }
   }
 };
 
@@ -166,15 +256,14 @@ struct WRow {
 template <class T>
 struct WRowLds {
   const char* at;   // the wave's, lane's 16 bytes of the first
-  __device__ __forceinline__ floatx4 get(int ks) const { return *reinterpret_cast<const floatx4*>(at + 1024 * ks); }
 };
 template <class T>
-__device__ __forceinline__ floatx4 operand(const WRow<T>& r, int ks) {
-  return r.f[ks];
+__device__ __forceinline__ floatx4 operand(const WRow<T>& r, int ks, int plane) {
+  return r.f[plane][ks];
 }
 template <class T>
-__device__ __forceinline__ floatx4 operand(const WRowLds<T>& r, int ks) {
-  return r.get(ks);
+__device__ __forceinline__ floatx4 operand(const WRowLds<T>& r, int ks, int) {
+  return *reinterpret_cast<const floatx4*>(r.at + 1024 * ks);
 }
 
 // Where a lane's operands lie in a half tile: all of one kind differ by
@@ -185,7 +274,7 @@ struct WLane {
   __device__ __forceinline__ explicit WLane(int lane) {
     const int l32 = lane & 31, hw = lane >> 5;
     row = l32 * T::ROWB + 16 * wswz<T>(l32, hw);
-    if constexpr (T::F32) {
+    if constexpr (T::NATIVE) {
       col = 4 * hw * T::ROWB + 16 * wswz<T>(4 * hw, l32 >> 2) + 4 * (l32 & 3);
     } else {
       // As tr_frag: rows 4 hw + li / 4, channels 16 (G & 1) + 4 (li & 3) ..
@@ -219,7 +308,7 @@ __device__ __forceinline__ bf16x8 col_operand(const char* half, const WLane<T>& 
 
 template <class T>
 __device__ __forceinline__ void multiply(floatx16& acc, floatx4 x, floatx4 y) {
-  if constexpr (T::F32) {
+  if constexpr (T::NATIVE) {
 #pragma unroll
     for (int e = 0; e < 4; ++e) acc = __builtin_amdgcn_mfma_f32_32x32x2f32(x[e], y[e], acc, 0, 0, 0);
   } else {
@@ -227,10 +316,22 @@ __device__ __forceinline__ void multiply(floatx16& acc, floatx4 x, floatx4 y) {
   }
 }
 
+// acc += operand ks of the half's rows times that of b: small pairs of terms first.
+template <class T, class Row>
+__device__ __forceinline__ void row_step(floatx16& acc, const char* half, const Row& b, const WLane<T>& l, int ks) {
+  floatx4 x[T::PL];
+#pragma unroll
+  for (int t = 0; t < T::PL; ++t) x[t] = row_operand<T>(half + t * T::HALF, l, ks);
+#pragma unroll
+  for (int sum = T::PL - 1; sum >= 0; --sum)
+#pragma unroll
+    for (int t = 0; t <= sum; ++t) multiply<T>(acc, x[t], operand<T>(b, ks, sum - t));
+}
+
 template <class T>
 __device__ __forceinline__ void rows_product(floatx16& acc, const char* half, const WRow<T>& b, const WLane<T>& l) {
 #pragma unroll
-  for (int ks = 0; ks < T::NKS; ++ks) multiply<T>(acc, row_operand<T>(half, l, ks), b.f[ks]);
+  for (int ks = 0; ks < T::NKS; ++ks) row_step<T>(acc, half, b, l, ks);
 }
 
 // Two of them in turn.
@@ -239,8 +340,8 @@ __device__ __forceinline__ void rows_products(floatx16& acc1, const char* half1,
                                               const char* half2, const Row2& b2, const WLane<T>& l) {
 #pragma unroll
   for (int ks = 0; ks < T::NKS; ++ks) {
-    multiply<T>(acc1, row_operand<T>(half1, l, ks), operand<T>(b1, ks));
-    multiply<T>(acc2, row_operand<T>(half2, l, ks), operand<T>(b2, ks));
+    row_step<T>(acc1, half1, b1, l, ks);
+    row_step<T>(acc2, half2, b2, l, ks);
   }
 }
 
@@ -248,7 +349,7 @@ __device__ __forceinline__ void rows_products(floatx16& acc1, const char* half1,
 // TERMS: bf16 terms of x, each the rounding of what the ones before leave.
 template <class T, int TERMS = 1>
 __device__ __forceinline__ void cols_product(floatx16 (&acc)[T::NDB], const char* half, const floatx16& x, const WLane<T>& l) {
-  if constexpr (T::F32) {
+  if constexpr (T::NATIVE) {
 #pragma unroll
     for (int j = 0; j < 16; ++j)
 #pragma unroll
@@ -257,17 +358,36 @@ __device__ __forceinline__ void cols_product(floatx16 (&acc)[T::NDB], const char
                                                         (8 * (j >> 2) + (j & 3)) * T::ROWB + 128 * db);
         acc[db] = __builtin_amdgcn_mfma_f32_32x32x2f32(w, x[j], acc[db], 0, 0, 0);
       }
+  } else if constexpr (T::SPLIT) {
+    uint32_t pk[3][8];
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+      uint32_t w[3];
+      split2(x[2 * j], x[2 * j + 1], w);
+#pragma unroll
+      for (int t = 0; t < 3; ++t) pk[t][j] = w[t];
+    }
+#pragma unroll
+    for (int ks = 0; ks < 2; ++ks)
+#pragma unroll
+      for (int db = 0; db < T::NDB; ++db) {
+        bf16x8 w[3];
+#pragma unroll
+        for (int t = 0; t < 3; ++t) w[t] = col_operand<T>(half + t * T::HALF, l, ks, db);
+#pragma unroll
+        for (int sum = 2; sum >= 0; --sum)
+#pragma unroll
+          for (int t = 0; t <= sum; ++t)
+            acc[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(w[t], packed_frag(pk[sum - t], ks), acc[db], 0, 0, 0);
+      }
   } else {
     uint32_t pk[TERMS][8];
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
-      float a = x[2 * j], b = x[2 * j + 1];
+      uint32_t w[TERMS];
+      split2(x[2 * j], x[2 * j + 1], w);
 #pragma unroll
-      for (int t = 0; t < TERMS; ++t) {
-        pk[t][j] = pack2(a, b);
-        a -= __uint_as_float(pk[t][j] << 16);
-        b -= __uint_as_float(pk[t][j] & 0xFFFF0000u);
-      }
+      for (int t = 0; t < TERMS; ++t) pk[t][j] = w[t];
     }
 #pragma unroll
     for (int ks = 0; ks < 2; ++ks)
@@ -303,7 +423,7 @@ __device__ __forceinline__ void cols_product_seen(floatx16 (&acc)[T::NDB], const
         const int ch = 32 * db + 8 * (e >> 2) + 4 * hw + (e & 3), at = ch * T::SIZE;
         const char* p = half + row * T::ROWB + 16 * wswz<T>(row, at >> 4) + (at & 15);
         float y;
-        if constexpr (T::F32)
+        if constexpr (T::NATIVE)
           y = *reinterpret_cast<const float*>(p);
         else
           y = __uint_as_float((uint32_t)*reinterpret_cast<const u16*>(p) << 16);
