@@ -121,6 +121,7 @@ __device__ __forceinline__ void forward_pass(const WindowArgs& a, const WPlace& 
       }
 #pragma unroll
       for (int nb = 0; nb < NB; ++nb) l += sum[nb];
+      __builtin_amdgcn_s_setprio(1);
 #pragma unroll
       for (int nb = 0; nb < NB; ++nb) {
         if constexpr (CAREFUL) {
@@ -134,6 +135,7 @@ __device__ __forceinline__ void forward_pass(const WindowArgs& a, const WPlace& 
         }
         cols_product<T>(o, vc + nb * T::HALF, pr[nb], at);
       }
+      __builtin_amdgcn_s_setprio(0);
     }
     if (!CAREFUL && c + 1 < n) {
       ck.land(kn, wave, lane);
