@@ -35,11 +35,6 @@ __device__ __forceinline__ void forward_pass(const WindowArgs& a, const WPlace& 
   const int i = w0 + l32;
   const bool in = i < p.len;
 
-  WRow<T> q;
-  {
-    const int64_t at = (int64_t)p.b * a.sq.b + (int64_t)p.h * a.sq.h + (int64_t)(p.begin + min(i, p.len - 1)) * a.sq.t;
-    q.load(static_cast<const char*>(a.q) + at * T::SIZE, hw);
-  }
   WCopy<T> ck, cv;
   ck.init(a.k, (int64_t)p.b * a.sk.b + (int64_t)p.kvh * a.sk.h + (int64_t)p.begin * a.sk.t, a.sk.t, wave, lane);
   cv.init(a.v, (int64_t)p.b * a.sv.b + (int64_t)p.kvh * a.sv.h + (int64_t)p.begin * a.sv.t, a.sv.t, wave, lane);
@@ -50,7 +45,25 @@ __device__ __forceinline__ void forward_pass(const WindowArgs& a, const WPlace& 
   const int n_sink = min((int)(((unsigned)min(a.sinks, last + 1) + T::ROWS - 1) / T::ROWS), low);
   const int n = n_sink + last / T::ROWS - low + 1;
   auto first_of = [&](int c) { return (c < n_sink ? c : low + c - n_sink) * T::ROWS; };
+  auto issue = [&](int c, char* kn, char* vn) {
+    ck.issue(first_of(c), p.len, kn, wave);
+    cv.issue(first_of(c), p.len, vn, wave);
+  };
+  // The end of a tile's copy.
+  auto arrive = [&](char* kn, char* vn) {
+    ck.land(kn, wave, lane);
+    cv.land(vn, wave, lane);
+  };
+  auto all_there = [&]() {
+    __builtin_amdgcn_s_waitcnt(kWaitVm0);
+    __syncthreads();
+  };
+  issue(0, kA, vA);   // before the queries: both are on their way at once
 
+  WRow<T> q;
+  q.load(static_cast<const char*>(a.q) +
+             ((int64_t)p.b * a.sq.b + (int64_t)p.h * a.sq.h + (int64_t)(p.begin + min(i, p.len - 1)) * a.sq.t) * T::SIZE,
+         hw);
   WLane<T> at(lane);
   bool settled = false;
   const float scale = a.scale_log2;
@@ -60,10 +73,7 @@ __device__ __forceinline__ void forward_pass(const WindowArgs& a, const WPlace& 
   for (int db = 0; db < NDB; ++db) o[db] = floatx16{};
 
   auto body = [&](int c, const char* kc, const char* vc, char* kn, char* vn) {
-    if (!CAREFUL && c + 1 < n) {
-      ck.issue(first_of(c + 1), p.len, kn, wave);
-      cv.issue(first_of(c + 1), p.len, vn, wave);
-    }
+    if (!CAREFUL && c + 1 < n) issue(c + 1, kn, vn);
     const int j0 = first_of(c);
     const bool none = j0 > w1 || (j0 + T::ROWS - 1 <= w0 - a.window && j0 >= a.sinks);
     if (!none) {
@@ -137,29 +147,21 @@ __device__ __forceinline__ void forward_pass(const WindowArgs& a, const WPlace& 
       }
       __builtin_amdgcn_s_setprio(0);
     }
-    if (!CAREFUL && c + 1 < n) {
-      ck.land(kn, wave, lane);
-      cv.land(vn, wave, lane);
-    }
-    __builtin_amdgcn_s_waitcnt(kWaitVm0);
-    __syncthreads();
+    if (!CAREFUL && c + 1 < n) arrive(kn, vn);
+    all_there();
   };
 
-  auto begin = [&](int c) {
-    ck.issue(first_of(c), p.len, kA, wave);
-    cv.issue(first_of(c), p.len, vA, wave);
-    ck.land(kA, wave, lane);
-    cv.land(vA, wave, lane);
-    __builtin_amdgcn_s_waitcnt(kWaitVm0);
-    __syncthreads();
-  };
+  arrive(kA, vA);
+  all_there();
   if constexpr (CAREFUL) {
     for (int c = 0; c < n; ++c) {
-      begin(c);
       body(c, kA, vA, kB, vB);
+      if (c + 1 == n) break;
+      issue(c + 1, kA, vA);
+      arrive(kA, vA);
+      all_there();
     }
   } else {
-    begin(0);
     for (int c = 0; c < n; c += 2) {
       body(c, kA, vA, kB, vB);
       if (c + 1 < n) body(c + 1, kB, vB, kA, vA);

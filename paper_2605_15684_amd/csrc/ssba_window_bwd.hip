@@ -52,15 +52,12 @@ __device__ __forceinline__ void order_rows() {
 // --------------------------------------------------------------------------
 template <class T, bool CAREFUL, int TERMS>
 __device__ __forceinline__ void dq_pass(const WindowArgs& a, const WPlace& p, int wave, int lane, char* kA, char* kB,
-                                        char* vA, char* vB, float delta, float lse2, floatx16 (&acc)[T::NDB], float& off) {
+                                        char* vA, char* vB, floatx16 (&acc)[T::NDB], float& ndelta, float& lse2) {
   constexpr int NB = T::NB, NDB = T::NDB;
   const int l32 = lane & 31, hw = lane >> 5;
   const int w0 = p.r0 + 32 * wave, w1 = min(w0 + 31, p.len - 1);
   const int i = w0 + l32;
   const int64_t row = p.begin + min(i, p.len - 1);
-  WRow<T> q, g;
-  q.load(static_cast<const char*>(a.q) + ((int64_t)p.b * a.sq.b + (int64_t)p.h * a.sq.h + row * a.sq.t) * T::SIZE, hw);
-  g.load(static_cast<const char*>(a.dout) + ((int64_t)p.b * a.sdo.b + (int64_t)p.h * a.sdo.h + row * a.sdo.t) * T::SIZE, hw);
   WCopy<T> ck, cv;
   ck.init(a.k, (int64_t)p.b * a.sk.b + (int64_t)p.kvh * a.sk.h + (int64_t)p.begin * a.sk.t, a.sk.t, wave, lane);
   cv.init(a.v, (int64_t)p.b * a.sv.b + (int64_t)p.kvh * a.sv.h + (int64_t)p.begin * a.sv.t, a.sv.t, wave, lane);
@@ -70,17 +67,54 @@ __device__ __forceinline__ void dq_pass(const WindowArgs& a, const WPlace& p, in
   const int n_sink = min((int)(((unsigned)min(a.sinks, last + 1) + T::ROWS - 1) / T::ROWS), low);
   const int n = n_sink + last / T::ROWS - low + 1;
   auto first_of = [&](int c) { return (c < n_sink ? c : low + c - n_sink) * T::ROWS; };
+  auto issue = [&](int c, char* kn, char* vn) {
+    ck.issue(first_of(c), p.len, kn, wave);
+    cv.issue(first_of(c), p.len, vn, wave);
+  };
+  // The end of a tile's copy.
+  auto arrive = [&](char* kn, char* vn) {
+    ck.land(kn, wave, lane);
+    cv.land(vn, wave, lane);
+  };
+  auto all_there = [&]() {
+    __builtin_amdgcn_s_waitcnt(kWaitVm0);
+    __syncthreads();
+  };
+  issue(0, kA, vA);   // before the rows: all are on their way at once
+
+  const char* gp = static_cast<const char*>(a.dout) + ((int64_t)p.b * a.sdo.b + (int64_t)p.h * a.sdo.h + row * a.sdo.t) * T::SIZE;
+  WRow<T> q, g;
+  q.load(static_cast<const char*>(a.q) + ((int64_t)p.b * a.sq.b + (int64_t)p.h * a.sq.h + row * a.sq.t) * T::SIZE, hw);
+  g.load(gp, hw);
+  lse2 = a.lse[((int64_t)p.b * a.heads + p.h) * a.seq + row] * kLog2e;
+  float delta = 0.f;
+  {
+    using R = WTile<T::D, T::F32 ? kF32 : kBf16>;   // values as they are
+    WRow<R> o, y;
+    o.load(static_cast<const char*>(a.o) + ((int64_t)p.b * a.so.b + (int64_t)p.h * a.so.h + row * a.so.t) * T::SIZE, hw);
+    y.load(gp, hw);
+#pragma unroll
+    for (int ks = 0; ks < R::NKS; ++ks)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        if constexpr (T::F32) {
+          delta = __builtin_fmaf(o.f[0][ks][e], y.f[0][ks][e], delta);
+        } else {
+          const uint32_t u = __float_as_uint(o.f[0][ks][e]), v = __float_as_uint(y.f[0][ks][e]);
+          delta = __builtin_fmaf(__uint_as_float(u << 16), __uint_as_float(v << 16), delta);
+          delta = __builtin_fmaf(__uint_as_float(u & 0xFFFF0000u), __uint_as_float(v & 0xFFFF0000u), delta);
+        }
+      }
+    delta += __shfl_xor(delta, 32);
+  }
 
   WLane<T> at(lane);
-  off = 0.f;
+  float off = 0.f;   // sum of the lane's ds
 #pragma unroll
   for (int db = 0; db < NDB; ++db) acc[db] = floatx16{};
 
   auto body = [&](int c, const char* kc, const char* vc, char* kn, char* vn) {
-    if (!CAREFUL && c + 1 < n) {
-      ck.issue(first_of(c + 1), p.len, kn, wave);
-      cv.issue(first_of(c + 1), p.len, vn, wave);
-    }
+    if (!CAREFUL && c + 1 < n) issue(c + 1, kn, vn);
     const int j0 = first_of(c);
     const bool none = j0 > w1 || (j0 + T::ROWS - 1 <= w0 - a.window && j0 >= a.sinks);
     if (!none) {
@@ -118,34 +152,27 @@ __device__ __forceinline__ void dq_pass(const WindowArgs& a, const WPlace& p, in
         if constexpr (T::ORDERED) __builtin_amdgcn_sched_barrier(0);
       }
     }
-    if (!CAREFUL && c + 1 < n) {
-      ck.land(kn, wave, lane);
-      cv.land(vn, wave, lane);
-    }
-    __builtin_amdgcn_s_waitcnt(kWaitVm0);
-    __syncthreads();
+    if (!CAREFUL && c + 1 < n) arrive(kn, vn);
+    all_there();
   };
 
-  auto begin = [&](int c) {
-    ck.issue(first_of(c), p.len, kA, wave);
-    cv.issue(first_of(c), p.len, vA, wave);
-    ck.land(kA, wave, lane);
-    cv.land(vA, wave, lane);
-    __builtin_amdgcn_s_waitcnt(kWaitVm0);
-    __syncthreads();
-  };
+  arrive(kA, vA);
+  all_there();
   if constexpr (CAREFUL) {   // one tile at a time: the other buffers are room for the rows' weights
     for (int c = 0; c < n; ++c) {
-      begin(c);
       body(c, kA, vA, kB, vB);
+      if (c + 1 == n) break;
+      issue(c + 1, kA, vA);
+      arrive(kA, vA);
+      all_there();
     }
   } else {
-    begin(0);
     for (int c = 0; c < n; c += 2) {
       body(c, kA, vA, kB, vB);
       if (c + 1 < n) body(c + 1, kB, vB, kA, vA);
     }
   }
+  ndelta = -(delta + off + __shfl_xor(off, 32));
 }
 
 // T: tiles of the first pass; TC: of the careful one.
@@ -166,37 +193,16 @@ __global__ __launch_bounds__(256, T::SPLIT && T::D == 128 ? 1 : 2) void k_window
   const int64_t row = p.begin + min(i, p.len - 1);
   const int64_t to = ((int64_t)p.b * a.heads + p.h) * a.seq + row;
 
-  float delta = 0.f;
-  {
-    WRow<TC> o, g;
-    g.load(static_cast<const char*>(a.dout) + ((int64_t)p.b * a.sdo.b + (int64_t)p.h * a.sdo.h + row * a.sdo.t) * T::SIZE, hw);
-    o.load(static_cast<const char*>(a.o) + ((int64_t)p.b * a.so.b + (int64_t)p.h * a.so.h + row * a.so.t) * T::SIZE, hw);
-#pragma unroll
-    for (int ks = 0; ks < TC::NKS; ++ks)
-#pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        if constexpr (T::F32) {
-          delta = __builtin_fmaf(o.f[0][ks][e], g.f[0][ks][e], delta);
-        } else {
-          const uint32_t x = __float_as_uint(o.f[0][ks][e]), y = __float_as_uint(g.f[0][ks][e]);
-          delta = __builtin_fmaf(__uint_as_float(x << 16), __uint_as_float(y << 16), delta);
-          delta = __builtin_fmaf(__uint_as_float(x & 0xFFFF0000u), __uint_as_float(y & 0xFFFF0000u), delta);
-        }
-      }
-    delta += __shfl_xor(delta, 32);
-  }
-  const float lse2 = a.lse[to] * kLog2e;
   floatx16 acc[NDB];
-  float off;   // sum of the lane's ds
+  float ndelta, lse2;
   if (threadIdx.x == 0) s_bad = 0;
-  dq_pass<T, false, TERMS>(a, p, wave, lane, kA, kB, vA, vB, delta, lse2, acc, off);
+  dq_pass<T, false, TERMS>(a, p, wave, lane, kA, kB, vA, vB, acc, ndelta, lse2);
   if (__builtin_amdgcn_ballot_w64(in && not_finite<NDB>(acc)) && lane == 0) s_bad = 1;
   __syncthreads();
-  if (s_bad) dq_pass<TC, true, TERMS>(a, p, wave, lane, kA, kB, vA, vB, delta, lse2, acc, off);
-  off += __shfl_xor(off, 32);
+  if (s_bad) dq_pass<TC, true, TERMS>(a, p, wave, lane, kA, kB, vA, vB, acc, ndelta, lse2);
   if (!in) return;
   if (hw == 0) {
-    a.ndelta[to] = -(delta + off);
+    a.ndelta[to] = ndelta;
     a.lse2[to] = lse2;
   }
   store_cols<T>(static_cast<char*>(a.dq) + ((int64_t)p.b * a.sdq.b + (int64_t)p.h * a.sdq.h + row * a.sdq.t) * T::SIZE, acc,
@@ -289,23 +295,6 @@ __device__ __forceinline__ void dkdv_pass(const WindowArgs& a, const KeyPlace& p
   const int w0 = p.k0 + 32 * wave, w1 = min(w0 + 31, p.len - 1);   // the wave's keys
   const int j = w0 + l32;
 
-  using KRow = typename std::conditional<KLDS, WRowLds<T>, WRow<T>>::type;
-  KRow k;
-  WRow<T> v;
-  {
-    const int64_t row = p.begin + min(j, p.len - 1);
-    WRow<T> kr;
-    kr.load(static_cast<const char*>(a.k) + ((int64_t)p.b * a.sk.b + (int64_t)p.kvh * a.sk.h + row * a.sk.t) * T::SIZE, hw);
-    if constexpr (KLDS) {   // read by this wave alone
-      k.at = s_k + 1024 * T::NKS * wave + 16 * lane;
-#pragma unroll
-      for (int ks = 0; ks < T::NKS; ++ks)
-        *reinterpret_cast<floatx4*>(s_k + 1024 * (T::NKS * wave + ks) + 16 * lane) = kr.f[0][ks];
-    } else {
-      k = kr;
-    }
-    v.load(static_cast<const char*>(a.v) + ((int64_t)p.b * a.sv.b + (int64_t)p.kvh * a.sv.h + row * a.sv.t) * T::SIZE, hw);
-  }
   WCopy<T> cq, cg;
   cq.init(a.q, (int64_t)p.b * a.sq.b + ((int64_t)p.kvh * a.group + p.g0) * a.sq.h + (int64_t)p.begin * a.sq.t, a.sq.t, wave,
           lane);
@@ -333,6 +322,34 @@ __device__ __forceinline__ void dkdv_pass(const WindowArgs& a, const KeyPlace& p
     }
   };
 
+  // The end of a tile's copy.
+  auto arrive = [&](char* qn, char* gn) {
+    cq.land(qn, wave, lane);
+    cg.land(gn, wave, lane);
+  };
+  auto all_there = [&]() {
+    __builtin_amdgcn_s_waitcnt(kWaitVm0);
+    __syncthreads();
+  };
+  issue(qA, gA, rA);   // before the keys: all are on their way at once
+
+  using KRow = typename std::conditional<KLDS, WRowLds<T>, WRow<T>>::type;
+  KRow k;
+  WRow<T> v;
+  {
+    const int64_t row = p.begin + min(j, p.len - 1);
+    WRow<T> kr;
+    kr.load(static_cast<const char*>(a.k) + ((int64_t)p.b * a.sk.b + (int64_t)p.kvh * a.sk.h + row * a.sk.t) * T::SIZE, hw);
+    if constexpr (KLDS) {   // read by this wave alone
+      k.at = s_k + 1024 * T::NKS * wave + 16 * lane;
+#pragma unroll
+      for (int ks = 0; ks < T::NKS; ++ks)
+        *reinterpret_cast<floatx4*>(s_k + 1024 * (T::NKS * wave + ks) + 16 * lane) = kr.f[0][ks];
+    } else {
+      k = kr;
+    }
+    v.load(static_cast<const char*>(a.v) + ((int64_t)p.b * a.sv.b + (int64_t)p.kvh * a.sv.h + row * a.sv.t) * T::SIZE, hw);
+  }
   WLane<T> place(lane);
   int at = 0;   // tile of the head
 #pragma unroll
@@ -395,28 +412,21 @@ __device__ __forceinline__ void dkdv_pass(const WindowArgs& a, const KeyPlace& p
         if constexpr (T::ORDERED) __builtin_amdgcn_sched_barrier(0);
       }
     }
-    if (!CAREFUL && c + 1 < n) {
-      cq.land(qn, wave, lane);
-      cg.land(gn, wave, lane);
-    }
-    __builtin_amdgcn_s_waitcnt(kWaitVm0);
-    __syncthreads();
+    if (!CAREFUL && c + 1 < n) arrive(qn, gn);
+    all_there();
   };
 
-  auto begin = [&]() {
-    issue(qA, gA, rA);
-    cq.land(qA, wave, lane);
-    cg.land(gA, wave, lane);
-    __builtin_amdgcn_s_waitcnt(kWaitVm0);
-    __syncthreads();
-  };
+  arrive(qA, gA);
+  all_there();
   if constexpr (CAREFUL) {   // one tile at a time: the other buffers are room for the rows' weights
     for (int c = 0; c < n; ++c) {
-      begin();
       body(c, qA, gA, rA, qB, gB, rB);
+      if (c + 1 == n) break;
+      issue(qA, gA, rA);
+      arrive(qA, gA);
+      all_there();
     }
   } else {
-    begin();
     for (int c = 0; c < n; c += 2) {
       body(c, qA, gA, rA, qB, gB, rB);
       if (c + 1 < n) body(c + 1, qB, gB, rB, qA, gA, rA);
