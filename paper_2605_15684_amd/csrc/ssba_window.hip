@@ -86,12 +86,14 @@ __device__ __forceinline__ void forward_pass(const WindowArgs& a, const WPlace& 
       }
       if (!whole) {
 #pragma unroll
-        for (int nb = 0; nb < NB; ++nb)
+        for (int nb = 0; nb < NB; ++nb) {
+          const uint32_t bits = keys_seen(i, j0 + 32 * nb, a.window, a.sinks) >> (4 * hw);
 #pragma unroll
           for (int e = 0; e < 16; ++e) {
-            const int j = j0 + 32 * nb + 8 * (e >> 2) + 4 * hw + (e & 3);
-            s[nb][e] = window_sees(i, j, a.window, a.sinks) ? s[nb][e] : -INFINITY;
+            const uint32_t seen = bit_of(bits, e);
+            s[nb][e] = __uint_as_float((__float_as_uint(s[nb][e]) & seen) | (0xFF800000u & ~seen));   // -infinity
           }
+        }
       }
       floatx16 pr[NB];
       float sum[NB];
@@ -139,7 +141,7 @@ __device__ __forceinline__ void forward_pass(const WindowArgs& a, const WPlace& 
             cols_product_seen<T>(
                 o, vc + nb * T::HALF, pr[nb],
                 reinterpret_cast<float*>((wave < T::TILE / 4096 ? kn : vn) + 4096 * (wave % (T::TILE / 4096))), lane,
-                [&](int row) { return window_sees(i, j0 + 32 * nb + row, a.window, a.sinks); });
+                keys_seen(i, j0 + 32 * nb, a.window, a.sinks));
             continue;
           }
         }

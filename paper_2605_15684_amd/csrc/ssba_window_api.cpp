@@ -69,7 +69,7 @@ ssba_status plan(const ssba_window* w, WindowArgs* a) {
   a->heads = w->heads;
   a->kv_heads = w->kv_heads;
   a->group = w->heads / w->kv_heads;
-  a->window = w->window;
+  a->window = std::max(1, std::min(w->window, w->seq));   // no token sees further back
   a->sinks = std::min(w->sinks, w->seq);
   a->seqs = w->seqs;
   a->scale = w->softmax_scale > 0.f ? w->softmax_scale : 1.0f / std::sqrt((float)w->head_dim);

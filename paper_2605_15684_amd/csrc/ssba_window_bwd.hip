@@ -131,11 +131,9 @@ __device__ __forceinline__ void dq_pass(const WindowArgs& a, const WPlace& p, in
 #pragma unroll
         for (int e = 0; e < 16; ++e) ds[e] *= __builtin_amdgcn_exp2f(__builtin_fmaf(s[e], a.scale_log2, -lse2));
         if (!whole) {
+          const uint32_t bits = keys_seen(i, j0 + 32 * nb, a.window, a.sinks) >> (4 * hw);
 #pragma unroll
-          for (int e = 0; e < 16; ++e) {
-            const int j = j0 + 32 * nb + 8 * (e >> 2) + 4 * hw + (e & 3);
-            ds[e] = window_sees(i, j, a.window, a.sinks) ? ds[e] : 0.f;
-          }
+          for (int e = 0; e < 16; ++e) ds[e] = keep_if(bit_of(bits, e), ds[e]);
         }
 #pragma unroll
         for (int e = 0; e < 16; ++e) off += ds[e];
@@ -144,7 +142,7 @@ __device__ __forceinline__ void dq_pass(const WindowArgs& a, const WPlace& p, in
             cols_product_seen<T>(
                 acc, kc + nb * T::HALF, ds,
                 reinterpret_cast<float*>((wave < T::TILE / 4096 ? kn : vn) + 4096 * (wave % (T::TILE / 4096))), lane,
-                [&](int r) { return window_sees(i, j0 + 32 * nb + r, a.window, a.sinks); });
+                keys_seen(i, j0 + 32 * nb, a.window, a.sinks));
             continue;
           }
         }
@@ -365,10 +363,6 @@ __device__ __forceinline__ void dkdv_pass(const WindowArgs& a, const KeyPlace& p
                          (w0 + 32 <= a.sinks || w0 > i0 + T::ROWS - 1 - a.window);
 #pragma unroll
       for (int nb = 0; nb < NB; ++nb) {
-        auto sees = [&](int r) {
-          const int i = i0 + 32 * nb + r;
-          return (i >= p.q0) & (i < p.q1) & window_sees(i, j, a.window, a.sinks);
-        };
         if constexpr (T::ORDERED) __builtin_amdgcn_sched_barrier(0);
         place.forget();
         floatx16 pr = {}, ds;
@@ -391,18 +385,20 @@ __device__ __forceinline__ void dkdv_pass(const WindowArgs& a, const KeyPlace& p
           }
         }
         if (!whole) {
+          const uint32_t bits = queries_seeing(j, i0 + 32 * nb, p.q0, p.q1, a.window, a.sinks) >> (4 * hw);
 #pragma unroll
           for (int e = 0; e < 16; ++e) {
-            const bool seen = sees(8 * (e >> 2) + 4 * hw + (e & 3));
-            pr[e] = seen ? pr[e] : 0.f;
-            ds[e] = seen ? ds[e] : 0.f;
+            const uint32_t seen = bit_of(bits, e);
+            pr[e] = keep_if(seen, pr[e]);
+            ds[e] = keep_if(seen, ds[e]);
           }
         }
         if constexpr (CAREFUL) {
           if (!whole) {
             float* room = reinterpret_cast<float*>((wave < T::TILE / 4096 ? qn : gn) + 4096 * (wave % (T::TILE / 4096)));
-            cols_product_seen<T>(dv, gc + nb * T::HALF, pr, room, lane, sees);
-            cols_product_seen<T>(dk, qc + nb * T::HALF, ds, room, lane, sees);
+            const uint32_t bits = queries_seeing(j, i0 + 32 * nb, p.q0, p.q1, a.window, a.sinks);
+            cols_product_seen<T>(dv, gc + nb * T::HALF, pr, room, lane, bits);
+            cols_product_seen<T>(dk, qc + nb * T::HALF, ds, room, lane, bits);
             continue;
           }
         }

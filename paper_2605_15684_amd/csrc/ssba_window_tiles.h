@@ -402,11 +402,11 @@ __device__ __forceinline__ void cols_product(floatx16 (&acc)[T::NDB], const char
 }
 
 // The same where rows that a column does not see must not reach it whatever
-// they hold (0 times NaN): one row after another.  sees(row): this lane's
-// column sees it.  `room`: 4 KB of LDS of the wave.
-template <class T, class Sees>
+// they hold (0 times NaN): one row after another.  `seen`: a bit for each row
+// that this lane's column sees.  `room`: 4 KB of LDS of the wave.
+template <class T>
 __device__ __forceinline__ void cols_product_seen(floatx16 (&acc)[T::NDB], const char* half, const floatx16& x,
-                                                            float* room, int lane, Sees sees) {
+                                                            float* room, int lane, uint32_t seen) {
   const int l32 = lane & 31, hw = lane >> 5;
 #pragma unroll
   for (int j = 0; j < 16; ++j) room[j * 64 + lane] = x[j];
@@ -417,7 +417,7 @@ __device__ __forceinline__ void cols_product_seen(floatx16 (&acc)[T::NDB], const
     for (int row = 0; row < 32; ++row) {
       const int j = 4 * (row >> 3) + (row & 3), from = (row >> 2) & 1;
       const float w = room[j * 64 + l32 + 32 * from];
-      const bool in = sees(row);
+      const bool in = (seen >> row) & 1;
 #pragma unroll
       for (int e = 0; e < 16; ++e) {
         const int ch = 32 * db + 8 * (e >> 2) + 4 * hw + (e & 3), at = ch * T::SIZE;
@@ -460,10 +460,25 @@ __device__ __forceinline__ bool not_finite(const floatx16 (&acc)[N]) {
   return t != 0.f;   // NaN
 }
 
-// Whether token i sees token j.  Without branches: a wave decides for 16 pairs a
-// lane.
-__device__ __forceinline__ bool window_sees(int i, int j, int window, int sinks) {
-  return ((unsigned)(i - j) < (unsigned)window) | (j < min(sinks, i + 1));
+// The low n bits, n clamped to 0 .. 32.
+__device__ __forceinline__ uint32_t low_bits(int n) { return n <= 0 ? 0u : ~0u >> (32 - min(n, 32)); }
+
+// Which of the tokens j0 .. j0 + 31 token i sees, a bit each.
+__device__ __forceinline__ uint32_t keys_seen(int i, int j0, int window, int sinks) {
+  return low_bits(i + 1 - j0) & (~low_bits(i + 1 - window - j0) | low_bits(sinks - j0));
 }
+
+// Which of the tokens i0 .. i0 + 31, of q0 .. q1 - 1, see token j.
+__device__ __forceinline__ uint32_t queries_seeing(int j, int i0, int q0, int q1, int window, int sinks) {
+  const int end = j < sinks ? q1 : min(q1, j + window);
+  return low_bits(end - i0) & ~low_bits(max(j, q0) - i0);
+}
+
+// Of such bits, all ones or zeros for element e of a 32 x 32 result (its row
+// 8 (e / 4) + 4 hw + e % 4); `bits` shifted right by 4 hw.
+__device__ __forceinline__ uint32_t bit_of(uint32_t bits, int e) {
+  return (uint32_t)((int32_t)(bits << (31 - (8 * (e >> 2) + (e & 3)))) >> 31);
+}
+__device__ __forceinline__ float keep_if(uint32_t ones, float x) { return __uint_as_float(__float_as_uint(x) & ones); }
 
 }  // namespace ssba
