@@ -49,48 +49,46 @@ __device__ __forceinline__ float2 turn(int pos, double f, bool inverse) {
   return make_float2(cosine, inverse ? -sine : sine);
 }
 
-// Eight consecutive channels (fp32 rows may begin at any multiple of 4 bytes).
+__device__ __forceinline__ void turn_pair(float& a, float& b, float2 w) {
+  const float x = __builtin_fmaf(a, w.x, -(b * w.y)), y = __builtin_fmaf(b, w.x, a * w.y);
+  a = w.x == kStays ? a : x;
+  b = w.x == kStays ? b : y;
+}
+
+// Sixteen bytes of a row (fp32 rows may begin at any multiple of 4 bytes).
 template <bool F32>
-struct Eight {
+struct Chunk {
+  static constexpr int N = F32 ? 4 : 8;   // channels
   typedef float vec4 __attribute__((ext_vector_type(4), aligned(4)));
   typedef typename std::conditional<F32, vec4, floatx4>::type vec;
-  floatx4 v[F32 ? 2 : 1];
-  __device__ __forceinline__ void load(const char* p) {
-#pragma unroll
-    for (int i = 0; i < (F32 ? 2 : 1); ++i) v[i] = *reinterpret_cast<const vec*>(p + 16 * i);
-  }
-  __device__ __forceinline__ void store(char* p) const {
-#pragma unroll
-    for (int i = 0; i < (F32 ? 2 : 1); ++i) *reinterpret_cast<vec*>(p + 16 * i) = v[i];
-  }
-  __device__ __forceinline__ floatx8 get() const {
+  floatx4 v;
+  __device__ __forceinline__ void load(const char* p) { v = *reinterpret_cast<const vec*>(p); }
+  __device__ __forceinline__ void store(char* p) const { *reinterpret_cast<vec*>(p) = v; }
+  __device__ __forceinline__ void get(float (&x)[N]) const {
     if constexpr (F32) {
-      return floatx8{v[0][0], v[0][1], v[0][2], v[0][3], v[1][0], v[1][1], v[1][2], v[1][3]};
+#pragma unroll
+      for (int j = 0; j < N; ++j) x[j] = v[j];
     } else {
-      return __builtin_convertvector(__builtin_bit_cast(bf16x8, v[0]), floatx8);
+      const floatx8 y = __builtin_convertvector(__builtin_bit_cast(bf16x8, v), floatx8);
+#pragma unroll
+      for (int j = 0; j < N; ++j) x[j] = y[j];
     }
   }
-  __device__ __forceinline__ void set(floatx8 x) {
+  __device__ __forceinline__ void set(const float (&x)[N]) {
     if constexpr (F32) {
-      v[0] = floatx4{x[0], x[1], x[2], x[3]};
-      v[1] = floatx4{x[4], x[5], x[6], x[7]};
+      v = floatx4{x[0], x[1], x[2], x[3]};
     } else {
-      v[0] = __builtin_bit_cast(floatx4, __builtin_convertvector(x, bf16x8));
+      v = __builtin_bit_cast(floatx4, __builtin_convertvector(floatx8{x[0], x[1], x[2], x[3], x[4], x[5], x[6], x[7]}, bf16x8));
     }
   }
 };
 
-__device__ __forceinline__ void turn_pair(float& a, float& b, float c, float s) {
-  const float x = __builtin_fmaf(a, c, -(b * s)), y = __builtin_fmaf(b, c, a * s);
-  a = c == kStays ? a : x;
-  b = c == kStays ? b : y;
-}
-
-// One workgroup: kRopeRows tokens, a part of the heads.  A thread holds two
-// eights (HALVES: channels c .. and D/2 + c ..) or one.
+// One workgroup: kRopeRows tokens, a part of the heads.  A thread holds a chunk
+// of a row, or two, D/2 channels apart (HALVES: each other's partners; fp32).
 template <int D, bool F32, bool HALVES>
 __global__ __launch_bounds__(256) void k_rope(TurnArgs a) {
-  constexpr int R = kRopeRows, H2 = D / 2, E = HALVES ? 2 : 1, PER = 4 * E;   // pairs of a thread
+  constexpr int R = kRopeRows, H2 = D / 2, N = Chunk<F32>::N, E = HALVES || F32 ? 2 : 1;
+  constexpr int PER = N * E / 2;   // pairs of a thread
   constexpr int TPR = H2 / PER, SLOTS = 256 / (TPR * R), SIZE = F32 ? 4 : 2;
   constexpr int U = 4;   // heads of a thread under way at once
   __shared__ float2 s_turn[R][H2];
@@ -103,11 +101,11 @@ __global__ __launch_bounds__(256) void k_rope(TurnArgs a) {
   const int all = a.heads[0] + a.heads[1];
   const int each = (all + a.head_parts - 1) / a.head_parts;
   const int h_end = in ? min(all, (part + 1) * each) : 0;
-  const int ch = at * 8;
+  const int ch = at * N;
   const int64_t x0 = b * a.x_sb[0] + t * a.x_st[0] + ch, x1 = b * a.x_sb[1] + t * a.x_st[1] + ch;
   const int64_t y0 = b * a.y_sb[0] + t * a.y_st[0] + ch, y1 = b * a.y_sb[1] + t * a.y_st[1] + ch;
 
-  Eight<F32> v[U][E];
+  Chunk<F32> v[U][E];
   auto load = [&](int h0) {
 #pragma unroll
     for (int u = 0; u < U; ++u) {
@@ -134,40 +132,35 @@ __global__ __launch_bounds__(256) void k_rope(TurnArgs a) {
     s_turn[r][j] = w;
   }
   __syncthreads();
-  float2 w[PER];
+  float2 w[PER];   // HALVES: of pairs ch ..; else of each chunk's
 #pragma unroll
-  for (int j = 0; j < PER; ++j) w[j] = s_turn[row][at * PER + j];
+  for (int j = 0; j < PER; ++j)
+    w[j] = s_turn[row][HALVES ? ch + j : ch / 2 + j % (N / 2) + j / (N / 2) * (H2 / 2)];
 
   for (; h < h_end; h += U * SLOTS) {
 #pragma unroll
     for (int u = 0; u < U; ++u) {
       const int hu = h + u * SLOTS;
       if (hu >= h_end) continue;
-      floatx8 x = v[u][0].get(), y;
-      if constexpr (HALVES) {
-        y = v[u][1].get();
+      float x[E][N];
 #pragma unroll
-        for (int j = 0; j < 8; ++j) {
-          float p = x[j], q = y[j];
-          turn_pair(p, q, w[j].x, w[j].y);
-          x[j] = p;
-          y[j] = q;
-        }
-        v[u][1].set(y);
+      for (int e = 0; e < E; ++e) v[u][e].get(x[e]);
+      if constexpr (HALVES) {
+#pragma unroll
+        for (int j = 0; j < N; ++j) turn_pair(x[0][j], x[1][j], w[j]);
       } else {
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          float p = x[2 * j], q = x[2 * j + 1];
-          turn_pair(p, q, w[j].x, w[j].y);
-          x[2 * j] = p;
-          x[2 * j + 1] = q;
-        }
+        for (int e = 0; e < E; ++e)
+#pragma unroll
+          for (int j = 0; j < N / 2; ++j) turn_pair(x[e][2 * j], x[e][2 * j + 1], w[e * (N / 2) + j]);
       }
-      v[u][0].set(x);
       const bool second = hu >= a.heads[0];
       char* o = a.y[second] + (second ? y1 + (hu - a.heads[0]) * a.y_sh[1] : y0 + hu * a.y_sh[0]) * SIZE;
 #pragma unroll
-      for (int e = 0; e < E; ++e) v[u][e].store(o + e * H2 * SIZE);
+      for (int e = 0; e < E; ++e) {
+        v[u][e].set(x[e]);
+        v[u][e].store(o + e * H2 * SIZE);
+      }
     }
     load(h + U * SLOTS);
   }
