@@ -12,7 +12,8 @@
 //
 // A value that a query does not see must not reach it, and 0 times a NaN would:
 // where a result is not finite, the workgroup computes once more with the tiles
-// that some query sees in part taken row by row.
+// that some query sees in part taken row by row.  So it does where the sum of a
+// query's probabilities is far off: the rounding of scores past 2^29 can do it.
 #include <hip/hip_runtime.h>
 
 #include "ssba_common.h"
@@ -22,7 +23,15 @@ namespace ssba {
 namespace {
 
 constexpr float kMost = 1048576.f;   // a lane's sum of probabilities of a half tile: 2^20
+constexpr float kLeast = 0x1p-60f;   // see k_window_forward
 constexpr float kLn2 = 0.69314718055994530942f;
+
+// x y - z, not fused.
+__device__ __forceinline__ float two_roundings(float x, float y, float z) {
+#pragma clang fp contract(off)
+  const float xy = x * y;
+  return xy - z;
+}
 
 // The wave's queries over all key tiles.  CAREFUL: one tile at a time, the
 // other buffers are room for the rows' weights.
@@ -104,7 +113,10 @@ __device__ __forceinline__ void forward_pass(const WindowArgs& a, const WPlace& 
           sum[nb] = 0.f;
 #pragma unroll
           for (int e = 0; e < 16; ++e) {
-            pr[nb][e] = __builtin_amdgcn_exp2f(__builtin_fmaf(s[nb][e], scale, -mu));
+            // With the product rounded as m's is, the largest of all gives 1 at any size of the scores (past 2^31 their
+            // rounding alone is beyond what exp2 takes).
+            const float x = CAREFUL ? two_roundings(s[nb][e], scale, mu) : __builtin_fmaf(s[nb][e], scale, -mu);
+            pr[nb][e] = __builtin_amdgcn_exp2f(x);
             sum[nb] += pr[nb][e];
           }
         }
@@ -190,7 +202,10 @@ __global__ __launch_bounds__(256, T::SPLIT && T::D == 128 ? 1 : 2) void k_window
   float m, l;
   if (threadIdx.x == 0) s_bad = 0;
   forward_pass<T, false>(a, p, wave, lane, kA, kB, vA, vB, o, m, l);
-  if (__builtin_amdgcn_ballot_w64(in && not_finite<NDB>(o)) && lane == 0) s_bad = 1;
+  // At least about 1, and 2^20 of each lane and half tile at most, but for what m's own rounding does.
+  const float all = l + __shfl_xor(l, 32);
+  const bool off = !(all > kLeast && all < 1.f / kLeast);
+  if (__builtin_amdgcn_ballot_w64(in && (off || not_finite<NDB>(o))) && lane == 0) s_bad = 1;
   __syncthreads();
   if (s_bad) forward_pass<TC, true>(a, p, wave, lane, kA, kB, vA, vB, o, m, l);
 

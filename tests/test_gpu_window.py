@@ -118,6 +118,32 @@ def test_scores_that_outgrow_the_running_maximum():
 
 @pytest.mark.parametrize("dtype", [BF16, F32])
 @pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("exponent", [5, 20, 35])
+def test_scores_past_what_exp2_takes(dtype, d, exponent):
+    """Scores of distinct multiples of 2^exponent, exact in fp32: the largest takes all, to the last bit; those behind
+    it are at most exp(-32) of it, together 2^-45."""
+    rng = np.random.default_rng(d + exponent)
+    n, window, sinks = 200, 70, 5
+    q, k = torch.zeros(1, 1, n, d, dtype=dtype), torch.zeros(1, 1, n, d, dtype=dtype)
+    rank = rng.permutation(n).astype(np.int64) + 1          # up to 8 bits: exact in bf16
+    q[..., 7] = 2.0 ** exponent
+    k[..., 7] = torch.from_numpy(rank).to(dtype)
+    v = normal(rng, (1, 1, n, d), dtype)
+    got = run(q.cuda(), k.cuda(), v.cuda(), None, window=window, sinks=sinks, scale=1.0)
+    for i in range(n):
+        seen = [j for j in range(i + 1) if j < sinks or j > i - window]
+        best = max(seen, key=lambda j: rank[j])
+        want = v[0, 0, best].double().numpy()
+        # o = (p v) (1 / p).  bf16: p and the result are rounded.  fp32: six products of terms in turn, three left out
+        # of 2^-24 each, 1 / p, the product.
+        bound = (11 * 2.0 ** -24 if dtype == F32 else 2 * 2.0 ** -8) * np.abs(want) + 2.0 ** -36
+        assert np.all(np.abs(got["o"][0, 0, i].double().cpu().numpy() - want) <= bound), i
+        # To base 2 and back: two constants, three operations, and the logarithm of p.
+        assert abs(float(got["lse"][0, 0, i]) / (2.0 ** exponent * rank[best]) - 1) <= 6 * 2.0 ** -24, i
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("d", [64, 128])
 def test_hidden_places_hold_anything(dtype, d):
     """NaN and infinities in single rows of one input at a time: what does not see them keeps its result."""
     rng = np.random.default_rng(d)
