@@ -226,14 +226,16 @@ AttendPlan plan(const ssba_cache* c, const ssba_cache_batch* b, const ssba_cache
 }
 
 // A window's keys: of the first token to the last one's, and the sinks.  Windows are as long as each other, whatever
-// the sequences, so 8 waves of a workgroup also replace parts where whole sequences would be split for their lengths
-// (64 sequences, 4 heads, 4096 + 64 keys, D 128: 36.8 us, in two parts 36.6 and 4.1 for the join).
+// the sequences, so from 256 workgroups on 8 waves of one also replace parts where whole sequences would be split for
+// their lengths, from 128 on of the larger rows of bf16 at D 128 (256 items, 4096 keys: bf16 D 64 24.4 to 27.0 us, fp32
+// 25.4 to 27.5 and D 128 46.0 to 48.7; 8128 keys 46.0 to 45.5, 41.4 to 46.4, 99.6 to 108.5; bf16 D 128, 128 items 25.2
+// to 27.9, 8128 keys 44.6 to 48.3; but bf16 D 64 30.6 to 26.5, fp32 36.9 to 27.3 of 128 items, 64 items 37 to 28).
 AttendPlan plan_window(const ssba_cache* c, const ssba_cache_batch* b, const ssba_cache_query* q, int32_t window,
                        int32_t sinks) {
   const int64_t cols = std::max<int64_t>(1, (int64_t)(q->heads / c->kv_heads) * b->max_new);
   AttendPlan p = plan(c, b, q, false, b->seqs, cols,
                       std::min<int64_t>((int64_t)window + sinks + b->max_new, std::max<int64_t>(1, long_of(c, b))));
-  if (p.tiles == 1 && p.splits > 1 && p.items >= (q->dtype == SSBA_DT_F32 ? 256 : 128) &&
+  if (p.tiles == 1 && p.splits > 1 && p.items >= (q->dtype == SSBA_DT_BF16 && c->head_dim == 128 ? 128 : 256) &&
       (int64_t)window + sinks + b->max_new <= 8192) {
     p.splits = 1;
     p.threads = 512;
