@@ -33,11 +33,11 @@ __device__ __forceinline__ float two_roundings(float x, float y, float z) {
   return xy - z;
 }
 
-// The wave's queries over all key tiles.  CAREFUL: one tile at a time, the
-// other buffers are room for the rows' weights.
-template <class T, bool CAREFUL>
-__device__ __forceinline__ void forward_pass(const WindowArgs& a, const WPlace& p, int wave, int lane, char* kA, char* kB,
-                                             char* vA, char* vB, floatx16 (&o)[T::NDB], float& m, float& l) {
+// The wave's queries over every G-th key tile from the `group`-th on.  CAREFUL:
+// one tile at a time, the other buffers are room for the rows' weights.
+template <class T, bool CAREFUL, int G>
+__device__ __forceinline__ void forward_pass(const WindowArgs& a, const WPlace& p, int group, int wave, int lane, char* kA,
+                                             char* kB, char* vA, char* vB, floatx16 (&o)[T::NDB], float& m, float& l) {
   constexpr int NB = T::NB, NDB = T::NDB;
   const int l32 = lane & 31, hw = lane >> 5;
   const int w0 = p.r0 + 32 * wave, w1 = min(w0 + 31, p.len - 1);   // the wave's queries; w1 < w0: none
@@ -52,8 +52,11 @@ __device__ __forceinline__ void forward_pass(const WindowArgs& a, const WPlace& 
   const int last = min(p.r0 + kWindowRows, p.len) - 1;
   const int low = max(p.r0 - a.window + 1, 0) / T::ROWS;
   const int n_sink = min((int)(((unsigned)min(a.sinks, last + 1) + T::ROWS - 1) / T::ROWS), low);
-  const int n = n_sink + last / T::ROWS - low + 1;
-  auto first_of = [&](int c) { return (c < n_sink ? c : low + c - n_sink) * T::ROWS; };
+  const int n = (n_sink + last / T::ROWS - low + 1 + G - 1) / G;   // turns: those behind the last tile see nothing
+  auto first_of = [&](int turn) {
+    const int c = G * turn + group;
+    return (c < n_sink ? c : low + c - n_sink) * T::ROWS;
+  };
   auto issue = [&](int c, char* kn, char* vn) {
     ck.issue(first_of(c), p.len, kn, wave);
     cv.issue(first_of(c), p.len, vn, wave);
@@ -183,17 +186,20 @@ __device__ __forceinline__ void forward_pass(const WindowArgs& a, const WPlace& 
   }
 }
 
-// T: tiles of the first pass; TC: of the careful one.
-template <class T, class TC>
-__global__ __launch_bounds__(256, T::SPLIT && T::D == 128 ? 1 : 2) void k_window_forward(WindowArgs a) {
+// T: tiles of the first pass; TC: of the careful one.  G: groups of four waves
+// that share the key tiles.
+template <class T, class TC, int G>
+__global__ __launch_bounds__(256 * G, T::SPLIT && T::D == 128 ? 1 : 2) void k_window_forward(WindowArgs a) {
   constexpr int NDB = T::NDB, BYTES = T::TILE > TC::TILE ? T::TILE : TC::TILE;
-  __shared__ __attribute__((aligned(16))) char kA[BYTES];
-  __shared__ __attribute__((aligned(16))) char kB[BYTES];
-  __shared__ __attribute__((aligned(16))) char vA[BYTES];
-  __shared__ __attribute__((aligned(16))) char vB[BYTES];
+  __shared__ __attribute__((aligned(16))) char kA[G][BYTES];
+  __shared__ __attribute__((aligned(16))) char kB[G][BYTES];
+  __shared__ __attribute__((aligned(16))) char vA[G][BYTES];
+  __shared__ __attribute__((aligned(16))) char vB[G][BYTES];
+  __shared__ float s_ml[G == 1 ? 1 : 2 * G][256];
   __shared__ int s_bad;
   const int lane = threadIdx.x & 63, hw = lane >> 5;
-  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) % 4;
+  const int group = G == 1 ? 0 : __builtin_amdgcn_readfirstlane(threadIdx.x >> 8);
   WPlace p;
   if (!place_query(a, lane, &p)) return;
   const int i = p.r0 + 32 * wave + (lane & 31);
@@ -201,26 +207,46 @@ __global__ __launch_bounds__(256, T::SPLIT && T::D == 128 ? 1 : 2) void k_window
   floatx16 o[NDB];
   float m, l;
   if (threadIdx.x == 0) s_bad = 0;
-  forward_pass<T, false>(a, p, wave, lane, kA, kB, vA, vB, o, m, l);
+  forward_pass<T, false, G>(a, p, group, wave, lane, kA[group], kB[group], vA[group], vB[group], o, m, l);
   // At least about 1, and 2^20 of each lane and half tile at most, but for what m's own rounding does.
   const float all = l + __shfl_xor(l, 32);
-  const bool off = !(all > kLeast && all < 1.f / kLeast);
+  const bool off = (G == 1 || m != -INFINITY) && !(all > kLeast && all < 1.f / kLeast);
   if (__builtin_amdgcn_ballot_w64(in && (off || not_finite<NDB>(o))) && lane == 0) s_bad = 1;
   __syncthreads();
-  if (s_bad) forward_pass<TC, true>(a, p, wave, lane, kA, kB, vA, vB, o, m, l);
+  if (s_bad) forward_pass<TC, true, G>(a, p, group, wave, lane, kA[group], kB[group], vA[group], vB[group], o, m, l);
 
   l += __shfl_xor(l, 32);
+  if constexpr (G == 2) {
+    const int thread = threadIdx.x & 255;
+    s_ml[2 * group][thread] = m;
+    s_ml[2 * group + 1][thread] = l;
+    __syncthreads();
+    const float m2 = s_ml[2 - 2 * group][thread], l2 = s_ml[3 - 2 * group][thread], top = fmaxf(m, m2);
+    const float f = m == top ? 1.f : __builtin_amdgcn_exp2f(m - top), f2 = m2 == top ? 1.f : __builtin_amdgcn_exp2f(m2 - top);
+    m = top;
+    l = l * f + l2 * f2;
+#pragma unroll
+    for (int db = 0; db < NDB; ++db) o[db] *= f;
+    join_groups<NDB>(o, group, thread, kA[0], kB[0], vA[0], vB[0]);
+  }
   if (!in) return;
   const int64_t row = p.begin + i;
-  store_cols<T>(static_cast<char*>(a.o) + ((int64_t)p.b * a.so.b + (int64_t)p.h * a.so.h + row * a.so.t) * T::SIZE, o,
-                1.f / l, hw);
-  if (a.lse && hw == 0)
+  char* to = static_cast<char*>(a.o) + ((int64_t)p.b * a.so.b + (int64_t)p.h * a.so.h + row * a.so.t) * T::SIZE;
+  store_cols<T, NDB / G>(to + group * (NDB / G) * 32 * T::SIZE, o, 1.f / l, hw);
+  if (a.lse && hw == 0 && group == 0)
     a.lse[((int64_t)p.b * a.heads + p.h) * a.seq + row] = (m + __builtin_amdgcn_logf(l)) * kLn2;
 }
 
 template <class T, class TC>
 hipError_t launch(const WindowArgs& a, hipStream_t s) {
-  k_window_forward<T, TC><<<(unsigned)((int64_t)a.batch * a.heads * a.slots), 256, 0, s>>>(a);
+  const unsigned groups = (unsigned)((int64_t)a.batch * a.heads * a.slots);
+  if constexpr (!(T::SPLIT && T::D == 128)) {
+    if (share_tiles(a, groups)) {
+      k_window_forward<T, TC, 2><<<groups, 512, 0, s>>>(a);
+      return hipGetLastError();
+    }
+  }
+  k_window_forward<T, TC, 1><<<groups, 256, 0, s>>>(a);
   return hipGetLastError();
 }
 

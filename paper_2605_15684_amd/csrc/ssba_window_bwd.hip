@@ -50,9 +50,10 @@ __device__ __forceinline__ void order_rows() {
 // to 8 bits.  Errors of dq and dk against 64 bits, over that of a result's own
 // rounding (window 64, D 64, 200 rows): 1.58 and 1.53 without either.
 // --------------------------------------------------------------------------
-template <class T, bool CAREFUL, int TERMS>
-__device__ __forceinline__ void dq_pass(const WindowArgs& a, const WPlace& p, int wave, int lane, char* kA, char* kB,
-                                        char* vA, char* vB, floatx16 (&acc)[T::NDB], float& ndelta, float& lse2) {
+template <class T, bool CAREFUL, int TERMS, int G>
+__device__ __forceinline__ void dq_pass(const WindowArgs& a, const WPlace& p, int group, int wave, int lane, char* kA,
+                                        char* kB, char* vA, char* vB, floatx16 (&acc)[T::NDB], float& delta, float& off,
+                                        float& lse2) {
   constexpr int NB = T::NB, NDB = T::NDB;
   const int l32 = lane & 31, hw = lane >> 5;
   const int w0 = p.r0 + 32 * wave, w1 = min(w0 + 31, p.len - 1);
@@ -65,8 +66,11 @@ __device__ __forceinline__ void dq_pass(const WindowArgs& a, const WPlace& p, in
   const int last = min(p.r0 + kWindowRows, p.len) - 1;
   const int low = max(p.r0 - a.window + 1, 0) / T::ROWS;
   const int n_sink = min((int)(((unsigned)min(a.sinks, last + 1) + T::ROWS - 1) / T::ROWS), low);
-  const int n = n_sink + last / T::ROWS - low + 1;
-  auto first_of = [&](int c) { return (c < n_sink ? c : low + c - n_sink) * T::ROWS; };
+  const int n = (n_sink + last / T::ROWS - low + 1 + G - 1) / G;   // turns: those behind the last tile see nothing
+  auto first_of = [&](int turn) {
+    const int c = G * turn + group;
+    return (c < n_sink ? c : low + c - n_sink) * T::ROWS;
+  };
   auto issue = [&](int c, char* kn, char* vn) {
     ck.issue(first_of(c), p.len, kn, wave);
     cv.issue(first_of(c), p.len, vn, wave);
@@ -87,7 +91,7 @@ __device__ __forceinline__ void dq_pass(const WindowArgs& a, const WPlace& p, in
   q.load(static_cast<const char*>(a.q) + ((int64_t)p.b * a.sq.b + (int64_t)p.h * a.sq.h + row * a.sq.t) * T::SIZE, hw);
   g.load(gp, hw);
   lse2 = a.lse[((int64_t)p.b * a.heads + p.h) * a.seq + row] * kLog2e;
-  float delta = 0.f;
+  delta = 0.f;
   {
     using R = WTile<T::D, T::F32 ? kF32 : kBf16>;   // values as they are
     WRow<R> o, y;
@@ -109,7 +113,7 @@ __device__ __forceinline__ void dq_pass(const WindowArgs& a, const WPlace& p, in
   }
 
   WLane<T> at(lane);
-  float off = 0.f;   // sum of the lane's ds
+  off = 0.f;   // sum of the lane's ds
 #pragma unroll
   for (int db = 0; db < NDB; ++db) acc[db] = floatx16{};
 
@@ -170,20 +174,23 @@ __device__ __forceinline__ void dq_pass(const WindowArgs& a, const WPlace& p, in
       if (c + 1 < n) body(c + 1, kB, vB, kA, vA);
     }
   }
-  ndelta = -(delta + off + __shfl_xor(off, 32));
+  off += __shfl_xor(off, 32);
 }
 
-// T: tiles of the first pass; TC: of the careful one.
-template <class T, class TC, int TERMS>
-__global__ __launch_bounds__(256, T::SPLIT && T::D == 128 ? 1 : 2) void k_window_dq(WindowArgs a) {
+// T: tiles of the first pass; TC: of the careful one.  G: groups of four waves
+// that share the key tiles.
+template <class T, class TC, int TERMS, int G>
+__global__ __launch_bounds__(256 * G, T::SPLIT && T::D == 128 ? 1 : 2) void k_window_dq(WindowArgs a) {
   constexpr int NDB = T::NDB, BYTES = T::TILE > TC::TILE ? T::TILE : TC::TILE;
-  __shared__ __attribute__((aligned(16))) char kA[BYTES];
-  __shared__ __attribute__((aligned(16))) char kB[BYTES];
-  __shared__ __attribute__((aligned(16))) char vA[BYTES];
-  __shared__ __attribute__((aligned(16))) char vB[BYTES];
+  __shared__ __attribute__((aligned(16))) char kA[G][BYTES];
+  __shared__ __attribute__((aligned(16))) char kB[G][BYTES];
+  __shared__ __attribute__((aligned(16))) char vA[G][BYTES];
+  __shared__ __attribute__((aligned(16))) char vB[G][BYTES];
+  __shared__ float s_off[G == 1 ? 1 : 256];
   __shared__ int s_bad;
   const int lane = threadIdx.x & 63, hw = lane >> 5;
-  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) % 4;
+  const int group = G == 1 ? 0 : __builtin_amdgcn_readfirstlane(threadIdx.x >> 8);
   WPlace p;
   if (!place_query(a, lane, &p)) return;
   const int i = p.r0 + 32 * wave + (lane & 31);
@@ -192,19 +199,26 @@ __global__ __launch_bounds__(256, T::SPLIT && T::D == 128 ? 1 : 2) void k_window
   const int64_t to = ((int64_t)p.b * a.heads + p.h) * a.seq + row;
 
   floatx16 acc[NDB];
-  float ndelta, lse2;
+  float delta, off, lse2;
   if (threadIdx.x == 0) s_bad = 0;
-  dq_pass<T, false, TERMS>(a, p, wave, lane, kA, kB, vA, vB, acc, ndelta, lse2);
+  dq_pass<T, false, TERMS, G>(a, p, group, wave, lane, kA[group], kB[group], vA[group], vB[group], acc, delta, off, lse2);
   if (__builtin_amdgcn_ballot_w64(in && not_finite<NDB>(acc)) && lane == 0) s_bad = 1;
   __syncthreads();
-  if (s_bad) dq_pass<TC, true, TERMS>(a, p, wave, lane, kA, kB, vA, vB, acc, ndelta, lse2);
+  if (s_bad)
+    dq_pass<TC, true, TERMS, G>(a, p, group, wave, lane, kA[group], kB[group], vA[group], vB[group], acc, delta, off, lse2);
+  if constexpr (G == 2) {
+    const int thread = threadIdx.x & 255;
+    if (group) s_off[thread] = off;
+    join_groups<NDB>(acc, group, thread, kA[0], kB[0], vA[0], vB[0]);
+    if (!group) off += s_off[thread];
+  }
   if (!in) return;
-  if (hw == 0) {
-    a.ndelta[to] = ndelta;
+  if (hw == 0 && group == 0) {
+    a.ndelta[to] = -(delta + off);
     a.lse2[to] = lse2;
   }
-  store_cols<T>(static_cast<char*>(a.dq) + ((int64_t)p.b * a.sdq.b + (int64_t)p.h * a.sdq.h + row * a.sdq.t) * T::SIZE, acc,
-                a.scale, hw);
+  char* dq = static_cast<char*>(a.dq) + ((int64_t)p.b * a.sdq.b + (int64_t)p.h * a.sdq.h + row * a.sdq.t) * T::SIZE;
+  store_cols<T, NDB / G>(dq + group * (NDB / G) * 32 * T::SIZE, acc, a.scale, hw);
 }
 
 // --------------------------------------------------------------------------
@@ -282,9 +296,9 @@ __device__ __forceinline__ void copy_values(const float* from, int n, float* dst
   __builtin_amdgcn_raw_ptr_buffer_load_lds(rs, (lds_void*)dst, 4, 4 * lane, 0, 0, 0);
 }
 
-template <class T, bool CAREFUL>
-__device__ __forceinline__ void dkdv_pass(const WindowArgs& a, const KeyPlace& p, int wave, int lane, char* s_k, char* qA,
-                                          char* qB, char* gA, char* gB, float (*rA)[64], float (*rB)[64],
+template <class T, bool CAREFUL, int G>
+__device__ __forceinline__ void dkdv_pass(const WindowArgs& a, const KeyPlace& p, int group, int wave, int lane, char* s_k,
+                                          char* qA, char* qB, char* gA, char* gB, float (*rA)[64], float (*rB)[64],
                                           floatx16 (&dk)[T::NDB], floatx16 (&dv)[T::NDB]) {
   constexpr int NB = T::NB, NDB = T::NDB;
   // The wave's keys as operands in the LDS where registers are short.
@@ -304,18 +318,20 @@ __device__ __forceinline__ void dkdv_pass(const WindowArgs& a, const KeyPlace& p
   const float* l_base = a.lse2 + head * a.seq + p.begin;
   const float* d_base = a.ndelta + head * a.seq + p.begin;
 
-  // Tiles of queries, head after head.
-  const int t0 = p.q0 / T::ROWS, per_head = (p.q1 - 1) / T::ROWS - t0 + 1, n = per_head * (p.g1 - p.g0);
-  int next_g = 0, next_t = 0;   // of the tile that is copied next
+  // Every G-th tile of queries, head after head: as many for each group (one behind the last tile of a head sees
+  // nothing).
+  const int t0 = p.q0 / T::ROWS, tiles = (p.q1 - 1) / T::ROWS - t0 + 1;
+  const int per_head = (tiles + G - 1) / G * G, n = per_head / G * (p.g1 - p.g0);
+  int next_g = 0, next_t = group;   // of the tile that is copied next
   auto issue = [&](char* qd, char* gd, float (*rd)[64]) {
     cq.base = q_base + (int64_t)next_g * a.sq.h * T::SIZE;
     cg.base = g_base + (int64_t)next_g * a.sdo.h * T::SIZE;
     const int i0 = (t0 + next_t) * T::ROWS;
     cq.issue(i0, p.len, qd, wave);
     cg.issue(i0, p.len, gd, wave);
-    if (wave < 2) copy_values((wave ? d_base : l_base) + (int64_t)next_g * a.seq + i0, min(p.len - i0, T::ROWS), rd[wave], lane);
-    if (++next_t == per_head) {
-      next_t = 0;
+    if (wave < 2) copy_values((wave ? d_base : l_base) + (int64_t)next_g * a.seq + i0, max(min(p.len - i0, T::ROWS), 0), rd[wave], lane);
+    if ((next_t += G) >= per_head) {
+      next_t = group;
       ++next_g;
     }
   };
@@ -349,15 +365,15 @@ __device__ __forceinline__ void dkdv_pass(const WindowArgs& a, const KeyPlace& p
     v.load(static_cast<const char*>(a.v) + ((int64_t)p.b * a.sv.b + (int64_t)p.kvh * a.sv.h + row * a.sv.t) * T::SIZE, hw);
   }
   WLane<T> place(lane);
-  int at = 0;   // tile of the head
+  int at = group;   // tile of the head
 #pragma unroll
   for (int db = 0; db < NDB; ++db) dk[db] = dv[db] = floatx16{};
 
   auto body = [&](int c, const char* qc, const char* gc, float (*rc)[64], char* qn, char* gn, float (*rn)[64]) {
     if (!CAREFUL && c + 1 < n) issue(qn, gn, rn);
     const int i0 = (t0 + at) * T::ROWS;
-    if (++at == per_head) at = 0;
-    const bool none = i0 + T::ROWS - 1 < w0 || (w1 <= i0 - a.window && w0 >= a.sinks) || w0 >= p.len;
+    if ((at += G) >= per_head) at = group;
+    const bool none = i0 + T::ROWS - 1 < w0 || (G > 1 && i0 >= p.q1) || (w1 <= i0 - a.window && w0 >= a.sinks) || w0 >= p.len;
     if (!none) {
       const bool whole = i0 >= max(w0 + 31, p.q0) && i0 + T::ROWS <= p.q1 &&
                          (w0 + 32 <= a.sinks || w0 > i0 + T::ROWS - 1 - a.window);
@@ -430,43 +446,56 @@ __device__ __forceinline__ void dkdv_pass(const WindowArgs& a, const KeyPlace& p
   }
 }
 
-// T: tiles of the first pass; TC: of the careful one.
-template <class T, class TC>
-__global__ __launch_bounds__(256, T::SPLIT && T::D == 128 ? 1 : 2) void k_window_dkdv(WindowArgs a) {
+// T: tiles of the first pass; TC: of the careful one.  G: groups of four waves
+// that share the tiles of queries.
+template <class T, class TC, int G>
+__global__ __launch_bounds__(256 * G, T::SPLIT && T::D == 128 ? 1 : 2) void k_window_dkdv(WindowArgs a) {
   constexpr int NDB = T::NDB, BYTES = T::TILE > TC::TILE ? T::TILE : TC::TILE;
-  __shared__ __attribute__((aligned(16))) char s_k[T::ORDERED ? 4 * T::NKS * 1024 : 16];
-  __shared__ __attribute__((aligned(16))) char qA[BYTES];
-  __shared__ __attribute__((aligned(16))) char qB[BYTES];
-  __shared__ __attribute__((aligned(16))) char gA[BYTES];
-  __shared__ __attribute__((aligned(16))) char gB[BYTES];
-  __shared__ __attribute__((aligned(16))) float rA[2][64];   // lse2, -delta of the tile's rows
-  __shared__ __attribute__((aligned(16))) float rB[2][64];
+  __shared__ __attribute__((aligned(16))) char s_k[T::ORDERED ? G * 4 * T::NKS * 1024 : 16];
+  __shared__ __attribute__((aligned(16))) char qA[G][BYTES];
+  __shared__ __attribute__((aligned(16))) char qB[G][BYTES];
+  __shared__ __attribute__((aligned(16))) char gA[G][BYTES];
+  __shared__ __attribute__((aligned(16))) char gB[G][BYTES];
+  __shared__ __attribute__((aligned(16))) float rA[G][2][64];   // lse2, -delta of the tile's rows
+  __shared__ __attribute__((aligned(16))) float rB[G][2][64];
   __shared__ int s_bad;
   const int lane = threadIdx.x & 63, l32 = lane & 31, hw = lane >> 5;
-  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) % 4;
+  const int group = G == 1 ? 0 : __builtin_amdgcn_readfirstlane(threadIdx.x >> 8);
   KeyPlace p;
   if (!place_keys(a, lane, &p)) return;
   const int j = p.k0 + 32 * wave + l32;
   const bool in = j < p.len;
   floatx16 dk[NDB], dv[NDB];
   if (threadIdx.x == 0) s_bad = 0;
-  dkdv_pass<T, false>(a, p, wave, lane, s_k, qA, qB, gA, gB, rA, rB, dk, dv);
+  char* keys = s_k + (T::ORDERED ? group * 4 * T::NKS * 1024 : 0);
+  dkdv_pass<T, false, G>(a, p, group, wave, lane, keys, qA[group], qB[group], gA[group], gB[group], rA[group], rB[group], dk,
+                         dv);
   if (__builtin_amdgcn_ballot_w64(in && (not_finite<NDB>(dk) || not_finite<NDB>(dv))) && lane == 0) s_bad = 1;
   __syncthreads();
-  if (s_bad) dkdv_pass<TC, true>(a, p, wave, lane, s_k, qA, qB, gA, gB, rA, rB, dk, dv);
+  if (s_bad)
+    dkdv_pass<TC, true, G>(a, p, group, wave, lane, keys, qA[group], qB[group], gA[group], gB[group], rA[group], rB[group],
+                           dk, dv);
+  if constexpr (G == 2) {
+    join_groups<NDB>(dk, group, threadIdx.x & 255, qA[0], qB[0], gA[0], gB[0]);
+    join_groups<NDB>(dv, group, threadIdx.x & 255, qA[0], qB[0], gA[0], gB[0]);
+  }
   if (!in) return;
+  const int ch = group * (NDB / G) * 32;   // first channel
   if (p.part >= 0) {
     using P = WTile<T::D, kF32>;
-    char* to = reinterpret_cast<char*>(a.part + (p.part + 32 * wave + l32) * T::D);
-    store_cols<P>(to, dk, 1.f, hw);
-    store_cols<P>(to + (int64_t)kWindowRows * T::D * 4, dv, 1.f, hw);
+    char* to = reinterpret_cast<char*>(a.part + (p.part + 32 * wave + l32) * T::D + ch);
+    store_cols<P, NDB / G>(to, dk, 1.f, hw);
+    store_cols<P, NDB / G>(to + (int64_t)kWindowRows * T::D * 4, dv, 1.f, hw);
     return;
   }
   const int64_t row = p.begin + j;
-  store_cols<T>(static_cast<char*>(a.dk) + ((int64_t)p.b * a.sdk.b + (int64_t)p.kvh * a.sdk.h + row * a.sdk.t) * T::SIZE, dk,
-                a.scale, hw);
-  store_cols<T>(static_cast<char*>(a.dv) + ((int64_t)p.b * a.sdv.b + (int64_t)p.kvh * a.sdv.h + row * a.sdv.t) * T::SIZE, dv,
-                1.f, hw);
+  store_cols<T, NDB / G>(
+      static_cast<char*>(a.dk) + ((int64_t)p.b * a.sdk.b + (int64_t)p.kvh * a.sdk.h + row * a.sdk.t + ch) * T::SIZE, dk,
+      a.scale, hw);
+  store_cols<T, NDB / G>(
+      static_cast<char*>(a.dv) + ((int64_t)p.b * a.sdv.b + (int64_t)p.kvh * a.sdv.h + row * a.sdv.t + ch) * T::SIZE, dv,
+      1.f, hw);
 }
 
 // Adds up the parts of a tile's chunks and heads, in their order: a workgroup
@@ -536,19 +565,32 @@ __global__ __launch_bounds__(256) void k_window_join(WindowArgs a) {
 
 // T: tiles of the query side, TK: of the key side; TC: of the careful passes
 // (the key side's in those of TK where it is bf16).
+template <class T, class TC, int TERMS>
+void launch_dq(const WindowArgs& a, hipStream_t s) {
+  const unsigned groups = (unsigned)((int64_t)a.batch * a.heads * a.slots);
+  if constexpr (!(T::SPLIT && T::D == 128))
+    if (share_tiles(a, groups)) return k_window_dq<T, TC, TERMS, 2><<<groups, 512, 0, s>>>(a);
+  k_window_dq<T, TC, TERMS, 1><<<groups, 256, 0, s>>>(a);
+}
+
 template <class T, class TK, class TC>
 hipError_t launch(const WindowArgs& a, hipStream_t s) {
   using TKC = typename std::conditional<T::F32, TC, TK>::type;
   const int64_t units = (int64_t)a.batch * a.kv_heads, cut = (int64_t)a.sink_tiles * a.chunk_slots;
   const int64_t kept = cut + (a.head_parts > 1 ? a.slots : 0);
-  const unsigned groups = (unsigned)((int64_t)a.batch * a.heads * a.slots);
   if (!T::F32 && (int64_t)a.window + a.sinks <= 1024)
-    k_window_dq<T, TC, T::F32 ? 1 : 2><<<groups, 256, 0, s>>>(a);
+    launch_dq<T, TC, T::F32 ? 1 : 2>(a, s);
   else
-    k_window_dq<T, TC, 1><<<groups, 256, 0, s>>>(a);
+    launch_dq<T, TC, 1>(a, s);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
-  k_window_dkdv<TK, TKC><<<(unsigned)(units * (a.slots + cut) * a.head_parts), 256, 0, s>>>(a);
+  const unsigned groups = (unsigned)(units * (a.slots + cut) * a.head_parts);
+  bool few = false;
+  if constexpr (!(T::SPLIT && T::D == 128)) {
+    few = share_tiles(a, groups, T::SPLIT ? 1024 : 256);
+    if (few) k_window_dkdv<TK, TKC, 2><<<groups, 512, 0, s>>>(a);
+  }
+  if (!few) k_window_dkdv<TK, TKC, 1><<<groups, 256, 0, s>>>(a);
   if ((e = hipGetLastError()) != hipSuccess || !kept) return e;
   k_window_join<T><<<(unsigned)(units * kept * (kWindowRows * T::D / 2048)), 256, 0, s>>>(a);
   return hipGetLastError();

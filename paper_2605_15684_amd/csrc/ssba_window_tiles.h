@@ -433,11 +433,12 @@ __device__ __forceinline__ void cols_product_seen(floatx16 (&acc)[T::NDB], const
   __builtin_amdgcn_wave_barrier();
 }
 
-// A result as rows of the lane's column: 4 consecutive channels at a time.
-template <class T>
+// A result as rows of the lane's column: 4 consecutive channels at a time, of
+// the first N blocks of acc.
+template <class T, int N = T::NDB>
 __device__ __forceinline__ void store_cols(char* row, const floatx16 (&acc)[T::NDB], float f, int hw) {
 #pragma unroll
-  for (int db = 0; db < T::NDB; ++db)
+  for (int db = 0; db < N; ++db)
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
       const float x[4] = {acc[db][4 * j] * f, acc[db][4 * j + 1] * f, acc[db][4 * j + 2] * f, acc[db][4 * j + 3] * f};
@@ -446,6 +447,39 @@ __device__ __forceinline__ void store_cols(char* row, const floatx16 (&acc)[T::N
         *reinterpret_cast<floatx4*>(p) = floatx4{x[0], x[1], x[2], x[3]};
       else
         *reinterpret_cast<uint2*>(p) = make_uint2(pack2(x[0], x[1]), pack2(x[2], x[3]));
+    }
+}
+
+// The sums of two groups of four waves that had the same rows or keys: group 0
+// has the first half of the channel blocks of both then, group 1 the second, in
+// acc[0 .. NDB / 2 - 1].  A quarter of the passed values goes through each buffer:
+// NDB / 2 * 8 KB of them.
+template <int NDB>
+__device__ __forceinline__ void join_groups(floatx16 (&acc)[NDB], int group, int thread, char* b0, char* b1, char* b2, char* b3) {
+  float* const room[4] = {reinterpret_cast<float*>(b0), reinterpret_cast<float*>(b1), reinterpret_cast<float*>(b2),
+                          reinterpret_cast<float*>(b3)};
+  constexpr int H = NDB / 2, PER = 4 * H;   // values of a thread in a buffer
+  // Selected by bits: a choice of registers by index would put them into memory.
+  const uint32_t second = group ? ~0u : 0u;
+  auto pick = [&](float x, float y) {
+    return __uint_as_float((__float_as_uint(x) & ~second) | (__float_as_uint(y) & second));
+  };
+  __syncthreads();
+#pragma unroll
+  for (int db = 0; db < H; ++db)
+#pragma unroll
+    for (int e = 0; e < 16; ++e) {
+      const int n = 16 * db + e;
+      room[n / PER][(group * PER + n % PER) * 256 + thread] = pick(acc[db + H][e], acc[db][e]);
+      acc[db][e] = pick(acc[db][e], acc[db + H][e]);
+    }
+  __syncthreads();
+#pragma unroll
+  for (int db = 0; db < H; ++db)
+#pragma unroll
+    for (int e = 0; e < 16; ++e) {
+      const int n = 16 * db + e;
+      acc[db][e] += room[n / PER][((1 - group) * PER + n % PER) * 256 + thread];
     }
 }
 

@@ -161,6 +161,38 @@ def test_hidden_places_hold_anything(dtype, d):
                 check(name, got[name][0], want, np.where(np.isfinite(bound), bound, np.inf))
 
 
+SHARED = [  # few rows of long windows: the tiles of a workgroup go to two groups of waves
+    (1, 2, 1, 64, 600, 300, 5, F32),
+    (2, 2, 2, 64, 390, 390, 0, BF16),
+    (1, 4, 2, 128, 520, 260, 130, BF16),
+    (1, 2, 1, 64, 300, 250, 6, F32),
+    (1, 2, 1, 128, 257, 500, 0, BF16),
+    (1, 2, 1, 64, 1500, 257, 2, BF16),     # queries of the sinks in chunks
+]
+
+
+@pytest.mark.parametrize("b,h,kv,d,n,window,sinks,dtype", SHARED)
+def test_shared_tiles(b, h, kv, d, n, window, sinks, dtype):
+    test_batch(b, h, kv, d, n, window, sinks, dtype)
+
+
+@pytest.mark.parametrize("d,dtype", [(64, BF16), (128, BF16), (64, F32)])
+def test_hidden_places_of_shared_tiles(d, dtype):
+    """As test_hidden_places_hold_anything: a group of waves that sees the value computes once more, and the other."""
+    rng = np.random.default_rng(d + 1)
+    n, window, sinks, h = 400, 256, 3, 2
+    base = [normal(rng, (1, x, n, d), dtype) for x in (h, 1, 1, h)]
+    bad = [float("nan"), float("inf"), float("-inf")]
+    for which in range(4):
+        for case, row in enumerate((2, 70, 300)):
+            t = [x.clone() for x in base]
+            t[which][0, 0, row, case * 7 % d] = bad[(which + case) % 3]
+            got = run(*(x.cuda() for x in t), window=window, sinks=sinks)
+            ref = grouped(*(x[0].double().numpy() for x in t), window, sinks, dtype)
+            for name, (want, bound) in ref.items():
+                check(name, got[name][0], want, np.where(np.isfinite(bound), bound, np.inf))
+
+
 def test_strides():
     """q, k and v as views of one projection's output, outputs into views too."""
     from paper_2605_15684_amd import window
