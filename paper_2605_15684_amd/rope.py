@@ -123,6 +123,19 @@ def _tensor(t, dtype, dim: int, batch: int, rows: int, d: int, index: int, what:
     return h, sb, sh, st
 
 
+def _pair(t, out, dtype, dim: int, batch: int, rows: int, d: int, index: int, what: str):
+    """A tensor and where it goes (None: allocated): (heads, output, ssba_rope_tensor)."""
+    h, *strides = _tensor(t, dtype, dim, batch, rows, d, index, what)
+    if out is None:
+        out = torch.empty_like(t, memory_format=torch.contiguous_format)
+        to = (0, d, h * d) if dim == 3 else (h * rows * d, rows * d, d)
+    else:
+        if isinstance(out, torch.Tensor) and out.shape != t.shape:
+            raise ValueError(f"{what}_out: expected the shape of {what}")
+        to = _tensor(out, dtype, dim, batch, rows, d, index, what + "_out")[1:]
+    return h, out, _TENSOR.pack(h, t.data_ptr(), out.data_ptr(), *strides, *to)
+
+
 def rotate(plan: Plan, pos: torch.Tensor, q: torch.Tensor, k: Optional[torch.Tensor] = None, *, inverse: bool = False,
            q_out: Optional[torch.Tensor] = None, k_out: Optional[torch.Tensor] = None):
     """q (and k, of another number of heads) turned by the positions of their tokens; with `inverse` turned back, which
@@ -132,40 +145,33 @@ def rotate(plan: Plan, pos: torch.Tensor, q: torch.Tensor, k: Optional[torch.Ten
         raise ValueError("plan: expected a rope.Plan")
     if not isinstance(q, torch.Tensor) or not q.is_cuda or q.dim() not in (3, 4) or q.dtype not in _DTYPES:
         raise ValueError("q: expected a [tokens, heads, D] or [B, H, T, D] GPU tensor, bf16 or fp32")
-    index, dim, dtype, d = q.get_device(), q.dim(), q.dtype, plan.head_dim
-    batch, rows = (1, q.shape[0]) if dim == 3 else (q.shape[0], q.shape[2])
-    if not isinstance(pos, torch.Tensor) or pos.dtype is not torch.int32 or pos.get_device() != index or \
-            pos.dim() not in (2, dim - 1) or pos.shape[-1] != plan.axes or pos.shape[-2] != rows or \
-            (pos.dim() == 3 and pos.shape[0] != batch):
+    index, dim, dtype, d, shape = q.get_device(), q.dim(), q.dtype, plan.head_dim, q.shape
+    batch, rows = (1, shape[0]) if dim == 3 else (shape[0], shape[2])
+    own = False   # positions of each batch entry
+    if isinstance(pos, torch.Tensor) and pos.dtype is torch.int32 and pos.get_device() == index:
+        where = tuple(pos.shape)
+        own = where == (batch, rows, plan.axes) and dim == 4
+        fits = own or where == (rows, plan.axes)
+    else:
+        fits = False
+    if not fits:
         raise ValueError(f"pos: expected an int32 tensor [tokens, {plan.axes}]" +
                          (f" or [B, T, {plan.axes}]" if dim == 4 else "") + " on q's device")
-    if plan.axes > 1 and pos.numel() and pos.stride(-1) != 1:
+    step = pos.stride()
+    if plan.axes > 1 and step[-1] != 1 and pos.numel():
         raise ValueError("pos: the axes of a token must be contiguous")
-    h, *strides = _tensor(q, dtype, dim, batch, rows, d, index, "q")
-    if q_out is None:
-        q_out = torch.empty_like(q, memory_format=torch.contiguous_format)
-    elif isinstance(q_out, torch.Tensor) and q_out.shape != q.shape:
-        raise ValueError("q_out: expected the shape of q")
-    most = h
-    desc = _TENSOR.pack(h, q.data_ptr(), q_out.data_ptr(), *strides,
-                        *_tensor(q_out, dtype, dim, batch, rows, d, index, "q_out")[1:])
+    most, q_out, desc = _pair(q, q_out, dtype, dim, batch, rows, d, index, "q")
     if k is not None:
-        h, *strides = _tensor(k, dtype, dim, batch, rows, d, index, "k")
-        if k_out is None:
-            k_out = torch.empty_like(k, memory_format=torch.contiguous_format)
-        elif isinstance(k_out, torch.Tensor) and k_out.shape != k.shape:
-            raise ValueError("k_out: expected the shape of k")
+        h, k_out, more = _pair(k, k_out, dtype, dim, batch, rows, d, index, "k")
         most = max(most, h)
-        desc += _TENSOR.pack(h, k.data_ptr(), k_out.data_ptr(), *strides,
-                             *_tensor(k_out, dtype, dim, batch, rows, d, index, "k_out")[1:])
+        desc += more
     elif k_out is not None:
         raise ValueError("k_out without k")
-    for x in (batch, rows, most):
-        if x >= 1 << 31:
-            raise ValueError("q: outside int32")
+    if batch >= 1 << 31 or rows >= 1 << 31 or most >= 1 << 31:
+        raise ValueError("q: outside int32")
     if q.numel() or (k is not None and k.numel()):
         args = (plan.desc, _DTYPES[dtype], 1 if inverse else 0, batch, rows, pos.data_ptr(),
-                pos.stride(0) if pos.dim() == 3 and batch > 1 else 0, pos.stride(-2) if rows > 1 else 0,
+                step[0] if own and batch > 1 else 0, step[-2] if rows > 1 else 0,
                 1 if k is None else 2, desc)
         if _current_device() == index:
             status = _L.ssba_rope_rotate(*args, _raw_stream(index))
