@@ -25,8 +25,13 @@
  * (NaN and infinities too); the same holds for gradients.
  *
  * bf16: products of bf16 values with fp32 sums; probabilities and ds enter the
- * second products rounded to bf16 (half a step each, like the results).  fp32:
- * fp32 products and sums.  Softmax statistics are fp32.
+ * second products rounded to bf16 (half a step each, like the results; the ds of
+ * dq as two bf16 terms where window + sinks is at most 1024).  fp32: values as
+ * three bf16 terms, products within 2^-22 of exact ones, fp32 sums; of values
+ * below 2^-110 the last bits are lost.  Softmax statistics are fp32: p of the
+ * backward comes from lse, so it is off by |lse| 2^-23, which scores of some
+ * thousands begin to show.  How the work is split goes by the sizes of the call
+ * and max_len, and the rounding of partial sums with it.
  *
  * Ownership, streams and errors as in ssba.h: the caller owns every buffer,
  * calls are asynchronous on `hip_stream`, checks come before any launch, and
@@ -56,7 +61,7 @@ typedef struct ssba_window {
   int32_t dtype;             /* ssba_dtype of every tensor                       */
   int32_t window, sinks;     /* window >= 1, sinks >= 0                          */
   int32_t seqs;              /* packed: sequences, 1 .. 65535; else 0            */
-  int32_t max_len;           /* packed: about the longest sequence (only how work is split goes by it); 0: seq */
+  int32_t max_len;           /* packed: about the longest sequence (how work is split goes by it); 0: seq */
   float softmax_scale;       /* <= 0 selects 1 / sqrt(head_dim); at most 2^127   */
   const int32_t* cu;         /* packed: device int32 [seqs + 1]; else NULL       */
   ssba_strides q, k, v, o;   /* k, v: of kv_heads heads                          */

@@ -48,6 +48,19 @@
 //                 1024 tokens x 8 kv heads x 20 pages of 32, D 64, G 3: 44 us, 16
 //                 TB/s from the L2 (with bf16 probabilities 43; there J 1 took
 //                 48 us, J 4 49: registers).
+//   window        as few columns, of the window's and the sinks' pages: 64
+//                 sequences, 4096 + 64 keys, 4 kv heads, D 128: 36 us, 6.1 TB/s.
+//                 One sequence, window 1024: 9.4 us, 8 steps of a wave in turn.
+//   prefix, rest  a group's sequences are the columns of its prefix, so its pages
+//                 are read and decoded once for 32 columns instead of once a
+//                 sequence; parts of the prefix are added in the epilogue of the
+//                 rests where these are in one part, which saves a launch.  64
+//                 sequences of 4 columns that share 8192 tokens and hold up to 512
+//                 more, 4 kv heads, D 128: 15.8 + 10.7 us (by sequence, 8192
+//                 tokens of 64 sequences read 540 MB, 100 us at 5.4 TB/s).  The
+//                 prefix is bound by decoding: a workgroup has 32 of 256 columns
+//                 and about 256 keys a wave (more columns a workgroup leave fewer
+//                 of them); the rest by a chain of loads, a few steps, and parts.
 #include <hip/hip_runtime.h>
 #include <hip/hip_bf16.h>
 
@@ -996,9 +1009,9 @@ __global__ __launch_bounds__(256) void k_cache_join(AttendArgs a) {
 }
 
 // Joins the parts of shared prefixes and of what is behind them where that is
-// in parts as well (else its own launch adds the prefix's), as the join above: r has the launch of the rests (its items are this one's), p that of the
-// prefixes.  A token's columns of its group begin with those of the sequences
-// before it.
+// in parts as well (else its own launch adds the prefix's), as the join above: r
+// has the launch of the rests (its items are this one's), p that of the prefixes.
+// A token's columns of its group begin with those of the sequences before it.
 template <int D, bool F32>
 __global__ __launch_bounds__(256) void k_cache_join_shared(AttendArgs r, AttendArgs p) {
   __shared__ float s_w[2 * kMaxSplits][16];

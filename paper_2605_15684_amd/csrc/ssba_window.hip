@@ -10,6 +10,25 @@
 // probabilities passes 2^20, or a query has none yet; it may lag behind
 // otherwise, which is harmless in fp32 and bf16.
 //
+// 32 queries a wave is what a 32 x 32 product takes, so that K and V are read
+// from the LDS once for 32; tiles of 64 keys (bf16) leave two workgroups a CU.
+// Partly seen tiles take their mask from a word of bits a lane, made once a tile.
+// The wave in its second products goes first (s_setprio): the other one of its
+// SIMD has exponentials to do then (16384 tokens below: 185 to 177 us).
+//
+// fp32: values are split into three bf16 terms on their way to the LDS, and six
+// of the nine pairs of terms multiplied: 192 cycles where v_mfma_f32_32x32x2_f32
+// takes 512 (packed, 5 sequences, 6 heads on 2, D 64: 43.6 to 32.8 us).
+//
+// Measured, and what bounds it.  bf16, 16384 tokens, 16 heads on 4, D 128, window
+// 1024 + 4: 167 us a call, 800 TFLOP/s of what the rows see; the matrix units are
+// busy 46 % of the time and vector instructions issue in 41 %, which overlap only
+// in part at two waves a SIMD (the registers allow no more).  2 x 8192, window
+// 2048: 290 us, matrix units 52 %.  fp32, D 64, 5 sequences of up to 1101, window
+// 333: 25 us, one workgroup a CU that waits for its own tiles.  fp32, D 128: one
+// wave a SIMD; 318 workgroups leave the chip half empty in their second turn (130
+// us, matrix units 37 % where they run).
+//
 // A value that a query does not see must not reach it, and 0 times a NaN would:
 // where a result is not finite, the workgroup computes once more with the tiles
 // that some query sees in part taken row by row.  So it does where the sum of a

@@ -10,8 +10,24 @@
 //                   that see some of them, head after head of the group:
 //                   S = Q K^T, dV^T += dO^T P, dS = P (dO V^T - delta),
 //                   dK^T += Q^T dS.  Keys that are sinks are seen by every later
-//                   query: their queries are cut into chunks, whose parts
-//   k_window_join   adds up in the chunks' order.
+//                   query: their queries are cut into chunks.  Where there are
+//                   few tiles, several workgroups share the heads of a group.
+//   k_window_join   adds up the parts of chunks and heads, in their order.
+//
+// S and dP are formed twice, on either side: one pass that also added dQ would
+// need atomics, whose order changes results, or dQ in as many parts as key tiles.
+// fp32 as in the forward.  bf16 at D 128 holds dK, dV and V of 32 keys in
+// registers and K as operands in the LDS, with tiles of 32 queries: two waves a
+// SIMD (K in registers as well leaves one).
+//
+// Measured, and what bounds it.  bf16, 2 x 8192, 16 heads on 4, D 128, window 2048
+// + 16: dq 390 us, dkdv 555, join 6 (with the forward 1120 a call): 930 and 870
+// TFLOP/s of what the two compute; matrix units are busy 58 and 55 %, the rest are
+// exponentials, masks and conversions that overlap only in part, and waits for the
+// LDS.  2 x 200 rows, 4 heads, D 64: 11.4 and 11.4 us, chains of a few tiles.
+// fp32, packed 6269 rows, 6 heads on 2, D 128, window 512: 180, 200 and 12 us; one
+// wave a SIMD, and a second turn of few workgroups (the chip is busy 49 and 59 %
+// of the time, the matrix units 40 % of that).
 //
 // What a query does not see must not reach it, nor it what it does not see, and
 // 0 times a NaN would: where a result is not finite, the workgroup computes once
@@ -26,8 +42,9 @@
 namespace ssba {
 namespace {
 
-// Reads of the LDS run six ahead of the products that use them: with two waves
-// a SIMD a product that waits for its own read leaves the matrix cores idle.
+// Reads of the LDS run AHEAD ahead of the products that use them, READS for every
+// two: with two waves a SIMD a product that waits for its own read leaves the
+// matrix cores idle.
 template <class T, int AHEAD, int READS>
 __device__ __forceinline__ void order_rows() {
   if constexpr (T::ORDERED) {
@@ -48,7 +65,8 @@ __device__ __forceinline__ void order_rows() {
 // how much: the key side gets it corrected.  Here ds itself is formed with the
 // one from o; TERMS 2 (up to 1024 keys a row) makes up for it by not rounding ds
 // to 8 bits.  Errors of dq and dk against 64 bits, over that of a result's own
-// rounding (window 64, D 64, 200 rows): 1.58 and 1.53 without either.
+// rounding (window 64, D 64, 200 rows): 1.58 and 1.53 without either, 1.20 and
+// 1.42 with both.
 // --------------------------------------------------------------------------
 template <class T, bool CAREFUL, int TERMS, int G>
 __device__ __forceinline__ void dq_pass(const WindowArgs& a, const WPlace& p, int group, int wave, int lane, char* kA,

@@ -129,8 +129,8 @@ def forward(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, *, window: int, s
             out: Optional[torch.Tensor] = None, lse: Optional[torch.Tensor] = None) -> Tuple[torch.Tensor, torch.Tensor]:
     """Attention of every token over itself, the window - 1 tokens before it and the first `sinks` tokens of its
     sequence.  Returns (out, lse): lse fp32 [B, H, T], or [H, rows] of packed tensors, is what `backward` needs.
-    scale: positive; None: 1 / sqrt(D).  max_len: about the longest packed sequence (work is split by it; results are
-    not).  Rows of no sequence are left as they are."""
+    scale: positive; None: 1 / sqrt(D).  max_len: about the longest packed sequence (work is split by it, results
+    differ by the rounding of partial sums).  Rows of no sequence are left as they are."""
     if out is None and isinstance(q, torch.Tensor):
         out = torch.empty_like(q, memory_format=torch.contiguous_format)
     desc = _desc(q, k, v, out, window, sinks, scale, cu, max_len)
