@@ -117,3 +117,25 @@ def test_gradient_by_differences():
         down[at] -= 1.0
         # both sums hold 2 * 64 terms of the row that moved by up to 4 U (|a| + |b|) |w| each; |x| < 8, |w| < 8
         assert abs((f(up) - f(down)) / 2 - float(grad[at])) < 2 * 4 * U * 20 * 8 + 1e-9
+
+
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("pairs", ["adjacent", "halves"])
+def test_fp32_rows_may_begin_anywhere(d, pairs):
+    """Rows at odd multiples of 4 bytes: the values of aligned ones, and nothing beside them is written."""
+    from paper_2605_15684_amd import rope
+    n, h, kv = 9, 3, 2
+    g = torch.Generator(device="cuda").manual_seed(d)
+    plan = rope.plan(d, (d // 4, d // 4), pairs=pairs)
+    pos = torch.randint(0, 900, (n, 2), generator=g, device="cuda", dtype=torch.int32)
+    wide = lambda heads: torch.randn((n, heads, d + 3), generator=g, device="cuda")
+    q, k, q_to, k_to = wide(h), wide(kv), wide(h), wide(kv)
+    before = [x.clone() for x in (q_to, k_to)]
+    mid = lambda x: x[..., 1:1 + d]
+    want = rope.rotate(plan, pos, mid(q).contiguous(), mid(k).contiguous())
+    rope.rotate(plan, pos, mid(q), mid(k), q_out=mid(q_to), k_out=mid(k_to))
+    for got, y, old in zip((q_to, k_to), want, before):
+        assert torch.equal(mid(got), y)
+        assert torch.equal(got[..., 0], old[..., 0]) and torch.equal(got[..., 1 + d:], old[..., 1 + d:])
+    rope.rotate(plan, pos, mid(q), mid(k), q_out=mid(q), k_out=mid(k))
+    assert torch.equal(mid(q), want[0]) and torch.equal(mid(k), want[1])

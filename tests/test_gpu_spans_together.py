@@ -296,3 +296,39 @@ def test_whatever_cu_holds(cu):
     for x in held:
         assert (x[:128] == 9.0).all() and (x[128 + rows:] == 9.0).all()
     assert (lse_all[0] == 9.0).all() and (lse_all[3] == 9.0).all()
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+def test_shared_tiles_in_a_graph_and_twice(dtype):
+    """Few rows of a long window (the tiles of a workgroup go to two groups of waves): the same bits in every run, eager,
+    captured and on another stream."""
+    from paper_2605_15684_amd import window
+    rng = np.random.default_rng(11)
+    cu = ints([2, 300, 300, 771])
+    q, do = (normal(rng, (775, 4, 64), dtype).cuda() for _ in range(2))
+    k, v = (normal(rng, (775, 2, 64), dtype).cuda() for _ in range(2))
+    kw = dict(window=256, sinks=3, cu=cu)
+
+    def run(out):
+        o, lse = window.forward(q, k, v, out=out[0], lse=out[1], **kw)
+        window.backward(q, k, v, o, do, lse, dq=out[2], dk=out[3], dv=out[4], **kw)
+
+    room = lambda: [torch.zeros_like(q), torch.zeros((4, 775), device="cuda")] + [torch.zeros_like(x) for x in (q, k, v)]
+    want, other, held = room(), room(), room()
+    run(want)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        run(other)
+    run(held)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        run(held)
+    for _ in range(3):
+        for x in held:
+            x.zero_()
+        graph.replay()
+        torch.cuda.synchronize()
+        for x, y, z in zip(held, want, other):
+            assert torch.equal(x, y) and torch.equal(z, y)
