@@ -78,6 +78,7 @@ def _strides(t, shape, dtype, index: int, what: str) -> Tuple[int, int, int]:
 
 
 def _desc(q, k, v, o, window: int, sinks: int, scale: Optional[float], cu, max_len: Optional[int]) -> bytes:
+    """ssba_window of a call, its tensors checked; o None: a contiguous one that is still to be allocated."""
     if not isinstance(q, torch.Tensor) or not q.is_cuda or q.dim() not in (3, 4) or q.dtype not in _DTYPES:
         raise ValueError("q: expected a [B, H, T, D] or [rows, H, D] GPU tensor, bf16 or fp32")
     if not isinstance(k, torch.Tensor) or k.dim() != q.dim():
@@ -106,8 +107,11 @@ def _desc(q, k, v, o, window: int, sinks: int, scale: Optional[float], cu, max_l
         scale = ctypes.c_float(scale).value
         if not scale > 0.0:
             raise ValueError("scale must be positive in fp32 (None: 1 / sqrt(D))")
+    os = (heads * rows * d, rows * d, d) if len(qs) == 4 else (0, d, heads * d)
+    if o is not None:
+        os = _strides(o, qs, dtype, index, "out")
     strides = _strides(q, qs, dtype, index, "q") + _strides(k, shape, dtype, index, "k") + \
-        _strides(v, shape, dtype, index, "v") + _strides(o, qs, dtype, index, "out")
+        _strides(v, shape, dtype, index, "v") + os
     try:
         return _DESC.pack(batch, rows, heads, kv, d, _DTYPES[dtype], window, sinks, seqs, max_len, scale, at, *strides)
     except struct.error as e:
@@ -131,12 +135,13 @@ def forward(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, *, window: int, s
     sequence.  Returns (out, lse): lse fp32 [B, H, T], or [H, rows] of packed tensors, is what `backward` needs.
     scale: positive; None: 1 / sqrt(D).  max_len: about the longest packed sequence (work is split by it, results
     differ by the rounding of partial sums).  Rows of no sequence are left as they are."""
-    if out is None and isinstance(q, torch.Tensor):
-        out = torch.empty_like(q, memory_format=torch.contiguous_format)
     desc = _desc(q, k, v, out, window, sinks, scale, cu, max_len)
+    if out is None:
+        out = torch.empty_like(q, memory_format=torch.contiguous_format)
     if lse is None:
-        lse = torch.empty(_lse_shape(q), dtype=torch.float32, device=q.device)
-    _check_lse(lse, q)
+        lse = q.new_empty(_lse_shape(q), dtype=torch.float32)
+    else:
+        _check_lse(lse, q)
     _call(q.get_device(), _L.ssba_window_forward, "ssba_window_forward", desc, q.data_ptr(), k.data_ptr(), v.data_ptr(),
           out.data_ptr(), lse.data_ptr())
     return out, lse
@@ -149,6 +154,8 @@ def backward(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, out: torch.Tenso
              scratch: Optional[torch.Tensor] = None) -> Tuple[torch.Tensor, torch.Tensor, torch.Tensor]:
     """Gradients (dq, dk, dv) of `forward` for the upstream gradient `dout`, with its out, lse and arguments.  Rows of
     no sequence are left as they are."""
+    if out is None:
+        raise ValueError("out: expected the forward's")
     desc = _desc(q, k, v, out, window, sinks, scale, cu, max_len)
     _check_lse(lse, q)
     mk = lambda t, like: torch.empty_like(like, memory_format=torch.contiguous_format) if t is None else t
