@@ -49,22 +49,29 @@ _GRADS = struct.Struct("=12q")
 assert _DESC.size == ctypes.sizeof(_lib.WindowDesc) and _GRADS.size == ctypes.sizeof(_lib.WindowGrads)
 
 
+def _contiguous(shape) -> Tuple[int, int, int]:
+    """(batch, head, row) strides of a contiguous tensor."""
+    if len(shape) == 3:
+        _, h, d = shape
+        return 0, d, h * d
+    _, h, n, d = shape
+    return h * n * d, n * d, d
+
+
 def _strides(t, shape, dtype, index: int, what: str) -> Tuple[int, int, int]:
     """Checks a tensor of a shape, type and device; its (batch, head, row) strides."""
     if not isinstance(t, torch.Tensor) or t.dtype is not dtype or t.shape != shape:
         raise ValueError(f"{what}: expected a {dtype} GPU tensor of shape {tuple(shape)}")
     if t.get_device() != index:
         raise ValueError(f"{what}: all tensors must be on one device")
+    if t.is_contiguous():
+        return _contiguous(shape)
     if len(shape) == 3:
         n, h, d = shape
-        if t.is_contiguous():
-            return 0, d, h * d
         st, sh, sc = t.stride()
         b, sb = 1, 0
     else:
         b, h, n, d = shape
-        if t.is_contiguous():
-            return h * n * d, n * d, d
         sb, sh, st, sc = t.stride()
     if sc != 1:
         raise ValueError(f"{what}: channel stride must be 1")
@@ -75,6 +82,13 @@ def _strides(t, shape, dtype, index: int, what: str) -> Tuple[int, int, int]:
     if st < d or sh < d or (b > 1 and sb < d):
         raise ValueError(f"{what}: rows and heads must not overlap")
     return sb, sh, st
+
+
+def _place(t, like, dtype, index: int, what: str):
+    """A tensor of the shape of `like` (None: allocated) and its strides."""
+    if t is not None:
+        return t, _strides(t, like.shape, dtype, index, what)
+    return torch.empty_like(like, memory_format=torch.contiguous_format), _contiguous(like.shape)
 
 
 def _desc(q, k, v, o, window: int, sinks: int, scale: Optional[float], cu, max_len: Optional[int]) -> bytes:
@@ -107,9 +121,7 @@ def _desc(q, k, v, o, window: int, sinks: int, scale: Optional[float], cu, max_l
         scale = ctypes.c_float(scale).value
         if not scale > 0.0:
             raise ValueError("scale must be positive in fp32 (None: 1 / sqrt(D))")
-    os = (heads * rows * d, rows * d, d) if len(qs) == 4 else (0, d, heads * d)
-    if o is not None:
-        os = _strides(o, qs, dtype, index, "out")
+    os = _contiguous(qs) if o is None else _strides(o, qs, dtype, index, "out")
     strides = _strides(q, qs, dtype, index, "q") + _strides(k, shape, dtype, index, "k") + \
         _strides(v, shape, dtype, index, "v") + os
     try:
@@ -158,18 +170,19 @@ def backward(q: torch.Tensor, k: torch.Tensor, v: torch.Tensor, out: torch.Tenso
         raise ValueError("out: expected the forward's")
     desc = _desc(q, k, v, out, window, sinks, scale, cu, max_len)
     _check_lse(lse, q)
-    mk = lambda t, like: torch.empty_like(like, memory_format=torch.contiguous_format) if t is None else t
-    dq, dk, dv = mk(dq, q), mk(dk, k), mk(dv, v)
     index, dtype = q.get_device(), q.dtype
-    grads = _GRADS.pack(*_strides(dout, q.shape, dtype, index, "dout"), *_strides(dq, q.shape, dtype, index, "dq"),
-                        *_strides(dk, k.shape, dtype, index, "dk"), *_strides(dv, v.shape, dtype, index, "dv"))
+    ds = _strides(dout, q.shape, dtype, index, "dout")
+    dq, dqs = _place(dq, q, dtype, index, "dq")
+    dk, dks = _place(dk, k, dtype, index, "dk")
+    dv, dvs = _place(dv, k, dtype, index, "dv")
+    grads = _GRADS.pack(*ds, *dqs, *dks, *dvs)
     size = ctypes.c_size_t(0)
     _lib.check(_L.ssba_window_backward_workspace_size(desc, size), "ssba_window_backward_workspace_size")
     if scratch is None:
-        scratch = torch.empty(size.value, dtype=torch.uint8, device=q.device)
-    elif not (isinstance(scratch, torch.Tensor) and scratch.get_device() == q.get_device() and scratch.is_contiguous()):
+        scratch = q.new_empty(size.value, dtype=torch.uint8)
+    elif not (isinstance(scratch, torch.Tensor) and scratch.get_device() == index and scratch.is_contiguous()):
         raise ValueError("scratch must be a contiguous GPU tensor on q's device")
-    _call(q.get_device(), _L.ssba_window_backward, "ssba_window_backward", desc, grads, q.data_ptr(), k.data_ptr(),
+    _call(index, _L.ssba_window_backward, "ssba_window_backward", desc, grads, q.data_ptr(), k.data_ptr(),
           v.data_ptr(), out.data_ptr(), dout.data_ptr(), lse.data_ptr(), dq.data_ptr(), dk.data_ptr(), dv.data_ptr(),
           scratch.data_ptr(), scratch.numel() * scratch.element_size())
     return dq, dk, dv
