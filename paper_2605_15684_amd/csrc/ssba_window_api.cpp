@@ -99,17 +99,30 @@ ssba_status plan(const ssba_window* w, WindowArgs* a) {
   a->head_parts = 1;
   for (int n = 2; n <= a->group && n <= most && tiles * a->head_parts < room; ++n)
     if (a->group % n == 0) a->head_parts = n;
+  // Then the queries, in shares of at least 128 (fp32) or 256 (bf16, D 128), whose tiles take long enough to be worth
+  // their parts; the join walks a tile's parts in turn, so at most 16.  Backward, one share against several: 1024 rows, 8
+  // heads, window 256, fp32 D 128 208 to 128 us, D 64 104 to 76 (shares of 64: 117, 72); 16 heads on 4, window 1024, bf16 D 128 80 to 71; but
+  // D 64 49 to 52.  8 heads on 2, 512 rows, fp32 D 64: 20 parts 68, 32 parts 80.
+  a->query_parts = 1;
+  const int64_t least = w->dtype == SSBA_DT_F32 ? kWindowRows : w->head_dim == 128 ? 256 : 0;
+  if (least) {
+    const int64_t queries = std::min<int64_t>((int64_t)a->window + kWindowRows, longest);
+    const int64_t n = std::min<int64_t>({room / (tiles * a->head_parts), queries / least, std::min<int64_t>(most, 16) / a->head_parts});
+    a->query_parts = (int)std::max<int64_t>(1, n);
+  }
+  const int64_t shares = (int64_t)a->head_parts * a->query_parts;
   // The key side's launch, and the join's of 8 workgroups a part.
-  const int64_t kept = cut + (a->head_parts > 1 ? a->slots : 0);
-  if ((double)units * (a->slots + cut) * a->head_parts > (double)ssba::kMaxGroups256 ||
+  const int64_t kept = cut + (shares > 1 ? a->slots : 0);
+  if ((double)units * (a->slots + cut) * shares > (double)ssba::kMaxGroups256 ||
       (double)units * kept * 8 > (double)ssba::kMaxGroups256)
     return SSBA_ERR_UNSUPPORTED;
   return SSBA_OK;
 }
 
 size_t part_bytes(const ssba_window* w, const WindowArgs& a) {
-  const size_t kept = (size_t)a.sink_tiles * a.chunk_slots + (a.head_parts > 1 ? a.slots : 0);
-  return (size_t)w->batch * w->kv_heads * kept * a.head_parts * 2 * kWindowRows * w->head_dim * 4;
+  const size_t shares = (size_t)a.head_parts * a.query_parts;
+  const size_t kept = (size_t)a.sink_tiles * a.chunk_slots + (shares > 1 ? a.slots : 0);
+  return (size_t)w->batch * w->kv_heads * kept * shares * 2 * kWindowRows * w->head_dim * 4;
 }
 
 size_t row_bytes(const ssba_window* w) { return ceil_div((int64_t)w->batch * w->heads * w->seq * 4, 256) * 256; }

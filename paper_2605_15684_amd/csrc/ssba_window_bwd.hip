@@ -11,8 +11,9 @@
 //                   S = Q K^T, dV^T += dO^T P, dS = P (dO V^T - delta),
 //                   dK^T += Q^T dS.  Keys that are sinks are seen by every later
 //                   query: their queries are cut into chunks.  Where there are
-//                   few tiles, several workgroups share the heads of a group.
-//   k_window_join   adds up the parts of chunks and heads, in their order.
+//                   few tiles, several workgroups share the heads of a group
+//                   and the queries.
+//   k_window_join   adds up the parts of chunks and shares, in their order.
 //
 // S and dP are formed twice, on either side: one pass that also added dQ would
 // need atomics, whose order changes results, or dQ in as many parts as key tiles.
@@ -253,9 +254,18 @@ struct KeyPlace {
 // Slot of a sequence's chunk 0, as place_slot counts tiles.
 __device__ __forceinline__ int chunk_slot(const WindowArgs& a, int begin, int s) { return begin / a.chunk + s; }
 
+// The part-th of `parts` of the queries, in multiples of 32; none: q0 = q1.
+__device__ __forceinline__ void share_queries(int parts, int part, KeyPlace* p) {
+  if (parts == 1) return;
+  const int all = p->q1 - p->q0, each = ((all + parts - 1) / parts + 31) / 32 * 32;
+  const int from = min((int64_t)part * each, (int64_t)all), to = min((int64_t)from + each, (int64_t)all);
+  p->q1 = p->q0 + to;
+  p->q0 += from;
+}
+
 __device__ __forceinline__ bool place_keys(const WindowArgs& a, int lane, KeyPlace* p) {
   const unsigned units = (unsigned)a.batch * a.kv_heads, cut = (unsigned)a.sink_tiles * a.chunk_slots;
-  const unsigned per = (a.slots + cut) * a.head_parts;
+  const unsigned shares = a.head_parts * a.query_parts, per = (a.slots + cut) * shares;
   unsigned id = blockIdx.x, unit, at;
   if (a.spread) {
     unit = id % units;
@@ -265,14 +275,14 @@ __device__ __forceinline__ bool place_keys(const WindowArgs& a, int lane, KeyPla
     unit = id / per;
     at = id % per;
   }
-  const int share = at % a.head_parts;
-  at /= a.head_parts;
-  p->g0 = share * a.group / a.head_parts;
-  p->g1 = (share + 1) * a.group / a.head_parts;
+  const int share = at % shares, heads = share % a.head_parts, part = share / a.head_parts;
+  at /= shares;
+  p->g0 = heads * a.group / a.head_parts;
+  p->g1 = (heads + 1) * a.group / a.head_parts;
   p->b = unit / a.kv_heads;
   p->kvh = unit % a.kv_heads;
-  const unsigned kept = cut + (a.head_parts > 1 ? a.slots : 0);   // tiles and chunks that leave parts
-  p->part = at < kept ? (((int64_t)unit * kept + at) * a.head_parts + share) * 2 * kWindowRows : -1;
+  const unsigned kept = cut + (shares > 1 ? a.slots : 0);   // tiles and chunks that leave parts
+  p->part = at < kept ? (((int64_t)unit * kept + at) * shares + share) * 2 * kWindowRows : -1;
   if (at >= cut) {   // a tile of keys; its queries, or the first chunk of them, end with the window
     WPlace w;
     if (!place_slot(a, at - cut, lane, &w)) return false;
@@ -286,6 +296,7 @@ __device__ __forceinline__ bool place_keys(const WindowArgs& a, int lane, KeyPla
     } else {
       p->q1 = a.window < w.len - w.r0 - kWindowRows ? w.r0 + kWindowRows - 1 + a.window : w.len;
     }
+    share_queries(a.query_parts, part, p);
     return true;
   }
   const int tile = at / a.chunk_slots, slot = at % a.chunk_slots;
@@ -304,6 +315,7 @@ __device__ __forceinline__ bool place_keys(const WindowArgs& a, int lane, KeyPla
   if (q0 >= p->len) return false;
   p->q0 = (int)q0;
   p->q1 = p->len - p->q0 < a.chunk ? p->len : p->q0 + a.chunk;
+  share_queries(a.query_parts, part, p);
   return true;
 }
 
@@ -487,13 +499,18 @@ __global__ __launch_bounds__(256 * G, T::SPLIT && T::D == 128 ? 1 : 2) void k_wi
   floatx16 dk[NDB], dv[NDB];
   if (threadIdx.x == 0) s_bad = 0;
   char* keys = s_k + (T::ORDERED ? group * 4 * T::NKS * 1024 : 0);
-  dkdv_pass<T, false, G>(a, p, group, wave, lane, keys, qA[group], qB[group], gA[group], gB[group], rA[group], rB[group], dk,
-                         dv);
-  if (__builtin_amdgcn_ballot_w64(in && (not_finite<NDB>(dk) || not_finite<NDB>(dv))) && lane == 0) s_bad = 1;
-  __syncthreads();
-  if (s_bad)
-    dkdv_pass<TC, true, G>(a, p, group, wave, lane, keys, qA[group], qB[group], gA[group], gB[group], rA[group], rB[group],
+  if (p.q0 < p.q1) {
+    dkdv_pass<T, false, G>(a, p, group, wave, lane, keys, qA[group], qB[group], gA[group], gB[group], rA[group], rB[group],
                            dk, dv);
+    if (__builtin_amdgcn_ballot_w64(in && (not_finite<NDB>(dk) || not_finite<NDB>(dv))) && lane == 0) s_bad = 1;
+    __syncthreads();
+    if (s_bad)
+      dkdv_pass<TC, true, G>(a, p, group, wave, lane, keys, qA[group], qB[group], gA[group], gB[group], rA[group], rB[group],
+                             dk, dv);
+  } else {
+#pragma unroll
+    for (int db = 0; db < NDB; ++db) dk[db] = dv[db] = floatx16{};
+  }
   if constexpr (G == 2) {
     join_groups<NDB>(dk, group, threadIdx.x & 255, qA[0], qB[0], gA[0], gB[0]);
     join_groups<NDB>(dv, group, threadIdx.x & 255, qA[0], qB[0], gA[0], gB[0]);
@@ -516,7 +533,7 @@ __global__ __launch_bounds__(256 * G, T::SPLIT && T::D == 128 ? 1 : 2) void k_wi
       1.f, hw);
 }
 
-// Adds up the parts of a tile's chunks and heads, in their order: a workgroup
+// Adds up the parts of a tile's chunks and shares, in their order: a workgroup
 // has a tile's 2048 / D rows, 8 channels a thread.  Of a tile that is cut into
 // chunks the first chunk's does all.
 template <class T>
@@ -526,9 +543,10 @@ __global__ __launch_bounds__(256) void k_window_join(WindowArgs a) {
   unsigned id = blockIdx.x;
   const int sub = id % PARTS;
   id /= PARTS;
-  const unsigned cut = (unsigned)a.sink_tiles * a.chunk_slots, kept = cut + (a.head_parts > 1 ? a.slots : 0);
+  const int shares = a.head_parts * a.query_parts;
+  const unsigned cut = (unsigned)a.sink_tiles * a.chunk_slots, kept = cut + (shares > 1 ? a.slots : 0);
   const unsigned unit = id / kept, at = id % kept;
-  int begin = 0, len = a.seq, k0, parts = a.head_parts;
+  int begin = 0, len = a.seq, k0, parts = shares;
   if (at >= cut) {
     WPlace w;
     if (!place_slot(a, at - cut, lane, &w)) return;
@@ -551,7 +569,7 @@ __global__ __launch_bounds__(256) void k_window_join(WindowArgs a) {
   }
   const int r = sub * ROWS + (int)threadIdx.x / (D / 8), ch = (int)threadIdx.x % (D / 8) * 8;
   if (k0 + r >= len) return;
-  const float* from = a.part + (((int64_t)unit * kept + at) * a.head_parts * 2 * kWindowRows + r) * D + ch;
+  const float* from = a.part + (((int64_t)unit * kept + at) * shares * 2 * kWindowRows + r) * D + ch;
   const int b = unit / a.kv_heads, kvh = unit % a.kv_heads;
   const int64_t row = begin + k0 + r;
 #pragma unroll
@@ -595,14 +613,14 @@ template <class T, class TK, class TC>
 hipError_t launch(const WindowArgs& a, hipStream_t s) {
   using TKC = typename std::conditional<T::F32, TC, TK>::type;
   const int64_t units = (int64_t)a.batch * a.kv_heads, cut = (int64_t)a.sink_tiles * a.chunk_slots;
-  const int64_t kept = cut + (a.head_parts > 1 ? a.slots : 0);
+  const int64_t shares = (int64_t)a.head_parts * a.query_parts, kept = cut + (shares > 1 ? a.slots : 0);
   if (!T::F32 && (int64_t)a.window + a.sinks <= 1024)
     launch_dq<T, TC, T::F32 ? 1 : 2>(a, s);
   else
     launch_dq<T, TC, 1>(a, s);
   hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
-  const unsigned groups = (unsigned)(units * (a.slots + cut) * a.head_parts);
+  const unsigned groups = (unsigned)(units * (a.slots + cut) * shares);
   bool few = false;
   if constexpr (!(T::SPLIT && T::D == 128)) {
     few = share_tiles(a, groups, T::SPLIT ? 1024 : 256);

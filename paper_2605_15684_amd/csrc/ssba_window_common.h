@@ -26,7 +26,7 @@ struct WindowArgs {
   void* dv;
   float* lse2;         // backward scratch: lse in log2 units, -delta [batch][heads][seq]
   float* ndelta;
-  float* part;         // parts of dk and dv [unit][sink tile and chunk slot, then slot][share of the heads][2][128][D]
+  float* part;         // parts of dk and dv [unit][sink tile and chunk slot, then slot][share][2][128][D]
   Strides sq, sk, sv, so, sdo, sdq, sdk, sdv;
   const int32_t* cu;
   int batch, seq, heads, kv_heads, group, window, sinks, seqs;
@@ -36,7 +36,8 @@ struct WindowArgs {
   int sink_tiles;      // tiles of kWindowRows keys that hold sinks
   int chunk;           // queries of a chunk of a sink tile
   int chunk_slots;     // of a (batch, head): 0: no tile is cut
-  int head_parts;      // workgroups that share the heads of a group on the key side
+  int head_parts;      // key side: workgroups that share the heads of a group,
+  int query_parts;     // and the queries of a tile or chunk
 };
 
 // Whether a launch of `groups` workgroups takes 8 waves, in two groups that

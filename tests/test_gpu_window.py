@@ -214,3 +214,17 @@ def test_strides():
         ref = grouped(*(x[0].double().cpu().numpy() for x in (q, k, v, do)), 60, 2, dtype, 0.2)
         for name, (value, bound) in ref.items():
             check(name, want[name][0], value, bound)
+
+
+@pytest.mark.parametrize("h,kv,d,n,window,sinks,dtype", [
+    (2, 2, 64, 500, 200, 5, F32), (3, 1, 128, 300, 130, 0, F32), (2, 1, 64, 333, 64, 140, F32), (1, 1, 128, 700, 511, 3, F32),
+    (2, 2, 128, 900, 600, 2, BF16), (1, 1, 64, 1500, 100, 130, F32)])
+def test_shared_queries(h, kv, d, n, window, sinks, dtype):
+    """Few tiles: several workgroups share the queries of each, and the heads."""
+    test_batch(1, h, kv, d, n, window, sinks, dtype)
+
+
+@pytest.mark.parametrize("d", [64, 128])
+def test_shared_queries_of_packed_sequences(d):
+    """Shares of sequences of any length, of which short ones leave most shares without a query."""
+    test_packed([1, 400, 0, 33, 128], 2, 1, d, 300, 2, F32)
