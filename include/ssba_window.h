@@ -29,9 +29,11 @@
  * dq as two bf16 terms where window + sinks is at most 1024).  fp32: values as
  * three bf16 terms, products within 2^-22 of exact ones, fp32 sums; of values
  * below 2^-110 the last bits are lost.  Softmax statistics are fp32: p of the
- * backward comes from lse, so it is off by |lse| 2^-23, which scores of some
- * thousands begin to show.  How the work is split goes by the sizes of the call
- * and max_len, and the rounding of partial sums with it.
+ * backward comes from lse, so it is off by about |lse| 2^-23, which scores of some
+ * thousands begin to show.  Where a row's |lse| is 2^20 or more p is kept at most
+ * 1, so that finite inputs have finite gradients, but says little else.  How the
+ * work is split goes by the sizes of the call and max_len, and the rounding of
+ * partial sums with it.
  *
  * Ownership, streams and errors as in ssba.h: the caller owns every buffer,
  * calls are asynchronous on `hip_stream`, checks come before any launch, and

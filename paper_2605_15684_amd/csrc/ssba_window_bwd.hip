@@ -32,7 +32,8 @@
 //
 // What a query does not see must not reach it, nor it what it does not see, and
 // 0 times a NaN would: where a result is not finite, the workgroup computes once
-// more with the tiles that are seen in part taken row by row.
+// more with the tiles that are seen in part taken row by row.  So it does where a
+// row's log-sum-exp is very large (kFar).
 #include <hip/hip_runtime.h>
 
 #include <type_traits>
@@ -58,6 +59,20 @@ __device__ __forceinline__ void order_rows() {
       __builtin_amdgcn_sched_group_barrier(kDsRead, READS - READS / 2, 0);
     }
   }
+}
+
+// exp2(scale s - lse2).  The scores are the forward's, to the bit, so lse2's own
+// rounding is all that takes a probability past 1: by a third at most at 2^20, by
+// more than exp2 holds from about 2^28 on, which made infinities of finite inputs.
+// Where rows are past kFar the careful passes compute, which bound it by 1.  In us,
+// dq and dkdv of 2 x 8192 rows, 16 heads on 4, window 2048, bf16, without a bound,
+// as it is, and bounded everywhere: D 128 847, 853, 860; D 64 478, 481, 496.  NaN
+// stays NaN (IEEE minimum).
+constexpr float kFar = 1048576.f;
+template <bool CAREFUL>
+__device__ __forceinline__ float probability(float s, float scale, float lse2) {
+  const float x = __builtin_fmaf(s, scale, -lse2);
+  return __builtin_amdgcn_exp2f(CAREFUL ? __builtin_elementwise_minimum(x, 0.f) : x);
 }
 
 // --------------------------------------------------------------------------
@@ -149,10 +164,10 @@ __device__ __forceinline__ void dq_pass(const WindowArgs& a, const WPlace& p, in
         floatx16 s = {}, ds;
 #pragma unroll
         for (int e = 0; e < 16; ++e) ds[e] = -delta;
-        rows_products<T>(s, kc + nb * T::HALF, q, ds, vc + nb * T::HALF, g, at);
+        rows_products<T, false>(s, kc + nb * T::HALF, q, ds, vc + nb * T::HALF, g, at);
         order_rows<T, 6, 2>();
 #pragma unroll
-        for (int e = 0; e < 16; ++e) ds[e] *= __builtin_amdgcn_exp2f(__builtin_fmaf(s[e], a.scale_log2, -lse2));
+        for (int e = 0; e < 16; ++e) ds[e] *= probability<CAREFUL>(s[e], a.scale_log2, lse2);
         if (!whole) {
           const uint32_t bits = keys_seen(i, j0 + 32 * nb, a.window, a.sinks) >> (4 * hw);
 #pragma unroll
@@ -221,7 +236,8 @@ __global__ __launch_bounds__(256 * G, T::SPLIT && T::D == 128 ? 1 : 2) void k_wi
   float delta, off, lse2;
   if (threadIdx.x == 0) s_bad = 0;
   dq_pass<T, false, TERMS, G>(a, p, group, wave, lane, kA[group], kB[group], vA[group], vB[group], acc, delta, off, lse2);
-  if (__builtin_amdgcn_ballot_w64(in && not_finite<NDB>(acc)) && lane == 0) s_bad = 1;
+  const bool far = fabsf(lse2) > kFar;
+  if (__builtin_amdgcn_ballot_w64(in && (far || not_finite<NDB>(acc))) && lane == 0) s_bad = 1;
   __syncthreads();
   if (s_bad)
     dq_pass<TC, true, TERMS, G>(a, p, group, wave, lane, kA[group], kB[group], vA[group], vB[group], acc, delta, off, lse2);
@@ -329,7 +345,7 @@ __device__ __forceinline__ void copy_values(const float* from, int n, float* dst
 template <class T, bool CAREFUL, int G>
 __device__ __forceinline__ void dkdv_pass(const WindowArgs& a, const KeyPlace& p, int group, int wave, int lane, char* s_k,
                                           char* qA, char* qB, char* gA, char* gB, float (*rA)[64], float (*rB)[64],
-                                          floatx16 (&dk)[T::NDB], floatx16 (&dv)[T::NDB]) {
+                                          int* s_bad, floatx16 (&dk)[T::NDB], floatx16 (&dv)[T::NDB]) {
   constexpr int NB = T::NB, NDB = T::NDB;
   // The wave's keys as operands in the LDS where registers are short.
   constexpr bool KLDS = T::ORDERED;
@@ -405,6 +421,7 @@ __device__ __forceinline__ void dkdv_pass(const WindowArgs& a, const KeyPlace& p
     if ((at += G) >= per_head) at = group;
     const bool none = i0 + T::ROWS - 1 < w0 || (G > 1 && i0 >= p.q1) || (w1 <= i0 - a.window && w0 >= a.sinks) || w0 >= p.len;
     if (!none) {
+      if (!CAREFUL && __builtin_amdgcn_ballot_w64(fabsf(rc[0][lane]) > kFar)) *s_bad = 1;   // some row of the tile
       const bool whole = i0 >= max(w0 + 31, p.q0) && i0 + T::ROWS <= p.q1 &&
                          (w0 + 32 <= a.sinks || w0 > i0 + T::ROWS - 1 - a.window);
 #pragma unroll
@@ -418,7 +435,7 @@ __device__ __forceinline__ void dkdv_pass(const WindowArgs& a, const KeyPlace& p
 #pragma unroll
           for (int x = 0; x < 4; ++x) ds[e + x] = d[x];
         }
-        rows_products<T>(pr, qc + nb * T::HALF, k, ds, gc + nb * T::HALF, v, place);
+        rows_products<T, true>(pr, qc + nb * T::HALF, k, ds, gc + nb * T::HALF, v, place);
         order_rows<T, 8, 3>();
         if constexpr (T::ORDERED) __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
@@ -426,7 +443,7 @@ __device__ __forceinline__ void dkdv_pass(const WindowArgs& a, const KeyPlace& p
           const floatx4 l = *reinterpret_cast<const floatx4*>(&rc[0][32 * nb + 2 * e + 4 * hw]);
 #pragma unroll
           for (int x = 0; x < 4; ++x) {
-            pr[e + x] = __builtin_amdgcn_exp2f(__builtin_fmaf(pr[e + x], a.scale_log2, -l[x]));
+            pr[e + x] = probability<CAREFUL>(pr[e + x], a.scale_log2, l[x]);
             ds[e + x] *= pr[e + x];
           }
         }
@@ -501,12 +518,12 @@ __global__ __launch_bounds__(256 * G, T::SPLIT && T::D == 128 ? 1 : 2) void k_wi
   char* keys = s_k + (T::ORDERED ? group * 4 * T::NKS * 1024 : 0);
   if (p.q0 < p.q1) {
     dkdv_pass<T, false, G>(a, p, group, wave, lane, keys, qA[group], qB[group], gA[group], gB[group], rA[group], rB[group],
-                           dk, dv);
+                           &s_bad, dk, dv);
     if (__builtin_amdgcn_ballot_w64(in && (not_finite<NDB>(dk) || not_finite<NDB>(dv))) && lane == 0) s_bad = 1;
     __syncthreads();
     if (s_bad)
       dkdv_pass<TC, true, G>(a, p, group, wave, lane, keys, qA[group], qB[group], gA[group], gB[group], rA[group], rB[group],
-                             dk, dv);
+                             &s_bad, dk, dv);
   } else {
 #pragma unroll
     for (int db = 0; db < NDB; ++db) dk[db] = dv[db] = floatx16{};

@@ -316,32 +316,38 @@ __device__ __forceinline__ void multiply(floatx16& acc, floatx4 x, floatx4 y) {
   }
 }
 
-// acc += operand ks of the half's rows times that of b: small pairs of terms first.
-template <class T, class Row>
+// acc += operand ks of the half's rows times that of b: small pairs of terms first,
+// and of these the half's largest term first, or b's (B_FIRST): with it the two
+// change places and the sum stays the same to the bit.
+template <class T, bool B_FIRST, class Row>
 __device__ __forceinline__ void row_step(floatx16& acc, const char* half, const Row& b, const WLane<T>& l, int ks) {
   floatx4 x[T::PL];
 #pragma unroll
-  for (int t = 0; t < T::PL; ++t) x[t] = row_operand<T>(half + t * T::HALF, l, ks);
+  for (int i = 0; i < T::PL; ++i) {
+    const int t = B_FIRST ? T::PL - 1 - i : i;
+    x[t] = row_operand<T>(half + t * T::HALF, l, ks);
+  }
 #pragma unroll
   for (int sum = T::PL - 1; sum >= 0; --sum)
 #pragma unroll
-    for (int t = 0; t <= sum; ++t) multiply<T>(acc, x[t], operand<T>(b, ks, sum - t));
+    for (int t = 0; t <= sum; ++t)
+      multiply<T>(acc, x[B_FIRST ? sum - t : t], operand<T>(b, ks, B_FIRST ? t : sum - t));
 }
 
 template <class T>
 __device__ __forceinline__ void rows_product(floatx16& acc, const char* half, const WRow<T>& b, const WLane<T>& l) {
 #pragma unroll
-  for (int ks = 0; ks < T::NKS; ++ks) row_step<T>(acc, half, b, l, ks);
+  for (int ks = 0; ks < T::NKS; ++ks) row_step<T, false>(acc, half, b, l, ks);
 }
 
 // Two of them in turn.
-template <class T, class Row1, class Row2>
+template <class T, bool B_FIRST, class Row1, class Row2>
 __device__ __forceinline__ void rows_products(floatx16& acc1, const char* half1, const Row1& b1, floatx16& acc2,
                                               const char* half2, const Row2& b2, const WLane<T>& l) {
 #pragma unroll
   for (int ks = 0; ks < T::NKS; ++ks) {
-    row_step<T>(acc1, half1, b1, l, ks);
-    row_step<T>(acc2, half2, b2, l, ks);
+    row_step<T, B_FIRST>(acc1, half1, b1, l, ks);
+    row_step<T, B_FIRST>(acc2, half2, b2, l, ks);
   }
 }
 
