@@ -190,7 +190,8 @@ typedef struct ssba_cache_prefix {
  * group are attended as they are.  A prefix counts as far as it lies before the
  * new tokens of every sequence of its group; the rest is read by sequence.
  * Precision as without lists, where G * max_new also stands for the columns of a
- * group, G times its new tokens.  `scratch` is always needed. */
+ * group, G times its new tokens (or of an average one).  `scratch` is always
+ * needed; it goes by the rows of the call, however large max_seqs is. */
 ssba_status ssba_cache_attend_shared_workspace_size(const ssba_cache* c, const ssba_cache_batch* b,
                                                     const ssba_cache_query* q, const ssba_cache_prefix* x,
                                                     size_t* scratch_bytes);

@@ -249,22 +249,34 @@ int64_t shared_cols(const ssba_cache* c, const ssba_cache_batch* b, const ssba_c
   return (int64_t)(q->heads / c->kv_heads) * std::min<int64_t>((int64_t)b->max_new * x->max_seqs, b->rows);
 }
 
+// Column tiles of the prefixes.  All groups together have no more columns than the rows, so where the tiles of groups
+// that are all as large as any may be take more than twice the columns that this leaves, they are packed: group g begins
+// with tile floor(its first column / columns of a tile) + g.  Else each has as many as the largest, and no workgroup
+// searches for its group.  In us, max_seqs exact and so not packed, and max_seqs that of the batch, packed and not (16
+// heads on 4, D 128, 1024 shared tokens and 100 more): 16 groups of 4 sequences, a token each 17.0, 18.6 and 26.4; 64 of 4
+// 28.6, 41.7 and 161; 64 of 4, 16 tokens each 113, 117 and 322.
 AttendPlan plan_shared(const ssba_cache* c, const ssba_cache_batch* b, const ssba_cache_query* q,
                        const ssba_cache_prefix* x) {
   const int64_t most = long_of(c, b), prefix = std::max<int64_t>(1, std::min<int64_t>(x->max_len, most));
   const int64_t columns = std::max<int64_t>(1, shared_cols(c, b, q, x));
+  const int64_t all = (int64_t)(q->heads / c->kv_heads) * b->rows;
+  const int64_t average = std::max<int64_t>(1, std::min(columns, ceil_div(all, x->groups)));
   AttendPlan f = plan(c, b, q, false, x->groups, columns, prefix);
-  const int64_t narrow = (int64_t)x->groups * c->kv_heads * ceil_div(columns, 32);
+  const int wide = plan(c, b, q, false, x->groups, average, prefix).tiles * 16;
+  auto slots = [&](int64_t cols) { return all / cols + x->groups; };
+  const bool packed = (double)x->groups * f.col_tiles * f.tiles * 16 > 2.0 * slots(wide) * wide;
+  if (packed) f = plan(c, b, q, false, x->groups, average, prefix);
+  const int64_t narrow = (int64_t)x->groups * c->kv_heads * ceil_div(packed ? average : columns, 32);
   if (f.tiles > 2 && (double)narrow * prefix <= 512 * 1024) {
     // Columns for more than 32 a workgroup, but not the keys to fill the chip with such: 32 columns, about 256
     // workgroups (256 columns of 4 heads over 8192 keys, D 128: 15 us, 256 columns a workgroup 28 to 32, 128 20 to 22,
     // 64 18 to 21; 512 workgroups of 32 columns 16).
     f.tiles = 2;
     f.threads = 256;
-    f.col_tiles = (int)ceil_div(columns, 32);
     f.items = narrow;
     f.splits = (int)std::max<int64_t>(1, std::min<int64_t>(256 / narrow, prefix / 256));
   }
+  if (packed) f.items = slots(16 * f.tiles) * c->kv_heads;
   const int64_t cols = std::max<int64_t>(1, (int64_t)(q->heads / c->kv_heads) * b->max_new);
   const int64_t rest = std::max<int64_t>(1, most - prefix);
   AttendPlan p = plan(c, b, q, false, b->seqs, cols, rest);
@@ -275,7 +287,8 @@ AttendPlan plan_shared(const ssba_cache* c, const ssba_cache_batch* b, const ssb
   p.kind = ssba::kAttendShared;
   p.prefix_tiles = f.tiles;
   p.prefix_threads = f.threads;
-  p.prefix_col_tiles = f.col_tiles;
+  p.prefix_col_tiles = (int)ceil_div(columns, 16 * f.tiles);
+  p.prefix_slots = packed ? (int)std::min<int64_t>(slots(16 * f.tiles), 1 << 30) : 0;
   p.prefix_splits = f.splits;
   p.prefix_items = f.items;
   return p;
@@ -527,6 +540,7 @@ ssba_status ssba_cache_attend_shared(const ssba_cache* c, int32_t layer, const s
   a.prefix_cols = p.prefix_tiles * 16;
   a.prefix_col_tiles = p.prefix_col_tiles;
   a.prefix_splits = p.prefix_splits;
+  a.prefix_slots = p.prefix_slots;
   a.part = static_cast<float*>(scratch);
   a.prefix_part = a.part + rest_columns(p) * c->head_dim;
   a.part_ml = a.prefix_part + prefix_columns(p) * c->head_dim;

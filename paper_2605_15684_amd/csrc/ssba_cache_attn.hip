@@ -225,15 +225,59 @@ __device__ __forceinline__ int group_of_seq(const AttendArgs& a, int s, int lane
   return n > a.groups ? -1 : n - 1;
 }
 
+// Columns of an item of the prefixes are 16 to 256, a power of two.
+__device__ __forceinline__ int prefix_log2(const AttendArgs& a) { return 31 - __builtin_clz(a.prefix_cols); }
+
+// Packed column tiles of the prefixes: group g's begin with this one, and reach
+// no other group's where the first rows do not decrease.
+__device__ __forceinline__ int first_row(const AttendArgs& a, int g) {
+  return min(max(a.b.cu[min(max(a.first[g], 0), a.b.seqs)], 0), a.b.rows);
+}
+__device__ __forceinline__ int first_tile(const AttendArgs& a, int row, int g) {
+  return (int)((int64_t)row * a.group >> prefix_log2(a)) + g;
+}
+
+// The group of packed tile x, -1: none, or first rows that decrease somewhere.
+// One wave, every lane gets the result.
+__device__ __forceinline__ int group_of_tile(const AttendArgs& a, int x, int lane) {
+  int n = 0, before = 0;
+  for (int g0 = 0; g0 < a.groups; g0 += 64) {
+    const int g = g0 + lane;
+    const int row = g < a.groups ? first_row(a, g) : a.b.rows;
+    const int left = __shfl_up(row, 1);
+    if (__builtin_amdgcn_ballot_w64(row < (lane ? left : before))) return -1;
+    n += __popcll(__builtin_amdgcn_ballot_w64(g < a.groups && first_tile(a, row, g) <= x));
+    before = __builtin_amdgcn_readlane(row, 63);
+  }
+  return n - 1;
+}
+
 // How many pages of sequence s are read with its group's, and its group and
 // that group's view if any.
 __device__ __forceinline__ int pages_shared(const AttendArgs& a, int s, const SeqView& sv, int lane, int* g, GroupView* v) {
   *g = group_of_seq(a, s, lane);
   if (*g < 0) return 0;
   *v = group_view(a, *g, lane);
+  if (a.prefix_slots && v->pages && group_of_tile(a, first_tile(a, v->begin, *g), lane) != *g) return 0;
   // Arrays that decrease somewhere: not a sequence or not rows of that group.
   if (s < v->first || sv.begin < v->begin || sv.begin + sv.n > v->begin + v->rows) return 0;
   return v->pages;
+}
+
+// Where the parts of a group's prefix lie: item and column of its column `col`.
+// Its column tiles are consecutive items, or packed, of all heads in turn.
+struct PrefixPart {
+  int64_t item;
+  int col, step;
+};
+__device__ __forceinline__ PrefixPart prefix_part(const AttendArgs& a, int g, const GroupView& v, int h, int col) {
+  if (a.prefix_slots) return {(int64_t)first_tile(a, v.begin, g) * a.c.kv_heads + h, col, a.c.kv_heads};
+  return {((int64_t)g * a.c.kv_heads + h) * a.prefix_col_tiles, col, 1};
+}
+// Slot of its column col + c of part 0; a part has prefix_cols of them.
+__device__ __forceinline__ int64_t part_slot(const AttendArgs& a, const PrefixPart& x, int c) {
+  const int col = x.col + c, log2 = prefix_log2(a);
+  return ((x.item + (int64_t)(col >> log2) * x.step) * a.prefix_splits << log2) + (col & (a.prefix_cols - 1));
 }
 
 // Which item a workgroup (or a part to be joined) belongs to.
@@ -304,11 +348,16 @@ __global__ __launch_bounds__(P::THREADS, P::R > 1 || (P::D == 128 && (P::J > 1 |
   const int unit = id / a.c.kv_heads;
   // LISTED with several column groups: they are rows.
   int prefix = 0;   // tokens of the shared pages
-  int64_t prefix_item = 0;   // kSpanRest: first item of the prefixes of this group and head, and the column there of
-  int prefix_col = 0;        // this sequence's first
+  PrefixPart pre = {0, 0, 1};   // kSpanRest: of this sequence's first column
   bool there = true;
   if (P::SPAN == kSpanPrefix) {
-    const GroupView v = group_view(a, unit, lane);
+    int gr = unit;
+    if (a.prefix_slots) {   // unit is a tile
+      gr = group_of_tile(a, unit, lane);
+      if (gr < 0) return;
+      ct = unit - first_tile(a, first_row(a, gr), gr);
+    }
+    const GroupView v = group_view(a, gr, lane);
     if (v.pages == 0) return;
     prefix = v.pages << page_log2;
     it.seq = v.first;
@@ -323,10 +372,7 @@ __global__ __launch_bounds__(P::THREADS, P::R > 1 || (P::D == 128 && (P::J > 1 |
     int gr;
     GroupView v;
     prefix = pages_shared(a, it.seq, it.sv, lane, &gr, &v) << page_log2;
-    if (prefix) {
-      prefix_item = ((int64_t)gr * a.c.kv_heads + it.h) * a.prefix_col_tiles;
-      prefix_col = (it.sv.begin - v.begin) * a.group;
-    }
+    if (prefix) pre = prefix_part(a, gr, v, it.h, (it.sv.begin - v.begin) * a.group);
   }
   const int cbase = (P::LISTED ? ct : ct * P::CG + cg) * P::COLS;
   if ((P::CG == 1 || P::KP == 1) && cbase >= it.ncols) return;
@@ -906,8 +952,7 @@ __global__ __launch_bounds__(P::THREADS, P::R > 1 || (P::D == 128 && (P::J > 1 |
     } else {
       if (P::SPAN == kSpanRest && prefix) {
         // The parts of the prefix, of which there are few: their maxima first.
-        const int col = prefix_col + cc;
-        const int64_t slot = (prefix_item + col / a.prefix_cols) * a.prefix_splits * a.prefix_cols + col % a.prefix_cols;
+        const int64_t slot = part_slot(a, pre, cc);
         const float* ml = a.prefix_ml + slot * 2;
         const float* part = a.prefix_part + slot * D + ch;
         float top = cm;
@@ -1031,37 +1076,41 @@ __global__ __launch_bounds__(256) void k_cache_join_shared(AttendArgs r, AttendA
   item_of<false>(r, id / r.c.kv_heads, lane, &it);
   const int c0 = (ct * r.tiles + tile) * 16;
   if (c0 >= it.ncols) return;
-  int shared = 0;        // parts of the prefix
-  int64_t pitem = 0;     // item and column of the prefix of column 0 of this tile
-  int pcol = 0;
+  int shared = 0;                // parts of the prefix
+  PrefixPart pre = {0, 0, 1};    // of column 0 of this tile
   int g;
   GroupView v;
   if (pages_shared(r, it.seq, it.sv, lane, &g, &v)) {
-    shared = p.splits;
-    pcol = (it.sv.begin - v.begin) * r.group + c0;
-    pitem = ((int64_t)g * r.c.kv_heads + it.h) * p.col_tiles;
+    shared = r.prefix_splits;
+    pre = prefix_part(r, g, v, it.h, (it.sv.begin - v.begin) * r.group + c0);
   }
   const int parts = shared + r.splits;
-  const int pw = p.tiles * 16, rw = r.tiles * 16;   // columns of an item
-  // Column c of part s: its place among the parts of its launch.
-  auto slot = [&](int s, int c) {
-    const int col = pcol + c;
-    return s < shared ? ((pitem + col / pw) * p.splits + s) * pw + col % pw
-                      : ((int64_t)item * r.splits + s - shared) * rw + tile * 16 + c;
+  const int rw = r.tiles * 16;   // columns of an item
+  // This thread's column c of part s: its place among the parts of its launch.
+  struct Slots {
+    int64_t of_prefix, of_rest;   // of part 0 (of the rest: were it part 0)
+    int prefix_step, rest_step, shared;
+    __device__ __forceinline__ int64_t at(int s) const {
+      return s < shared ? of_prefix + (int64_t)s * prefix_step : of_rest + (int64_t)s * rest_step;
+    }
+  };
+  auto slots = [&](int c) {
+    return Slots{part_slot(r, pre, c), ((int64_t)item * r.splits - shared) * rw + tile * 16 + c, r.prefix_cols, rw, shared};
   };
   {
     // 16 threads a column: maximum, weights and sum over the parts.
     const int c = threadIdx.x >> 4, j = threadIdx.x & 15;
     const bool in = c0 + c < it.ncols;
+    const Slots slot = slots(c);
     float m = -INFINITY;
     if (in)
-      for (int s = j; s < parts; s += 16) m = fmaxf(m, (s < shared ? p : r).part_ml[slot(s, c) * 2]);
+      for (int s = j; s < parts; s += 16) m = fmaxf(m, (s < shared ? p : r).part_ml[slot.at(s) * 2]);
 #pragma unroll
     for (int x = 1; x < 16; x <<= 1) m = fmaxf(m, __shfl_xor(m, x));
     float sum = 0.f;
     if (in)
       for (int s = j; s < parts; s += 16) {
-        const float* ml = (s < shared ? p : r).part_ml + slot(s, c) * 2;
+        const float* ml = (s < shared ? p : r).part_ml + slot.at(s) * 2;
         const float ms = ml[0];
         s_w[s][c] = ms == m ? 1.f : exp2_(ms - m);
         sum += ms == m ? ml[1] : shrink(ml[1], ms - m);
@@ -1074,10 +1123,11 @@ __global__ __launch_bounds__(256) void k_cache_join_shared(AttendArgs r, AttendA
   const int half = threadIdx.x >> 7, t = threadIdx.x & 127, c = t >> 3, ch = ch32 * 32 + (t & 7) * 4;
   floatx4 acc = {0.f, 0.f, 0.f, 0.f};
   const bool in = c0 + c < it.ncols;
+  const Slots slot = slots(c);
   if (in)
 #pragma unroll 4
     for (int s = half; s < parts; s += 2)
-      acc += *reinterpret_cast<const floatx4*>((s < shared ? p : r).part + slot(s, c) * D + ch) * s_w[s][c];
+      acc += *reinterpret_cast<const floatx4*>((s < shared ? p : r).part + slot.at(s) * D + ch) * s_w[s][c];
   if (half) s_acc[t] = acc;
   __syncthreads();
   if (half || !in) return;
@@ -1139,7 +1189,7 @@ hipError_t launch_d(const AttendArgs& a, const AttendPlan& p, int dtype, hipStre
       pre.part = a.prefix_part;
       pre.part_ml = a.prefix_ml;
       pre.tiles = pp.tiles = p.prefix_tiles;
-      pre.col_tiles = pp.col_tiles = p.prefix_col_tiles;
+      pre.col_tiles = pp.col_tiles = p.prefix_slots ? 1 : p.prefix_col_tiles;
       pre.splits = pp.splits = p.prefix_splits;
       pp.threads = p.prefix_threads;
       pp.items = p.prefix_items;

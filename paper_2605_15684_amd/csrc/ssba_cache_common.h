@@ -122,7 +122,8 @@ struct AttendArgs {
   int tiles;              // tiles of 16 columns of an item
   float* prefix_part;     // part and part_ml of the prefixes
   float* prefix_ml;
-  int prefix_cols, prefix_col_tiles, prefix_splits;   // of the prefixes: columns of an item, column tiles, splits
+  int prefix_cols, prefix_col_tiles, prefix_splits;   // of the prefixes: columns of an item, most column tiles, splits
+  int prefix_slots;       // column tiles of all groups where they are packed, 0: prefix_col_tiles for each
 };
 
 // What the attention launch does (ssba_cache_api.cpp decides).
@@ -131,7 +132,8 @@ enum AttendKind {
   kAttendRow,    // lists; items: (row, kv head, column tile), the waves of a workgroup share the keys
   kAttendRows,   // lists; a wave per such item
   kAttendWindow, // as kAttendSeq, keys of the sinks and the window
-  kAttendShared, // as kAttendSeq for what is behind the prefixes; items of these: (group, kv head, column tile)
+  kAttendShared, // as kAttendSeq for what is behind the prefixes; items of these: (group, kv head, column tile), or
+                 // (slot, kv head) where the groups' column tiles are packed
 };
 struct AttendPlan {
   AttendKind kind;
@@ -139,7 +141,7 @@ struct AttendPlan {
   int threads;
   int col_tiles, splits;
   int64_t items;          // workgroups without the splits
-  int prefix_tiles, prefix_threads, prefix_col_tiles, prefix_splits;   // kAttendShared: the same of the prefixes
+  int prefix_tiles, prefix_threads, prefix_col_tiles, prefix_splits, prefix_slots;   // kAttendShared: the same of the prefixes
   int64_t prefix_items;
 };
 
