@@ -179,7 +179,7 @@ ssba_status ssba_cache_attend_window(const ssba_cache* c, int32_t layer, const s
 typedef struct ssba_cache_prefix {
   int32_t groups;            /* 1 .. 65535                                       */
   int32_t max_seqs;          /* at least the sequences of any group, 1 .. 65535; a group of more is attended by sequence */
-  int32_t max_len;           /* about the longest prefix in tokens (only how work is split goes by it) */
+  int32_t max_len;           /* about the longest prefix in tokens (only how work is split goes by it); 0: unknown */
   const int32_t* first;      /* [groups + 1]                                     */
   const int32_t* pages;      /* [groups]                                         */
 } ssba_cache_prefix;

@@ -137,7 +137,7 @@ class Prefix:
     """Groups of consecutive sequences that share their first pages: sequences first[g] .. first[g+1]-1 share pages[g]
     complete pages (first int32 [groups + 1], pages int32 [groups]), named by the table for the first of them.
     max_seqs: at least the sequences of any group (None: those of the batch); max_len: about the longest prefix in
-    tokens (work is split by it, results differ by the rounding of partial sums)."""
+    tokens (None or 0: unknown; work is split by it, results differ by the rounding of partial sums)."""
 
     __slots__ = ("first", "pages", "index", "max_seqs", "_desc")
 
@@ -149,17 +149,17 @@ class Prefix:
         if groups < 1:
             raise ValueError("first: expected [groups + 1]")
         _check(pages, (groups,), torch.int32, index, "pages")
-        max_len = None if max_len is None else int(max_len)
+        max_len = int(max_len or 0)
         max_seqs = None if max_seqs is None else int(max_seqs)
-        _int32("first, max_seqs or max_len", groups, max_seqs or 0, max_len or 0)
-        if max_seqs is not None and max_seqs < 1 or max_len is not None and max_len < 0:
+        _int32("first, max_seqs or max_len", groups, max_seqs or 0, max_len)
+        if max_seqs is not None and max_seqs < 1 or max_len < 0:
             raise ValueError("max_seqs must be 1 or more, max_len 0 or more")
         self.first, self.pages, self.index, self.max_seqs = first, pages, index, max_seqs
         self._desc = (groups, max_len, first.data_ptr(), pages.data_ptr())
 
-    def desc(self, seqs: int, tokens: int) -> _lib.CachePrefix:
+    def desc(self, seqs: int) -> _lib.CachePrefix:
         groups, max_len, first, pages = self._desc
-        return _lib.CachePrefix(groups, self.max_seqs or seqs, tokens if max_len is None else max_len, first, pages)
+        return _lib.CachePrefix(groups, self.max_seqs or seqs, max_len, first, pages)
 
 
 def alloc(layers: int, pages: int, kv_heads: int, head_dim: int, page: int = 64, device="cuda") -> PagedCache:
@@ -343,7 +343,7 @@ def attend_shared(pool: PagedCache, layer: int, batch: Batch, prefix: Prefix, q:
     out, b, desc = _query(pool, layer, batch, q, causal, scale, out)
     if not isinstance(prefix, Prefix) or prefix.index != pool.index:
         raise ValueError("prefix: expected a cache.Prefix on the cache's device")
-    x = prefix.desc(*batch.table.shape[:1], batch.table.shape[1] * pool.page)
+    x = prefix.desc(batch.table.shape[0])
     size = ctypes.c_size_t(0)
     _lib.check(_L.ssba_cache_attend_shared_workspace_size(pool.desc, b, desc, x, size),
                "ssba_cache_attend_shared_workspace_size")

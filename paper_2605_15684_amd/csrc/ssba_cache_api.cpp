@@ -225,17 +225,22 @@ AttendPlan plan(const ssba_cache* c, const ssba_cache_batch* b, const ssba_cache
               listed ? std::min<int64_t>((int64_t)q->keep * c->page, long_of(c, b)) : long_of(c, b));
 }
 
+// Items from which on 8 waves of one workgroup fill the chip as well as parts do: 256, or 128 of the larger rows of bf16
+// at D 128 (256 items, 4096 keys: bf16 D 64 24.4 to 27.0 us, fp32 25.4 to 27.5 and D 128 46.0 to 48.7; 8128 keys 46.0 to
+// 45.5, 41.4 to 46.4, 99.6 to 108.5; bf16 D 128, 128 items 25.2 to 27.9, 8128 keys 44.6 to 48.3; but bf16 D 64 30.6 to
+// 26.5, fp32 36.9 to 27.3 of 128 items, 64 items 37 to 28).
+int64_t items_of_eight_waves(const ssba_cache* c, const ssba_cache_query* q) {
+  return q->dtype == SSBA_DT_BF16 && c->head_dim == 128 ? 128 : 256;
+}
+
 // A window's keys: of the first token to the last one's, and the sinks.  Windows are as long as each other, whatever
-// the sequences, so from 256 workgroups on 8 waves of one also replace parts where whole sequences would be split for
-// their lengths, from 128 on of the larger rows of bf16 at D 128 (256 items, 4096 keys: bf16 D 64 24.4 to 27.0 us, fp32
-// 25.4 to 27.5 and D 128 46.0 to 48.7; 8128 keys 46.0 to 45.5, 41.4 to 46.4, 99.6 to 108.5; bf16 D 128, 128 items 25.2
-// to 27.9, 8128 keys 44.6 to 48.3; but bf16 D 64 30.6 to 26.5, fp32 36.9 to 27.3 of 128 items, 64 items 37 to 28).
+// the sequences, so 8 waves also replace parts where whole sequences would be split for their lengths.
 AttendPlan plan_window(const ssba_cache* c, const ssba_cache_batch* b, const ssba_cache_query* q, int32_t window,
                        int32_t sinks) {
   const int64_t cols = std::max<int64_t>(1, (int64_t)(q->heads / c->kv_heads) * b->max_new);
   AttendPlan p = plan(c, b, q, false, b->seqs, cols,
                       std::min<int64_t>((int64_t)window + sinks + b->max_new, std::max<int64_t>(1, long_of(c, b))));
-  if (p.tiles == 1 && p.splits > 1 && p.items >= (q->dtype == SSBA_DT_BF16 && c->head_dim == 128 ? 128 : 256) &&
+  if (p.tiles == 1 && p.splits > 1 && p.items >= items_of_eight_waves(c, q) &&
       (int64_t)window + sinks + b->max_new <= 8192) {
     p.splits = 1;
     p.threads = 512;
@@ -257,7 +262,8 @@ int64_t shared_cols(const ssba_cache* c, const ssba_cache_batch* b, const ssba_c
 // 28.6, 41.7 and 161; 64 of 4, 16 tokens each 113, 117 and 322.
 AttendPlan plan_shared(const ssba_cache* c, const ssba_cache_batch* b, const ssba_cache_query* q,
                        const ssba_cache_prefix* x) {
-  const int64_t most = long_of(c, b), prefix = std::max<int64_t>(1, std::min<int64_t>(x->max_len, most));
+  const int64_t most = long_of(c, b);
+  const int64_t prefix = std::max<int64_t>(1, x->max_len ? std::min<int64_t>(x->max_len, most) : most);
   const int64_t columns = std::max<int64_t>(1, shared_cols(c, b, q, x));
   const int64_t all = (int64_t)(q->heads / c->kv_heads) * b->rows;
   const int64_t average = std::max<int64_t>(1, std::min(columns, ceil_div(all, x->groups)));
@@ -270,7 +276,9 @@ AttendPlan plan_shared(const ssba_cache* c, const ssba_cache_batch* b, const ssb
   if (f.tiles > 2 && (double)narrow * prefix <= 512 * 1024) {
     // Columns for more than 32 a workgroup, but not the keys to fill the chip with such: 32 columns, about 256
     // workgroups (256 columns of 4 heads over 8192 keys, D 128: 15 us, 256 columns a workgroup 28 to 32, 128 20 to 22,
-    // 64 18 to 21; 512 workgroups of 32 columns 16).
+    // 64 18 to 21; 512 workgroups of 32 columns 16).  Whole calls, 64 to 4096 columns of 1 and 4 heads over 1024 to 32768
+    // keys, wider and 32: at 512 x 1024 in all D 64 30 to 38 us and 23 to 26, D 128 39 to 55 and 28 to 36; at twice as
+    // many 39 to 42 and 31 to 34, 54 to 59 and 39 to 47; at eight times 58 to 61 and 87 to 90, 94 to 98 and 111 to 118.
     f.tiles = 2;
     f.threads = 256;
     f.items = narrow;
@@ -278,11 +286,20 @@ AttendPlan plan_shared(const ssba_cache* c, const ssba_cache_batch* b, const ssb
   }
   if (packed) f.items = slots(16 * f.tiles) * c->kv_heads;
   const int64_t cols = std::max<int64_t>(1, (int64_t)(q->heads / c->kv_heads) * b->max_new);
-  const int64_t rest = std::max<int64_t>(1, most - prefix);
+  // Of an unknown prefix either part may be all of a sequence (max_len exact, 0, and as long as the sequence; a token
+  // each, 16 heads on 4, D 128: 8 sequences of 8192 + 4000 tokens 36, 36 and 47 us, 4 of 2048 + 16000 37, 33 and
+  // 104, 64 that share 8192 and have 300 more 23 each; but 4 such 17, 24 and 17, the launch that joins the parts).
+  const int64_t rest = std::max<int64_t>(1, x->max_len ? most - prefix : most);
   AttendPlan p = plan(c, b, q, false, b->seqs, cols, rest);
-  if (p.tiles == 1 && rest <= 2048) {   // one workgroup each, that also adds the prefix's parts
+  // Short rests: one workgroup each, that also adds the prefix's parts (2 sequences, 4 heads, behind 4096 tokens, whole
+  // and in parts: 1900 keys bf16 D 64 17.9 and 19.7 us, D 128 20.9 and 21.2, fp32 20.6 and 21.1, 25.4 and 23.2; 3000 keys
+  // 20.8 and 19.1, 25.0 and 20.6, 24.6 and 20.5, 30.7 and 22.7).
+  if (p.tiles == 1 && rest <= 2048) {
     p.splits = 1;
     if (rest > 256) p.threads = 512;
+  } else if (!x->max_len && p.tiles == 1 && p.splits > 1 && p.items >= items_of_eight_waves(c, q)) {
+    p.splits = 1;
+    p.threads = 512;
   }
   p.kind = ssba::kAttendShared;
   p.prefix_tiles = f.tiles;

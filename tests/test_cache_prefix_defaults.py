@@ -42,7 +42,7 @@ def size(groups, each, new, held, prefix_pages, heads=32, kv=8, d=128, page=64, 
     b = _lib.CacheBatch(seqs, pages, seqs * new if rows is None else rows, new, 0, P, P, P)
     q = _lib.CacheQuery(heads, dtype, 1, 0, 0, 0, 0.0, 0, 0, 0, 0)
     out = ctypes.c_size_t(0)
-    st = L.ssba_cache_attend_shared_workspace_size(c, b, q, x.desc(seqs, pages * page), out)
+    st = L.ssba_cache_attend_shared_workspace_size(c, b, q, x.desc(seqs), out)
     return st, out.value
 
 
@@ -72,3 +72,16 @@ def test_one_large_group_among_small_ones():
     """max_seqs is that of the large group: the small ones do not each take as much room (13 tiles of 256 columns)."""
     st, need = size(200, 1, 8, 8192, 16, seqs=300, max_seqs=101, max_len=1024)
     assert st == OK and need < 200 * 13 * 256 * 8 * (128 + 2) * 4 // 4
+
+
+@pytest.mark.parametrize("seqs,held,heads,kv", [(8, 12288, 16, 4), (4, 18432, 16, 4), (2, 100000, 8, 1), (1, 5000, 4, 4)])
+def test_rests_are_planned_without_a_hint(seqs, held, heads, kv):
+    """A prefix of unknown length is not taken to be all that a sequence holds: what is behind it is in parts, which a
+    hint of the whole length leaves out (the prefixes' own parts are the same)."""
+    for groups in (1, seqs):
+        for dtype in (0, 1):
+            kw = dict(each=seqs // groups, new=1, held=held, prefix_pages=0, heads=heads, kv=kv, dtype=dtype)
+            whole = -(-held // 64) * 64
+            unknown, zero, all_of_it = (size(groups, **kw, **hint) for hint in ({}, dict(max_len=0), dict(max_len=whole)))
+            assert unknown == zero and unknown[0] == all_of_it[0] == OK
+            assert unknown[1] > all_of_it[1]
