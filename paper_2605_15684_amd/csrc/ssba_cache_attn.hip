@@ -50,7 +50,10 @@
 //                 48 us, J 4 49: registers).
 //   window        as few columns, of the window's and the sinks' pages: 64
 //                 sequences, 4096 + 64 keys, 4 kv heads, D 128: 36 us, 6.1 TB/s.
-//                 One sequence, window 1024: 9.4 us, 8 steps of a wave in turn.
+//                 One sequence, window 1024: 9.4 us, of which 4.5 are the launch,
+//                 the chain to the first codes (lengths, page table, scales) and
+//                 the join of the waves, the rest 5 steps of a wave in turn (window
+//                 16: 4.5, 512: 6.7, 2040, 9 steps: 12.8).
 //   prefix, rest  a group's sequences are the columns of its prefix, so its pages
 //                 are read and decoded once for 32 columns instead of once a
 //                 sequence; parts of the prefix are added in the epilogue of the
@@ -61,6 +64,9 @@
 //                 prefix is bound by decoding: a workgroup has 32 of 256 columns
 //                 and about 256 keys a wave (more columns a workgroup leave fewer
 //                 of them); the rest by a chain of loads, a few steps, and parts.
+//                 With many new tokens both are bound by products, as without
+//                 sharing, and the joining costs: 16 sequences of 256 tokens behind
+//                 4096 168 us (840 TFLOP/s), read by sequence 140.
 #include <hip/hip_runtime.h>
 #include <hip/hip_bf16.h>
 

@@ -66,7 +66,7 @@ __device__ __forceinline__ void order_rows() {
 // more than exp2 holds from about 2^28 on, which made infinities of finite inputs.
 // Where rows are past kFar the careful passes compute, which bound it by 1.  In us,
 // dq and dkdv of 2 x 8192 rows, 16 heads on 4, window 2048, bf16, without a bound,
-// as it is, and bounded everywhere: D 128 847, 853, 860; D 64 478, 481, 496.  NaN
+// as it is, and bounded everywhere: D 128 857, 862, 869; D 64 485, 487, 502.  NaN
 // stays NaN (IEEE minimum).
 constexpr float kFar = 1048576.f;
 template <bool CAREFUL>

@@ -9,6 +9,7 @@ import pytest
 
 from test_cache_host_sanitize import CSRC, FLAGS, HIPCC, SAN
 
+
 @pytest.mark.skipif(not os.path.exists(HIPCC), reason="hipcc not installed")
 def test_plans_under_asan_ubsan(tmp_path):
     objs = []
