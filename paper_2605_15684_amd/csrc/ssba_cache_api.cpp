@@ -259,7 +259,8 @@ int64_t shared_cols(const ssba_cache* c, const ssba_cache_batch* b, const ssba_c
 // with tile floor(its first column / columns of a tile) + g.  Else each has as many as the largest, and no workgroup
 // searches for its group.  In us, max_seqs exact and so not packed, and max_seqs that of the batch, packed and not (16
 // heads on 4, D 128, 1024 shared tokens and 100 more): 16 groups of 4 sequences, a token each 17.0, 18.6 and 26.4; 64 of 4
-// 28.6, 41.7 and 161; 64 of 4, 16 tokens each 113, 117 and 322.
+// 28.6, 41.7 and 161; 64 of 4, 16 tokens each 113, 117 and 322; 1000 of 3, 8 heads on 2, D 64, 128 tokens and 30 more 51
+// and 98: a workgroup reads the first rows of all groups, so that arrays that decrease are seen by all alike.
 AttendPlan plan_shared(const ssba_cache* c, const ssba_cache_batch* b, const ssba_cache_query* q,
                        const ssba_cache_prefix* x) {
   const int64_t most = long_of(c, b);
