@@ -137,8 +137,8 @@ class Prefix:
     """Groups of consecutive sequences that share their first pages: sequences first[g] .. first[g+1]-1 share pages[g]
     complete pages (first int32 [groups + 1], pages int32 [groups]), named by the table for the first of them.
     max_seqs: at least the sequences of any group (None: those of the batch, which costs time from some tens of groups
-    on); max_len: about the longest prefix in
-    tokens (None or 0: unknown; work is split by it, results differ by the rounding of partial sums)."""
+    on); max_len: about the longest prefix in tokens (None or 0: unknown; work is split by it, results differ by the
+    rounding of partial sums)."""
 
     __slots__ = ("first", "pages", "index", "max_seqs", "_desc")
 
